@@ -32,6 +32,10 @@ EXPORTS = (
     "pg_set_half_step", "pg_params_device", "pg_set_random_projection",
     "pg_round_sgd", "pg_stack_elems", "pg_stack_offset", "pg_comm_floats", "pg_comm_floats_round",
     "pg_round_bytes", "pg_selftest_bounds_check",
+    "pg_add_rms_norm", "pg_add_rms_norm_grad", "pg_add_rms_norm_grad_workspace_bytes",
+    "pg_linear", "pg_linear_workspace_bytes", "pg_linear_input_grad", "pg_linear_input_grad_workspace_bytes",
+    "pg_linear_weight_grad", "pg_linear_weight_grad_workspace_bytes", "pg_activation_grad",
+    "pg_checkpoint_write", "pg_checkpoint_read", "pg_training_status",
 )
 PG_POWER_ITERATION, PG_RANDOM_RIGHT, PG_RANDOM_LEFT = 0, 1, 2
 KERNEL_KINDS = ("forward", "edge_left", "transposed", "edge_right", "update_forward",
@@ -104,6 +108,12 @@ def load_library() -> ctypes.CDLL:
                                  ctypes.POINTER(i64)]
     L.pg_comm_floats_round.argtypes = [vp, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     L.pg_round_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
+    for name in ("pg_add_rms_norm", "pg_activation_grad", "pg_checkpoint_write", "pg_checkpoint_read"):
+        getattr(L, name).argtypes = [vp, vp]                          # (args, stream), see training.py
+    for name in ("pg_add_rms_norm_grad", "pg_linear", "pg_linear_input_grad", "pg_linear_weight_grad"):
+        getattr(L, name).argtypes = [vp, vp, ctypes.c_size_t, vp]     # (args, workspace, bytes, stream)
+        getattr(L, name + "_workspace_bytes").argtypes = [vp, szp]
+    L.pg_training_status.argtypes = [vp]
     L.pg_status_string.argtypes = [ctypes.c_int]
     L.pg_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -338,6 +348,26 @@ class PowerGossip:
         off, ld = self.pg_stack_offset(worker, layer)
         n, m = self.layer_shapes[layer]
         return torch.as_strided(grads, (n, m), (ld, 1), storage_offset=off)
+
+    def gradient_layer(self, grads, layer: int):
+        """(workers x rows x cols) view of one layer of all workers inside a buffer made by gradient_buffer()."""
+        return self._layer_of_all(grads, layer, *self.pg_stack_offset(0, layer))
+
+    def params_layer(self, layer: int, stream=None):
+        """(workers x rows x cols) view of one layer of all workers in the workspace (see pg_params_device)."""
+        import torch
+
+        x = self.pg_params_device(0, layer, stream)
+        return self._layer_of_all(self._workspace.view(torch.float32), layer, x.storage_offset(), x.stride(0))
+
+    def _layer_of_all(self, flat, layer: int, offset: int, ld: int):
+        import torch
+
+        off = [self.pg_stack_offset(i, layer)[0] for i in range(self.n_workers)]
+        step = off[1] - off[0]                   # every worker's block of the stack has the same layout
+        assert all(o == off[0] + i * step for i, o in enumerate(off))
+        n, m = self.layer_shapes[layer]
+        return torch.as_strided(flat, (self.n_workers, n, m), (step, ld, 1), storage_offset=offset)
 
     def pg_round_sgd(self, grads, eta: float, stream=None) -> None:
         """grads: fp32 CUDA tensor of pg_stack_elems floats laid out like the parameter stack."""

@@ -10,6 +10,7 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -17,9 +18,10 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libpowergossip.so")
 LIB_CHECKED = os.path.join(HERE, "libpowergossip_checked.so")     # the same sources with -DPG_BOUNDS_CHECK
 
-NVCC_FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--shared",
+ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
+NVCC_FLAGS = ARCH + [
+    "-lineinfo", "-O3", "-std=c++17",
+    "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
     "-DPG_BUILDING_LIBRARY",
 ]
 
@@ -50,11 +52,20 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = lib + ".%d.tmp" % os.getpid()
     extra = ["-DPG_BOUNDS_CHECK"] if checked else []
-    cmd = [nvcc] + NVCC_FLAGS + extra + ["-I", INCLUDE, "-I", CSRC, "-o", tmp] + sources()
     if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-        print(" ".join(cmd))
-    subprocess.check_call(cmd)
+        extra.append("-Xptxas=-v")
+    with tempfile.TemporaryDirectory() as work:      # one compiler process per source, then one link
+        jobs = []
+        for src in sources():
+            obj = os.path.join(work, os.path.basename(src) + ".o")
+            cmd = [nvcc] + NVCC_FLAGS + extra + ["-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj]
+            if verbose:
+                print(" ".join(cmd))
+            jobs.append((cmd, obj, subprocess.Popen(cmd)))
+        failed = [(cmd, p.returncode) for cmd, _, p in jobs if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(failed[0][1], failed[0][0])
+        subprocess.check_call([nvcc] + ARCH + ["--shared", "-o", tmp] + [obj for _, obj, _ in jobs])
     os.replace(tmp, lib)
     return lib
 
