@@ -1,118 +1,624 @@
-// The batched linear layer and its gradients.
+// The batched linear layer and its gradients on the fifth-generation tensor cores.
 //
-// All three products are computed as D[m][n] = sum_k A[m][k] B[n][k] with m the output's contiguous
-// dimension, so that neighbouring lanes always store neighbouring addresses:
-//     y  = x W^T     m = out feature  n = token        k = in feature
-//     dx = dz W      m = in feature   n = token        k = out feature
-//     dW = dz^T x    m = in feature   n = out feature  k = token
+// All three products are D[m][n] = sum_k A[m][k] B[n][k] with m the output's contiguous dimension:
+//     y  = x W^T     m = out feature  n = token        k = in feature     A rows of W, B rows of x
+//     dx = dz W      m = in feature   n = token        k = out feature    A columns of W, B rows of dz
+//     dW = dz^T x    m = in feature   n = out feature  k = token          A columns of x, B columns of dz
+// m is the accumulator's lane, so the 32 lanes of an epilogue warp store 32 neighbouring elements and
+// hold exactly one block of the 8-bit form, and a single token costs a 16-column tile, not a 128-row one.
+//
+// A block computes 128 x BN tiles (BN up to 256, a multiple of 16 that wastes the least of n), 64 deep
+// stages: one thread feeds shared memory by TMA, one issues tcgen05.mma, eight warps empty the
+// accumulator of one tile while the next one is summed in the other half of tensor memory.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
+#include <algorithm>
 #include <initializer_list>
+#include <mutex>
 
 #include "pg_train_device.h"
 
 namespace pgt {
 namespace {
 
+constexpr int kBM = 128;              // lanes of an accumulator
+constexpr int kBK = 64;               // elements of k in a stage: one 128-byte swizzled row
+constexpr int kMaxStages = 12;
+constexpr int kSmemBytes = 232448;    // what a block may have
+constexpr int kABytes = kBM * kBK * 2;
+constexpr int kRawBytes = kBM * kBK;  // an 8-bit A stage before it is widened
+constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
+constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
+
+enum Mode { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kWeightGrad8 = 3 };
+
 // What happens to D: stored as fp32 (dW), or passed through bias, activation and residual to 16 bits.
 struct Epilogue {
-    int32_t fp32, accumulate, activation;
+    int32_t accumulate, activation;
     pg_matrix out;             // n rows of m elements
     pg_matrix residual;
     const float* bias;
     int64_t bias_stride;
     pg_matrix8 z8;
 };
-struct Operand {               // element (row, k) of worker b at data + b stride + row ld + k step
-    const void* data;
-    int64_t ld, step, stride;
-    const uint8_t* scales;     // set for an 8-bit operand; its blocks run along the rows index (m)
+struct Problem {
+    Epilogue ep;
+    int M, N, K, batch;
+    int BN, m_tiles, n_tiles, stages, k_blocks, splits;
+    int64_t tiles;
+    int a_shared, b_shared;    // operand is the same for every worker
+    const uint8_t* scales;     // of an 8-bit A
     int64_t scale_ld, scale_stride;
 };
 
-constexpr int kTile = 64, kDepth = 16;
+__device__ unsigned g_training_error;   // a bounded wait gave up; read and cleared by pg_training_status
 
-template <typename H>
-__global__ void __launch_bounds__(256)
-product_kernel(Operand A, Operand B, Epilogue ep, int M, int N, int K) {
-    __shared__ float s_a[kDepth][kTile + 1], s_b[kDepth][kTile + 1];
-    __shared__ float s_d[kTile][kTile + 1];
-    const int64_t b = blockIdx.z;
-    const int m0 = blockIdx.x * kTile, n0 = blockIdx.y * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < K; k0 += kDepth) {
-        __syncthreads();
-        for (int t = threadIdx.x; t < kTile * kDepth; t += 256) {
-            const int r = t / kDepth, k = t % kDepth;
-            float va = 0.0f, vb = 0.0f;
-            if (m0 + r < M && k0 + k < K) {
-                const int64_t at = b * A.stride + (m0 + r) * A.ld + (k0 + k) * A.step;
-                if (A.scales)
-                    va = static_cast<const int8_t*>(A.data)[at] *
-                         scale_value(A.scales[b * A.scale_stride + (k0 + k) * A.scale_ld + (m0 + r) / kBlock8]);
-                else
-                    va = Elem<H>::up(static_cast<const uint16_t*>(A.data)[at]);
-            }
-            if (n0 + r < N && k0 + k < K)
-                vb = Elem<H>::up(static_cast<const uint16_t*>(B.data)[b * B.stride + (n0 + r) * B.ld + (k0 + k) * B.step]);
-            s_a[k][r] = va;
-            s_b[k][r] = vb;
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up) {
+    if (bar_try(b, parity)) return true;
+    long long t0, t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (bar_try(b, parity)) return true;
+        if (*gave_up) return false;
+        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+        if (t - t0 > kWaitNs) {
+            *gave_up = 1;
+            atomicOr(&g_training_error, 1u);
+            return false;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(s_a[k][tx * 4 + i], s_b[k][ty * 4 + j], acc[i][j]);
     }
+}
+__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(idesc), "r"(add)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+// Shared-memory operand descriptors, 128-byte swizzle.  K-major: rows of 64 k, 8-row groups 1024 bytes
+// apart.  MN-major: rows of 64 m (one per k), 8-k groups 1024 bytes apart, the next 64 m 8192 bytes on.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major) {
+    const uint64_t lead = mn_major ? 8192 >> 4 : 1, group = 1024 >> 4;
+    return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | lead << 16 | group << 32 | uint64_t{1} << 46 | uint64_t{2} << 61;
+}
+
+// ------------------------------------------------------------------ epilogue
+// Columns n .. n + count - 1 (16 at most) of lane m.
+template <typename H, int ACT, bool FP32>
+__device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t b, int64_t n, int count, int m, bool live, float bias) {
+    if constexpr (FP32) {
+        float* o = static_cast<float*>(ep.out.data) + b * ep.out.stride + n * ep.out.ld + m;
+        if (!live) return;
+        if (ep.accumulate) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s_d[ty * 4 + j][tx * 4 + i] = acc[i][j];
-    __syncthreads();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int m = m0 + (warp & 1) * 32 + lane;
-    const float bias = ep.bias && m < M ? ep.bias[b * ep.bias_stride + m] : 0.0f;
-    for (int j = warp >> 1; j < kTile && n0 + j < N; j += 4) {
-        float v = s_d[j][(warp & 1) * 32 + lane];
-        const int64_t n = n0 + j;
-        if (ep.fp32) {
-            if (m < M) {
-                float* o = static_cast<float*>(ep.out.data) + b * ep.out.stride + n * ep.out.ld + m;
-                *o = ep.accumulate ? *o + v : v;
-            }
-            continue;
+            for (int i = 0; i < 16; ++i)
+                if (i < count) v[i] += o[i * ep.out.ld];
         }
-        v += bias;
-        if (ep.z8.values) {
-            const uint32_t s = scale_byte<H>(block_top<1>(m < M ? __float_as_uint(v) & 0x7fffffffu : 0u));
-            if (m < M) {
-                ep.z8.values[b * ep.z8.stride + n * ep.z8.ld + m] = static_cast<int8_t>(to8(v, scale_inverse(s)));
-                if (lane == 0) ep.z8.scales[b * ep.z8.scale_stride + n * ep.z8.scale_ld + m / kBlock8] = static_cast<uint8_t>(s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < count) o[i * ep.out.ld] = v[i];
+    } else {
+        uint16_t res[16];
+        const bool add = ep.residual.data != nullptr;
+        if (add && live) {
+            const uint16_t* r = static_cast<const uint16_t*>(ep.residual.data) + b * ep.residual.stride + n * ep.residual.ld + m;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) res[i] = i < count ? r[i * ep.residual.ld] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += bias;
+        if (ep.z8.values) {        // the warp's 32 lanes are one block
+            int8_t* q = ep.z8.values + b * ep.z8.stride + n * ep.z8.ld + m;
+            uint8_t* s = ep.z8.scales + b * ep.z8.scale_stride + n * ep.z8.scale_ld + m / kBlock8;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, live ? __float_as_uint(v[i]) & 0x7fffffffu : 0u));
+                if (live && i < count) {
+                    q[i * ep.z8.ld] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)));
+                    if (m % kBlock8 == 0) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
+                }
             }
         }
-        if (ep.activation == PG_ACT_RELU) v = activate<PG_ACT_RELU>(v);
-        if (ep.activation == PG_ACT_GELU) v = activate<PG_ACT_GELU>(v);
-        if (ep.activation == PG_ACT_SILU) v = activate<PG_ACT_SILU>(v);
-        if (m < M) {
-            if (ep.residual.data)
-                v += Elem<H>::up(static_cast<const uint16_t*>(ep.residual.data)[b * ep.residual.stride + n * ep.residual.ld + m]);
-            static_cast<uint16_t*>(ep.out.data)[b * ep.out.stride + n * ep.out.ld + m] = Elem<H>::down(v);
+        if (!live) return;
+        uint16_t* o = static_cast<uint16_t*>(ep.out.data) + b * ep.out.stride + n * ep.out.ld + m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float y = activate<ACT>(v[i]);
+            if (add) y += Elem<H>::up(res[i]);
+            if (i < count) o[i * ep.out.ld] = Elem<H>::down(y);
         }
     }
 }
 
-int run_product(int dtype, int batch, int64_t M, int64_t N, int64_t K, const Operand& A, const Operand& B, const Epilogue& ep, void* stream) {
-    const dim3 grid((M + kTile - 1) / kTile, (N + kTile - 1) / kTile, batch);
-    if (grid.y > 65535) return PG_ERR_TOO_LARGE;
-    if (dtype == PG_BF16) product_kernel<__nv_bfloat16><<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(A, B, ep, M, N, K);
-    else product_kernel<__half><<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(A, B, ep, M, N, K);
+struct Shared {
+    uint64_t loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
+    uint32_t tmem;
+    int gave_up;
+};
+
+// One tile's accumulator to the output, or (split k) to this block's part in shared memory.
+template <typename H, int ACT, bool FP32>
+__device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, float* part, int64_t b, int m0, int n0, int half, int quarter, int lane) {
+    const int m = m0 + quarter * 32 + lane;
+    const bool live = m < p.M;
+    const float bias = !FP32 && p.ep.bias && live ? p.ep.bias[b * p.ep.bias_stride + m] : 0.0f;
+    // the two warps of a quarter take every other 16 columns
+    for (int j = half * 16; j < p.BN && (part || n0 + j < p.N); j += 32) {
+        float v[16];
+        if (p.K > 0) tmem_load16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j, v);
+        else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+        }
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[(j + i) * kBM + quarter * 32 + lane] = v[i];
+        } else {
+            emit<H, ACT, FP32>(p.ep, v, b, n0 + j, min(16, p.N - n0 - j), m, live, bias);
+        }
+    }
+}
+// Split k: this block adds up all parts of its share of the columns, in the order of the blocks.
+template <typename H, int ACT, bool FP32>
+__device__ __forceinline__ void join_parts(const Problem& p, float* part, int64_t b, int m0, int n0, int rank, int half, int quarter, int lane) {
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    const int m = m0 + quarter * 32 + lane;
+    const bool live = m < p.M;
+    const float bias = !FP32 && p.ep.bias && live ? p.ep.bias[b * p.ep.bias_stride + m] : 0.0f;
+    const int per = p.BN / p.splits, each = per / 2;       // BN is a multiple of 16 and splits at most 8
+    const int j0 = rank * per + half * each;
+    for (int j = j0; j < j0 + each && n0 + j < p.N; j += 16) {
+        const int count = min(min(16, j0 + each - j), p.N - n0 - j);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+        for (int r = 0; r < p.splits; ++r) {
+            const float* far = cluster.map_shared_rank(part, r) + j * kBM + quarter * 32 + lane;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < count) v[i] += far[i * kBM];
+        }
+        emit<H, ACT, FP32>(p.ep, v, b, n0 + j, count, m, live, bias);
+    }
+}
+template <typename H, Mode MODE, typename F>
+__device__ __forceinline__ void with_activation(int act, F&& f) {
+    if constexpr (MODE == kForward) {
+        if (act == PG_ACT_GELU) f(std::integral_constant<int, PG_ACT_GELU>{});
+        else if (act == PG_ACT_SILU) f(std::integral_constant<int, PG_ACT_SILU>{});
+        else if (act == PG_ACT_RELU) f(std::integral_constant<int, PG_ACT_RELU>{});
+        else f(std::integral_constant<int, PG_ACT_NONE>{});
+    } else {
+        f(std::integral_constant<int, PG_ACT_NONE>{});
+    }
+}
+
+// ------------------------------------------------------------------ 8-bit operand
+// Four 8-bit values to two pairs of 16-bit ones times a power of two, exactly: with bit 7 set aside, a
+// byte's low bits L under the exponent of 128 (bf16) or 1024 (fp16) read 128 + L, the sign bit alone
+// 128 or 256, and their difference is L - 128 sign, the byte's value.
+template <typename H>
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t scale2, uint32_t& lo, uint32_t& hi) {
+    constexpr uint32_t kOne = std::is_same<H, __half>::value ? 0x64006400u : 0x43004300u;
+    using H2 = typename std::conditional<std::is_same<H, __half>::value, __half2, __nv_bfloat162>::type;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t t = __byte_perm(w, 0, i ? 0x4342 : 0x4140);
+        uint32_t a = (t & 0x007f007fu) | kOne, s = (t & 0x00800080u) | kOne;
+        H2 d = __hmul2(__hsub2(*reinterpret_cast<H2*>(&a), *reinterpret_cast<H2*>(&s)), *reinterpret_cast<H2*>(&scale2));
+        (i ? hi : lo) = *reinterpret_cast<uint32_t*>(&d);
+    }
+}
+template <typename H>
+__device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
+    const float f = scale_value(s);
+    return Elem<H>::down2(f, f);
+}
+
+// ------------------------------------------------------------------ the kernel
+// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 4 - 11 empty accumulators, 12 - 15 widen an
+// 8-bit A.  Every wait ends: it is for work that this block has already started, and a wait that takes
+// two seconds makes the whole block give up, see g_training_error.
+template <typename H, Mode MODE>
+__global__ void __launch_bounds__(MODE == kWeightGrad8 ? 512 : 384, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Problem p) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ Shared sh;
+    constexpr bool kAMn = MODE != kForward, kBMn = MODE == kWeightGrad || MODE == kWeightGrad8;
+    constexpr bool kFp32 = kBMn;
+    uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
+    const int b_bytes = p.BN * kBK * 2;
+    const int stage_bytes = kABytes + b_bytes + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            bar_init(&sh.loaded[s], 1);
+            bar_init(&sh.widened[s], 4);
+            bar_init(&sh.empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&sh.summed[i], 1);
+            bar_init(&sh.drained[i], 8);
+        }
+        bar_init(&sh.last, 1);
+        sh.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = sh.tmem;
+    volatile int* gave_up = &sh.gave_up;
+
+    // a block's tiles: every gridDim-th, or with split k the one of its cluster
+    const int rank = p.splits > 1 ? blockIdx.x % p.splits : 0;
+    const int64_t first = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x;
+    const int64_t step = p.splits > 1 ? p.tiles : gridDim.x;
+    const int kb0 = p.k_blocks * rank / p.splits, kb1 = p.k_blocks * (rank + 1) / p.splits;
+    const int64_t per_worker = int64_t{p.m_tiles} * p.n_tiles;
+    auto place = [&](int64_t tile, int64_t& b, int& m0, int& n0) {
+        b = tile / per_worker;
+        const int64_t in = tile - b * per_worker;
+        n0 = static_cast<int>(in / p.m_tiles) * p.BN;
+        m0 = static_cast<int>(in % p.m_tiles) * kBM;
+    };
+
+    if (warp == 0 && lane == 0) {
+        int it = 0;
+        bool ok = true;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
+            int64_t b;
+            int m0, n0;
+            place(tile, b, m0, n0);
+            const int ba = p.a_shared ? 0 : static_cast<int>(b), bb = p.b_shared ? 0 : static_cast<int>(b);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int s = it % p.stages;
+                if (it >= p.stages && !(ok = bar_wait(&sh.empty[s], (it / p.stages - 1) & 1, gave_up))) break;
+                uint8_t* a = ring + s * stage_bytes;
+                uint8_t* bt = a + kABytes;
+                const int k0 = kb * kBK;
+                bar_expect(&sh.loaded[s], (MODE == kWeightGrad8 ? kRawBytes : kABytes) + b_bytes);
+                if constexpr (MODE == kForward) {
+                    tma_load(a, &map_a, k0, m0, ba, &sh.loaded[s]);
+                } else if constexpr (MODE == kWeightGrad8) {
+                    tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.loaded[s]);
+                } else {
+                    tma_load(a, &map_a, m0, k0, ba, &sh.loaded[s]);
+                    tma_load(a + 8192, &map_a, m0 + 64, k0, ba, &sh.loaded[s]);
+                }
+                if constexpr (kBMn) {
+                    for (int j = 0; j < p.BN; j += 64) tma_load(bt + j * 128, &map_b, n0 + j, k0, bb, &sh.loaded[s]);
+                } else {
+                    tma_load(bt, &map_b, k0, n0, bb, &sh.loaded[s]);
+                }
+            }
+        }
+        if (!ok)       // copies still on their way must land before the block ends
+            for (int i = max(0, it - p.stages); i < it; ++i)
+                for (int t = 0; t < 100000 && !bar_try(&sh.loaded[i % p.stages], (i / p.stages) & 1); ++t) {}
+    } else if (warp == 1 && lane == 0) {
+        constexpr uint32_t fmt = std::is_same<H, __half>::value ? 0 : 1;
+        const uint32_t idesc = 1u << 4 | fmt << 7 | fmt << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
+                               static_cast<uint32_t>(p.BN >> 3) << 17 | static_cast<uint32_t>(kBM >> 4) << 24;
+        int it = 0, done = 0;
+        bool ok = true;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step, ++done) {
+            const int acc = done & 1;
+            if (done >= 2 && !(ok = bar_wait(&sh.drained[acc], (done / 2 - 1) & 1, gave_up))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int s = it % p.stages;
+                if (!(ok = bar_wait(&sh.loaded[s], (it / p.stages) & 1, gave_up))) break;
+                if (MODE == kWeightGrad8 && !(ok = bar_wait(&sh.widened[s], (it / p.stages) & 1, gave_up))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t a = smem_u32(ring + s * stage_bytes);
+                const int steps = (min(kBK, p.K - kb * kBK) + 15) / 16;
+                for (int k = 0; k < steps; ++k)
+                    mma_f16(tmem + acc * p.BN, operand_desc(a + k * (kAMn ? 2048 : 32), kAMn),
+                            operand_desc(a + kABytes + k * (kBMn ? 2048 : 32), kBMn), idesc, kb > kb0 || k > 0);
+                mma_commit(&sh.empty[s]);
+            }
+            if (ok) mma_commit(&sh.summed[acc]);
+        }
+        if (!ok) {
+            mma_commit(&sh.last);
+            for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
+        }
+    } else if (warp >= 4 && warp < 12) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        int done = 0;
+        for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
+            const int acc = done & 1;
+            int64_t b;
+            int m0, n0;
+            place(tile, b, m0, n0);
+            if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            __syncwarp();
+            with_activation<H, MODE>(p.ep.activation, [&](auto act) {
+                empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0, n0,
+                                                           half, quarter, lane);
+            });
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.drained[acc]);
+        }
+    } else if (MODE == kWeightGrad8 && warp >= 12) {
+        // thread: row k = r of the stage, 64 of its 128 values (two blocks).  The 16-byte pieces are taken in
+        // an order that puts the 8 threads of a shared-memory phase on different banks, reading and writing.
+        const int r = (threadIdx.x - 384) >> 1, h = threadIdx.x & 1;
+        int it = 0;
+        bool ok = true;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
+            int64_t b;
+            int m0, n0;
+            place(tile, b, m0, n0);
+            const uint8_t* scales = p.scales + b * p.scale_stride + (m0 + h * 64) / kBlock8;
+            const bool one = m0 + h * 64 < p.M, two = m0 + h * 64 + 32 < p.M;
+            auto fetch = [&](int kb, uint32_t& s0, uint32_t& s1) {
+                const int64_t k = static_cast<int64_t>(kb) * kBK + r;
+                const bool in = kb < kb1 && k < p.K;
+                s0 = in && one ? scales[k * p.scale_ld] : 0u;
+                s1 = in && two ? scales[k * p.scale_ld + 1] : 0u;
+            };
+            uint32_t s0[2], s1[2];
+            fetch(kb0, s0[0], s1[0]);
+            fetch(kb0 + 1, s0[1], s1[1]);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int s = it % p.stages;
+                uint32_t n0s, n1s;
+                fetch(kb + 2, n0s, n1s);
+                if (!(ok = bar_wait(&sh.loaded[s], (it / p.stages) & 1, gave_up))) break;
+                uint8_t* a = ring + s * stage_bytes;
+                const uint8_t* raw = a + kABytes + b_bytes + r * 128 + h * 64;
+                const uint32_t f0 = scale_pair<H>(s0[0]), f1 = scale_pair<H>(s1[0]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = (i + (r & 3) + 2 * h) & 3;
+                    const uint4 w = *reinterpret_cast<const uint4*>(raw + c * 16);
+                    const uint32_t f = c < 2 ? f0 : f1;
+                    uint4 o0, o1;
+                    widen4<H>(w.x, f, o0.x, o0.y);
+                    widen4<H>(w.y, f, o0.z, o0.w);
+                    widen4<H>(w.z, f, o1.x, o1.y);
+                    widen4<H>(w.w, f, o1.z, o1.w);
+                    uint8_t* row = a + h * 8192 + r * 128;
+                    *reinterpret_cast<uint4*>(row + (((2 * c) ^ (r & 7)) << 4)) = o0;
+                    *reinterpret_cast<uint4*>(row + (((2 * c + 1) ^ (r & 7)) << 4)) = o1;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.widened[s]);
+                s0[0] = s0[1];
+                s1[0] = s1[1];
+                s0[1] = n0s;
+                s1[1] = n1s;
+            }
+        }
+    }
+
+    if (p.splits > 1) {
+        __syncwarp();
+        cooperative_groups::this_cluster().sync();
+        if (warp >= 4 && warp < 12 && !*gave_up) {
+            int64_t b;
+            int m0, n0;
+            place(first, b, m0, n0);
+            with_activation<H, MODE>(p.ep.activation, [&](auto act) {
+                join_parts<H, decltype(act)::value, kFp32>(p, reinterpret_cast<float*>(ring), b, m0, n0, rank, (warp - 4) >> 2, warp & 3, lane);
+            });
+        }
+        __syncwarp();
+        cooperative_groups::this_cluster().sync();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 2) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+    }
+}
+
+// Rows of 16-bit elements copied to rows that start on 16-byte boundaries, for operands TMA cannot read
+// where they are: 8 elements a thread.
+__global__ void __launch_bounds__(256)
+align_rows_kernel(const uint16_t* __restrict__ src, int64_t src_ld, int64_t src_stride, uint16_t* __restrict__ dst, int64_t dst_ld, int rows, int cols,
+                  int64_t total) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (at >= total) return;
+    const int chunks = static_cast<int>(dst_ld / 8);
+    const int64_t row = at / chunks;
+    const int col = static_cast<int>(at - row * chunks) * 8;
+    const int64_t b = row / rows, r = row - b * rows;
+    const uint16_t* p = src + b * src_stride + r * src_ld + col;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = col + 2 * i < cols ? p[2 * i] : 0, hi = col + 2 * i + 1 < cols ? p[2 * i + 1] : 0;
+        w[i] = lo | hi << 16;
+    }
+    *reinterpret_cast<uint4*>(dst + row * dst_ld + col) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ------------------------------------------------------------------ host
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+    static EncodeFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
+}
+
+// An operand as TMA sees it: `rows` rows of `cols` elements per worker, boxes of box_rows x 128 bytes (8-bit: no swizzle).
+bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_rows) {
+    EncodeFn fn = encoder();
+    if (!fn) return false;
+    const int size = eight ? 1 : 2;
+    const bool shared = batch > 1 && m.stride == 0;
+    const int64_t unit = 16 / size;
+    const int64_t ld = rows > 1 ? m.ld : (cols + unit - 1) / unit * unit;
+    const int64_t stride = batch > 1 && !shared ? m.stride : ld * rows;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(shared ? 1 : batch)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * size), static_cast<cuuint64_t>(stride * size)};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / size), static_cast<cuuint32_t>(box_rows), 1};
+    const cuuint32_t one[3] = {1, 1, 1};
+    const CUtensorMapDataType type = eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return fn(&map, type, 3, m.data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Can TMA read the operand where it is?
+bool aligned(const pg_matrix& m, int64_t batch, int64_t rows) {
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows <= 1 || m.ld % 8 == 0) && (batch <= 1 || m.stride % 8 == 0);
+}
+size_t copy_bytes(const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols) {
+    if (batch == 0 || rows == 0 || aligned(m, batch, rows)) return 0;
+    const int64_t workers = m.stride == 0 ? 1 : batch;
+    return static_cast<size_t>((workers * rows * ((cols + 7) / 8 * 8) * 2 + 255) / 256 * 256);
+}
+// The operand, or its copy with aligned rows in the workspace.
+int aligned_operand(pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, uint8_t*& workspace, cudaStream_t st) {
+    const size_t bytes = copy_bytes(m, batch, rows, cols);
+    if (bytes == 0) return PG_OK;
+    const int64_t workers = m.stride == 0 ? 1 : batch;
+    const int64_t ld = (cols + 7) / 8 * 8, total = workers * rows * (ld / 8);
+    if ((total + 255) / 256 > 0x7fffffff) return PG_ERR_TOO_LARGE;
+    align_rows_kernel<<<static_cast<unsigned>((total + 255) / 256), 256, 0, st>>>(static_cast<const uint16_t*>(m.data), m.ld, m.stride,
+                                                                                  reinterpret_cast<uint16_t*>(workspace), ld, static_cast<int>(rows),
+                                                                                  static_cast<int>(cols), total);
+    m.data = workspace;
+    m.ld = ld;
+    m.stride = m.stride == 0 ? 0 : rows * ld;
+    workspace += bytes;
     return launch_status();
+}
+
+template <typename H, Mode MODE>
+int launch(const CUtensorMap& a, const CUtensorMap& b, const Problem& p, cudaStream_t st) {
+    static std::once_flag once[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
+    bool fine = true;
+    std::call_once(once[dev], [&] {
+        fine = cudaFuncSetAttribute(product_kernel<H, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - 2048) == cudaSuccess;
+    });
+    if (!fine) return PG_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.splits > 1 ? p.tiles * p.splits : std::min<int64_t>(p.tiles, kSMs)));
+    cfg.blockDim = dim3(MODE == kWeightGrad8 ? 512 : 384);
+    cfg.dynamicSmemBytes = p.stages * (kABytes + p.BN * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0)) + 1024;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = p.splits;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE>, a, b, p) != cudaSuccess) {
+        cudaGetLastError();
+        return PG_ERR_CUDA;
+    }
+    return PG_OK;
+}
+
+template <Mode MODE>
+int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const pg_matrix& A, const pg_matrix& B, const Epilogue& ep, const pg_matrix8* a8,
+                cudaStream_t st) {
+    constexpr bool kBMn = MODE == kWeightGrad || MODE == kWeightGrad8;
+    constexpr bool kAMn = MODE != kForward;
+    Problem p = {};
+    p.ep = ep;
+    p.M = static_cast<int>(M);
+    p.N = static_cast<int>(N);
+    p.K = static_cast<int>(K);
+    p.batch = static_cast<int>(batch);
+    p.m_tiles = static_cast<int>((M + kBM - 1) / kBM);
+    // the fewest column tiles, and those as narrow as they cover N; a tile that TMA loads in boxes of 64
+    // columns (MN-major) has a multiple of them
+    const int unit = kBMn ? 64 : 16;
+    p.n_tiles = static_cast<int>((N + 255) / 256);
+    p.BN = static_cast<int>(((N + p.n_tiles - 1) / p.n_tiles + unit - 1) / unit * unit);
+    p.n_tiles = static_cast<int>((N + p.BN - 1) / p.BN);
+    p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
+    p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
+    p.splits = 1;
+    while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
+    const int stage = kABytes + p.BN * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    p.stages = std::min(kMaxStages, (kSmemBytes - 3072) / stage);
+    p.a_shared = A.stride == 0;
+    p.b_shared = B.stride == 0;
+    if (a8) {
+        p.scales = a8->scales;
+        p.scale_ld = a8->scale_ld;
+        p.scale_stride = a8->scale_stride;
+    }
+    CUtensorMap map_a = {}, map_b = {};
+    if (K > 0) {
+        const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, kAMn ? kBK : kBM) &&
+                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, kBMn ? kBK : p.BN);
+        if (!fine) return PG_ERR_CUDA;
+    }
+    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE>(map_a, map_b, p, st) : launch<__half, MODE>(map_a, map_b, p, st);
 }
 
 int current_device() {
     int d = 0;
     return cudaGetDevice(&d) == cudaSuccess ? d : -1;
+}
+bool workspace_ok(size_t need, const void* workspace, size_t bytes, int dev) {
+    return need == 0 || (bytes >= need && device_pointer(workspace, 16, dev));
 }
 
 }  // namespace
@@ -124,10 +630,11 @@ extern "C" {
 
 int pg_linear_workspace_bytes(const pg_linear_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->in_features, args->out_features)) return PG_ERR_INVALID;
-    *bytes_out = 0;
+    *bytes_out = copy_bytes(args->x, args->batch, args->tokens, args->in_features) +
+                 copy_bytes(args->weight, args->batch, args->tokens ? args->out_features : 0, args->in_features);
     return PG_OK;
 }
-int pg_linear(const pg_linear_args* args, void*, size_t, void* stream) {
+int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_bytes, void* stream) {
     if (!args) return PG_ERR_INVALID;
     const pg_linear_args& a = *args;
     const int dev = current_device();
@@ -139,19 +646,26 @@ int pg_linear(const pg_linear_args* args, void*, size_t, void* stream) {
     if (a.residual.data && !matrix_ok(a.residual, a.batch, a.tokens, a.out_features, 2, false, dev)) return PG_ERR_INVALID;
     if (!matrix_ok(a.y, a.batch, a.tokens, a.out_features, 2, true, dev)) return PG_ERR_INVALID;
     if ((a.z8.values || a.z8.scales) && !matrix8_ok(a.z8, a.batch, a.tokens, a.out_features, true, dev)) return PG_ERR_INVALID;
+    size_t need = 0;
+    pg_linear_workspace_bytes(args, &need);
+    if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
-    const Operand A{a.weight.data, a.weight.ld, 1, a.weight.stride, nullptr, 0, 0};
-    const Operand B{a.x.data, a.x.ld, 1, a.x.stride, nullptr, 0, 0};
-    const Epilogue ep{0, 0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
-    return run_product(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, A, B, ep, stream);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    pg_matrix x = a.x, w = a.weight;
+    int rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
+    if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
+    const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
+    return rc != PG_OK ? rc : run_product<kForward>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
 
 int pg_linear_input_grad_workspace_bytes(const pg_input_grad_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->in_features, args->out_features)) return PG_ERR_INVALID;
-    *bytes_out = 0;
+    *bytes_out = copy_bytes(args->dz, args->batch, args->tokens, args->out_features) +
+                 copy_bytes(args->weight, args->batch, args->tokens ? args->out_features : 0, args->in_features);
     return PG_OK;
 }
-int pg_linear_input_grad(const pg_input_grad_args* args, void*, size_t, void* stream) {
+int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
     if (!args) return PG_ERR_INVALID;
     const pg_input_grad_args& a = *args;
     const int dev = current_device();
@@ -160,19 +674,26 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void*, size_t, void* st
     if (!matrix_ok(a.weight, a.batch, a.out_features, a.in_features, 2, false, dev)) return PG_ERR_INVALID;
     if (a.residual.data && !matrix_ok(a.residual, a.batch, a.tokens, a.in_features, 2, false, dev)) return PG_ERR_INVALID;
     if (!matrix_ok(a.dx, a.batch, a.tokens, a.in_features, 2, true, dev)) return PG_ERR_INVALID;
+    size_t need = 0;
+    pg_linear_input_grad_workspace_bytes(args, &need);
+    if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
-    const Operand A{a.weight.data, 1, a.weight.ld, a.weight.stride, nullptr, 0, 0};
-    const Operand B{a.dz.data, a.dz.ld, 1, a.dz.stride, nullptr, 0, 0};
-    const Epilogue ep{0, 0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
-    return run_product(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, A, B, ep, stream);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    pg_matrix dz = a.dz, w = a.weight;
+    int rc = aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st);
+    if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
+    const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
+    return rc != PG_OK ? rc : run_product<kInputGrad>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
 
 int pg_linear_weight_grad_workspace_bytes(const pg_weight_grad_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->in_features, args->out_features)) return PG_ERR_INVALID;
-    *bytes_out = 0;
+    *bytes_out = copy_bytes(args->dz, args->batch, args->tokens, args->out_features) +
+                 (args->x8.values ? 0 : copy_bytes(args->x, args->batch, args->tokens, args->in_features));
     return PG_OK;
 }
-int pg_linear_weight_grad(const pg_weight_grad_args* args, void*, size_t, void* stream) {
+int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
     if (!args) return PG_ERR_INVALID;
     const pg_weight_grad_args& a = *args;
     const int dev = current_device();
@@ -184,16 +705,35 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void*, size_t, void* 
               : !matrix_ok(a.x, a.batch, a.tokens, a.in_features, 2, false, dev))
         return PG_ERR_INVALID;
     if (!matrix_ok(a.dweight, a.batch, a.out_features, a.in_features, 4, true, dev)) return PG_ERR_INVALID;
+    size_t need = 0;
+    pg_linear_weight_grad_workspace_bytes(args, &need);
+    if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0) return PG_OK;
-    const Operand A = eight ? Operand{a.x8.values, 1, a.x8.ld, a.x8.stride, a.x8.scales, a.x8.scale_ld, a.x8.scale_stride}
-                            : Operand{a.x.data, 1, a.x.ld, a.x.stride, nullptr, 0, 0};
-    const Operand B{a.dz.data, 1, a.dz.ld, a.dz.stride, nullptr, 0, 0};
-    const Epilogue ep{1, a.accumulate, PG_ACT_NONE, a.dweight, {}, nullptr, 0, {}};
-    return run_product(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, A, B, ep, stream);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    const Epilogue ep{a.accumulate, PG_ACT_NONE, a.dweight, {}, nullptr, 0, {}};
+    pg_matrix dz = a.dz, x = a.x;
+    int rc = a.tokens > 0 ? aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st) : PG_OK;
+    if (eight) {
+        x = pg_matrix{a.x8.values, a.x8.ld, a.x8.stride};
+        return rc != PG_OK ? rc : run_product<kWeightGrad8>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st);
+    }
+    if (rc == PG_OK && a.tokens > 0) rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
+    return rc != PG_OK ? rc : run_product<kWeightGrad>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
 }
 
 int pg_training_status(void* stream) {
-    return cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) == cudaSuccess ? PG_OK : PG_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    unsigned word = 0;
+    const unsigned none = 0;
+    if (cudaMemcpyFromSymbolAsync(&word, g_training_error, sizeof word, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess)
+        return PG_ERR_CUDA;
+    if (word == 0) return PG_OK;
+    if (cudaMemcpyToSymbolAsync(g_training_error, &none, sizeof none, 0, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess)
+        return PG_ERR_CUDA;
+    return PG_ERR_TIMEOUT;
 }
 
 }  // extern "C"

@@ -548,8 +548,7 @@ def test_refusals_of_the_library(tr):
                 dict(dtype=2), dict(act=4), dict(act=-1), dict(tokens=-1), dict(n_in=0), dict(yp=None), dict(out_ld=7), dict(out_stride=0)):
         assert linear(**bad) == pg.PG_ERR_INVALID, bad
     # rows that are not 16-byte aligned go through the workspace, so there has to be one
-    spare = torch.empty_like(y)
-    assert linear(xp=x.data_ptr() + 2, ld=17, stride=68, tokens=3, yp=spare.data_ptr()) in (pg.PG_ERR_WORKSPACE, pg.PG_OK)
+    assert linear(xp=x.data_ptr() + 2, ld=17, stride=68, tokens=3) == pg.PG_ERR_WORKSPACE
     c8 = tr.pg_checkpoint_write(x)
     a = tr.pg_checkpoint_args(0, 2, 4, 16, tr.pg_matrix(x.data_ptr(), 16, 64),
                               tr.pg_matrix8(c8.values.data_ptr(), c8.scales.data_ptr(), 24, 96, 1, 4))
