@@ -36,25 +36,42 @@ template <> struct Elem<__half> {
     }
 };
 
-// V neighbouring 16-bit elements in one access.  V = 8 and 2 need 16- and 4-byte addresses.
-template <typename H, int V>
-__device__ __forceinline__ void load16(const void* base, int64_t at, float (&v)[V]) {
+// V neighbouring 16-bit elements in one access, as they lie in memory (two to a word).  V = 8 and 2 need
+// 16- and 4-byte addresses.  Loading is kept apart from widening so that all loads of a row are on their
+// way before the first one is needed.
+template <int V> struct Raw { uint32_t w[(V + 1) / 2]; };
+
+template <int V>
+__device__ __forceinline__ Raw<V> load_raw(const void* base, int64_t at) {
     const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+    Raw<V> r;
     if constexpr (V == 8) {
-        const uint4 w = *reinterpret_cast<const uint4*>(p);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = Elem<H>::up(static_cast<uint16_t>(u[i] & 0xffffu));
-            v[2 * i + 1] = Elem<H>::up(static_cast<uint16_t>(u[i] >> 16));
-        }
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        r.w[0] = u.x;
+        r.w[1] = u.y;
+        r.w[2] = u.z;
+        r.w[3] = u.w;
     } else if constexpr (V == 2) {
-        const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
-        v[0] = Elem<H>::up(static_cast<uint16_t>(u & 0xffffu));
-        v[1] = Elem<H>::up(static_cast<uint16_t>(u >> 16));
+        r.w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-        v[0] = Elem<H>::up(*p);
+        r.w[0] = *p;
     }
+    return r;
+}
+// The first n < V of them (the end of a row); the rest are zero.
+template <int V>
+__device__ __forceinline__ Raw<V> load_raw_end(const void* base, int64_t at, int n) {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+    Raw<V> r = {};
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < n) r.w[i / 2] |= static_cast<uint32_t>(p[i]) << (16 * (i & 1));
+    return r;
+}
+template <typename H, int V>
+__device__ __forceinline__ void widen(const Raw<V>& r, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = Elem<H>::up(static_cast<uint16_t>(i & 1 ? r.w[i / 2] >> 16 : r.w[i / 2] & 0xffffu));
 }
 template <typename H, int V>
 __device__ __forceinline__ void store16(void* base, int64_t at, const float (&v)[V]) {
@@ -71,16 +88,6 @@ __device__ __forceinline__ void store16(void* base, int64_t at, const float (&v)
     } else {
         *p = Elem<H>::down(v[0]);
     }
-}
-// The same with the first n of V elements only (the end of a row); the rest read as zero.
-template <typename H, int V>
-__device__ __forceinline__ void load16n(const void* base, int64_t at, int n, float (&v)[V]) {
-    if (n >= V) {
-        load16<H, V>(base, at, v);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = i < n ? Elem<H>::up(static_cast<const uint16_t*>(base)[at + i]) : 0.0f;
 }
 template <typename H, int V>
 __device__ __forceinline__ void store16n(void* base, int64_t at, int n, const float (&v)[V]) {
@@ -128,24 +135,45 @@ __device__ __forceinline__ void store8n(int8_t* p, int n, const int (&q)[V]) {
             if (i < n) p[i] = static_cast<int8_t>(q[i]);
     }
 }
+// V neighbouring 8-bit values as they lie in memory, and their numbers.
+template <int V> struct Raw8 { uint32_t w[(V + 3) / 4]; };
 template <int V>
-__device__ __forceinline__ void load8n(const int8_t* p, int n, int (&q)[V]) {
-    if (V == 8 && n >= V) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p);
-#pragma unroll
-        for (int i = 0; i < V; ++i) q[i] = static_cast<int8_t>((i < 4 ? w.x : w.y) >> (8 * (i & 3)) & 255);
-    } else if (V == 2 && n >= V) {
-        const uint32_t w = *reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-        for (int i = 0; i < V; ++i) q[i] = static_cast<int8_t>(w >> (8 * i) & 255);
+__device__ __forceinline__ Raw8<V> load_raw8(const int8_t* p) {
+    Raw8<V> r;
+    if constexpr (V == 8) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        r.w[0] = u.x;
+        r.w[1] = u.y;
+    } else if constexpr (V == 2) {
+        r.w[0] = *reinterpret_cast<const uint16_t*>(p);
     } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) q[i] = i < n ? p[i] : 0;
+        r.w[0] = static_cast<uint8_t>(*p);
     }
+    return r;
+}
+template <int V>
+__device__ __forceinline__ Raw8<V> load_raw8_end(const int8_t* p, int n) {
+    Raw8<V> r = {};
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < n) r.w[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i & 3));
+    return r;
+}
+template <int V>
+__device__ __forceinline__ void widen8(const Raw8<V>& r, float scale, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = static_cast<float>(static_cast<int8_t>(r.w[i / 4] >> (8 * (i & 3)) & 255u)) * scale;
 }
 
 // ------------------------------------------------------------------ activations
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
+// s(v) = 1 / (1 + 2^(-v log2 e)); both approximations are good to two units in the last place, 2^x overflows to
+// infinity and 1 / infinity is 0, so the ends are exact.
+__device__ __forceinline__ float sigmoid(float v) {
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+    return s;
+}
 constexpr float kGelu0 = 1.5957691216057308f;             // 2 sqrt(2/pi)
 constexpr float kGelu1 = 0.044715f * 1.5957691216057308f;
 

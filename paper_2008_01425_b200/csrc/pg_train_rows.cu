@@ -14,11 +14,10 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// ---------------------------------------------------------------- norm
+// ---------------------------------------------------------------- rows in registers
 // A group of T threads holds one row in registers: chunk c of a thread is the V neighbouring
 // elements at (c T + t) V, so a warp reads consecutive addresses whatever V is, and a block of the
-// 8-bit form lies in 32 / V neighbouring lanes.  The row is read once; the sum of squares comes
-// from the registers.
+// 8-bit form lies in 32 / V neighbouring lanes.
 template <int T>
 __device__ __forceinline__ float group_sum(float v, float* s_part) {
 #pragma unroll
@@ -33,7 +32,41 @@ __device__ __forceinline__ float group_sum(float v, float* s_part) {
     }
     return v;
 }
-
+// All loads of a row, with no branch between them; only a row whose end cuts a chunk short takes a second look.
+template <int V, int C, int T>
+__device__ __forceinline__ void read_row(const void* base, int64_t at, int cols, int t, Raw<V> (&r)[C]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * T + t) * V;
+        r[c] = Raw<V>{};
+        if (col + V <= cols) r[c] = load_raw<V>(base, at + col);
+    }
+    if (V > 1 && cols % V != 0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * T + t) * V;
+            if (col < cols && col + V > cols) r[c] = load_raw_end<V>(base, at + col, cols - col);
+        }
+    }
+}
+template <typename H, int V, int C, int T>
+__device__ __forceinline__ void write_row(void* base, int64_t at, int cols, int t, const float (&v)[C][V]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * T + t) * V;
+        if (col < cols) store16n<H, V>(base, at + col, cols - col, v[c]);
+    }
+}
+// fp32 vectors (gains) come from the L1 cache, which the rows of a worker share.
+template <int V>
+__device__ __forceinline__ void read_gain(const float* gain, int col, int cols, float (&g)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = 1.0f;
+    if (gain) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = col + i < cols ? gain[col + i] : 0.0f;
+    }
+}
 // The 8-bit form of a row held in registers, and back in v the values it stands for.
 template <typename H, int V, int C, int T>
 __device__ __forceinline__ void row_to_8(float (&v)[C][V], int cols, int t, int8_t* values, uint8_t* scales) {
@@ -59,188 +92,221 @@ __device__ __forceinline__ void row_to_8(float (&v)[C][V], int cols, int t, int8
     }
 }
 
+// ---------------------------------------------------------------- norm
+// Block: kGroups rows of one worker.  The row is read once; the sum of squares comes from the registers.
 template <typename H, int V, int C, int T>
 __global__ void __launch_bounds__(T > 32 ? T : 256)
-norm_kernel(const pg_norm_args a, int64_t rows, int64_t rows_per_group) {
+norm_kernel(const pg_norm_args a) {
     __shared__ float s_part[32];
-    constexpr int kGroups = T > 32 ? 1 : 256 / T;
     const int t = T > 32 ? threadIdx.x : threadIdx.x & 31;
-    const int64_t group = static_cast<int64_t>(blockIdx.x) * kGroups + (T > 32 ? 0 : threadIdx.x >> 5);
-    const int64_t r0 = group * rows_per_group;
-    const int64_t r1 = min(rows, r0 + rows_per_group);
-    constexpr bool kKeep = T <= 256;   // registers left for the gain of the rows' worker
-    int64_t held = -1;             // worker whose gain is in registers
-    float gain[C][V];
-    for (int64_t r = r0; r < r1; ++r) {
-        const int64_t b = r / a.tokens, tok = r - b * a.tokens;
-        float v[C][V];
+    const int64_t b = blockIdx.y;
+    const int tok = T > 32 ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (tok >= a.tokens) return;                       // the whole group
+    float v[C][V];
+    {
+        Raw<V> x[C], r[C];
+        read_row<V, C, T>(a.x.data, b * a.x.stride + tok * a.x.ld, a.cols, t, x);
+        if (a.residual.data) read_row<V, C, T>(a.residual.data, b * a.residual.stride + tok * a.residual.ld, a.cols, t, r);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * T + t) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[c][i] = 0.0f;
-            if (col < a.cols) load16n<H, V>(a.x.data, b * a.x.stride + tok * a.x.ld + col, a.cols - col, v[c]);
-        }
+        for (int c = 0; c < C; ++c) widen<H, V>(x[c], v[c]);
         if (a.residual.data) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int col = (c * T + t) * V;
                 float w[V];
-                if (col < a.cols) {
-                    load16n<H, V>(a.residual.data, b * a.residual.stride + tok * a.residual.ld + col, a.cols - col, w);
+                widen<H, V>(r[c], w);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) v[c][i] += w[i];
-                }
-            }
-        }
-        if (kKeep && b != held) {
-            held = b;
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int col = (c * T + t) * V + i;
-                    gain[c][i] = !a.gain ? 1.0f : col < a.cols ? a.gain[b * a.gain_stride + col] : 0.0f;
-                }
-        }
-        float sum = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum = fmaf(v[c][i], v[c][i], sum);
-        sum = group_sum<T>(sum, s_part);
-        const float rstd = rsqrtf(sum / a.cols + a.eps);
-        if (a.rstd && t == 0) a.rstd[r] = rstd;
-        if (a.h.data) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int col = (c * T + t) * V;
-                if (col < a.cols) store16n<H, V>(a.h.data, b * a.h.stride + tok * a.h.ld + col, a.cols - col, v[c]);
-            }
-        }
-        if (a.h8.values) {
-            float w[C][V];
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < V; ++i) w[c][i] = v[c][i];
-            row_to_8<H, V, C, T>(w, a.cols, t, a.h8.values + b * a.h8.stride + tok * a.h8.ld,
-                                 a.h8.scales + b * a.h8.scale_stride + tok * a.h8.scale_ld);
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int col = (c * T + t) * V + i;
-                if constexpr (!kKeep) gain[c][i] = a.gain && col < a.cols ? a.gain[b * a.gain_stride + col] : 1.0f;
-                v[c][i] *= rstd * gain[c][i];
-            }
-        if (a.y8.values)
-            row_to_8<H, V, C, T>(v, a.cols, t, a.y8.values + b * a.y8.stride + tok * a.y8.ld,
-                                 a.y8.scales + b * a.y8.scale_stride + tok * a.y8.scale_ld);
-        if (a.y.data) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int col = (c * T + t) * V;
-                if (col < a.cols) store16n<H, V>(a.y.data, b * a.y.stride + tok * a.y.ld + col, a.cols - col, v[c]);
+                for (int i = 0; i < V; ++i) v[c][i] += w[i];
             }
         }
     }
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+    sum = group_sum<T>(sum, s_part);
+    const float rstd = rsqrtf(sum / a.cols + a.eps);
+    if (a.rstd && t == 0) a.rstd[b * a.tokens + tok] = rstd;
+    if (a.h.data) write_row<H, V, C, T>(a.h.data, b * a.h.stride + tok * a.h.ld, a.cols, t, v);
+    if (a.h8.values) {
+        float w[C][V];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[c][i] = v[c][i];
+        row_to_8<H, V, C, T>(w, a.cols, t, a.h8.values + b * a.h8.stride + tok * a.h8.ld,
+                             a.h8.scales + b * a.h8.scale_stride + tok * a.h8.scale_ld);
+    }
+    if (!a.y.data && !a.y8.values) return;
+    const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        float g[V];
+        read_gain<V>(gain, (c * T + t) * V, a.cols, g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[c][i] *= rstd * g[i];
+    }
+    if (a.y8.values)
+        row_to_8<H, V, C, T>(v, a.cols, t, a.y8.values + b * a.y8.stride + tok * a.y8.ld,
+                             a.y8.scales + b * a.y8.scale_stride + tok * a.y8.scale_ld);
+    if (a.y.data) write_row<H, V, C, T>(a.y.data, b * a.y.stride + tok * a.y.ld, a.cols, t, v);
 }
 
 // ---------------------------------------------------------------- norm gradient
-// Rows as above; every group also keeps the sum of dy u over its rows of one worker in registers.
-// partial[b][k][cols]: what group k of worker b added up; summed in that order by the second kernel.
-template <typename H, int V, int C, int T, bool EIGHT>
-__global__ void __launch_bounds__(T > 32 ? T : 256)
-norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int groups, int rows_per_group) {
-    __shared__ float s_part[32];
-    constexpr int kGroups = T > 32 ? 1 : 256 / T;
+// Rows as above, R of them at a time so that one exchange serves R dot products and R rows are on their way
+// together; every group also keeps the sum of dy u over its rows of one worker in registers.  What was
+// read stays packed and is widened again for the second use: dx needs the row's dot product first.
+// partial[b][k][cols]: what block k of worker b added up; summed in that order by the second kernel.
+constexpr int kGradBlock = 128;
+template <typename H, int V, int C, int T, int R, bool EIGHT>
+__global__ void __launch_bounds__(T > 32 ? T : kGradBlock)
+norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int rows_per_group) {
+    extern __shared__ float s_sum[];                   // warps x cols, T == 32 only
+    __shared__ float s_part[2][R][32];
+    constexpr int kGroups = T > 32 ? 1 : kGradBlock / T;
     const int t = T > 32 ? threadIdx.x : threadIdx.x & 31;
     const int64_t b = blockIdx.y;
     const int group = blockIdx.x * kGroups + (T > 32 ? 0 : threadIdx.x >> 5);
-    if (group >= groups) return;                       // T > 32: the whole block; T == 32: the whole warp
-    const int r0 = group * rows_per_group;
-    const int r1 = min(a.tokens, r0 + rows_per_group);
-    float gain[C][V], sum_dg[C][V];
+    const int64_t r0 = static_cast<int64_t>(group) * rows_per_group;
+    const int64_t r1 = min(static_cast<int64_t>(a.tokens), r0 + rows_per_group);
+    const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
+    float sum_dg[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum_dg[c][i] = 0.0f;
+    int flip = 0;
+    for (int64_t r = r0; r < r1; r += R, flip ^= 1) {
+        Raw<V> dy_raw[R][C], h_raw[R][C], dh_raw[R][C];
+        Raw8<V> q_raw[R][C];
+        uint32_t q_scale[R][C];
+        float rstd[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {                  // a row past the last one reads the last one again, and counts for nothing
+            const int64_t row = min(r + k, r1 - 1);
+            read_row<V, C, T>(a.dy.data, b * a.dy.stride + row * a.dy.ld, a.cols, t, dy_raw[k]);
+            if constexpr (EIGHT) {
+                const int8_t* q = a.h8.values + b * a.h8.stride + row * a.h8.ld;
+                const uint8_t* s = a.h8.scales + b * a.h8.scale_stride + row * a.h8.scale_ld;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int col = (c * T + t) * V;
+                    q_raw[k][c] = Raw8<V>{};
+                    q_scale[k][c] = 0;
+                    if (col + V <= a.cols) q_raw[k][c] = load_raw8<V>(q + col);
+                    if (col < a.cols) q_scale[k][c] = s[col / kBlock8];
+                }
+                if (V > 1 && a.cols % V != 0) {
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        const int col = (c * T + t) * V;
+                        if (col < a.cols && col + V > a.cols) q_raw[k][c] = load_raw8_end<V>(q + col, a.cols - col);
+                    }
+                }
+            } else {
+                read_row<V, C, T>(a.h.data, b * a.h.stride + row * a.h.ld, a.cols, t, h_raw[k]);
+            }
+            if (a.dh.data) read_row<V, C, T>(a.dh.data, b * a.dh.stride + row * a.dh.ld, a.cols, t, dh_raw[k]);
+            rstd[k] = a.rstd[b * a.tokens + row];
+        }
+        // u of a chunk; past the end of the row it is zero, as dy is
+        auto unit = [&](int k, int c, float (&u)[V]) {
+            if constexpr (EIGHT) widen8<V>(q_raw[k][c], scale_value(q_scale[k][c]), u);
+            else widen<H, V>(h_raw[k][c], u);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                u[i] *= rstd[k];
+                if (EIGHT && (c * T + t) * V + i >= a.cols) u[i] = 0.0f;     // not NaN, where the last block's scale says so
+            }
+        };
+        float dot[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) dot[k] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float g[V];
+            read_gain<V>(gain, (c * T + t) * V, a.cols, g);
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                float dy[V], u[V];
+                widen<H, V>(dy_raw[k][c], dy);
+                unit(k, c, u);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float w = dy[i] * u[i];
+                    if (r + k < r1) sum_dg[c][i] += w;
+                    dot[k] = fmaf(w, g[i], dot[k]);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < R; ++k) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], o);
+        if constexpr (T > 32) {        // (the other half of s_part is still being read by slower warps)
+            if ((threadIdx.x & 31) == 0)
+#pragma unroll
+                for (int k = 0; k < R; ++k) s_part[flip][k][threadIdx.x >> 5] = dot[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                dot[k] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < T / 32; ++w) dot[k] += s_part[flip][k][w];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) dot[k] /= a.cols;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * T + t) * V;
+            float g[V];
+            read_gain<V>(gain, col, a.cols, g);
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                float dy[V], u[V], dx[V];
+                widen<H, V>(dy_raw[k][c], dy);
+                unit(k, c, u);
+#pragma unroll
+                for (int i = 0; i < V; ++i) dx[i] = 0.0f;
+                if (a.dh.data) widen<H, V>(dh_raw[k][c], dx);
+#pragma unroll
+                for (int i = 0; i < V; ++i) dx[i] += rstd[k] * (dy[i] * g[i] - u[i] * dot[k]);
+                if (col < a.cols && r + k < r1)
+                    store16n<H, V>(a.dx.data, b * a.dx.stride + (r + k) * a.dx.ld + col, a.cols - col, dx);
+            }
+        }
+    }
+    if (!a.dgain) return;
+    float* out = partial + (b * gridDim.x + blockIdx.x) * a.cols;
+    float* mine = T > 32 ? out : s_sum + (threadIdx.x >> 5) * a.cols;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int col = (c * T + t) * V + i;
-            if constexpr (T <= 256) gain[c][i] = !a.gain ? 1.0f : col < a.cols ? a.gain[b * a.gain_stride + col] : 0.0f;
-            sum_dg[c][i] = 0.0f;
+            if (col < a.cols) mine[col] = sum_dg[c][i];
         }
-    for (int r = r0; r < r1; ++r) {
-        float dy[C][V], u[C][V];
-        const float rstd = a.rstd[b * a.tokens + r];
+    if constexpr (T == 32) {
+        __syncthreads();
+        for (int col = threadIdx.x; col < a.cols; col += kGradBlock) {
+            float v = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * T + t) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) dy[c][i] = u[c][i] = 0.0f;
-            if (col < a.cols) {
-                load16n<H, V>(a.dy.data, b * a.dy.stride + r * a.dy.ld + col, a.cols - col, dy[c]);
-                if constexpr (EIGHT) {
-                    int q[V];
-                    load8n<V>(a.h8.values + b * a.h8.stride + r * a.h8.ld + col, a.cols - col, q);
-                    const float s = scale_value(a.h8.scales[b * a.h8.scale_stride + r * a.h8.scale_ld + col / kBlock8]);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) u[c][i] = i < a.cols - col ? q[i] * s : 0.0f;
-                } else {
-                    load16n<H, V>(a.h.data, b * a.h.stride + r * a.h.ld + col, a.cols - col, u[c]);
-                }
-            }
+            for (int w = 0; w < kGroups; ++w) v += s_sum[w * a.cols + col];
+            out[col] = v;
         }
-        float dot = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                u[c][i] *= rstd;
-                sum_dg[c][i] = fmaf(dy[c][i], u[c][i], sum_dg[c][i]);
-                if constexpr (T > 256) {
-                    const int col = (c * T + t) * V + i;
-                    gain[c][i] = a.gain && col < a.cols ? a.gain[b * a.gain_stride + col] : 1.0f;
-                }
-                dy[c][i] *= gain[c][i];
-                dot = fmaf(dy[c][i], u[c][i], dot);
-            }
-        dot = group_sum<T>(dot, s_part) / a.cols;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * T + t) * V;
-            if (col < a.cols) {
-                float dx[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] = 0.0f;
-                if (a.dh.data) load16n<H, V>(a.dh.data, b * a.dh.stride + r * a.dh.ld + col, a.cols - col, dx);
-#pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] += rstd * (dy[c][i] - u[c][i] * dot);
-                store16n<H, V>(a.dx.data, b * a.dx.stride + r * a.dx.ld + col, a.cols - col, dx);
-            }
-        }
-    }
-    if (a.dgain) {
-        float* out = partial + (b * groups + group) * a.cols;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int col = (c * T + t) * V + i;
-                if (col < a.cols) out[col] = sum_dg[c][i];
-            }
     }
 }
 
 __global__ void __launch_bounds__(256)
-sum_partials_kernel(const float* __restrict__ partial, int groups, int cols, float* __restrict__ out, int64_t out_stride, int accumulate) {
+sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ out, int64_t out_stride, int accumulate) {
     __shared__ float s_sum[8][32];
     const int64_t b = blockIdx.y;
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
     float sum = 0.0f;
     if (col < cols)
-        for (int k = w; k < groups; k += 8) sum += partial[(b * groups + k) * cols + col];
+#pragma unroll 4
+        for (int k = w; k < parts; k += 8) sum += partial[(b * parts + k) * cols + col];
     s_sum[w][threadIdx.x & 31] = sum;
     __syncthreads();
     if (w == 0 && col < cols) {
@@ -254,8 +320,9 @@ sum_partials_kernel(const float* __restrict__ partial, int groups, int cols, flo
 
 // ---------------------------------------------------------------- activation gradient
 // A block takes a strip of 32 V columns and a share of a worker's tokens; 8 rows at a time, one per
-// warp.  Column sums stay in registers, are joined over the warps in shared memory and over the
-// blocks of a cluster (the shares of one strip) through distributed shared memory, in a fixed order.
+// warp, four times that in flight.  Column sums stay in registers, are joined over the warps in shared
+// memory and over the blocks of a cluster (the shares of one strip) through distributed shared memory, in
+// a fixed order.
 template <typename H, int V, int ACT>
 __global__ void __launch_bounds__(256)
 activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
@@ -264,28 +331,61 @@ activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int splits = gridDim.z, split = blockIdx.z;
     const int col = (blockIdx.x * 32 + lane) * V;
-    const int r1 = min(a.tokens, (split + 1) * rows_per_block);
+    const int64_t r0 = static_cast<int64_t>(split) * rows_per_block;
+    const int r1 = static_cast<int>(min(static_cast<int64_t>(a.tokens), r0 + rows_per_block));
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-    if (col < a.cols) {
-        const int n = a.cols - col;
-#pragma unroll 4
-        for (int r = split * rows_per_block + warp; r < r1; r += 8) {
-            float dy[V], z[V];
-            load16n<H, V>(a.dy.data, b * a.dy.stride + r * a.dy.ld + col, n, dy);
-            if (a.z8.values) {
-                int q[V];
-                load8n<V>(a.z8.values + b * a.z8.stride + r * a.z8.ld + col, n, q);
-                const float s = scale_value(a.z8.scales[b * a.z8.scale_stride + r * a.z8.scale_ld + col / kBlock8]);
+    const void* dy_at = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + col;
+    void* dz_at = a.dz.data ? static_cast<uint16_t*>(a.dz.data) + b * a.dz.stride + col : nullptr;
+    const int8_t* q_at = a.z8.values ? a.z8.values + b * a.z8.stride + col : nullptr;
+    const uint8_t* s_at = a.z8.values ? a.z8.scales + b * a.z8.scale_stride + col / kBlock8 : nullptr;
+    auto one = [&](const Raw<V>& dy_raw, const Raw8<V>& q_raw, uint32_t scale, float (&dy)[V]) {
+        widen<H, V>(dy_raw, dy);
+        if (q_at) {
+            float z[V];
+            widen8<V>(q_raw, scale_value(scale), z);
 #pragma unroll
-                for (int i = 0; i < V; ++i) z[i] = q[i] * s;
+            for (int i = 0; i < V; ++i) dy[i] *= slope<ACT>(z[i]);
+        }
 #pragma unroll
-                for (int i = 0; i < V; ++i) dy[i] *= slope<ACT>(z[i]);
+        for (int i = 0; i < V; ++i) sum[i] += dy[i];
+    };
+    if (col + V <= a.cols) {
+        int64_t r = r0 + warp;
+        for (; r + 24 < r1; r += 32) {
+            Raw<V> d[4];
+            Raw8<V> q[4];
+            uint32_t s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[k] = load_raw<V>(dy_at, (r + 8 * k) * a.dy.ld);
+            if (q_at) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    q[k] = load_raw8<V>(q_at + (r + 8 * k) * a.z8.ld);
+                    s[k] = s_at[(r + 8 * k) * a.z8.scale_ld];
+                }
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += dy[i];
-            if (a.dz.data) store16n<H, V>(a.dz.data, b * a.dz.stride + r * a.dz.ld + col, n, dy);
+            for (int k = 0; k < 4; ++k) {
+                float dy[V];
+                one(d[k], q[k], s[k], dy);
+                if (dz_at) store16<H, V>(dz_at, (r + 8 * k) * a.dz.ld, dy);
+            }
+        }
+        for (; r < r1; r += 8) {
+            float dy[V];
+            const Raw8<V> q = q_at ? load_raw8<V>(q_at + r * a.z8.ld) : Raw8<V>{};
+            one(load_raw<V>(dy_at, r * a.dy.ld), q, q_at ? s_at[r * a.z8.scale_ld] : 0u, dy);
+            if (dz_at) store16<H, V>(dz_at, r * a.dz.ld, dy);
+        }
+    } else if (col < a.cols) {             // the lane that the row's end cuts short
+        const int n = a.cols - col;
+        for (int64_t r = r0 + warp; r < r1; r += 8) {
+            float dy[V];
+            const Raw8<V> q = q_at ? load_raw8_end<V>(q_at + r * a.z8.ld, n) : Raw8<V>{};
+            one(load_raw_end<V>(dy_at, r * a.dy.ld, n), q, q_at ? s_at[r * a.z8.scale_ld] : 0u, dy);
+            if (dz_at) store16n<H, V>(dz_at, r * a.dz.ld, n, dy);
         }
     }
     if (!a.dbias) return;
@@ -330,11 +430,14 @@ checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int chunks) {
     int8_t* values = a.x8.values + b * a.x8.stride + tok * a.x8.ld + col;
     uint8_t* scale = a.x8.scales + b * a.x8.scale_stride + tok * a.x8.scale_ld + col / kBlock8;
     float v[V];
-    int q[V];
     if constexpr (WRITE) {
+        int q[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = 0.0f;
-        if (live) load16n<H, V>(a.x.data, b * a.x.stride + tok * a.x.ld + col, n, v);
+        if (live) {
+            const int64_t from = b * a.x.stride + tok * a.x.ld + col;
+            widen<H, V>(n >= V ? load_raw<V>(a.x.data, from) : load_raw_end<V>(a.x.data, from, n), v);
+        }
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
@@ -348,10 +451,7 @@ checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int chunks) {
             if (col % kBlock8 == 0) *scale = static_cast<uint8_t>(s);
         }
     } else if (live) {
-        load8n<V>(values, n, q);
-        const float s = scale_value(*scale);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = q[i] * s;
+        widen8<V>(n >= V ? load_raw8<V>(values) : load_raw8_end<V>(values, n), scale_value(*scale), v);
         store16n<H, V>(a.x.data, b * a.x.stride + tok * a.x.ld + col, n, v);
     }
 }
@@ -389,15 +489,38 @@ void with_row(int cols, F&& f) {
 }
 constexpr int kMaxNormCols = 16384;
 
-int row_threads(int cols) { return cols <= 1024 ? 32 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024; }
+// The gradient holds three packed rows and a sum per column besides: a warp to 512 columns only, then half the
+// elements a thread, and as many rows at a time as registers allow.
+struct GradRow { int elements, threads, rows; };
+constexpr GradRow kGradRows[] = {{8, 32, 2}, {16, 32, 2}, {8, 128, 4}, {16, 128, 2}, {16, 256, 2}, {16, 512, 2}, {16, 1024, 1}};
+int grad_row(int cols) {
+    int k = 0;
+    while (kGradRows[k].elements * kGradRows[k].threads < cols) ++k;
+    return k;
+}
+template <typename F>
+void with_grad_row(int cols, F&& f) {
+    using std::integral_constant;
+    switch (grad_row(cols)) {
+        case 0: f(integral_constant<int, 0>{}); break;
+        case 1: f(integral_constant<int, 1>{}); break;
+        case 2: f(integral_constant<int, 2>{}); break;
+        case 3: f(integral_constant<int, 3>{}); break;
+        case 4: f(integral_constant<int, 4>{}); break;
+        case 5: f(integral_constant<int, 5>{}); break;
+        default: f(integral_constant<int, 6>{});
+    }
+}
 
-// Groups that share the rows of one worker in the gradient: about two waves of warps on the GPU, each
-// with four rows at least.
-int norm_grad_groups(const pg_norm_grad_args& a) {
-    const int64_t per_gpu = int64_t{kSMs} * 2048 / 2 / row_threads(a.cols);
-    int64_t g = a.batch > 0 ? (per_gpu + a.batch - 1) / a.batch : 1;
-    g = std::min<int64_t>(g, (a.tokens + 3) / 4);
-    return static_cast<int>(std::max<int64_t>(g, 1));
+// Blocks that share the rows of one worker in the gradient: as many as are resident at once (about 512
+// threads' worth of registers per SM), with two steps of R rows a group at least.
+int norm_grad_blocks(const pg_norm_grad_args& a) {
+    const GradRow g = kGradRows[grad_row(a.cols)];
+    const int groups = g.threads > 32 ? 1 : kGradBlock / 32;
+    const int64_t resident = int64_t{kSMs} * std::max(1, 512 / (g.threads > 32 ? g.threads : kGradBlock));
+    int64_t n = a.batch > 0 ? resident / a.batch : 1;
+    n = std::min<int64_t>(n, (a.tokens + 2 * g.rows * groups - 1) / (2 * g.rows * groups));
+    return static_cast<int>(std::max<int64_t>(n, 1));
 }
 
 }  // namespace
@@ -421,20 +544,15 @@ int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
     if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
     if (a.rstd && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
     if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
-    const int64_t rows = int64_t{a.batch} * a.tokens;
-    if (rows == 0) return PG_OK;
+    if (a.batch == 0 || a.tokens == 0) return PG_OK;
     const int width = access_width({&a.x, &a.residual, &a.h, &a.y}, a.batch);
     with_type(a.dtype, width, [&](auto h, auto v) {
         using H = decltype(h);
         constexpr int V = decltype(v)::value;
         with_row(a.cols, [&](auto e, auto threads) {
             constexpr int T = decltype(threads)::value, C = decltype(e)::value / V;
-            constexpr int kGroups = T > 32 ? 1 : 8, kBlock = T > 32 ? T : 256;
-            const int64_t most = int64_t{kSMs} * 8 * (2048 / 8 / kBlock > 0 ? 2048 / 8 / kBlock : 1) * kGroups;
-            const int64_t per = std::max<int64_t>(1, (rows + most - 1) / most);
-            const int64_t groups = (rows + per - 1) / per;
-            norm_kernel<H, V, C, T><<<static_cast<unsigned>((groups + kGroups - 1) / kGroups), kBlock, 0,
-                                      static_cast<cudaStream_t>(stream)>>>(a, rows, per);
+            const dim3 grid(T > 32 ? a.tokens : (a.tokens + 7) / 8, a.batch);
+            norm_kernel<H, V, C, T><<<grid, T > 32 ? T : 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
         });
     });
     return launch_status();
@@ -442,7 +560,7 @@ int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
 
 int pg_add_rms_norm_grad_workspace_bytes(const pg_norm_grad_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->cols, 1)) return PG_ERR_INVALID;
-    *bytes_out = args->dgain ? sizeof(float) * norm_grad_groups(*args) * static_cast<size_t>(args->batch) * args->cols : 0;
+    *bytes_out = args->dgain ? sizeof(float) * norm_grad_blocks(*args) * static_cast<size_t>(args->batch) * args->cols : 0;
     return PG_OK;
 }
 
@@ -467,8 +585,7 @@ int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t 
     pg_add_rms_norm_grad_workspace_bytes(args, &need);
     if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
     if (a.batch == 0) return PG_OK;
-    const int groups = norm_grad_groups(a);
-    const int per = (a.tokens + groups - 1) / groups;
+    const int blocks = norm_grad_blocks(a);
     float* partial = static_cast<float*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a.tokens > 0 || a.dgain) {
@@ -476,16 +593,18 @@ int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t 
         with_type(a.dtype, width, [&](auto h, auto v) {
             using H = decltype(h);
             constexpr int V = decltype(v)::value;
-            with_row(a.cols, [&](auto e, auto threads) {
-                constexpr int T = decltype(threads)::value, C = decltype(e)::value / V;
-                constexpr int kGroups = T > 32 ? 1 : 8, kBlock = T > 32 ? T : 256;
-                const dim3 grid((groups + kGroups - 1) / kGroups, a.batch);
-                if (eight) norm_grad_kernel<H, V, C, T, true><<<grid, kBlock, 0, st>>>(a, partial, groups, per);
-                else norm_grad_kernel<H, V, C, T, false><<<grid, kBlock, 0, st>>>(a, partial, groups, per);
+            with_grad_row(a.cols, [&](auto shape) {
+                constexpr GradRow g = kGradRows[decltype(shape)::value];
+                constexpr int T = g.threads, C = g.elements / V, kGroups = T > 32 ? 1 : kGradBlock / 32;
+                const int per = (a.tokens + blocks * kGroups - 1) / (blocks * kGroups);
+                const dim3 grid(blocks, a.batch);
+                const size_t smem = T > 32 ? 0 : sizeof(float) * kGroups * a.cols;
+                if (eight) norm_grad_kernel<H, V, C, T, g.rows, true><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
+                else norm_grad_kernel<H, V, C, T, g.rows, false><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
             });
         });
         if (a.dgain)
-            sum_partials_kernel<<<dim3((a.cols + 31) / 32, a.batch), 256, 0, st>>>(partial, groups, a.cols, a.dgain, a.dgain_stride,
+            sum_partials_kernel<<<dim3((a.cols + 31) / 32, a.batch), 256, 0, st>>>(partial, blocks, a.cols, a.dgain, a.dgain_stride,
                                                                                   a.accumulate);
     }
     return launch_status();
