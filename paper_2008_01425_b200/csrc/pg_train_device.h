@@ -111,7 +111,18 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top_bits) {
 // 2^-(scale - 127); a block marked 255 gets a factor that keeps its values away from the clamp's edge cases.
 __device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - (s < 254u ? s : 253u)) << 23); }
 __device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
-__device__ __forceinline__ int to8(float v, float inverse) { return max(-127, min(127, __float2int_rn(v * inverse))); }
+// Adding 1.5 * 2^23 rounds a number below 2^22 to an integer, ties to even, and leaves that integer in
+// the sum's low bits: one fused multiply-add instead of two conversions, which run at a quarter of the rate.
+// The clamp acts on the sum; a NaN comes out as some valid byte and is marked by its block's scale.
+constexpr float kRound = 12582912.0f;
+struct Q8 {
+    float t;                                           // kRound + q
+    __device__ float value(float scale) const { return (t - kRound) * scale; }
+    __device__ uint32_t bits() const { return __float_as_uint(t); }   // q in the low byte
+};
+__device__ __forceinline__ Q8 to8(float v, float inverse) {
+    return Q8{fminf(fmaxf(fmaf(v, inverse, kRound), kRound - 127.0f), kRound + 127.0f)};
+}
 
 // Largest bits among the lanes that share a block when every lane holds V neighbouring values.
 template <int V>
@@ -121,20 +132,21 @@ __device__ __forceinline__ uint32_t block_top(uint32_t top) {
     return top;
 }
 template <int V>
-__device__ __forceinline__ void store8n(int8_t* p, int n, const int (&q)[V]) {
+__device__ __forceinline__ void store8n(int8_t* p, int n, const Q8 (&q)[V]) {
     if (V == 8 && n >= V) {
         uint2 w;
-        w.x = (q[0] & 255) | (q[1 % V] & 255) << 8 | (q[2 % V] & 255) << 16 | static_cast<uint32_t>(q[3 % V]) << 24;
-        w.y = (q[4 % V] & 255) | (q[5 % V] & 255) << 8 | (q[6 % V] & 255) << 16 | static_cast<uint32_t>(q[7 % V]) << 24;
+        w.x = __byte_perm(__byte_perm(q[0].bits(), q[1 % V].bits(), 0x0040), __byte_perm(q[2 % V].bits(), q[3 % V].bits(), 0x0040), 0x5410);
+        w.y = __byte_perm(__byte_perm(q[4 % V].bits(), q[5 % V].bits(), 0x0040), __byte_perm(q[6 % V].bits(), q[7 % V].bits(), 0x0040), 0x5410);
         *reinterpret_cast<uint2*>(p) = w;
     } else if (V == 2 && n >= V) {
-        *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>((q[0] & 255) | (q[1 % V] & 255) << 8);
+        *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(__byte_perm(q[0].bits(), q[1 % V].bits(), 0x0040));
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = static_cast<int8_t>(q[i]);
+            if (i < n) p[i] = static_cast<int8_t>(q[i].bits() & 255u);
     }
 }
+
 // V neighbouring 8-bit values as they lie in memory, and their numbers.
 template <int V> struct Raw8 { uint32_t w[(V + 3) / 4]; };
 template <int V>
@@ -159,10 +171,14 @@ __device__ __forceinline__ Raw8<V> load_raw8_end(const int8_t* p, int n) {
         if (i < n) r.w[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i & 3));
     return r;
 }
+// A byte with its sign bit flipped (q + 128) under the exponent of 2^23 reads 2^23 + 128 + q.
 template <int V>
 __device__ __forceinline__ void widen8(const Raw8<V>& r, float scale, float (&v)[V]) {
+    uint32_t w[(V + 3) / 4];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = static_cast<float>(static_cast<int8_t>(r.w[i / 4] >> (8 * (i & 3)) & 255u)) * scale;
+    for (int i = 0; i < (V + 3) / 4; ++i) w[i] = r.w[i] ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (__uint_as_float(__byte_perm(w[i / 4], 0x4b000000u, 0x7650 + (i & 3))) - 8388736.0f) * scale;
 }
 
 // ------------------------------------------------------------------ activations
@@ -188,12 +204,10 @@ template <int ACT>
 __device__ __forceinline__ float slope(float z) {
     if constexpr (ACT == PG_ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
     if constexpr (ACT == PG_ACT_GELU) {
-        // beyond +-16 the slope is 1 or 0 to the last bit, and z^2 could overflow; NaN passes through
-        asm("min.NaN.f32 %0, %0, 0f41800000;" : "+f"(z));
-        asm("max.NaN.f32 %0, %0, 0fc1800000;" : "+f"(z));
-        const float z2 = z * z;
+        // z^2 is kept from overflowing; far from zero s (1 - s) is 0 and stays so
+        const float z2 = fminf(z * z, 300.0f);
         const float s = sigmoid(z * fmaf(kGelu1, z2, kGelu0));
-        return fmaf(z * fmaf(3.0f * kGelu1, z2, kGelu0), s * (1.0f - s), s);
+        return fmaf(s * (1.0f - s) * z, fmaf(3.0f * kGelu1, z2, kGelu0), s);
     }
     if constexpr (ACT == PG_ACT_SILU) {
         const float s = sigmoid(z);

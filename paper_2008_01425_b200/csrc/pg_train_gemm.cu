@@ -155,7 +155,7 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
             for (int i = 0; i < 16; ++i) {
                 const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, live ? __float_as_uint(v[i]) & 0x7fffffffu : 0u));
                 if (live && i < count) {
-                    q[i * ep.z8.ld] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)));
+                    q[i * ep.z8.ld] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)).bits() & 255u);
                     if (m % kBlock8 == 0) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
                 }
             }
@@ -177,26 +177,113 @@ struct Shared {
     int gave_up;
 };
 
-// One tile's accumulator to the output, or (split k) to this block's part in shared memory.
+// 16 whole columns for a warp whose lanes are all inside: no predicates, residuals fetched beforehand.
+// Addresses are a base that is the same for the warp and a lane's 32-bit offset.
+template <typename H, int ACT>
+__device__ __forceinline__ void emit_full(const Epilogue& ep, float (&v)[16], const uint16_t (&res)[16], char* out, int8_t* q, uint8_t* s,
+                                          uint32_t lane_out, uint32_t lane_q, bool first, float bias) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += bias;
+    if (q) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
+            (q + i * ep.z8.ld)[lane_q] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)).bits() & 255u);
+            if (first) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = activate<ACT>(v[i]);
+    if (ep.residual.data) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += Elem<H>::up(res[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint16_t*>(out + i * ep.out.ld * 2 + lane_out) = Elem<H>::down(v[i]);
+}
+
+// One tile's accumulator to the output, or (split k) to this block's part in shared memory.  The two warps of a
+// quarter take every other 16 columns.
 template <typename H, int ACT, bool FP32>
 __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, float* part, int64_t b, int m0, int n0, int half, int quarter, int lane) {
+    const Epilogue& ep = p.ep;
     const int m = m0 + quarter * 32 + lane;
     const bool live = m < p.M;
-    const float bias = !FP32 && p.ep.bias && live ? p.ep.bias[b * p.ep.bias_stride + m] : 0.0f;
-    // the two warps of a quarter take every other 16 columns
-    for (int j = half * 16; j < p.BN && (part || n0 + j < p.N); j += 32) {
-        float v[16];
-        if (p.K > 0) tmem_load16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j, v);
-        else {
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    const int end = part ? p.BN : min(p.BN, p.N - n0);
+    const float bias = !FP32 && ep.bias && live ? ep.bias[b * ep.bias_stride + m] : 0.0f;
+    float v[16];
+    if (part || p.K == 0) {
+        for (int j = half * 16; j < end; j += 32) {
+            if (p.K > 0) tmem_load16(lanes + j, v);
+            else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+            }
+            if (part) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[(j + i) * kBM + quarter * 32 + lane] = v[i];
+            } else {
+                emit<H, ACT, FP32>(ep, v, b, n0 + j, min(16, end - j), m, live, bias);
+            }
         }
-        if (part) {
+        return;
+    }
+    int j = half * 16;
+    if (m0 + quarter * 32 + 32 <= p.M) {
+        if constexpr (FP32) {
+            float* o = static_cast<float*>(ep.out.data) + b * ep.out.stride + static_cast<int64_t>(n0 + j) * ep.out.ld + m;
+            const bool add = ep.accumulate;
+            for (; j + 16 <= end; j += 32, o += 32 * ep.out.ld) {
+                float old[16];
+                if (add) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[(j + i) * kBM + quarter * 32 + lane] = v[i];
+                    for (int i = 0; i < 16; ++i) old[i] = o[i * ep.out.ld];
+                }
+                tmem_load16(lanes + j, v);
+                if (add) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += old[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i * ep.out.ld] = v[i];
+            }
         } else {
-            emit<H, ACT, FP32>(p.ep, v, b, n0 + j, min(16, p.N - n0 - j), m, live, bias);
+            const int64_t n = n0 + j;
+            char* out = static_cast<char*>(ep.out.data) + (b * ep.out.stride + n * ep.out.ld) * 2;
+            const char* in = static_cast<const char*>(ep.residual.data) + (b * ep.residual.stride + n * ep.residual.ld) * 2;
+            int8_t* q = ep.z8.values ? ep.z8.values + b * ep.z8.stride + n * ep.z8.ld : nullptr;
+            uint8_t* s = ep.z8.values ? ep.z8.scales + b * ep.z8.scale_stride + n * ep.z8.scale_ld + (m0 + quarter * 32) / kBlock8 : nullptr;
+            const uint32_t lane_m = static_cast<uint32_t>(m);
+            const bool add = ep.residual.data != nullptr;
+            uint16_t res[16], next[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) next[i] = 0;
+            auto fetch = [&](int at) {
+                if (add && at + 16 <= end) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) next[i] = *reinterpret_cast<const uint16_t*>(in + i * ep.residual.ld * 2 + lane_m * 2);
+                }
+                in += 64 * ep.residual.ld;
+            };
+            fetch(j);
+            for (; j + 16 <= end; j += 32) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) res[i] = next[i];
+                fetch(j + 32);
+                tmem_load16(lanes + j, v);
+                emit_full<H, ACT>(ep, v, res, out, q, s, lane_m * 2, lane_m, lane == 0, bias);
+                out += 64 * ep.out.ld;
+                if (q) {
+                    q += 32 * ep.z8.ld;
+                    s += 32 * ep.z8.scale_ld;
+                }
+            }
         }
+    }
+    for (; j < end; j += 32) {             // the last columns, or lanes past the last row
+        tmem_load16(lanes + j, v);
+        emit<H, ACT, FP32>(ep, v, b, n0 + j, min(16, end - j), m, live, bias);
     }
 }
 // Split k: this block adds up all parts of its share of the columns, in the order of the blocks.
@@ -270,7 +357,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
     const int b_bytes = p.BN * kBK * 2;
     const int stage_bytes = kABytes + b_bytes + (MODE == kWeightGrad8 ? kRawBytes : 0);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {

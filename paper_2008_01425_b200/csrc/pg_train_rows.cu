@@ -57,16 +57,26 @@ __device__ __forceinline__ void write_row(void* base, int64_t at, int cols, int 
         if (col < cols) store16n<H, V>(base, at + col, cols - col, v[c]);
     }
 }
-// fp32 vectors (gains) come from the L1 cache, which the rows of a worker share.
+// A worker's gains for a thread's columns; `wide`: V = 8 and 16-byte addresses.
 template <int V>
-__device__ __forceinline__ void read_gain(const float* gain, int col, int cols, float (&g)[V]) {
+__device__ __forceinline__ void read_gain(const float* gain, bool wide, int col, int cols, float (&g)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = 1.0f;
-    if (gain) {
+    if (!gain) return;
+    if (V == 8 && wide) {
+        if (col + V <= cols) {
+            const float4 lo = *reinterpret_cast<const float4*>(gain + col), hi = *reinterpret_cast<const float4*>(gain + col + 4);
+            const float u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-        for (int i = 0; i < V; ++i) g[i] = col + i < cols ? gain[col + i] : 0.0f;
+            for (int i = 0; i < V; ++i) g[i] = u[i];
+            return;
+        }
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (col + i < cols) g[i] = gain[col + i];
 }
+__device__ __forceinline__ bool wide_gain(const float* gain) { return reinterpret_cast<uintptr_t>(gain) % 16 == 0; }
 // The 8-bit form of a row held in registers, and back in v the values it stands for.
 template <typename H, int V, int C, int T>
 __device__ __forceinline__ void row_to_8(float (&v)[C][V], int cols, int t, int8_t* values, uint8_t* scales) {
@@ -79,11 +89,11 @@ __device__ __forceinline__ void row_to_8(float (&v)[C][V], int cols, int t, int8
         top = block_top<V>(top);
         const uint32_t s = scale_byte<H>(top);
         const float inverse = scale_inverse(s), value = scale_value(s);
-        int q[V];
+        Q8 q[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             q[i] = to8(v[c][i], inverse);
-            v[c][i] = q[i] * value;
+            v[c][i] = q[i].value(value);
         }
         if (col < cols) {
             store8n<V>(values + col, cols - col, q);
@@ -142,7 +152,7 @@ norm_kernel(const pg_norm_args a) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         float g[V];
-        read_gain<V>(gain, (c * T + t) * V, a.cols, g);
+        read_gain<V>(gain, wide_gain(gain), (c * T + t) * V, a.cols, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[c][i] *= rstd * g[i];
     }
@@ -170,11 +180,13 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
     const int64_t r0 = static_cast<int64_t>(group) * rows_per_group;
     const int64_t r1 = min(static_cast<int64_t>(a.tokens), r0 + rows_per_group);
     const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
-    float sum_dg[C][V];
+    float sum_dg[C][V], g[C][V];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+        read_gain<V>(gain, wide_gain(gain), (c * T + t) * V, a.cols, g[c]);
 #pragma unroll
         for (int i = 0; i < V; ++i) sum_dg[c][i] = 0.0f;
+    }
     int flip = 0;
     for (int64_t r = r0; r < r1; r += R, flip ^= 1) {
         Raw<V> dy_raw[R][C], h_raw[R][C], dh_raw[R][C];
@@ -224,8 +236,6 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
         for (int k = 0; k < R; ++k) dot[k] = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            float g[V];
-            read_gain<V>(gain, (c * T + t) * V, a.cols, g);
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 float dy[V], u[V];
@@ -235,7 +245,7 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
                 for (int i = 0; i < V; ++i) {
                     const float w = dy[i] * u[i];
                     if (r + k < r1) sum_dg[c][i] += w;
-                    dot[k] = fmaf(w, g[i], dot[k]);
+                    dot[k] = fmaf(w, g[c][i], dot[k]);
                 }
             }
         }
@@ -260,8 +270,6 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * T + t) * V;
-            float g[V];
-            read_gain<V>(gain, col, a.cols, g);
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 float dy[V], u[V], dx[V];
@@ -271,7 +279,7 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
                 for (int i = 0; i < V; ++i) dx[i] = 0.0f;
                 if (a.dh.data) widen<H, V>(dh_raw[k][c], dx);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] += rstd[k] * (dy[i] * g[i] - u[i] * dot[k]);
+                for (int i = 0; i < V; ++i) dx[i] += rstd[k] * (dy[i] * g[c][i] - u[i] * dot[k]);
                 if (col < a.cols && r + k < r1)
                     store16n<H, V>(a.dx.data, b * a.dx.stride + (r + k) * a.dx.ld + col, a.cols - col, dx);
             }
@@ -324,7 +332,7 @@ sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, floa
 // memory and over the blocks of a cluster (the shares of one strip) through distributed shared memory, in
 // a fixed order.
 template <typename H, int V, int ACT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 3)
 activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
     __shared__ float s_sum[8][32 * V];
     const int64_t b = blockIdx.y;
@@ -352,32 +360,27 @@ activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
         for (int i = 0; i < V; ++i) sum[i] += dy[i];
     };
     if (col + V <= a.cols) {
-        int64_t r = r0 + warp;
-        for (; r + 24 < r1; r += 32) {
-            Raw<V> d[4];
-            Raw8<V> q[4];
-            uint32_t s[4];
+        for (int64_t r = r0 + warp; r < r1; r += 32) {      // rows past the end read as zeros
+            Raw<V> d[4] = {};
+            Raw8<V> q[4] = {};
+            uint32_t s[4] = {};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) d[k] = load_raw<V>(dy_at, (r + 8 * k) * a.dy.ld);
+            for (int k = 0; k < 4; ++k)
+                if (r + 8 * k < r1) d[k] = load_raw<V>(dy_at, (r + 8 * k) * a.dy.ld);
             if (q_at) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    q[k] = load_raw8<V>(q_at + (r + 8 * k) * a.z8.ld);
-                    s[k] = s_at[(r + 8 * k) * a.z8.scale_ld];
-                }
+                for (int k = 0; k < 4; ++k)
+                    if (r + 8 * k < r1) {
+                        q[k] = load_raw8<V>(q_at + (r + 8 * k) * a.z8.ld);
+                        s[k] = s_at[(r + 8 * k) * a.z8.scale_ld];
+                    }
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 float dy[V];
                 one(d[k], q[k], s[k], dy);
-                if (dz_at) store16<H, V>(dz_at, (r + 8 * k) * a.dz.ld, dy);
+                if (dz_at && r + 8 * k < r1) store16<H, V>(dz_at, (r + 8 * k) * a.dz.ld, dy);
             }
-        }
-        for (; r < r1; r += 8) {
-            float dy[V];
-            const Raw8<V> q = q_at ? load_raw8<V>(q_at + r * a.z8.ld) : Raw8<V>{};
-            one(load_raw<V>(dy_at, r * a.dy.ld), q, q_at ? s_at[r * a.z8.scale_ld] : 0u, dy);
-            if (dz_at) store16<H, V>(dz_at, r * a.dz.ld, dy);
         }
     } else if (col < a.cols) {             // the lane that the row's end cuts short
         const int n = a.cols - col;
@@ -431,7 +434,7 @@ checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int chunks) {
     uint8_t* scale = a.x8.scales + b * a.x8.scale_stride + tok * a.x8.scale_ld + col / kBlock8;
     float v[V];
     if constexpr (WRITE) {
-        int q[V];
+        Q8 q[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = 0.0f;
         if (live) {
@@ -489,10 +492,10 @@ void with_row(int cols, F&& f) {
 }
 constexpr int kMaxNormCols = 16384;
 
-// The gradient holds three packed rows and a sum per column besides: a warp to 512 columns only, then half the
-// elements a thread, and as many rows at a time as registers allow.
-struct GradRow { int elements, threads, rows; };
-constexpr GradRow kGradRows[] = {{8, 32, 2}, {16, 32, 2}, {8, 128, 4}, {16, 128, 2}, {16, 256, 2}, {16, 512, 2}, {16, 1024, 1}};
+// The gradient holds three packed rows, the gains and a sum per column: 8 elements a thread, or 16 where that saves
+// the exchange between warps or there is no room for more threads.  `blocks`: resident per SM.
+struct GradRow { int elements, threads, rows, blocks; };
+constexpr GradRow kGradRows[] = {{8, 32, 2, 4}, {16, 32, 2, 3}, {8, 128, 2, 5}, {8, 256, 2, 2}, {8, 512, 2, 1}, {16, 512, 2, 1}, {16, 1024, 1, 1}};
 int grad_row(int cols) {
     int k = 0;
     while (kGradRows[k].elements * kGradRows[k].threads < cols) ++k;
@@ -512,13 +515,12 @@ void with_grad_row(int cols, F&& f) {
     }
 }
 
-// Blocks that share the rows of one worker in the gradient: as many as are resident at once (about 512
-// threads' worth of registers per SM), with two steps of R rows a group at least.
+// Blocks that share the rows of one worker in the gradient: as many as are resident at once, with two steps of R
+// rows a group at least.
 int norm_grad_blocks(const pg_norm_grad_args& a) {
     const GradRow g = kGradRows[grad_row(a.cols)];
     const int groups = g.threads > 32 ? 1 : kGradBlock / 32;
-    const int64_t resident = int64_t{kSMs} * std::max(1, 512 / (g.threads > 32 ? g.threads : kGradBlock));
-    int64_t n = a.batch > 0 ? resident / a.batch : 1;
+    int64_t n = a.batch > 0 ? int64_t{kSMs} * g.blocks / a.batch : 1;
     n = std::min<int64_t>(n, (a.tokens + 2 * g.rows * groups - 1) / (2 * g.rows * groups));
     return static_cast<int>(std::max<int64_t>(n, 1));
 }
@@ -624,10 +626,10 @@ int pg_activation_grad(const pg_activation_grad_args* args, void* stream) {
     if (a.batch == 0 || (a.tokens == 0 && !a.dbias)) return PG_OK;
     const int width = access_width({&a.dy, &a.dz}, a.batch);
     const int strips = (a.cols + 32 * width - 1) / (32 * width);
-    // Shares of a strip's tokens: until the GPU has about four blocks per SM, eight at most (the portable
-    // cluster size), no share under 32 tokens.
+    // Shares of a strip's tokens: until the GPU has about 16 blocks per SM (five waves, so that the last one weighs
+    // little), eight at most (the portable cluster size), no share under 32 tokens.
     int splits = 1;
-    while (splits < 8 && int64_t{strips} * a.batch * splits < kSMs * 4 && a.tokens >= 64 * splits) splits *= 2;
+    while (splits < 8 && int64_t{strips} * a.batch * splits < kSMs * 16 && a.tokens >= 64 * splits) splits *= 2;
     const int per = (a.tokens + splits - 1) / splits;
     int rc = PG_OK;
     with_type(a.dtype, width, [&](auto h, auto v) {
