@@ -1,15 +1,21 @@
 // The batched linear layer and its gradients on the fifth-generation tensor cores.
 //
-// All three products are D[m][n] = sum_k A[m][k] B[n][k] with m the output's contiguous dimension:
+// All products are D[m][n] = sum_k A[m][k] B[n][k]; m is the accumulator's lane.
+//   few tokens, m = the output's contiguous dimension:
 //     y  = x W^T     m = out feature  n = token        k = in feature     A rows of W, B rows of x
 //     dx = dz W      m = in feature   n = token        k = out feature    A columns of W, B rows of dz
+//   many tokens, m = token:
+//     y  = x W^T     m = token        n = out feature  k = in feature     A rows of x, B rows of W
+//     dx = dz W      m = token        n = in feature   k = out feature    A rows of dz, B columns of W
+//   always m = the output's contiguous dimension:
 //     dW = dz^T x    m = in feature   n = out feature  k = token          A columns of x, B columns of dz
-// m is the accumulator's lane, so the 32 lanes of an epilogue warp store 32 neighbouring elements and
-// hold exactly one block of the 8-bit form, and a single token costs a 16-column tile, not a 128-row one.
+// With features as lanes a single token costs a 16-column tile, not a 128-row one, and 32 lanes store 32 neighbouring
+// elements.  With tokens as lanes a thread holds 32 neighbouring elements of one row: one block of the 8-bit form,
+// packed conversions, and 16-byte pieces that leave through shared memory and TMA.
 //
-// A block computes 128 x BN tiles (BN up to 256, a multiple of 16 that wastes the least of n), 64 deep
-// stages: one thread feeds shared memory by TMA, one issues tcgen05.mma, eight warps empty the
-// accumulator of one tile while the next one is summed in the other half of tensor memory.
+// A block computes 128 x BN tiles (BN up to 256), 64 deep stages: one thread feeds shared memory by TMA, one issues
+// tcgen05.mma, eight warps empty the accumulator of one tile while the next one is summed in the other half of tensor
+// memory.
 #include <cooperative_groups.h>
 #include <cuda.h>
 
@@ -31,7 +37,15 @@ constexpr int kRawBytes = kBM * kBK;  // an 8-bit A stage before it is widened
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
 constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
 
-enum Mode { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kWeightGrad8 = 3 };
+enum Mode { kForward, kInputGrad, kForwardRows, kInputGradRows, kWeightGrad, kWeightGrad8 };
+template <Mode M> constexpr bool kWeightGrads = M == kWeightGrad || M == kWeightGrad8;
+template <Mode M> constexpr bool kTokenRows = M == kForwardRows || M == kInputGradRows;
+template <Mode M> constexpr bool kAMnMajor = M == kInputGrad || kWeightGrads<M>;
+template <Mode M> constexpr bool kBMnMajor = M == kInputGradRows || kWeightGrads<M>;
+constexpr int kRowWarps = 16;         // epilogue warps where lanes are tokens
+constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out
+template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
+template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 128 : 0);
 
 // What happens to D: stored as fp32 (dW), or passed through bias, activation and residual to 16 bits.
 struct Epilogue {
@@ -48,6 +62,7 @@ struct Problem {
     int BN, m_tiles, n_tiles, stages, k_blocks, splits;
     int64_t tiles;
     int a_shared, b_shared;    // operand is the same for every worker
+    int residual_aligned;      // its rows start on 16-byte boundaries
     const uint8_t* scales;     // of an 8-bit A
     int64_t scale_ld, scale_stride;
 };
@@ -96,6 +111,12 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
 }
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y),
+                 "r"(z)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
                  "r"(idesc), "r"(add)
@@ -116,6 +137,21 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
 // Shared-memory operand descriptors, 128-byte swizzle.  K-major: rows of 64 k, 8-row groups 1024 bytes
 // apart.  MN-major: rows of 64 m (one per k), 8-k groups 1024 bytes apart, the next 64 m 8192 bytes on.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major) {
@@ -124,6 +160,8 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major) {
 }
 
 // ------------------------------------------------------------------ epilogue
+__device__ __forceinline__ uint32_t byte8(float v, float inverse) { return __float_as_uint(clamp8(fmaf(v, inverse, kRound))) & 255u; }
+
 // Columns n .. n + count - 1 (16 at most) of lane m.
 template <typename H, int ACT, bool FP32>
 __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t b, int64_t n, int count, int m, bool live, float bias) {
@@ -140,8 +178,8 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
             if (i < count) o[i * ep.out.ld] = v[i];
     } else {
         uint16_t res[16];
-        const bool add = ep.residual.data != nullptr;
-        if (add && live) {
+        const bool residual = ep.residual.data != nullptr;
+        if (residual && live) {
             const uint16_t* r = static_cast<const uint16_t*>(ep.residual.data) + b * ep.residual.stride + n * ep.residual.ld + m;
 #pragma unroll
             for (int i = 0; i < 16; ++i) res[i] = i < count ? r[i * ep.residual.ld] : 0;
@@ -155,7 +193,7 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
             for (int i = 0; i < 16; ++i) {
                 const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, live ? __float_as_uint(v[i]) & 0x7fffffffu : 0u));
                 if (live && i < count) {
-                    q[i * ep.z8.ld] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)).bits() & 255u);
+                    q[i * ep.z8.ld] = static_cast<int8_t>(byte8(v[i], scale_inverse(sb)));
                     if (m % kBlock8 == 0) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
                 }
             }
@@ -163,10 +201,12 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
         if (!live) return;
         uint16_t* o = static_cast<uint16_t*>(ep.out.data) + b * ep.out.stride + n * ep.out.ld + m;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float y = activate<ACT>(v[i]);
-            if (add) y += Elem<H>::up(res[i]);
-            if (i < count) o[i * ep.out.ld] = Elem<H>::down(y);
+        for (int i = 0; i < 16; i += 2) {
+            F2 y = activate<ACT>(pair(v[i], v[i + 1]));
+            if (residual) y = add(y, pair(Elem<H>::up(res[i]), Elem<H>::up(res[i + 1])));
+            const uint32_t w = Elem<H>::down2(y);
+            if (i < count) o[i * ep.out.ld] = static_cast<uint16_t>(w & 0xffffu);
+            if (i + 1 < count) o[(i + 1) * ep.out.ld] = static_cast<uint16_t>(w >> 16);
         }
     }
 }
@@ -177,29 +217,135 @@ struct Shared {
     int gave_up;
 };
 
+// Lanes are tokens: 16 warps take groups of 32 columns of 32 rows each.  Four warps per scheduler hide each other's
+// loads of residuals.  The result goes to shared memory in the 64-byte swizzle of the output's tensor map and leaves by
+// TMA, which also cuts off what lies outside the matrix.
+template <typename H, int ACT, bool ALIGNED>
+__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, int64_t b, int m0,
+                                           int n0, int share, int quarter, int lane) {
+    const Epilogue& ep = p.ep;
+    const int row = m0 + quarter * 32 + lane;
+    const bool live = row < p.M;
+    const int end = min(p.BN, p.N - n0);
+    const bool add_residual = ep.residual.data != nullptr;
+    for (int j = share * 32; j < end; j += kRowWarps / 4 * 32) {
+        const int n = n0 + j;
+        // the residual's 32 elements of this row: four 16-byte pieces, five where the row starts between two of them
+        uint4 piece[ALIGNED ? 4 : 5];
+        int off = 0;
+        if (add_residual) {
+            const uint16_t* res = static_cast<const uint16_t*>(ep.residual.data) + b * ep.residual.stride + (live ? row : 0) * ep.residual.ld;
+            if (!ALIGNED) off = static_cast<int>(reinterpret_cast<uintptr_t>(res) & 15) / 2;
+            const uint4* at = reinterpret_cast<const uint4*>(res + n - off);
+#pragma unroll
+            for (int i = 0; i < (ALIGNED ? 4 : 5); ++i) {
+                piece[i] = make_uint4(0, 0, 0, 0);
+                if (live && n - off + 8 * i < p.N && (i < 4 || off > 0)) piece[i] = at[i];
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last group's copy has been read
+        __syncwarp();
+        float* s_bias = reinterpret_cast<float*>(out);         // the same 32 numbers for all lanes, until the result takes their place
+        s_bias[lane] = ep.bias && n + lane < p.N ? ep.bias[b * ep.bias_stride + n + lane] : 0.0f;
+        __syncwarp();
+        const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j;
+        if (ep.z8.values) {
+            F2 v[4][4];
+            float acc[32];
+            tmem_load32(from, acc);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 f = reinterpret_cast<const float4*>(s_bias)[i];
+                v[i / 2][2 * (i & 1)] = add(pair(acc[4 * i], acc[4 * i + 1]), pair(f.x, f.y));
+                v[i / 2][2 * (i & 1) + 1] = add(pair(acc[4 * i + 2], acc[4 * i + 3]), pair(f.z, f.w));
+            }
+            const uint32_t s = scale_byte<H>(max(max(top_bits(v[0]), top_bits(v[1])), max(top_bits(v[2]), top_bits(v[3]))));
+            const F2 inverse = both(scale_inverse(s));
+            Oct8 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                F2 t[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) t[k] = to8(v[i][k], inverse);
+                q[i] = pack8(t);
+            }
+            if (live) {
+                int8_t* to = ep.z8.values + b * ep.z8.stride + row * ep.z8.ld;
+                if (n + 32 <= p.N) {
+                    uint4* w = reinterpret_cast<uint4*>(to + n);
+                    w[0] = make_uint4(q[0].w[0], q[0].w[1], q[1].w[0], q[1].w[1]);
+                    w[1] = make_uint4(q[2].w[0], q[2].w[1], q[3].w[0], q[3].w[1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (n + 8 * i < p.N) store_oct8(to, n + 8 * i, p.N, q[i]);
+                }
+                ep.z8.scales[b * ep.z8.scale_stride + row * ep.z8.scale_ld + n / kBlock8] = static_cast<uint8_t>(s);
+            }
+        }
+        // (the accumulator is read again: tensor memory is faster than registers are plenty)
+        uint32_t w[16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float acc[16];
+            tmem_load16(from + 16 * h, acc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 f = reinterpret_cast<const float4*>(s_bias)[4 * h + i];
+                F2 lo = activate<ACT>(add(pair(acc[4 * i], acc[4 * i + 1]), pair(f.x, f.y)));
+                F2 hi = activate<ACT>(add(pair(acc[4 * i + 2], acc[4 * i + 3]), pair(f.z, f.w)));
+                if (add_residual) {
+                    const int k = 2 * h + i / 2;
+                    const Oct o = ALIGNED ? Oct{{piece[k].x, piece[k].y, piece[k].z, piece[k].w}} : cut(piece[k], piece[k + !ALIGNED], off);
+                    lo = add(lo, Elem<H>::up2(o.w[2 * (i & 1)]));
+                    hi = add(hi, Elem<H>::up2(o.w[2 * (i & 1) + 1]));
+                }
+                w[8 * h + 2 * i] = Elem<H>::down2(lo);
+                w[8 * h + 2 * i + 1] = Elem<H>::down2(hi);
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(out + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tma_store(map_out, out, n, m0 + quarter * 32, static_cast<int>(b));
+    }
+}
+
 // 16 whole columns for a warp whose lanes are all inside: no predicates, residuals fetched beforehand.
 // Addresses are a base that is the same for the warp and a lane's 32-bit offset.
 template <typename H, int ACT>
 __device__ __forceinline__ void emit_full(const Epilogue& ep, float (&v)[16], const uint16_t (&res)[16], char* out, int8_t* q, uint8_t* s,
                                           uint32_t lane_out, uint32_t lane_q, bool first, float bias) {
+    F2 y[8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += bias;
+    for (int i = 0; i < 8; ++i) y[i] = add(pair(v[2 * i], v[2 * i + 1]), both(bias));
     if (q) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
-            (q + i * ep.z8.ld)[lane_q] = static_cast<int8_t>(to8(v[i], scale_inverse(sb)).bits() & 255u);
-            if (first) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
+        for (int i = 0; i < 8; ++i) {
+            float lo, hi;
+            split(y[i], lo, hi);
+            const uint32_t s0 = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(lo) & 0x7fffffffu));
+            const uint32_t s1 = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(hi) & 0x7fffffffu));
+            (q + 2 * i * ep.z8.ld)[lane_q] = static_cast<int8_t>(byte8(lo, scale_inverse(s0)));
+            (q + (2 * i + 1) * ep.z8.ld)[lane_q] = static_cast<int8_t>(byte8(hi, scale_inverse(s1)));
+            if (first) {
+                s[2 * i * ep.z8.scale_ld] = static_cast<uint8_t>(s0);
+                s[(2 * i + 1) * ep.z8.scale_ld] = static_cast<uint8_t>(s1);
+            }
         }
     }
+    const bool residual = ep.residual.data != nullptr;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = activate<ACT>(v[i]);
-    if (ep.residual.data) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += Elem<H>::up(res[i]);
+    for (int i = 0; i < 8; ++i) {
+        y[i] = activate<ACT>(y[i]);
+        if (residual) y[i] = add(y[i], pair(Elem<H>::up(res[2 * i]), Elem<H>::up(res[2 * i + 1])));
+        const uint32_t w = Elem<H>::down2(y[i]);
+        *reinterpret_cast<uint16_t*>(out + 2 * i * ep.out.ld * 2 + lane_out) = static_cast<uint16_t>(w & 0xffffu);
+        *reinterpret_cast<uint16_t*>(out + (2 * i + 1) * ep.out.ld * 2 + lane_out) = static_cast<uint16_t>(w >> 16);
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint16_t*>(out + i * ep.out.ld * 2 + lane_out) = Elem<H>::down(v[i]);
 }
 
 // One tile's accumulator to the output, or (split k) to this block's part in shared memory.  The two warps of a
@@ -311,7 +457,7 @@ __device__ __forceinline__ void join_parts(const Problem& p, float* part, int64_
 }
 template <typename H, Mode MODE, typename F>
 __device__ __forceinline__ void with_activation(int act, F&& f) {
-    if constexpr (MODE == kForward) {
+    if constexpr (MODE == kForward || MODE == kForwardRows) {
         if (act == PG_ACT_GELU) f(std::integral_constant<int, PG_ACT_GELU>{});
         else if (act == PG_ACT_SILU) f(std::integral_constant<int, PG_ACT_SILU>{});
         else if (act == PG_ACT_RELU) f(std::integral_constant<int, PG_ACT_RELU>{});
@@ -339,8 +485,7 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t scale2, uint32_t& lo
 }
 template <typename H>
 __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
-    const float f = scale_value(s);
-    return Elem<H>::down2(f, f);
+    return Elem<H>::down2(both(scale_value(s)));
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -348,14 +493,14 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 // 8-bit A.  Every wait ends: it is for work that this block has already started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
 template <typename H, Mode MODE>
-__global__ void __launch_bounds__(MODE == kWeightGrad8 ? 512 : 384, 1)
-product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Problem p) {
+__global__ void __launch_bounds__(kThreads<MODE>, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+               const __grid_constant__ Problem p) {
     extern __shared__ uint8_t s_raw[];
     __shared__ Shared sh;
-    constexpr bool kAMn = MODE != kForward, kBMn = MODE == kWeightGrad || MODE == kWeightGrad8;
-    constexpr bool kFp32 = kBMn;
+    constexpr bool kAMn = kAMnMajor<MODE>, kBMn = kBMnMajor<MODE>, kFp32 = kWeightGrads<MODE>;
     uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
-    const int b_bytes = p.BN * kBK * 2;
+    const int b_bytes = (kBMn ? (p.BN + 63) / 64 * 64 : p.BN) * kBK * 2;
     const int stage_bytes = kABytes + b_bytes + (MODE == kWeightGrad8 ? kRawBytes : 0);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
@@ -367,7 +512,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&sh.summed[i], 1);
-            bar_init(&sh.drained[i], 8);
+            bar_init(&sh.drained[i], kEpilogueWarps<MODE>);
         }
         bar_init(&sh.last, 1);
         sh.gave_up = 0;
@@ -412,7 +557,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 uint8_t* bt = a + kABytes;
                 const int k0 = kb * kBK;
                 bar_expect(&sh.loaded[s], (MODE == kWeightGrad8 ? kRawBytes : kABytes) + b_bytes);
-                if constexpr (MODE == kForward) {
+                if constexpr (!kAMn) {
                     tma_load(a, &map_a, k0, m0, ba, &sh.loaded[s]);
                 } else if constexpr (MODE == kWeightGrad8) {
                     tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.loaded[s]);
@@ -458,7 +603,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             mma_commit(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
         }
-    } else if (warp >= 4 && warp < 12) {
+    } else if (warp >= 4 && warp < 4 + kEpilogueWarps<MODE>) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         int done = 0;
         for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
@@ -469,7 +614,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
-            with_activation<H, MODE>(p.ep.activation, [&](auto act) {
+            if constexpr (kTokenRows<MODE>) {
+                uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutBytes;
+                with_activation<H, MODE>(p.ep.activation, [&](auto act) {
+                    if (p.residual_aligned)
+                        empty_rows<H, decltype(act)::value, true>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane);
+                    else
+                        empty_rows<H, decltype(act)::value, false>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane);
+                });
+            } else with_activation<H, MODE>(p.ep.activation, [&](auto act) {
                 empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0, n0,
                                                            half, quarter, lane);
             });
@@ -477,6 +630,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.drained[acc]);
         }
+        if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (MODE == kWeightGrad8 && warp >= 12) {
         // thread: row k = r of the stage, 64 of its 128 values (two blocks).  The 16-byte pieces are taken in
         // an order that puts the 8 threads of a shared-memory phase on different banks, reading and writing.
@@ -531,7 +685,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
     }
 
-    if (p.splits > 1) {
+    if (!kTokenRows<MODE> && p.splits > 1) {
         __syncwarp();
         cooperative_groups::this_cluster().sync();
         if (warp >= 4 && warp < 12 && !*gave_up) {
@@ -564,14 +718,9 @@ align_rows_kernel(const uint16_t* __restrict__ src, int64_t src_ld, int64_t src_
     const int64_t row = at / chunks;
     const int col = static_cast<int>(at - row * chunks) * 8;
     const int64_t b = row / rows, r = row - b * rows;
-    const uint16_t* p = src + b * src_stride + r * src_ld + col;
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = col + 2 * i < cols ? p[2 * i] : 0, hi = col + 2 * i + 1 < cols ? p[2 * i + 1] : 0;
-        w[i] = lo | hi << 16;
-    }
-    *reinterpret_cast<uint4*>(dst + row * dst_ld + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    const uint16_t* p = src + b * src_stride + r * src_ld;
+    const Oct o = octet<1>(load_oct<1>(p, col, cols), p, col, cols);
+    *reinterpret_cast<uint4*>(dst + row * dst_ld + col) = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
 }
 
 // ------------------------------------------------------------------ host
@@ -588,8 +737,8 @@ EncodeFn encoder() {
     return fn;
 }
 
-// An operand as TMA sees it: `rows` rows of `cols` elements per worker, boxes of box_rows x 128 bytes (8-bit: no swizzle).
-bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_rows) {
+// A matrix as TMA sees it: `rows` rows of `cols` elements per worker, boxes of box_rows x box_bytes, swizzled (8-bit: not).
+bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_bytes, int box_rows) {
     EncodeFn fn = encoder();
     if (!fn) return false;
     const int size = eight ? 1 : 2;
@@ -599,10 +748,10 @@ bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64
     const int64_t stride = batch > 1 && !shared ? m.stride : ld * rows;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(shared ? 1 : batch)};
     const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * size), static_cast<cuuint64_t>(stride * size)};
-    const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / size), static_cast<cuuint32_t>(box_rows), 1};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / size), static_cast<cuuint32_t>(box_rows), 1};
     const cuuint32_t one[3] = {1, 1, 1};
     const CUtensorMapDataType type = eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    return fn(&map, type, 3, m.data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+    return fn(&map, type, 3, m.data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -633,7 +782,7 @@ int aligned_operand(pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, uin
 }
 
 template <typename H, Mode MODE>
-int launch(const CUtensorMap& a, const CUtensorMap& b, const Problem& p, cudaStream_t st) {
+int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const Problem& p, int smem, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
@@ -644,8 +793,8 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Problem& p, cudaStr
     if (!fine) return PG_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.splits > 1 ? p.tiles * p.splits : std::min<int64_t>(p.tiles, kSMs)));
-    cfg.blockDim = dim3(MODE == kWeightGrad8 ? 512 : 384);
-    cfg.dynamicSmemBytes = p.stages * (kABytes + p.BN * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0)) + 1024;
+    cfg.blockDim = dim3(kThreads<MODE>);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -653,7 +802,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Problem& p, cudaStr
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE>, a, b, p) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE>, a, b, out, p) != cudaSuccess) {
         cudaGetLastError();
         return PG_ERR_CUDA;
     }
@@ -663,8 +812,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Problem& p, cudaStr
 template <Mode MODE>
 int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const pg_matrix& A, const pg_matrix& B, const Epilogue& ep, const pg_matrix8* a8,
                 cudaStream_t st) {
-    constexpr bool kBMn = MODE == kWeightGrad || MODE == kWeightGrad8;
-    constexpr bool kAMn = MODE != kForward;
+    constexpr bool kBMn = kBMnMajor<MODE>, kAMn = kAMnMajor<MODE>, kRows = kTokenRows<MODE>;
     Problem p = {};
     p.ep = ep;
     p.M = static_cast<int>(M);
@@ -672,33 +820,48 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     p.K = static_cast<int>(K);
     p.batch = static_cast<int>(batch);
     p.m_tiles = static_cast<int>((M + kBM - 1) / kBM);
-    // the fewest column tiles, and those as narrow as they cover N; a tile that TMA loads in boxes of 64
-    // columns (MN-major) has a multiple of them
-    const int unit = kBMn ? 64 : 16;
-    p.n_tiles = static_cast<int>((N + 255) / 256);
-    p.BN = static_cast<int>(((N + p.n_tiles - 1) / p.n_tiles + unit - 1) / unit * unit);
+    // Widths of a tile: multiples of 16 columns, of 32 where a thread holds blocks of 32, of 64 where TMA loads boxes of
+    // 64 columns and every other one is stored.  The one that covers N with the fewest columns, a tile's start and
+    // end counted as 64 more; the widest of equals.
+    const int unit = kWeightGrads<MODE> ? 64 : kRows ? 32 : 16;
+    int64_t least = 0;
+    for (int w = 256; w >= unit && w >= std::min<int64_t>(N, kRows || kWeightGrads<MODE> ? 128 : 16); w -= unit) {
+        const int64_t tiles = (N + w - 1) / w, cost = tiles * (w + 64);
+        if (least == 0 || cost < least) {
+            least = cost;
+            p.BN = w;
+        }
+    }
     p.n_tiles = static_cast<int>((N + p.BN - 1) / p.BN);
     p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
     p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
     p.splits = 1;
-    while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
-    const int stage = kABytes + p.BN * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
-    p.stages = std::min(kMaxStages, (kSmemBytes - 3072) / stage);
+    if (!kRows)
+        while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
+    const int stage = kABytes + (kBMn ? (p.BN + 63) / 64 * 64 : p.BN) * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    const int rest = kRows ? kRowWarps * kOutBytes : 0;
+    p.stages = std::min(kMaxStages, (kSmemBytes - 3072 - rest) / stage);
     p.a_shared = A.stride == 0;
     p.b_shared = B.stride == 0;
+    p.residual_aligned = access_width({&ep.residual}, batch) == 8;
     if (a8) {
         p.scales = a8->scales;
         p.scale_ld = a8->scale_ld;
         p.scale_stride = a8->scale_stride;
     }
-    CUtensorMap map_a = {}, map_b = {};
+    CUtensorMap map_a = {}, map_b = {}, map_out = {};
     if (K > 0) {
-        const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, kAMn ? kBK : kBM) &&
-                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, kBMn ? kBK : p.BN);
+        const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
+                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : p.BN) &&
+                          (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
-    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE>(map_a, map_b, p, st) : launch<__half, MODE>(map_a, map_b, p, st);
+    const int smem = p.stages * stage + rest + 1024;
+    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE>(map_a, map_b, map_out, p, smem, st) : launch<__half, MODE>(map_a, map_b, map_out, p, smem, st);
 }
+
+// Tokens from which they become the accumulator's lanes.
+constexpr int kRowTokens = 64;
 
 int current_device() {
     int d = 0;
@@ -743,7 +906,10 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     int rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
-    return rc != PG_OK ? rc : run_product<kForward>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
+    if (rc != PG_OK) return rc;
+    if (a.tokens > kRowTokens && aligned(a.y, a.batch, a.tokens))
+        return run_product<kForwardRows>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
+    return run_product<kForward>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
 
 int pg_linear_input_grad_workspace_bytes(const pg_input_grad_args* args, size_t* bytes_out) {
@@ -771,7 +937,10 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     int rc = aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st);
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
-    return rc != PG_OK ? rc : run_product<kInputGrad>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
+    if (rc != PG_OK) return rc;
+    if (a.tokens > kRowTokens && aligned(a.dx, a.batch, a.tokens))
+        return run_product<kInputGradRows>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
+    return run_product<kInputGrad>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
 
 int pg_linear_weight_grad_workspace_bytes(const pg_weight_grad_args* args, size_t* bytes_out) {

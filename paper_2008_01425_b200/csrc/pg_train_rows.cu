@@ -1,6 +1,7 @@
 // Row-wise training operators: the norm and its gradient, the activation's gradient, the 8-bit form.
 // All of them are bound by memory: every element is read once, held in registers as fp32, and
-// written once.
+// written once.  A lane holds octets (eight neighbouring elements), so four lanes make a block of the 8-bit form
+// whatever the alignment of the rows is; only the width of the accesses goes by that.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -14,152 +15,130 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// ---------------------------------------------------------------- rows in registers
-// A group of T threads holds one row in registers: chunk c of a thread is the V neighbouring
-// elements at (c T + t) V, so a warp reads consecutive addresses whatever V is, and a block of the
-// 8-bit form lies in 32 / V neighbouring lanes.
-template <int T>
-__device__ __forceinline__ float group_sum(float v, float* s_part) {
+// A worker's gains for an octet; `wide`: 16-byte addresses.
+__device__ __forceinline__ void load_gain(const float* gain, bool wide, int col, int cols, F2 (&g)[4]) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (T > 32) {        // one group per block
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < T / 32; ++w) v += s_part[w];
-    }
-    return v;
-}
-// All loads of a row, with no branch between them; only a row whose end cuts a chunk short takes a second look.
-template <int V, int C, int T>
-__device__ __forceinline__ void read_row(const void* base, int64_t at, int cols, int t, Raw<V> (&r)[C]) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col = (c * T + t) * V;
-        r[c] = Raw<V>{};
-        if (col + V <= cols) r[c] = load_raw<V>(base, at + col);
-    }
-    if (V > 1 && cols % V != 0) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * T + t) * V;
-            if (col < cols && col + V > cols) r[c] = load_raw_end<V>(base, at + col, cols - col);
-        }
-    }
-}
-template <typename H, int V, int C, int T>
-__device__ __forceinline__ void write_row(void* base, int64_t at, int cols, int t, const float (&v)[C][V]) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col = (c * T + t) * V;
-        if (col < cols) store16n<H, V>(base, at + col, cols - col, v[c]);
-    }
-}
-// A worker's gains for a thread's columns; `wide`: V = 8 and 16-byte addresses.
-template <int V>
-__device__ __forceinline__ void read_gain(const float* gain, bool wide, int col, int cols, float (&g)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) g[i] = 1.0f;
+    for (int i = 0; i < 4; ++i) g[i] = both(1.0f);
     if (!gain) return;
-    if (V == 8 && wide) {
-        if (col + V <= cols) {
-            const float4 lo = *reinterpret_cast<const float4*>(gain + col), hi = *reinterpret_cast<const float4*>(gain + col + 4);
-            const float u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (wide && col + 8 <= cols) {
+        const float4 lo = *reinterpret_cast<const float4*>(gain + col), hi = *reinterpret_cast<const float4*>(gain + col + 4);
+        g[0] = pair(lo.x, lo.y);
+        g[1] = pair(lo.z, lo.w);
+        g[2] = pair(hi.x, hi.y);
+        g[3] = pair(hi.z, hi.w);
+    } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = u[i];
-            return;
-        }
+        for (int i = 0; i < 4; ++i)
+            g[i] = pair(col + 2 * i < cols ? gain[col + 2 * i] : 0.0f, col + 2 * i + 1 < cols ? gain[col + 2 * i + 1] : 0.0f);
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (col + i < cols) g[i] = gain[col + i];
 }
 __device__ __forceinline__ bool wide_gain(const float* gain) { return reinterpret_cast<uintptr_t>(gain) % 16 == 0; }
-// The 8-bit form of a row held in registers, and back in v the values it stands for.
-template <typename H, int V, int C, int T>
-__device__ __forceinline__ void row_to_8(float (&v)[C][V], int cols, int t, int8_t* values, uint8_t* scales) {
+
+// The 8-bit form of an octet, stored, and back in v the values it stands for.  All lanes of a warp take part.
+template <typename H>
+__device__ __forceinline__ void octet_to_8(F2 (&v)[4], int8_t* row, uint8_t* scales, int col, int cols) {
+    const uint32_t s = scale_byte<H>(block_top(top_bits(v)));
+    const F2 inverse = both(scale_inverse(s)), value = both(scale_value(s));
+    F2 t[4];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col = (c * T + t) * V;
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[c][i]) & 0x7fffffffu);
-        top = block_top<V>(top);
-        const uint32_t s = scale_byte<H>(top);
-        const float inverse = scale_inverse(s), value = scale_value(s);
-        Q8 q[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            q[i] = to8(v[c][i], inverse);
-            v[c][i] = q[i].value(value);
-        }
-        if (col < cols) {
-            store8n<V>(values + col, cols - col, q);
-            if (col % kBlock8 == 0) scales[col / kBlock8] = static_cast<uint8_t>(s);
-        }
+    for (int i = 0; i < 4; ++i) {
+        t[i] = to8(v[i], inverse);
+        v[i] = value8(t[i], value);
+    }
+    if (col < cols) {
+        store_oct8(row, col, cols, pack8(t));
+        if (col % kBlock8 == 0) scales[col / kBlock8] = static_cast<uint8_t>(s);
     }
 }
 
 // ---------------------------------------------------------------- norm
-// Block: kGroups rows of one worker.  The row is read once; the sum of squares comes from the registers.
-template <typename H, int V, int C, int T>
+// T threads hold one row, C octets each; a block has 256 / T rows of one worker, at least one.  The row is read
+// once; the sum of squares comes from the registers.
+template <typename H, int W, int WO, int C, int T>
 __global__ void __launch_bounds__(T > 32 ? T : 256)
 norm_kernel(const pg_norm_args a) {
     __shared__ float s_part[32];
+    __shared__ __align__(16) float s_gain[T > 32 ? 4 : C * 256];
     const int t = T > 32 ? threadIdx.x : threadIdx.x & 31;
     const int64_t b = blockIdx.y;
     const int tok = T > 32 ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (tok >= a.tokens) return;                       // the whole group
-    float v[C][V];
-    {
-        Raw<V> x[C], r[C];
-        read_row<V, C, T>(a.x.data, b * a.x.stride + tok * a.x.ld, a.cols, t, x);
-        if (a.residual.data) read_row<V, C, T>(a.residual.data, b * a.residual.stride + tok * a.residual.ld, a.cols, t, r);
+    const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
+    if constexpr (T == 32) {                           // eight rows share the gains
 #pragma unroll
-        for (int c = 0; c < C; ++c) widen<H, V>(x[c], v[c]);
+        for (int c = 0; c < C; ++c) {
+            const int col = c * 256 + threadIdx.x;
+            s_gain[col] = gain && col < a.cols ? gain[col] : 1.0f;
+        }
+        __syncthreads();
+    }
+    if (tok >= a.tokens) return;                       // the whole group
+    F2 v[C][4];
+    {
+        const uint16_t* x_row = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + tok * a.x.ld;
+        const uint16_t* r_row = static_cast<const uint16_t*>(a.residual.data) + b * a.residual.stride + tok * a.residual.ld;
+        Piece<W> x[C], r[C];
+        load_row<W, C, T>(x_row, a.cols, t, x);
+        if (a.residual.data) load_row<W, C, T>(r_row, a.cols, t, r);
+#pragma unroll
+        for (int c = 0; c < C; ++c) widen<H>(octet<W>(x[c], x_row, (c * T + t) * 8, a.cols), v[c]);
         if (a.residual.data) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float w[V];
-                widen<H, V>(r[c], w);
+                F2 w[4];
+                widen<H>(octet<W>(r[c], r_row, (c * T + t) * 8, a.cols), w);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[c][i] += w[i];
+                for (int i = 0; i < 4; ++i) v[c][i] = add(v[c][i], w[i]);
             }
         }
     }
-    float sum = 0.0f;
+    F2 sums = both(0.0f);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum = fmaf(v[c][i], v[c][i], sum);
-    sum = group_sum<T>(sum, s_part);
+        for (int i = 0; i < 4; ++i) sums = fma(v[c][i], v[c][i], sums);
+    float sum = sum2(sums);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if constexpr (T > 32) {
+        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < T / 32; ++w) sum += s_part[w];
+    }
     const float rstd = rsqrtf(sum / a.cols + a.eps);
     if (a.rstd && t == 0) a.rstd[b * a.tokens + tok] = rstd;
-    if (a.h.data) write_row<H, V, C, T>(a.h.data, b * a.h.stride + tok * a.h.ld, a.cols, t, v);
-    if (a.h8.values) {
-        float w[C][V];
+    if (a.h.data) {
+        uint16_t* h = static_cast<uint16_t*>(a.h.data) + b * a.h.stride + tok * a.h.ld;
 #pragma unroll
         for (int c = 0; c < C; ++c)
+            if ((c * T + t) * 8 < a.cols) store_oct<H, WO>(h, (c * T + t) * 8, a.cols, v[c]);
+    }
+    if (a.h8.values) {
+        int8_t* q = a.h8.values + b * a.h8.stride + tok * a.h8.ld;
+        uint8_t* s = a.h8.scales + b * a.h8.scale_stride + tok * a.h8.scale_ld;
 #pragma unroll
-            for (int i = 0; i < V; ++i) w[c][i] = v[c][i];
-        row_to_8<H, V, C, T>(w, a.cols, t, a.h8.values + b * a.h8.stride + tok * a.h8.ld,
-                             a.h8.scales + b * a.h8.scale_stride + tok * a.h8.scale_ld);
+        for (int c = 0; c < C; ++c) {
+            F2 w[4] = {v[c][0], v[c][1], v[c][2], v[c][3]};
+            octet_to_8<H>(w, q, s, (c * T + t) * 8, a.cols);
+        }
     }
     if (!a.y.data && !a.y8.values) return;
-    const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
+    const bool wide = wide_gain(gain);
+    uint16_t* y = a.y.data ? static_cast<uint16_t*>(a.y.data) + b * a.y.stride + tok * a.y.ld : nullptr;
+    int8_t* q = a.y8.values + b * a.y8.stride + tok * a.y8.ld;
+    uint8_t* s = a.y8.scales + b * a.y8.scale_stride + tok * a.y8.scale_ld;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        float g[V];
-        read_gain<V>(gain, wide_gain(gain), (c * T + t) * V, a.cols, g);
+        const int col = (c * T + t) * 8;
+        F2 g[4];
+        if constexpr (T == 32) load_gain(s_gain, true, col, C * 256, g);
+        else load_gain(gain, wide, col, a.cols, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[c][i] *= rstd * g[i];
+        for (int i = 0; i < 4; ++i) v[c][i] = mul(v[c][i], mul(both(rstd), g[i]));
+        if (a.y8.values) octet_to_8<H>(v[c], q, s, col, a.cols);
+        if (y && col < a.cols) store_oct<H, WO>(y, col, a.cols, v[c]);
     }
-    if (a.y8.values)
-        row_to_8<H, V, C, T>(v, a.cols, t, a.y8.values + b * a.y8.stride + tok * a.y8.ld,
-                             a.y8.scales + b * a.y8.scale_stride + tok * a.y8.scale_ld);
-    if (a.y.data) write_row<H, V, C, T>(a.y.data, b * a.y.stride + tok * a.y.ld, a.cols, t, v);
 }
 
 // ---------------------------------------------------------------- norm gradient
@@ -168,8 +147,8 @@ norm_kernel(const pg_norm_args a) {
 // read stays packed and is widened again for the second use: dx needs the row's dot product first.
 // partial[b][k][cols]: what block k of worker b added up; summed in that order by the second kernel.
 constexpr int kGradBlock = 128;
-template <typename H, int V, int C, int T, int R, bool EIGHT>
-__global__ void __launch_bounds__(T > 32 ? T : kGradBlock)
+template <typename H, int W, int WO, int C, int T, int R, int BLOCKS, bool EIGHT>
+__global__ void __launch_bounds__(T > 32 ? T : kGradBlock, BLOCKS)
 norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int rows_per_group) {
     extern __shared__ float s_sum[];                   // warps x cols, T == 32 only
     __shared__ float s_part[2][R][32];
@@ -180,74 +159,79 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
     const int64_t r0 = static_cast<int64_t>(group) * rows_per_group;
     const int64_t r1 = min(static_cast<int64_t>(a.tokens), r0 + rows_per_group);
     const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
-    float sum_dg[C][V], g[C][V];
+    F2 sum_dg[C][4], g[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        read_gain<V>(gain, wide_gain(gain), (c * T + t) * V, a.cols, g[c]);
+        load_gain(gain, wide_gain(gain), (c * T + t) * 8, a.cols, g[c]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum_dg[c][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) sum_dg[c][i] = both(0.0f);
     }
     int flip = 0;
     for (int64_t r = r0; r < r1; r += R, flip ^= 1) {
-        Raw<V> dy_raw[R][C], h_raw[R][C], dh_raw[R][C];
-        Raw8<V> q_raw[R][C];
+        Oct dy_raw[R][C], h_raw[R][C], dh_raw[R][C];
+        Oct8 q_raw[R][C];
         uint32_t q_scale[R][C];
         float rstd[R];
+        Piece<W> dy_piece[R][C], h_piece[R][C], dh_piece[R][C];
+        auto row_of = [&](const pg_matrix& m, int k) {         // a row past the last one reads the last one again, and counts for nothing
+            return static_cast<const uint16_t*>(m.data) + b * m.stride + min(r + k, r1 - 1) * m.ld;
+        };
 #pragma unroll
-        for (int k = 0; k < R; ++k) {                  // a row past the last one reads the last one again, and counts for nothing
+        for (int k = 0; k < R; ++k) {
             const int64_t row = min(r + k, r1 - 1);
-            read_row<V, C, T>(a.dy.data, b * a.dy.stride + row * a.dy.ld, a.cols, t, dy_raw[k]);
+            load_row<W, C, T>(row_of(a.dy, k), a.cols, t, dy_piece[k]);
             if constexpr (EIGHT) {
                 const int8_t* q = a.h8.values + b * a.h8.stride + row * a.h8.ld;
                 const uint8_t* s = a.h8.scales + b * a.h8.scale_stride + row * a.h8.scale_ld;
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    const int col = (c * T + t) * V;
-                    q_raw[k][c] = Raw8<V>{};
-                    q_scale[k][c] = 0;
-                    if (col + V <= a.cols) q_raw[k][c] = load_raw8<V>(q + col);
-                    if (col < a.cols) q_scale[k][c] = s[col / kBlock8];
-                }
-                if (V > 1 && a.cols % V != 0) {
-#pragma unroll
-                    for (int c = 0; c < C; ++c) {
-                        const int col = (c * T + t) * V;
-                        if (col < a.cols && col + V > a.cols) q_raw[k][c] = load_raw8_end<V>(q + col, a.cols - col);
-                    }
+                    const int col = (c * T + t) * 8;
+                    q_raw[k][c] = load_oct8(q, col, a.cols);
+                    q_scale[k][c] = col < a.cols ? s[col / kBlock8] : 0;
                 }
             } else {
-                read_row<V, C, T>(a.h.data, b * a.h.stride + row * a.h.ld, a.cols, t, h_raw[k]);
+                load_row<W, C, T>(row_of(a.h, k), a.cols, t, h_piece[k]);
             }
-            if (a.dh.data) read_row<V, C, T>(a.dh.data, b * a.dh.stride + row * a.dh.ld, a.cols, t, dh_raw[k]);
+            if (a.dh.data) load_row<W, C, T>(row_of(a.dh, k), a.cols, t, dh_piece[k]);
             rstd[k] = a.rstd[b * a.tokens + row];
         }
-        // u of a chunk; past the end of the row it is zero, as dy is
-        auto unit = [&](int k, int c, float (&u)[V]) {
-            if constexpr (EIGHT) widen8<V>(q_raw[k][c], scale_value(q_scale[k][c]), u);
-            else widen<H, V>(h_raw[k][c], u);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                u[i] *= rstd[k];
-                if (EIGHT && (c * T + t) * V + i >= a.cols) u[i] = 0.0f;     // not NaN, where the last block's scale says so
+        for (int k = 0; k < R; ++k)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * T + t) * 8;
+                dy_raw[k][c] = octet<W>(dy_piece[k][c], row_of(a.dy, k), col, a.cols);
+                if constexpr (!EIGHT) h_raw[k][c] = octet<W>(h_piece[k][c], row_of(a.h, k), col, a.cols);
+                if (a.dh.data) dh_raw[k][c] = octet<W>(dh_piece[k][c], row_of(a.dh, k), col, a.cols);
             }
+        auto unit = [&](int k, int c, F2 (&u)[4]) {
+            if constexpr (EIGHT) widen8(q_raw[k][c], scale_value(q_scale[k][c]), u);
+            else widen<H>(h_raw[k][c], u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = mul(u[i], both(rstd[k]));
         };
         float dot[R];
 #pragma unroll
-        for (int k = 0; k < R; ++k) dot[k] = 0.0f;
+        for (int k = 0; k < R; ++k) {
+            F2 d = both(0.0f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                float dy[V], u[V];
-                widen<H, V>(dy_raw[k][c], dy);
+            for (int c = 0; c < C; ++c) {
+                F2 dy[4], u[4];
+                widen<H>(dy_raw[k][c], dy);
                 unit(k, c, u);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float w = dy[i] * u[i];
-                    if (r + k < r1) sum_dg[c][i] += w;
-                    dot[k] = fmaf(w, g[c][i], dot[k]);
+                for (int i = 0; i < 4; ++i) {
+                    F2 w = mul(dy[i], u[i]);
+                    if (EIGHT && (c * T + t) * 8 + 2 * i + 1 >= a.cols) {       // values past the row's end are not the block's NaN
+                        float lo, hi;
+                        split(w, lo, hi);
+                        w = pair((c * T + t) * 8 + 2 * i < a.cols ? lo : 0.0f, 0.0f);
+                    }
+                    if (r + k < r1) sum_dg[c][i] = add(sum_dg[c][i], w);
+                    d = fma(w, g[c][i], d);
                 }
             }
+            dot[k] = sum2(d);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
@@ -266,22 +250,21 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
             }
         }
 #pragma unroll
-        for (int k = 0; k < R; ++k) dot[k] /= a.cols;
+        for (int k = 0; k < R; ++k) {
+            const F2 minus = both(-dot[k] / a.cols), by = both(rstd[k]);
+            uint16_t* out = static_cast<uint16_t*>(a.dx.data) + b * a.dx.stride + (r + k) * a.dx.ld;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * T + t) * V;
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                float dy[V], u[V], dx[V];
-                widen<H, V>(dy_raw[k][c], dy);
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * T + t) * 8;
+                F2 dy[4], u[4], dx[4];
+                widen<H>(dy_raw[k][c], dy);
                 unit(k, c, u);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] = 0.0f;
-                if (a.dh.data) widen<H, V>(dh_raw[k][c], dx);
+                for (int i = 0; i < 4; ++i) dx[i] = both(0.0f);
+                if (a.dh.data) widen<H>(dh_raw[k][c], dx);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] += rstd[k] * (dy[i] * g[c][i] - u[i] * dot[k]);
-                if (col < a.cols && r + k < r1)
-                    store16n<H, V>(a.dx.data, b * a.dx.stride + (r + k) * a.dx.ld + col, a.cols - col, dx);
+                for (int i = 0; i < 4; ++i) dx[i] = fma(by, fma(u[i], minus, mul(dy[i], g[c][i])), dx[i]);
+                if (col < a.cols && r + k < r1) store_oct<H, WO>(out, col, a.cols, dx);
             }
         }
     }
@@ -291,9 +274,12 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int col = (c * T + t) * V + i;
-            if (col < a.cols) mine[col] = sum_dg[c][i];
+        for (int i = 0; i < 4; ++i) {
+            const int col = (c * T + t) * 8 + 2 * i;
+            float lo, hi;
+            split(sum_dg[c][i], lo, hi);
+            if (col < a.cols) mine[col] = lo;
+            if (col + 1 < a.cols) mine[col + 1] = hi;
         }
     if constexpr (T == 32) {
         __syncthreads();
@@ -327,135 +313,108 @@ sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, floa
 }
 
 // ---------------------------------------------------------------- activation gradient
-// A block takes a strip of 32 V columns and a share of a worker's tokens; 8 rows at a time, one per
+// A block takes a strip of 256 columns and a share of a worker's tokens; 8 rows at a time, one per
 // warp, four times that in flight.  Column sums stay in registers, are joined over the warps in shared
 // memory and over the blocks of a cluster (the shares of one strip) through distributed shared memory, in
 // a fixed order.
-template <typename H, int V, int ACT>
+constexpr int kStrip = 256, kStripRows = 4;
+template <typename H, int W, int WO, int ACT>
 __global__ void __launch_bounds__(256, 3)
 activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
-    __shared__ float s_sum[8][32 * V];
+    __shared__ float s_sum[8][kStrip];
     const int64_t b = blockIdx.y;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int splits = gridDim.z, split = blockIdx.z;
-    const int col = (blockIdx.x * 32 + lane) * V;
-    const int64_t r0 = static_cast<int64_t>(split) * rows_per_block;
-    const int r1 = static_cast<int>(min(static_cast<int64_t>(a.tokens), r0 + rows_per_block));
-    float sum[V];
+    const int splits = gridDim.z, split_at = blockIdx.z;
+    const int col = blockIdx.x * kStrip + lane * 8;
+    const int64_t r0 = static_cast<int64_t>(split_at) * rows_per_block;
+    const int64_t r1 = min(static_cast<int64_t>(a.tokens), r0 + rows_per_block);
+    F2 sum[4];
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-    const void* dy_at = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + col;
-    void* dz_at = a.dz.data ? static_cast<uint16_t*>(a.dz.data) + b * a.dz.stride + col : nullptr;
-    const int8_t* q_at = a.z8.values ? a.z8.values + b * a.z8.stride + col : nullptr;
-    const uint8_t* s_at = a.z8.values ? a.z8.scales + b * a.z8.scale_stride + col / kBlock8 : nullptr;
-    auto one = [&](const Raw<V>& dy_raw, const Raw8<V>& q_raw, uint32_t scale, float (&dy)[V]) {
-        widen<H, V>(dy_raw, dy);
-        if (q_at) {
-            float z[V];
-            widen8<V>(q_raw, scale_value(scale), z);
+    for (int i = 0; i < 4; ++i) sum[i] = both(0.0f);
+    if (col < a.cols) {
+        const bool eight = a.z8.values != nullptr;
+        const uint16_t* dy_at = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + (r0 + warp) * a.dy.ld;
+        uint16_t* dz_at = a.dz.data ? static_cast<uint16_t*>(a.dz.data) + b * a.dz.stride + (r0 + warp) * a.dz.ld : nullptr;
+        const int8_t* q_at = a.z8.values + b * a.z8.stride + (r0 + warp) * a.z8.ld;
+        const uint8_t* s_at = a.z8.scales + b * a.z8.scale_stride + (r0 + warp) * a.z8.scale_ld + col / kBlock8;
+        for (int64_t r = r0 + warp; r < r1; r += 8 * kStripRows) {              // rows past the end read as zeros
+            Piece<W> d[kStripRows] = {};
+            Oct8 q[kStripRows] = {};
+            uint32_t s[kStripRows] = {};
 #pragma unroll
-            for (int i = 0; i < V; ++i) dy[i] *= slope<ACT>(z[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += dy[i];
-    };
-    if (col + V <= a.cols) {
-        for (int64_t r = r0 + warp; r < r1; r += 32) {      // rows past the end read as zeros
-            Raw<V> d[4] = {};
-            Raw8<V> q[4] = {};
-            uint32_t s[4] = {};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (r + 8 * k < r1) d[k] = load_raw<V>(dy_at, (r + 8 * k) * a.dy.ld);
-            if (q_at) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (r + 8 * k < r1) {
-                        q[k] = load_raw8<V>(q_at + (r + 8 * k) * a.z8.ld);
-                        s[k] = s_at[(r + 8 * k) * a.z8.scale_ld];
+            for (int k = 0; k < kStripRows; ++k)
+                if (r + 8 * k < r1) {
+                    d[k] = load_oct<W>(dy_at + 8 * k * a.dy.ld, col, a.cols);
+                    if (eight) {
+                        q[k] = load_oct8(q_at + 8 * k * a.z8.ld, col, a.cols);
+                        s[k] = s_at[8 * k * a.z8.scale_ld];
                     }
-            }
+                }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float dy[V];
-                one(d[k], q[k], s[k], dy);
-                if (dz_at && r + 8 * k < r1) store16<H, V>(dz_at, (r + 8 * k) * a.dz.ld, dy);
+            for (int k = 0; k < kStripRows; ++k) {
+                F2 dy[4];
+                widen<H>(octet<W>(d[k], dy_at + 8 * k * a.dy.ld, col, r + 8 * k < r1 ? a.cols : 0), dy);
+                if (eight) {
+                    F2 z[4];
+                    widen8(q[k], scale_value(s[k] == 255u ? 255u : min(s[k], 183u)), z);      // 127 * 2^56 is as far from zero as any
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dy[i] = mul(dy[i], slope<ACT>(z[i]));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = add(sum[i], dy[i]);
+                if (dz_at && r + 8 * k < r1) store_oct<H, WO>(dz_at + 8 * k * a.dz.ld, col, a.cols, dy);
             }
-        }
-    } else if (col < a.cols) {             // the lane that the row's end cuts short
-        const int n = a.cols - col;
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
-            float dy[V];
-            const Raw8<V> q = q_at ? load_raw8_end<V>(q_at + r * a.z8.ld, n) : Raw8<V>{};
-            one(load_raw_end<V>(dy_at, r * a.dy.ld, n), q, q_at ? s_at[r * a.z8.scale_ld] : 0u, dy);
-            if (dz_at) store16n<H, V>(dz_at, r * a.dz.ld, n, dy);
+            dy_at += 8 * kStripRows * a.dy.ld;
+            if (dz_at) dz_at += 8 * kStripRows * a.dz.ld;
+            q_at += 8 * kStripRows * a.z8.ld;
+            s_at += 8 * kStripRows * a.z8.scale_ld;
         }
     }
     if (!a.dbias) return;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s_sum[warp][lane * V + i] = sum[i];
+    for (int i = 0; i < 4; ++i) split(sum[i], s_sum[warp][lane * 8 + 2 * i], s_sum[warp][lane * 8 + 2 * i + 1]);
     __syncthreads();
-    float mine = 0.0f;
     const int at = threadIdx.x;
-    if (at < 32 * V) {
+    float mine = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) mine += s_sum[w][at];
-    }
-    cg::cluster_group cluster = cg::this_cluster();
+    for (int w = 0; w < 8; ++w) mine += s_sum[w][at];
     if (splits > 1) {
+        cg::cluster_group cluster = cg::this_cluster();
         __syncthreads();
-        if (at < 32 * V) s_sum[0][at] = mine;
+        s_sum[0][at] = mine;
         cluster.sync();
-        if (split == 0 && at < 32 * V) {
+        if (split_at == 0)
             for (int k = 1; k < splits; ++k) mine += cluster.map_shared_rank(&s_sum[0][0], k)[at];
-        }
         cluster.sync();
     }
-    const int out_col = blockIdx.x * 32 * V + at;
-    if (split == 0 && at < 32 * V && out_col < a.cols) {
+    const int out_col = blockIdx.x * kStrip + at;
+    if (split_at == 0 && out_col < a.cols) {
         float* o = a.dbias + b * a.dbias_stride + out_col;
         *o = a.accumulate ? *o + mine : mine;
     }
 }
 
 // ---------------------------------------------------------------- checkpoints
-template <typename H, int V, bool WRITE>
+// One thread per octet; a row takes a whole number of blocks of 32 values, so the four lanes of a block are neighbours.
+template <typename H, int W, int WO, bool WRITE>
 __global__ void __launch_bounds__(256)
-checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int chunks) {
-    // one thread per V elements of a row; the lanes of a block of 32 values are neighbours because a
-    // row takes a whole number of blocks (chunks is a multiple of 32 / V)
+checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int octets) {
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t r = at / chunks;
-    const int col = static_cast<int>(at - r * chunks) * V;
+    const int64_t r = at / octets;
+    const int col = static_cast<int>(at - r * octets) * 8;
     const bool live = r < rows && col < a.cols;
     const int64_t b = live ? r / a.tokens : 0, tok = live ? r - b * a.tokens : 0;
-    const int n = a.cols - col;
-    int8_t* values = a.x8.values + b * a.x8.stride + tok * a.x8.ld + col;
-    uint8_t* scale = a.x8.scales + b * a.x8.scale_stride + tok * a.x8.scale_ld + col / kBlock8;
-    float v[V];
+    uint16_t* row = static_cast<uint16_t*>(a.x.data) + b * a.x.stride + tok * a.x.ld;
+    int8_t* q = a.x8.values + b * a.x8.stride + tok * a.x8.ld;
+    uint8_t* s = a.x8.scales + b * a.x8.scale_stride + tok * a.x8.scale_ld;
+    const int cols = live ? a.cols : 0;
+    F2 v[4];
     if constexpr (WRITE) {
-        Q8 q[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = 0.0f;
-        if (live) {
-            const int64_t from = b * a.x.stride + tok * a.x.ld + col;
-            widen<H, V>(n >= V ? load_raw<V>(a.x.data, from) : load_raw_end<V>(a.x.data, from, n), v);
-        }
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-        top = block_top<V>(top);
-        const uint32_t s = scale_byte<H>(top);
-        const float inverse = scale_inverse(s);
-#pragma unroll
-        for (int i = 0; i < V; ++i) q[i] = to8(v[i], inverse);
-        if (live) {
-            store8n<V>(values, n, q);
-            if (col % kBlock8 == 0) *scale = static_cast<uint8_t>(s);
-        }
+        widen<H>(octet<W>(load_oct<W>(row, col, cols), row, col, cols), v);
+        octet_to_8<H>(v, q, s, col, cols);
     } else if (live) {
-        widen8<V>(n >= V ? load_raw8<V>(values) : load_raw8_end<V>(values, n), scale_value(*scale), v);
-        store16n<H, V>(a.x.data, b * a.x.stride + tok * a.x.ld + col, n, v);
+        widen8(load_oct8(q, col, cols), scale_value(s[col / kBlock8]), v);
+        store_oct<H, WO>(row, col, cols, v);
     }
 }
 
@@ -464,41 +423,42 @@ int current_device() {
     return cudaGetDevice(&d) == cudaSuccess ? d : -1;
 }
 
-// Calls f with a compile-time element type and access width.
+// Calls f with a compile-time element type, the width of read accesses and that of written ones.
 template <typename F>
-void with_type(int dtype, int width, F&& f) {
+void with_type(int dtype, int in, int out, F&& f) {
+    using std::integral_constant;
     auto w = [&](auto h) {
         using H = decltype(h);
-        if (width == 8) f(H{}, std::integral_constant<int, 8>{});
-        else if (width == 2) f(H{}, std::integral_constant<int, 2>{});
-        else f(H{}, std::integral_constant<int, 1>{});
+        if (out < 8) f(H{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
+        else if (in == 8) f(H{}, integral_constant<int, 8>{}, integral_constant<int, 8>{});
+        else f(H{}, integral_constant<int, 1>{}, integral_constant<int, 8>{});
     };
     if (dtype == PG_BF16) w(__nv_bfloat16{});
     else w(__half{});
 }
-// Calls f with the number of elements a thread holds and the threads that share a row: a warp to
-// 1024 columns, then 16 elements a thread and up to 1024 threads.
+// Calls f with the number of octets a thread holds and the threads that share a row: a warp to 1024 columns, then two
+// octets a thread and up to 1024 threads.
 template <typename F>
 void with_row(int cols, F&& f) {
     using std::integral_constant;
-    if (cols <= 256) f(integral_constant<int, 8>{}, integral_constant<int, 32>{});
-    else if (cols <= 512) f(integral_constant<int, 16>{}, integral_constant<int, 32>{});
-    else if (cols <= 768) f(integral_constant<int, 24>{}, integral_constant<int, 32>{});
-    else if (cols <= 1024) f(integral_constant<int, 32>{}, integral_constant<int, 32>{});
-    else if (cols <= 2048) f(integral_constant<int, 16>{}, integral_constant<int, 128>{});
-    else if (cols <= 4096) f(integral_constant<int, 16>{}, integral_constant<int, 256>{});
-    else if (cols <= 8192) f(integral_constant<int, 16>{}, integral_constant<int, 512>{});
-    else f(integral_constant<int, 16>{}, integral_constant<int, 1024>{});
+    if (cols <= 256) f(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+    else if (cols <= 512) f(integral_constant<int, 2>{}, integral_constant<int, 32>{});
+    else if (cols <= 768) f(integral_constant<int, 3>{}, integral_constant<int, 32>{});
+    else if (cols <= 1024) f(integral_constant<int, 4>{}, integral_constant<int, 32>{});
+    else if (cols <= 2048) f(integral_constant<int, 2>{}, integral_constant<int, 128>{});
+    else if (cols <= 4096) f(integral_constant<int, 2>{}, integral_constant<int, 256>{});
+    else if (cols <= 8192) f(integral_constant<int, 2>{}, integral_constant<int, 512>{});
+    else f(integral_constant<int, 2>{}, integral_constant<int, 1024>{});
 }
 constexpr int kMaxNormCols = 16384;
 
-// The gradient holds three packed rows, the gains and a sum per column: 8 elements a thread, or 16 where that saves
+// The gradient holds three packed rows, the gains and a sum per column: one octet a thread, or two where that saves
 // the exchange between warps or there is no room for more threads.  `blocks`: resident per SM.
-struct GradRow { int elements, threads, rows, blocks; };
-constexpr GradRow kGradRows[] = {{8, 32, 2, 4}, {16, 32, 2, 3}, {8, 128, 2, 5}, {8, 256, 2, 2}, {8, 512, 2, 1}, {16, 512, 2, 1}, {16, 1024, 1, 1}};
+struct GradRow { int octets, threads, rows, blocks; };
+constexpr GradRow kGradRows[] = {{1, 32, 2, 4}, {2, 32, 2, 3}, {1, 128, 2, 5}, {1, 256, 2, 2}, {1, 512, 2, 1}, {2, 512, 2, 1}, {2, 1024, 1, 1}};
 int grad_row(int cols) {
     int k = 0;
-    while (kGradRows[k].elements * kGradRows[k].threads < cols) ++k;
+    while (kGradRows[k].octets * 8 * kGradRows[k].threads < cols) ++k;
     return k;
 }
 template <typename F>
@@ -525,6 +485,23 @@ int norm_grad_blocks(const pg_norm_grad_args& a) {
     return static_cast<int>(std::max<int64_t>(n, 1));
 }
 
+// Shares of a strip's tokens in the activation's gradient, eight at most (the portable cluster size): the number whose
+// blocks (three per SM at once) take the fewest steps of eight rows, a block's start and end counted as six.  700 tokens x
+// 2600 columns of 32 workers: 81, 76, 86 and 96 us for 1, 2, 4 and 8 shares.
+int strip_splits(int64_t strips, int64_t tokens) {
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 8; s *= 2) {
+        const double waves = std::max(1.0, strips * s / (3.0 * kSMs));
+        const double cost = waves * ((tokens + s - 1) / s / 8.0 + 6.0);
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
+}
+
 }  // namespace
 }  // namespace pgt
 
@@ -547,14 +524,13 @@ int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
     if (a.rstd && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
     if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
-    const int width = access_width({&a.x, &a.residual, &a.h, &a.y}, a.batch);
-    with_type(a.dtype, width, [&](auto h, auto v) {
+    with_type(a.dtype, access_width({&a.x, &a.residual}, a.batch), access_width({&a.h, &a.y}, a.batch), [&](auto h, auto in, auto out) {
         using H = decltype(h);
-        constexpr int V = decltype(v)::value;
-        with_row(a.cols, [&](auto e, auto threads) {
-            constexpr int T = decltype(threads)::value, C = decltype(e)::value / V;
+        constexpr int W = decltype(in)::value, WO = decltype(out)::value;
+        with_row(a.cols, [&](auto octets, auto threads) {
+            constexpr int T = decltype(threads)::value, C = decltype(octets)::value;
             const dim3 grid(T > 32 ? a.tokens : (a.tokens + 7) / 8, a.batch);
-            norm_kernel<H, V, C, T><<<grid, T > 32 ? T : 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
+            norm_kernel<H, W, WO, C, T><<<grid, T > 32 ? T : 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
         });
     });
     return launch_status();
@@ -591,18 +567,17 @@ int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t 
     float* partial = static_cast<float*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a.tokens > 0 || a.dgain) {
-        const int width = access_width({&a.dy, &a.h, &a.dh, &a.dx}, a.batch);
-        with_type(a.dtype, width, [&](auto h, auto v) {
+        with_type(a.dtype, access_width({&a.dy, &a.h, &a.dh}, a.batch), access_width({&a.dx}, a.batch), [&](auto h, auto in, auto out) {
             using H = decltype(h);
-            constexpr int V = decltype(v)::value;
+            constexpr int W = decltype(in)::value, WO = decltype(out)::value;
             with_grad_row(a.cols, [&](auto shape) {
                 constexpr GradRow g = kGradRows[decltype(shape)::value];
-                constexpr int T = g.threads, C = g.elements / V, kGroups = T > 32 ? 1 : kGradBlock / 32;
+                constexpr int T = g.threads, C = g.octets, kGroups = T > 32 ? 1 : kGradBlock / 32;
                 const int per = (a.tokens + blocks * kGroups - 1) / (blocks * kGroups);
                 const dim3 grid(blocks, a.batch);
                 const size_t smem = T > 32 ? 0 : sizeof(float) * kGroups * a.cols;
-                if (eight) norm_grad_kernel<H, V, C, T, g.rows, true><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
-                else norm_grad_kernel<H, V, C, T, g.rows, false><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
+                if (eight) norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, true><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
+                else norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, false><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
             });
         });
         if (a.dgain)
@@ -624,17 +599,13 @@ int pg_activation_grad(const pg_activation_grad_args* args, void* stream) {
     if (a.dz.data && !matrix_ok(a.dz, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
     if (a.dbias && !vector_ok(a.dbias, a.dbias_stride, a.batch, a.cols, true, dev)) return PG_ERR_INVALID;
     if (a.batch == 0 || (a.tokens == 0 && !a.dbias)) return PG_OK;
-    const int width = access_width({&a.dy, &a.dz}, a.batch);
-    const int strips = (a.cols + 32 * width - 1) / (32 * width);
-    // Shares of a strip's tokens: until the GPU has about 16 blocks per SM (five waves, so that the last one weighs
-    // little), eight at most (the portable cluster size), no share under 32 tokens.
-    int splits = 1;
-    while (splits < 8 && int64_t{strips} * a.batch * splits < kSMs * 16 && a.tokens >= 64 * splits) splits *= 2;
+    const int strips = (a.cols + kStrip - 1) / kStrip;
+    const int splits = strip_splits(int64_t{strips} * a.batch, a.tokens);
     const int per = (a.tokens + splits - 1) / splits;
     int rc = PG_OK;
-    with_type(a.dtype, width, [&](auto h, auto v) {
+    with_type(a.dtype, access_width({&a.dy}, a.batch), access_width({&a.dz}, a.batch), [&](auto h, auto in, auto out) {
         using H = decltype(h);
-        constexpr int V = decltype(v)::value;
+        constexpr int W = decltype(in)::value, WO = decltype(out)::value;
         auto launch = [&](auto kernel) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(strips, a.batch, splits);
@@ -651,10 +622,10 @@ int pg_activation_grad(const pg_activation_grad_args* args, void* stream) {
                 rc = PG_ERR_CUDA;
             }
         };
-        if (a.activation == PG_ACT_RELU) launch(activation_grad_kernel<H, V, PG_ACT_RELU>);
-        else if (a.activation == PG_ACT_GELU) launch(activation_grad_kernel<H, V, PG_ACT_GELU>);
-        else if (a.activation == PG_ACT_SILU) launch(activation_grad_kernel<H, V, PG_ACT_SILU>);
-        else launch(activation_grad_kernel<H, V, PG_ACT_NONE>);
+        if (a.activation == PG_ACT_RELU) launch(activation_grad_kernel<H, W, WO, PG_ACT_RELU>);
+        else if (a.activation == PG_ACT_GELU) launch(activation_grad_kernel<H, W, WO, PG_ACT_GELU>);
+        else if (a.activation == PG_ACT_SILU) launch(activation_grad_kernel<H, W, WO, PG_ACT_SILU>);
+        else launch(activation_grad_kernel<H, W, WO, PG_ACT_NONE>);
     });
     return rc;
 }
@@ -669,14 +640,15 @@ static int checkpoint(const pg_checkpoint_args* args, bool write, void* stream) 
     const int64_t rows = int64_t{a.batch} * a.tokens;
     if (rows == 0) return PG_OK;
     const int width = access_width({&a.x}, a.batch);
-    const int chunks = (a.cols + kBlock8 - 1) / kBlock8 * (kBlock8 / width);
-    const int64_t blocks = (rows * chunks + 255) / 256;
+    const int octets = (a.cols + kBlock8 - 1) / kBlock8 * (kBlock8 / 8);
+    const int64_t blocks = (rows * octets + 255) / 256;
     if (blocks > 0x7fffffff) return PG_ERR_TOO_LARGE;
-    with_type(a.dtype, width, [&](auto h, auto v) {
+    with_type(a.dtype, write ? width : 8, write ? 8 : width, [&](auto h, auto in, auto out) {
         using H = decltype(h);
-        constexpr int V = decltype(v)::value;
-        if (write) checkpoint_kernel<H, V, true><<<static_cast<unsigned>(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(a, rows, chunks);
-        else checkpoint_kernel<H, V, false><<<static_cast<unsigned>(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(a, rows, chunks);
+        constexpr int W = decltype(in)::value, WO = decltype(out)::value;
+        cudaStream_t st = static_cast<cudaStream_t>(stream);
+        if (write) checkpoint_kernel<H, W, WO, true><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, rows, octets);
+        else checkpoint_kernel<H, W, WO, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, rows, octets);
     });
     return launch_status();
 }
