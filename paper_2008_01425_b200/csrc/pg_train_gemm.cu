@@ -42,10 +42,9 @@ template <Mode M> constexpr bool kWeightGrads = M == kWeightGrad || M == kWeight
 template <Mode M> constexpr bool kTokenRows = M == kForwardRows || M == kInputGradRows;
 template <Mode M> constexpr bool kAMnMajor = M == kInputGrad || kWeightGrads<M>;
 template <Mode M> constexpr bool kBMnMajor = M == kInputGradRows || kWeightGrads<M>;
-constexpr int kRowWarps = 16;         // epilogue warps where lanes are tokens
-constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out
-template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
-template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 128 : 0);
+constexpr int kOutBytes = 2048;       // 32 rows x 32 elements on their way out, two per epilogue warp
+constexpr int kOutRing = 8 * 2 * kOutBytes;
+template <Mode M> constexpr int kThreads = M == kWeightGrad8 ? 640 : 384;
 
 // What happens to D: stored as fp32 (dW), or passed through bias, activation and residual to 16 bits.
 struct Epilogue {
@@ -111,19 +110,53 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
 }
+// The same with a barrier of the pair's first block.
+__device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+// The address of one of this block's barriers in the first block of its pair.
+__device__ __forceinline__ uint32_t first_of_pair(uint64_t* b) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(b)));
+    return r;
+}
+__device__ __forceinline__ void bar_arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y),
                  "r"(z)
                  : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// PAIR: two blocks on neighbouring SMs multiply together, each with its 128 rows of A and half of B's rows in its own
+// shared memory; the first of them issues, and its commits reach the same barrier of both.
+template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(idesc), "r"(add)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(idesc), "r"(add)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(idesc), "r"(add)
+                     : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                     "h"(static_cast<uint16_t>(3))
+                     : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
     uint32_t r[16];
@@ -212,30 +245,28 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
 }
 
 struct Shared {
-    uint64_t loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
+    uint64_t loaded[kMaxStages], raw[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
     uint32_t tmem;
     int gave_up;
+    float bias[8][32];
 };
 
-// Lanes are tokens: 16 warps take groups of 32 columns of 32 rows each.  Four warps per scheduler hide each other's
-// loads of residuals.  The result goes to shared memory in the 64-byte swizzle of the output's tensor map and leaves by
-// TMA, which also cuts off what lies outside the matrix.
-template <typename H, int ACT, bool ALIGNED>
-__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, int64_t b, int m0,
-                                           int n0, int share, int quarter, int lane) {
-    const Epilogue& ep = p.ep;
-    const int row = m0 + quarter * 32 + lane;
-    const bool live = row < p.M;
-    const int end = min(p.BN, p.N - n0);
-    const bool add_residual = ep.residual.data != nullptr;
-    for (int j = share * 32; j < end; j += kRowWarps / 4 * 32) {
-        const int n = n0 + j;
-        // the residual's 32 elements of this row: four 16-byte pieces, five where the row starts between two of them
-        uint4 piece[ALIGNED ? 4 : 5];
-        int off = 0;
-        if (add_residual) {
-            const uint16_t* res = static_cast<const uint16_t*>(ep.residual.data) + b * ep.residual.stride + (live ? row : 0) * ep.residual.ld;
-            if (!ALIGNED) off = static_cast<int>(reinterpret_cast<uintptr_t>(res) & 15) / 2;
+// Lanes are tokens: a warp takes every other group of 32 columns of its 32 rows.  What belongs to the next group (the
+// residual's pieces, a bias per lane) is on its way while one group is computed, and while the first one's accumulator is
+// waited for.  The result goes to shared memory in the 64-byte swizzle of the output's tensor map and leaves by TMA,
+// which also cuts off what lies outside the matrix.
+template <bool ALIGNED>
+struct RowGroup {              // what a lane holds for a group before its accumulator is read
+    uint4 piece[ALIGNED ? 4 : 5];      // 32 residuals of its row: four 16-byte pieces, five where the row starts between two
+    int off;
+    float bias;
+
+    __device__ __forceinline__ void fetch(const Problem& p, int64_t b, int row, int n, int lane, bool wanted) {
+        if (!wanted) return;
+        if (p.ep.residual.data) {
+            const bool live = row < p.M;
+            const uint16_t* res = static_cast<const uint16_t*>(p.ep.residual.data) + b * p.ep.residual.stride + (live ? row : 0) * p.ep.residual.ld;
+            off = ALIGNED ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(res) & 15) / 2;
             const uint4* at = reinterpret_cast<const uint4*>(res + n - off);
 #pragma unroll
             for (int i = 0; i < (ALIGNED ? 4 : 5); ++i) {
@@ -243,10 +274,25 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 if (live && n - off + 8 * i < p.N && (i < 4 || off > 0)) piece[i] = at[i];
             }
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last group's copy has been read
-        __syncwarp();
-        float* s_bias = reinterpret_cast<float*>(out);         // the same 32 numbers for all lanes, until the result takes their place
-        s_bias[lane] = ep.bias && n + lane < p.N ? ep.bias[b * ep.bias_stride + n + lane] : 0.0f;
+        bias = p.ep.bias && n + lane < p.N ? p.ep.bias[b * p.ep.bias_stride + n + lane] : 0.0f;
+    }
+};
+template <typename H, int ACT, bool ALIGNED>
+__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* ring, float* s_bias, int64_t b, int m0,
+                                           int n0, int half, int quarter, int lane, int& flip, RowGroup<ALIGNED>& next) {
+    const Epilogue& ep = p.ep;
+    const int row = m0 + quarter * 32 + lane;
+    const bool live = row < p.M;
+    const int end = min(p.BN, p.N - n0);
+    const bool add_residual = ep.residual.data != nullptr;
+    for (int j = half * 32; j < end; j += 64) {
+        const int n = n0 + j;
+        const RowGroup<ALIGNED> here = next;
+        next.fetch(p, b, row, n + 64, lane, j + 64 < end);
+        uint8_t* out = ring + flip * kOutBytes;
+        flip ^= 1;
+        s_bias[lane] = here.bias;                              // the same 32 numbers for all lanes
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the copy before the last has been read
         __syncwarp();
         const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j;
         if (ep.z8.values) {
@@ -296,7 +342,8 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 F2 hi = activate<ACT>(add(pair(acc[4 * i + 2], acc[4 * i + 3]), pair(f.z, f.w)));
                 if (add_residual) {
                     const int k = 2 * h + i / 2;
-                    const Oct o = ALIGNED ? Oct{{piece[k].x, piece[k].y, piece[k].z, piece[k].w}} : cut(piece[k], piece[k + !ALIGNED], off);
+                    const uint4& w0 = here.piece[k];
+                    const Oct o = ALIGNED ? Oct{{w0.x, w0.y, w0.z, w0.w}} : cut(w0, here.piece[k + !ALIGNED], here.off);
                     lo = add(lo, Elem<H>::up2(o.w[2 * (i & 1)]));
                     hi = add(hi, Elem<H>::up2(o.w[2 * (i & 1) + 1]));
                 }
@@ -310,7 +357,7 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
             *reinterpret_cast<uint4*>(out + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) tma_store(map_out, out, n, m0 + quarter * 32, static_cast<int>(b));
+        if (lane == 0 && m0 + quarter * 32 < p.M) tma_store(map_out, out, n, m0 + quarter * 32, static_cast<int>(b));
     }
 }
 
@@ -489,30 +536,34 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 }
 
 // ------------------------------------------------------------------ the kernel
-// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 4 - 11 empty accumulators, 12 - 15 widen an
-// 8-bit A.  Every wait ends: it is for work that this block has already started, and a wait that takes
+// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 4 - 11 empty accumulators, 12 - 19 widen an 8-bit A, one half
+// of them every other stage.  Every wait ends: it is for work that has already been started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
-template <typename H, Mode MODE>
+template <typename H, Mode MODE, bool PAIR>
 __global__ void __launch_bounds__(kThreads<MODE>, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
                const __grid_constant__ Problem p) {
     extern __shared__ uint8_t s_raw[];
     __shared__ Shared sh;
-    constexpr bool kAMn = kAMnMajor<MODE>, kBMn = kBMnMajor<MODE>, kFp32 = kWeightGrads<MODE>;
+    constexpr bool kAMn = kAMnMajor<MODE>, kBMn = kBMnMajor<MODE>, kFp32 = kWeightGrads<MODE>, kEight = MODE == kWeightGrad8;
+    constexpr int kBlocks = PAIR ? 2 : 1;
     uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
-    const int b_bytes = (kBMn ? (p.BN + 63) / 64 * 64 : p.BN) * kBK * 2;
-    const int stage_bytes = kABytes + b_bytes + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    const int b_rows = p.BN / kBlocks;                  // of B in this block's shared memory
+    const int b_bytes = (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
+    const int stage_bytes = kABytes + b_bytes + (kEight ? kRawBytes : 0);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
+    const int in_pair = PAIR ? blockIdx.x & 1 : 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&sh.loaded[s], 1);
-            bar_init(&sh.widened[s], 4);
+            bar_init(&sh.raw[s], 1);
+            bar_init(&sh.widened[s], 4 * kBlocks);
             bar_init(&sh.empty[s], 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&sh.summed[i], 1);
-            bar_init(&sh.drained[i], kEpilogueWarps<MODE>);
+            bar_init(&sh.drained[i], 8 * kBlocks);
         }
         bar_init(&sh.last, 1);
         sh.gave_up = 0;
@@ -520,122 +571,160 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         asm volatile("fence.proxy.async;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(tmem_cols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh.tmem;
     volatile int* gave_up = &sh.gave_up;
 
-    // a block's tiles: every gridDim-th, or with split k the one of its cluster
-    const int rank = p.splits > 1 ? blockIdx.x % p.splits : 0;
-    const int64_t first = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x;
-    const int64_t step = p.splits > 1 ? p.tiles : gridDim.x;
-    const int kb0 = p.k_blocks * rank / p.splits, kb1 = p.k_blocks * (rank + 1) / p.splits;
+    // the tiles of a block (or pair): every so many, or with split k the one of its cluster
+    const int rank = !PAIR && p.splits > 1 ? blockIdx.x % p.splits : 0;
+    const int64_t first = PAIR ? blockIdx.x >> 1 : p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x;
+    const int64_t step = PAIR ? gridDim.x >> 1 : p.splits > 1 ? p.tiles : gridDim.x;
+    const int kb0 = PAIR ? 0 : p.k_blocks * rank / p.splits, kb1 = PAIR ? p.k_blocks : p.k_blocks * (rank + 1) / p.splits;
     const int64_t per_worker = int64_t{p.m_tiles} * p.n_tiles;
+    // worker, this block's first row, the tile's first column
     auto place = [&](int64_t tile, int64_t& b, int& m0, int& n0) {
         b = tile / per_worker;
         const int64_t in = tile - b * per_worker;
         n0 = static_cast<int>(in / p.m_tiles) * p.BN;
-        m0 = static_cast<int>(in % p.m_tiles) * kBM;
+        m0 = (static_cast<int>(in % p.m_tiles) * kBlocks + in_pair) * kBM;
     };
 
     if (warp == 0 && lane == 0) {
-        int it = 0;
+        int s = 0, turn = 0;
+        int64_t issued = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int64_t b;
             int m0, n0;
             place(tile, b, m0, n0);
+            n0 += in_pair * b_rows;
             const int ba = p.a_shared ? 0 : static_cast<int>(b), bb = p.b_shared ? 0 : static_cast<int>(b);
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int s = it % p.stages;
-                if (it >= p.stages && !(ok = bar_wait(&sh.empty[s], (it / p.stages - 1) & 1, gave_up))) break;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (turn > 0 && !(ok = bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up))) break;
                 uint8_t* a = ring + s * stage_bytes;
                 uint8_t* bt = a + kABytes;
                 const int k0 = kb * kBK;
-                bar_expect(&sh.loaded[s], (MODE == kWeightGrad8 ? kRawBytes : kABytes) + b_bytes);
-                if constexpr (!kAMn) {
-                    tma_load(a, &map_a, k0, m0, ba, &sh.loaded[s]);
-                } else if constexpr (MODE == kWeightGrad8) {
-                    tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.loaded[s]);
+                // the pair's first block is told of the bytes of both
+                if (in_pair == 0) bar_expect(&sh.loaded[s], ((kEight ? 0 : kABytes) + b_bytes) * kBlocks);
+                const uint32_t at = PAIR ? first_of_pair(&sh.loaded[s]) : 0;
+                auto load = [&](void* dst, const CUtensorMap* map, int x, int y, int z) {
+                    if constexpr (PAIR) tma_load_pair(dst, map, x, y, z, at);
+                    else tma_load(dst, map, x, y, z, &sh.loaded[s]);
+                };
+                if constexpr (kEight) {
+                    bar_expect(&sh.raw[s], kRawBytes);
+                    tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.raw[s]);
+                } else if constexpr (kAMn) {
+                    load(a, &map_a, m0, k0, ba);
+                    load(a + 8192, &map_a, m0 + 64, k0, ba);
                 } else {
-                    tma_load(a, &map_a, m0, k0, ba, &sh.loaded[s]);
-                    tma_load(a + 8192, &map_a, m0 + 64, k0, ba, &sh.loaded[s]);
+                    load(a, &map_a, k0, m0, ba);
                 }
                 if constexpr (kBMn) {
-                    for (int j = 0; j < p.BN; j += 64) tma_load(bt + j * 128, &map_b, n0 + j, k0, bb, &sh.loaded[s]);
+                    for (int j = 0; j < b_rows; j += 64) load(bt + j * 128, &map_b, n0 + j, k0, bb);
                 } else {
-                    tma_load(bt, &map_b, k0, n0, bb, &sh.loaded[s]);
+                    load(bt, &map_b, k0, n0, bb);
+                }
+                ++issued;
+                if (++s == p.stages) {
+                    s = 0;
+                    ++turn;
                 }
             }
         }
-        if (!ok)       // copies still on their way must land before the block ends
-            for (int i = max(0, it - p.stages); i < it; ++i)
-                for (int t = 0; t < 100000 && !bar_try(&sh.loaded[i % p.stages], (i / p.stages) & 1); ++t) {}
-    } else if (warp == 1 && lane == 0) {
+        if (!ok)       // copies still on their way must land before the block ends (those of a second block: see the end)
+            for (int64_t i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i) {
+                const int st = static_cast<int>(i % p.stages), parity = static_cast<int>(i / p.stages) & 1;
+                for (int t = 0; t < 100000 && in_pair == 0 && !bar_try(&sh.loaded[st], parity); ++t) {}
+                for (int t = 0; t < 100000 && kEight && !bar_try(&sh.raw[st], parity); ++t) {}
+            }
+    } else if (warp == 1 && lane == 0 && in_pair == 0) {
         constexpr uint32_t fmt = std::is_same<H, __half>::value ? 0 : 1;
         const uint32_t idesc = 1u << 4 | fmt << 7 | fmt << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
-                               static_cast<uint32_t>(p.BN >> 3) << 17 | static_cast<uint32_t>(kBM >> 4) << 24;
-        int it = 0, done = 0;
+                               static_cast<uint32_t>(p.BN >> 3) << 17 | static_cast<uint32_t>(kBM * kBlocks >> 4) << 24;
+        int s = 0, parity = 0, done = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step, ++done) {
             const int acc = done & 1;
             if (done >= 2 && !(ok = bar_wait(&sh.drained[acc], (done / 2 - 1) & 1, gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int s = it % p.stages;
-                if (!(ok = bar_wait(&sh.loaded[s], (it / p.stages) & 1, gave_up))) break;
-                if (MODE == kWeightGrad8 && !(ok = bar_wait(&sh.widened[s], (it / p.stages) & 1, gave_up))) break;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
+                if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t a = smem_u32(ring + s * stage_bytes);
+                const uint32_t at = smem_u32(ring + s * stage_bytes);
+                const uint64_t a = operand_desc(at, kAMn), bd = operand_desc(at + kABytes, kBMn);
                 const int steps = (min(kBK, p.K - kb * kBK) + 15) / 16;
                 for (int k = 0; k < steps; ++k)
-                    mma_f16(tmem + acc * p.BN, operand_desc(a + k * (kAMn ? 2048 : 32), kAMn),
-                            operand_desc(a + kABytes + k * (kBMn ? 2048 : 32), kBMn), idesc, kb > kb0 || k > 0);
-                mma_commit(&sh.empty[s]);
+                    mma_f16<PAIR>(tmem + acc * p.BN, a + k * ((kAMn ? 2048 : 32) >> 4), bd + k * ((kBMn ? 2048 : 32) >> 4), idesc, kb > kb0 || k > 0);
+                mma_commit<PAIR>(&sh.empty[s]);
+                if (++s == p.stages) {
+                    s = 0;
+                    parity ^= 1;
+                }
             }
-            if (ok) mma_commit(&sh.summed[acc]);
+            if (ok) mma_commit<PAIR>(&sh.summed[acc]);
         }
         if (!ok) {
-            mma_commit(&sh.last);
+            mma_commit<PAIR>(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
         }
-    } else if (warp >= 4 && warp < 4 + kEpilogueWarps<MODE>) {
+    } else if (warp >= 4 && warp < 12) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        int done = 0;
-        for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
-            const int acc = done & 1;
-            int64_t b;
-            int m0, n0;
-            place(tile, b, m0, n0);
-            if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            __syncwarp();
-            if constexpr (kTokenRows<MODE>) {
-                uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutBytes;
-                with_activation<H, MODE>(p.ep.activation, [&](auto act) {
-                    if (p.residual_aligned)
-                        empty_rows<H, decltype(act)::value, true>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane);
+        const uint32_t drained[2] = {PAIR ? first_of_pair(&sh.drained[0]) : 0u, PAIR ? first_of_pair(&sh.drained[1]) : 0u};
+        // the body for every combination that the epilogue is compiled for
+        with_activation<H, MODE>(p.ep.activation, [&](auto act) {
+            auto tiles = [&](auto residual_aligned) {
+                constexpr bool kAligned = decltype(residual_aligned)::value;
+                RowGroup<kAligned> next;
+                int done = 0;
+                [[maybe_unused]] int flip = 0;
+                for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
+                    const int acc = done & 1;
+                    int64_t b;
+                    int m0, n0;
+                    place(tile, b, m0, n0);
+                    if constexpr (kTokenRows<MODE>)
+                        next.fetch(p, b, m0 + quarter * 32 + lane, n0 + half * 32, lane, half * 32 < min(p.BN, p.N - n0));
+                    if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if constexpr (kTokenRows<MODE>)
+                        empty_rows<H, decltype(act)::value, kAligned>(p, &map_out, tmem + acc * p.BN, ring + p.stages * stage_bytes + (warp - 4) * 2 * kOutBytes,
+                                                                      sh.bias[warp - 4], b, m0, n0, half, quarter, lane, flip, next);
                     else
-                        empty_rows<H, decltype(act)::value, false>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane);
-                });
-            } else with_activation<H, MODE>(p.ep.activation, [&](auto act) {
-                empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0, n0,
-                                                           half, quarter, lane);
-            });
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.drained[acc]);
-        }
+                        empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b,
+                                                                   m0, n0, half, quarter, lane);
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) bar_arrive_at(drained[acc]);
+                        else bar_arrive(&sh.drained[acc]);
+                    }
+                }
+            };
+            if (!kTokenRows<MODE> || p.residual_aligned) tiles(std::true_type{});
+            else tiles(std::false_type{});
+        });
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    } else if (MODE == kWeightGrad8 && warp >= 12) {
+    } else if (kEight && warp >= 12) {
         // thread: row k = r of the stage, 64 of its 128 values (two blocks).  The 16-byte pieces are taken in
         // an order that puts the 8 threads of a shared-memory phase on different banks, reading and writing.
-        const int r = (threadIdx.x - 384) >> 1, h = threadIdx.x & 1;
-        int it = 0;
+        const int mine = (warp - 12) >> 2;             // of every two stages
+        const int r = (threadIdx.x & 127) >> 1, h = threadIdx.x & 1;
+        const uint32_t widened = PAIR ? first_of_pair(&sh.widened[0]) : smem_u32(&sh.widened[0]);
+        int s = 0, parity = 0, turn = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int64_t b;
@@ -649,45 +738,52 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 s0 = in && one ? scales[k * p.scale_ld] : 0u;
                 s1 = in && two ? scales[k * p.scale_ld + 1] : 0u;
             };
-            uint32_t s0[2], s1[2];
-            fetch(kb0, s0[0], s1[0]);
-            fetch(kb0 + 1, s0[1], s1[1]);
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int s = it % p.stages;
-                uint32_t n0s, n1s;
-                fetch(kb + 2, n0s, n1s);
-                if (!(ok = bar_wait(&sh.loaded[s], (it / p.stages) & 1, gave_up))) break;
-                uint8_t* a = ring + s * stage_bytes;
-                const uint8_t* raw = a + kABytes + b_bytes + r * 128 + h * 64;
-                const uint32_t f0 = scale_pair<H>(s0[0]), f1 = scale_pair<H>(s1[0]);
+            uint32_t s0, s1;
+            fetch(kb0 + (turn ^ mine), s0, s1);
+            for (int kb = kb0; kb < kb1; ++kb, turn ^= 1) {
+                if (turn == mine) {
+                    uint32_t t0, t1;
+                    fetch(kb + 2, t0, t1);
+                    if (!(ok = bar_wait(&sh.raw[s], parity, gave_up))) break;
+                    uint8_t* a = ring + s * stage_bytes;
+                    const uint8_t* raw = a + kABytes + b_bytes + r * 128 + h * 64;
+                    const uint32_t f0 = scale_pair<H>(s0), f1 = scale_pair<H>(s1);
+                    uint4 w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = (i + (r & 3) + 2 * h) & 3;
-                    const uint4 w = *reinterpret_cast<const uint4*>(raw + c * 16);
-                    const uint32_t f = c < 2 ? f0 : f1;
-                    uint4 o0, o1;
-                    widen4<H>(w.x, f, o0.x, o0.y);
-                    widen4<H>(w.y, f, o0.z, o0.w);
-                    widen4<H>(w.z, f, o1.x, o1.y);
-                    widen4<H>(w.w, f, o1.z, o1.w);
-                    uint8_t* row = a + h * 8192 + r * 128;
-                    *reinterpret_cast<uint4*>(row + (((2 * c) ^ (r & 7)) << 4)) = o0;
-                    *reinterpret_cast<uint4*>(row + (((2 * c + 1) ^ (r & 7)) << 4)) = o1;
+                    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(raw + ((i + (r & 3) + 2 * h) & 3) * 16);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = (i + (r & 3) + 2 * h) & 3;
+                        const uint32_t f = c < 2 ? f0 : f1;
+                        uint4 o0, o1;
+                        widen4<H>(w[i].x, f, o0.x, o0.y);
+                        widen4<H>(w[i].y, f, o0.z, o0.w);
+                        widen4<H>(w[i].z, f, o1.x, o1.y);
+                        widen4<H>(w[i].w, f, o1.z, o1.w);
+                        uint8_t* row = a + h * 8192 + r * 128;
+                        *reinterpret_cast<uint4*>(row + (((2 * c) ^ (r & 7)) << 4)) = o0;
+                        *reinterpret_cast<uint4*>(row + (((2 * c + 1) ^ (r & 7)) << 4)) = o1;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) bar_arrive_at(widened + s * 8);
+                        else bar_arrive(&sh.widened[s]);
+                    }
+                    s0 = t0;
+                    s1 = t1;
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive(&sh.widened[s]);
-                s0[0] = s0[1];
-                s1[0] = s1[1];
-                s0[1] = n0s;
-                s1[1] = n1s;
+                if (++s == p.stages) {
+                    s = 0;
+                    parity ^= 1;
+                }
             }
         }
     }
 
-    if (!kTokenRows<MODE> && p.splits > 1) {
-        __syncwarp();
-        cooperative_groups::this_cluster().sync();
+    __syncwarp();
+    if (!PAIR && !kTokenRows<MODE> && p.splits > 1) {
+        cluster_barrier();
         if (warp >= 4 && warp < 12 && !*gave_up) {
             int64_t b;
             int m0, n0;
@@ -697,13 +793,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             });
         }
         __syncwarp();
-        cooperative_groups::this_cluster().sync();
+        cluster_barrier();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();             // neither block goes while the other's copies, products or arrivals may reach it
     if (warp == 2) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
     }
 }
 
@@ -781,45 +879,46 @@ int aligned_operand(pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, uin
     return launch_status();
 }
 
-template <typename H, Mode MODE>
+template <typename H, Mode MODE, bool PAIR>
 int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const Problem& p, int smem, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
     bool fine = true;
     std::call_once(once[dev], [&] {
-        fine = cudaFuncSetAttribute(product_kernel<H, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - 2048) == cudaSuccess;
+        fine = cudaFuncSetAttribute(product_kernel<H, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - 2048) == cudaSuccess;
     });
     if (!fine) return PG_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.splits > 1 ? p.tiles * p.splits : std::min<int64_t>(p.tiles, kSMs)));
+    cfg.gridDim = dim3(static_cast<unsigned>(PAIR ? 2 * std::min<int64_t>(p.tiles, kSMs / 2) : p.splits > 1 ? p.tiles * p.splits : std::min<int64_t>(p.tiles, kSMs)));
     cfg.blockDim = dim3(kThreads<MODE>);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = p.splits;
+    at[0].val.clusterDim.x = PAIR ? 2 : p.splits;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE>, a, b, out, p) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE, PAIR>, a, b, out, p) != cudaSuccess) {
         cudaGetLastError();
         return PG_ERR_CUDA;
     }
     return PG_OK;
 }
 
-template <Mode MODE>
+template <Mode MODE, bool PAIR>
 int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const pg_matrix& A, const pg_matrix& B, const Epilogue& ep, const pg_matrix8* a8,
                 cudaStream_t st) {
     constexpr bool kBMn = kBMnMajor<MODE>, kAMn = kAMnMajor<MODE>, kRows = kTokenRows<MODE>;
+    constexpr int kBlocks = PAIR ? 2 : 1;
     Problem p = {};
     p.ep = ep;
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
     p.K = static_cast<int>(K);
     p.batch = static_cast<int>(batch);
-    p.m_tiles = static_cast<int>((M + kBM - 1) / kBM);
+    p.m_tiles = static_cast<int>((M + kBM * kBlocks - 1) / (kBM * kBlocks));
     // Widths of a tile: multiples of 16 columns, of 32 where a thread holds blocks of 32, of 64 where TMA loads boxes of
     // 64 columns and every other one is stored.  The one that covers N with the fewest columns, a tile's start and
     // end counted as 64 more; the widest of equals.
@@ -836,10 +935,11 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
     p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
     p.splits = 1;
-    if (!kRows)
+    if (!PAIR)
         while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
-    const int stage = kABytes + (kBMn ? (p.BN + 63) / 64 * 64 : p.BN) * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
-    const int rest = kRows ? kRowWarps * kOutBytes : 0;
+    const int b_rows = p.BN / kBlocks;
+    const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    const int rest = kRows ? kOutRing : 0;
     p.stages = std::min(kMaxStages, (kSmemBytes - 3072 - rest) / stage);
     p.a_shared = A.stride == 0;
     p.b_shared = B.stride == 0;
@@ -852,16 +952,20 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     CUtensorMap map_a = {}, map_b = {}, map_out = {};
     if (K > 0) {
         const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
-                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : p.BN) &&
+                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
                           (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
     const int smem = p.stages * stage + rest + 1024;
-    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE>(map_a, map_b, map_out, p, smem, st) : launch<__half, MODE>(map_a, map_b, map_out, p, smem, st);
+    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, p, smem, st)
+                            : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
 }
 
-// Tokens from which they become the accumulator's lanes.
-constexpr int kRowTokens = 64;
+// Pairs of blocks multiply 256-row tiles; one row more than a block's 128 has to be there, and tiles for about half of
+// the GPU: with fewer, single blocks that share the k of a tile finish earlier.
+bool enough_for_pairs(int64_t batch, int64_t M, int64_t N) {
+    return M > kBM && batch * ((M + 2 * kBM - 1) / (2 * kBM)) * ((N + 255) / 256) * 2 >= kSMs / 2;
+}
 
 int current_device() {
     int d = 0;
@@ -907,9 +1011,9 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
     if (rc != PG_OK) return rc;
-    if (a.tokens > kRowTokens && aligned(a.y, a.batch, a.tokens))
-        return run_product<kForwardRows>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
-    return run_product<kForward>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
+    if (enough_for_pairs(a.batch, a.tokens, a.out_features) && aligned(a.y, a.batch, a.tokens))
+        return run_product<kForwardRows, true>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
+    return run_product<kForward, false>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
 
 int pg_linear_input_grad_workspace_bytes(const pg_input_grad_args* args, size_t* bytes_out) {
@@ -938,9 +1042,9 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
     if (rc != PG_OK) return rc;
-    if (a.tokens > kRowTokens && aligned(a.dx, a.batch, a.tokens))
-        return run_product<kInputGradRows>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
-    return run_product<kInputGrad>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
+    if (enough_for_pairs(a.batch, a.tokens, a.in_features) && aligned(a.dx, a.batch, a.tokens))
+        return run_product<kInputGradRows, true>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
+    return run_product<kInputGrad, false>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
 
 int pg_linear_weight_grad_workspace_bytes(const pg_weight_grad_args* args, size_t* bytes_out) {
@@ -970,12 +1074,17 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
     const Epilogue ep{a.accumulate, PG_ACT_NONE, a.dweight, {}, nullptr, 0, {}};
     pg_matrix dz = a.dz, x = a.x;
     int rc = a.tokens > 0 ? aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st) : PG_OK;
+    if (rc != PG_OK) return rc;
+    const bool pairs = enough_for_pairs(a.batch, a.in_features, a.out_features);
     if (eight) {
         x = pg_matrix{a.x8.values, a.x8.ld, a.x8.stride};
-        return rc != PG_OK ? rc : run_product<kWeightGrad8>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st);
+        return pairs ? run_product<kWeightGrad8, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st)
+                     : run_product<kWeightGrad8, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st);
     }
-    if (rc == PG_OK && a.tokens > 0) rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
-    return rc != PG_OK ? rc : run_product<kWeightGrad>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
+    if (a.tokens > 0) rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
+    if (rc != PG_OK) return rc;
+    return pairs ? run_product<kWeightGrad, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st)
+                 : run_product<kWeightGrad, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
 }
 
 int pg_training_status(void* stream) {

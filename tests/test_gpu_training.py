@@ -229,7 +229,9 @@ def test_norm_gradient_against_differences(tr):
 # ------------------------------------------------------------------ products
 PRODUCT_SHAPES = [(1, 1, 1, 1), (2, 1, 650, 260), (3, 5, 16, 16), (2, 33, 147, 65), (1, 64, 64, 128), (2, 130, 72, 136), (1, 257, 200, 129),
                   (5, 40, 650, 96), (1, 300, 512, 520), (2, 16, 1024, 256), (1, 1040, 64, 24), (3, 129, 136, 384), (1, 2, 4608, 512),
-                  (40, 3, 24, 40), (1, 600, 1032, 1288), (2, 513, 328, 2600)]
+                  (40, 3, 24, 40), (1, 600, 1032, 1288), (2, 513, 328, 2600),
+                  # enough tiles for pairs of blocks, in one, two or all of the products
+                  (5, 300, 650, 1000), (40, 257, 136, 72), (20, 200, 520, 700), (38, 129, 64, 33), (19, 385, 257, 513), (37, 7, 300, 200)]
 
 
 @pytest.mark.parametrize("shape", PRODUCT_SHAPES)
