@@ -86,14 +86,17 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
         : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).
+// Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).  The time is looked at
+// after a few thousand tries only.
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up) {
-    if (bar_try(b, parity)) return true;
+#pragma unroll 1
+    for (int i = 0; i < 4096; ++i)
+        if (bar_try(b, parity)) return true;
     long long t0, t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
     for (;;) {
 #pragma unroll 1
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < 1024; ++i)
             if (bar_try(b, parity)) return true;
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
@@ -154,6 +157,13 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
                      : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// One lane of a converged warp.  The loops that feed the tensor cores run in whole warps and choose a lane only to issue:
+// then descriptors, coordinates and barriers stay in uniform registers (one lane's own loop fell behind the tensor cores).
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0;
 }
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -600,7 +610,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         m0 = (static_cast<int>(in % p.m_tiles) * kBlocks + in_pair) * kBM;
     };
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         int s = 0, turn = 0;
         int64_t issued = 0;
         bool ok = true;
@@ -612,30 +622,33 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const int ba = p.a_shared ? 0 : static_cast<int>(b), bb = p.b_shared ? 0 : static_cast<int>(b);
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (turn > 0 && !(ok = bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up))) break;
-                uint8_t* a = ring + s * stage_bytes;
-                uint8_t* bt = a + kABytes;
-                const int k0 = kb * kBK;
-                // the pair's first block is told of the bytes of both
-                if (in_pair == 0) bar_expect(&sh.loaded[s], ((kEight ? 0 : kABytes) + b_bytes) * kBlocks);
-                const uint32_t at = PAIR ? first_of_pair(&sh.loaded[s]) : 0;
-                auto load = [&](void* dst, const CUtensorMap* map, int x, int y, int z) {
-                    if constexpr (PAIR) tma_load_pair(dst, map, x, y, z, at);
-                    else tma_load(dst, map, x, y, z, &sh.loaded[s]);
-                };
-                if constexpr (kEight) {
-                    bar_expect(&sh.raw[s], kRawBytes);
-                    tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.raw[s]);
-                } else if constexpr (kAMn) {
-                    load(a, &map_a, m0, k0, ba);
-                    load(a + 8192, &map_a, m0 + 64, k0, ba);
-                } else {
-                    load(a, &map_a, k0, m0, ba);
+                if (elected()) {
+                    uint8_t* a = ring + s * stage_bytes;
+                    uint8_t* bt = a + kABytes;
+                    const int k0 = kb * kBK;
+                    // the pair's first block is told of the bytes of both
+                    if (in_pair == 0) bar_expect(&sh.loaded[s], ((kEight ? 0 : kABytes) + b_bytes) * kBlocks);
+                    const uint32_t at = PAIR ? first_of_pair(&sh.loaded[s]) : 0;
+                    auto load = [&](void* dst, const CUtensorMap* map, int x, int y, int z) {
+                        if constexpr (PAIR) tma_load_pair(dst, map, x, y, z, at);
+                        else tma_load(dst, map, x, y, z, &sh.loaded[s]);
+                    };
+                    if constexpr (kEight) {
+                        bar_expect(&sh.raw[s], kRawBytes);
+                        tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.raw[s]);
+                    } else if constexpr (kAMn) {
+                        load(a, &map_a, m0, k0, ba);
+                        load(a + 8192, &map_a, m0 + 64, k0, ba);
+                    } else {
+                        load(a, &map_a, k0, m0, ba);
+                    }
+                    if constexpr (kBMn) {
+                        for (int j = 0; j < b_rows; j += 64) load(bt + j * 128, &map_b, n0 + j, k0, bb);
+                    } else {
+                        load(bt, &map_b, k0, n0, bb);
+                    }
                 }
-                if constexpr (kBMn) {
-                    for (int j = 0; j < b_rows; j += 64) load(bt + j * 128, &map_b, n0 + j, k0, bb);
-                } else {
-                    load(bt, &map_b, k0, n0, bb);
-                }
+                __syncwarp();
                 ++issued;
                 if (++s == p.stages) {
                     s = 0;
@@ -649,35 +662,46 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (int t = 0; t < 100000 && in_pair == 0 && !bar_try(&sh.loaded[st], parity); ++t) {}
                 for (int t = 0; t < 100000 && kEight && !bar_try(&sh.raw[st], parity); ++t) {}
             }
-    } else if (warp == 1 && lane == 0 && in_pair == 0) {
+    } else if (warp == 1 && in_pair == 0) {
         constexpr uint32_t fmt = std::is_same<H, __half>::value ? 0 : 1;
         const uint32_t idesc = 1u << 4 | fmt << 7 | fmt << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
                                static_cast<uint32_t>(p.BN >> 3) << 17 | static_cast<uint32_t>(kBM * kBlocks >> 4) << 24;
+        constexpr int kStepA = (kAMn ? 2048 : 32) >> 4, kStepB = (kBMn ? 2048 : 32) >> 4;     // 16 of k in a descriptor
+        const uint64_t ring_a = operand_desc(smem_u32(ring), kAMn), ring_b = operand_desc(smem_u32(ring) + kABytes, kBMn);
+        const int last_steps = (p.K - (p.k_blocks - 1) * kBK + 15) / 16;        // of the last block of k; the others have four
         int s = 0, parity = 0, done = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step, ++done) {
-            const int acc = done & 1;
-            if (done >= 2 && !(ok = bar_wait(&sh.drained[acc], (done / 2 - 1) & 1, gave_up))) break;
+            const uint32_t d = tmem + (done & 1) * p.BN;
+            if (done >= 2 && !(ok = bar_wait(&sh.drained[done & 1], (done / 2 - 1) & 1, gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
                 if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t at = smem_u32(ring + s * stage_bytes);
-                const uint64_t a = operand_desc(at, kAMn), bd = operand_desc(at + kABytes, kBMn);
-                const int steps = (min(kBK, p.K - kb * kBK) + 15) / 16;
-                for (int k = 0; k < steps; ++k)
-                    mma_f16<PAIR>(tmem + acc * p.BN, a + k * ((kAMn ? 2048 : 32) >> 4), bd + k * ((kBMn ? 2048 : 32) >> 4), idesc, kb > kb0 || k > 0);
-                mma_commit<PAIR>(&sh.empty[s]);
+                const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
+                if (elected()) {
+                    mma_f16<PAIR>(d, a, bd, idesc, kb > kb0);
+                    if (kb + 1 < p.k_blocks) {
+#pragma unroll
+                        for (int k = 1; k < 4; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
+                    } else {
+                        for (int k = 1; k < last_steps; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
+                    }
+                    mma_commit<PAIR>(&sh.empty[s]);
+                    if (kb + 1 == kb1) mma_commit<PAIR>(&sh.summed[done & 1]);
+                }
+                __syncwarp();
                 if (++s == p.stages) {
                     s = 0;
                     parity ^= 1;
                 }
             }
-            if (ok) mma_commit<PAIR>(&sh.summed[acc]);
+            if (kb0 == kb1 && elected()) mma_commit<PAIR>(&sh.summed[done & 1]);
+            __syncwarp();
         }
         if (!ok) {
-            mma_commit<PAIR>(&sh.last);
+            if (elected()) mma_commit<PAIR>(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
         }
     } else if (warp >= 4 && warp < 12) {
