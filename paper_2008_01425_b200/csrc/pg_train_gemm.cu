@@ -42,9 +42,17 @@ template <Mode M> constexpr bool kWeightGrads = M == kWeightGrad || M == kWeight
 template <Mode M> constexpr bool kTokenRows = M == kForwardRows || M == kInputGradRows;
 template <Mode M> constexpr bool kAMnMajor = M == kInputGrad || kWeightGrads<M>;
 template <Mode M> constexpr bool kBMnMajor = M == kInputGradRows || kWeightGrads<M>;
-constexpr int kOutBytes = 2048;       // 32 rows x 32 elements on their way out, two per epilogue warp
-constexpr int kOutRing = 8 * 2 * kOutBytes;
-template <Mode M> constexpr int kThreads = M == kWeightGrad8 ? 640 : 384;
+#ifndef ROWWARPS
+#define ROWWARPS 12
+#endif
+constexpr int kRowWarps = ROWWARPS;   // epilogue warps where lanes are tokens
+constexpr int kShares = kRowWarps / 4;
+constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out,
+constexpr int kHeldBytes = 32 * 80;   // and five 16-byte pieces of residuals for each of the rows
+constexpr int kOutWarp = kOutBytes + kHeldBytes;   // (a multiple of 512, the period of the swizzle)
+constexpr int kOutRing = kRowWarps * kOutWarp;
+template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
+template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 256 : 0);
 
 // What happens to D: stored as fp32 (dW), or passed through bias, activation and residual to 16 bits.
 struct Epilogue {
@@ -258,52 +266,78 @@ struct Shared {
     uint64_t loaded[kMaxStages], raw[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
     uint32_t tmem;
     int gave_up;
-    float bias[8][32];
+    float bias[kRowWarps][32];
 };
 
-// Lanes are tokens: a warp takes every other group of 32 columns of its 32 rows.  What belongs to the next group (the
-// residual's pieces, a bias per lane) is on its way while one group is computed, and while the first one's accumulator is
-// waited for.  The result goes to shared memory in the 64-byte swizzle of the output's tensor map and leaves by TMA,
-// which also cuts off what lies outside the matrix.
-template <bool ALIGNED>
-struct RowGroup {              // what a lane holds for a group before its accumulator is read
-    uint4 piece[ALIGNED ? 4 : 5];      // 32 residuals of its row: four 16-byte pieces, five where the row starts between two
-    int off;
-    float bias;
+// Lanes are tokens: a warp takes every third group of 32 columns of its 32 rows.  The residuals of the next group are on
+// their way to shared memory while one group is computed, and while the first one's accumulator is waited for: neighbouring
+// lanes copy neighbouring 16-byte pieces, four of a row or five where it starts between two (a lane that fetched its own row
+// touched 32 lines per load, which cost a quarter of the time).  The result goes through shared memory too, in the
+// 64-byte swizzle of the output's tensor map, and leaves by TMA, which also cuts off what lies outside the matrix.
+struct Residuals {             // of a tile: where a lane's five pieces start, from the tile's first column on
+    const char* base;
+    uint32_t at[5];            // bytes from the first of the warp's 32 rows
+    uint32_t wanted;           // bit i: the row is inside and has such a piece
+    int off;                   // elements from the first piece's start to this lane's own row
 
-    __device__ __forceinline__ void fetch(const Problem& p, int64_t b, int row, int n, int lane, bool wanted) {
-        if (!wanted) return;
-        if (p.ep.residual.data) {
-            const bool live = row < p.M;
-            const uint16_t* res = static_cast<const uint16_t*>(p.ep.residual.data) + b * p.ep.residual.stride + (live ? row : 0) * p.ep.residual.ld;
-            off = ALIGNED ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(res) & 15) / 2;
-            const uint4* at = reinterpret_cast<const uint4*>(res + n - off);
+    __device__ __forceinline__ void start(const Epilogue& ep, int64_t b, int row0, int rows, int n0, int lane) {
+        const int64_t first = b * ep.residual.stride + static_cast<int64_t>(row0) * ep.residual.ld + n0;
+        const uintptr_t from = reinterpret_cast<uintptr_t>(ep.residual.data) + first * 2;
+        base = reinterpret_cast<const char*>(from & ~uintptr_t{15});
+        const uint32_t low = from & 15, ld = static_cast<uint32_t>(ep.residual.ld) * 2;
+        wanted = 0;
 #pragma unroll
-            for (int i = 0; i < (ALIGNED ? 4 : 5); ++i) {
-                piece[i] = make_uint4(0, 0, 0, 0);
-                if (live && n - off + 8 * i < p.N && (i < 4 || off > 0)) piece[i] = at[i];
-            }
+        for (int i = 0; i < 5; ++i) {
+            const uint32_t k = lane + 32 * i, r = k / 5, c = k - r * 5, start_at = low + r * ld;
+            at[i] = (start_at & ~15u) + c * 16;
+            if (row0 + static_cast<int>(r) < rows && (c < 4 || (start_at & 15) != 0)) wanted |= 1u << i;
         }
-        bias = p.ep.bias && n + lane < p.N ? p.ep.bias[b * p.ep.bias_stride + n + lane] : 0.0f;
+        off = static_cast<int>(low + lane * ld & 15) / 2;
+    }
+    // Copies the pieces of the 32 columns from n0 + j on; `left`: columns from there to the matrix's end.
+    __device__ __forceinline__ void fetch(uint8_t* held, int j, int left, int lane) const {
+        const char* from = base + 2 * j;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const uint32_t k = lane + 32 * i, c = k - k / 5 * 5;
+            // a row's piece c holds its columns from 8 c - (up to 7) on; the last ones of a row may have none left
+            if ((wanted >> i & 1) && static_cast<int>(8 * c) < left + 7)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(held) + k * 16), "l"(from + at[i]) : "memory");
+        }
     }
 };
-template <typename H, int ACT, bool ALIGNED>
-__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* ring, float* s_bias, int64_t b, int m0,
-                                           int n0, int half, int quarter, int lane, int& flip, RowGroup<ALIGNED>& next) {
+template <typename H, int ACT>
+__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, float* s_bias, int64_t b, int m0,
+                                           int n0, int share, int quarter, int lane, const Residuals& residuals, float& next_bias) {
     const Epilogue& ep = p.ep;
+    uint8_t* held = out + kOutBytes;
     const int row = m0 + quarter * 32 + lane;
     const bool live = row < p.M;
     const int end = min(p.BN, p.N - n0);
     const bool add_residual = ep.residual.data != nullptr;
-    for (int j = half * 32; j < end; j += 64) {
+    for (int j = share * 32; j < end; j += kShares * 32) {
         const int n = n0 + j;
-        const RowGroup<ALIGNED> here = next;
-        next.fetch(p, b, row, n + 64, lane, j + 64 < end);
-        uint8_t* out = ring + flip * kOutBytes;
-        flip ^= 1;
-        s_bias[lane] = here.bias;                              // the same 32 numbers for all lanes
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the copy before the last has been read
+        uint4 piece[5];
+        if (add_residual) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 5; ++i) piece[i] = *reinterpret_cast<const uint4*>(held + (lane * 5 + i) * 16);
+            if (!p.residual_aligned) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Oct o = cut(piece[i], piece[i + 1], residuals.off);
+                    piece[i] = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
+                }
+            }
+        }
+        s_bias[lane] = next_bias;                              // the same 32 numbers for all lanes
         __syncwarp();
+        const int next = j + kShares * 32;
+        if (next < end) {
+            if (add_residual) residuals.fetch(held, next, p.N - n0 - next, lane);
+            next_bias = ep.bias && n0 + next + lane < p.N ? ep.bias[b * ep.bias_stride + n0 + next + lane] : 0.0f;
+        }
         const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j;
         if (ep.z8.values) {
             F2 v[4][4];
@@ -352,15 +386,14 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 F2 hi = activate<ACT>(add(pair(acc[4 * i + 2], acc[4 * i + 3]), pair(f.z, f.w)));
                 if (add_residual) {
                     const int k = 2 * h + i / 2;
-                    const uint4& w0 = here.piece[k];
-                    const Oct o = ALIGNED ? Oct{{w0.x, w0.y, w0.z, w0.w}} : cut(w0, here.piece[k + !ALIGNED], here.off);
-                    lo = add(lo, Elem<H>::up2(o.w[2 * (i & 1)]));
-                    hi = add(hi, Elem<H>::up2(o.w[2 * (i & 1) + 1]));
+                    lo = add(lo, Elem<H>::up2(i & 1 ? piece[k].z : piece[k].x));
+                    hi = add(hi, Elem<H>::up2(i & 1 ? piece[k].w : piece[k].y));
                 }
                 w[8 * h + 2 * i] = Elem<H>::down2(lo);
                 w[8 * h + 2 * i + 1] = Elem<H>::down2(hi);
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last group's copy has been read
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -573,7 +606,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&sh.summed[i], 1);
-            bar_init(&sh.drained[i], 8 * kBlocks);
+            bar_init(&sh.drained[i], kEpilogueWarps<MODE> * kBlocks);
         }
         bar_init(&sh.last, 1);
         sh.gave_up = 0;
@@ -704,43 +737,44 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (elected()) mma_commit<PAIR>(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
         }
-    } else if (warp >= 4 && warp < 12) {
+    } else if (warp >= 4 && warp < 4 + kEpilogueWarps<MODE>) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t drained[2] = {PAIR ? first_of_pair(&sh.drained[0]) : 0u, PAIR ? first_of_pair(&sh.drained[1]) : 0u};
         // the body for every combination that the epilogue is compiled for
         with_activation<H, MODE>(p.ep.activation, [&](auto act) {
-            auto tiles = [&](auto residual_aligned) {
-                constexpr bool kAligned = decltype(residual_aligned)::value;
-                RowGroup<kAligned> next;
-                int done = 0;
-                [[maybe_unused]] int flip = 0;
-                for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
-                    const int acc = done & 1;
-                    int64_t b;
-                    int m0, n0;
-                    place(tile, b, m0, n0);
-                    if constexpr (kTokenRows<MODE>)
-                        next.fetch(p, b, m0 + quarter * 32 + lane, n0 + half * 32, lane, half * 32 < min(p.BN, p.N - n0));
-                    if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if constexpr (kTokenRows<MODE>)
-                        empty_rows<H, decltype(act)::value, kAligned>(p, &map_out, tmem + acc * p.BN, ring + p.stages * stage_bytes + (warp - 4) * 2 * kOutBytes,
-                                                                      sh.bias[warp - 4], b, m0, n0, half, quarter, lane, flip, next);
-                    else
-                        empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b,
-                                                                   m0, n0, half, quarter, lane);
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) bar_arrive_at(drained[acc]);
-                        else bar_arrive(&sh.drained[acc]);
-                    }
+            [[maybe_unused]] uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutWarp;
+            [[maybe_unused]] float next_bias = 0.0f;
+            int done = 0;
+            for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
+                const int acc = done & 1;
+                int64_t b;
+                int m0, n0;
+                place(tile, b, m0, n0);
+                [[maybe_unused]] Residuals residuals;
+                if constexpr (kTokenRows<MODE>) {
+                    const int j = half * 32;
+                    if (p.ep.residual.data) residuals.start(p.ep, b, m0 + quarter * 32, p.M, n0, lane);
+                    if (p.ep.residual.data && j < min(p.BN, p.N - n0)) residuals.fetch(out + kOutBytes, j, p.N - n0 - j, lane);
+                    next_bias = p.ep.bias && n0 + j + lane < p.N ? p.ep.bias[b * p.ep.bias_stride + n0 + j + lane] : 0.0f;
                 }
-            };
-            if (!kTokenRows<MODE> || p.residual_aligned) tiles(std::true_type{});
-            else tiles(std::false_type{});
+                if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                __syncwarp();
+                if constexpr (kTokenRows<MODE>)
+                    empty_rows<H, decltype(act)::value>(p, &map_out, tmem + acc * p.BN, out, sh.bias[warp - 4], b, m0, n0, half, quarter, lane, residuals,
+                                                        next_bias);
+                else
+                    empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0,
+                                                               n0, half, quarter, lane);
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) bar_arrive_at(drained[acc]);
+                    else bar_arrive(&sh.drained[acc]);
+                }
+            }
         });
+        asm volatile("cp.async.wait_all;" ::: "memory");
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (kEight && warp >= 12) {
         // thread: row k = r of the stage, 64 of its 128 values (two blocks).  The 16-byte pieces are taken in
@@ -985,6 +1019,8 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
                             : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
 }
 
+constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are addressed with 32 bits
+
 // Pairs of blocks multiply 256-row tiles; one row more than a block's 128 has to be there, and tiles for about half of
 // the GPU: with fewer, single blocks that share the k of a tile finish earlier.
 bool enough_for_pairs(int64_t batch, int64_t M, int64_t N) {
@@ -1035,7 +1071,7 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
     if (rc != PG_OK) return rc;
-    if (enough_for_pairs(a.batch, a.tokens, a.out_features) && aligned(a.y, a.batch, a.tokens))
+    if (enough_for_pairs(a.batch, a.tokens, a.out_features) && aligned(a.y, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
         return run_product<kForwardRows, true>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
     return run_product<kForward, false>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
@@ -1066,7 +1102,7 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
     if (rc != PG_OK) return rc;
-    if (enough_for_pairs(a.batch, a.tokens, a.in_features) && aligned(a.dx, a.batch, a.tokens))
+    if (enough_for_pairs(a.batch, a.tokens, a.in_features) && aligned(a.dx, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
         return run_product<kInputGradRows, true>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
     return run_product<kInputGrad, false>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
