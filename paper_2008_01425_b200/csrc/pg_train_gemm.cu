@@ -33,7 +33,6 @@ constexpr int kBK = 64;               // elements of k in a stage: one 128-byte 
 constexpr int kMaxStages = 12;
 constexpr int kSmemBytes = 232448;    // what a block may have
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kRawBytes = kBM * kBK;  // an 8-bit A stage before it is widened
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
 constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
 
@@ -70,8 +69,9 @@ struct Problem {
     int64_t tiles;
     int a_shared, b_shared;    // operand is the same for every worker
     int residual_aligned;      // its rows start on 16-byte boundaries
-    const uint8_t* scales;     // of an 8-bit A
-    int64_t scale_ld, scale_stride;
+    const int8_t* values;      // an 8-bit A
+    const uint8_t* scales;
+    int64_t value_ld, value_stride, scale_ld, scale_stride;
 };
 
 __device__ unsigned g_training_error;   // a bounded wait gave up; read and cleared by pg_training_status
@@ -263,7 +263,7 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
 }
 
 struct Shared {
-    uint64_t loaded[kMaxStages], raw[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
+    uint64_t loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
     uint32_t tmem;
     int gave_up;
     float bias[kRowWarps][32];
@@ -593,14 +593,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
     const int b_rows = p.BN / kBlocks;                  // of B in this block's shared memory
     const int b_bytes = (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
-    const int stage_bytes = kABytes + b_bytes + (kEight ? kRawBytes : 0);
+    const int stage_bytes = kABytes + b_bytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
     const int in_pair = PAIR ? blockIdx.x & 1 : 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&sh.loaded[s], 1);
-            bar_init(&sh.raw[s], 1);
             bar_init(&sh.widened[s], 4 * kBlocks);
             bar_init(&sh.empty[s], 1);
         }
@@ -666,9 +665,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         if constexpr (PAIR) tma_load_pair(dst, map, x, y, z, at);
                         else tma_load(dst, map, x, y, z, &sh.loaded[s]);
                     };
-                    if constexpr (kEight) {
-                        bar_expect(&sh.raw[s], kRawBytes);
-                        tma_load(bt + b_bytes, &map_a, m0, k0, ba, &sh.raw[s]);
+                    if constexpr (kEight) {            // A comes from the widening warps
                     } else if constexpr (kAMn) {
                         load(a, &map_a, m0, k0, ba);
                         load(a + 8192, &map_a, m0 + 64, k0, ba);
@@ -693,7 +690,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int64_t i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i) {
                 const int st = static_cast<int>(i % p.stages), parity = static_cast<int>(i / p.stages) & 1;
                 for (int t = 0; t < 100000 && in_pair == 0 && !bar_try(&sh.loaded[st], parity); ++t) {}
-                for (int t = 0; t < 100000 && kEight && !bar_try(&sh.raw[st], parity); ++t) {}
             }
     } else if (warp == 1 && in_pair == 0) {
         constexpr uint32_t fmt = std::is_same<H, __half>::value ? 0 : 1;
@@ -777,64 +773,104 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (kEight && warp >= 12) {
-        // thread: row k = r of the stage, 64 of its 128 values (two blocks).  The 16-byte pieces are taken in
-        // an order that puts the 8 threads of a shared-memory phase on different banks, reading and writing.
+        // Eight lanes take the 128 values of a row (one k) of the stage, 16 each, and a thread four rows.  They come from
+        // memory to registers, two of this half's stages ahead: through shared memory they would cost as much of its
+        // bandwidth again as the tensor cores' reading of A, and it is what limits these products.
         const int mine = (warp - 12) >> 2;             // of every two stages
-        const int r = (threadIdx.x & 127) >> 1, h = threadIdx.x & 1;
+        const int c = lane & 7, r0 = (warp & 3) * 4 + (lane >> 3);     // rows r0, r0 + 16, r0 + 32, r0 + 48
         const uint32_t widened = PAIR ? first_of_pair(&sh.widened[0]) : smem_u32(&sh.widened[0]);
-        int s = 0, parity = 0, turn = 0;
-        bool ok = true;
-        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
+        struct Stage {
+            uint4 v[4];
+            uint32_t s[4];
+        } held[2];
+        // where this half's next stage to fetch is
+        int64_t at_tile = first;
+        int at_kb = kb0;
+        const int8_t* v_at = nullptr;
+        const uint8_t* s_at = nullptr;
+        bool inside = false;
+        auto enter = [&] {                             // the tile at_tile
+            if (at_tile >= p.tiles) return;
             int64_t b;
             int m0, n0;
-            place(tile, b, m0, n0);
-            const uint8_t* scales = p.scales + b * p.scale_stride + (m0 + h * 64) / kBlock8;
-            const bool one = m0 + h * 64 < p.M, two = m0 + h * 64 + 32 < p.M;
-            auto fetch = [&](int kb, uint32_t& s0, uint32_t& s1) {
-                const int64_t k = static_cast<int64_t>(kb) * kBK + r;
-                const bool in = kb < kb1 && k < p.K;
-                s0 = in && one ? scales[k * p.scale_ld] : 0u;
-                s1 = in && two ? scales[k * p.scale_ld + 1] : 0u;
-            };
-            uint32_t s0, s1;
-            fetch(kb0 + (turn ^ mine), s0, s1);
-            for (int kb = kb0; kb < kb1; ++kb, turn ^= 1) {
-                if (turn == mine) {
-                    uint32_t t0, t1;
-                    fetch(kb + 2, t0, t1);
-                    if (!(ok = bar_wait(&sh.raw[s], parity, gave_up))) break;
-                    uint8_t* a = ring + s * stage_bytes;
-                    const uint8_t* raw = a + kABytes + b_bytes + r * 128 + h * 64;
-                    const uint32_t f0 = scale_pair<H>(s0), f1 = scale_pair<H>(s1);
-                    uint4 w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(raw + ((i + (r & 3) + 2 * h) & 3) * 16);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = (i + (r & 3) + 2 * h) & 3;
-                        const uint32_t f = c < 2 ? f0 : f1;
-                        uint4 o0, o1;
-                        widen4<H>(w[i].x, f, o0.x, o0.y);
-                        widen4<H>(w[i].y, f, o0.z, o0.w);
-                        widen4<H>(w[i].z, f, o1.x, o1.y);
-                        widen4<H>(w[i].w, f, o1.z, o1.w);
-                        uint8_t* row = a + h * 8192 + r * 128;
-                        *reinterpret_cast<uint4*>(row + (((2 * c) ^ (r & 7)) << 4)) = o0;
-                        *reinterpret_cast<uint4*>(row + (((2 * c + 1) ^ (r & 7)) << 4)) = o1;
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) bar_arrive_at(widened + s * 8);
-                        else bar_arrive(&sh.widened[s]);
-                    }
-                    s0 = t0;
-                    s1 = t1;
+            place(at_tile, b, m0, n0);
+            const int m = m0 + c * 16;
+            inside = m < p.M;
+            v_at = p.values + b * p.value_stride + m;
+            s_at = p.scales + b * p.scale_stride + m / kBlock8;
+        };
+        auto skip = [&](int n) {
+            at_kb += n;
+            if (at_kb >= kb1) {
+                while (at_kb >= kb1) {
+                    at_kb -= kb1 - kb0;
+                    at_tile += step;
                 }
-                if (++s == p.stages) {
-                    s = 0;
-                    parity ^= 1;
+                enter();
+            }
+        };
+        auto fetch = [&](Stage& to) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                to.v[j] = make_uint4(0, 0, 0, 0);
+                to.s[j] = 0;
+            }
+            const int64_t k = static_cast<int64_t>(at_kb) * kBK + r0;
+            if (at_tile < p.tiles && inside) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k + 16 * j < p.K) {
+                        to.v[j] = *reinterpret_cast<const uint4*>(v_at + (k + 16 * j) * p.value_ld);
+                        to.s[j] = s_at[(k + 16 * j) * p.scale_ld];
+                    }
+            }
+            skip(2);
+        };
+        const int64_t my_tiles = p.tiles > first ? (p.tiles - first + step - 1) / step : 0;
+        const int64_t left = my_tiles * (kb1 - kb0);   // stages of this block
+        if (left > 0) {
+            enter();
+            skip(mine);
+            fetch(held[0]);
+            fetch(held[1]);
+        }
+        int s = mine % p.stages, turn = mine / p.stages;
+        bool ok = true;
+        for (int64_t i = mine; ok && i < left; i += 4) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (i + 2 * u >= left) break;
+                Stage& here = held[u];
+                if (turn > 0 && !(ok = bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up))) break;
+                uint8_t* a = ring + s * stage_bytes + (c >> 2) * 8192;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = r0 + 16 * j;
+                    const uint32_t f = scale_pair<H>(here.s[j]);
+                    uint4 o[2];
+                    widen4<H>(here.v[j].x, f, o[0].x, o[0].y);
+                    widen4<H>(here.v[j].y, f, o[0].z, o[0].w);
+                    widen4<H>(here.v[j].z, f, o[1].x, o[1].y);
+                    widen4<H>(here.v[j].w, f, o[1].z, o[1].w);
+                    // the lanes of the upper 64 values take their two pieces the other way round: eight lanes, eight banks
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int w = q ^ (c >> 2);
+                        *reinterpret_cast<uint4*>(a + r * 128 + (((2 * (c & 3) + w) ^ (r & 7)) << 4)) = w ? o[1] : o[0];
+                    }
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) bar_arrive_at(widened + s * 8);
+                    else bar_arrive(&sh.widened[s]);
+                }
+                s += 2;
+                if (s >= p.stages) {
+                    s -= p.stages;
+                    ++turn;
+                }
+                fetch(here);
             }
         }
     }
@@ -893,22 +929,20 @@ EncodeFn encoder() {
     return fn;
 }
 
-// A matrix as TMA sees it: `rows` rows of `cols` elements per worker, boxes of box_rows x box_bytes, swizzled (8-bit: not).
-bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_bytes, int box_rows) {
+// A matrix as TMA sees it: `rows` rows of `cols` 16-bit elements per worker, boxes of box_rows x box_bytes, swizzled over them.
+bool make_map(CUtensorMap& map, int dtype, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_bytes, int box_rows) {
     EncodeFn fn = encoder();
     if (!fn) return false;
-    const int size = eight ? 1 : 2;
     const bool shared = batch > 1 && m.stride == 0;
-    const int64_t unit = 16 / size;
-    const int64_t ld = rows > 1 ? m.ld : (cols + unit - 1) / unit * unit;
+    const int64_t ld = rows > 1 ? m.ld : (cols + 7) / 8 * 8;
     const int64_t stride = batch > 1 && !shared ? m.stride : ld * rows;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(shared ? 1 : batch)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * size), static_cast<cuuint64_t>(stride * size)};
-    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / size), static_cast<cuuint32_t>(box_rows), 1};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(stride * 2)};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / 2), static_cast<cuuint32_t>(box_rows), 1};
     const cuuint32_t one[3] = {1, 1, 1};
-    const CUtensorMapDataType type = eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    return fn(&map, type, 3, m.data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, eight ? CU_TENSOR_MAP_SWIZZLE_NONE : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(&map, dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, m.data, dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Can TMA read the operand where it is?
@@ -996,22 +1030,25 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     if (!PAIR)
         while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
     const int b_rows = p.BN / kBlocks;
-    const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2 + (MODE == kWeightGrad8 ? kRawBytes : 0);
+    const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
     const int rest = kRows ? kOutRing : 0;
     p.stages = std::min(kMaxStages, (kSmemBytes - 3072 - rest) / stage);
     p.a_shared = A.stride == 0;
     p.b_shared = B.stride == 0;
     p.residual_aligned = access_width({&ep.residual}, batch) == 8;
     if (a8) {
+        p.values = a8->values;
+        p.value_ld = a8->ld;
+        p.value_stride = a8->stride;
         p.scales = a8->scales;
         p.scale_ld = a8->scale_ld;
         p.scale_stride = a8->scale_stride;
     }
     CUtensorMap map_a = {}, map_b = {}, map_out = {};
     if (K > 0) {
-        const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
-                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
-                          (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
+        const bool fine = (MODE == kWeightGrad8 || make_map(map_a, dtype, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM)) &&
+                          make_map(map_b, dtype, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
+                          (!kRows || make_map(map_out, dtype, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
     const int smem = p.stages * stage + rest + 1024;
@@ -1119,10 +1156,11 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
     const int dev = current_device();
     const bool eight = a.x8.values != nullptr;
     if (!sizes_ok(a.dtype, a.batch, a.tokens, a.in_features, a.out_features)) return PG_ERR_INVALID;
-    if (eight == (a.x.data != nullptr) && int64_t{a.batch} * a.tokens > 0) return PG_ERR_INVALID;
+    const bool any = int64_t{a.batch} * a.tokens > 0;              // without tokens there is no x to be had
+    if (any && eight == (a.x.data != nullptr)) return PG_ERR_INVALID;
     if (!matrix_ok(a.dz, a.batch, a.tokens, a.out_features, 2, false, dev)) return PG_ERR_INVALID;
-    if (eight ? !matrix8_ok(a.x8, a.batch, a.tokens, a.in_features, false, dev)
-              : !matrix_ok(a.x, a.batch, a.tokens, a.in_features, 2, false, dev))
+    if (any && (eight ? !matrix8_ok(a.x8, a.batch, a.tokens, a.in_features, false, dev)
+                      : !matrix_ok(a.x, a.batch, a.tokens, a.in_features, 2, false, dev)))
         return PG_ERR_INVALID;
     if (!matrix_ok(a.dweight, a.batch, a.out_features, a.in_features, 4, true, dev)) return PG_ERR_INVALID;
     size_t need = 0;

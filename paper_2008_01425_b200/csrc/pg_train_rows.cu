@@ -548,10 +548,11 @@ int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t 
     const int dev = current_device();
     const bool eight = a.h8.values != nullptr;
     if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1)) return PG_ERR_INVALID;
-    if (eight == (a.h.data != nullptr) && int64_t{a.batch} * a.tokens > 0) return PG_ERR_INVALID;
+    const bool any = int64_t{a.batch} * a.tokens > 0;              // without tokens there is no h to be had
+    if (any && eight == (a.h.data != nullptr)) return PG_ERR_INVALID;
     if (!matrix_ok(a.dy, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
-    if (eight ? !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, false, dev)
-              : !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, false, dev))
+    if (any && (eight ? !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, false, dev)
+              : !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, false, dev)))
         return PG_ERR_INVALID;
     if (a.tokens > 0 && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, false, dev)) return PG_ERR_INVALID;
     if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;

@@ -98,108 +98,131 @@ class NormOutput(NamedTuple):
     rstd: torch.Tensor
 
 
-def _lib() -> ctypes.CDLL:
-    return load_library()
-
-
 def _refuse(where: str, why: str):
     raise ValueError("%s: %s" % (where, why))
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_empty = torch.empty_strided
+_NONE = pg_matrix(None, 0, 0)
+_NONE8 = pg_matrix8(None, None, 0, 0, 0, 0)
+
+
 class _Call:
-    """Shape and device of one call, taken from its first tensor; checks the others against it."""
+    """Shape, device and stream of one call, taken from its first tensor; checks the others against it.  (Small calls cost
+    what this costs, so it asks torch for as little as it can.)"""
+
+    __slots__ = ("where", "dtype", "kind", "index", "device", "single", "batch", "tokens", "cols", "handle", "other")
 
     def __init__(self, where: str, first, stream):
         dtype = getattr(first, "dtype", None)
-        first = first.values if isinstance(first, Checkpoint8) else first
-        if not isinstance(first, torch.Tensor) or not first.is_cuda or first.dim() not in (2, 3) or dtype not in _DTYPES:
-            _refuse(where, "expected a bf16 or fp16 CUDA tensor of two or three dimensions")
-        if max(first.shape) > 1 << 30:
-            _refuse(where, "shape %s is too large" % (tuple(first.shape),))
-        self.where, self.device, self.dtype = where, first.device, dtype
-        self.single = first.dim() == 2
-        self.batch = 1 if self.single else first.shape[0]
-        self.tokens, self.cols = first.shape[-2:]
-        current = torch.cuda.current_stream(self.device)
-        self.other = None
-        if stream is None:
-            self.handle = current.cuda_stream
+        if type(first) is Checkpoint8:
+            first = first.values
+        kind = _DTYPES.get(dtype)
+        if kind is None or not isinstance(first, torch.Tensor) or not first.is_cuda:
+            _refuse(where, "expected a bf16 or fp16 CUDA tensor")
+        shape = first.shape
+        if len(shape) == 3:
+            self.single = False
+            self.batch, self.tokens, self.cols = shape
+        elif len(shape) == 2:
+            self.single = True
+            self.batch = 1
+            self.tokens, self.cols = shape
         else:
-            self.handle = stream if isinstance(stream, int) else stream.cuda_stream
-            if self.handle != current.cuda_stream:
-                self.other = torch.cuda.ExternalStream(self.handle, device=self.device)
+            _refuse(where, "expected two or three dimensions")
+        if self.batch > 65535 or self.tokens > 1 << 30 or self.cols > 1 << 30:
+            _refuse(where, "shape %s is too large" % (tuple(shape),))
+        self.where, self.dtype, self.kind = where, dtype, kind
+        self.device = first.device
+        self.index = first.get_device()
+        self.handle, self.other = _raw_stream(self.index), None
+        if stream is not None:
+            handle = stream if isinstance(stream, int) else stream.cuda_stream
+            if handle != self.handle:
+                self.handle, self.other = handle, torch.cuda.ExternalStream(handle, device=self.device)
+
+    def matrix(self, t, rows: int, cols: int, dtype, name: str) -> pg_matrix:
+        if t is None:
+            return _NONE
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != self.index:
+            _refuse(self.where, "%s must be a %s tensor on %s" % (name, dtype, self.device))
+        shape, strides = t.shape, t.stride()
+        if len(shape) == 3 and shape == (self.batch, rows, cols):
+            stride, ld, one = strides
+        elif self.single and shape == (rows, cols):
+            ld, one = strides
+            stride = 0
+        else:
+            _refuse(self.where, "%s has shape %s, expected %s" % (name, tuple(shape), (rows, cols) if self.single else (self.batch, rows, cols)))
+        if one != 1 and cols > 1:
+            _refuse(self.where, "%s must have its last dimension contiguous" % name)
+        return pg_matrix(t.data_ptr(), ld if rows > 1 else max(ld, cols), stride if self.batch > 1 else 0)
+
+    def matrix8(self, c, rows: int, cols: int, name: str) -> pg_matrix8:
+        if c is None:
+            return _NONE8
+        if type(c) is not Checkpoint8 or c.dtype is not self.dtype:
+            _refuse(self.where, "%s must be a checkpoint of %s" % (name, self.dtype))
+        v = self.matrix(c.values, rows, cols, torch.int8, name + ".values")
+        s = self.matrix(c.scales, rows, (cols + BLOCK8 - 1) // BLOCK8, torch.uint8, name + ".scales")
+        return pg_matrix8(v.data, s.data, v.ld if rows > 1 else (v.ld + 15) // 16 * 16, v.stride, s.ld, s.stride)
+
+    def vector(self, t, n: int, name: str):
+        """(pointer, stride) of an fp32 (workers, n) tensor; (n,) for one worker or shared by all."""
+        if t is None:
+            return None, 0
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.get_device() != self.index:
+            _refuse(self.where, "%s must be an fp32 tensor on %s" % (name, self.device))
+        shape, strides = t.shape, t.stride()
+        if shape != (self.batch, n) and shape != (n,):
+            _refuse(self.where, "%s has shape %s, expected %s" % (name, tuple(shape), (self.batch, n)))
+        if n > 1 and strides[-1] != 1:
+            _refuse(self.where, "%s must have its last dimension contiguous" % name)
+        return t.data_ptr(), strides[0] if len(shape) == 2 and self.batch > 1 else 0
 
     def _own(self, t: torch.Tensor) -> torch.Tensor:
         if self.other is not None:
             t.record_stream(self.other)
         return t
 
-    def matrix(self, t: Optional[torch.Tensor], rows: int, cols: int, dtype=None, name: str = "") -> pg_matrix:
-        if t is None:
-            return pg_matrix(None, cols, 0)
-        dtype = dtype or self.dtype
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != dtype:
-            _refuse(self.where, "%s must be a %s tensor on %s" % (name, dtype, self.device))
-        want = (rows, cols) if self.single else (self.batch, rows, cols)
-        if t.dim() == 3 and self.single and t.shape[0] == 1:
-            want = (1, rows, cols)
-        if tuple(t.shape) != want:
-            _refuse(self.where, "%s has shape %s, expected %s" % (name, tuple(t.shape), want))
-        s = t.stride()
-        if cols > 1 and s[-1] != 1:
-            _refuse(self.where, "%s must have its last dimension contiguous" % name)
-        ld = s[-2] if rows > 1 else max(cols, s[-2] if s[-2] >= cols else cols)
-        return pg_matrix(t.data_ptr(), ld, s[0] if t.dim() == 3 and self.batch > 1 else 0)
+    def empty(self, rows: int, cols: int, dtype, unit: int) -> torch.Tensor:
+        """Rows start on 16-byte boundaries: a multiple of `unit` elements."""
+        ld = (cols + unit - 1) // unit * unit
+        if self.single:
+            return self._own(_empty((rows, cols), (ld, 1), dtype=dtype, device=self.device))
+        return self._own(_empty((self.batch, rows, cols), (rows * ld, ld, 1), dtype=dtype, device=self.device))
 
-    def matrix8(self, c: Optional[Checkpoint8], rows: int, cols: int, name: str = "") -> pg_matrix8:
-        if c is None:
-            return pg_matrix8(None, None, (cols + 15) // 16 * 16, 0, (cols + 31) // 32, 0)
-        if c.dtype != self.dtype:
-            _refuse(self.where, "%s is a checkpoint of %s, expected %s" % (name, c.dtype, self.dtype))
-        v = self.matrix(c.values, rows, cols, torch.int8, name + ".values")
-        s = self.matrix(c.scales, rows, (cols + BLOCK8 - 1) // BLOCK8, torch.uint8, name + ".scales")
-        if rows <= 1:
-            v.ld = (v.ld + 15) // 16 * 16
-        return pg_matrix8(v.data, s.data, v.ld, v.stride, s.ld, s.stride)
-
-    def vector(self, t: Optional[torch.Tensor], n: int, name: str):
-        """(pointer, stride) of an fp32 (workers, n) tensor; (n,) for one worker or shared by all."""
-        if t is None:
-            return None, 0
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.float32 or t.shape[-1] != n \
-                or t.dim() not in (1, 2) or (t.dim() == 2 and t.shape[0] != self.batch) or (n > 1 and t.stride(-1) != 1):
-            _refuse(self.where, "%s must be an fp32 tensor of shape (%d, %d) on %s" % (name, self.batch, n, self.device))
-        return t.data_ptr(), t.stride(0) if t.dim() == 2 and self.batch > 1 else 0
-
-    def empty(self, rows: int, cols: int, dtype=None) -> torch.Tensor:
-        """Rows start on 16-byte boundaries."""
-        dtype = dtype or self.dtype
-        unit = 4 if dtype == torch.float32 else 16 if dtype == torch.int8 else 8
-        t = self._own(torch.empty((self.batch, rows, (cols + unit - 1) // unit * unit), dtype=dtype, device=self.device))
-        if t.shape[-1] != cols:
-            t = t[..., :cols]
-        return t[0] if self.single else t
+    def like(self, rows: int, cols: int) -> torch.Tensor:
+        return self.empty(rows, cols, self.dtype, 8)
 
     def empty8(self, rows: int, cols: int) -> Checkpoint8:
-        scales = self._own(torch.empty((self.batch, rows, (cols + BLOCK8 - 1) // BLOCK8), dtype=torch.uint8, device=self.device))
-        return Checkpoint8(self.empty(rows, cols, torch.int8), scales[0] if self.single else scales, self.dtype)
+        return Checkpoint8(self.empty(rows, cols, torch.int8, 16), self.empty(rows, (cols + BLOCK8 - 1) // BLOCK8, torch.uint8, 1), self.dtype)
 
-    def flat(self, *shape: int, zero: bool = False) -> torch.Tensor:
-        shape = shape[1:] if self.single else shape
-        return self._own((torch.zeros if zero else torch.empty)(shape, dtype=torch.float32, device=self.device))
+    def flat(self, n: int) -> torch.Tensor:
+        """fp32 (workers, n), or (n,) for one worker."""
+        if self.single:
+            return self._own(_empty((n,), (1,), dtype=torch.float32, device=self.device))
+        return self._own(_empty((self.batch, n), (n, 1), dtype=torch.float32, device=self.device))
 
     def run(self, fn, args, size_fn=None) -> None:
-        with torch.cuda.device(self.device):
-            if size_fn is None:
-                _check(fn(ctypes.byref(args), _vp(self.handle)), self.where)
-                return
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.run(fn, args, size_fn)
+        args = ctypes.byref(args)
+        if size_fn is None:
+            status = fn(args, self.handle)
+        else:
             need = ctypes.c_size_t(0)
-            _check(size_fn(ctypes.byref(args), ctypes.byref(need)), self.where)
-            scratch = None
-            if need.value:
-                scratch = self._own(torch.empty(need.value, dtype=torch.uint8, device=self.device))
-            _check(fn(ctypes.byref(args), _vp(scratch.data_ptr() if need.value else None), ctypes.c_size_t(need.value),
-                      _vp(self.handle)), self.where)
+            status = size_fn(args, ctypes.byref(need))
+            if status == 0:
+                if need.value:
+                    scratch = self._own(_empty((need.value,), (1,), dtype=torch.uint8, device=self.device))
+                    status = fn(args, scratch.data_ptr(), need.value, self.handle)
+                else:
+                    status = fn(args, None, 0, self.handle)
+        if status != 0:
+            _check(status, self.where)
 
 
 def _activation(where: str, name: str) -> int:
@@ -215,17 +238,17 @@ def pg_add_rms_norm(x, gain=None, residual=None, eps: float = 1e-5, eight_bit: b
     residual, h is x itself."""
     c = _Call("pg_add_rms_norm", x, stream)
     t, n = c.tokens, c.cols
-    h = x if residual is None else c.empty(t, n)
-    y = c.empty(t, n) if out is None else out
+    h = x if residual is None else c.like(t, n)
+    y = c.like(t, n) if out is None else out
     y8 = c.empty8(t, n) if eight_bit else None
     h8 = c.empty8(t, n) if save_h8 else None
-    rstd = c.flat(c.batch, t)
+    rstd = c.flat(t)
     gp, gs = c.vector(gain, n, "gain")
-    args = pg_norm_args(_DTYPES[c.dtype], c.batch, t, n, eps, c.matrix(x, t, n, name="x"),
-                        c.matrix(residual, t, n, name="residual"), gp, gs,
-                        c.matrix(None if residual is None else h, t, n, name="h"), c.matrix(y, t, n, name="out"),
-                        c.matrix8(y8, t, n), c.matrix8(h8, t, n), rstd.data_ptr())
-    c.run(_lib().pg_add_rms_norm, args)
+    args = pg_norm_args(c.kind, c.batch, t, n, eps, c.matrix(x, t, n, c.dtype, "x"),
+                        c.matrix(residual, t, n, c.dtype, "residual"), gp, gs,
+                        c.matrix(None if residual is None else h, t, n, c.dtype, "h"), c.matrix(y, t, n, c.dtype, "out"),
+                        c.matrix8(y8, t, n, "y8"), c.matrix8(h8, t, n, "h8"), rstd.data_ptr())
+    c.run(load_library().pg_add_rms_norm, args)
     return NormOutput(h, y, y8, h8, rstd)
 
 
@@ -238,18 +261,18 @@ def pg_add_rms_norm_grad(dy, h: Union[torch.Tensor, Checkpoint8], rstd, gain=Non
     t, n = c.tokens, c.cols
     if accumulate and gain_grad is None:
         _refuse(c.where, "accumulate needs gain_grad")
-    dx = c.empty(t, n) if out is None else out
-    dgain = c.flat(c.batch, n) if gain_grad is None else gain_grad
+    dx = c.like(t, n) if out is None else out
+    dgain = c.flat(n) if gain_grad is None else gain_grad
     if not isinstance(rstd, torch.Tensor) or rstd.device != c.device or rstd.dtype != torch.float32 or rstd.numel() != c.batch * t \
             or not rstd.is_contiguous():
         _refuse(c.where, "rstd must be a contiguous fp32 tensor of %d x %d on %s" % (c.batch, t, c.device))
     eight = isinstance(h, Checkpoint8)
     gp, gs = c.vector(gain, n, "gain")
     dp, ds = c.vector(dgain, n, "gain_grad")
-    args = pg_norm_grad_args(_DTYPES[c.dtype], c.batch, t, n, int(accumulate), c.matrix(dy, t, n, name="dy"),
-                             c.matrix(None if eight else h, t, n, name="h"), c.matrix8(h if eight else None, t, n, "h"),
-                             rstd.data_ptr(), gp, gs, c.matrix(dh, t, n, name="dh"), c.matrix(dx, t, n, name="out"), dp, ds)
-    c.run(_lib().pg_add_rms_norm_grad, args, _lib().pg_add_rms_norm_grad_workspace_bytes)
+    args = pg_norm_grad_args(c.kind, c.batch, t, n, int(accumulate), c.matrix(dy, t, n, c.dtype, "dy"),
+                             c.matrix(None if eight else h, t, n, c.dtype, "h"), c.matrix8(h if eight else None, t, n, "h"),
+                             rstd.data_ptr(), gp, gs, c.matrix(dh, t, n, c.dtype, "dh"), c.matrix(dx, t, n, c.dtype, "out"), dp, ds)
+    c.run(load_library().pg_add_rms_norm_grad, args, load_library().pg_add_rms_norm_grad_workspace_bytes)
     return dx, dgain
 
 
@@ -268,13 +291,13 @@ def pg_linear(x, weight, bias=None, residual=None, activation: str = "none", sav
     c = _Call("pg_linear", x, stream)
     n_out, n_in = _weight(c, weight, True)
     t = c.tokens
-    y = c.empty(t, n_out) if out is None else out
+    y = c.like(t, n_out) if out is None else out
     z8 = c.empty8(t, n_out) if save_z else None
     bp, bs = c.vector(bias, n_out, "bias")
-    args = pg_linear_args(_DTYPES[c.dtype], _activation(c.where, activation), c.batch, t, n_in, n_out,
-                          c.matrix(x, t, n_in, name="x"), c.matrix(weight, n_out, n_in, name="weight"), bp, bs,
-                          c.matrix(residual, t, n_out, name="residual"), c.matrix(y, t, n_out, name="out"), c.matrix8(z8, t, n_out))
-    c.run(_lib().pg_linear, args, _lib().pg_linear_workspace_bytes)
+    args = pg_linear_args(c.kind, _activation(c.where, activation), c.batch, t, n_in, n_out,
+                          c.matrix(x, t, n_in, c.dtype, "x"), c.matrix(weight, n_out, n_in, c.dtype, "weight"), bp, bs,
+                          c.matrix(residual, t, n_out, c.dtype, "residual"), c.matrix(y, t, n_out, c.dtype, "out"), c.matrix8(z8, t, n_out, "z8"))
+    c.run(load_library().pg_linear, args, load_library().pg_linear_workspace_bytes)
     return (y, z8) if save_z else y
 
 
@@ -283,11 +306,11 @@ def pg_linear_input_grad(dz, weight, residual=None, out=None, stream=None):
     c = _Call("pg_linear_input_grad", dz, stream)
     n_out, n_in = _weight(c, weight, False)
     t = c.tokens
-    dx = c.empty(t, n_in) if out is None else out
-    args = pg_input_grad_args(_DTYPES[c.dtype], c.batch, t, n_in, n_out, c.matrix(dz, t, n_out, name="dz"),
-                              c.matrix(weight, n_out, n_in, name="weight"), c.matrix(residual, t, n_in, name="residual"),
-                              c.matrix(dx, t, n_in, name="out"))
-    c.run(_lib().pg_linear_input_grad, args, _lib().pg_linear_input_grad_workspace_bytes)
+    dx = c.like(t, n_in) if out is None else out
+    args = pg_input_grad_args(c.kind, c.batch, t, n_in, n_out, c.matrix(dz, t, n_out, c.dtype, "dz"),
+                              c.matrix(weight, n_out, n_in, c.dtype, "weight"), c.matrix(residual, t, n_in, c.dtype, "residual"),
+                              c.matrix(dx, t, n_in, c.dtype, "out"))
+    c.run(load_library().pg_linear_input_grad, args, load_library().pg_linear_input_grad_workspace_bytes)
     return dx
 
 
@@ -299,11 +322,11 @@ def pg_linear_weight_grad(dz, x: Union[torch.Tensor, Checkpoint8], out=None, acc
     t, n_out, n_in = c.tokens, c.cols, int((x.values if eight else x).shape[-1])
     if accumulate and out is None:
         _refuse(c.where, "accumulate needs out")
-    dw = c.empty(n_out, n_in, torch.float32) if out is None else out
-    args = pg_weight_grad_args(_DTYPES[c.dtype], c.batch, t, n_in, n_out, int(accumulate), c.matrix(dz, t, n_out, name="dz"),
-                               c.matrix(None if eight else x, t, n_in, name="x"), c.matrix8(x if eight else None, t, n_in, "x"),
+    dw = c.empty(n_out, n_in, torch.float32, 4) if out is None else out
+    args = pg_weight_grad_args(c.kind, c.batch, t, n_in, n_out, int(accumulate), c.matrix(dz, t, n_out, c.dtype, "dz"),
+                               c.matrix(None if eight else x, t, n_in, c.dtype, "x"), c.matrix8(x if eight else None, t, n_in, "x"),
                                c.matrix(dw, n_out, n_in, torch.float32, "out"))
-    c.run(_lib().pg_linear_weight_grad, args, _lib().pg_linear_weight_grad_workspace_bytes)
+    c.run(load_library().pg_linear_weight_grad, args, load_library().pg_linear_weight_grad_workspace_bytes)
     return dw
 
 
@@ -315,12 +338,12 @@ def pg_activation_grad(dy, z8: Optional[Checkpoint8], activation: str = "none", 
     t, n = c.tokens, c.cols
     if accumulate and bias_grad is None:
         _refuse(c.where, "accumulate needs bias_grad")
-    dz = c.empty(t, n) if out is None else out
-    dbias = c.flat(c.batch, n) if bias_grad is None else bias_grad
+    dz = c.like(t, n) if out is None else out
+    dbias = c.flat(n) if bias_grad is None else bias_grad
     dp, ds = c.vector(dbias, n, "bias_grad")
-    args = pg_activation_grad_args(_DTYPES[c.dtype], _activation(c.where, activation), c.batch, t, n, int(accumulate),
-                                   c.matrix(dy, t, n, name="dy"), c.matrix8(z8, t, n, "z8"), c.matrix(dz, t, n, name="out"), dp, ds)
-    c.run(_lib().pg_activation_grad, args)
+    args = pg_activation_grad_args(c.kind, _activation(c.where, activation), c.batch, t, n, int(accumulate),
+                                   c.matrix(dy, t, n, c.dtype, "dy"), c.matrix8(z8, t, n, "z8"), c.matrix(dz, t, n, c.dtype, "out"), dp, ds)
+    c.run(load_library().pg_activation_grad, args)
     return dz, dbias
 
 
@@ -328,19 +351,19 @@ def pg_checkpoint_write(x, out: Optional[Checkpoint8] = None, stream=None) -> Ch
     """The 8-bit form of a 16-bit tensor."""
     c = _Call("pg_checkpoint_write", x, stream)
     x8 = c.empty8(c.tokens, c.cols) if out is None else out
-    args = pg_checkpoint_args(_DTYPES[c.dtype], c.batch, c.tokens, c.cols, c.matrix(x, c.tokens, c.cols, name="x"),
+    args = pg_checkpoint_args(c.kind, c.batch, c.tokens, c.cols, c.matrix(x, c.tokens, c.cols, c.dtype, "x"),
                               c.matrix8(x8, c.tokens, c.cols, "out"))
-    c.run(_lib().pg_checkpoint_write, args)
+    c.run(load_library().pg_checkpoint_write, args)
     return x8
 
 
 def pg_checkpoint_read(x8: Checkpoint8, out=None, stream=None):
     """The 16-bit tensor that an 8-bit form stands for."""
     c = _Call("pg_checkpoint_read", x8, stream)
-    x = c.empty(c.tokens, c.cols) if out is None else out
-    args = pg_checkpoint_args(_DTYPES[c.dtype], c.batch, c.tokens, c.cols, c.matrix(x, c.tokens, c.cols, name="out"),
+    x = c.like(c.tokens, c.cols) if out is None else out
+    args = pg_checkpoint_args(c.kind, c.batch, c.tokens, c.cols, c.matrix(x, c.tokens, c.cols, c.dtype, "out"),
                               c.matrix8(x8, c.tokens, c.cols, "x8"))
-    c.run(_lib().pg_checkpoint_read, args)
+    c.run(load_library().pg_checkpoint_read, args)
     return x
 
 
@@ -351,4 +374,4 @@ def pg_training_status(stream=None, device="cuda") -> int:
     with torch.cuda.device(device):
         handle = torch.cuda.current_stream(device).cuda_stream if stream is None else \
             stream if isinstance(stream, int) else stream.cuda_stream
-        return int(_lib().pg_training_status(_vp(handle)))
+        return int(load_library().pg_training_status(_vp(handle)))
