@@ -31,8 +31,14 @@ namespace {
 constexpr int kBM = 128;              // lanes of an accumulator
 constexpr int kBK = 64;               // elements of k in a stage: one 128-byte swizzled row
 constexpr int kMaxStages = 12;
-constexpr int kSmemBytes = 232448;    // what a block may have
+constexpr int kSmemBytes = 232448;    // what a block may have,
+constexpr int kStaticBytes = 2304;    // and what of it Shared takes
+constexpr int kRingBytes = kSmemBytes - kStaticBytes - 1024;     // the rest, less what aligning it to 1024 bytes may cost
 constexpr int kABytes = kBM * kBK * 2;
+constexpr int kRawBytes = kBM * kBK;          // a stage of an 8-bit A before it is widened
+constexpr int kScaleStages = 8;               // stages whose scales are fetched at once, 4 bytes for each of their k
+constexpr int kScaleBytes = 2 * kScaleStages * kBK * 4;
+constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their own, since they are needed before A and B are
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
 constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
 
@@ -48,7 +54,9 @@ constexpr int kRowWarps = ROWWARPS;   // epilogue warps where lanes are tokens
 constexpr int kShares = kRowWarps / 4;
 constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out,
 constexpr int kHeldBytes = 32 * 80;   // and five 16-byte pieces of residuals for each of the rows
-constexpr int kOutWarp = kOutBytes + kHeldBytes;   // (a multiple of 512, the period of the swizzle)
+constexpr int kBiasBytes = 512;       // and the biases of its groups
+constexpr int kOutWarp = kOutBytes + kHeldBytes + kBiasBytes;    // (a multiple of 512, the period of the swizzle)
+static_assert((256 / 32 + kShares - 1) / kShares * 128 <= kBiasBytes && kOutWarp % 512 == 0, "a warp's share");
 constexpr int kOutRing = kRowWarps * kOutWarp;
 template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
 template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 256 : 0);
@@ -65,13 +73,12 @@ struct Epilogue {
 struct Problem {
     Epilogue ep;
     int M, N, K, batch;
-    int BN, m_tiles, n_tiles, stages, k_blocks, splits;
+    int BN, m_tiles, n_tiles, stages, raw_stages, k_blocks, splits;
     int64_t tiles;
     int a_shared, b_shared;    // operand is the same for every worker
     int residual_aligned;      // its rows start on 16-byte boundaries
-    const int8_t* values;      // an 8-bit A
-    const uint8_t* scales;
-    int64_t value_ld, value_stride, scale_ld, scale_stride;
+    const uint8_t* scales;     // of an 8-bit A
+    int64_t scale_ld, scale_stride;
 };
 
 __device__ unsigned g_training_error;   // a bounded wait gave up; read and cleared by pg_training_status
@@ -135,8 +142,18 @@ __device__ __forceinline__ uint32_t first_of_pair(uint64_t* b) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(b)));
     return r;
 }
+// An arrival there.  It releases what this thread wrote to its own block only, and that is what is read after it: each block's
+// tensor core takes its operands from its own shared memory.  (Released to the whole cluster, an arrival took about
+// a thousand cycles, two stages' worth.)
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Arrivals that say no more than that an accumulator has been read (tcgen05.wait::ld and the fence before them see to that).
+__device__ __forceinline__ void bar_arrive_read_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_arrive_read(uint64_t* b) {
+    asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y),
@@ -263,11 +280,11 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
 }
 
 struct Shared {
-    uint64_t loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
+    uint64_t raw[kMaxRaw], raw_empty[kMaxRaw], scaled[2], scales_empty[2], loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
     uint32_t tmem;
     int gave_up;
-    float bias[kRowWarps][32];
 };
+static_assert(sizeof(Shared) <= kStaticBytes, "Shared");
 
 // Lanes are tokens: a warp takes every third group of 32 columns of its 32 rows.  The residuals of the next group are on
 // their way to shared memory while one group is computed, and while the first one's accumulator is waited for: neighbouring
@@ -307,15 +324,16 @@ struct Residuals {             // of a tile: where a lane's five pieces start, f
     }
 };
 template <typename H, int ACT>
-__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, float* s_bias, int64_t b, int m0,
-                                           int n0, int share, int quarter, int lane, const Residuals& residuals, float& next_bias) {
+__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, int64_t b, int m0,
+                                           int n0, int share, int quarter, int lane, const Residuals& residuals) {
     const Epilogue& ep = p.ep;
     uint8_t* held = out + kOutBytes;
+    const float* s_bias = reinterpret_cast<const float*>(held + kHeldBytes);
     const int row = m0 + quarter * 32 + lane;
     const bool live = row < p.M;
     const int end = min(p.BN, p.N - n0);
     const bool add_residual = ep.residual.data != nullptr;
-    for (int j = share * 32; j < end; j += kShares * 32) {
+    for (int j = share * 32; j < end; j += kShares * 32, s_bias += 32) {
         const int n = n0 + j;
         uint4 piece[5];
         if (add_residual) {
@@ -331,13 +349,9 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 }
             }
         }
-        s_bias[lane] = next_bias;                              // the same 32 numbers for all lanes
         __syncwarp();
         const int next = j + kShares * 32;
-        if (next < end) {
-            if (add_residual) residuals.fetch(held, next, p.N - n0 - next, lane);
-            next_bias = ep.bias && n0 + next + lane < p.N ? ep.bias[b * ep.bias_stride + n0 + next + lane] : 0.0f;
-        }
+        if (add_residual && next < end) residuals.fetch(held, next, p.N - n0 - next, lane);
         const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j;
         if (ep.z8.values) {
             F2 v[4][4];
@@ -579,8 +593,8 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 }
 
 // ------------------------------------------------------------------ the kernel
-// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 4 - 11 empty accumulators, 12 - 19 widen an 8-bit A, one half
-// of them every other stage.  Every wait ends: it is for work that has already been started, and a wait that takes
+// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
+// empty accumulators, 12 - 19 widen it.  Every wait ends: it is for work that has already been started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
 template <typename H, Mode MODE, bool PAIR>
 __global__ void __launch_bounds__(kThreads<MODE>, 1)
@@ -594,16 +608,24 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int b_rows = p.BN / kBlocks;                  // of B in this block's shared memory
     const int b_bytes = (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
     const int stage_bytes = kABytes + b_bytes;
+    [[maybe_unused]] uint8_t* raw_ring = ring + p.stages * stage_bytes;
+    [[maybe_unused]] uint32_t* scale_ring = reinterpret_cast<uint32_t*>(raw_ring + p.raw_stages * kRawBytes);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
     const int in_pair = PAIR ? blockIdx.x & 1 : 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&sh.loaded[s], 1);
-            bar_init(&sh.widened[s], 4 * kBlocks);
+            bar_init(&sh.widened[s], 8 * kBlocks);
             bar_init(&sh.empty[s], 1);
         }
+        for (int s = 0; s < kMaxRaw; ++s) {
+            bar_init(&sh.raw[s], 1);
+            bar_init(&sh.raw_empty[s], 8);
+        }
         for (int i = 0; i < 2; ++i) {
+            bar_init(&sh.scaled[i], 1);
+            bar_init(&sh.scales_empty[i], 8);
             bar_init(&sh.summed[i], 1);
             bar_init(&sh.drained[i], kEpilogueWarps<MODE> * kBlocks);
         }
@@ -739,7 +761,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // the body for every combination that the epilogue is compiled for
         with_activation<H, MODE>(p.ep.activation, [&](auto act) {
             [[maybe_unused]] uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutWarp;
-            [[maybe_unused]] float next_bias = 0.0f;
             int done = 0;
             for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
                 const int acc = done & 1;
@@ -751,126 +772,161 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const int j = half * 32;
                     if (p.ep.residual.data) residuals.start(p.ep, b, m0 + quarter * 32, p.M, n0, lane);
                     if (p.ep.residual.data && j < min(p.BN, p.N - n0)) residuals.fetch(out + kOutBytes, j, p.N - n0 - j, lane);
-                    next_bias = p.ep.bias && n0 + j + lane < p.N ? p.ep.bias[b * p.ep.bias_stride + n0 + j + lane] : 0.0f;
+                    // the biases of its groups; not one by one in the groups, whose fences would wait for the load
+                    float bias[(8 + kShares - 1) / kShares];
+#pragma unroll
+                    for (int g = 0; g < (8 + kShares - 1) / kShares; ++g) {
+                        const int n = n0 + j + g * kShares * 32 + lane;
+                        bias[g] = p.ep.bias && n < p.N ? p.ep.bias[b * p.ep.bias_stride + n] : 0.0f;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int g = 0; g < (8 + kShares - 1) / kShares; ++g) reinterpret_cast<float*>(out + kOutBytes + kHeldBytes)[g * 32 + lane] = bias[g];
+                    __syncwarp();
                 }
                 if (!bar_wait(&sh.summed[acc], (done / 2) & 1, gave_up)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 __syncwarp();
                 if constexpr (kTokenRows<MODE>)
-                    empty_rows<H, decltype(act)::value>(p, &map_out, tmem + acc * p.BN, out, sh.bias[warp - 4], b, m0, n0, half, quarter, lane, residuals,
-                                                        next_bias);
+                    empty_rows<H, decltype(act)::value>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane, residuals);
                 else
                     empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0,
                                                                n0, half, quarter, lane);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (PAIR) bar_arrive_at(drained[acc]);
-                    else bar_arrive(&sh.drained[acc]);
+                    if constexpr (PAIR) bar_arrive_read_at(drained[acc]);
+                    else bar_arrive_read(&sh.drained[acc]);
                 }
             }
         });
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    } else if (kEight && warp >= 12) {
-        // Eight lanes take the 128 values of a row (one k) of the stage, 16 each, and a thread four rows.  They come from
-        // memory to registers, two of this half's stages ahead: through shared memory they would cost as much of its
-        // bandwidth again as the tensor cores' reading of A, and it is what limits these products.
-        const int mine = (warp - 12) >> 2;             // of every two stages
-        const int c = lane & 7, r0 = (warp & 3) * 4 + (lane >> 3);     // rows r0, r0 + 16, r0 + 32, r0 + 48
-        const uint32_t widened = PAIR ? first_of_pair(&sh.widened[0]) : smem_u32(&sh.widened[0]);
-        struct Stage {
-            uint4 v[4];
-            uint32_t s[4];
-        } held[2];
-        // where this half's next stage to fetch is
-        int64_t at_tile = first;
-        int at_kb = kb0;
-        const int8_t* v_at = nullptr;
-        const uint8_t* s_at = nullptr;
-        bool inside = false;
-        auto enter = [&] {                             // the tile at_tile
-            if (at_tile >= p.tiles) return;
+    } else if (kEight && warp == 2) {
+        int q = 0, turn = 0;
+        bool ok = true;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int64_t b;
             int m0, n0;
-            place(at_tile, b, m0, n0);
-            const int m = m0 + c * 16;
-            inside = m < p.M;
-            v_at = p.values + b * p.value_stride + m;
-            s_at = p.scales + b * p.scale_stride + m / kBlock8;
-        };
-        auto skip = [&](int n) {
-            at_kb += n;
-            if (at_kb >= kb1) {
-                while (at_kb >= kb1) {
-                    at_kb -= kb1 - kb0;
-                    at_tile += step;
+            place(tile, b, m0, n0);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (turn > 0 && !(ok = bar_wait(&sh.raw_empty[q], (turn - 1) & 1, gave_up))) break;
+                if (elected()) {
+                    bar_expect(&sh.raw[q], kRawBytes);
+                    tma_load(raw_ring + q * kRawBytes, &map_a, m0, kb * kBK, p.a_shared ? 0 : static_cast<int>(b), &sh.raw[q]);
                 }
-                enter();
-            }
-        };
-        auto fetch = [&](Stage& to) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                to.v[j] = make_uint4(0, 0, 0, 0);
-                to.s[j] = 0;
-            }
-            const int64_t k = static_cast<int64_t>(at_kb) * kBK + r0;
-            if (at_tile < p.tiles && inside) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (k + 16 * j < p.K) {
-                        to.v[j] = *reinterpret_cast<const uint4*>(v_at + (k + 16 * j) * p.value_ld);
-                        to.s[j] = s_at[(k + 16 * j) * p.scale_ld];
-                    }
-            }
-            skip(2);
-        };
-        const int64_t my_tiles = p.tiles > first ? (p.tiles - first + step - 1) / step : 0;
-        const int64_t left = my_tiles * (kb1 - kb0);   // stages of this block
-        if (left > 0) {
-            enter();
-            skip(mine);
-            fetch(held[0]);
-            fetch(held[1]);
-        }
-        int s = mine % p.stages, turn = mine / p.stages;
-        bool ok = true;
-        for (int64_t i = mine; ok && i < left; i += 4) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (i + 2 * u >= left) break;
-                Stage& here = held[u];
-                if (turn > 0 && !(ok = bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up))) break;
-                uint8_t* a = ring + s * stage_bytes + (c >> 2) * 8192;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = r0 + 16 * j;
-                    const uint32_t f = scale_pair<H>(here.s[j]);
-                    uint4 o[2];
-                    widen4<H>(here.v[j].x, f, o[0].x, o[0].y);
-                    widen4<H>(here.v[j].y, f, o[0].z, o[0].w);
-                    widen4<H>(here.v[j].z, f, o[1].x, o[1].y);
-                    widen4<H>(here.v[j].w, f, o[1].z, o[1].w);
-                    // the lanes of the upper 64 values take their two pieces the other way round: eight lanes, eight banks
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int w = q ^ (c >> 2);
-                        *reinterpret_cast<uint4*>(a + r * 128 + (((2 * (c & 3) + w) ^ (r & 7)) << 4)) = w ? o[1] : o[0];
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    if constexpr (PAIR) bar_arrive_at(widened + s * 8);
-                    else bar_arrive(&sh.widened[s]);
-                }
-                s += 2;
-                if (s >= p.stages) {
-                    s -= p.stages;
+                if (++q == p.raw_stages) {
+                    q = 0;
                     ++turn;
                 }
-                fetch(here);
+            }
+        }
+        if (!ok)       // copies still on their way must land before the block ends
+            for (int i = 0; i < p.raw_stages; ++i)
+                for (int t = 0; t < 100000 && i < q && !bar_try(&sh.raw[i], turn & 1); ++t) {}
+    } else if (kEight && warp == 3) {
+        // The scales of an 8-bit A, for eight stages at a time, so that no load is outstanding when they are handed over:
+        // an arrival on a barrier (and a fence) waits for the thread's earlier loads, and one per stage would wait for memory.
+        int half = 0, turn = 0;
+        bool ok = true;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
+            int64_t b;
+            int m0, n0;
+            place(tile, b, m0, n0);
+            const uint8_t* at = p.scales + b * p.scale_stride + m0 / kBlock8;
+            const int blocks = min(4, (p.M - m0 + kBlock8 - 1) / kBlock8);
+            for (int kb = kb0; kb < kb1; kb += kScaleStages) {
+                if (turn > 0 && !(ok = bar_wait(&sh.scales_empty[half], (turn - 1) & 1, gave_up))) break;
+                const int64_t k0 = static_cast<int64_t>(kb) * kBK, k1 = min(static_cast<int64_t>(p.K), k0 + kScaleStages * kBK);
+                uint32_t* to = scale_ring + half * kScaleStages * kBK;
+                // a row's four bytes, cut out of the one or two words that hold them; all rows' on their way together
+                constexpr int kRows = kScaleStages * kBK / 32;
+                uint32_t lo[kRows], hi[kRows];
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int64_t k = k0 + lane + 32 * u;
+                    const uintptr_t from = reinterpret_cast<uintptr_t>(at + k * p.scale_ld);
+                    const uint32_t* word = reinterpret_cast<const uint32_t*>(from & ~uintptr_t{3});
+                    lo[u] = hi[u] = 0;
+                    if (k < k1) lo[u] = word[0];
+                    if (k < k1 && static_cast<int>(from & 3) + blocks > 4) hi[u] = word[1];
+                }
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const uint32_t shift = (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at)) + static_cast<uint32_t>(k0 + lane + 32 * u) * static_cast<uint32_t>(p.scale_ld) & 3) * 8;
+                    to[lane + 32 * u] = __funnelshift_r(lo[u], hi[u], shift);
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.scaled[half]);
+                half ^= 1;
+                if (half == 0) ++turn;
+            }
+        }
+    } else if (kEight && warp >= 12) {
+        // Eight lanes take the 128 values of a row (one k) of the stage, 16 each, and a thread two rows.
+        const int c = lane & 7, r0 = (warp - 12) * 4 + (lane >> 3);    // rows r0 and r0 + 32
+        [[maybe_unused]] const uint32_t widened = first_of_pair(&sh.widened[0]);
+        const int64_t left = kb1 > kb0 && p.tiles > first ? (p.tiles - first + step - 1) / step * (kb1 - kb0) : 0;
+        int s = 0, turn = 0, q = 0, raw_parity = 0, kb = kb0, half = 0, scale_parity = 0;
+        for (int64_t i = 0; i < left; ++i) {
+            const int in_chunk = (kb - kb0) & (kScaleStages - 1);
+            if (in_chunk == 0 && !bar_wait(&sh.scaled[half], scale_parity, gave_up)) break;
+            if (!bar_wait(&sh.raw[q], raw_parity, gave_up)) break;
+            const uint8_t* raw = raw_ring + q * kRawBytes;
+            const uint8_t* scales = reinterpret_cast<const uint8_t*>(scale_ring + (half * kScaleStages + in_chunk) * kBK);
+            uint4 v[2];
+            uint32_t f[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                v[j] = *reinterpret_cast<const uint4*>(raw + (r0 + 32 * j) * 128 + c * 16);
+                f[j] = scales[(r0 + 32 * j) * 4 + (c >> 1)];
+            }
+            uint4 o[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f[j] = scale_pair<H>(f[j]);
+                widen4<H>(v[j].x, f[j], o[j][0].x, o[j][0].y);
+                widen4<H>(v[j].y, f[j], o[j][0].z, o[j][0].w);
+                widen4<H>(v[j].z, f[j], o[j][1].x, o[j][1].y);
+                widen4<H>(v[j].w, f[j], o[j][1].z, o[j][1].w);
+            }
+            __syncwarp();
+            const bool chunk_done = in_chunk == kScaleStages - 1 || kb + 1 == kb1;
+            if (lane == 0) {
+                bar_arrive(&sh.raw_empty[q]);
+                if (chunk_done) bar_arrive(&sh.scales_empty[half]);
+            }
+            if (++q == p.raw_stages) {
+                q = 0;
+                raw_parity ^= 1;
+            }
+            if (chunk_done) {
+                half ^= 1;
+                if (half == 0) scale_parity ^= 1;
+            }
+            if (++kb == kb1) kb = kb0;
+            if (turn > 0 && !bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up)) break;
+            uint8_t* a = ring + s * stage_bytes + (c >> 2) * 8192;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = r0 + 32 * j;
+                // the lanes of the upper 64 values take their two pieces the other way round: eight lanes, eight banks
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int w = e ^ (c >> 2);
+                    *reinterpret_cast<uint4*>(a + r * 128 + (((2 * (c & 3) + w) ^ (r & 7)) << 4)) = w ? o[j][1] : o[j][0];
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) bar_arrive_at(widened + s * 8);
+                else bar_arrive(&sh.widened[s]);
+            }
+            if (++s == p.stages) {
+                s = 0;
+                ++turn;
             }
         }
     }
@@ -929,20 +985,23 @@ EncodeFn encoder() {
     return fn;
 }
 
-// A matrix as TMA sees it: `rows` rows of `cols` 16-bit elements per worker, boxes of box_rows x box_bytes, swizzled over them.
-bool make_map(CUtensorMap& map, int dtype, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_bytes, int box_rows) {
+// A matrix as TMA sees it: `rows` rows of `cols` elements per worker, boxes of box_rows x box_bytes, swizzled over them (8-bit:
+// not).
+bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int box_bytes, int box_rows) {
     EncodeFn fn = encoder();
     if (!fn) return false;
+    const int64_t size = eight ? 1 : 2, unit = 16 / size;
     const bool shared = batch > 1 && m.stride == 0;
-    const int64_t ld = rows > 1 ? m.ld : (cols + 7) / 8 * 8;
+    const int64_t ld = rows > 1 ? m.ld : (cols + unit - 1) / unit * unit;
     const int64_t stride = batch > 1 && !shared ? m.stride : ld * rows;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(shared ? 1 : batch)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(stride * 2)};
-    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / 2), static_cast<cuuint32_t>(box_rows), 1};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld * size), static_cast<cuuint64_t>(stride * size)};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / size), static_cast<cuuint32_t>(box_rows), 1};
     const cuuint32_t one[3] = {1, 1, 1};
-    return fn(&map, dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, m.data, dims, strides, box, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const CUtensorMapDataType type = eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == PG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return fn(&map, type, 3, m.data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              eight ? CU_TENSOR_MAP_SWIZZLE_NONE : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Can TMA read the operand where it is?
@@ -978,7 +1037,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, c
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
     bool fine = true;
     std::call_once(once[dev], [&] {
-        fine = cudaFuncSetAttribute(product_kernel<H, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - 2048) == cudaSuccess;
+        fine = cudaFuncSetAttribute(product_kernel<H, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - kStaticBytes) == cudaSuccess;
     });
     if (!fine) return PG_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
@@ -1031,27 +1090,25 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
         while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
     const int b_rows = p.BN / kBlocks;
     const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
-    const int rest = kRows ? kOutRing : 0;
-    p.stages = std::min(kMaxStages, (kSmemBytes - 3072 - rest) / stage);
+    const int rest = kRows ? kOutRing : MODE == kWeightGrad8 ? kMinRaw * kRawBytes + kScaleBytes : 0;
+    p.stages = std::min(kMaxStages, (kRingBytes - rest) / stage);
+    p.raw_stages = MODE == kWeightGrad8 ? std::min(kMaxRaw, (kRingBytes - kScaleBytes - p.stages * stage) / kRawBytes) : 0;
     p.a_shared = A.stride == 0;
     p.b_shared = B.stride == 0;
     p.residual_aligned = access_width({&ep.residual}, batch) == 8;
     if (a8) {
-        p.values = a8->values;
-        p.value_ld = a8->ld;
-        p.value_stride = a8->stride;
         p.scales = a8->scales;
         p.scale_ld = a8->scale_ld;
         p.scale_stride = a8->scale_stride;
     }
     CUtensorMap map_a = {}, map_b = {}, map_out = {};
     if (K > 0) {
-        const bool fine = (MODE == kWeightGrad8 || make_map(map_a, dtype, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM)) &&
-                          make_map(map_b, dtype, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
-                          (!kRows || make_map(map_out, dtype, ep.out, batch, M, N, 64, 32));
+        const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
+                          make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
+                          (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
-    const int smem = p.stages * stage + rest + 1024;
+    const int smem = p.stages * stage + (MODE == kWeightGrad8 ? p.raw_stages * kRawBytes + kScaleBytes : rest) + 1024;
     return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, p, smem, st)
                             : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
 }
