@@ -395,26 +395,45 @@ activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
 }
 
 // ---------------------------------------------------------------- checkpoints
-// One thread per octet; a row takes a whole number of blocks of 32 values, so the four lanes of a block are neighbours.
+// A block takes kRowsPerThread * 256 / G rows, G octets of them side by side (G a power of two that divides 256, four at least,
+// so that the four lanes of a block of 32 values are neighbours); all loads of a thread are issued together.
+constexpr int kRowsPerThread = 4;
 template <typename H, int W, int WO, bool WRITE>
 __global__ void __launch_bounds__(256)
-checkpoint_kernel(const pg_checkpoint_args a, int64_t rows, int octets) {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t r = at / octets;
-    const int col = static_cast<int>(at - r * octets) * 8;
-    const bool live = r < rows && col < a.cols;
-    const int64_t b = live ? r / a.tokens : 0, tok = live ? r - b * a.tokens : 0;
-    uint16_t* row = static_cast<uint16_t*>(a.x.data) + b * a.x.stride + tok * a.x.ld;
-    int8_t* q = a.x8.values + b * a.x8.stride + tok * a.x8.ld;
-    uint8_t* s = a.x8.scales + b * a.x8.scale_stride + tok * a.x8.scale_ld;
-    const int cols = live ? a.cols : 0;
-    F2 v[4];
+checkpoint_kernel(const pg_checkpoint_args a, int log_g) {
+    const int64_t b = blockIdx.z;
+    const int col = ((blockIdx.y << log_g) + (threadIdx.x & ((1 << log_g) - 1))) * 8;
+    const int rows_at_once = 256 >> log_g;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRowsPerThread * rows_at_once + (threadIdx.x >> log_g);
+    uint16_t* x = static_cast<uint16_t*>(a.x.data) + b * a.x.stride;
+    int8_t* q = a.x8.values + b * a.x8.stride;
+    uint8_t* s = a.x8.scales + b * a.x8.scale_stride;
+    auto row = [&](int k) { return r0 + k * rows_at_once; };
+    auto cols = [&](int k) { return row(k) < a.tokens ? a.cols : 0; };
     if constexpr (WRITE) {
-        widen<H>(octet<W>(load_oct<W>(row, col, cols), row, col, cols), v);
-        octet_to_8<H>(v, q, s, col, cols);
-    } else if (live) {
-        widen8(load_oct8(q, col, cols), scale_value(s[col / kBlock8]), v);
-        store_oct<H, WO>(row, col, cols, v);
+        Piece<W> p[kRowsPerThread];
+#pragma unroll
+        for (int k = 0; k < kRowsPerThread; ++k) p[k] = load_oct<W>(x + row(k) * a.x.ld, col, cols(k));
+#pragma unroll
+        for (int k = 0; k < kRowsPerThread; ++k) {
+            F2 v[4];
+            widen<H>(octet<W>(p[k], x + row(k) * a.x.ld, col, cols(k)), v);
+            octet_to_8<H>(v, q + row(k) * a.x8.ld, s + row(k) * a.x8.scale_ld, col, cols(k));
+        }
+    } else {
+        Oct8 p[kRowsPerThread];
+        uint32_t scale[kRowsPerThread];
+#pragma unroll
+        for (int k = 0; k < kRowsPerThread; ++k) {
+            p[k] = load_oct8(q + row(k) * a.x8.ld, col, cols(k));
+            scale[k] = col < cols(k) ? s[row(k) * a.x8.scale_ld + col / kBlock8] : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < kRowsPerThread; ++k) {
+            F2 v[4];
+            widen8(p[k], scale_value(scale[k]), v);
+            if (col < cols(k)) store_oct<H, WO>(x + row(k) * a.x.ld, col, a.cols, v);
+        }
     }
 }
 
@@ -638,18 +657,21 @@ static int checkpoint(const pg_checkpoint_args* args, bool write, void* stream) 
     if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1)) return PG_ERR_INVALID;
     if (!matrix_ok(a.x, a.batch, a.tokens, a.cols, 2, !write, dev)) return PG_ERR_INVALID;
     if (!matrix8_ok(a.x8, a.batch, a.tokens, a.cols, write, dev)) return PG_ERR_INVALID;
-    const int64_t rows = int64_t{a.batch} * a.tokens;
-    if (rows == 0) return PG_OK;
+    if (a.batch == 0 || a.tokens == 0) return PG_OK;
     const int width = access_width({&a.x}, a.batch);
     const int octets = (a.cols + kBlock8 - 1) / kBlock8 * (kBlock8 / 8);
-    const int64_t blocks = (rows * octets + 255) / 256;
-    if (blocks > 0x7fffffff) return PG_ERR_TOO_LARGE;
+    int log_g = 2;
+    while (log_g < 8 && (1 << log_g) < octets) ++log_g;
+    while (log_g > 5 && (octets & ((1 << log_g) - 1)) != 0 && (1 << log_g) - (octets & ((1 << log_g) - 1)) > (octets >> 3)) --log_g;   // idle lanes: an eighth at most
+    const int64_t per_block = kRowsPerThread * (256 >> log_g);
+    const dim3 grid(static_cast<unsigned>((a.tokens + per_block - 1) / per_block), static_cast<unsigned>((octets + (1 << log_g) - 1) >> log_g), a.batch);
+    if (grid.y > 65535) return PG_ERR_TOO_LARGE;
     with_type(a.dtype, write ? width : 8, write ? 8 : width, [&](auto h, auto in, auto out) {
         using H = decltype(h);
         constexpr int W = decltype(in)::value, WO = decltype(out)::value;
         cudaStream_t st = static_cast<cudaStream_t>(stream);
-        if (write) checkpoint_kernel<H, W, WO, true><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, rows, octets);
-        else checkpoint_kernel<H, W, WO, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, rows, octets);
+        if (write) checkpoint_kernel<H, W, WO, true><<<grid, 256, 0, st>>>(a, log_g);
+        else checkpoint_kernel<H, W, WO, false><<<grid, 256, 0, st>>>(a, log_g);
     });
     return launch_status();
 }
