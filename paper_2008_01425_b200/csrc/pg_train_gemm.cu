@@ -59,7 +59,7 @@ constexpr int kOutWarp = kOutBytes + kHeldBytes + kBiasBytes;    // (a multiple 
 static_assert((256 / 32 + kShares - 1) / kShares * 128 <= kBiasBytes && kOutWarp % 512 == 0, "a warp's share");
 constexpr int kOutRing = kRowWarps * kOutWarp;
 template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
-template <Mode M, bool WORDS> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 256 : WORDS ? 128 : 0);
+template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 256 : 0);
 
 // What happens to D: stored as fp32 (dW), or passed through bias, activation and residual to 16 bits.
 struct Epilogue {
@@ -77,7 +77,6 @@ struct Problem {
     int64_t tiles;
     int a_shared, b_shared;    // operand is the same for every worker
     int residual_aligned;      // its rows start on 16-byte boundaries
-    pg_matrix words_a, words_b;        // the operands, where they are read in 4-byte pieces
     const uint8_t* scales;     // of an 8-bit A
     int64_t scale_ld, scale_stride;
 };
@@ -597,12 +596,8 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 // Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
 // empty accumulators, 12 - 19 widen it.  Every wait ends: it is for work that has already been started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
-//
-// WORDS (few tokens only, where the weights are read once and nothing is gained by copying them first): operands whose rows
-// start on 4-byte boundaries, which TMA cannot read, come in 4-byte asynchronous copies by warps 12 - 15, a 128-byte row of
-// a stage to a warp instruction.
-template <typename H, Mode MODE, bool PAIR, bool WORDS>
-__global__ void __launch_bounds__(kThreads<MODE, WORDS>, 1)
+template <typename H, Mode MODE, bool PAIR>
+__global__ void __launch_bounds__(kThreads<MODE>, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
                const __grid_constant__ Problem p) {
     extern __shared__ uint8_t s_raw[];
@@ -621,7 +616,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&sh.loaded[s], 1);
-            bar_init(&sh.widened[s], WORDS ? 128 : 8 * kBlocks);
+            bar_init(&sh.widened[s], 8 * kBlocks);
             bar_init(&sh.empty[s], 1);
         }
         for (int s = 0; s < kMaxRaw; ++s) {
@@ -669,7 +664,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         m0 = (static_cast<int>(in % p.m_tiles) * kBlocks + in_pair) * kBM;
     };
 
-    if (warp == 0 && !WORDS) {
+    if (warp == 0) {
         int s = 0, turn = 0;
         int64_t issued = 0;
         bool ok = true;
@@ -732,9 +727,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (done >= 2 && !(ok = bar_wait(&sh.drained[done & 1], (done / 2 - 1) & 1, gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!WORDS && !(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
-                if ((kEight || WORDS) && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
-                if (WORDS) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the copies were the threads' own writes
+                if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
+                if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
                 if (elected()) {
@@ -808,42 +802,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         });
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    } else if (WORDS && warp >= 12) {
-        int s = 0, turn = 0;
-        bool ok = true;
-        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
-            int64_t b;
-            int m0, n0;
-            place(tile, b, m0, n0);
-            const uint16_t* pa = static_cast<const uint16_t*>(p.words_a.data) + b * p.words_a.stride;
-            const uint16_t* pb = static_cast<const uint16_t*>(p.words_b.data) + b * p.words_b.stride;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (turn > 0 && !(ok = bar_wait(&sh.empty[s], (turn - 1) & 1, gave_up))) break;
-                const uint32_t at = smem_u32(ring + s * stage_bytes) + (lane & 3) * 4;
-                const int k0 = kb * kBK;
-                // row r of a stage: 128 bytes; what is outside of the matrix is filled with zeros
-                auto copy = [&](const uint16_t* base, int64_t ld, int row, int rows, int col, int cols, uint32_t stage_row) {
-                    const int n = row < rows ? min(2, cols - col) * 2 : 0;
-                    const uint16_t* from = n > 0 ? base + row * ld + col : base;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + stage_row * 128 + (((lane >> 2) ^ (stage_row & 7)) << 4)),
-                                 "l"(from), "r"(max(n, 0))
-                                 : "memory");
-                };
-#pragma unroll 8
-                for (int r = warp - 12; r < kBM; r += 4) {
-                    if constexpr (kAMn) copy(pa, p.words_a.ld, k0 + (r & 63), p.K, m0 + (r & 64) + 2 * lane, p.M, r);
-                    else copy(pa, p.words_a.ld, m0 + r, p.M, k0 + 2 * lane, p.K, r);
-                }
-#pragma unroll 4
-                for (int r = warp - 12; r < p.BN; r += 4) copy(pb, p.words_b.ld, n0 + r, p.N, k0 + 2 * lane, p.K, kBM + r);
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.widened[s])) : "memory");
-                if (++s == p.stages) {
-                    s = 0;
-                    ++turn;
-                }
-            }
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (kEight && warp == 2) {
         int q = 0, turn = 0;
         bool ok = true;
@@ -997,6 +955,141 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
 }
 
+// ------------------------------------------------------------------ few tokens
+// y for up to four tokens: the weights are read once, which is all the time there is, so they go from memory to registers
+// and are multiplied as fp32 pairs.  A block computes 32 features (one block of the 8-bit form), a warp four of them at a time
+// over all of k; which lane has which k does not matter to a sum, so a lane takes as many neighbours (8, 2 or 1) as the
+// rows' alignment lets it read at once.  The tokens wait in shared memory as they are stored.
+constexpr int kFewTokens = 4, kFewBytes = 48 * 1024;
+// W neighbouring elements as pairs; the second of a pair may lie past the row's end (`valid` elements are inside).
+template <typename H, int W> struct Few {
+    static constexpr int kPairs = W == 1 ? 1 : W / 2, kUnroll = W == 8 ? 2 : 6;
+    uint32_t w[kPairs];
+    __device__ __forceinline__ void load(const uint16_t* row, int e, int valid) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) w[i] = 0;
+        if (valid <= 0) return;
+        if constexpr (W == 8) {
+            const uint4 u = *reinterpret_cast<const uint4*>(row + e);
+            w[0] = u.x;
+            w[1] = u.y;
+            w[2] = u.z;
+            w[3] = u.w;
+        } else if constexpr (W == 2) {
+            w[0] = *reinterpret_cast<const uint32_t*>(row + e);
+        } else {
+            w[0] = row[e];
+        }
+    }
+    __device__ __forceinline__ void mask(int valid) {
+        if (W > 1 && valid < W) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) w[i] = 2 * i + 1 < valid ? w[i] : 2 * i < valid ? w[i] & 0xffffu : 0u;
+        }
+    }
+};
+template <typename H, int W, int T, int ACT>
+__global__ void __launch_bounds__(256)
+few_tokens_kernel(const pg_linear_args a) {
+    extern __shared__ uint4 s_x[];                     // T rows of octets
+    __shared__ float s_z[T][32];
+    using F = Few<H, W>;
+    const int64_t b = blockIdx.y;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int K = a.in_features, octets = (K + 7) / 8;
+    for (int i = threadIdx.x; i < T * octets; i += 256) {
+        const int t = i / octets, col = (i - t * octets) * 8;
+        const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + t * a.x.ld;
+        const Oct o = octet<1>(load_oct<1>(x, col, K), x, col, K);
+        s_x[i] = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
+    }
+    const uint16_t* x16 = reinterpret_cast<const uint16_t*>(s_x);
+    const int n0 = blockIdx.x * 32 + warp * 4;
+    const uint16_t* row[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)                        // a feature past the last one is computed again and not used
+        row[r] = static_cast<const uint16_t*>(a.weight.data) + b * a.weight.stride + min(n0 + r, a.out_features - 1) * a.weight.ld;
+    F2 acc[4][T];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[r][t] = both(0.0f);
+    bool first = true;
+    for (int k = 0; k < K; k += 32 * W * F::kUnroll) {
+        F w[F::kUnroll][4];
+#pragma unroll
+        for (int u = 0; u < F::kUnroll; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int e = k + (u * 32 + lane) * W;
+                w[u][r].load(row[r], e, K - e);
+            }
+        if (first) __syncthreads();                    // the tokens; the first weights are on their way meanwhile
+        first = false;
+#pragma unroll
+        for (int u = 0; u < F::kUnroll; ++u) {
+            const int e = k + (u * 32 + lane) * W;
+            if (e >= K) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[u][r].mask(K - e);
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                F x;
+                x.load(x16 + t * octets * 8, e, W);
+#pragma unroll
+                for (int i = 0; i < F::kPairs; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[r][t] = fma(Elem<H>::up2(w[u][r].w[i]), Elem<H>::up2(x.w[i]), acc[r][t]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            float v = sum2(acc[r][t]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == 0) s_z[t][warp * 4 + r] = v;
+        }
+    __syncthreads();
+    if (warp < T) {
+        const Epilogue ep{0, ACT, a.y, a.residual, a.bias, a.bias_stride, a.z8};
+        const int m = blockIdx.x * 32 + lane;
+        const bool live = m < a.out_features;
+        float v[16] = {s_z[warp][lane]};
+        emit<H, ACT, false>(ep, v, b, warp, 1, m, live, a.bias && live ? a.bias[b * a.bias_stride + m] : 0.0f);
+    }
+}
+template <typename H, int W, int T>
+int few_tokens(const pg_linear_args& a, cudaStream_t st) {
+    const dim3 grid((a.out_features + 31) / 32, a.batch);
+    const size_t smem = static_cast<size_t>(T) * ((a.in_features + 7) / 8) * 16;
+    if (a.activation == PG_ACT_GELU) few_tokens_kernel<H, W, T, PG_ACT_GELU><<<grid, 256, smem, st>>>(a);
+    else if (a.activation == PG_ACT_SILU) few_tokens_kernel<H, W, T, PG_ACT_SILU><<<grid, 256, smem, st>>>(a);
+    else if (a.activation == PG_ACT_RELU) few_tokens_kernel<H, W, T, PG_ACT_RELU><<<grid, 256, smem, st>>>(a);
+    else few_tokens_kernel<H, W, T, PG_ACT_NONE><<<grid, 256, smem, st>>>(a);
+    return launch_status();
+}
+template <typename H>
+int few_tokens(const pg_linear_args& a, cudaStream_t st) {
+    const uint64_t bits = reinterpret_cast<uintptr_t>(a.weight.data) | static_cast<uint64_t>(a.weight.ld) * 2 |
+                          (a.batch > 1 ? static_cast<uint64_t>(a.weight.stride) * 2 : 0);
+    auto with = [&](auto tokens) {
+        constexpr int T = decltype(tokens)::value;
+        return bits % 16 == 0 ? few_tokens<H, 8, T>(a, st) : bits % 4 == 0 ? few_tokens<H, 2, T>(a, st) : few_tokens<H, 1, T>(a, st);
+    };
+    switch (a.tokens) {
+        case 1: return with(std::integral_constant<int, 1>{});
+        case 2: return with(std::integral_constant<int, 2>{});
+        case 3: return with(std::integral_constant<int, 3>{});
+        default: return with(std::integral_constant<int, 4>{});
+    }
+}
+bool few(const pg_linear_args& a) {
+    return a.tokens <= kFewTokens && static_cast<int64_t>(a.tokens) * ((a.in_features + 7) / 8) * 16 <= kFewBytes;
+}
+
 // Rows of 16-bit elements copied to rows that start on 16-byte boundaries, for operands TMA cannot read
 // where they are: 8 elements a thread.
 __global__ void __launch_bounds__(256)
@@ -1072,19 +1165,19 @@ int aligned_operand(pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, uin
     return launch_status();
 }
 
-template <typename H, Mode MODE, bool PAIR, bool WORDS>
+template <typename H, Mode MODE, bool PAIR>
 int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const Problem& p, int smem, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
     bool fine = true;
     std::call_once(once[dev], [&] {
-        fine = cudaFuncSetAttribute(product_kernel<H, MODE, PAIR, WORDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - kStaticBytes) == cudaSuccess;
+        fine = cudaFuncSetAttribute(product_kernel<H, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes - kStaticBytes) == cudaSuccess;
     });
     if (!fine) return PG_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(PAIR ? 2 * std::min<int64_t>(p.tiles, kSMs / 2) : p.splits > 1 ? p.tiles * p.splits : std::min<int64_t>(p.tiles, kSMs)));
-    cfg.blockDim = dim3(kThreads<MODE, WORDS>);
+    cfg.blockDim = dim3(kThreads<MODE>);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -1093,14 +1186,14 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, c
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE, PAIR, WORDS>, a, b, out, p) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE, PAIR>, a, b, out, p) != cudaSuccess) {
         cudaGetLastError();
         return PG_ERR_CUDA;
     }
     return PG_OK;
 }
 
-template <Mode MODE, bool PAIR, bool WORDS = false>
+template <Mode MODE, bool PAIR>
 int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const pg_matrix& A, const pg_matrix& B, const Epilogue& ep, const pg_matrix8* a8,
                 cudaStream_t st) {
     constexpr bool kBMn = kBMnMajor<MODE>, kAMn = kAMnMajor<MODE>, kRows = kTokenRows<MODE>;
@@ -1143,18 +1236,16 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
         p.scale_ld = a8->scale_ld;
         p.scale_stride = a8->scale_stride;
     }
-    p.words_a = A;
-    p.words_b = B;
     CUtensorMap map_a = {}, map_b = {}, map_out = {};
-    if (K > 0 && !WORDS) {
+    if (K > 0) {
         const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
                           make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
                           (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
     const int smem = p.stages * stage + (MODE == kWeightGrad8 ? p.raw_stages * kRawBytes + kScaleBytes : rest) + 1024;
-    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR, WORDS>(map_a, map_b, map_out, p, smem, st)
-                            : launch<__half, MODE, PAIR, WORDS>(map_a, map_b, map_out, p, smem, st);
+    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, p, smem, st)
+                            : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
 }
 
 constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are addressed with 32 bits
@@ -1163,17 +1254,6 @@ constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are ad
 // the GPU: with fewer, single blocks that share the k of a tile finish earlier.
 bool enough_for_pairs(int64_t batch, int64_t M, int64_t N) {
     return M > kBM && batch * ((M + 2 * kBM - 1) / (2 * kBM)) * ((N + 255) / 256) * 2 >= kSMs / 2;
-}
-// How y = x W^T or dx = dz W is computed: `n` features come out, `left` is x or dz with `k` columns.
-enum Path { kPairs, kSingle, kSingleWords };
-Path path_of(int64_t batch, int64_t tokens, int64_t n, const pg_matrix& left, const pg_matrix& weight, int64_t weight_rows, const pg_matrix& out,
-             const pg_matrix& residual) {
-    if (enough_for_pairs(batch, tokens, n) && aligned(out, batch, tokens) && residual.ld < kMaxResidualLd) return kPairs;
-    auto words = [&](const pg_matrix& m, int64_t rows) {
-        return reinterpret_cast<uintptr_t>(m.data) % 4 == 0 && (rows <= 1 || m.ld % 2 == 0) && (batch <= 1 || m.stride % 2 == 0);
-    };
-    const bool tma = aligned(left, batch, tokens) && aligned(weight, batch, weight_rows);
-    return !tma && words(left, tokens) && words(weight, weight_rows) ? kSingleWords : kSingle;
 }
 
 int current_device() {
@@ -1193,11 +1273,9 @@ extern "C" {
 
 int pg_linear_workspace_bytes(const pg_linear_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->in_features, args->out_features)) return PG_ERR_INVALID;
-    *bytes_out = 0;
-    if (args->tokens > 0 &&
-        path_of(args->batch, args->tokens, args->out_features, args->x, args->weight, args->out_features, args->y, args->residual) != kSingleWords)
-        *bytes_out = copy_bytes(args->x, args->batch, args->tokens, args->in_features) +
-                     copy_bytes(args->weight, args->batch, args->out_features, args->in_features);
+    *bytes_out = few(*args) ? 0
+                            : copy_bytes(args->x, args->batch, args->tokens, args->in_features) +
+                                  copy_bytes(args->weight, args->batch, args->out_features, args->in_features);
     return PG_OK;
 }
 int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1217,25 +1295,22 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (few(a)) return a.dtype == PG_BF16 ? few_tokens<__nv_bfloat16>(a, st) : few_tokens<__half>(a, st);
     uint8_t* at = static_cast<uint8_t*>(workspace);
     pg_matrix x = a.x, w = a.weight;
-    const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
-    const Path path = path_of(a.batch, a.tokens, a.out_features, a.x, a.weight, a.out_features, a.y, a.residual);
-    if (path == kSingleWords) return run_product<kForward, false, true>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
     int rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
+    const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
     if (rc != PG_OK) return rc;
-    return path == kPairs ? run_product<kForwardRows, true>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st)
-                          : run_product<kForward, false>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
+    if (enough_for_pairs(a.batch, a.tokens, a.out_features) && aligned(a.y, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
+        return run_product<kForwardRows, true>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
+    return run_product<kForward, false>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
 
 int pg_linear_input_grad_workspace_bytes(const pg_input_grad_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->in_features, args->out_features)) return PG_ERR_INVALID;
-    *bytes_out = 0;
-    if (args->tokens > 0 &&
-        path_of(args->batch, args->tokens, args->in_features, args->dz, args->weight, args->out_features, args->dx, args->residual) != kSingleWords)
-        *bytes_out = copy_bytes(args->dz, args->batch, args->tokens, args->out_features) +
-                     copy_bytes(args->weight, args->batch, args->out_features, args->in_features);
+    *bytes_out = copy_bytes(args->dz, args->batch, args->tokens, args->out_features) +
+                 copy_bytes(args->weight, args->batch, args->tokens ? args->out_features : 0, args->in_features);
     return PG_OK;
 }
 int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1254,14 +1329,13 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* at = static_cast<uint8_t*>(workspace);
     pg_matrix dz = a.dz, w = a.weight;
-    const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
-    const Path path = path_of(a.batch, a.tokens, a.in_features, a.dz, a.weight, a.out_features, a.dx, a.residual);
-    if (path == kSingleWords) return run_product<kInputGrad, false, true>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
     int rc = aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st);
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
+    const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
     if (rc != PG_OK) return rc;
-    return path == kPairs ? run_product<kInputGradRows, true>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st)
-                          : run_product<kInputGrad, false>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
+    if (enough_for_pairs(a.batch, a.tokens, a.in_features) && aligned(a.dx, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
+        return run_product<kInputGradRows, true>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
+    return run_product<kInputGrad, false>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
 
 int pg_linear_weight_grad_workspace_bytes(const pg_weight_grad_args* args, size_t* bytes_out) {

@@ -549,8 +549,16 @@ def test_refusals_of_the_library(tr):
     for bad in (dict(xp=None), dict(xp=host.data_ptr()), dict(xp=x.data_ptr() + 1), dict(ld=15), dict(stride=-1), dict(out_stride=16),
                 dict(dtype=2), dict(act=4), dict(act=-1), dict(tokens=-1), dict(n_in=0), dict(yp=None), dict(out_ld=7), dict(out_stride=0)):
         assert linear(**bad) == pg.PG_ERR_INVALID, bad
-    # rows that are not 16-byte aligned go through the workspace, so there has to be one
-    assert linear(xp=x.data_ptr() + 2, ld=17, stride=68, tokens=3) == pg.PG_ERR_WORKSPACE
+    # a weight gradient's rows that are not 16-byte aligned go through the workspace, so there has to be one
+    dw = torch.full((2, 8, 16), 3.0, device="cuda")
+    a = tr.pg_weight_grad_args(0, 2, 4, 16, 8, 0, tr.pg_matrix(y.data_ptr(), 8, 32), tr.pg_matrix(x.data_ptr() + 2, 16, 64),
+                               tr.pg_matrix8(None, None, 0, 0, 0, 0), tr.pg_matrix(dw.data_ptr(), 16, 128))
+    need = ctypes.c_size_t(0)
+    assert lib.pg_linear_weight_grad_workspace_bytes(ctypes.byref(a), ctypes.byref(need)) == pg.PG_OK and need.value >= 2 * 4 * 16 * 2
+    assert lib.pg_linear_weight_grad(ctypes.byref(a), None, 0, None) == pg.PG_ERR_WORKSPACE
+    assert lib.pg_linear_weight_grad(ctypes.byref(a), x.data_ptr(), need.value - 1, None) == pg.PG_ERR_WORKSPACE
+    torch.cuda.synchronize()
+    assert bool((dw == 3.0).all())
     c8 = tr.pg_checkpoint_write(x)
     a = tr.pg_checkpoint_args(0, 2, 4, 16, tr.pg_matrix(x.data_ptr(), 16, 64),
                               tr.pg_matrix8(c8.values.data_ptr(), c8.scales.data_ptr(), 24, 96, 1, 4))
