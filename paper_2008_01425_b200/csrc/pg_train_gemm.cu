@@ -39,6 +39,11 @@ constexpr int kRawBytes = kBM * kBK;          // a stage of an 8-bit A before it
 constexpr int kScaleStages = 8;               // stages whose scales are fetched at once, 4 bytes for each of their k
 constexpr int kScaleBytes = 2 * kScaleStages * kBK * 4;
 constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their own, since they are needed before A and B are
+// Blocks of k that tensor memory sums in one go for a weight gradient.  The tensor cores cut a sum off where fp32 arithmetic
+// would round it, and the more bits the products have the more of them: of a gradient's size, 0.99e-6 over 1024 tokens
+// for bf16 and 1.25e-6 for fp16 operands, 0.45e-6 over 2048 for bf16 with x from 8 bits, 0.76e-6 over 1024 for fp16 with it.
+// Longer sums are added up, rounding, from parts that stay under 1e-6, as an fp32 product's do.
+constexpr int max_chunk(bool eight, int dtype) { return !eight ? 768 / kBK : dtype == PG_BF16 ? 2048 / kBK : 1024 / kBK; }
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
 constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
 
@@ -74,6 +79,8 @@ struct Problem {
     Epilogue ep;
     int M, N, K, batch;
     int BN, m_tiles, n_tiles, stages, raw_stages, k_blocks, splits;
+    int part_at;               // split k: where in shared memory a block's part is
+    int chunk;                 // blocks of k that are summed in tensor memory before they are added to the rest
     int64_t tiles;
     int a_shared, b_shared;    // operand is the same for every worker
     int residual_aligned;      // its rows start on 16-byte boundaries
@@ -232,11 +239,11 @@ __device__ __forceinline__ uint32_t byte8(float v, float inverse) { return __flo
 
 // Columns n .. n + count - 1 (16 at most) of lane m.
 template <typename H, int ACT, bool FP32>
-__device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t b, int64_t n, int count, int m, bool live, float bias) {
+__device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t b, int64_t n, int count, int m, bool live, float bias, bool more = false) {
     if constexpr (FP32) {
         float* o = static_cast<float*>(ep.out.data) + b * ep.out.stride + n * ep.out.ld + m;
         if (!live) return;
-        if (ep.accumulate) {
+        if (ep.accumulate || more) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (i < count) v[i] += o[i * ep.out.ld];
@@ -455,7 +462,7 @@ __device__ __forceinline__ void emit_full(const Epilogue& ep, float (&v)[16], co
 // One tile's accumulator to the output, or (split k) to this block's part in shared memory.  The two warps of a
 // quarter take every other 16 columns.
 template <typename H, int ACT, bool FP32>
-__device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, float* part, int64_t b, int m0, int n0, int half, int quarter, int lane) {
+__device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, float* part, bool more, int64_t b, int m0, int n0, int half, int quarter, int lane) {
     const Epilogue& ep = p.ep;
     const int m = m0 + quarter * 32 + lane;
     const bool live = m < p.M;
@@ -472,7 +479,10 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
             }
             if (part) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) part[(j + i) * kBM + quarter * 32 + lane] = v[i];
+                for (int i = 0; i < 16; ++i) {
+                    float* at = part + (j + i) * kBM + quarter * 32 + lane;
+                    *at = more ? *at + v[i] : v[i];
+                }
             } else {
                 emit<H, ACT, FP32>(ep, v, b, n0 + j, min(16, end - j), m, live, bias);
             }
@@ -483,7 +493,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
     if (m0 + quarter * 32 + 32 <= p.M) {
         if constexpr (FP32) {
             float* o = static_cast<float*>(ep.out.data) + b * ep.out.stride + static_cast<int64_t>(n0 + j) * ep.out.ld + m;
-            const bool add = ep.accumulate;
+            const bool add = ep.accumulate || more;
             for (; j + 16 <= end; j += 32, o += 32 * ep.out.ld) {
                 float old[16];
                 if (add) {
@@ -533,7 +543,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
     }
     for (; j < end; j += 32) {             // the last columns, or lanes past the last row
         tmem_load16(lanes + j, v);
-        emit<H, ACT, FP32>(ep, v, b, n0 + j, min(16, end - j), m, live, bias);
+        emit<H, ACT, FP32>(ep, v, b, n0 + j, min(16, end - j), m, live, bias, more);
     }
 }
 // Split k: this block adds up all parts of its share of the columns, in the order of the blocks.
@@ -609,6 +619,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int b_bytes = (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
     const int stage_bytes = kABytes + b_bytes;
     [[maybe_unused]] uint8_t* raw_ring = ring + p.stages * stage_bytes;
+    [[maybe_unused]] float* part = reinterpret_cast<float*>(ring + p.part_at);
     [[maybe_unused]] uint32_t* scale_ring = reinterpret_cast<uint32_t*>(raw_ring + p.raw_stages * kRawBytes);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform, and known to be
     const int tmem_cols = p.BN <= 16 ? 32 : p.BN <= 32 ? 64 : p.BN <= 64 ? 128 : p.BN <= 128 ? 256 : 512;
@@ -722,34 +733,40 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const int last_steps = (p.K - (p.k_blocks - 1) * kBK + 15) / 16;        // of the last block of k; the others have four
         int s = 0, parity = 0, done = 0;
         bool ok = true;
-        for (int64_t tile = first; ok && tile < p.tiles; tile += step, ++done) {
-            const uint32_t d = tmem + (done & 1) * p.BN;
-            if (done >= 2 && !(ok = bar_wait(&sh.drained[done & 1], (done / 2 - 1) & 1, gave_up))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
-                if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
+        for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
+            int kb = kb0;
+            do {                                       // chunks of k; without any k there is one of none
+                const uint32_t d = tmem + (done & 1) * p.BN;
+                const int from = kb, to = min(kb1, kb + p.chunk);
+                if (done >= 2 && !(ok = bar_wait(&sh.drained[done & 1], (done / 2 - 1) & 1, gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
-                if (elected()) {
-                    mma_f16<PAIR>(d, a, bd, idesc, kb > kb0);
-                    if (kb + 1 < p.k_blocks) {
+                for (; kb < to; ++kb) {
+                    if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
+                    if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
+                    if (elected()) {
+                        mma_f16<PAIR>(d, a, bd, idesc, kb > from);
+                        if (kb + 1 < p.k_blocks) {
 #pragma unroll
-                        for (int k = 1; k < 4; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
-                    } else {
-                        for (int k = 1; k < last_steps; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
+                            for (int k = 1; k < 4; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
+                        } else {
+                            for (int k = 1; k < last_steps; ++k) mma_f16<PAIR>(d, a + k * kStepA, bd + k * kStepB, idesc, 1);
+                        }
+                        mma_commit<PAIR>(&sh.empty[s]);
+                        if (kb + 1 == to) mma_commit<PAIR>(&sh.summed[done & 1]);
                     }
-                    mma_commit<PAIR>(&sh.empty[s]);
-                    if (kb + 1 == kb1) mma_commit<PAIR>(&sh.summed[done & 1]);
+                    __syncwarp();
+                    if (++s == p.stages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
                 }
+                if (!ok) break;
+                if (from == to && elected()) mma_commit<PAIR>(&sh.summed[done & 1]);
                 __syncwarp();
-                if (++s == p.stages) {
-                    s = 0;
-                    parity ^= 1;
-                }
-            }
-            if (kb0 == kb1 && elected()) mma_commit<PAIR>(&sh.summed[done & 1]);
-            __syncwarp();
+                ++done;
+            } while (kb < kb1);
         }
         if (!ok) {
             if (elected()) mma_commit<PAIR>(&sh.last);
@@ -761,9 +778,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // the body for every combination that the epilogue is compiled for
         with_activation<H, MODE>(p.ep.activation, [&](auto act) {
             [[maybe_unused]] uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutWarp;
-            int done = 0;
-            for (int64_t tile = first; tile < p.tiles; tile += step, ++done) {
+            int done = 0, kb = kb0;
+            for (int64_t tile = first; tile < p.tiles; ++done) {
                 const int acc = done & 1;
+                [[maybe_unused]] const bool more = kb > kb0;            // what comes is added to an earlier chunk
                 int64_t b;
                 int m0, n0;
                 place(tile, b, m0, n0);
@@ -790,13 +808,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if constexpr (kTokenRows<MODE>)
                     empty_rows<H, decltype(act)::value>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane, residuals);
                 else
-                    empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? reinterpret_cast<float*>(ring) : nullptr, b, m0,
-                                                               n0, half, quarter, lane);
+                    empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? part : nullptr, more, b, m0, n0, half, quarter,
+                                                               lane);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
                     if constexpr (PAIR) bar_arrive_read_at(drained[acc]);
                     else bar_arrive_read(&sh.drained[acc]);
+                }
+                kb += p.chunk;
+                if (kb >= kb1) {
+                    kb = kb0;
+                    tile += step;
                 }
             }
         });
@@ -939,7 +962,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int m0, n0;
             place(first, b, m0, n0);
             with_activation<H, MODE>(p.ep.activation, [&](auto act) {
-                join_parts<H, decltype(act)::value, kFp32>(p, reinterpret_cast<float*>(ring), b, m0, n0, rank, (warp - 4) >> 2, warp & 3, lane);
+                join_parts<H, decltype(act)::value, kFp32>(p, part, b, m0, n0, rank, (warp - 4) >> 2, warp & 3, lane);
             });
         }
         __syncwarp();
@@ -1208,9 +1231,11 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     // Widths of a tile: multiples of 16 columns, of 32 where a thread holds blocks of 32, of 64 where TMA loads boxes of
     // 64 columns and every other one is stored.  The one that covers N with the fewest columns, a tile's start and
     // end counted as 64 more; the widest of equals.
+    // (128 at most where a block's part of a split k may be a sum of chunks, and has to have a place beside the ring.)
     const int unit = kWeightGrads<MODE> ? 64 : kRows ? 32 : 16;
+    p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
     int64_t least = 0;
-    for (int w = 256; w >= unit && w >= std::min<int64_t>(N, kRows || kWeightGrads<MODE> ? 128 : 16); w -= unit) {
+    for (int w = kWeightGrads<MODE> && !PAIR && p.k_blocks > max_chunk(MODE == kWeightGrad8, dtype) ? 128 : 256; w >= unit && w >= std::min<int64_t>(N, kRows || kWeightGrads<MODE> ? 128 : 16); w -= unit) {
         const int64_t tiles = (N + w - 1) / w, cost = tiles * (w + 64);
         if (least == 0 || cost < least) {
             least = cost;
@@ -1219,15 +1244,19 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     }
     p.n_tiles = static_cast<int>((N + p.BN - 1) / p.BN);
     p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
-    p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
     p.splits = 1;
     if (!PAIR)
         while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
     const int b_rows = p.BN / kBlocks;
     const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
+    // (The other products are rounded to 16 bits, beside which what is cut off is nothing.)
+    const int most = max_chunk(MODE == kWeightGrad8, dtype);
+    const int per_split = std::max(1, (p.k_blocks + p.splits - 1) / p.splits), parts = kWeightGrads<MODE> ? (per_split + most - 1) / most : 1;
+    p.chunk = (per_split + parts - 1) / parts;
+    const int part_bytes = p.splits > 1 && parts > 1 ? kBM * p.BN * 4 : 0;
     const int rest = kRows ? kOutRing : MODE == kWeightGrad8 ? kMinRaw * kRawBytes + kScaleBytes : 0;
-    p.stages = std::min(kMaxStages, (kRingBytes - rest) / stage);
-    p.raw_stages = MODE == kWeightGrad8 ? std::min(kMaxRaw, (kRingBytes - kScaleBytes - p.stages * stage) / kRawBytes) : 0;
+    p.stages = std::min(kMaxStages, (kRingBytes - rest - part_bytes) / stage);
+    p.raw_stages = MODE == kWeightGrad8 ? std::min(kMaxRaw, (kRingBytes - kScaleBytes - part_bytes - p.stages * stage) / kRawBytes) : 0;
     p.a_shared = A.stride == 0;
     p.b_shared = B.stride == 0;
     p.residual_aligned = access_width({&ep.residual}, batch) == 8;
@@ -1243,7 +1272,9 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
                           (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
         if (!fine) return PG_ERR_CUDA;
     }
-    const int smem = p.stages * stage + (MODE == kWeightGrad8 ? p.raw_stages * kRawBytes + kScaleBytes : rest) + 1024;
+    const int ring = p.stages * stage + (MODE == kWeightGrad8 ? p.raw_stages * kRawBytes + kScaleBytes : rest);
+    p.part_at = part_bytes > 0 ? ring : 0;             // a sum of one chunk is only there when the ring is done with
+    const int smem = ring + part_bytes + 1024;
     return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, p, smem, st)
                             : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
 }

@@ -291,17 +291,22 @@ def test_weight_gradient(tr, shape, dtype, pad, from8, accumulate):
     assert bool((out[..., k:] == 5.0).all())            # nothing beside the rows is written
 
 
-def test_long_sums_keep_fp32(tr):
+@pytest.mark.parametrize("shape", [(1, 8192, 128, 64), (1, 40000, 96, 70), (20, 4096, 512, 264), (1, 5000, 1200, 1030)])
+@pytest.mark.parametrize("from8", [False, True])
+def test_long_sums_keep_fp32(tr, shape, from8):
     """A weight gradient over many tokens is as exact as a sum in fp32 with rounding: a few units of
-    its size, not one cut-off unit per token."""
+    its size, not one cut-off unit per token.  Split over blocks, in chunks, and both."""
     g = gen(11)
-    for from8 in (False, True):
-        dz, x = rand(g, 1, 8192, 64).to(BF), rand(g, 1, 8192, 128).to(BF)
-        kept = make8(tr, x.float(), BF) if from8 else x
-        xv = stored8(kept) if from8 else x.double()
-        want = dz.double().transpose(1, 2) @ xv
-        rel = float((tr.pg_linear_weight_grad(dz, kept).double() - want).norm() / want.norm())
-        assert rel <= 1e-6, rel
+    b, t, k, n = shape
+    dz, x = rand(g, b, t, n).to(BF), rand(g, b, t, k).to(BF)
+    kept = make8(tr, x.float(), BF) if from8 else x
+    xv = stored8(kept) if from8 else x.double()
+    want = dz.double().transpose(1, 2) @ xv
+    got = tr.pg_linear_weight_grad(dz, kept)
+    rel = float((got.double() - want).norm() / want.norm())
+    assert rel <= 1e-6, rel
+    twice = tr.pg_linear_weight_grad(dz, kept, out=got.clone(), accumulate=True)
+    assert float((twice.double() - 2 * want).norm() / want.norm()) <= 3e-6
 
 
 def test_linear_gradients_against_differences(tr):
