@@ -22,6 +22,9 @@
  *   - Sums, statistics and products are held in fp32 and rounded once, where a result is stored.
  *   - tokens = 0 and batch = 0 are valid: outputs per token are empty, sums over tokens are zero.
  *   - A NaN or an infinity in an input reaches the outputs that depend on it, and no others.
+ *   - Rows may start on any element.  Where they start on 16-byte boundaries the kernels take their
+ *     fastest path; elsewhere 16-byte pieces of memory that hold at least one element of a row are
+ *     read whole, and what else is in them is not used.  Outputs are written to their own elements only.
  *   - PG_ERR_INVALID: sizes out of range, a required pointer missing, misaligned, on the host or
  *     on another device, ld below the row length, overlapping outputs.  Nothing is launched then.
  */
@@ -70,7 +73,7 @@ typedef struct pg_matrix8 {
  * Residual addition and root-mean-square norm, row by row (tokens x cols per worker):
  *     s = x + residual;  rstd = (mean(s^2) + eps)^(-1/2);  y = s * rstd * gain
  * h gets s rounded to 16 bits (the next residual stream; may be x or residual in place), y the
- * result.  With y8, the 8-bit form of the result is written too and y holds the values it stands
+ * result.  At most 16384 columns (PG_ERR_TOO_LARGE).  With y8, the 8-bit form of the result is written too and y holds the values it stands
  * for: the layer behind the norm then sees in its forward pass what its weight gradient will read.
  * h8 gets the 8-bit form of h, the checkpoint that pg_add_rms_norm_grad reads.
  */
@@ -117,8 +120,9 @@ PG_API int pg_add_rms_norm_grad(const pg_norm_grad_args *args, void *workspace, 
  * z = x W^T + bias;  y = a(z) + residual, for every worker: x tokens x in, W out x in (a layer of
  * the stack: rows = out, cols = in), y tokens x out.  z8, if given, gets the 8-bit form of z for
  * pg_activation_grad (16-bit dtype decides its smallest step).
- * Rows of x or W that are not 16-byte aligned (ld or stride not a multiple of 8 elements, or such
- * a pointer) are first copied to aligned rows in the workspace; aligned operands need none.
+ * With more than four tokens, rows of x or W that are not 16-byte aligned (ld or stride not a multiple of 8
+ * elements, or such a pointer) are first copied to aligned rows in the workspace; otherwise none is
+ * needed.  The same goes for the operands of the two gradients below.
  */
 typedef struct pg_linear_args {
     int32_t dtype, activation, batch, tokens, in_features, out_features;
@@ -145,7 +149,8 @@ PG_API int pg_linear_input_grad_workspace_bytes(const pg_input_grad_args *args, 
 PG_API int pg_linear_input_grad(const pg_input_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
 /* dW = dz^T x in fp32, straight into a gradient buffer's layout (pg_stack_offset): overwritten, or
- * added to with accumulate.  x is a 16-bit matrix or an 8-bit checkpoint (exactly one of x, x8). */
+ * added to with accumulate.  x is a 16-bit matrix or an 8-bit checkpoint (exactly one of x, x8) whose values
+ * are in the 16-bit type's range, as those written from that type are. */
 typedef struct pg_weight_grad_args {
     int32_t dtype, batch, tokens, in_features, out_features;
     int32_t accumulate;
