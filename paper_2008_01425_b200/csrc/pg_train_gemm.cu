@@ -59,10 +59,10 @@ constexpr int kRowWarps = ROWWARPS;   // epilogue warps where lanes are tokens
 constexpr int kShares = kRowWarps / 4;
 constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out,
 constexpr int kHeldBytes = 32 * 80;   // and five 16-byte pieces of residuals for each of the rows
-constexpr int kBiasBytes = 512;       // and the biases of its groups
+constexpr int kBiasBytes = 512;       // and the biases of its groups;
+constexpr int kOut8Bytes = 1024;      // the 8-bit form of a group on its way out, where there is one
 constexpr int kOutWarp = kOutBytes + kHeldBytes + kBiasBytes;    // (a multiple of 512, the period of the swizzle)
 static_assert((256 / 32 + kShares - 1) / kShares * 128 <= kBiasBytes && kOutWarp % 512 == 0, "a warp's share");
-constexpr int kOutRing = kRowWarps * kOutWarp;
 template <Mode M> constexpr int kEpilogueWarps = kTokenRows<M> ? kRowWarps : 8;
 template <Mode M> constexpr int kThreads = 128 + 32 * kEpilogueWarps<M> + (M == kWeightGrad8 ? 256 : 0);
 
@@ -79,6 +79,7 @@ struct Problem {
     Epilogue ep;
     int M, N, K, batch;
     int BN, m_tiles, n_tiles, stages, raw_stages, k_blocks, splits;
+    int out_warp;              // bytes of an epilogue warp's share
     int part_at;               // split k: where in shared memory a block's part is
     int chunk;                 // blocks of k that are summed in tensor memory before they are added to the rest
     int64_t tiles;
@@ -331,7 +332,7 @@ struct Residuals {             // of a tile: where a lane's five pieces start, f
     }
 };
 template <typename H, int ACT>
-__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, uint32_t tmem, uint8_t* out, int64_t b, int m0,
+__device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* map_out, const CUtensorMap* map_out8, uint32_t tmem, uint8_t* out, int64_t b, int m0,
                                            int n0, int share, int quarter, int lane, const Residuals& residuals) {
     const Epilogue& ep = p.ep;
     uint8_t* held = out + kOutBytes;
@@ -380,19 +381,12 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 for (int k = 0; k < 4; ++k) t[k] = to8(v[i][k], inverse);
                 q[i] = pack8(t);
             }
-            if (live) {
-                int8_t* to = ep.z8.values + b * ep.z8.stride + row * ep.z8.ld;
-                if (n + 32 <= p.N) {
-                    uint4* w = reinterpret_cast<uint4*>(to + n);
-                    w[0] = make_uint4(q[0].w[0], q[0].w[1], q[1].w[0], q[1].w[1]);
-                    w[1] = make_uint4(q[2].w[0], q[2].w[1], q[3].w[0], q[3].w[1]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (n + 8 * i < p.N) store_oct8(to, n + 8 * i, p.N, q[i]);
-                }
-                ep.z8.scales[b * ep.z8.scale_stride + row * ep.z8.scale_ld + n / kBlock8] = static_cast<uint8_t>(s);
-            }
+            if (live) ep.z8.scales[b * ep.z8.scale_stride + row * ep.z8.scale_ld + n / kBlock8] = static_cast<uint8_t>(s);
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last group's copies have been read
+            __syncwarp();
+            uint4* to = reinterpret_cast<uint4*>(out + kOutWarp + lane * 32);
+            to[0] = make_uint4(q[0].w[0], q[0].w[1], q[1].w[0], q[1].w[1]);
+            to[1] = make_uint4(q[2].w[0], q[2].w[1], q[3].w[0], q[3].w[1]);
         }
         // (the accumulator is read again: tensor memory is faster than registers are plenty)
         uint32_t w[16];
@@ -421,7 +415,10 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
             *reinterpret_cast<uint4*>(out + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0 && m0 + quarter * 32 < p.M) tma_store(map_out, out, n, m0 + quarter * 32, static_cast<int>(b));
+        if (lane == 0 && m0 + quarter * 32 < p.M) {
+            if (ep.z8.values) tma_store(map_out8, out + kOutWarp, n, m0 + quarter * 32, static_cast<int>(b));
+            tma_store(map_out, out, n, m0 + quarter * 32, static_cast<int>(b));
+        }
     }
 }
 
@@ -609,7 +606,7 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 template <typename H, Mode MODE, bool PAIR>
 __global__ void __launch_bounds__(kThreads<MODE>, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
-               const __grid_constant__ Problem p) {
+               const __grid_constant__ CUtensorMap map_out8, const __grid_constant__ Problem p) {
     extern __shared__ uint8_t s_raw[];
     __shared__ Shared sh;
     constexpr bool kAMn = kAMnMajor<MODE>, kBMn = kBMnMajor<MODE>, kFp32 = kWeightGrads<MODE>, kEight = MODE == kWeightGrad8;
@@ -777,7 +774,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint32_t drained[2] = {PAIR ? first_of_pair(&sh.drained[0]) : 0u, PAIR ? first_of_pair(&sh.drained[1]) : 0u};
         // the body for every combination that the epilogue is compiled for
         with_activation<H, MODE>(p.ep.activation, [&](auto act) {
-            [[maybe_unused]] uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * kOutWarp;
+            [[maybe_unused]] uint8_t* out = ring + p.stages * stage_bytes + (warp - 4) * p.out_warp;
             int done = 0, kb = kb0;
             for (int64_t tile = first; tile < p.tiles; ++done) {
                 const int acc = done & 1;
@@ -806,7 +803,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 __syncwarp();
                 if constexpr (kTokenRows<MODE>)
-                    empty_rows<H, decltype(act)::value>(p, &map_out, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane, residuals);
+                    empty_rows<H, decltype(act)::value>(p, &map_out, &map_out8, tmem + acc * p.BN, out, b, m0, n0, half, quarter, lane, residuals);
                 else
                     empty_tile<H, decltype(act)::value, kFp32>(p, tmem + acc * p.BN, !PAIR && p.splits > 1 ? part : nullptr, more, b, m0, n0, half, quarter,
                                                                lane);
@@ -1189,7 +1186,7 @@ int aligned_operand(pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, uin
 }
 
 template <typename H, Mode MODE, bool PAIR>
-int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const Problem& p, int smem, cudaStream_t st) {
+int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const CUtensorMap& out8, const Problem& p, int smem, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return PG_ERR_CUDA;
@@ -1209,7 +1206,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, c
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE, PAIR>, a, b, out, p) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, product_kernel<H, MODE, PAIR>, a, b, out, out8, p) != cudaSuccess) {
         cudaGetLastError();
         return PG_ERR_CUDA;
     }
@@ -1254,7 +1251,8 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     const int per_split = std::max(1, (p.k_blocks + p.splits - 1) / p.splits), parts = kWeightGrads<MODE> ? (per_split + most - 1) / most : 1;
     p.chunk = (per_split + parts - 1) / parts;
     const int part_bytes = p.splits > 1 && parts > 1 ? kBM * p.BN * 4 : 0;
-    const int rest = kRows ? kOutRing : MODE == kWeightGrad8 ? kMinRaw * kRawBytes + kScaleBytes : 0;
+    p.out_warp = kOutWarp + (ep.z8.values ? kOut8Bytes : 0);
+    const int rest = kRows ? kRowWarps * p.out_warp : MODE == kWeightGrad8 ? kMinRaw * kRawBytes + kScaleBytes : 0;
     p.stages = std::min(kMaxStages, (kRingBytes - rest - part_bytes) / stage);
     p.raw_stages = MODE == kWeightGrad8 ? std::min(kMaxRaw, (kRingBytes - kScaleBytes - part_bytes - p.stages * stage) / kRawBytes) : 0;
     p.a_shared = A.stride == 0;
@@ -1265,18 +1263,19 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
         p.scale_ld = a8->scale_ld;
         p.scale_stride = a8->scale_stride;
     }
-    CUtensorMap map_a = {}, map_b = {}, map_out = {};
+    CUtensorMap map_a = {}, map_b = {}, map_out = {}, map_out8 = {};
     if (K > 0) {
         const bool fine = make_map(map_a, dtype, MODE == kWeightGrad8, A, batch, kAMn ? K : M, kAMn ? M : K, 128, kAMn ? kBK : kBM) &&
                           make_map(map_b, dtype, false, B, batch, kBMn ? K : N, kBMn ? N : K, 128, kBMn ? kBK : b_rows) &&
-                          (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32));
+                          (!kRows || make_map(map_out, dtype, false, ep.out, batch, M, N, 64, 32)) &&
+                          (!kRows || !ep.z8.values || make_map(map_out8, dtype, true, pg_matrix{ep.z8.values, ep.z8.ld, ep.z8.stride}, batch, M, N, 32, 32));
         if (!fine) return PG_ERR_CUDA;
     }
     const int ring = p.stages * stage + (MODE == kWeightGrad8 ? p.raw_stages * kRawBytes + kScaleBytes : rest);
     p.part_at = part_bytes > 0 ? ring : 0;             // a sum of one chunk is only there when the ring is done with
     const int smem = ring + part_bytes + 1024;
-    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, p, smem, st)
-                            : launch<__half, MODE, PAIR>(map_a, map_b, map_out, p, smem, st);
+    return dtype == PG_BF16 ? launch<__nv_bfloat16, MODE, PAIR>(map_a, map_b, map_out, map_out8, p, smem, st)
+                            : launch<__half, MODE, PAIR>(map_a, map_b, map_out, map_out8, p, smem, st);
 }
 
 constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are addressed with 32 bits
