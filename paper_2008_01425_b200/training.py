@@ -187,17 +187,18 @@ class _Call:
         return t
 
     def empty(self, rows: int, cols: int, dtype, unit: int) -> torch.Tensor:
-        """Rows start on 16-byte boundaries: a multiple of `unit` elements."""
+        """Rows start on multiples of `unit` elements."""
         ld = (cols + unit - 1) // unit * unit
         if self.single:
             return self._own(_empty((rows, cols), (ld, 1), dtype=dtype, device=self.device))
         return self._own(_empty((self.batch, rows, cols), (rows * ld, ld, 1), dtype=dtype, device=self.device))
 
     def like(self, rows: int, cols: int) -> torch.Tensor:
-        return self.empty(rows, cols, self.dtype, 8)
+        # 16-byte boundaries; 64-byte ones for long rows, whose pieces then fill whole 32-byte sectors of the cache
+        return self.empty(rows, cols, self.dtype, 32 if cols >= 256 else 8)
 
     def empty8(self, rows: int, cols: int) -> Checkpoint8:
-        return Checkpoint8(self.empty(rows, cols, torch.int8, 16), self.empty(rows, (cols + BLOCK8 - 1) // BLOCK8, torch.uint8, 1), self.dtype)
+        return Checkpoint8(self.empty(rows, cols, torch.int8, 32 if cols >= 256 else 16), self.empty(rows, (cols + BLOCK8 - 1) // BLOCK8, torch.uint8, 1), self.dtype)
 
     def flat(self, n: int) -> torch.Tensor:
         """fp32 (workers, n), or (n,) for one worker."""
