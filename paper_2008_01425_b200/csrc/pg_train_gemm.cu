@@ -303,13 +303,15 @@ struct Residuals {             // of a tile: where a lane's five pieces start, f
     const char* base;
     uint32_t at[5];            // bytes from the first of the warp's 32 rows
     uint32_t wanted;           // bit i: the row is inside and has such a piece
+    uint32_t low;              // the first row's own start, in bytes from its first piece's
     int off;                   // elements from the first piece's start to this lane's own row
 
     __device__ __forceinline__ void start(const Epilogue& ep, int64_t b, int row0, int rows, int n0, int lane) {
         const int64_t first = b * ep.residual.stride + static_cast<int64_t>(row0) * ep.residual.ld + n0;
         const uintptr_t from = reinterpret_cast<uintptr_t>(ep.residual.data) + first * 2;
         base = reinterpret_cast<const char*>(from & ~uintptr_t{15});
-        const uint32_t low = from & 15, ld = static_cast<uint32_t>(ep.residual.ld) * 2;
+        low = from & 15;
+        const uint32_t ld = static_cast<uint32_t>(ep.residual.ld) * 2;
         wanted = 0;
 #pragma unroll
         for (int i = 0; i < 5; ++i) {
@@ -319,15 +321,16 @@ struct Residuals {             // of a tile: where a lane's five pieces start, f
         }
         off = static_cast<int>(low + lane * ld & 15) / 2;
     }
-    // Copies the pieces of the 32 columns from n0 + j on; `left`: columns from there to the matrix's end.
-    __device__ __forceinline__ void fetch(uint8_t* held, int j, int left, int lane) const {
+    // Copies the pieces of the 32 columns from n0 + j on; `left`: columns from there to the matrix's end.  Where they are fewer
+    // than all pieces may hold, only those that hold one of them.
+    __device__ __forceinline__ void fetch(const Epilogue& ep, uint8_t* held, int j, int left, int lane) const {
         const char* from = base + 2 * j;
 #pragma unroll
         for (int i = 0; i < 5; ++i) {
-            const uint32_t k = lane + 32 * i, c = k - k / 5 * 5;
-            // a row's piece c holds its columns from 8 c - (up to 7) on; the last ones of a row may have none left
-            if ((wanted >> i & 1) && static_cast<int>(8 * c) < left + 7)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(held) + k * 16), "l"(from + at[i]) : "memory");
+            const uint32_t k = lane + 32 * i, r = k / 5, c = k - r * 5;
+            bool in = wanted >> i & 1;
+            if (left < 40) in = in && static_cast<int>(8 * c) - static_cast<int>(low + r * static_cast<uint32_t>(ep.residual.ld) * 2 & 15) / 2 < left;
+            if (in) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(held) + k * 16), "l"(from + at[i]) : "memory");
         }
     }
 };
@@ -359,7 +362,7 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
         }
         __syncwarp();
         const int next = j + kShares * 32;
-        if (add_residual && next < end) residuals.fetch(held, next, p.N - n0 - next, lane);
+        if (add_residual && next < end) residuals.fetch(ep, held, next, p.N - n0 - next, lane);
         const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j;
         if (ep.z8.values) {
             F2 v[4][4];
@@ -786,7 +789,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if constexpr (kTokenRows<MODE>) {
                     const int j = half * 32;
                     if (p.ep.residual.data) residuals.start(p.ep, b, m0 + quarter * 32, p.M, n0, lane);
-                    if (p.ep.residual.data && j < min(p.BN, p.N - n0)) residuals.fetch(out + kOutBytes, j, p.N - n0 - j, lane);
+                    if (p.ep.residual.data && j < min(p.BN, p.N - n0)) residuals.fetch(p.ep, out + kOutBytes, j, p.N - n0 - j, lane);
                     // the biases of its groups; not one by one in the groups, whose fences would wait for the load
                     float bias[(8 + kShares - 1) / kShares];
 #pragma unroll
@@ -980,7 +983,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // and are multiplied as fp32 pairs.  A block computes 32 features (one block of the 8-bit form), a warp four of them at a time
 // over all of k; which lane has which k does not matter to a sum, so a lane takes as many neighbours (8, 2 or 1) as the
 // rows' alignment lets it read at once.  The tokens wait in shared memory as they are stored.
-constexpr int kFewTokens = 4, kFewBytes = 48 * 1024;
+constexpr int kFewTokens = 4, kFewBytes = 40 * 1024;
 // W neighbouring elements as pairs; the second of a pair may lie past the row's end (`valid` elements are inside).
 template <typename H, int W> struct Few {
     static constexpr int kPairs = W == 1 ? 1 : W / 2, kUnroll = W == 8 ? 2 : 6;

@@ -258,6 +258,37 @@ def test_linear(tr, shape, dtype, pad, activation, residual, save):
     check(y, want, slack, dtype)
 
 
+@pytest.mark.parametrize("n", list(range(257, 300, 3)) + [264, 272, 288])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1), (BF, 8), (HF, 5)])
+def test_ends_of_residual_rows(tr, n, dtype, pad):
+    """Residual rows that start and end anywhere in a 16-byte piece, through the path with tokens as lanes; the residual
+    ends with its allocation."""
+    g = gen(n)
+    b, t, k = 19, 257, 24
+    x, w = rand(g, b, t, k).to(dtype), rand(g, b, n, k, scale=k ** -0.5).to(dtype)
+    r = strided(rand(g, b, t, n).to(dtype), pad)
+    y = tr.pg_linear(x, w, residual=r)
+    z = x.double() @ w.double().transpose(1, 2)
+    slack = (x.double().abs() @ w.double().abs().transpose(1, 2)) * (k + 2) * 2 * U
+    check(y, z + r.double(), slack + (z + r.double()).abs() * U, dtype)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("k", [7, 5120, 5128, 10240, 20480, 20488])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1), (BF, 2)])
+def test_few_tokens_at_the_limits_of_their_path(tr, tokens, k, dtype, pad):
+    g = gen(tokens * k)
+    b, n = 2, 45
+    x, w = strided(rand(g, b, tokens, k).to(dtype), pad), strided(rand(g, b, n, k, scale=k ** -0.5).to(dtype), pad)
+    bias, r = rand(g, b, n), rand(g, b, tokens, n).to(dtype)
+    y, z8 = tr.pg_linear(x, w, bias, residual=r, activation="silu", save_z=True)
+    z = x.double() @ w.double().transpose(1, 2) + bias.double()[:, None]
+    slack = (x.double().abs() @ w.double().abs().transpose(1, 2) + bias.double().abs()[:, None]) * (k + 2) * 2 * U
+    check8(z8, z, slack, dtype)
+    want = act(z, "silu") + r.double()
+    check(y, want, 1.13 * slack + z.abs() * 32 * U + want.abs() * U, dtype)
+
+
 @pytest.mark.parametrize("shape", PRODUCT_SHAPES)
 @pytest.mark.parametrize("dtype,pad,residual", [(BF, 0, True), (HF, 1, False), (BF, 8, False)])
 def test_input_gradient(tr, shape, dtype, pad, residual):
