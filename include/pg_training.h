@@ -120,7 +120,7 @@ PG_API int pg_add_rms_norm_grad(const pg_norm_grad_args *args, void *workspace, 
  * z = x W^T + bias;  y = a(z) + residual, for every worker: x tokens x in, W out x in (a layer of
  * the stack: rows = out, cols = in), y tokens x out.  z8, if given, gets the 8-bit form of z for
  * pg_activation_grad (16-bit dtype decides its smallest step).
- * With more than four tokens, rows of x or W that are not 16-byte aligned (ld or stride not a multiple of 8
+ * Unless there are very few tokens, rows of x or W that are not 16-byte aligned (ld or stride not a multiple of 8
  * elements, or such a pointer) are first copied to aligned rows in the workspace; otherwise none is
  * needed.  The same goes for the operands of the two gradients below.
  */

@@ -979,7 +979,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // ------------------------------------------------------------------ few tokens
-// y for up to four tokens: the weights are read once, which is all the time there is, so they go from memory to registers
+// y for one to four tokens: the weights are read once, which is all the time there is, so they go from memory to registers
 // and are multiplied as fp32 pairs.  A block computes 32 features (one block of the 8-bit form), a warp four of them at a time
 // over all of k; which lane has which k does not matter to a sum, so a lane takes as many neighbours (8, 2 or 1) as the
 // rows' alignment lets it read at once.  The tokens wait in shared memory as they are stored.
@@ -1109,10 +1109,6 @@ int few_tokens(const pg_linear_args& a, cudaStream_t st) {
         default: return with(std::integral_constant<int, 4>{});
     }
 }
-bool few(const pg_linear_args& a) {
-    return a.tokens <= kFewTokens && static_cast<int64_t>(a.tokens) * ((a.in_features + 7) / 8) * 16 <= kFewBytes;
-}
-
 // Rows of 16-bit elements copied to rows that start on 16-byte boundaries, for operands TMA cannot read
 // where they are: 8 elements a thread.
 __global__ void __launch_bounds__(256)
@@ -1166,6 +1162,13 @@ bool make_map(CUtensorMap& map, int dtype, bool eight, const pg_matrix& m, int64
 bool aligned(const pg_matrix& m, int64_t batch, int64_t rows) {
     return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows <= 1 || m.ld % 8 == 0) && (batch <= 1 || m.stride % 8 == 0);
 }
+// Up to four tokens where the product would have to copy the weights' rows first (32 workers x 2600 x 650: 27, 33, 44 and 47 us
+// for 1 to 4 tokens, 75 us by copy and product); one where it would not (2600 x 656: 24 us, and 35 for two; the product
+// takes 25 for up to 16).
+bool few(const pg_linear_args& a) {
+    return a.tokens <= (aligned(a.weight, a.batch, a.out_features) ? 1 : kFewTokens) && static_cast<int64_t>(a.tokens) * ((a.in_features + 7) / 8) * 16 <= kFewBytes;
+}
+
 size_t copy_bytes(const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols) {
     if (batch == 0 || rows == 0 || aligned(m, batch, rows)) return 0;
     const int64_t workers = m.stride == 0 ? 1 : batch;
@@ -1246,7 +1249,9 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
     p.splits = 1;
     if (!PAIR)
-        while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= kSMs && p.k_blocks >= p.splits * 2) p.splits *= 2;
+        // (eight blocks of a cluster have to find room in one GPC: 16 tiles in clusters of eight ran one after the other, 33 us
+        // where 24 in clusters of four take 16.5)
+        while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= (p.splits == 4 ? kSMs / 2 : kSMs) && p.k_blocks >= p.splits * 2) p.splits *= 2;
     const int b_rows = p.BN / kBlocks;
     const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
     // (The other products are rounded to 16 bits, beside which what is cut off is nothing.)
@@ -1283,10 +1288,12 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
 
 constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are addressed with 32 bits
 
-// Pairs of blocks multiply 256-row tiles; one row more than a block's 128 has to be there, and tiles for about half of
-// the GPU: with fewer, single blocks that share the k of a tile finish earlier.
-bool enough_for_pairs(int64_t batch, int64_t M, int64_t N) {
-    return M > kBM && batch * ((M + 2 * kBM - 1) / (2 * kBM)) * ((N + 255) / 256) * 2 >= kSMs / 2;
+// Pairs of blocks multiply 256-row tiles; one row more than a block's 128 has to be there, and tiles for a share of the GPU:
+// with fewer, single blocks that share the k of a tile finish earlier.  A quarter of the SMs where lanes are tokens (256 tokens,
+// 1024 to 1024: 12.4 us in pairs from 5 to 12 workers, 16.5 us by single blocks), half for the weight gradient (its single
+// blocks take 12.5 us up to 9 workers of 1024 x 1024, pairs 16.5 us from 10 on).
+bool enough_for_pairs(int64_t batch, int64_t M, int64_t N, int sms) {
+    return M > kBM && batch * ((M + 2 * kBM - 1) / (2 * kBM)) * ((N + 255) / 256) * 2 >= sms;
 }
 
 int current_device() {
@@ -1335,7 +1342,7 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, a.activation, a.y, a.residual, a.bias, a.bias_stride, a.z8};
     if (rc != PG_OK) return rc;
-    if (enough_for_pairs(a.batch, a.tokens, a.out_features) && aligned(a.y, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
+    if (enough_for_pairs(a.batch, a.tokens, a.out_features, kSMs / 4) && aligned(a.y, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
         return run_product<kForwardRows, true>(a.dtype, a.batch, a.tokens, a.out_features, a.in_features, x, w, ep, nullptr, st);
     return run_product<kForward, false>(a.dtype, a.batch, a.out_features, a.tokens, a.in_features, w, x, ep, nullptr, st);
 }
@@ -1366,7 +1373,7 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     if (rc == PG_OK) rc = aligned_operand(w, a.batch, a.out_features, a.in_features, at, st);
     const Epilogue ep{0, PG_ACT_NONE, a.dx, a.residual, nullptr, 0, {}};
     if (rc != PG_OK) return rc;
-    if (enough_for_pairs(a.batch, a.tokens, a.in_features) && aligned(a.dx, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
+    if (enough_for_pairs(a.batch, a.tokens, a.in_features, kSMs / 4) && aligned(a.dx, a.batch, a.tokens) && a.residual.ld < kMaxResidualLd)
         return run_product<kInputGradRows, true>(a.dtype, a.batch, a.tokens, a.in_features, a.out_features, dz, w, ep, nullptr, st);
     return run_product<kInputGrad, false>(a.dtype, a.batch, a.in_features, a.tokens, a.out_features, w, dz, ep, nullptr, st);
 }
@@ -1400,7 +1407,7 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
     pg_matrix dz = a.dz, x = a.x;
     int rc = a.tokens > 0 ? aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st) : PG_OK;
     if (rc != PG_OK) return rc;
-    const bool pairs = enough_for_pairs(a.batch, a.in_features, a.out_features);
+    const bool pairs = enough_for_pairs(a.batch, a.in_features, a.out_features, kSMs / 2);
     if (eight) {
         x = pg_matrix{a.x8.values, a.x8.ld, a.x8.stride};
         return pairs ? run_product<kWeightGrad8, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st)

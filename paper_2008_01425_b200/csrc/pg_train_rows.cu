@@ -316,7 +316,8 @@ sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, floa
 // A block takes a strip of 256 columns and a share of a worker's tokens; 8 rows at a time, one per
 // warp, four times that in flight.  Column sums stay in registers, are joined over the warps in shared
 // memory and over the blocks of a cluster (the shares of one strip) through distributed shared memory, in
-// a fixed order.
+// a fixed order.  (Three blocks per SM with four rows in flight: 76 us for 700 tokens x 2600 columns of 32 workers; two blocks with
+// more registers 97 us, four with two rows 86 us.)
 constexpr int kStrip = 256, kStripRows = 4;
 template <typename H, int W, int WO, int ACT>
 __global__ void __launch_bounds__(256, 3)
