@@ -296,8 +296,8 @@ static_assert(sizeof(Shared) <= kStaticBytes, "Shared");
 
 // Lanes are tokens: a warp takes every third group of 32 columns of its 32 rows.  The residuals of the next group are on
 // their way to shared memory while one group is computed, and while the first one's accumulator is waited for: neighbouring
-// lanes copy neighbouring 16-byte pieces, four of a row or five where it starts between two (a lane that fetched its own row
-// touched 32 lines per load, which cost a quarter of the time).  The result goes through shared memory too, in the
+// lanes copy neighbouring 16-byte pieces, four of a row or five where it starts between two (a lane that fetches its own row
+// touches 32 lines per load).  The result goes through shared memory too, in the
 // 64-byte swizzle of the output's tensor map, and leaves by TMA, which also cuts off what lies outside the matrix.
 struct Residuals {             // of a tile: where a lane's five pieces start, from the tile's first column on
     const char* base;
