@@ -24,6 +24,7 @@
 #include <mutex>
 
 #include "pg_train_device.h"
+#include "pg_train_ranges.h"
 
 namespace pgt {
 namespace {
@@ -858,12 +859,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int m0, n0;
             place(tile, b, m0, n0);
             const uint8_t* at = p.scales + b * p.scale_stride + m0 / kBlock8;
-            const int blocks = min(4, (p.M - m0 + kBlock8 - 1) / kBlock8);
+            const int count = scales_of_tile(p.M, m0);     // none for a second block that begins behind the last row of A
             for (int kb = kb0; kb < kb1; kb += kScaleStages) {
                 if (turn > 0 && !(ok = bar_wait(&sh.scales_empty[half], (turn - 1) & 1, gave_up))) break;
                 const int64_t k0 = static_cast<int64_t>(kb) * kBK, k1 = min(static_cast<int64_t>(p.K), k0 + kScaleStages * kBK);
                 uint32_t* to = scale_ring + half * kScaleStages * kBK;
-                // a row's four bytes, cut out of the one or two words that hold them; all rows' on their way together
+                // a row's four bytes, cut out of the one or two words that hold them (no others are read); all rows' on their way together
                 constexpr int kRows = kScaleStages * kBK / 32;
                 uint32_t lo[kRows], hi[kRows];
 #pragma unroll
@@ -871,9 +872,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const int64_t k = k0 + lane + 32 * u;
                     const uintptr_t from = reinterpret_cast<uintptr_t>(at + k * p.scale_ld);
                     const uint32_t* word = reinterpret_cast<const uint32_t*>(from & ~uintptr_t{3});
+                    const int words = k < k1 ? words_of_scales(from, count) : 0;
                     lo[u] = hi[u] = 0;
-                    if (k < k1) lo[u] = word[0];
-                    if (k < k1 && static_cast<int>(from & 3) + blocks > 4) hi[u] = word[1];
+                    if (words > 0) lo[u] = word[0];
+                    if (words > 1) hi[u] = word[1];
                 }
 #pragma unroll
                 for (int u = 0; u < kRows; ++u) {
