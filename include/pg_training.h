@@ -96,7 +96,8 @@ PG_API int pg_add_rms_norm(const pg_norm_args *args, void *stream);
  * Its gradient.  With u = h rstd and a = dy gain:
  *     dx = rstd (a - u mean(a u)) + dh          (also the gradient of `residual`)
  *     dgain = sum over tokens of dy u           (added to what is there with accumulate)
- * h is the stored sum, in 16 bits or as its 8-bit checkpoint (exactly one of h and h8).
+ * h is the stored sum, in 16 bits or as its 8-bit checkpoint (exactly one of h and h8).  At most
+ * 16384 columns: PG_ERR_TOO_LARGE from the call and from its workspace query.
  */
 typedef struct pg_norm_grad_args {
     int32_t dtype, batch, tokens, cols;

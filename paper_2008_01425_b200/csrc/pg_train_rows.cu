@@ -473,12 +473,14 @@ void with_row(int cols, F&& f) {
 constexpr int kMaxNormCols = 16384;
 
 // The gradient holds three packed rows, the gains and a sum per column: one octet a thread, or two where that saves
-// the exchange between warps or there is no room for more threads.  `blocks`: resident per SM.
+// the exchange between warps or there is no room for more threads.  `blocks`: resident per SM.  The last one holds kMaxNormCols.
 struct GradRow { int octets, threads, rows, blocks; };
-constexpr GradRow kGradRows[] = {{1, 32, 2, 4}, {2, 32, 2, 3}, {1, 128, 2, 5}, {1, 256, 2, 2}, {1, 512, 2, 1}, {2, 512, 2, 1}, {2, 1024, 1, 1}};
+constexpr int kGradShapes = 7;
+constexpr GradRow kGradRows[kGradShapes] = {{1, 32, 2, 4}, {2, 32, 2, 3}, {1, 128, 2, 5}, {1, 256, 2, 2}, {1, 512, 2, 1}, {2, 512, 2, 1}, {2, 1024, 1, 1}};
+static_assert(kGradRows[kGradShapes - 1].octets * 8 * kGradRows[kGradShapes - 1].threads == kMaxNormCols, "the widest rows");
 int grad_row(int cols) {
     int k = 0;
-    while (kGradRows[k].octets * 8 * kGradRows[k].threads < cols) ++k;
+    while (k + 1 < kGradShapes && kGradRows[k].octets * 8 * kGradRows[k].threads < cols) ++k;
     return k;
 }
 template <typename F>
@@ -558,6 +560,7 @@ int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
 
 int pg_add_rms_norm_grad_workspace_bytes(const pg_norm_grad_args* args, size_t* bytes_out) {
     if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->cols, 1)) return PG_ERR_INVALID;
+    if (args->cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
     *bytes_out = args->dgain ? sizeof(float) * norm_grad_blocks(*args) * static_cast<size_t>(args->batch) * args->cols : 0;
     return PG_OK;
 }

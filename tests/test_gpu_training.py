@@ -609,3 +609,12 @@ def test_refusals_of_the_library(tr):
     assert e.value.status == pg.PG_ERR_TOO_LARGE
     torch.cuda.synchronize()
     assert bool((y == 3.0).all())
+
+
+def test_refusal_of_a_norm_gradient_that_is_too_wide(tr):
+    from paper_2008_01425_b200 import binding as pg
+
+    x, rstd = torch.zeros(1, 2, 16392, device="cuda", dtype=BF), torch.ones(1, 2, device="cuda")
+    with pytest.raises(pg.PowerGossipError) as e:
+        tr.pg_add_rms_norm_grad(x, x, rstd)
+    assert e.value.status == pg.PG_ERR_TOO_LARGE

@@ -77,3 +77,15 @@ def test_the_binding_refuses_cpu_tensors():
         tr.pg_linear(x, x)
     with pytest.raises(ValueError):
         tr.pg_checkpoint_write(x)
+
+
+def test_a_norm_gradient_that_is_too_wide_has_no_workspace(lib):
+    """The query refuses what the call refuses, and does not touch the size."""
+    query = lib.pg_add_rms_norm_grad_workspace_bytes
+    for cols, status in ((1, pg.PG_OK), (16384, pg.PG_OK), (16385, pg.PG_ERR_TOO_LARGE), (20000, pg.PG_ERR_TOO_LARGE), (1 << 30, pg.PG_ERR_TOO_LARGE)):
+        a = tr.pg_norm_grad_args()
+        a.batch, a.tokens, a.cols, a.dgain = 2, 64, cols, 256
+        n = ctypes.c_size_t(7)
+        assert query(ctypes.byref(a), ctypes.byref(n)) == status, cols
+        # at least one row of partial sums per worker, at most one per token
+        assert n.value == 7 if status else 2 * cols * 4 <= n.value <= 2 * 64 * cols * 4, cols
