@@ -40,6 +40,12 @@ constexpr int kRawBytes = kBM * kBK;          // a stage of an 8-bit A before it
 constexpr int kScaleStages = 8;               // stages whose scales are fetched at once, 4 bytes for each of their k
 constexpr int kScaleBytes = 2 * kScaleStages * kBK * 4;
 constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their own, since they are needed before A and B are
+// Pairs, 8-bit A: the second block's widened stages are reported to the first block in groups.  An arrival that releases to the
+// cluster takes one to two thousand cycles, a stage's products 512; a group also waits for its last stage, and there are five
+// stages in all (64 workers x 2048 tokens, 1024 x 1024: 544, 315, 304 and 317 us for groups of one to four; 32 x 700, 650 x 2600:
+// 211, 137, 134 and 138 us).
+constexpr int kFarStages = 3, kFarGroups = 8;
+static_assert((kRingBytes - kMinRaw * kRawBytes - kScaleBytes) / (kABytes + 128 * kBK * 2) >= kFarStages, "a group fits the ring");
 // Blocks of k that tensor memory sums in one go for a weight gradient.  The tensor cores cut a sum off where fp32 arithmetic
 // would round it, and the more bits the products have the more of them: of a gradient's size, 0.99e-6 over 1024 tokens
 // for bf16 and 1.25e-6 for fp16 operands, 0.45e-6 over 2048 for bf16 with x from 8 bits, 0.76e-6 over 1024 for fp16 with it.
@@ -110,18 +116,28 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
         : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok != 0;
 }
+// The same, acquiring from the whole cluster.
+__device__ __forceinline__ bool bar_try_cluster(uint64_t* b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
 // Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).  The time is looked at
 // after a few thousand tries only.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up) {
+    auto over = [&] { return CLUSTER ? bar_try_cluster(b, parity) : bar_try(b, parity); };
 #pragma unroll 1
     for (int i = 0; i < 4096; ++i)
-        if (bar_try(b, parity)) return true;
+        if (over()) return true;
     long long t0, t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 1024; ++i)
-            if (bar_try(b, parity)) return true;
+            if (over()) return true;
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
         if (t - t0 > kWaitNs) {
@@ -151,11 +167,9 @@ __device__ __forceinline__ uint32_t first_of_pair(uint64_t* b) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(b)));
     return r;
 }
-// An arrival there.  It releases what this thread wrote to its own block only, and that is what is read after it: each block's
-// tensor core takes its operands from its own shared memory.  (Released to the whole cluster, an arrival took about
-// a thousand cycles, two stages' worth.)
+// An arrival there that releases to the whole cluster what this thread wrote or has seen written.
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Arrivals that say no more than that an accumulator has been read (tcgen05.wait::ld and the fence before them see to that).
 __device__ __forceinline__ void bar_arrive_read_at(uint32_t bar) {
@@ -290,6 +304,7 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
 
 struct Shared {
     uint64_t raw[kMaxRaw], raw_empty[kMaxRaw], scaled[2], scales_empty[2], loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
+    uint64_t far_widened[kFarGroups];     // pairs: the second block's stages, a group at a time
     uint32_t tmem;
     int gave_up;
 };
@@ -628,9 +643,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&sh.loaded[s], 1);
-            bar_init(&sh.widened[s], 8 * kBlocks);
+            bar_init(&sh.widened[s], 8);
             bar_init(&sh.empty[s], 1);
         }
+        for (int g = 0; g < kFarGroups; ++g) bar_init(&sh.far_widened[g], 1);
         for (int s = 0; s < kMaxRaw; ++s) {
             bar_init(&sh.raw[s], 1);
             bar_init(&sh.raw_empty[s], 8);
@@ -733,6 +749,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint64_t ring_a = operand_desc(smem_u32(ring), kAMn), ring_b = operand_desc(smem_u32(ring) + kABytes, kBMn);
         const int last_steps = (p.K - (p.k_blocks - 1) * kBK + 15) / 16;        // of the last block of k; the others have four
         int s = 0, parity = 0, done = 0;
+        [[maybe_unused]] int in_group = 0, group = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int kb = kb0;
@@ -744,6 +761,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (; kb < to; ++kb) {
                     if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
                     if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
+                    if constexpr (kEight && PAIR) {
+                        if (in_group == 0 && !(ok = bar_wait<true>(&sh.far_widened[group % kFarGroups], group / kFarGroups & 1, gave_up))) break;
+                        if (++in_group == kFarStages) {
+                            in_group = 0;
+                            ++group;
+                        }
+                    }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
                     if (elected()) {
@@ -772,6 +796,25 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (!ok) {
             if (elected()) mma_commit<PAIR>(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
+        }
+    } else if (kEight && PAIR && warp == 1) {
+        // The second block's widened stages, reported to the first block, whose thread issues the products that read them: the
+        // widening warps' writes are seen here by the block's own barrier, and passed on by one release to the cluster.
+        const uint32_t far = first_of_pair(&sh.far_widened[0]);
+        const int64_t left = p.tiles > first ? (p.tiles - first + step - 1) / step * (kb1 - kb0) : 0;
+        int s = 0, parity = 0, in_group = 0, group = 0;
+        for (int64_t i = 0; i < left; ++i) {
+            if (!bar_wait(&sh.widened[s], parity, gave_up)) break;
+            if (++in_group == kFarStages || i + 1 == left) {
+                if (elected()) bar_arrive_at(far + group % kFarGroups * 8);
+                __syncwarp();
+                in_group = 0;
+                ++group;
+            }
+            if (++s == p.stages) {
+                s = 0;
+                parity ^= 1;
+            }
         }
     } else if (warp >= 4 && warp < 4 + kEpilogueWarps<MODE>) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -891,7 +934,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else if (kEight && warp >= 12) {
         // Eight lanes take the 128 values of a row (one k) of the stage, 16 each, and a thread two rows.
         const int c = lane & 7, r0 = (warp - 12) * 4 + (lane >> 3);    // rows r0 and r0 + 32
-        [[maybe_unused]] const uint32_t widened = first_of_pair(&sh.widened[0]);
         const int64_t left = kb1 > kb0 && p.tiles > first ? (p.tiles - first + step - 1) / step * (kb1 - kb0) : 0;
         int s = 0, turn = 0, q = 0, raw_parity = 0, kb = kb0, half = 0, scale_parity = 0;
         for (int64_t i = 0; i < left; ++i) {
@@ -945,10 +987,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) bar_arrive_at(widened + s * 8);
-                else bar_arrive(&sh.widened[s]);
-            }
+            if (lane == 0) bar_arrive(&sh.widened[s]);
             if (++s == p.stages) {
                 s = 0;
                 ++turn;
