@@ -147,6 +147,18 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         }
     }
 }
+// After a wait that gave up: the last copies that were issued to a ring of `n` stages, `issued` in all, land (or a limit is reached).
+__device__ __noinline__ void await_copies(uint64_t* bars, int n, int64_t issued) {
+    for (int64_t i = issued > n ? issued - n : 0; i < issued; ++i)
+        for (int t = 0; t < 100000 && !bar_try(&bars[i % n], static_cast<uint32_t>(i / n) & 1); ++t) {}
+}
+// The same where they cannot be waited for: a hundred times what a copy takes.
+__device__ __noinline__ void pause() {
+    long long t0, t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+    do asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    while (t - t0 < 200000);
+}
 __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
@@ -736,11 +748,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
             }
         }
-        if (!ok)       // copies still on their way must land before the block ends (those of a second block: see the end)
-            for (int64_t i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i) {
-                const int st = static_cast<int>(i % p.stages), parity = static_cast<int>(i / p.stages) & 1;
-                for (int t = 0; t < 100000 && in_pair == 0 && !bar_try(&sh.loaded[st], parity); ++t) {}
-            }
+        // copies still on their way must land before the block ends
+        if (!ok && in_pair == 0) await_copies(sh.loaded, p.stages, issued);
+        if (!ok && in_pair != 0) pause();                  // a second block's are reported to the first
     } else if (warp == 1 && in_pair == 0) {
         constexpr uint32_t fmt = std::is_same<H, __half>::value ? 0 : 1;
         const uint32_t idesc = 1u << 4 | fmt << 7 | fmt << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
@@ -871,6 +881,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (kTokenRows<MODE> && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (kEight && warp == 2) {
         int q = 0, turn = 0;
+        int64_t issued = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int64_t b;
@@ -883,15 +894,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     tma_load(raw_ring + q * kRawBytes, &map_a, m0, kb * kBK, p.a_shared ? 0 : static_cast<int>(b), &sh.raw[q]);
                 }
                 __syncwarp();
+                ++issued;
                 if (++q == p.raw_stages) {
                     q = 0;
                     ++turn;
                 }
             }
         }
-        if (!ok)       // copies still on their way must land before the block ends
-            for (int i = 0; i < p.raw_stages; ++i)
-                for (int t = 0; t < 100000 && i < q && !bar_try(&sh.raw[i], turn & 1); ++t) {}
+        if (!ok) await_copies(sh.raw, p.raw_stages, issued);
     } else if (kEight && warp == 3) {
         // The scales of an 8-bit A, for eight stages at a time, so that no load is outstanding when they are handed over:
         // an arrival on a barrier (and a fence) waits for the thread's earlier loads, and one per stage would wait for memory.
