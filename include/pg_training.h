@@ -190,10 +190,19 @@ PG_API int pg_checkpoint_read(const pg_checkpoint_args *args, void *stream);
 
 /*
  * Wait for `stream` and report whether a bounded device-side wait of these kernels gave up on the
- * current device since the last call (PG_ERR_TIMEOUT; the outputs of that call are not valid), then
- * clear the word.  PG_OK otherwise.
+ * current device since the last call (PG_ERR_TIMEOUT), then clear the word.  PG_OK otherwise.  A wait
+ * gives up after two seconds; the outputs of its call are not valid then, and nothing else says so: ask
+ * before results are used, as after a training step.  There is one word per device, for all streams:
+ * whoever asks first is told, and has to take every call since the last answer for the one.
  */
 PG_API int pg_training_status(void *stream);
+
+/*
+ * Self-test of the bounded wait: a block waits, for a millisecond at most, on a barrier that nothing
+ * arrives on.  Waits for `stream` and returns PG_ERR_TIMEOUT when that was reported (the expected
+ * outcome), PG_OK if not.  Clears the word, as pg_training_status does.
+ */
+PG_API int pg_selftest_training_timeout(void *stream);
 
 #ifdef __cplusplus
 }

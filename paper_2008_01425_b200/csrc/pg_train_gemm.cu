@@ -127,7 +127,7 @@ __device__ __forceinline__ bool bar_try_cluster(uint64_t* b, uint32_t parity) {
 // Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).  The time is looked at
 // after a few thousand tries only.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up) {
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, long long limit = kWaitNs) {
     auto over = [&] { return CLUSTER ? bar_try_cluster(b, parity) : bar_try(b, parity); };
 #pragma unroll 1
     for (int i = 0; i < 4096; ++i)
@@ -140,7 +140,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
             if (over()) return true;
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-        if (t - t0 > kWaitNs) {
+        if (t - t0 > limit) {
             *gave_up = 1;
             atomicOr(&g_training_error, 1u);
             return false;
@@ -1176,6 +1176,18 @@ align_rows_kernel(const uint16_t* __restrict__ src, int64_t src_ld, int64_t src_
     *reinterpret_cast<uint4*>(dst + row * dst_ld + col) = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
 }
 
+// The products' wait on a barrier that nothing arrives on, by a whole block and with a limit of a millisecond.
+__global__ void __launch_bounds__(64) wait_probe_kernel() {
+    __shared__ uint64_t bar;
+    __shared__ int gave_up;
+    if (threadIdx.x == 0) {
+        bar_init(&bar, 1);
+        gave_up = 0;
+    }
+    __syncthreads();
+    bar_wait(&bar, 0, &gave_up, 1000000);
+}
+
 // ------------------------------------------------------------------ host
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1470,6 +1482,10 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
                  : run_product<kWeightGrad, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
 }
 
+int pg_selftest_training_timeout(void* stream) {
+    wait_probe_kernel<<<1, 64, 0, static_cast<cudaStream_t>(stream)>>>();
+    return launch_status() == PG_OK ? pg_training_status(stream) : PG_ERR_CUDA;
+}
 int pg_training_status(void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned word = 0;

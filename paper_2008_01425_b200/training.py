@@ -368,11 +368,21 @@ def pg_checkpoint_read(x8: Checkpoint8, out=None, stream=None):
     return x
 
 
-def pg_training_status(stream=None, device="cuda") -> int:
-    """Waits for `stream` (torch's current one if None) and returns PG_OK, or PG_ERR_TIMEOUT if a bounded
-    device-side wait gave up since the last call."""
+def _ask(fn, stream, device) -> int:
     device = torch.device(device)
     with torch.cuda.device(device):
         handle = torch.cuda.current_stream(device).cuda_stream if stream is None else \
             stream if isinstance(stream, int) else stream.cuda_stream
-        return int(load_library().pg_training_status(_vp(handle)))
+        return int(fn(_vp(handle)))
+
+
+def pg_training_status(stream=None, device="cuda") -> int:
+    """Waits for `stream` (torch's current one if None) and returns PG_OK, or PG_ERR_TIMEOUT if a bounded
+    device-side wait gave up on the device, on any stream, since the last call: outputs since then are not
+    to be trusted.  No other call asks, so ask before results are used (once a step, say)."""
+    return _ask(load_library().pg_training_status, stream, device)
+
+
+def pg_selftest_training_timeout(stream=None, device="cuda") -> int:
+    """Lets a bounded wait run out, within a millisecond; PG_ERR_TIMEOUT if that is reported."""
+    return _ask(load_library().pg_selftest_training_timeout, stream, device)

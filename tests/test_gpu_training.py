@@ -634,3 +634,15 @@ def test_weight_gradients_in_pairs_of_blocks_repeat_bit_for_bit(tr, shape, dtype
     x = tr.pg_checkpoint_read(x8)
     size = (dz[0].double().abs().transpose(0, 1) @ x[0].double().abs())
     assert float(((first[0] - tr.pg_linear_weight_grad(dz, x)[0]).double().abs() / size).max()) <= 2 * (t + 2) * 2 * U
+
+
+def test_a_wait_that_runs_out_is_reported_once(tr):
+    from paper_2008_01425_b200 import binding as pg
+
+    assert tr.pg_training_status() == pg.PG_OK
+    assert tr.pg_selftest_training_timeout() == pg.PG_ERR_TIMEOUT
+    assert tr.pg_training_status() == pg.PG_OK               # told once; the GPU goes on
+    s = torch.cuda.Stream()
+    assert tr.pg_selftest_training_timeout(stream=s) == pg.PG_ERR_TIMEOUT
+    x, w = torch.ones(1, 4, 64, device="cuda", dtype=BF), torch.ones(1, 32, 64, device="cuda", dtype=BF)
+    assert bool((tr.pg_linear(x, w) == 64).all()) and tr.pg_training_status() == pg.PG_OK
