@@ -8,8 +8,10 @@ expanded (stride 0) is shared by all workers.  Results are allocated with torch 
 given; their rows start on 16-byte boundaries, where every kernel takes its fastest path.
 
 ``stream`` is a torch stream or a raw handle; None means torch's current stream on the tensors'
-device, and a call is then ordered like any torch operation.  On another stream the caller orders
-inputs, and what this module allocates is kept from reuse until that stream has passed the call.
+device, and a call is then ordered like any torch operation.  On another stream the caller orders the
+call after what writes its inputs and before what reads its results.  The memory of both looks after
+itself: results and workspaces come from that stream's memory (torch's current stream may still have work
+to do on its own that is free again), and neither they nor the inputs are reused before both streams have passed.
 
     from paper_2008_01425_b200 import training as tr
     n = tr.pg_add_rms_norm(x, gain, residual=r, eight_bit=True)      # n.h, n.y, n.y8, n.rstd
@@ -157,6 +159,8 @@ class _Call:
             _refuse(self.where, "%s has shape %s, expected %s" % (name, tuple(shape), (rows, cols) if self.single else (self.batch, rows, cols)))
         if one != 1 and cols > 1:
             _refuse(self.where, "%s must have its last dimension contiguous" % name)
+        if self.other is not None:
+            t.record_stream(self.other)
         return pg_matrix(t.data_ptr(), ld if rows > 1 else max(ld, cols), stride if self.batch > 1 else 0)
 
     def matrix8(self, c, rows: int, cols: int, name: str) -> pg_matrix8:
@@ -179,19 +183,25 @@ class _Call:
             _refuse(self.where, "%s has shape %s, expected %s" % (name, tuple(shape), (self.batch, n)))
         if n > 1 and strides[-1] != 1:
             _refuse(self.where, "%s must have its last dimension contiguous" % name)
-        return t.data_ptr(), strides[0] if len(shape) == 2 and self.batch > 1 else 0
-
-    def _own(self, t: torch.Tensor) -> torch.Tensor:
         if self.other is not None:
             t.record_stream(self.other)
+        return t.data_ptr(), strides[0] if len(shape) == 2 and self.batch > 1 else 0
+
+    def _new(self, shape, strides, dtype) -> torch.Tensor:
+        if self.other is None:
+            return _empty(shape, strides, dtype=dtype, device=self.device)
+        current = torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(self.other):
+            t = _empty(shape, strides, dtype=dtype, device=self.device)
+        t.record_stream(current)
         return t
 
     def empty(self, rows: int, cols: int, dtype, unit: int) -> torch.Tensor:
         """Rows start on multiples of `unit` elements."""
         ld = (cols + unit - 1) // unit * unit
         if self.single:
-            return self._own(_empty((rows, cols), (ld, 1), dtype=dtype, device=self.device))
-        return self._own(_empty((self.batch, rows, cols), (rows * ld, ld, 1), dtype=dtype, device=self.device))
+            return self._new((rows, cols), (ld, 1), dtype)
+        return self._new((self.batch, rows, cols), (rows * ld, ld, 1), dtype)
 
     def like(self, rows: int, cols: int) -> torch.Tensor:
         # 16-byte boundaries; 64-byte ones for long rows, whose pieces then fill whole 32-byte sectors of the cache
@@ -203,8 +213,8 @@ class _Call:
     def flat(self, n: int) -> torch.Tensor:
         """fp32 (workers, n), or (n,) for one worker."""
         if self.single:
-            return self._own(_empty((n,), (1,), dtype=torch.float32, device=self.device))
-        return self._own(_empty((self.batch, n), (n, 1), dtype=torch.float32, device=self.device))
+            return self._new((n,), (1,), torch.float32)
+        return self._new((self.batch, n), (n, 1), torch.float32)
 
     def run(self, fn, args, size_fn=None) -> None:
         if _current_device() != self.index:
@@ -218,7 +228,7 @@ class _Call:
             status = size_fn(args, ctypes.byref(need))
             if status == 0:
                 if need.value:
-                    scratch = self._own(_empty((need.value,), (1,), dtype=torch.uint8, device=self.device))
+                    scratch = self._new((need.value,), (1,), torch.uint8)
                     status = fn(args, scratch.data_ptr(), need.value, self.handle)
                 else:
                     status = fn(args, None, 0, self.handle)
@@ -267,6 +277,8 @@ def pg_add_rms_norm_grad(dy, h: Union[torch.Tensor, Checkpoint8], rstd, gain=Non
     if not isinstance(rstd, torch.Tensor) or rstd.device != c.device or rstd.dtype != torch.float32 or rstd.numel() != c.batch * t \
             or not rstd.is_contiguous():
         _refuse(c.where, "rstd must be a contiguous fp32 tensor of %d x %d on %s" % (c.batch, t, c.device))
+    if c.other is not None:
+        rstd.record_stream(c.other)
     eight = isinstance(h, Checkpoint8)
     gp, gs = c.vector(gain, n, "gain")
     dp, ds = c.vector(dgain, n, "gain_grad")

@@ -646,3 +646,51 @@ def test_a_wait_that_runs_out_is_reported_once(tr):
     assert tr.pg_selftest_training_timeout(stream=s) == pg.PG_ERR_TIMEOUT
     x, w = torch.ones(1, 4, 64, device="cuda", dtype=BF), torch.ones(1, 32, 64, device="cuda", dtype=BF)
     assert bool((tr.pg_linear(x, w) == 64).all()) and tr.pg_training_status() == pg.PG_OK
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_memory_of_calls_on_another_stream(tr, raw):
+    """Results do not lie in memory that the current stream still writes, and inputs that are let go are not
+    reused under the call."""
+    g = gen(14)
+    x, w = rand(g, 4, 250, 515).to(BF), rand(g, 4, 520, 515, scale=0.05).to(BF)     # rows that need a workspace
+    want = tr.pg_linear(x, w, activation="gelu")
+    grads = tr.pg_linear_weight_grad(want, x)
+    s = torch.cuda.Stream()
+    stream = s.cuda_stream if raw else s
+    torch.cuda.synchronize()
+    for _ in range(3):
+        held = [torch.empty_strided(want.shape, want.stride(), dtype=BF, device="cuda"), torch.empty_like(grads),
+                torch.empty(16 << 20, dtype=torch.uint8, device="cuda")]
+        mine = [t.untyped_storage().data_ptr() for t in held]
+        torch.cuda._sleep(20_000_000)                     # some ten milliseconds
+        for t in held:
+            t.fill_(1)
+        del held, t
+        y = tr.pg_linear(x, w, activation="gelu", stream=stream)
+        dw = tr.pg_linear_weight_grad(want, x, stream=stream)
+        assert y.untyped_storage().data_ptr() not in mine and dw.untyped_storage().data_ptr() not in mine
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(dw, grads)
+    x2, w2 = x.clone(), w.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    y = tr.pg_linear(x2, w2, activation="gelu", stream=stream)
+    gone = [t.data_ptr() for t in (x2, w2)]
+    del x2, w2
+    over = [torch.full_like(x, float("nan")), torch.full_like(w, float("nan"))]
+    assert not set(gone) & {t.data_ptr() for t in over}
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_the_default_stream_by_its_handle(tr):
+    g = gen(15)
+    x, w = rand(g, 2, 30, 64).to(BF), rand(g, 2, 48, 64).to(BF)
+    want = tr.pg_linear(x, w)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = tr.pg_linear(x, w, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
