@@ -355,9 +355,15 @@ class PowerGossip:
         return self._layer_of_all(grads, layer, *self.pg_stack_offset(0, layer))
 
     def params_layer(self, layer: int, stream=None):
-        """(workers x rows x cols) view of one layer of all workers in the workspace (see pg_params_device)."""
+        """(workers x rows x cols) view of one layer of all workers in the workspace, what pg_params_device gives
+        for one: any pending correction is applied first, on `stream`, and the cached forward product is
+        dropped, since the view may be written to; call it again after every round.  `stream`: None is torch's
+        current stream here, as for the training calls that read the view (pg_params_device and the rounds take
+        None as the default stream; give them torch's current one where that is another)."""
         import torch
 
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
         x = self.pg_params_device(0, layer, stream)
         return self._layer_of_all(self._workspace.view(torch.float32), layer, x.storage_offset(), x.stride(0))
 

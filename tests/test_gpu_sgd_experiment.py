@@ -45,3 +45,29 @@ def test_the_ring_learns():
     errors = [c[1] for c in curve]
     assert all(b < a for a, b in zip(errors, errors[1:])) and errors[-1] < 0.5 * errors[0]
     assert curve[-1][2] < 0.05                     # the workers see different data and stay together
+
+
+def test_the_step_stays_on_the_current_stream(monkeypatch):
+    """Inside another current stream everything of a step, the view of the parameters included, is enqueued there."""
+    from paper_2008_01425_b200 import binding as pg
+    from paper_2008_01425_b200 import sgd_experiment as sgd
+
+    nets = [sgd.ResidualNet(n_workers=4, width=64, hidden=96, blocks=1, seed=3) for _ in range(2)]
+    batches = [sgd.data(nets[0], 40, 64, seed=k) for k in range(3)]
+    for x, target in batches:
+        nets[0].step(x, target, eta=0.5)
+    s, seen = torch.cuda.Stream(), []
+    inner = pg.PowerGossip.pg_params_device
+    monkeypatch.setattr(pg.PowerGossip, "pg_params_device",
+                        lambda self, worker, layer, stream=None: seen.append(stream) or inner(self, worker, layer, stream))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)                      # a step that left the stream would overtake the others
+        for x, target in batches:
+            nets[1].step(x, target, eta=0.5)
+    assert seen and all(getattr(v, "cuda_stream", v) == s.cuda_stream for v in seen)
+    torch.cuda.synchronize()
+    for layer in range(len(nets[0].net.layer_shapes)):
+        assert torch.equal(nets[0].net.params_layer(layer), nets[1].net.params_layer(layer))
+    for n in nets:
+        n.net.close()
