@@ -91,23 +91,43 @@ norm_kernel(const pg_norm_args a) {
             }
         }
     }
+    auto sum_of_row = [&](F2 sums) {
+        float sum = sum2(sums);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if constexpr (T > 32) {
+            if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
+            __syncthreads();
+            sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < T / 32; ++w) sum += s_part[w];
+        }
+        return sum;
+    };
     F2 sums = both(0.0f);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sums = fma(v[c][i], v[c][i], sums);
-    float sum = sum2(sums);
+    float sum = sum_of_row(sums), scale = 1.0f, eps = a.eps;
+    // bf16 reaches to 2^128 and fp32 squares do not: where the sum leaves fp32's range, at the upper end or (with an eps too small
+    // to matter there) at the lower one, it is taken once more of the row times a power of two.  The same for the whole row.
+    if (!(sum <= 3.4028235e38f) || (sum < 8.2718061e-25f && eps < 7.8886091e-31f)) {       // 2^-80, 2^-100
+        scale = sum < 1.0f ? 7.9228163e28f : 1.2621774e-29f;                               // 2^96, 2^-96
+        eps = eps * scale * scale;
+        sums = both(0.0f);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if constexpr (T > 32) {
-        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
-        __syncthreads();
-        sum = 0.0f;
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int w = 0; w < T / 32; ++w) sum += s_part[w];
+            for (int i = 0; i < 4; ++i) {
+                const F2 w = mul(v[c][i], both(scale));
+                sums = fma(w, w, sums);
+            }
+        if constexpr (T > 32) __syncthreads();         // (the shares of the first sum have been read)
+        sum = sum_of_row(sums);
     }
-    const float rstd = rsqrtf(sum / a.cols + a.eps);
-    if (a.rstd && t == 0) a.rstd[b * a.tokens + tok] = rstd;
+    const float rstd = rsqrtf(sum / a.cols + eps);     // of the scaled row
+    if (a.rstd && t == 0) a.rstd[b * a.tokens + tok] = rstd * scale;
     if (a.h.data) {
         uint16_t* h = static_cast<uint16_t*>(a.h.data) + b * a.h.stride + tok * a.h.ld;
 #pragma unroll
@@ -124,6 +144,12 @@ norm_kernel(const pg_norm_args a) {
         }
     }
     if (!a.y.data && !a.y8.values) return;
+    if (scale != 1.0f) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[c][i] = mul(v[c][i], both(scale));
+    }
     const bool wide = wide_gain(gain);
     uint16_t* y = a.y.data ? static_cast<uint16_t*>(a.y.data) + b * a.y.stride + tok * a.y.ld : nullptr;
     int8_t* q = a.y8.values + b * a.y8.stride + tok * a.y8.ld;

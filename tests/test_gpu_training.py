@@ -694,3 +694,29 @@ def test_the_default_stream_by_its_handle(tr):
         got = tr.pg_linear(x, w, stream=0)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n", [1, 650, 1000, 1100, 4608, 16384])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+@pytest.mark.parametrize("residual,with8", [(False, False), (True, True)])
+def test_norms_of_rows_whose_squares_leave_fp32(tr, n, eps, residual, with8):
+    """bf16 reaches from 2^-133 to 2^128; the squares' sum does not fit fp32 at either end, the result always does."""
+    g = gen(n)
+    sizes = [3e38, 1e37, 2e19, 1e18, 1.0, 1e-12, 1e-18, 1e-20, 1e-30, 1e-36]
+    v = (rand(g, 1, len(sizes), n) * 0.2).clamp(-0.99, 0.99)
+    v[..., 0] = 0.5
+    x = (v.double() * torch.tensor(sizes, device="cuda").double()[:, None]).to(BF)
+    r = (x * 0.25) if residual else None
+    x = x * 0.75 if residual else x
+    gain = 1 + 0.3 * rand(g, 1, n)
+    out = tr.pg_add_rms_norm(x, gain, residual=r, eps=eps, eight_bit=with8)
+    s = x.double() + (r.double() if residual else 0.0)
+    root = ((s * s).mean(-1) + float(torch.tensor(eps, dtype=torch.float32))) ** -0.5
+    # as for other rows; a root below fp32's smallest normal number is held in steps of 2^-149, and so are sums of numbers that small
+    check(out.rstd, root, root * (n + 40) * 2 * U + 2.0 ** -149)
+    y = s * root[..., None] * gain.double()[:, None]
+    slack = y.abs() * (n + 40) * 2 * U + 2.0 ** -149 * root[..., None] * gain.double()[:, None].abs()
+    if with8:
+        check8(out.y8, y, slack, BF)
+    else:
+        check(out.y, y, slack, BF)
