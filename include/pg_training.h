@@ -75,7 +75,8 @@ typedef struct pg_matrix8 {
  * h gets s rounded to 16 bits (the next residual stream; may be x or residual in place), y the
  * result.  At most 16384 columns (PG_ERR_TOO_LARGE).  With y8, the 8-bit form of the result is written too and y holds the values it stands
  * for: the layer behind the norm then sees in its forward pass what its weight gradient will read.
- * h8 gets the 8-bit form of h, the checkpoint that pg_add_rms_norm_grad reads.
+ * h8 gets the 8-bit form of h as it is stored, in 16 bits (what pg_checkpoint_write makes of it), the checkpoint
+ * that pg_add_rms_norm_grad reads.
  */
 typedef struct pg_norm_args {
     int32_t dtype, batch, tokens, cols;

@@ -139,7 +139,9 @@ norm_kernel(const pg_norm_args a) {
         uint8_t* s = a.h8.scales + b * a.h8.scale_stride + tok * a.h8.scale_ld;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            F2 w[4] = {v[c][0], v[c][1], v[c][2], v[c][3]};
+            F2 w[4];                                       // of h as it is stored, in 16 bits
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = Elem<H>::up2(Elem<H>::down2(v[c][i]));
             octet_to_8<H>(w, q, s, (c * T + t) * 8, a.cols);
         }
     }

@@ -720,3 +720,18 @@ def test_norms_of_rows_whose_squares_leave_fp32(tr, n, eps, residual, with8):
         check8(out.y8, y, slack, BF)
     else:
         check(out.y, y, slack, BF)
+
+
+@pytest.mark.parametrize("shape", [(3, 17, 33), (2, 33, 650), (2, 9, 1024), (1, 3, 4608), (1, 2, 16384)])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1)])
+def test_the_norms_checkpoint_is_that_of_its_stored_sum(tr, shape, dtype, pad):
+    g = gen(hash(shape) % 1000 + 7)
+    x, r = strided(rand(g, *shape, scale=2.0).to(dtype), pad), strided(rand(g, *shape).to(dtype), pad)
+    if dtype == HF:
+        x[0, 0, 0] = r[0, 0, 0] = 6e4                    # the sum has no place in fp16
+    out = tr.pg_add_rms_norm(x, residual=r, save_h8=True)
+    want = tr.pg_checkpoint_write(out.h)
+    fine = want.scales != 255                            # a block that is not finite has no values
+    assert torch.equal(out.h8.scales, want.scales)
+    fine = fine.repeat_interleave(32, dim=-1)[..., :shape[-1]]
+    assert torch.equal(out.h8.values[fine], want.values[fine])
