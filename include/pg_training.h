@@ -19,7 +19,9 @@
  *     must not overlap.  An optional matrix or vector is left out by a null pointer.
  *   - 16-bit elements are bf16 or fp16 (`dtype`), the same for all 16-bit matrices of a call;
  *     biases, gains, statistics and parameter gradients are fp32, as the parameter stack is.
- *   - Sums, statistics and products are held in fp32 and rounded once, where a result is stored.
+ *   - Sums, statistics and products are held in fp32 and rounded once, where a result is stored.  (The
+ *     tensor cores cut sums off instead of rounding them: of a weight gradient's size that is under
+ *     1e-6, as for an fp32 product, and up to 5e-6 where all products have the same sign.)
  *   - tokens = 0 and batch = 0 are valid: outputs per token are empty, sums over tokens are zero.
  *   - A NaN or an infinity in an input reaches the outputs that depend on it, and no others.
  *   - Rows may start on any element.  Where they start on 16-byte boundaries the kernels take their

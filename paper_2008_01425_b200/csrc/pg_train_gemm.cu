@@ -47,10 +47,15 @@ constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their ow
 constexpr int kFarStages = 3, kFarGroups = 8;
 static_assert((kRingBytes - kMinRaw * kRawBytes - kScaleBytes) / (kABytes + 128 * kBK * 2) >= kFarStages, "a group fits the ring");
 // Blocks of k that tensor memory sums in one go for a weight gradient.  The tensor cores cut a sum off where fp32 arithmetic
-// would round it, and the more bits the products have the more of them: of a gradient's size, 0.99e-6 over 1024 tokens
-// for bf16 and 1.25e-6 for fp16 operands, 0.45e-6 over 2048 for bf16 with x from 8 bits, 0.76e-6 over 1024 for fp16 with it.
-// Longer sums are added up, rounding, from parts that stay under 1e-6, as an fp32 product's do.
-constexpr int max_chunk(bool eight, int dtype) { return !eight ? 768 / kBK : dtype == PG_BF16 ? 2048 / kBK : 1024 / kBK; }
+// would round it, so the error grows with the length of the sum and, unlike a rounded one's, does not average out; the more bits
+// the products have the sooner.  Longer sums are added up, rounding, from parts of this length.  Error of a gradient relative to
+// its size for tokens of different sizes, by blocks in a part (an fp32 product's over 768 tokens: 0.25e-6 bf16, 0.49e-6 fp16):
+//   bf16         8: 0.55e-6   12: 0.83e-6   16: 1.12e-6           fp16         8: 0.65e-6   12: 0.95e-6   16: 1.25e-6
+//   bf16, x8    12: 0.26e-6   16: 0.38e-6   32: 0.87e-6           fp16, x8    12: 0.74e-6   16: 1.0e-6    32: 2.1e-6
+// and time over 2048 tokens for 64 workers of 1024 x 1024: 519, 317, 277, 241 and 215 us for 4, 8, 12, 16 and 32 (x8: 590, 363, 336,
+// 319 and 309 us).  Chosen: the longest parts that stay under 1e-6, and half of that for bf16 from 8 bits, where it costs 3 %.
+// Sums of products that all have one sign lose more: 1.5e-6 (bf16), 4.4e-6 (fp16), 0.75e-6 and 1.2e-6 (x8).
+constexpr int max_chunk(bool eight, int dtype) { return eight && dtype == PG_BF16 ? 1024 / kBK : 768 / kBK; }
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
 constexpr long long kWaitNs = 2000000000;   // a wait longer than this gives up
 
@@ -1317,7 +1322,9 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
         while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= (p.splits == 4 ? kSMs / 2 : kSMs) && p.k_blocks >= p.splits * 2) p.splits *= 2;
     const int b_rows = p.BN / kBlocks;
     const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
-    // (The other products are rounded to 16 bits, beside which what is cut off is nothing.)
+    // The other products sum all of k in tensor memory: their results are rounded to 16 bits, beside which what is cut off is
+    // little.  It is most for fp16 products of one sign, 5.6e-9 of the sum for each k: 2.6e-5 at 4608, where half a step of
+    // fp16 is 4.9e-4 at most and 2.4e-4 at least (bf16, both signs, 2600: 4e-6 of half a step's 2e-3).
     const int most = max_chunk(MODE == kWeightGrad8, dtype);
     const int per_split = std::max(1, (p.k_blocks + p.splits - 1) / p.splits), parts = kWeightGrads<MODE> ? (per_split + most - 1) / most : 1;
     p.chunk = (per_split + parts - 1) / parts;

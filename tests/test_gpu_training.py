@@ -735,3 +735,23 @@ def test_the_norms_checkpoint_is_that_of_its_stored_sum(tr, shape, dtype, pad):
     assert torch.equal(out.h8.scales, want.scales)
     fine = fine.repeat_interleave(32, dim=-1)[..., :shape[-1]]
     assert torch.equal(out.h8.values[fine], want.values[fine])
+
+
+@pytest.mark.parametrize("tokens", [512, 768, 769, 1024, 1025, 1500, 2048, 8192])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("from8", [False, True])
+@pytest.mark.parametrize("sizes", [False, True])
+def test_weight_gradients_are_within_a_millionth(tr, tokens, dtype, from8, sizes):
+    """Of the gradient's size, for both types, at and beside the lengths at which a sum is put together from parts, for tokens
+    alike and for tokens that differ in size; by enough workers for the parts not to be split over blocks, and by one."""
+    g = gen(tokens)
+    for b in (20, 1):
+        def make(cols, scale):
+            v = rand(g, b, tokens, cols, scale=scale)
+            return (v * torch.exp(0.5 * rand(g, b, tokens, 1)) * torch.exp(0.5 * rand(g, 1, 1, cols)) if sizes else v).to(dtype)
+
+        dz, x = make(512, 0.05), make(512, 1.0)
+        kept = tr.pg_checkpoint_write(x) if from8 else x
+        xv = stored8(kept) if from8 else x.double()
+        want = dz.double().transpose(1, 2) @ xv
+        assert float((tr.pg_linear_weight_grad(dz, kept).double() - want).norm() / want.norm()) <= 1e-6
