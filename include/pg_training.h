@@ -207,6 +207,15 @@ PG_API int pg_training_status(void *stream);
  */
 PG_API int pg_selftest_training_timeout(void *stream);
 
+/*
+ * Self-test of the bounds-checked build, whose training kernels look every address up in the operands of
+ * their call (accesses outside are skipped, and pg_training_status returns PG_ERR_BOUNDS; one call at
+ * a time on a device): a kernel asks the check about the word behind an operand, without touching it.
+ * Waits for `stream` and returns PG_ERR_BOUNDS from a library built with -DPG_BOUNDS_CHECK, PG_OK from
+ * the regular one.  Clears the word.
+ */
+PG_API int pg_selftest_training_bounds(void *stream);
+
 #ifdef __cplusplus
 }
 #endif

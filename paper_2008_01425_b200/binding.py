@@ -35,7 +35,7 @@ EXPORTS = (
     "pg_add_rms_norm", "pg_add_rms_norm_grad", "pg_add_rms_norm_grad_workspace_bytes",
     "pg_linear", "pg_linear_workspace_bytes", "pg_linear_input_grad", "pg_linear_input_grad_workspace_bytes",
     "pg_linear_weight_grad", "pg_linear_weight_grad_workspace_bytes", "pg_activation_grad",
-    "pg_checkpoint_write", "pg_checkpoint_read", "pg_training_status", "pg_selftest_training_timeout",
+    "pg_checkpoint_write", "pg_checkpoint_read", "pg_training_status", "pg_selftest_training_timeout", "pg_selftest_training_bounds",
 )
 PG_POWER_ITERATION, PG_RANDOM_RIGHT, PG_RANDOM_LEFT = 0, 1, 2
 KERNEL_KINDS = ("forward", "edge_left", "transposed", "edge_right", "update_forward",
@@ -115,6 +115,7 @@ def load_library() -> ctypes.CDLL:
         getattr(L, name + "_workspace_bytes").argtypes = [vp, szp]
     L.pg_training_status.argtypes = [vp]
     L.pg_selftest_training_timeout.argtypes = [vp]
+    L.pg_selftest_training_bounds.argtypes = [vp]
     L.pg_status_string.argtypes = [ctypes.c_int]
     L.pg_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:

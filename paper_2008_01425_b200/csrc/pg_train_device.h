@@ -15,6 +15,42 @@ constexpr int kBlock8 = 32;        // values that share a scale in the 8-bit for
 constexpr int kSMs = 148;          // streaming multiprocessors of a B200
 constexpr int64_t kMaxDim = 1 << 30;
 
+// ------------------------------------------------------------------ bounds-checked build
+// With -DPG_BOUNDS_CHECK every access that a kernel makes by an address of its own is looked up in the operands of its call
+// first: a read has to touch one (16- and 4-byte pieces may reach past its ends), a write has to lie in an output.  Another one is
+// skipped and reported by pg_training_status (PG_ERR_BOUNDS).  Copies by TMA are bounded by their tensor maps.  That build takes one
+// call at a time on a device.
+#ifdef PG_BOUNDS_CHECK
+constexpr bool kChecked = true;
+#else
+constexpr bool kChecked = false;
+#endif
+constexpr int kMaxSpans = 16;
+struct Span { uintptr_t lo, hi; };
+struct Spans {
+    Span at[kMaxSpans];
+    int count, outputs;        // the outputs come first
+};
+constexpr unsigned kTimedOut = 1, kOutside = 2;        // bits of the error words
+#ifdef PG_BOUNDS_CHECK
+static __device__ Spans g_spans;
+static __device__ unsigned g_outside;
+static __device__ __noinline__ bool may_access(const void* p, int bytes, bool write) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p), hi = lo + bytes;
+    for (int i = 0; i < (write ? g_spans.outputs : g_spans.count); ++i)
+        if (write ? lo >= g_spans.at[i].lo && hi <= g_spans.at[i].hi : lo < g_spans.at[i].hi && hi > g_spans.at[i].lo) return true;
+    atomicOr(&g_outside, kOutside);
+    return false;
+}
+#define PGT_READ(p, bytes) may_access(p, bytes, false)
+#define PGT_WRITE(p, bytes) may_access(p, bytes, true)
+#else
+#define PGT_READ(p, bytes) ((void)sizeof(p), true)       // names its operand, evaluates nothing
+#define PGT_WRITE(p, bytes) ((void)sizeof(p), true)
+#endif
+#define PGT_LOAD(ref) (PGT_READ(&(ref), sizeof(ref)) ? (ref) : decltype((ref) + 0)(0))
+#define PGT_STORE(ref, value) do { if (PGT_WRITE(&(ref), sizeof(ref))) (ref) = (value); } while (0)
+
 // ------------------------------------------------------------------ pairs of fp32
 // Two fp32 numbers in one 64-bit register pair: add, multiply and fused multiply-add take both at once.
 struct F2 { unsigned long long u; };
@@ -89,12 +125,12 @@ template <int W>
 __device__ __forceinline__ Piece<W> load_oct(const uint16_t* row, int col, int cols) {
     Piece<W> r = {};
     if constexpr (W == 8) {
-        if (col < cols) r.a = *reinterpret_cast<const uint4*>(row + col);
+        if (col < cols && PGT_READ(row + col, 16)) r.a = *reinterpret_cast<const uint4*>(row + col);
     } else {
         const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15) / 2;         // the same for all lanes of a row
         const uint4* p = reinterpret_cast<const uint4*>(row + col - off);
-        if (col < cols) r.a = p[0];
-        if (col + 8 - off < cols && off > 0) r.b = p[1];
+        if (col < cols && PGT_READ(p, 16)) r.a = p[0];
+        if (col + 8 - off < cols && off > 0 && PGT_READ(p + 1, 16)) r.b = p[1];
     }
     return r;
 }
@@ -139,11 +175,11 @@ __device__ __forceinline__ void store_oct(uint16_t* row, int col, int cols, cons
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = Elem<H>::down2(v[i]);
     if (W == 8 && col + 8 <= cols) {
-        *reinterpret_cast<uint4*>(row + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        PGT_STORE(*reinterpret_cast<uint4*>(row + col), make_uint4(w[0], w[1], w[2], w[3]));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu);
+            if (col + i < cols) PGT_STORE(row[col + i], static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu));
     }
 }
 
@@ -200,17 +236,17 @@ __device__ __forceinline__ Oct8 pack8(const F2 (&t)[4]) {      // the low bytes 
 }
 __device__ __forceinline__ void store_oct8(int8_t* row, int col, int cols, Oct8 o) {
     if (col + 8 <= cols) {
-        *reinterpret_cast<uint2*>(row + col) = make_uint2(o.w[0], o.w[1]);
+        PGT_STORE(*reinterpret_cast<uint2*>(row + col), make_uint2(o.w[0], o.w[1]));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = static_cast<int8_t>(o.w[i / 4] >> (8 * (i & 3)) & 255u);
+            if (col + i < cols) PGT_STORE(row[col + i], static_cast<int8_t>(o.w[i / 4] >> (8 * (i & 3)) & 255u));
     }
 }
 // An octet of an 8-bit row (rows start on 16-byte boundaries); what it holds past the row's end is not masked.
 __device__ __forceinline__ Oct8 load_oct8(const int8_t* row, int col, int cols) {
     Oct8 r = {};
-    if (col < cols) {
+    if (col < cols && PGT_READ(row + col, 8)) {
         const uint2 u = *reinterpret_cast<const uint2*>(row + col);
         r.w[0] = u.x;
         r.w[1] = u.y;
@@ -326,6 +362,49 @@ inline int access_width(std::initializer_list<const pg_matrix*> ms, int64_t batc
         }
     return bits % 16 == 0 ? 8 : 1;
 }
+// The operands of a call, for the bounds-checked build (elsewhere nothing is kept): all outputs first.
+class Operands {
+public:
+    Operands& output(const pg_matrix& m, int64_t batch, int64_t rows, int64_t cols, int size) {
+        if (kChecked && m.data && batch > 0 && rows > 0) add(m.data, ((batch - 1) * m.stride + (rows - 1) * m.ld + cols) * size);
+        if (kChecked) spans_.outputs = spans_.count;
+        return *this;
+    }
+    Operands& output(const pg_matrix8& m, int64_t batch, int64_t rows, int64_t cols) {
+        output(pg_matrix{m.values, m.ld, m.stride}, batch, rows, cols, 1);
+        return output(pg_matrix{m.values ? m.scales : nullptr, m.scale_ld, m.scale_stride}, batch, rows, (cols + kBlock8 - 1) / kBlock8, 1);
+    }
+    Operands& output(const void* p, int64_t stride, int64_t batch, int64_t n) { return output(pg_matrix{const_cast<void*>(p), n, stride}, batch, 1, n, 4); }
+    template <typename... A> Operands& input(const A&... a) {
+        const int outputs = spans_.outputs;
+        output(a...);
+        spans_.outputs = outputs;
+        return *this;
+    }
+    int publish(cudaStream_t st) const {
+#ifdef PG_BOUNDS_CHECK
+        if (cudaMemcpyToSymbolAsync(g_spans, &spans_, sizeof spans_, 0, cudaMemcpyHostToDevice, st) != cudaSuccess) return PG_ERR_CUDA;
+#else
+        static_cast<void>(st);
+#endif
+        return PG_OK;
+    }
+
+private:
+    void add(const void* p, int64_t bytes) {
+        if (spans_.count < kMaxSpans) spans_.at[spans_.count++] = Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes};
+    }
+    Spans spans_ = {};
+};
+// Waits for `st`, reads a word of device memory and clears it.
+inline int take_word(unsigned* word, unsigned& value, cudaStream_t st) {
+    const unsigned none = 0;
+    if (cudaMemcpyAsync(&value, word, sizeof value, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return PG_ERR_CUDA;
+    if (value != 0 && (cudaMemcpyAsync(word, &none, sizeof none, cudaMemcpyHostToDevice, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+        return PG_ERR_CUDA;
+    return PG_OK;
+}
+int take_row_errors(unsigned& value, cudaStream_t st);     // of the row kernels (pg_train_rows.cu)
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PG_OK : PG_ERR_CUDA; }
 
 }  // namespace pgt

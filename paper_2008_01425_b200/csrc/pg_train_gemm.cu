@@ -147,7 +147,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
         if (t - t0 > limit) {
             *gave_up = 1;
-            atomicOr(&g_training_error, 1u);
+            atomicOr(&g_training_error, kTimedOut);
             return false;
         }
     }
@@ -279,18 +279,18 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
         if (ep.accumulate || more) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (i < count) v[i] += o[i * ep.out.ld];
+                if (i < count) v[i] += PGT_LOAD(o[i * ep.out.ld]);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (i < count) o[i * ep.out.ld] = v[i];
+            if (i < count) PGT_STORE(o[i * ep.out.ld], v[i]);
     } else {
         uint16_t res[16];
         const bool residual = ep.residual.data != nullptr;
         if (residual && live) {
             const uint16_t* r = static_cast<const uint16_t*>(ep.residual.data) + b * ep.residual.stride + n * ep.residual.ld + m;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) res[i] = i < count ? r[i * ep.residual.ld] : 0;
+            for (int i = 0; i < 16; ++i) res[i] = i < count ? PGT_LOAD(r[i * ep.residual.ld]) : 0;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += bias;
@@ -301,8 +301,8 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
             for (int i = 0; i < 16; ++i) {
                 const uint32_t sb = scale_byte<H>(__reduce_max_sync(0xffffffffu, live ? __float_as_uint(v[i]) & 0x7fffffffu : 0u));
                 if (live && i < count) {
-                    q[i * ep.z8.ld] = static_cast<int8_t>(byte8(v[i], scale_inverse(sb)));
-                    if (m % kBlock8 == 0) s[i * ep.z8.scale_ld] = static_cast<uint8_t>(sb);
+                    PGT_STORE(q[i * ep.z8.ld], static_cast<int8_t>(byte8(v[i], scale_inverse(sb))));
+                    if (m % kBlock8 == 0) PGT_STORE(s[i * ep.z8.scale_ld], static_cast<uint8_t>(sb));
                 }
             }
         }
@@ -313,8 +313,8 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
             F2 y = activate<ACT>(pair(v[i], v[i + 1]));
             if (residual) y = add(y, pair(Elem<H>::up(res[i]), Elem<H>::up(res[i + 1])));
             const uint32_t w = Elem<H>::down2(y);
-            if (i < count) o[i * ep.out.ld] = static_cast<uint16_t>(w & 0xffffu);
-            if (i + 1 < count) o[(i + 1) * ep.out.ld] = static_cast<uint16_t>(w >> 16);
+            if (i < count) PGT_STORE(o[i * ep.out.ld], static_cast<uint16_t>(w & 0xffffu));
+            if (i + 1 < count) PGT_STORE(o[(i + 1) * ep.out.ld], static_cast<uint16_t>(w >> 16));
         }
     }
 }
@@ -363,7 +363,7 @@ struct Residuals {             // of a tile: where a lane's five pieces start, f
             const uint32_t k = lane + 32 * i, r = k / 5, c = k - r * 5;
             bool in = wanted >> i & 1;
             if (left < 40) in = in && static_cast<int>(8 * c) - static_cast<int>(low + r * static_cast<uint32_t>(ep.residual.ld) * 2 & 15) / 2 < left;
-            if (in) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(held) + k * 16), "l"(from + at[i]) : "memory");
+            if (in && PGT_READ(from + at[i], 16)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(held) + k * 16), "l"(from + at[i]) : "memory");
         }
     }
 };
@@ -417,7 +417,7 @@ __device__ __forceinline__ void empty_rows(const Problem& p, const CUtensorMap* 
                 for (int k = 0; k < 4; ++k) t[k] = to8(v[i][k], inverse);
                 q[i] = pack8(t);
             }
-            if (live) ep.z8.scales[b * ep.z8.scale_stride + row * ep.z8.scale_ld + n / kBlock8] = static_cast<uint8_t>(s);
+            if (live) PGT_STORE(ep.z8.scales[b * ep.z8.scale_stride + row * ep.z8.scale_ld + n / kBlock8], static_cast<uint8_t>(s));
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last group's copies have been read
             __syncwarp();
             uint4* to = reinterpret_cast<uint4*>(out + kOutWarp + lane * 32);
@@ -473,11 +473,11 @@ __device__ __forceinline__ void emit_full(const Epilogue& ep, float (&v)[16], co
             split(y[i], lo, hi);
             const uint32_t s0 = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(lo) & 0x7fffffffu));
             const uint32_t s1 = scale_byte<H>(__reduce_max_sync(0xffffffffu, __float_as_uint(hi) & 0x7fffffffu));
-            (q + 2 * i * ep.z8.ld)[lane_q] = static_cast<int8_t>(byte8(lo, scale_inverse(s0)));
-            (q + (2 * i + 1) * ep.z8.ld)[lane_q] = static_cast<int8_t>(byte8(hi, scale_inverse(s1)));
+            PGT_STORE((q + 2 * i * ep.z8.ld)[lane_q], static_cast<int8_t>(byte8(lo, scale_inverse(s0))));
+            PGT_STORE((q + (2 * i + 1) * ep.z8.ld)[lane_q], static_cast<int8_t>(byte8(hi, scale_inverse(s1))));
             if (first) {
-                s[2 * i * ep.z8.scale_ld] = static_cast<uint8_t>(s0);
-                s[(2 * i + 1) * ep.z8.scale_ld] = static_cast<uint8_t>(s1);
+                PGT_STORE(s[2 * i * ep.z8.scale_ld], static_cast<uint8_t>(s0));
+                PGT_STORE(s[(2 * i + 1) * ep.z8.scale_ld], static_cast<uint8_t>(s1));
             }
         }
     }
@@ -487,8 +487,8 @@ __device__ __forceinline__ void emit_full(const Epilogue& ep, float (&v)[16], co
         y[i] = activate<ACT>(y[i]);
         if (residual) y[i] = add(y[i], pair(Elem<H>::up(res[2 * i]), Elem<H>::up(res[2 * i + 1])));
         const uint32_t w = Elem<H>::down2(y[i]);
-        *reinterpret_cast<uint16_t*>(out + 2 * i * ep.out.ld * 2 + lane_out) = static_cast<uint16_t>(w & 0xffffu);
-        *reinterpret_cast<uint16_t*>(out + (2 * i + 1) * ep.out.ld * 2 + lane_out) = static_cast<uint16_t>(w >> 16);
+        PGT_STORE(*reinterpret_cast<uint16_t*>(out + 2 * i * ep.out.ld * 2 + lane_out), static_cast<uint16_t>(w & 0xffffu));
+        PGT_STORE(*reinterpret_cast<uint16_t*>(out + (2 * i + 1) * ep.out.ld * 2 + lane_out), static_cast<uint16_t>(w >> 16));
     }
 }
 
@@ -501,7 +501,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
     const bool live = m < p.M;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const int end = part ? p.BN : min(p.BN, p.N - n0);
-    const float bias = !FP32 && ep.bias && live ? ep.bias[b * ep.bias_stride + m] : 0.0f;
+    const float bias = !FP32 && ep.bias && live ? PGT_LOAD(ep.bias[b * ep.bias_stride + m]) : 0.0f;
     float v[16];
     if (part || p.K == 0) {
         for (int j = half * 16; j < end; j += 32) {
@@ -531,7 +531,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
                 float old[16];
                 if (add) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) old[i] = o[i * ep.out.ld];
+                    for (int i = 0; i < 16; ++i) old[i] = PGT_LOAD(o[i * ep.out.ld]);
                 }
                 tmem_load16(lanes + j, v);
                 if (add) {
@@ -539,7 +539,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
                     for (int i = 0; i < 16; ++i) v[i] += old[i];
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[i * ep.out.ld] = v[i];
+                for (int i = 0; i < 16; ++i) PGT_STORE(o[i * ep.out.ld], v[i]);
             }
         } else {
             const int64_t n = n0 + j;
@@ -555,7 +555,7 @@ __device__ __forceinline__ void empty_tile(const Problem& p, uint32_t tmem, floa
             auto fetch = [&](int at) {
                 if (add && at + 16 <= end) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) next[i] = *reinterpret_cast<const uint16_t*>(in + i * ep.residual.ld * 2 + lane_m * 2);
+                    for (int i = 0; i < 16; ++i) next[i] = PGT_LOAD(*reinterpret_cast<const uint16_t*>(in + i * ep.residual.ld * 2 + lane_m * 2));
                 }
                 in += 64 * ep.residual.ld;
             };
@@ -585,7 +585,7 @@ __device__ __forceinline__ void join_parts(const Problem& p, float* part, int64_
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     const int m = m0 + quarter * 32 + lane;
     const bool live = m < p.M;
-    const float bias = !FP32 && p.ep.bias && live ? p.ep.bias[b * p.ep.bias_stride + m] : 0.0f;
+    const float bias = !FP32 && p.ep.bias && live ? PGT_LOAD(p.ep.bias[b * p.ep.bias_stride + m]) : 0.0f;
     const int per = p.BN / p.splits, each = per / 2;       // BN is a multiple of 16 and splits at most 8
     const int j0 = rank * per + half * each;
     for (int j = j0; j < j0 + each && n0 + j < p.N; j += 16) {
@@ -854,7 +854,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
                     for (int g = 0; g < (8 + kShares - 1) / kShares; ++g) {
                         const int n = n0 + j + g * kShares * 32 + lane;
-                        bias[g] = p.ep.bias && n < p.N ? p.ep.bias[b * p.ep.bias_stride + n] : 0.0f;
+                        bias[g] = p.ep.bias && n < p.N ? PGT_LOAD(p.ep.bias[b * p.ep.bias_stride + n]) : 0.0f;
                     }
                     __syncwarp();
 #pragma unroll
@@ -932,8 +932,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const uint32_t* word = reinterpret_cast<const uint32_t*>(from & ~uintptr_t{3});
                     const int words = k < k1 ? words_of_scales(from, count) : 0;
                     lo[u] = hi[u] = 0;
-                    if (words > 0) lo[u] = word[0];
-                    if (words > 1) hi[u] = word[1];
+                    if (words > 0) lo[u] = PGT_LOAD(word[0]);
+                    if (words > 1) hi[u] = PGT_LOAD(word[1]);
                 }
 #pragma unroll
                 for (int u = 0; u < kRows; ++u) {
@@ -1044,10 +1044,10 @@ constexpr int kFewTokens = 4, kFewBytes = 40 * 1024;
 template <typename H, int W> struct Few {
     static constexpr int kPairs = W == 1 ? 1 : W / 2, kUnroll = W == 8 ? 2 : 6;
     uint32_t w[kPairs];
-    __device__ __forceinline__ void load(const uint16_t* row, int e, int valid) {
+    template <bool SHARED> __device__ __forceinline__ void load(const uint16_t* row, int e, int valid) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) w[i] = 0;
-        if (valid <= 0) return;
+        if (valid <= 0 || !(SHARED || PGT_READ(row + e, 2 * W))) return;
         if constexpr (W == 8) {
             const uint4 u = *reinterpret_cast<const uint4*>(row + e);
             w[0] = u.x;
@@ -1101,7 +1101,7 @@ few_tokens_kernel(const pg_linear_args a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int e = k + (u * 32 + lane) * W;
-                w[u][r].load(row[r], e, K - e);
+                w[u][r].template load<false>(row[r], e, K - e);
             }
         if (first) __syncthreads();                    // the tokens; the first weights are on their way meanwhile
         first = false;
@@ -1114,7 +1114,7 @@ few_tokens_kernel(const pg_linear_args a) {
 #pragma unroll
             for (int t = 0; t < T; ++t) {
                 F x;
-                x.load(x16 + t * octets * 8, e, W);
+                x.template load<true>(x16 + t * octets * 8, e, W);
 #pragma unroll
                 for (int i = 0; i < F::kPairs; ++i)
 #pragma unroll
@@ -1137,7 +1137,7 @@ few_tokens_kernel(const pg_linear_args a) {
         const int m = blockIdx.x * 32 + lane;
         const bool live = m < a.out_features;
         float v[16] = {s_z[warp][lane]};
-        emit<H, ACT, false>(ep, v, b, warp, 1, m, live, a.bias && live ? a.bias[b * a.bias_stride + m] : 0.0f);
+        emit<H, ACT, false>(ep, v, b, warp, 1, m, live, a.bias && live ? PGT_LOAD(a.bias[b * a.bias_stride + m]) : 0.0f);
     }
 }
 template <typename H, int W, int T>
@@ -1178,7 +1178,7 @@ align_rows_kernel(const uint16_t* __restrict__ src, int64_t src_ld, int64_t src_
     const int64_t b = row / rows, r = row - b * rows;
     const uint16_t* p = src + b * src_stride + r * src_ld;
     const Oct o = octet<1>(load_oct<1>(p, col, cols), p, col, cols);
-    *reinterpret_cast<uint4*>(dst + row * dst_ld + col) = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
+    PGT_STORE(*reinterpret_cast<uint4*>(dst + row * dst_ld + col), make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]));
 }
 
 // The products' wait on a barrier that nothing arrives on, by a whole block and with a limit of a millisecond.
@@ -1191,6 +1191,12 @@ __global__ void __launch_bounds__(64) wait_probe_kernel() {
     }
     __syncthreads();
     bar_wait(&bar, 0, &gave_up, 1000000);
+}
+
+// Asks the bounds check about a word that is an operand, then about the one behind it; touches neither.
+__global__ void bounds_probe_kernel(const char* word) {
+    if (!PGT_READ(word, 4) || !PGT_WRITE(word, 4)) atomicOr(&g_training_error, kTimedOut);     // must not happen
+    if (PGT_READ(word + 4, 4) && kChecked) atomicOr(&g_training_error, kTimedOut);
 }
 
 // ------------------------------------------------------------------ host
@@ -1405,6 +1411,11 @@ int pg_linear(const pg_linear_args* args, void* workspace, size_t workspace_byte
     if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.y, a.batch, a.tokens, a.out_features, 2).output(a.z8, a.batch, a.tokens, a.out_features).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
+    operands.input(a.x, a.batch, a.tokens, a.in_features, 2).input(a.weight, a.batch, a.out_features, a.in_features, 2);
+    operands.input(a.bias, a.bias_stride, a.batch, a.out_features).input(a.residual, a.batch, a.tokens, a.out_features, 2);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     if (few(a)) return a.dtype == PG_BF16 ? few_tokens<__nv_bfloat16>(a, st) : few_tokens<__half>(a, st);
     uint8_t* at = static_cast<uint8_t*>(workspace);
     pg_matrix x = a.x, w = a.weight;
@@ -1437,6 +1448,11 @@ int pg_linear_input_grad(const pg_input_grad_args* args, void* workspace, size_t
     if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.dx, a.batch, a.tokens, a.in_features, 2).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
+    operands.input(a.dz, a.batch, a.tokens, a.out_features, 2).input(a.weight, a.batch, a.out_features, a.in_features, 2);
+    operands.input(a.residual, a.batch, a.tokens, a.in_features, 2);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     uint8_t* at = static_cast<uint8_t*>(workspace);
     pg_matrix dz = a.dz, w = a.weight;
     int rc = aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st);
@@ -1472,6 +1488,10 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
     if (!workspace_ok(need, workspace, workspace_bytes, dev)) return PG_ERR_WORKSPACE;
     if (a.batch == 0) return PG_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.dweight, a.batch, a.out_features, a.in_features, 4).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
+    operands.input(a.dz, a.batch, a.tokens, a.out_features, 2).input(a.x, a.batch, a.tokens, a.in_features, 2).input(a.x8, a.batch, a.tokens, a.in_features);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     uint8_t* at = static_cast<uint8_t*>(workspace);
     const Epilogue ep{a.accumulate, PG_ACT_NONE, a.dweight, {}, nullptr, 0, {}};
     pg_matrix dz = a.dz, x = a.x;
@@ -1493,18 +1513,27 @@ int pg_selftest_training_timeout(void* stream) {
     wait_probe_kernel<<<1, 64, 0, static_cast<cudaStream_t>(stream)>>>();
     return launch_status() == PG_OK ? pg_training_status(stream) : PG_ERR_CUDA;
 }
+int pg_selftest_training_bounds(void* stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_training_error) != cudaSuccess) return PG_ERR_CUDA;
+    Operands operands;
+    operands.output(p, 0, 1, 1);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    bounds_probe_kernel<<<1, 1, 0, st>>>(static_cast<const char*>(p));
+    return launch_status() == PG_OK ? pg_training_status(stream) : PG_ERR_CUDA;
+}
 int pg_training_status(void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    unsigned word = 0;
-    const unsigned none = 0;
-    if (cudaMemcpyFromSymbolAsync(&word, g_training_error, sizeof word, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-        cudaStreamSynchronize(st) != cudaSuccess)
+    unsigned word = 0, rows = 0, outside = 0;
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_training_error) != cudaSuccess || take_word(static_cast<unsigned*>(p), word, st) != PG_OK ||
+        take_row_errors(rows, st) != PG_OK)
         return PG_ERR_CUDA;
-    if (word == 0) return PG_OK;
-    if (cudaMemcpyToSymbolAsync(g_training_error, &none, sizeof none, 0, cudaMemcpyHostToDevice, st) != cudaSuccess ||
-        cudaStreamSynchronize(st) != cudaSuccess)
-        return PG_ERR_CUDA;
-    return PG_ERR_TIMEOUT;
+#ifdef PG_BOUNDS_CHECK
+    if (cudaGetSymbolAddress(&p, g_outside) != cudaSuccess || take_word(static_cast<unsigned*>(p), outside, st) != PG_OK) return PG_ERR_CUDA;
+#endif
+    return word & kTimedOut ? PG_ERR_TIMEOUT : (rows | outside) & kOutside ? PG_ERR_BOUNDS : PG_OK;
 }
 
 }  // extern "C"

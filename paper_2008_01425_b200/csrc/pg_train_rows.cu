@@ -15,12 +15,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// A worker's gains for an octet; `wide`: 16-byte addresses.
+// A worker's gains for an octet (of global memory, or where a block has copied them to); `wide`: 16-byte addresses.
+template <bool SHARED = false>
 __device__ __forceinline__ void load_gain(const float* gain, bool wide, int col, int cols, F2 (&g)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) g[i] = both(1.0f);
     if (!gain) return;
-    if (wide && col + 8 <= cols) {
+    if (wide && col + 8 <= cols && (SHARED || (PGT_READ(gain + col, 16) && PGT_READ(gain + col + 4, 16)))) {
         const float4 lo = *reinterpret_cast<const float4*>(gain + col), hi = *reinterpret_cast<const float4*>(gain + col + 4);
         g[0] = pair(lo.x, lo.y);
         g[1] = pair(lo.z, lo.w);
@@ -29,7 +30,7 @@ __device__ __forceinline__ void load_gain(const float* gain, bool wide, int col,
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            g[i] = pair(col + 2 * i < cols ? gain[col + 2 * i] : 0.0f, col + 2 * i + 1 < cols ? gain[col + 2 * i + 1] : 0.0f);
+            g[i] = pair(col + 2 * i < cols ? PGT_LOAD(gain[col + 2 * i]) : 0.0f, col + 2 * i + 1 < cols ? PGT_LOAD(gain[col + 2 * i + 1]) : 0.0f);
     }
 }
 __device__ __forceinline__ bool wide_gain(const float* gain) { return reinterpret_cast<uintptr_t>(gain) % 16 == 0; }
@@ -47,7 +48,7 @@ __device__ __forceinline__ void octet_to_8(F2 (&v)[4], int8_t* row, uint8_t* sca
     }
     if (col < cols) {
         store_oct8(row, col, cols, pack8(t));
-        if (col % kBlock8 == 0) scales[col / kBlock8] = static_cast<uint8_t>(s);
+        if (col % kBlock8 == 0) PGT_STORE(scales[col / kBlock8], static_cast<uint8_t>(s));
     }
 }
 
@@ -67,7 +68,7 @@ norm_kernel(const pg_norm_args a) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = c * 256 + threadIdx.x;
-            s_gain[col] = gain && col < a.cols ? gain[col] : 1.0f;
+            s_gain[col] = gain && col < a.cols ? PGT_LOAD(gain[col]) : 1.0f;
         }
         __syncthreads();
     }
@@ -127,7 +128,7 @@ norm_kernel(const pg_norm_args a) {
         sum = sum_of_row(sums);
     }
     const float rstd = rsqrtf(sum / a.cols + eps);     // of the scaled row
-    if (a.rstd && t == 0) a.rstd[b * a.tokens + tok] = rstd * scale;
+    if (a.rstd && t == 0) PGT_STORE(a.rstd[b * a.tokens + tok], rstd * scale);
     if (a.h.data) {
         uint16_t* h = static_cast<uint16_t*>(a.h.data) + b * a.h.stride + tok * a.h.ld;
 #pragma unroll
@@ -160,7 +161,7 @@ norm_kernel(const pg_norm_args a) {
     for (int c = 0; c < C; ++c) {
         const int col = (c * T + t) * 8;
         F2 g[4];
-        if constexpr (T == 32) load_gain(s_gain, true, col, C * 256, g);
+        if constexpr (T == 32) load_gain<true>(s_gain, true, col, C * 256, g);
         else load_gain(gain, wide, col, a.cols, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[c][i] = mul(v[c][i], mul(both(rstd), g[i]));
@@ -215,13 +216,13 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
                 for (int c = 0; c < C; ++c) {
                     const int col = (c * T + t) * 8;
                     q_raw[k][c] = load_oct8(q, col, a.cols);
-                    q_scale[k][c] = col < a.cols ? s[col / kBlock8] : 0;
+                    q_scale[k][c] = col < a.cols ? PGT_LOAD(s[col / kBlock8]) : 0;
                 }
             } else {
                 load_row<W, C, T>(row_of(a.h, k), a.cols, t, h_piece[k]);
             }
             if (a.dh.data) load_row<W, C, T>(row_of(a.dh, k), a.cols, t, dh_piece[k]);
-            rstd[k] = a.rstd[b * a.tokens + row];
+            rstd[k] = PGT_LOAD(a.rstd[b * a.tokens + row]);
         }
 #pragma unroll
         for (int k = 0; k < R; ++k)
@@ -306,8 +307,8 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
             const int col = (c * T + t) * 8 + 2 * i;
             float lo, hi;
             split(sum_dg[c][i], lo, hi);
-            if (col < a.cols) mine[col] = lo;
-            if (col + 1 < a.cols) mine[col + 1] = hi;
+            if (col < a.cols && (T == 32 || PGT_WRITE(mine + col, 4))) mine[col] = lo;
+            if (col + 1 < a.cols && (T == 32 || PGT_WRITE(mine + col + 1, 4))) mine[col + 1] = hi;
         }
     if constexpr (T == 32) {
         __syncthreads();
@@ -315,7 +316,7 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < kGroups; ++w) v += s_sum[w * a.cols + col];
-            out[col] = v;
+            PGT_STORE(out[col], v);
         }
     }
 }
@@ -328,15 +329,15 @@ sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, floa
     float sum = 0.0f;
     if (col < cols)
 #pragma unroll 4
-        for (int k = w; k < parts; k += 8) sum += partial[(b * parts + k) * cols + col];
+        for (int k = w; k < parts; k += 8) sum += PGT_LOAD(partial[(b * parts + k) * cols + col]);
     s_sum[w][threadIdx.x & 31] = sum;
     __syncthreads();
     if (w == 0 && col < cols) {
         float* o = out + b * out_stride + col;
-        sum = accumulate ? *o : 0.0f;
+        sum = accumulate ? PGT_LOAD(*o) : 0.0f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum += s_sum[k][threadIdx.x];
-        *o = sum;
+        PGT_STORE(*o, sum);
     }
 }
 
@@ -376,7 +377,7 @@ activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
                     d[k] = load_oct<W>(dy_at + 8 * k * a.dy.ld, col, a.cols);
                     if (eight) {
                         q[k] = load_oct8(q_at + 8 * k * a.z8.ld, col, a.cols);
-                        s[k] = s_at[8 * k * a.z8.scale_ld];
+                        s[k] = PGT_LOAD(s_at[8 * k * a.z8.scale_ld]);
                     }
                 }
 #pragma unroll
@@ -419,7 +420,7 @@ activation_grad_kernel(const pg_activation_grad_args a, int rows_per_block) {
     const int out_col = blockIdx.x * kStrip + at;
     if (split_at == 0 && out_col < a.cols) {
         float* o = a.dbias + b * a.dbias_stride + out_col;
-        *o = a.accumulate ? *o + mine : mine;
+        PGT_STORE(*o, a.accumulate ? PGT_LOAD(*o) + mine : mine);
     }
 }
 
@@ -455,7 +456,7 @@ checkpoint_kernel(const pg_checkpoint_args a, int log_g) {
 #pragma unroll
         for (int k = 0; k < kRowsPerThread; ++k) {
             p[k] = load_oct8(q + row(k) * a.x8.ld, col, cols(k));
-            scale[k] = col < cols(k) ? s[row(k) * a.x8.scale_ld + col / kBlock8] : 0u;
+            scale[k] = col < cols(k) ? PGT_LOAD(s[row(k) * a.x8.scale_ld + col / kBlock8]) : 0u;
         }
 #pragma unroll
         for (int k = 0; k < kRowsPerThread; ++k) {
@@ -553,6 +554,19 @@ int strip_splits(int64_t strips, int64_t tokens) {
 }
 
 }  // namespace
+
+int take_row_errors(unsigned& value, cudaStream_t st) {
+    value = 0;
+#ifdef PG_BOUNDS_CHECK
+    void* word = nullptr;
+    if (cudaGetSymbolAddress(&word, g_outside) != cudaSuccess) return PG_ERR_CUDA;
+    return take_word(static_cast<unsigned*>(word), value, st);
+#else
+    static_cast<void>(st);
+    return PG_OK;
+#endif
+}
+
 }  // namespace pgt
 
 using namespace pgt;
@@ -574,6 +588,11 @@ int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
     if (a.rstd && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
     if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
     if (a.batch == 0 || a.tokens == 0) return PG_OK;
+    Operands operands;
+    operands.output(a.h, a.batch, a.tokens, a.cols, 2).output(a.y, a.batch, a.tokens, a.cols, 2).output(a.y8, a.batch, a.tokens, a.cols);
+    operands.output(a.h8, a.batch, a.tokens, a.cols).output(a.rstd, a.tokens, a.batch, a.tokens);
+    operands.input(a.x, a.batch, a.tokens, a.cols, 2).input(a.residual, a.batch, a.tokens, a.cols, 2).input(a.gain, a.gain_stride, a.batch, a.cols);
+    if (operands.publish(static_cast<cudaStream_t>(stream)) != PG_OK) return PG_ERR_CUDA;
     with_type(a.dtype, access_width({&a.x, &a.residual}, a.batch), access_width({&a.h, &a.y}, a.batch), [&](auto h, auto in, auto out) {
         using H = decltype(h);
         constexpr int W = decltype(in)::value, WO = decltype(out)::value;
@@ -618,6 +637,11 @@ int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t 
     const int blocks = norm_grad_blocks(a);
     float* partial = static_cast<float*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.dx, a.batch, a.tokens, a.cols, 2).output(a.dgain, a.dgain_stride, a.batch, a.cols).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
+    operands.input(a.dy, a.batch, a.tokens, a.cols, 2).input(a.dh, a.batch, a.tokens, a.cols, 2).input(a.h, a.batch, a.tokens, a.cols, 2);
+    operands.input(a.h8, a.batch, a.tokens, a.cols).input(a.rstd, a.tokens, a.batch, a.tokens).input(a.gain, a.gain_stride, a.batch, a.cols);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     if (a.tokens > 0 || a.dgain) {
         with_type(a.dtype, access_width({&a.dy, &a.h, &a.dh}, a.batch), access_width({&a.dx}, a.batch), [&](auto h, auto in, auto out) {
             using H = decltype(h);
@@ -654,6 +678,10 @@ int pg_activation_grad(const pg_activation_grad_args* args, void* stream) {
     const int strips = (a.cols + kStrip - 1) / kStrip;
     const int splits = strip_splits(int64_t{strips} * a.batch, a.tokens);
     const int per = (a.tokens + splits - 1) / splits;
+    Operands operands;
+    operands.output(a.dz, a.batch, a.tokens, a.cols, 2).output(a.dbias, a.dbias_stride, a.batch, a.cols);
+    operands.input(a.dy, a.batch, a.tokens, a.cols, 2).input(a.z8, a.batch, a.tokens, a.cols);
+    if (operands.publish(static_cast<cudaStream_t>(stream)) != PG_OK) return PG_ERR_CUDA;
     int rc = PG_OK;
     with_type(a.dtype, access_width({&a.dy}, a.batch), access_width({&a.dz}, a.batch), [&](auto h, auto in, auto out) {
         using H = decltype(h);
@@ -698,6 +726,10 @@ static int checkpoint(const pg_checkpoint_args* args, bool write, void* stream) 
     const int64_t per_block = kRowsPerThread * (256 >> log_g);
     const dim3 grid(static_cast<unsigned>((a.tokens + per_block - 1) / per_block), static_cast<unsigned>((octets + (1 << log_g) - 1) >> log_g), a.batch);
     if (grid.y > 65535) return PG_ERR_TOO_LARGE;
+    Operands operands;
+    if (write) operands.output(a.x8, a.batch, a.tokens, a.cols).input(a.x, a.batch, a.tokens, a.cols, 2);
+    else operands.output(a.x, a.batch, a.tokens, a.cols, 2).input(a.x8, a.batch, a.tokens, a.cols);
+    if (operands.publish(static_cast<cudaStream_t>(stream)) != PG_OK) return PG_ERR_CUDA;
     with_type(a.dtype, write ? width : 8, write ? 8 : width, [&](auto h, auto in, auto out) {
         using H = decltype(h);
         constexpr int W = decltype(in)::value, WO = decltype(out)::value;

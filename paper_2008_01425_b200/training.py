@@ -398,3 +398,8 @@ def pg_training_status(stream=None, device="cuda") -> int:
 def pg_selftest_training_timeout(stream=None, device="cuda") -> int:
     """Lets a bounded wait run out, within a millisecond; PG_ERR_TIMEOUT if that is reported."""
     return _ask(load_library().pg_selftest_training_timeout, stream, device)
+
+
+def pg_selftest_training_bounds(stream=None, device="cuda") -> int:
+    """PG_ERR_BOUNDS from the bounds-checked build, whose check it asks about an address outside; PG_OK elsewhere."""
+    return _ask(load_library().pg_selftest_training_bounds, stream, device)
