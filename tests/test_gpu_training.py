@@ -755,3 +755,64 @@ def test_weight_gradients_are_within_a_millionth(tr, tokens, dtype, from8, sizes
         xv = stored8(kept) if from8 else x.double()
         want = dz.double().transpose(1, 2) @ xv
         assert float((tr.pg_linear_weight_grad(dz, kept).double() - want).norm() / want.norm()) <= 1e-6
+
+
+def scale_bytes(top, dtype):
+    """floor(log2(top)) - 6 with its bias, from the exponent itself: log2 of a power of two may come out under it."""
+    e = torch.where(top > 0, torch.frexp(top)[1] - 7, torch.full_like(top, -1000).int())
+    return e.clamp(min=LEAST[dtype]) + 127
+
+
+def check8_half(c, want, slack, dtype):
+    """An 8-bit result is the rounded one: within half a step of its block, of a whole one only where 127 is the limit, and the
+    step is the one that a largest value within its slack has."""
+    cols = want.shape[-1]
+    step = torch.exp2(c.scales.double() - 127).repeat_interleave(32, dim=-1)[..., :cols]
+    top, err = blocks_of(want).abs().amax(-1), blocks_of(slack).amax(-1)
+    assert bool((c.scales >= scale_bytes(top - err, dtype)).all()) and bool((c.scales <= scale_bytes(top + err, dtype)).all())
+    limit = slack + step * torch.where(c.values.abs() == 127, 1.0, 0.5)
+    over = (stored8(c) - want).abs() - limit
+    assert float(over.max()) <= 0.0, "off by %.3e more than allowed" % float(over.max())
+
+
+@pytest.mark.parametrize("shape", [(3, 17, 33), (2, 33, 650), (2, 9, 1024), (1, 3, 4608)])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1)])
+def test_the_norms_8_bit_result_is_rounded_to_nearest(tr, shape, dtype, pad):
+    g = gen(hash(shape) % 1000 + 8)
+    b, t, n = shape
+    x, gain = strided(rand(g, b, t, n, scale=2.0).to(dtype), pad), 1 + 0.3 * rand(g, b, n)
+    out = tr.pg_add_rms_norm(x, gain, eight_bit=True)
+    s = x.double()
+    y = s * ((s * s).mean(-1, keepdim=True) + 1e-5) ** -0.5 * gain.double()[:, None]
+    check8_half(out.y8, y, y.abs() * (n + 40) * 2 * U, dtype)
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 650, 260), (2, 33, 147, 65), (1, 64, 64, 128), (1, 257, 200, 129), (20, 200, 520, 700), (19, 385, 257, 513)])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1)])
+def test_the_layers_8_bit_result_is_rounded_to_nearest(tr, shape, dtype, pad):
+    """One token, features as lanes, tokens as lanes; the slack is the exact sum's, so small integers have none."""
+    g = gen(hash(shape) % 1000 + 9)
+    b, t, k, n = shape
+    x = strided(torch.randint(-4, 5, (b, t, k), device="cuda", generator=g).to(dtype), pad)
+    w = strided((torch.randint(-4, 5, (b, n, k), device="cuda", generator=g) / 8).to(dtype), pad)
+    bias = torch.randint(-40, 41, (b, n), device="cuda", generator=g) / 8.0
+    _, z8 = tr.pg_linear(x, w, bias, save_z=True)
+    z = x.double() @ w.double().transpose(1, 2) + bias.double()[:, None]       # multiples of 1/8 below 2^14: exact in fp32
+    check8_half(z8, z, torch.zeros_like(z), dtype)
+    byte = scale_bytes(blocks_of(z).abs().amax(-1), dtype)
+    q = torch.round(blocks_of(z) * torch.exp2(127.0 - byte.double())[..., None]).clamp(-127, 127).flatten(-2)[..., :n]
+    assert torch.equal(z8.scales.int(), byte) and torch.equal(z8.values.double(), q)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 4, 5])
+@pytest.mark.parametrize("k", [7, 63, 650, 5120, 5128, 10240, 20480, 20488])
+@pytest.mark.parametrize("dtype,pad", [(BF, 0), (HF, 1), (BF, 2)])
+def test_the_last_products_of_long_rows_count(tr, tokens, k, dtype, pad):
+    """Only the last values of k are not zero, and small integers: any that is left out changes the sum, which is exact."""
+    g = gen(tokens + k)
+    for tail in (1, 3, 8, 16):
+        x, w = torch.zeros(2, tokens, k, device="cuda"), torch.zeros(2, 45, k, device="cuda")
+        x[..., -tail:] = torch.randint(1, 4, x[..., -tail:].shape, device="cuda", generator=g).float()
+        w[..., -tail:] = torch.randint(1, 4, w[..., -tail:].shape, device="cuda", generator=g).float()
+        y = tr.pg_linear(strided(x.to(dtype), pad), strided(w.to(dtype), pad))
+        assert torch.equal(y.double(), x.double() @ w.double().transpose(1, 2))           # at most 144: exact in 16 bits
