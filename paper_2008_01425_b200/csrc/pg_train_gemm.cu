@@ -33,8 +33,8 @@ constexpr int kBM = 128;              // lanes of an accumulator
 constexpr int kBK = 64;               // elements of k in a stage: one 128-byte swizzled row
 constexpr int kMaxStages = 12;
 constexpr int kSmemBytes = 232448;    // what a block may have,
-constexpr int kStaticBytes = 2304;    // and what of it Shared takes
-constexpr int kRingBytes = kSmemBytes - kStaticBytes - 1024;     // the rest, less what aligning it to 1024 bytes may cost
+constexpr int kStaticBytes = 2304;    // what of it is left to Shared and the compiler (Shared takes less than 600 bytes),
+constexpr int kRingBytes = kSmemBytes - kStaticBytes - 1024;     // and the rest, less what aligning it to 1024 bytes may cost
 constexpr int kABytes = kBM * kBK * 2;
 constexpr int kRawBytes = kBM * kBK;          // a stage of an 8-bit A before it is widened
 constexpr int kScaleStages = 8;               // stages whose scales are fetched at once, 4 bytes for each of their k
@@ -53,7 +53,8 @@ static_assert((kRingBytes - kMinRaw * kRawBytes - kScaleBytes) / (kABytes + 128 
 //   bf16         8: 0.55e-6   12: 0.83e-6   16: 1.12e-6           fp16         8: 0.65e-6   12: 0.95e-6   16: 1.25e-6
 //   bf16, x8    12: 0.26e-6   16: 0.38e-6   32: 0.87e-6           fp16, x8    12: 0.74e-6   16: 1.0e-6    32: 2.1e-6
 // and time over 2048 tokens for 64 workers of 1024 x 1024: 519, 317, 277, 241 and 215 us for 4, 8, 12, 16 and 32 (x8: 590, 363, 336,
-// 319 and 309 us).  Chosen: the longest parts that stay under 1e-6, and half of that for bf16 from 8 bits, where it costs 3 %.
+// 319 and 309 us; 20 workers x 1500 tokens of 656 x 1000 from 8 bits, one part 78 us, two 102).  Chosen: the longest parts that stay
+// under 1e-6, and for bf16 from 8 bits half of that, about twice an fp32 product's error instead of five times.
 // Sums of products that all have one sign lose more: 1.5e-6 (bf16), 4.4e-6 (fp16), 0.75e-6 and 1.2e-6 (x8).
 constexpr int max_chunk(bool eight, int dtype) { return eight && dtype == PG_BF16 ? 1024 / kBK : 768 / kBK; }
 constexpr int kMaxSplits = 8;         // blocks of a cluster that share the k of one tile
@@ -64,10 +65,7 @@ template <Mode M> constexpr bool kWeightGrads = M == kWeightGrad || M == kWeight
 template <Mode M> constexpr bool kTokenRows = M == kForwardRows || M == kInputGradRows;
 template <Mode M> constexpr bool kAMnMajor = M == kInputGrad || kWeightGrads<M>;
 template <Mode M> constexpr bool kBMnMajor = M == kInputGradRows || kWeightGrads<M>;
-#ifndef ROWWARPS
-#define ROWWARPS 12
-#endif
-constexpr int kRowWarps = ROWWARPS;   // epilogue warps where lanes are tokens
+constexpr int kRowWarps = 12;         // epilogue warps where lanes are tokens
 constexpr int kShares = kRowWarps / 4;
 constexpr int kOutBytes = 2048;       // 32 rows x 32 elements of one of them on their way out,
 constexpr int kHeldBytes = 32 * 80;   // and five 16-byte pieces of residuals for each of the rows
@@ -89,7 +87,7 @@ struct Epilogue {
 };
 struct Problem {
     Epilogue ep;
-    int M, N, K, batch;
+    int M, N, K;
     int BN, m_tiles, n_tiles, stages, raw_stages, k_blocks, splits;
     int out_warp;              // bytes of an epilogue warp's share
     int part_at;               // split k: where in shared memory a block's part is
@@ -325,7 +323,7 @@ struct Shared {
     uint32_t tmem;
     int gave_up;
 };
-static_assert(sizeof(Shared) <= kStaticBytes, "Shared");
+static_assert(sizeof(Shared) <= 600, "Shared");
 
 // Lanes are tokens: a warp takes every third group of 32 columns of its 32 rows.  The residuals of the next group are on
 // their way to shared memory while one group is computed, and while the first one's accumulator is waited for: neighbouring
@@ -636,7 +634,7 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 }
 
 // ------------------------------------------------------------------ the kernel
-// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
+// Warps: 0 loads, 1 multiplies (in a pair's second block: reports its widened stages), 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
 // empty accumulators, 12 - 19 widen it.  Every wait ends: it is for work that has already been started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
 template <typename H, Mode MODE, bool PAIR>
@@ -1303,35 +1301,39 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
     p.K = static_cast<int>(K);
-    p.batch = static_cast<int>(batch);
     p.m_tiles = static_cast<int>((M + kBM * kBlocks - 1) / (kBM * kBlocks));
     // Widths of a tile: multiples of 16 columns, of 32 where a thread holds blocks of 32, of 64 where TMA loads boxes of
     // 64 columns and every other one is stored.  The one that covers N with the fewest columns, a tile's start and
     // end counted as 64 more; the widest of equals.
-    // (128 at most where a block's part of a split k may be a sum of chunks, and has to have a place beside the ring.)
     const int unit = kWeightGrads<MODE> ? 64 : kRows ? 32 : 16;
+    const int most = max_chunk(MODE == kWeightGrad8, dtype);
     p.k_blocks = static_cast<int>((K + kBK - 1) / kBK);
-    int64_t least = 0;
-    for (int w = kWeightGrads<MODE> && !PAIR && p.k_blocks > max_chunk(MODE == kWeightGrad8, dtype) ? 128 : 256; w >= unit && w >= std::min<int64_t>(N, kRows || kWeightGrads<MODE> ? 128 : 16); w -= unit) {
-        const int64_t tiles = (N + w - 1) / w, cost = tiles * (w + 64);
-        if (least == 0 || cost < least) {
-            least = cost;
-            p.BN = w;
+    auto cover = [&](int widest) {
+        int64_t least = 0;
+        for (int w = widest; w >= unit && w >= std::min<int64_t>(N, kRows || kWeightGrads<MODE> ? 128 : 16); w -= unit) {
+            const int64_t tiles = (N + w - 1) / w, cost = tiles * (w + 64);
+            if (least == 0 || cost < least) {
+                least = cost;
+                p.BN = w;
+            }
         }
-    }
-    p.n_tiles = static_cast<int>((N + p.BN - 1) / p.BN);
-    p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
-    p.splits = 1;
-    if (!PAIR)
-        // (eight blocks of a cluster have to find room in one GPC: 16 tiles in clusters of eight ran one after the other, 33 us
-        // where 24 in clusters of four take 16.5)
-        while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= (p.splits == 4 ? kSMs / 2 : kSMs) && p.k_blocks >= p.splits * 2) p.splits *= 2;
+        p.n_tiles = static_cast<int>((N + p.BN - 1) / p.BN);
+        p.tiles = int64_t{p.m_tiles} * p.n_tiles * batch;
+        p.splits = 1;
+        if (!PAIR)
+            // (eight blocks of a cluster have to find room in one GPC: 16 tiles in clusters of eight ran one after the other, 33 us
+            // where 24 in clusters of four take 16.5)
+            while (p.splits < kMaxSplits && p.tiles * p.splits * 2 <= (p.splits == 4 ? kSMs / 2 : kSMs) && p.k_blocks >= p.splits * 2) p.splits *= 2;
+    };
+    cover(256);
+    // A block's part of a split k that is itself a sum of chunks has to have a place beside the ring: 128 columns at most.  Where the
+    // tiles are so few and k is long, narrow ones also share it among more blocks (1536 tokens, 512 x 512: 12.4 us, wide 18.5).
+    if (kWeightGrads<MODE> && p.splits > 1 && p.k_blocks > most) cover(128);
     const int b_rows = p.BN / kBlocks;
     const int stage = kABytes + (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
     // The other products sum all of k in tensor memory: their results are rounded to 16 bits, beside which what is cut off is
     // little.  It is most for fp16 products of one sign, 5.6e-9 of the sum for each k: 2.6e-5 at 4608, where half a step of
     // fp16 is 4.9e-4 at most and 2.4e-4 at least (bf16, both signs, 2600: 4e-6 of half a step's 2e-3).
-    const int most = max_chunk(MODE == kWeightGrad8, dtype);
     const int per_split = std::max(1, (p.k_blocks + p.splits - 1) / p.splits), parts = kWeightGrads<MODE> ? (per_split + most - 1) / most : 1;
     p.chunk = (per_split + parts - 1) / parts;
     const int part_bytes = p.splits > 1 && parts > 1 ? kBM * p.BN * 4 : 0;
