@@ -40,12 +40,6 @@ constexpr int kRawBytes = kBM * kBK;          // a stage of an 8-bit A before it
 constexpr int kScaleStages = 8;               // stages whose scales are fetched at once, 4 bytes for each of their k
 constexpr int kScaleBytes = 2 * kScaleStages * kBK * 4;
 constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their own, since they are needed before A and B are
-// Pairs, 8-bit A: the second block's widened stages are reported to the first block in groups.  An arrival that releases to the
-// cluster takes one to two thousand cycles, a stage's products 512; a group also waits for its last stage, and there are five
-// stages in all (64 workers x 2048 tokens, 1024 x 1024: 544, 315, 304 and 317 us for groups of one to four; 32 x 700, 650 x 2600:
-// 211, 137, 134 and 138 us).
-constexpr int kFarStages = 3, kFarGroups = 8;
-static_assert((kRingBytes - kMinRaw * kRawBytes - kScaleBytes) / (kABytes + 128 * kBK * 2) >= kFarStages, "a group fits the ring");
 // Blocks of k that tensor memory sums in one go for a weight gradient.  The tensor cores cut a sum off where fp32 arithmetic
 // would round it, so the error grows with the length of the sum and, unlike a rounded one's, does not average out; the more bits
 // the products have the sooner.  Longer sums are added up, rounding, from parts of this length.  Error of a gradient relative to
@@ -119,28 +113,18 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
         : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok != 0;
 }
-// The same, acquiring from the whole cluster.
-__device__ __forceinline__ bool bar_try_cluster(uint64_t* b, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
-        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-    return ok != 0;
-}
 // Waits for the phase; false when the block gave up (this wait ran out, or another thread's did).  The time is looked at
 // after a few thousand tries only.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, long long limit = kWaitNs) {
-    auto over = [&] { return CLUSTER ? bar_try_cluster(b, parity) : bar_try(b, parity); };
 #pragma unroll 1
     for (int i = 0; i < 4096; ++i)
-        if (over()) return true;
+        if (bar_try(b, parity)) return true;
     long long t0, t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 1024; ++i)
-            if (over()) return true;
+            if (bar_try(b, parity)) return true;
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
         if (t - t0 > limit) {
@@ -182,11 +166,7 @@ __device__ __forceinline__ uint32_t first_of_pair(uint64_t* b) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(b)));
     return r;
 }
-// An arrival there that releases to the whole cluster what this thread wrote or has seen written.
-__device__ __forceinline__ void bar_arrive_at(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// Arrivals that say no more than that an accumulator has been read (tcgen05.wait::ld and the fence before them see to that).
+// Arrivals, there and in this block, that say no more than that an accumulator has been read (tcgen05.wait::ld and the fence before them see to that).
 __device__ __forceinline__ void bar_arrive_read_at(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -319,7 +299,6 @@ __device__ __forceinline__ void emit(const Epilogue& ep, float (&v)[16], int64_t
 
 struct Shared {
     uint64_t raw[kMaxRaw], raw_empty[kMaxRaw], scaled[2], scales_empty[2], loaded[kMaxStages], widened[kMaxStages], empty[kMaxStages], summed[2], drained[2], last;
-    uint64_t far_widened[kFarGroups];     // pairs: the second block's stages, a group at a time
     uint32_t tmem;
     int gave_up;
 };
@@ -634,7 +613,7 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t s) {
 }
 
 // ------------------------------------------------------------------ the kernel
-// Warps: 0 loads, 1 multiplies (in a pair's second block: reports its widened stages), 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
+// Warps: 0 loads, 1 multiplies, 2 owns the tensor memory, 2 and 3 load an 8-bit A and its scales, 4 - 11 (with tokens as lanes 15)
 // empty accumulators, 12 - 19 widen it.  Every wait ends: it is for work that has already been started, and a wait that takes
 // two seconds makes the whole block give up, see g_training_error.
 template <typename H, Mode MODE, bool PAIR>
@@ -645,6 +624,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __shared__ Shared sh;
     constexpr bool kAMn = kAMnMajor<MODE>, kBMn = kBMnMajor<MODE>, kFp32 = kWeightGrads<MODE>, kEight = MODE == kWeightGrad8;
     constexpr int kBlocks = PAIR ? 2 : 1;
+    static_assert(!PAIR || !kEight, "see pg_linear_weight_grad");
     uint8_t* ring = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
     const int b_rows = p.BN / kBlocks;                  // of B in this block's shared memory
     const int b_bytes = (kBMn ? (b_rows + 63) / 64 * 64 : b_rows) * kBK * 2;
@@ -661,7 +641,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bar_init(&sh.widened[s], 8);
             bar_init(&sh.empty[s], 1);
         }
-        for (int g = 0; g < kFarGroups; ++g) bar_init(&sh.far_widened[g], 1);
         for (int s = 0; s < kMaxRaw; ++s) {
             bar_init(&sh.raw[s], 1);
             bar_init(&sh.raw_empty[s], 8);
@@ -762,7 +741,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint64_t ring_a = operand_desc(smem_u32(ring), kAMn), ring_b = operand_desc(smem_u32(ring) + kABytes, kBMn);
         const int last_steps = (p.K - (p.k_blocks - 1) * kBK + 15) / 16;        // of the last block of k; the others have four
         int s = 0, parity = 0, done = 0;
-        [[maybe_unused]] int in_group = 0, group = 0;
         bool ok = true;
         for (int64_t tile = first; ok && tile < p.tiles; tile += step) {
             int kb = kb0;
@@ -774,13 +752,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 for (; kb < to; ++kb) {
                     if (!(ok = bar_wait(&sh.loaded[s], parity, gave_up))) break;
                     if (kEight && !(ok = bar_wait(&sh.widened[s], parity, gave_up))) break;
-                    if constexpr (kEight && PAIR) {
-                        if (in_group == 0 && !(ok = bar_wait<true>(&sh.far_widened[group % kFarGroups], group / kFarGroups & 1, gave_up))) break;
-                        if (++in_group == kFarStages) {
-                            in_group = 0;
-                            ++group;
-                        }
-                    }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t a = ring_a + (s * stage_bytes >> 4), bd = ring_b + (s * stage_bytes >> 4);
                     if (elected()) {
@@ -809,25 +780,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (!ok) {
             if (elected()) mma_commit<PAIR>(&sh.last);
             for (int t = 0; t < 100000 && !bar_try(&sh.last, 0); ++t) {}
-        }
-    } else if (kEight && PAIR && warp == 1) {
-        // The second block's widened stages, reported to the first block, whose thread issues the products that read them: the
-        // widening warps' writes are seen here by the block's own barrier, and passed on by one release to the cluster.
-        const uint32_t far = first_of_pair(&sh.far_widened[0]);
-        const int64_t left = p.tiles > first ? (p.tiles - first + step - 1) / step * (kb1 - kb0) : 0;
-        int s = 0, parity = 0, in_group = 0, group = 0;
-        for (int64_t i = 0; i < left; ++i) {
-            if (!bar_wait(&sh.widened[s], parity, gave_up)) break;
-            if (++in_group == kFarStages || i + 1 == left) {
-                if (elected()) bar_arrive_at(far + group % kFarGroups * 8);
-                __syncwarp();
-                in_group = 0;
-                ++group;
-            }
-            if (++s == p.stages) {
-                s = 0;
-                parity ^= 1;
-            }
         }
     } else if (warp >= 4 && warp < 4 + kEpilogueWarps<MODE>) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -915,7 +867,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int m0, n0;
             place(tile, b, m0, n0);
             const uint8_t* at = p.scales + b * p.scale_stride + m0 / kBlock8;
-            const int count = scales_of_tile(p.M, m0);     // none for a second block that begins behind the last row of A
+            const int count = scales_of_tile(p.M, m0);
             for (int kb = kb0; kb < kb1; kb += kScaleStages) {
                 if (turn > 0 && !(ok = bar_wait(&sh.scales_empty[half], (turn - 1) & 1, gave_up))) break;
                 const int64_t k0 = static_cast<int64_t>(kb) * kBK, k1 = min(static_cast<int64_t>(p.K), k0 + kScaleStages * kBK);
@@ -1499,16 +1451,19 @@ int pg_linear_weight_grad(const pg_weight_grad_args* args, void* workspace, size
     pg_matrix dz = a.dz, x = a.x;
     int rc = a.tokens > 0 ? aligned_operand(dz, a.batch, a.tokens, a.out_features, at, st) : PG_OK;
     if (rc != PG_OK) return rc;
-    const bool pairs = enough_for_pairs(a.batch, a.in_features, a.out_features, kSMs / 2);
     if (eight) {
         x = pg_matrix{a.x8.values, a.x8.ld, a.x8.stride};
-        return pairs ? run_product<kWeightGrad8, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st)
-                     : run_product<kWeightGrad8, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st);
+        // Single blocks only.  In a pair the first block's thread issues products that read what the second block's warps have
+        // widened, and the release to the cluster that this takes costs what a pair saves, three stages at a time (one at a time, 544
+        // us where single blocks take 322; pairs and single blocks: 64 workers x 2048 tokens, 1024 x 1024 322 and 322 us, 32 x 700,
+        // 650 x 2600 134 and 130, 64 x 512, 512 x 512 39 and 34, 10 x 256, 1024 x 1024 20.6 and 18.5).
+        return run_product<kWeightGrad8, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, &a.x8, st);
     }
     if (a.tokens > 0) rc = aligned_operand(x, a.batch, a.tokens, a.in_features, at, st);
     if (rc != PG_OK) return rc;
-    return pairs ? run_product<kWeightGrad, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st)
-                 : run_product<kWeightGrad, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
+    return enough_for_pairs(a.batch, a.in_features, a.out_features, kSMs / 2)
+               ? run_product<kWeightGrad, true>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st)
+               : run_product<kWeightGrad, false>(a.dtype, a.batch, a.in_features, a.out_features, a.tokens, x, dz, ep, nullptr, st);
 }
 
 int pg_selftest_training_timeout(void* stream) {

@@ -11,8 +11,7 @@
 
 namespace pgt {
 
-// Scales (one byte for 32 columns) that a row of `cols` columns has for the 128 columns from `col` on.  A tile's second half may
-// begin behind the row's end: none then.
+// Scales (one byte for 32 columns) that a row of `cols` columns has for the 128 columns from `col` on: none behind the row's end.
 PG_HOST_DEVICE int scales_of_tile(int cols, int col) {
     const int left = col < cols ? (cols - col + 31) / 32 : 0;
     return left < 4 ? left : 4;

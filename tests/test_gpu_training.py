@@ -622,8 +622,8 @@ def test_refusal_of_a_norm_gradient_that_is_too_wide(tr):
 
 @pytest.mark.parametrize("shape", [(64, 512, 512, 512), (32, 700, 650, 2600), (20, 4096, 512, 264), (37, 65, 300, 200)])
 @pytest.mark.parametrize("dtype", [BF, HF])
-def test_weight_gradients_in_pairs_of_blocks_repeat_bit_for_bit(tr, shape, dtype):
-    """Enough tiles for pairs, x widened from 8 bits by both blocks of a pair for one block's products."""
+def test_weight_gradients_of_many_tiles_repeat_bit_for_bit(tr, shape, dtype):
+    """Enough tiles for every block to take several: x widened from 8 bits beside the products, and pairs of blocks."""
     g = gen(21)
     b, t, k, n = shape
     dz, x8 = rand(g, b, t, n).to(dtype), tr.pg_checkpoint_write(rand(g, b, t, k).to(dtype))
@@ -633,7 +633,10 @@ def test_weight_gradients_in_pairs_of_blocks_repeat_bit_for_bit(tr, shape, dtype
     # the same products from the 16-bit values x8 stands for: the operands are equal, only the chunks of a sum differ
     x = tr.pg_checkpoint_read(x8)
     size = (dz[0].double().abs().transpose(0, 1) @ x[0].double().abs())
-    assert float(((first[0] - tr.pg_linear_weight_grad(dz, x)[0]).double().abs() / size).max()) <= 2 * (t + 2) * 2 * U
+    from16 = tr.pg_linear_weight_grad(dz, x)
+    assert float(((first[0] - from16[0]).double().abs() / size).max()) <= 2 * (t + 2) * 2 * U
+    for _ in range(8):
+        assert torch.equal(tr.pg_linear_weight_grad(dz, x), from16)
 
 
 def test_a_wait_that_runs_out_is_reported_once(tr):
