@@ -23,12 +23,15 @@
  *     tensor cores cut sums off instead of rounding them: of a weight gradient's size that is under
  *     1e-6, as for an fp32 product, and up to 5e-6 where all products have the same sign.)
  *   - tokens = 0 and batch = 0 are valid: outputs per token are empty, sums over tokens are zero.
- *   - A NaN or an infinity in an input reaches the outputs that depend on it, and no others.
+ *   - A NaN or an infinity in an input reaches the outputs that depend on it, and no others; in the
+ *     8-bit form it takes its block of 32 values with it (below).
  *   - Rows may start on any element.  Where they start on 16-byte boundaries the kernels take their
  *     fastest path; elsewhere 16-byte pieces of memory that hold at least one element of a row are
  *     read whole, and what else is in them is not used.  Outputs are written to their own elements only.
  *   - PG_ERR_INVALID: sizes out of range, a required pointer missing, misaligned, on the host or
- *     on another device, ld below the row length, overlapping outputs.  Nothing is launched then.
+ *     on another device, ld below the row length, rows of an output that overlap from worker to worker.
+ *     Nothing is launched then.  That different operands do not overlap (but for what may be in place)
+ *     is up to the caller.
  */
 #ifndef PG_TRAINING_H_
 #define PG_TRAINING_H_
@@ -59,7 +62,8 @@ typedef struct pg_matrix {
  *     scale - 127 = max(floor(log2(max |v| in the block)) - 6, least)
  *     q           = v * 2^-(scale - 127) rounded to nearest, ties to even, clamped to +-127
  * with least = -126 for bf16 and -24 for fp16 (whose own step that is), so that every value the
- * form stands for is exact in 16 bits.  A block that holds a NaN or an infinity gets scale 255
+ * form stands for is exact in 16 bits, where it is in the type's range (a result that goes to 8 bits
+ * from fp32 may be beyond fp16's, and reads back as an infinity).  A block that holds a NaN or an infinity gets scale 255
  * and reads back as NaN.  A row has ceil(cols / 32) scales; the last block may be short.
  * values: 16-byte aligned, ld and stride multiples of 16 (bytes from row to row, worker to worker).
  */

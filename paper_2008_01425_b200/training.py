@@ -7,6 +7,9 @@ Weights are (workers, out, in), biases and gains fp32 (workers, n).  An axis of 
 expanded (stride 0) is shared by all workers.  Results are allocated with torch unless ``out`` is
 given; their rows start on 16-byte boundaries, where every kernel takes its fastest path.
 
+The calls are not part of torch's differentiation: results do not require gradients, whatever the inputs
+do, and the gradients are calls of their own.
+
 ``stream`` is a torch stream or a raw handle; None means torch's current stream on the tensors'
 device, and a call is then ordered like any torch operation.  On another stream the caller orders the
 call after what writes its inputs and before what reads its results.  The memory of both looks after
