@@ -1319,9 +1319,16 @@ int run_product(int dtype, int64_t batch, int64_t M, int64_t N, int64_t K, const
 constexpr int64_t kMaxResidualLd = 1 << 25;       // 32 rows of residuals are addressed with 32 bits
 
 // Pairs of blocks multiply 256-row tiles; one row more than a block's 128 has to be there, and tiles for a share of the GPU:
-// with fewer, single blocks that share the k of a tile finish earlier.  A quarter of the SMs where lanes are tokens (256 tokens,
-// 1024 to 1024: 12.4 us in pairs from 5 to 12 workers, 16.5 us by single blocks), half for the weight gradient (its single
-// blocks take 12.5 us up to 9 workers of 1024 x 1024, pairs 16.5 us from 10 on).
+// with fewer, single blocks that share the k of a tile finish earlier.  A quarter of the SMs where lanes are tokens, half for the
+// weight gradient.  Pairs / single blocks in us, by 128-row blocks of tiles in pairs (37 and 74 are the limits):
+//   layer, 256 tokens, 1024 to 1024      8: 12.4 / 18.6   32: 12.4 / 16.5   64: 12.4 / 16.5   96: 12.5 / 12.5  192: 18.6 / 20.0
+//   layer, 1024 tokens, 256 to 256      16:  8.4 / 14.5   48:  8.4 / 14.4   96:  8.6 /  9.2  192: 10.4 / 12.5
+//   layer, 200 tokens, 2048 to 640      12: 15.5 / 14.5   24: 15.6 / 14.9   48: 16.4 / 16.6   96: 16.5 / 16.5
+//   input gradient, 320, 2600 to 656    12: 20.6 / 16.5   24: 20.7 / 16.5   36: 20.6 / 28.9   48: 20.7 / 18.6
+//   weight gradient, 256, 1024 x 1024   32:  9.8 / 14.5   64: 10.2 / 13.3   96: 10.4 /  8.6  192: 12.5 / 12.4  768: 30.8 / 30.0
+//   weight gradient, 2000, 1024 x 328   16: 20.6 / 12.4   64: 21.7 / 18.6   96: 21.9 / 18.5  128: 22.5 / 30.9
+//   weight gradient, 512, 512 x 512     16: 10.4 / 14.4   64: 10.4 / 14.4   96: 10.4 / 10.4  192: 14.5 / 15.0
+// Long k and few tiles are for single blocks, short k for pairs at once; the limits are where pairs lose little at either.
 bool enough_for_pairs(int64_t batch, int64_t M, int64_t N, int sms) {
     return M > kBM && batch * ((M + 2 * kBM - 1) / (2 * kBM)) * ((N + 255) / 256) * 2 >= sms;
 }
