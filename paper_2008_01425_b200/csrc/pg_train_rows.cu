@@ -539,8 +539,10 @@ int norm_grad_blocks(const pg_norm_grad_args& a) {
 }
 
 // Shares of a strip's tokens in the activation's gradient, eight at most (the portable cluster size): the number whose
-// blocks (three per SM at once) take the fewest steps of eight rows, a block's start and end counted as six.  700 tokens x
-// 2600 columns of 32 workers: 81, 76, 86 and 96 us for 1, 2, 4 and 8 shares.
+// blocks (three per SM at once) take the fewest steps of eight rows, a block's start and end counted as six.  Workers x tokens x
+// columns by 1, 2, 4 and 8 shares, and by the rule: 32 x 700 x 2600 80, 75, 86 and 95 us (75); 64 x 1024 x 1024 92.5, 92.8, 86.8 and
+// 92.7 (92.6); 16 x 300 x 4096 32.6, 32.9, 37.6 and 49.6 (32.9); 8 x 2000 x 512 129, 69, 38 and 25 (25); 1 x 4096 x 2048 254, 131, 70
+// and 39 (38); 64 x 2048 x 256 142, 78, 51 and 56 (55).
 int strip_splits(int64_t strips, int64_t tokens) {
     int best = 1;
     double least = 0.0;
