@@ -46,8 +46,8 @@ constexpr int kMaxRaw = 8, kMinRaw = 4;       // such stages: a ring of their ow
 // its size for tokens of different sizes, by blocks in a part (an fp32 product's over 768 tokens: 0.25e-6 bf16, 0.49e-6 fp16):
 //   bf16         8: 0.55e-6   12: 0.83e-6   16: 1.12e-6           fp16         8: 0.65e-6   12: 0.95e-6   16: 1.25e-6
 //   bf16, x8    12: 0.26e-6   16: 0.38e-6   32: 0.87e-6           fp16, x8    12: 0.74e-6   16: 1.0e-6    32: 2.1e-6
-// and time over 2048 tokens for 64 workers of 1024 x 1024: 519, 317, 277, 241 and 215 us for 4, 8, 12, 16 and 32 (x8: 590, 363, 336,
-// 319 and 309 us; 20 workers x 1500 tokens of 656 x 1000 from 8 bits, one part 78 us, two 102).  Chosen: the longest parts that stay
+// and time over 2048 tokens for 64 workers of 1024 x 1024: 523, 336, 298, 264 and 233 us for 4, 8, 12, 16 and 32 (x8: 572, 387, 358,
+// 331 and 305 us; 20 workers x 1500 tokens of 656 x 1000 from 8 bits, one part 69 us, two 98).  Chosen: the longest parts that stay
 // under 1e-6, and for bf16 from 8 bits half of that, about twice an fp32 product's error instead of five times.
 // Sums of products that all have one sign lose more: 1.5e-6 (bf16), 4.4e-6 (fp16), 0.75e-6 and 1.2e-6 (x8).
 constexpr int max_chunk(bool eight, int dtype) { return eight && dtype == PG_BF16 ? 1024 / kBK : 768 / kBK; }
