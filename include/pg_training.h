@@ -123,6 +123,55 @@ typedef struct pg_norm_grad_args {
 PG_API int pg_add_rms_norm_grad_workspace_bytes(const pg_norm_grad_args *args, size_t *bytes_out);
 PG_API int pg_add_rms_norm_grad(const pg_norm_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Residual addition and layer norm:
+ *     s = x + residual;  mean = mean(s);  rstd = (mean((s - mean)^2) + eps)^(-1/2);  y = (s - mean) rstd gain + bias
+ * Otherwise as pg_add_rms_norm.  With eps = 0 a row of equal values has no result.
+ */
+typedef struct pg_layer_norm_args {
+    int32_t dtype, batch, tokens, cols;
+    float eps;                 /* finite, >= 0 */
+    pg_matrix x;               /* 16-bit */
+    pg_matrix residual;        /* 16-bit, optional */
+    const float *gain;         /* cols per worker, optional (1) */
+    int64_t gain_stride;
+    const float *bias;         /* cols per worker, optional (0) */
+    int64_t bias_stride;
+    pg_matrix h;               /* out, 16-bit, optional */
+    pg_matrix y;               /* out, 16-bit, optional */
+    pg_matrix8 y8;             /* out, optional */
+    pg_matrix8 h8;             /* out, optional */
+    float *mean;               /* out, batch x tokens, optional */
+    float *rstd;               /* out, batch x tokens, optional */
+} pg_layer_norm_args;
+PG_API int pg_add_layer_norm(const pg_layer_norm_args *args, void *stream);
+
+/*
+ * Its gradient.  With u = (h - mean) rstd and a = dy gain:
+ *     dx = rstd (a - mean(a) - u mean(a u)) + dh    (also the gradient of `residual`)
+ *     dgain = sum over tokens of dy u,  dbias = sum over tokens of dy      (added to with accumulate)
+ * Otherwise as pg_add_rms_norm_grad.
+ */
+typedef struct pg_layer_norm_grad_args {
+    int32_t dtype, batch, tokens, cols;
+    int32_t accumulate;        /* 0: dgain and dbias are overwritten, 1: added to */
+    pg_matrix dy;              /* 16-bit */
+    pg_matrix h;               /* 16-bit, or */
+    pg_matrix8 h8;
+    const float *mean;         /* batch x tokens */
+    const float *rstd;         /* batch x tokens */
+    const float *gain;         /* optional (1) */
+    int64_t gain_stride;
+    pg_matrix dh;              /* 16-bit, optional: gradient that reaches h on the residual path */
+    pg_matrix dx;              /* out, 16-bit; may be dy or dh in place */
+    float *dgain;              /* out, cols per worker, optional */
+    int64_t dgain_stride;
+    float *dbias;              /* out, cols per worker, optional */
+    int64_t dbias_stride;
+} pg_layer_norm_grad_args;
+PG_API int pg_add_layer_norm_grad_workspace_bytes(const pg_layer_norm_grad_args *args, size_t *bytes_out);
+PG_API int pg_add_layer_norm_grad(const pg_layer_norm_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- linear */
 /*
  * z = x W^T + bias;  y = a(z) + residual, for every worker: x tokens x in, W out x in (a layer of
@@ -184,6 +233,144 @@ typedef struct pg_activation_grad_args {
     int64_t dbias_stride;
 } pg_activation_grad_args;
 PG_API int pg_activation_grad(const pg_activation_grad_args *args, void *stream);
+
+/* ---------------------------------------------------------- sequences */
+/*
+ * Operators along tokens.  A worker's tokens are `sequences` sequences of `length` tokens, one after another: row
+ * s length + t of a matrix is token t of sequence s.  With `lengths` (int32, batch x sequences) only the first lengths[s] tokens of a
+ * sequence are there (0 to length; other values count as the nearer of these): what the inputs hold behind them is not used, and
+ * the outputs' rows are zero there, as are what they would add to a sum.  A state, if given, is what came before a sequence's first
+ * token (zeros, if not); state_out gets what comes before the next one, and may be `state` in place.  Gradients stop at states,
+ * as in truncated back-propagation.  At most 524288 channels (PG_ERR_TOO_LARGE).
+ */
+
+/*
+ * Causal convolution of every channel with `width` taps of its own, 2 to 4:
+ *     z_t = bias + sum over j of weight[j] x_{t - width + 1 + j},   y_t = a(z_t)
+ * activation is PG_ACT_NONE or PG_ACT_SILU.  The state is the last width - 1 inputs, the oldest first.
+ */
+typedef struct pg_conv_args {
+    int32_t dtype, activation, batch, sequences, length, channels, width;
+    pg_matrix x;               /* 16-bit, tokens x channels */
+    pg_matrix weight;          /* fp32, channels x width */
+    const float *bias;         /* channels per worker, optional */
+    int64_t bias_stride;
+    const int32_t *lengths;    /* batch x sequences, optional */
+    const void *state;         /* 16-bit, batch x sequences x (width - 1) x channels, optional */
+    void *state_out;           /* out, the same, optional */
+    pg_matrix y;               /* out, 16-bit, tokens x channels */
+} pg_conv_args;
+PG_API int pg_causal_conv(const pg_conv_args *args, void *stream);
+
+/* Its gradient: dx, and with dz = dy a'(z) the sums over tokens dweight[j] of dz_t x_{t - width + 1 + j} and dbias of dz. */
+typedef struct pg_conv_grad_args {
+    int32_t dtype, activation, batch, sequences, length, channels, width;
+    int32_t accumulate;        /* 0: dweight and dbias are overwritten, 1: added to */
+    pg_matrix dy;              /* 16-bit, tokens x channels */
+    pg_matrix x;
+    pg_matrix weight;
+    const float *bias;
+    int64_t bias_stride;
+    const int32_t *lengths;
+    const void *state;
+    pg_matrix dx;              /* out, 16-bit, tokens x channels */
+    pg_matrix dweight;         /* out, fp32, channels x width, optional */
+    float *dbias;              /* out, channels per worker, optional */
+    int64_t dbias_stride;
+} pg_conv_grad_args;
+PG_API int pg_causal_conv_grad_workspace_bytes(const pg_conv_grad_args *args, size_t *bytes_out);
+PG_API int pg_causal_conv_grad(const pg_conv_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Selective scan, for every channel and `states` states (at most 64, PG_ERR_TOO_LARGE):
+ *     D_t = log(1 + exp(delta_t + delta_bias))
+ *     h_t = exp(D_t a) h_{t-1} + D_t u_t b_t,   y_t = (sum over states of c_t h_t + skip u_t) s(z_t) z_t
+ * with s as above; without z the last factors are left out.  u, delta, z and y have a column per channel, b and c one per state, a
+ * is fp32, channels x states (a layer of the stack), and not positive where states are to decay.  States are fp32.
+ * Where there are few sequences they are cut into chunks that run side by side, whose states the workspace joins.
+ */
+typedef struct pg_scan_args {
+    int32_t dtype, batch, sequences, length, channels, states;
+    pg_matrix u;               /* 16-bit, tokens x channels */
+    pg_matrix delta;           /* 16-bit, tokens x channels */
+    pg_matrix a;               /* fp32, channels x states */
+    pg_matrix b;               /* 16-bit, tokens x states */
+    pg_matrix c;               /* 16-bit, tokens x states */
+    pg_matrix z;               /* 16-bit, tokens x channels, optional */
+    const float *delta_bias;   /* channels per worker, optional (0) */
+    int64_t delta_bias_stride;
+    const float *skip;         /* channels per worker, optional (0) */
+    int64_t skip_stride;
+    const int32_t *lengths;    /* batch x sequences, optional */
+    const float *state;        /* batch x sequences x channels x states, optional */
+    float *state_out;          /* out, the same, optional */
+    pg_matrix y;               /* out, 16-bit, tokens x channels */
+} pg_scan_args;
+PG_API int pg_selective_scan_workspace_bytes(const pg_scan_args *args, size_t *bytes_out);
+PG_API int pg_selective_scan(const pg_scan_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradient, from the inputs alone (states are computed once more).  db and dc are sums over channels, da, dskip and ddelta_bias sums over
+ * tokens. */
+typedef struct pg_scan_grad_args {
+    int32_t dtype, batch, sequences, length, channels, states;
+    int32_t accumulate;        /* 0: da, dskip and ddelta_bias are overwritten, 1: added to */
+    pg_matrix dy;              /* 16-bit, tokens x channels */
+    pg_matrix u;
+    pg_matrix delta;
+    pg_matrix a;
+    pg_matrix b;
+    pg_matrix c;
+    pg_matrix z;
+    const float *delta_bias;
+    int64_t delta_bias_stride;
+    const float *skip;
+    int64_t skip_stride;
+    const int32_t *lengths;
+    const float *state;
+    pg_matrix du;              /* out, 16-bit, tokens x channels */
+    pg_matrix ddelta;          /* out, 16-bit, tokens x channels: of delta, before the softplus */
+    pg_matrix da;              /* out, fp32, channels x states */
+    pg_matrix db;              /* out, 16-bit, tokens x states */
+    pg_matrix dc;              /* out, 16-bit, tokens x states */
+    pg_matrix dz;              /* out, 16-bit, tokens x channels; with z */
+    float *dskip;              /* out, channels per worker, optional */
+    int64_t dskip_stride;
+    float *ddelta_bias;        /* out, channels per worker, optional */
+    int64_t ddelta_bias_stride;
+} pg_scan_grad_args;
+PG_API int pg_selective_scan_grad_workspace_bytes(const pg_scan_grad_args *args, size_t *bytes_out);
+PG_API int pg_selective_scan_grad(const pg_scan_grad_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* -------------------------------------------------------------- loss */
+/*
+ * Loss of a row of logits x against a teacher's top logits, and against a label: with tau = temperature,
+ *     p = softmax(teacher / tau) over the list's entries,  q = softmax(x / tau) over all classes
+ *     loss = alpha tau^2 sum p (log p - log q)  +  (1 - alpha) (log sum exp(x) - x[label])
+ * The first term is there with top > 0, the second with labels; a weight of 0 leaves a term out.  Rows whose label is no class
+ * (negative, or too large) have no second term.  Entries whose id is no class do not count, nor do those whose logit is -inf;
+ * a row without any other has no first term.  An id may occur more than once: each entry counts.  A logit x of -inf has probability 0
+ * (and an infinite loss, where p is not 0); a row of nothing else, or with a NaN or +inf, gives NaN.
+ * lse gets log sum exp(x) and log sum exp(x / tau) of every row, 0 where the loss does not need it.
+ *
+ * The gradient dloss (alpha tau (q - p) + (1 - alpha) (softmax(x) - [label])) goes to dlogits: by pg_distillation_loss
+ * together with the loss, reading the logits once (to 100000 classes; twice above), or by pg_distillation_loss_grad from lse,
+ * which it reads.  At most 1024 entries in a list (PG_ERR_TOO_LARGE).
+ */
+typedef struct pg_distillation_args {
+    int32_t dtype, batch, tokens, classes, top;
+    float temperature;         /* 1e-30 to 1e30 */
+    float alpha;               /* 0 to 1 */
+    pg_matrix logits;          /* 16-bit, tokens x classes */
+    pg_matrix ids;             /* int32, tokens x top: classes */
+    pg_matrix teacher;         /* 16-bit, tokens x top: their logits */
+    const int32_t *labels;     /* batch x tokens, optional */
+    const float *dloss;        /* batch x tokens, optional (1) */
+    float *loss;               /* out, batch x tokens, optional; not of _grad */
+    float *lse;                /* batch x tokens x 2: out, optional; read by _grad */
+    pg_matrix dlogits;         /* out, 16-bit, tokens x classes, optional but of _grad; may be logits in place */
+} pg_distillation_args;
+PG_API int pg_distillation_loss(const pg_distillation_args *args, void *stream);
+PG_API int pg_distillation_loss_grad(const pg_distillation_args *args, void *stream);
 
 /* ------------------------------------------------------------ checkpoints */
 /* tokens x cols per worker between 16 bits and the 8-bit form. */

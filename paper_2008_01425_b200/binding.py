@@ -35,6 +35,10 @@ EXPORTS = (
     "pg_add_rms_norm", "pg_add_rms_norm_grad", "pg_add_rms_norm_grad_workspace_bytes",
     "pg_linear", "pg_linear_workspace_bytes", "pg_linear_input_grad", "pg_linear_input_grad_workspace_bytes",
     "pg_linear_weight_grad", "pg_linear_weight_grad_workspace_bytes", "pg_activation_grad",
+    "pg_add_layer_norm", "pg_add_layer_norm_grad", "pg_add_layer_norm_grad_workspace_bytes",
+    "pg_causal_conv", "pg_causal_conv_grad", "pg_causal_conv_grad_workspace_bytes",
+    "pg_selective_scan", "pg_selective_scan_workspace_bytes", "pg_selective_scan_grad", "pg_selective_scan_grad_workspace_bytes",
+    "pg_distillation_loss", "pg_distillation_loss_grad",
     "pg_checkpoint_write", "pg_checkpoint_read", "pg_training_status", "pg_selftest_training_timeout", "pg_selftest_training_bounds",
 )
 PG_POWER_ITERATION, PG_RANDOM_RIGHT, PG_RANDOM_LEFT = 0, 1, 2
@@ -108,9 +112,11 @@ def load_library() -> ctypes.CDLL:
                                  ctypes.POINTER(i64)]
     L.pg_comm_floats_round.argtypes = [vp, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     L.pg_round_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
-    for name in ("pg_add_rms_norm", "pg_activation_grad", "pg_checkpoint_write", "pg_checkpoint_read"):
+    for name in ("pg_add_rms_norm", "pg_activation_grad", "pg_checkpoint_write", "pg_checkpoint_read", "pg_add_layer_norm", "pg_causal_conv",
+                 "pg_distillation_loss", "pg_distillation_loss_grad"):
         getattr(L, name).argtypes = [vp, vp]                          # (args, stream), see training.py
-    for name in ("pg_add_rms_norm_grad", "pg_linear", "pg_linear_input_grad", "pg_linear_weight_grad"):
+    for name in ("pg_add_rms_norm_grad", "pg_linear", "pg_linear_input_grad", "pg_linear_weight_grad", "pg_add_layer_norm_grad",
+                 "pg_causal_conv_grad", "pg_selective_scan", "pg_selective_scan_grad"):
         getattr(L, name).argtypes = [vp, vp, ctypes.c_size_t, vp]     # (args, workspace, bytes, stream)
         getattr(L, name + "_workspace_bytes").argtypes = [vp, szp]
     L.pg_training_status.argtypes = [vp]

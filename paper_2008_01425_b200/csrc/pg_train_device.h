@@ -25,7 +25,7 @@ constexpr bool kChecked = true;
 #else
 constexpr bool kChecked = false;
 #endif
-constexpr int kMaxSpans = 16;
+constexpr int kMaxSpans = 24;
 struct Span { uintptr_t lo, hi; };
 struct Spans {
     Span at[kMaxSpans];
@@ -268,6 +268,7 @@ __device__ __forceinline__ void widen8(const Oct8& r, float scale, F2 (&v)[4]) {
 // s(v) = 1 / (1 + 2^(-v log2 e)); both approximations are good to two units in the last place, 2^x overflows to
 // infinity and 1 / infinity is 0, so the ends are exact.  Given v (-log2 e).
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ F2 sigmoid_of(F2 v) {
     float a, b;
     split(v, a, b);
@@ -405,6 +406,8 @@ inline int take_word(unsigned* word, unsigned& value, cudaStream_t st) {
     return PG_OK;
 }
 int take_row_errors(unsigned& value, cudaStream_t st);     // of the row kernels (pg_train_rows.cu)
+int take_loss_errors(unsigned& value, cudaStream_t st);    // of the loss (pg_train_loss.cu)
+int take_sequence_errors(unsigned& value, cudaStream_t st);    // of convolution and scan (pg_train_sequence.cu)
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PG_OK : PG_ERR_CUDA; }
 
 }  // namespace pgt

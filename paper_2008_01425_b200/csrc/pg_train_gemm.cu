@@ -1489,15 +1489,15 @@ int pg_selftest_training_bounds(void* stream) {
 }
 int pg_training_status(void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    unsigned word = 0, rows = 0, outside = 0;
+    unsigned word = 0, rows = 0, loss = 0, sequence = 0, outside = 0;
     void* p = nullptr;
     if (cudaGetSymbolAddress(&p, g_training_error) != cudaSuccess || take_word(static_cast<unsigned*>(p), word, st) != PG_OK ||
-        take_row_errors(rows, st) != PG_OK)
+        take_row_errors(rows, st) != PG_OK || take_loss_errors(loss, st) != PG_OK || take_sequence_errors(sequence, st) != PG_OK)
         return PG_ERR_CUDA;
 #ifdef PG_BOUNDS_CHECK
     if (cudaGetSymbolAddress(&p, g_outside) != cudaSuccess || take_word(static_cast<unsigned*>(p), outside, st) != PG_OK) return PG_ERR_CUDA;
 #endif
-    return word & kTimedOut ? PG_ERR_TIMEOUT : (rows | outside) & kOutside ? PG_ERR_BOUNDS : PG_OK;
+    return word & kTimedOut ? PG_ERR_TIMEOUT : (rows | loss | sequence | outside) & kOutside ? PG_ERR_BOUNDS : PG_OK;
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Row-wise training operators: the norm and its gradient, the activation's gradient, the 8-bit form.
+// Row-wise training operators: the norms and their gradients, the activation's gradient, the 8-bit form.
 // All of them are bound by memory: every element is read once, held in registers as fp32, and
 // written once.  A lane holds octets (eight neighbouring elements), so four lanes make a block of the 8-bit form
 // whatever the alignment of the rows is; only the width of the accesses goes by that.
@@ -54,12 +54,16 @@ __device__ __forceinline__ void octet_to_8(F2 (&v)[4], int8_t* row, uint8_t* sca
 
 // ---------------------------------------------------------------- norm
 // T threads hold one row, C octets each; a block has 256 / T rows of one worker, at least one.  The row is read
-// once; the sum of squares comes from the registers.
-template <typename H, int W, int WO, int C, int T>
+// once; the sum of squares comes from the registers, and so does the mean before it in the layer norm (Args =
+// pg_layer_norm_args), whose squares are those of the differences from the mean: no digits cancel, at the price of a second sum.
+template <typename Args> constexpr bool kCentred = std::is_same_v<Args, pg_layer_norm_args> || std::is_same_v<Args, pg_layer_norm_grad_args>;
+template <typename H, int W, int WO, int C, int T, typename Args>
 __global__ void __launch_bounds__(T > 32 ? T : 256)
-norm_kernel(const pg_norm_args a) {
+norm_kernel(const Args a) {
+    constexpr bool kMean = kCentred<Args>;
     __shared__ float s_part[32];
     __shared__ __align__(16) float s_gain[T > 32 ? 4 : C * 256];
+    __shared__ __align__(16) float s_bias[T > 32 || !kMean ? 4 : C * 256];
     const int t = T > 32 ? threadIdx.x : threadIdx.x & 31;
     const int64_t b = blockIdx.y;
     const int tok = T > 32 ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -69,6 +73,7 @@ norm_kernel(const pg_norm_args a) {
         for (int c = 0; c < C; ++c) {
             const int col = c * 256 + threadIdx.x;
             s_gain[col] = gain && col < a.cols ? PGT_LOAD(gain[col]) : 1.0f;
+            if constexpr (kMean) s_bias[col] = a.bias && col < a.cols ? PGT_LOAD(a.bias[b * a.bias_stride + col]) : 0.0f;
         }
         __syncthreads();
     }
@@ -105,30 +110,57 @@ norm_kernel(const pg_norm_args a) {
         }
         return sum;
     };
-    F2 sums = both(0.0f);
+    float scale = 1.0f, mean = 0.0f;
+    // Sum of the squares of the row times scale, less their mean (which stays behind in `mean`).
+    auto sum_of_squares = [&](auto scaled) {
+        auto value = [&](F2 w) { return decltype(scaled)::value ? mul(w, both(scale)) : w; };
+        F2 sums = both(0.0f);
+        if constexpr (kMean) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums = fma(v[c][i], v[c][i], sums);
-    float sum = sum_of_row(sums), scale = 1.0f, eps = a.eps;
+                for (int i = 0; i < 4; ++i) sums = add(sums, value(v[c][i]));
+            mean = sum_of_row(sums) / a.cols;
+            if constexpr (T > 32) __syncthreads();     // (the shares of that sum have been read)
+            sums = both(0.0f);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * T + t) * 8;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    F2 w = add(value(v[c][i]), both(-mean));
+                    if (col + 8 > a.cols) {            // what is past the row's end is zero and not -mean
+                        float lo, hi;
+                        split(w, lo, hi);
+                        w = pair(col + 2 * i < a.cols ? lo : 0.0f, col + 2 * i + 1 < a.cols ? hi : 0.0f);
+                    }
+                    sums = fma(w, w, sums);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const F2 w = value(v[c][i]);
+                    sums = fma(w, w, sums);
+                }
+        }
+        return sum_of_row(sums);
+    };
+    float sum = sum_of_squares(std::false_type{}), eps = a.eps;
     // bf16 reaches to 2^128 and fp32 squares do not: where the sum leaves fp32's range, at the upper end or (with an eps too small
     // to matter there) at the lower one, it is taken once more of the row times a power of two.  The same for the whole row.
     if (!(sum <= 3.4028235e38f) || (sum < 8.2718061e-25f && eps < 7.8886091e-31f)) {       // 2^-80, 2^-100
         scale = sum < 1.0f ? 7.9228163e28f : 1.2621774e-29f;                               // 2^96, 2^-96
         eps = eps * scale * scale;
-        sums = both(0.0f);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const F2 w = mul(v[c][i], both(scale));
-                sums = fma(w, w, sums);
-            }
         if constexpr (T > 32) __syncthreads();         // (the shares of the first sum have been read)
-        sum = sum_of_row(sums);
+        sum = sum_of_squares(std::true_type{});
     }
     const float rstd = rsqrtf(sum / a.cols + eps);     // of the scaled row
     if (a.rstd && t == 0) PGT_STORE(a.rstd[b * a.tokens + tok], rstd * scale);
+    if constexpr (kMean)
+        if (a.mean && t == 0) PGT_STORE(a.mean[b * a.tokens + tok], mean * (1.0f / scale));
     if (a.h.data) {
         uint16_t* h = static_cast<uint16_t*>(a.h.data) + b * a.h.stride + tok * a.h.ld;
 #pragma unroll
@@ -163,8 +195,23 @@ norm_kernel(const pg_norm_args a) {
         F2 g[4];
         if constexpr (T == 32) load_gain<true>(s_gain, true, col, C * 256, g);
         else load_gain(gain, wide, col, a.cols, g);
+        if constexpr (kMean) {
+            F2 o[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+            if constexpr (T == 32) load_gain<true>(s_bias, true, col, C * 256, o);
+            else if (a.bias) load_gain(a.bias + b * a.bias_stride, wide_gain(a.bias + b * a.bias_stride), col, a.cols, o);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[c][i] = mul(v[c][i], mul(both(rstd), g[i]));
+            for (int i = 0; i < 4; ++i) {
+                v[c][i] = fma(mul(add(v[c][i], both(-mean)), both(rstd)), g[i], o[i]);
+                if (col + 8 > a.cols) {                // and is zero for the 8-bit form, too
+                    float lo, hi;
+                    split(v[c][i], lo, hi);
+                    v[c][i] = pair(col + 2 * i < a.cols ? lo : 0.0f, col + 2 * i + 1 < a.cols ? hi : 0.0f);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[c][i] = mul(v[c][i], mul(both(rstd), g[i]));
+        }
         if (a.y8.values) octet_to_8<H>(v[c], q, s, col, a.cols);
         if (y && col < a.cols) store_oct<H, WO>(y, col, a.cols, v[c]);
     }
@@ -175,12 +222,16 @@ norm_kernel(const pg_norm_args a) {
 // together; every group also keeps the sum of dy u over its rows of one worker in registers.  What was
 // read stays packed and is widened again for the second use: dx needs the row's dot product first.
 // partial[b][k][cols]: what block k of worker b added up; summed in that order by the second kernel.
+// The layer norm (Args = pg_layer_norm_grad_args) has a second dot product per row, the sum of a, and a second sum over rows, that
+// of dy, whose partials follow the others.
 constexpr int kGradBlock = 128;
-template <typename H, int W, int WO, int C, int T, int R, int BLOCKS, bool EIGHT>
+template <typename H, int W, int WO, int C, int T, int R, int BLOCKS, bool EIGHT, typename Args>
 __global__ void __launch_bounds__(T > 32 ? T : kGradBlock, BLOCKS)
-norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int rows_per_group) {
+norm_grad_kernel(const Args a, float* __restrict__ partial, int rows_per_group) {
+    constexpr bool kMean = kCentred<Args>;
+    constexpr int D = kMean ? 2 : 1;                   // dot products of a row
     extern __shared__ float s_sum[];                   // warps x cols, T == 32 only
-    __shared__ float s_part[2][R][32];
+    __shared__ float s_part[2][R][32 * D];
     constexpr int kGroups = T > 32 ? 1 : kGradBlock / T;
     const int t = T > 32 ? threadIdx.x : threadIdx.x & 31;
     const int64_t b = blockIdx.y;
@@ -188,19 +239,23 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
     const int64_t r0 = static_cast<int64_t>(group) * rows_per_group;
     const int64_t r1 = min(static_cast<int64_t>(a.tokens), r0 + rows_per_group);
     const float* gain = a.gain ? a.gain + b * a.gain_stride : nullptr;
-    F2 sum_dg[C][4], g[C][4];
+    F2 sum_dg[C][4], sum_db[kMean ? C : 1][4], g[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         load_gain(gain, wide_gain(gain), (c * T + t) * 8, a.cols, g[c]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum_dg[c][i] = both(0.0f);
     }
+#pragma unroll
+    for (int c = 0; c < (kMean ? C : 1); ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum_db[c][i] = both(0.0f);
     int flip = 0;
     for (int64_t r = r0; r < r1; r += R, flip ^= 1) {
         Oct dy_raw[R][C], h_raw[R][C], dh_raw[R][C];
         Oct8 q_raw[R][C];
         uint32_t q_scale[R][C];
-        float rstd[R];
+        float rstd[R], mean[R];
         Piece<W> dy_piece[R][C], h_piece[R][C], dh_piece[R][C];
         auto row_of = [&](const pg_matrix& m, int k) {         // a row past the last one reads the last one again, and counts for nothing
             return static_cast<const uint16_t*>(m.data) + b * m.stride + min(r + k, r1 - 1) * m.ld;
@@ -223,6 +278,8 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
             }
             if (a.dh.data) load_row<W, C, T>(row_of(a.dh, k), a.cols, t, dh_piece[k]);
             rstd[k] = PGT_LOAD(a.rstd[b * a.tokens + row]);
+            mean[k] = 0.0f;
+            if constexpr (kMean) mean[k] = PGT_LOAD(a.mean[b * a.tokens + row]);
         }
 #pragma unroll
         for (int k = 0; k < R; ++k)
@@ -237,12 +294,12 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
             if constexpr (EIGHT) widen8(q_raw[k][c], scale_value(q_scale[k][c]), u);
             else widen<H>(h_raw[k][c], u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = mul(u[i], both(rstd[k]));
+            for (int i = 0; i < 4; ++i) u[i] = mul(kMean ? add(u[i], both(-mean[k])) : u[i], both(rstd[k]));
         };
-        float dot[R];
+        float dot[R * D];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            F2 d = both(0.0f);
+            F2 d = both(0.0f), d1 = both(0.0f);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 F2 dy[4], u[4];
@@ -258,29 +315,34 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
                     }
                     if (r + k < r1) sum_dg[c][i] = add(sum_dg[c][i], w);
                     d = fma(w, g[c][i], d);
+                    if constexpr (kMean) {
+                        if (r + k < r1) sum_db[c][i] = add(sum_db[c][i], dy[i]);
+                        d1 = fma(dy[i], g[c][i], d1);
+                    }
                 }
             }
-            dot[k] = sum2(d);
+            dot[k * D] = sum2(d);
+            if constexpr (kMean) dot[k * D + 1] = sum2(d1);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-            for (int k = 0; k < R; ++k) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], o);
+            for (int k = 0; k < R * D; ++k) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], o);
         if constexpr (T > 32) {        // (the other half of s_part is still being read by slower warps)
             if ((threadIdx.x & 31) == 0)
 #pragma unroll
-                for (int k = 0; k < R; ++k) s_part[flip][k][threadIdx.x >> 5] = dot[k];
+                for (int k = 0; k < R * D; ++k) s_part[flip][k / D][(threadIdx.x >> 5) * D + k % D] = dot[k];
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
+            for (int k = 0; k < R * D; ++k) {
                 dot[k] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < T / 32; ++w) dot[k] += s_part[flip][k][w];
+                for (int w = 0; w < T / 32; ++w) dot[k] += s_part[flip][k / D][w * D + k % D];
             }
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const F2 minus = both(-dot[k] / a.cols), by = both(rstd[k]);
+            const F2 minus = both(-dot[k * D] / a.cols), by = both(rstd[k]), less = both(kMean ? -dot[k * D + D - 1] / a.cols : 0.0f);
             uint16_t* out = static_cast<uint16_t*>(a.dx.data) + b * a.dx.stride + (r + k) * a.dx.ld;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -292,39 +354,54 @@ norm_grad_kernel(const pg_norm_grad_args a, float* __restrict__ partial, int row
                 for (int i = 0; i < 4; ++i) dx[i] = both(0.0f);
                 if (a.dh.data) widen<H>(dh_raw[k][c], dx);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) dx[i] = fma(by, fma(u[i], minus, mul(dy[i], g[c][i])), dx[i]);
+                for (int i = 0; i < 4; ++i) dx[i] = fma(by, fma(u[i], minus, kMean ? fma(dy[i], g[c][i], less) : mul(dy[i], g[c][i])), dx[i]);
                 if (col < a.cols && r + k < r1) store_oct<H, WO>(out, col, a.cols, dx);
             }
         }
     }
-    if (!a.dgain) return;
-    float* out = partial + (b * gridDim.x + blockIdx.x) * a.cols;
-    float* mine = T > 32 ? out : s_sum + (threadIdx.x >> 5) * a.cols;
+    if constexpr (kMean) {
+        if (!a.dgain && !a.dbias) return;
+    } else if (!a.dgain) {
+        return;
+    }
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int which = 0; which < D; ++which) {
+        float* out = partial + ((static_cast<int64_t>(which) * gridDim.y + b) * gridDim.x + blockIdx.x) * a.cols;
+        float* mine = T > 32 ? out : s_sum + (threadIdx.x >> 5) * a.cols;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = (c * T + t) * 8 + 2 * i;
-            float lo, hi;
-            split(sum_dg[c][i], lo, hi);
-            if (col < a.cols && (T == 32 || PGT_WRITE(mine + col, 4))) mine[col] = lo;
-            if (col + 1 < a.cols && (T == 32 || PGT_WRITE(mine + col + 1, 4))) mine[col + 1] = hi;
-        }
-    if constexpr (T == 32) {
-        __syncthreads();
-        for (int col = threadIdx.x; col < a.cols; col += kGradBlock) {
-            float v = 0.0f;
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int w = 0; w < kGroups; ++w) v += s_sum[w * a.cols + col];
-            PGT_STORE(out[col], v);
+            for (int i = 0; i < 4; ++i) {
+                const int col = (c * T + t) * 8 + 2 * i;
+                float lo, hi;
+                split(which ? sum_db[kMean ? c : 0][i] : sum_dg[c][i], lo, hi);
+                if (col < a.cols && (T == 32 || PGT_WRITE(mine + col, 4))) mine[col] = lo;
+                if (col + 1 < a.cols && (T == 32 || PGT_WRITE(mine + col + 1, 4))) mine[col + 1] = hi;
+            }
+        if constexpr (T == 32) {
+            __syncthreads();
+            for (int col = threadIdx.x; col < a.cols; col += kGradBlock) {
+                float v = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kGroups; ++w) v += s_sum[w * a.cols + col];
+                PGT_STORE(out[col], v);
+            }
+            if (which + 1 < D) __syncthreads();
         }
     }
 }
 
 __global__ void __launch_bounds__(256)
-sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ out, int64_t out_stride, int accumulate) {
+sum_partials_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ out, int64_t out_stride, int accumulate,
+                    float* __restrict__ second, int64_t second_stride) {
     __shared__ float s_sum[8][32];
     const int64_t b = blockIdx.y;
+    if (blockIdx.z) {                                  // the second sum of the layer norm
+        partial += static_cast<int64_t>(gridDim.y) * parts * cols;
+        out = second;
+        out_stride = second_stride;
+    }
+    if (!out) return;
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
     float sum = 0.0f;
     if (col < cols)
@@ -530,7 +607,8 @@ void with_grad_row(int cols, F&& f) {
 
 // Blocks that share the rows of one worker in the gradient: as many as are resident at once, with two steps of R
 // rows a group at least.
-int norm_grad_blocks(const pg_norm_grad_args& a) {
+template <typename Args>
+int norm_grad_blocks(const Args& a) {
     const GradRow g = kGradRows[grad_row(a.cols)];
     const int groups = g.threads > 32 ? 1 : kGradBlock / 32;
     int64_t n = a.batch > 0 ? int64_t{kSMs} * g.blocks / a.batch : 1;
@@ -557,6 +635,115 @@ int strip_splits(int64_t strips, int64_t tokens) {
     return best;
 }
 
+template <typename Args>
+int norm(const Args* args, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const Args& a = *args;
+    const int dev = current_device();
+    if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1) || !(a.eps >= 0.0f) || a.eps > 3e38f) return PG_ERR_INVALID;
+    if (!matrix_ok(a.x, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
+    if (a.residual.data && !matrix_ok(a.residual, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
+    if (a.h.data && !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
+    if (a.y.data && !matrix_ok(a.y, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
+    if ((a.y8.values || a.y8.scales) && !matrix8_ok(a.y8, a.batch, a.tokens, a.cols, true, dev)) return PG_ERR_INVALID;
+    if ((a.h8.values || a.h8.scales) && !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, true, dev)) return PG_ERR_INVALID;
+    if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
+    if (a.rstd && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
+    if constexpr (kCentred<Args>) {
+        if (a.bias && !vector_ok(a.bias, a.bias_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
+        if (a.mean && !vector_ok(a.mean, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
+    }
+    if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
+    if (a.batch == 0 || a.tokens == 0) return PG_OK;
+    Operands operands;
+    operands.output(a.h, a.batch, a.tokens, a.cols, 2).output(a.y, a.batch, a.tokens, a.cols, 2).output(a.y8, a.batch, a.tokens, a.cols);
+    operands.output(a.h8, a.batch, a.tokens, a.cols).output(a.rstd, a.tokens, a.batch, a.tokens);
+    if constexpr (kCentred<Args>) operands.output(a.mean, a.tokens, a.batch, a.tokens).input(a.bias, a.bias_stride, a.batch, a.cols);
+    operands.input(a.x, a.batch, a.tokens, a.cols, 2).input(a.residual, a.batch, a.tokens, a.cols, 2).input(a.gain, a.gain_stride, a.batch, a.cols);
+    if (operands.publish(static_cast<cudaStream_t>(stream)) != PG_OK) return PG_ERR_CUDA;
+    with_type(a.dtype, access_width({&a.x, &a.residual}, a.batch), access_width({&a.h, &a.y}, a.batch), [&](auto h, auto in, auto out) {
+        using H = decltype(h);
+        constexpr int W = decltype(in)::value, WO = decltype(out)::value;
+        with_row(a.cols, [&](auto octets, auto threads) {
+            constexpr int T = decltype(threads)::value, C = decltype(octets)::value;
+            const dim3 grid(T > 32 ? a.tokens : (a.tokens + 7) / 8, a.batch);
+            norm_kernel<H, W, WO, C, T><<<grid, T > 32 ? T : 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
+        });
+    });
+    return launch_status();
+}
+
+template <typename Args>
+int norm_grad_workspace(const Args* args, size_t* bytes_out) {
+    if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->cols, 1)) return PG_ERR_INVALID;
+    if (args->cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
+    bool sums = args->dgain != nullptr;
+    if constexpr (kCentred<Args>) sums = sums || args->dbias != nullptr;
+    *bytes_out = sums ? sizeof(float) * (kCentred<Args> ? 2 : 1) * norm_grad_blocks(*args) * static_cast<size_t>(args->batch) * args->cols : 0;
+    return PG_OK;
+}
+
+template <typename Args>
+int norm_grad(const Args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const Args& a = *args;
+    const int dev = current_device();
+    const bool eight = a.h8.values != nullptr;
+    if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1)) return PG_ERR_INVALID;
+    const bool any = int64_t{a.batch} * a.tokens > 0;              // without tokens there is no h to be had
+    if (any && eight == (a.h.data != nullptr)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.dy, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
+    if (any && (eight ? !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, false, dev)
+              : !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, false, dev)))
+        return PG_ERR_INVALID;
+    if (a.tokens > 0 && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, false, dev)) return PG_ERR_INVALID;
+    if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
+    if (a.dh.data && !matrix_ok(a.dh, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.dx, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
+    if (a.dgain && !vector_ok(a.dgain, a.dgain_stride, a.batch, a.cols, true, dev)) return PG_ERR_INVALID;
+    float* dbias = nullptr;
+    int64_t dbias_stride = 0;
+    if constexpr (kCentred<Args>) {
+        if (a.tokens > 0 && !vector_ok(a.mean, a.tokens, a.batch, a.tokens, false, dev)) return PG_ERR_INVALID;
+        if (a.dbias && !vector_ok(a.dbias, a.dbias_stride, a.batch, a.cols, true, dev)) return PG_ERR_INVALID;
+        dbias = a.dbias;
+        dbias_stride = a.dbias_stride;
+    }
+    if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
+    size_t need = 0;
+    norm_grad_workspace(args, &need);
+    if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
+    if (a.batch == 0) return PG_OK;
+    const int blocks = norm_grad_blocks(a);
+    float* partial = static_cast<float*>(workspace);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.dx, a.batch, a.tokens, a.cols, 2).output(a.dgain, a.dgain_stride, a.batch, a.cols).output(dbias, dbias_stride, a.batch, a.cols).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
+    operands.input(a.dy, a.batch, a.tokens, a.cols, 2).input(a.dh, a.batch, a.tokens, a.cols, 2).input(a.h, a.batch, a.tokens, a.cols, 2);
+    operands.input(a.h8, a.batch, a.tokens, a.cols).input(a.rstd, a.tokens, a.batch, a.tokens).input(a.gain, a.gain_stride, a.batch, a.cols);
+    if constexpr (kCentred<Args>) operands.input(a.mean, a.tokens, a.batch, a.tokens);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    if (a.tokens > 0 || a.dgain || dbias) {
+        with_type(a.dtype, access_width({&a.dy, &a.h, &a.dh}, a.batch), access_width({&a.dx}, a.batch), [&](auto h, auto in, auto out) {
+            using H = decltype(h);
+            constexpr int W = decltype(in)::value, WO = decltype(out)::value;
+            with_grad_row(a.cols, [&](auto shape) {
+                constexpr GradRow g = kGradRows[decltype(shape)::value];
+                constexpr int T = g.threads, C = g.octets, kGroups = T > 32 ? 1 : kGradBlock / 32;
+                const int per = (a.tokens + blocks * kGroups - 1) / (blocks * kGroups);
+                const dim3 grid(blocks, a.batch);
+                const size_t smem = T > 32 ? 0 : sizeof(float) * kGroups * a.cols;
+                if (eight) norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, true><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
+                else norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, false><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
+            });
+        });
+        if (a.dgain || dbias)
+            sum_partials_kernel<<<dim3((a.cols + 31) / 32, a.batch, dbias ? 2 : 1), 256, 0, st>>>(partial, blocks, a.cols, a.dgain, a.dgain_stride,
+                                                                                                  a.accumulate, dbias, dbias_stride);
+    }
+    return launch_status();
+}
+
 }  // namespace
 
 int take_row_errors(unsigned& value, cudaStream_t st) {
@@ -577,94 +764,15 @@ using namespace pgt;
 
 extern "C" {
 
-int pg_add_rms_norm(const pg_norm_args* args, void* stream) {
-    if (!args) return PG_ERR_INVALID;
-    const pg_norm_args& a = *args;
-    const int dev = current_device();
-    if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1) || !(a.eps >= 0.0f) || a.eps > 3e38f) return PG_ERR_INVALID;
-    if (!matrix_ok(a.x, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
-    if (a.residual.data && !matrix_ok(a.residual, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
-    if (a.h.data && !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
-    if (a.y.data && !matrix_ok(a.y, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
-    if ((a.y8.values || a.y8.scales) && !matrix8_ok(a.y8, a.batch, a.tokens, a.cols, true, dev)) return PG_ERR_INVALID;
-    if ((a.h8.values || a.h8.scales) && !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, true, dev)) return PG_ERR_INVALID;
-    if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
-    if (a.rstd && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, true, dev)) return PG_ERR_INVALID;
-    if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
-    if (a.batch == 0 || a.tokens == 0) return PG_OK;
-    Operands operands;
-    operands.output(a.h, a.batch, a.tokens, a.cols, 2).output(a.y, a.batch, a.tokens, a.cols, 2).output(a.y8, a.batch, a.tokens, a.cols);
-    operands.output(a.h8, a.batch, a.tokens, a.cols).output(a.rstd, a.tokens, a.batch, a.tokens);
-    operands.input(a.x, a.batch, a.tokens, a.cols, 2).input(a.residual, a.batch, a.tokens, a.cols, 2).input(a.gain, a.gain_stride, a.batch, a.cols);
-    if (operands.publish(static_cast<cudaStream_t>(stream)) != PG_OK) return PG_ERR_CUDA;
-    with_type(a.dtype, access_width({&a.x, &a.residual}, a.batch), access_width({&a.h, &a.y}, a.batch), [&](auto h, auto in, auto out) {
-        using H = decltype(h);
-        constexpr int W = decltype(in)::value, WO = decltype(out)::value;
-        with_row(a.cols, [&](auto octets, auto threads) {
-            constexpr int T = decltype(threads)::value, C = decltype(octets)::value;
-            const dim3 grid(T > 32 ? a.tokens : (a.tokens + 7) / 8, a.batch);
-            norm_kernel<H, W, WO, C, T><<<grid, T > 32 ? T : 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
-        });
-    });
-    return launch_status();
-}
-
-int pg_add_rms_norm_grad_workspace_bytes(const pg_norm_grad_args* args, size_t* bytes_out) {
-    if (!args || !bytes_out || !sizes_ok(args->dtype, args->batch, args->tokens, args->cols, 1)) return PG_ERR_INVALID;
-    if (args->cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
-    *bytes_out = args->dgain ? sizeof(float) * norm_grad_blocks(*args) * static_cast<size_t>(args->batch) * args->cols : 0;
-    return PG_OK;
-}
-
+int pg_add_rms_norm(const pg_norm_args* args, void* stream) { return norm(args, stream); }
+int pg_add_layer_norm(const pg_layer_norm_args* args, void* stream) { return norm(args, stream); }
+int pg_add_rms_norm_grad_workspace_bytes(const pg_norm_grad_args* args, size_t* bytes_out) { return norm_grad_workspace(args, bytes_out); }
+int pg_add_layer_norm_grad_workspace_bytes(const pg_layer_norm_grad_args* args, size_t* bytes_out) { return norm_grad_workspace(args, bytes_out); }
 int pg_add_rms_norm_grad(const pg_norm_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!args) return PG_ERR_INVALID;
-    const pg_norm_grad_args& a = *args;
-    const int dev = current_device();
-    const bool eight = a.h8.values != nullptr;
-    if (!sizes_ok(a.dtype, a.batch, a.tokens, a.cols, 1)) return PG_ERR_INVALID;
-    const bool any = int64_t{a.batch} * a.tokens > 0;              // without tokens there is no h to be had
-    if (any && eight == (a.h.data != nullptr)) return PG_ERR_INVALID;
-    if (!matrix_ok(a.dy, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
-    if (any && (eight ? !matrix8_ok(a.h8, a.batch, a.tokens, a.cols, false, dev)
-              : !matrix_ok(a.h, a.batch, a.tokens, a.cols, 2, false, dev)))
-        return PG_ERR_INVALID;
-    if (a.tokens > 0 && !vector_ok(a.rstd, a.tokens, a.batch, a.tokens, false, dev)) return PG_ERR_INVALID;
-    if (a.gain && !vector_ok(a.gain, a.gain_stride, a.batch, a.cols, false, dev)) return PG_ERR_INVALID;
-    if (a.dh.data && !matrix_ok(a.dh, a.batch, a.tokens, a.cols, 2, false, dev)) return PG_ERR_INVALID;
-    if (!matrix_ok(a.dx, a.batch, a.tokens, a.cols, 2, true, dev)) return PG_ERR_INVALID;
-    if (a.dgain && !vector_ok(a.dgain, a.dgain_stride, a.batch, a.cols, true, dev)) return PG_ERR_INVALID;
-    if (a.cols > kMaxNormCols) return PG_ERR_TOO_LARGE;
-    size_t need = 0;
-    pg_add_rms_norm_grad_workspace_bytes(args, &need);
-    if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
-    if (a.batch == 0) return PG_OK;
-    const int blocks = norm_grad_blocks(a);
-    float* partial = static_cast<float*>(workspace);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Operands operands;
-    operands.output(a.dx, a.batch, a.tokens, a.cols, 2).output(a.dgain, a.dgain_stride, a.batch, a.cols).output(need > 0 ? workspace : nullptr, 0, 1, need / 4);
-    operands.input(a.dy, a.batch, a.tokens, a.cols, 2).input(a.dh, a.batch, a.tokens, a.cols, 2).input(a.h, a.batch, a.tokens, a.cols, 2);
-    operands.input(a.h8, a.batch, a.tokens, a.cols).input(a.rstd, a.tokens, a.batch, a.tokens).input(a.gain, a.gain_stride, a.batch, a.cols);
-    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
-    if (a.tokens > 0 || a.dgain) {
-        with_type(a.dtype, access_width({&a.dy, &a.h, &a.dh}, a.batch), access_width({&a.dx}, a.batch), [&](auto h, auto in, auto out) {
-            using H = decltype(h);
-            constexpr int W = decltype(in)::value, WO = decltype(out)::value;
-            with_grad_row(a.cols, [&](auto shape) {
-                constexpr GradRow g = kGradRows[decltype(shape)::value];
-                constexpr int T = g.threads, C = g.octets, kGroups = T > 32 ? 1 : kGradBlock / 32;
-                const int per = (a.tokens + blocks * kGroups - 1) / (blocks * kGroups);
-                const dim3 grid(blocks, a.batch);
-                const size_t smem = T > 32 ? 0 : sizeof(float) * kGroups * a.cols;
-                if (eight) norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, true><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
-                else norm_grad_kernel<H, W, WO, C, T, g.rows, g.blocks, false><<<grid, T > 32 ? T : kGradBlock, smem, st>>>(a, partial, per);
-            });
-        });
-        if (a.dgain)
-            sum_partials_kernel<<<dim3((a.cols + 31) / 32, a.batch), 256, 0, st>>>(partial, blocks, a.cols, a.dgain, a.dgain_stride,
-                                                                                  a.accumulate);
-    }
-    return launch_status();
+    return norm_grad(args, workspace, workspace_bytes, stream);
+}
+int pg_add_layer_norm_grad(const pg_layer_norm_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    return norm_grad(args, workspace, workspace_bytes, stream);
 }
 
 int pg_activation_grad(const pg_activation_grad_args* args, void* stream) {

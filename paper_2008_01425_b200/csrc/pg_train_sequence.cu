@@ -1,0 +1,1076 @@
+// Operators along the tokens of a sequence: the short causal convolution of every channel, the selective scan, and their gradients.
+#include <algorithm>
+#include <type_traits>
+
+#include "pg_train_device.h"
+
+namespace pgt {
+namespace {
+
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// Tokens that are there of sequence s of worker b.
+__device__ __forceinline__ int tokens_of(const int32_t* lengths, int64_t b, int sequences, int s, int length) {
+    return lengths ? max(0, min(length, PGT_LOAD(lengths[b * sequences + s]))) : length;
+}
+
+// ---------------------------------------------------------------- convolution
+// A thread has eight neighbouring channels and runs along up to kRun tokens of one sequence, with the inputs of the last
+// width - 1 tokens in registers: every input is read once, but for the few before a run.  A block's four warps have runs of
+// their own.  Bound by memory, 4 bytes a value (6 in the gradient).
+constexpr int kRun = 64;
+constexpr int kConvThreads = 128;
+
+// Inputs at token t of the sequence that starts in row r0: of x, or for t < 0 of the state before it.
+template <typename H, int W>
+__device__ __forceinline__ void input_at(const uint16_t* x, int64_t ld, const uint16_t* state, int t, int taps, int col, int cols, F2 (&v)[4]) {
+    if (t >= 0) {
+        const uint16_t* row = x + t * ld;
+        widen<H>(octet<W>(load_oct<W>(row, col, cols), row, col, cols), v);
+    } else {
+        const uint16_t* row = state + static_cast<int64_t>(taps - 1 + t) * cols;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = col + 2 * i;
+            v[i] = pair(state && c < cols ? Elem<H>::up(PGT_LOAD(row[c])) : 0.0f, state && c + 1 < cols ? Elem<H>::up(PGT_LOAD(row[c + 1])) : 0.0f);
+        }
+    }
+}
+// A thread's taps, [tap][pair of channels], and biases.
+template <int TAPS>
+__device__ __forceinline__ void load_taps(const pg_matrix& weight, const float* bias, int64_t bias_stride, int64_t b, int col, int cols, F2 (&w)[TAPS][4], F2 (&o)[4]) {
+    const float* base = static_cast<const float*>(weight.data) + b * weight.stride;
+    const float* add = bias ? bias + b * bias_stride : nullptr;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = col + 2 * i;
+#pragma unroll
+        for (int j = 0; j < TAPS; ++j)
+            w[j][i] = pair(c < cols ? PGT_LOAD(base[c * weight.ld + j]) : 0.0f, c + 1 < cols ? PGT_LOAD(base[(c + 1) * weight.ld + j]) : 0.0f);
+        o[i] = pair(add && c < cols ? PGT_LOAD(add[c]) : 0.0f, add && c + 1 < cols ? PGT_LOAD(add[c + 1]) : 0.0f);
+    }
+}
+
+template <typename H, int W, int WO, int TAPS, int ACT>
+__global__ void __launch_bounds__(kConvThreads)
+conv_kernel(const pg_conv_args a, int run, int runs) {
+    const int col = (blockIdx.y * 32 + (threadIdx.x & 31)) * 8;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+    const int64_t sequence = item / runs;              // of all workers
+    if (sequence >= static_cast<int64_t>(a.batch) * a.sequences || col >= a.channels) return;
+    const int64_t b = sequence / a.sequences;
+    const int s = static_cast<int>(sequence % a.sequences);
+    const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+    const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run);
+    const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + static_cast<int64_t>(s) * a.length * a.x.ld;
+    uint16_t* y = static_cast<uint16_t*>(a.y.data) + b * a.y.stride + static_cast<int64_t>(s) * a.length * a.y.ld;
+    const int64_t held = sequence * (TAPS - 1) * a.channels;
+    const uint16_t* state = a.state ? static_cast<const uint16_t*>(a.state) + held : nullptr;
+    F2 w[TAPS][4], o[4], before[TAPS - 1][4];
+    load_taps<TAPS>(a.weight, a.bias, a.bias_stride, b, col, a.channels, w, o);
+#pragma unroll
+    for (int j = 0; j < TAPS - 1; ++j)
+        if (t0 == 0 || t0 < have) input_at<H, W>(x, a.x.ld, state, t0 - (TAPS - 1) + j, TAPS, col, a.channels, before[j]);
+    if (t0 == 0 && a.state_out) {                      // the last inputs of the sequence; this thread has read the old ones
+        uint16_t* out = static_cast<uint16_t*>(a.state_out) + held;
+        F2 last[TAPS - 1][4];
+#pragma unroll
+        for (int j = 0; j < TAPS - 1; ++j) input_at<H, W>(x, a.x.ld, state, have - (TAPS - 1) + j, TAPS, col, a.channels, last[j]);
+#pragma unroll
+        for (int j = 0; j < TAPS - 1; ++j) store_oct<H, 1>(out + j * a.channels, col, a.channels, last[j]);
+    }
+    const int stop = min(t1, have);
+    constexpr int U = 4;                               // tokens on their way at once
+    int t = t0;
+    for (; t < stop; t += U) {
+        Piece<W> p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) p[u] = load_oct<W>(x + (t + u) * a.x.ld, col, t + u < stop ? a.channels : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t + u >= stop) break;
+            F2 v[4], z[4];
+            const uint16_t* row = x + (t + u) * a.x.ld;
+            widen<H>(octet<W>(p[u], row, col, a.channels), v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                z[i] = o[i];
+#pragma unroll
+                for (int j = 0; j < TAPS - 1; ++j) z[i] = fma(before[j][i], w[j][i], z[i]);
+                z[i] = activate<ACT>(fma(v[i], w[TAPS - 1][i], z[i]));
+#pragma unroll
+                for (int j = 0; j + 1 < TAPS - 1; ++j) before[j][i] = before[j + 1][i];
+                before[TAPS - 2][i] = v[i];
+            }
+            store_oct<H, WO>(y + (t + u) * a.y.ld, col, a.channels, z);
+        }
+    }
+    const F2 none[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+    for (t = max(t0, stop); t < t1; ++t) store_oct<H, WO>(y + t * a.y.ld, col, a.channels, none);
+}
+
+// The gradient.  dx of token t needs the pre-activations' gradients up to token t + TAPS - 1: a run recomputes those of the
+// tokens behind it.  Sums over tokens: a thread's run, the four warps of the block (shared memory), then the blocks, whose sums
+// go to partial[worker][part][TAPS + 1][channels], the bias last.
+template <typename H, int W, int WO, int TAPS, int ACT>
+__global__ void __launch_bounds__(kConvThreads)
+conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run, int runs, int parts) {
+    __shared__ float s_sum[4][TAPS + 1][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = (blockIdx.y * 32 + lane) * 8;
+    const int64_t b = blockIdx.x / parts;
+    const int part = static_cast<int>(blockIdx.x % parts);
+    const int64_t items = static_cast<int64_t>(a.sequences) * runs;      // of a worker
+    F2 dw[TAPS][4], db[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        db[i] = both(0.0f);
+#pragma unroll
+        for (int j = 0; j < TAPS; ++j) dw[j][i] = both(0.0f);
+    }
+    if (col < a.channels) {
+        F2 w[TAPS][4], o[4];
+        load_taps<TAPS>(a.weight, a.bias, a.bias_stride, b, col, a.channels, w, o);
+        for (int64_t item = part * 4 + warp; item < items; item += 4 * parts) {
+            const int s = static_cast<int>(item / runs);
+            const int64_t sequence = b * a.sequences + s;
+            const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+            const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run);
+            const int64_t first = static_cast<int64_t>(s) * a.length;
+            const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + first * a.x.ld;
+            const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + first * a.dy.ld;
+            uint16_t* dx = static_cast<uint16_t*>(a.dx.data) + b * a.dx.stride + first * a.dx.ld;
+            const uint16_t* state = a.state ? static_cast<const uint16_t*>(a.state) + sequence * (TAPS - 1) * a.channels : nullptr;
+            const int own = min(t1, have);             // tokens to own have sums here
+            if (t0 < own) {
+                F2 before[TAPS - 1][4], dz[TAPS - 1][4];
+#pragma unroll
+                for (int j = 0; j < TAPS - 1; ++j) {
+                    input_at<H, W>(x, a.x.ld, state, t0 - (TAPS - 1) + j, TAPS, col, a.channels, before[j]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dz[j][i] = both(0.0f);
+                }
+                const int stop = min(have, own + TAPS - 1);              // and those behind, for dx alone
+                constexpr int U = 2;
+                for (int t = t0; t < own + TAPS - 1; t += U) {
+                    Piece<W> px[U], pd[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        px[u] = load_oct<W>(x + (t + u) * a.x.ld, col, t + u < stop ? a.channels : 0);
+                        pd[u] = load_oct<W>(dy + (t + u) * a.dy.ld, col, t + u < stop ? a.channels : 0);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int at = t + u, to = at - (TAPS - 1);
+                        if (at >= own + TAPS - 1) break;
+                        F2 v[4], g[4], out[4];
+                        widen<H>(octet<W>(px[u], x + at * a.x.ld, col, at < stop ? a.channels : 0), v);
+                        widen<H>(octet<W>(pd[u], dy + at * a.dy.ld, col, at < stop ? a.channels : 0), g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (ACT != PG_ACT_NONE) {
+                                F2 z = o[i];
+#pragma unroll
+                                for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j][i], w[j][i], z);
+                                z = fma(v[i], w[TAPS - 1][i], z);
+                                if (at < stop) g[i] = mul(g[i], slope<ACT>(z));
+                            }
+                            if (at < own) {
+                                db[i] = add(db[i], g[i]);
+#pragma unroll
+                                for (int j = 0; j < TAPS - 1; ++j) dw[j][i] = fma(g[i], before[j][i], dw[j][i]);
+                                dw[TAPS - 1][i] = fma(g[i], v[i], dw[TAPS - 1][i]);
+                            }
+                            // dz holds the gradients of tokens at - (TAPS - 1) to at - 1
+                            out[i] = mul(g[i], w[0][i]);
+#pragma unroll
+                            for (int j = 0; j < TAPS - 1; ++j) out[i] = fma(dz[j][i], w[TAPS - 1 - j][i], out[i]);
+#pragma unroll
+                            for (int j = 0; j + 1 < TAPS - 1; ++j) {
+                                before[j][i] = before[j + 1][i];
+                                dz[j][i] = dz[j + 1][i];
+                            }
+                            before[TAPS - 2][i] = v[i];
+                            dz[TAPS - 2][i] = g[i];
+                        }
+                        if (to >= t0) store_oct<H, WO>(dx + to * a.dx.ld, col, a.channels, out);
+                    }
+                }
+            }
+            const F2 none[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+            for (int t = max(t0, own); t < t1; ++t) store_oct<H, WO>(dx + t * a.dx.ld, col, a.channels, none);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int j = 0; j < TAPS; ++j) split(dw[j][i], s_sum[warp][j][lane * 8 + 2 * i], s_sum[warp][j][lane * 8 + 2 * i + 1]);
+        split(db[i], s_sum[warp][TAPS][lane * 8 + 2 * i], s_sum[warp][TAPS][lane * 8 + 2 * i + 1]);
+    }
+    __syncthreads();
+    float* out = partial + static_cast<int64_t>(blockIdx.x) * (TAPS + 1) * a.channels;
+    for (int i = threadIdx.x; i < (TAPS + 1) * 256; i += kConvThreads) {
+        const int j = i >> 8, c = i & 255, at = blockIdx.y * 256 + c;
+        if (at < a.channels) PGT_STORE(out[static_cast<int64_t>(j) * a.channels + at], s_sum[0][j][c] + s_sum[1][j][c] + s_sum[2][j][c] + s_sum[3][j][c]);
+    }
+}
+
+// out[worker][row][col] = sum over parts of partial[worker][part][row * row_step + col * col_step], 0 <= row < rows, 0 <= col < cols, in the
+// order of the parts: eight shares, one a warp, then those.
+__global__ void __launch_bounds__(256)
+sum_parts_kernel(const float* __restrict__ partial, int64_t parts, int64_t part_size, int rows, int cols, int64_t row_step, int64_t col_step, bool rows_first,
+                 float* __restrict__ out, int64_t ld, int64_t stride, int accumulate) {
+    __shared__ float s_sum[8][32];
+    const int64_t b = blockIdx.y;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 32 + (threadIdx.x & 31);
+    const int w = threadIdx.x >> 5;
+    const bool is = at < static_cast<int64_t>(rows) * cols;
+    const int row = static_cast<int>(rows_first ? at % rows : at / cols), col = static_cast<int>(rows_first ? at / rows : at % cols);   // neighbours in `partial`
+    const float* from = partial + b * parts * part_size + row * row_step + col * col_step;
+    float sum = 0.0f;
+    if (is)
+#pragma unroll 4
+        for (int64_t k = w; k < parts; k += 8) sum += PGT_LOAD(from[k * part_size]);
+    s_sum[w][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (w == 0 && is) {
+        float* o = out + b * stride + row * ld + col;
+        sum = accumulate ? PGT_LOAD(*o) : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += s_sum[k][threadIdx.x];
+        PGT_STORE(*o, sum);
+    }
+}
+
+// ---------------------------------------------------------------- scan
+// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), with log(1 + e) = 2 artanh(s), s = e / (2 + e) <= 1/3: the series to s^13 is
+// good to 2^-26 of it, for small e too, where a logarithm of 1 + e would lose e's digits.
+__device__ __forceinline__ float softplus(float v) {
+    const float e = ex2(-kLog2e * fabsf(v)), s = e * rcp(2.0f + e), q = s * s;
+    float p = 2.0f / 13.0f;
+    p = fmaf(p, q, 2.0f / 11.0f);
+    p = fmaf(p, q, 2.0f / 9.0f);
+    p = fmaf(p, q, 2.0f / 7.0f);
+    p = fmaf(p, q, 2.0f / 5.0f);
+    p = fmaf(p, q, 2.0f / 3.0f);
+    p = fmaf(p, q, 2.0f);
+    return fmaf(s, p, fmaxf(v, 0.0f));
+}
+__device__ __forceinline__ float sigmoid(float v) { return rcp(1.0f + ex2(-kLog2e * v)); }
+
+// A channel's states lie in LANES neighbouring threads, P each.  A block has CH channels of one sequence.
+constexpr int kScanThreads = 128;
+constexpr int kScanTile = 16;                          // tokens whose b and c are in shared memory
+
+// LOCAL: a chunk's own part: its last state from a zero one, and the sum of its steps.  Otherwise the chunk's results, from the
+// state before it.
+template <typename H, int P, int LANES, bool LOCAL>
+__global__ void __launch_bounds__(kScanThreads)
+scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict__ sums, int chunk, int chunks) {
+    constexpr int N = P * LANES;
+    __shared__ __align__(16) float s_b[kScanTile][N], s_c[kScanTile][N];
+    const int64_t sequence = blockIdx.x / chunks;      // of all workers
+    const int at_chunk = static_cast<int>(blockIdx.x % chunks);
+    const int64_t b = sequence / a.sequences;
+    const int s = static_cast<int>(sequence % a.sequences);
+    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
+    const bool is = d < a.channels;
+    const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+    const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), stop = min(t1, have);
+    const int64_t first = static_cast<int64_t>(s) * a.length;
+    const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + first * a.u.ld + d;
+    const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + first * a.delta.ld + d;
+    const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + first * a.z.ld + d : nullptr;
+    const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + first * a.b.ld;
+    const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + first * a.c.ld;
+    uint16_t* y = static_cast<uint16_t*>(a.y.data) + b * a.y.stride + first * a.y.ld + d;
+    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
+    const float skip = is && a.skip ? PGT_LOAD(a.skip[b * a.skip_stride + d]) : 0.0f;
+    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
+    const int64_t held = (sequence * a.channels + d) * a.states;
+    float rate[P], h[P], sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const bool there = is && n0 + p < a.states;
+        rate[p] = there ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
+        h[p] = 0.0f;
+        if constexpr (!LOCAL) {
+            if (there && chunks > 1) h[p] = PGT_LOAD(states[(static_cast<int64_t>(blockIdx.x) * a.channels + d) * a.states + n0 + p]);
+            else if (there && a.state) h[p] = PGT_LOAD(a.state[held + n0 + p]);
+        }
+    }
+    for (int tile = t0; tile < stop; tile += kScanTile) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kScanTile * N; i += kScanThreads) {
+            const int k = i / N, n = i % N;
+            const bool there = tile + k < stop && n < a.states;
+            s_b[k][n] = there ? Elem<H>::up(PGT_LOAD(bb[(tile + k) * a.b.ld + n])) : 0.0f;
+            if constexpr (!LOCAL) s_c[k][n] = there ? Elem<H>::up(PGT_LOAD(cc[(tile + k) * a.c.ld + n])) : 0.0f;
+        }
+        __syncthreads();
+        constexpr int U = 8;
+        for (int k0 = 0; k0 < kScanTile && tile + k0 < stop; k0 += U) {
+            uint16_t ru[U], rd[U], rz[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int t = tile + k0 + k;
+                const bool there = is && t < stop;
+                ru[k] = there ? PGT_LOAD(u[t * a.u.ld]) : 0;
+                rd[k] = there ? PGT_LOAD(delta[t * a.delta.ld]) : 0;
+                if constexpr (!LOCAL) rz[k] = there && z ? PGT_LOAD(z[t * a.z.ld]) : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int t = tile + k0 + k;
+                if (t >= stop) break;
+                const float step = softplus(Elem<H>::up(rd[k]) + bias), in = Elem<H>::up(ru[k]), drive = step * in;
+                float out = 0.0f;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    h[p] = fmaf(ex2(step * rate[p]), h[p], drive * s_b[k0 + k][n0 + p]);
+                    if constexpr (!LOCAL) out = fmaf(h[p], s_c[k0 + k][n0 + p], out);
+                }
+                if constexpr (LOCAL) {
+                    sum += step;
+                } else {
+#pragma unroll
+                    for (int o = 1; o < LANES; o <<= 1) out += __shfl_xor_sync(0xffffffffu, out, o);
+                    out = fmaf(skip, in, out);
+                    if (z) {
+                        const float v = Elem<H>::up(rz[k]);
+                        out *= v * sigmoid(v);
+                    }
+                    if (is && n0 == 0) PGT_STORE(y[t * a.y.ld], Elem<H>::down(out));
+                }
+            }
+        }
+    }
+    if constexpr (LOCAL) {
+        const int64_t at = static_cast<int64_t>(blockIdx.x) * a.channels + d;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (is && n0 + p < a.states) PGT_STORE(states[at * a.states + n0 + p], h[p]);
+        if (is && n0 == 0) PGT_STORE(sums[at], sum);
+    } else {
+        if (is && n0 == 0)
+            for (int t = max(t0, stop); t < t1; ++t) PGT_STORE(y[t * a.y.ld], static_cast<uint16_t>(0));
+        if (a.state_out && at_chunk == chunks - 1)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if (is && n0 + p < a.states) PGT_STORE(a.state_out[held + n0 + p], h[p]);
+    }
+}
+
+// From the chunks' own parts to the states before them, in place; carries: backwards, from the adjoints' own parts to what reaches
+// a chunk from those behind it.
+__global__ void __launch_bounds__(128)
+join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float* __restrict__ states, float* __restrict__ carries, const float* __restrict__ sums,
+                   int sequences, int channels, int n_states, int chunks) {
+    const int64_t sequence = blockIdx.x, b = sequence / sequences;
+    const int64_t width = static_cast<int64_t>(channels) * n_states, at = static_cast<int64_t>(blockIdx.y) * 128 + threadIdx.x;
+    if (at >= width) return;
+    const int64_t d = at / n_states, n = at % n_states;
+    const float rate = PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]) * kLog2e;
+    float h = state ? PGT_LOAD(state[sequence * width + at]) : 0.0f;
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+        const int64_t k = sequence * chunks + c;
+        const float own = PGT_LOAD(states[k * width + at]), sum = PGT_LOAD(sums[k * channels + d]);
+        PGT_STORE(states[k * width + at], h);
+        h = fmaf(ex2(sum * rate), h, own);
+    }
+    if (!carries) return;
+    float g = 0.0f;
+#pragma unroll 4
+    for (int c = chunks - 1; c >= 0; --c) {
+        const int64_t k = sequence * chunks + c;
+        const float own = PGT_LOAD(carries[k * width + at]), sum = PGT_LOAD(sums[k * channels + d]);
+        PGT_STORE(carries[k * width + at], g);
+        g = fmaf(ex2(sum * rate), g, own);
+    }
+}
+
+// ---------------------------------------------------------------- scan gradient
+// Backwards along a chunk with g_t = exp(D_t+1 A) g_t+1 + C_t dv_t the gradient of h_t (dv: of y before the gate):
+//     dC_t = sum over channels of dv_t h_t,  dB_t = sum over channels of g_t D_t u_t
+//     du_t = D_t (g_t . B_t) + skip dv_t
+//     dD_t = u_t (g_t . B_t) + sum over states of A e_t,   e_t = g_t h_t-1 exp(D_t A)
+//     dA = sum over tokens of D_t e_t,  dskip = sum of dv_t u_t,  ddelta_t = dD_t sigmoid(delta_t + delta_bias)
+// The states before groups of kGroup tokens are kept in shared memory on a way forward through the chunk; backwards the
+// states of a group are computed once more.
+constexpr int kGradStates = 8;                         // states of a thread
+constexpr int kGroup = 4;
+constexpr int kGradChunk = 64;                         // tokens of a chunk at most
+
+template <typename H, int LANES>
+struct GradChannel {                                   // what a thread knows of its channel in one sequence
+    const uint16_t *u, *delta, *z, *dy;
+    float bias, skip;
+    bool is;
+};
+
+// Own parts of a chunk for the way in both directions: the last state from a zero one, and the gradient that reaches the state before it.
+template <typename H, int LANES>
+__global__ void __launch_bounds__(kScanThreads)
+scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, float* __restrict__ carries, float* __restrict__ sums, int chunk, int chunks) {
+    constexpr int P = kGradStates, N = P * LANES;
+    __shared__ __align__(16) float s_b[kScanTile][N], s_c[kScanTile][N];
+    const int64_t sequence = blockIdx.x / chunks;
+    const int at_chunk = static_cast<int>(blockIdx.x % chunks);
+    const int64_t b = sequence / a.sequences;
+    const int s = static_cast<int>(sequence % a.sequences);
+    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
+    const bool is = d < a.channels;
+    const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+    const int t0 = at_chunk * chunk, stop = min(min(a.length, t0 + chunk), have);
+    const int64_t first = static_cast<int64_t>(s) * a.length;
+    const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + first * a.u.ld + d;
+    const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + first * a.delta.ld + d;
+    const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + first * a.z.ld + d : nullptr;
+    const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + first * a.dy.ld + d;
+    const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + first * a.b.ld;
+    const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + first * a.c.ld;
+    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
+    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
+    float rate[P], h[P], g[P], product[P], sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        rate[p] = is && n0 + p < a.states ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
+        h[p] = g[p] = 0.0f;
+        product[p] = 1.0f;
+    }
+    for (int tile = t0; tile < stop; tile += kScanTile) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kScanTile * N; i += kScanThreads) {
+            const int k = i / N, n = i % N;
+            const bool there = tile + k < stop && n < a.states;
+            s_b[k][n] = there ? Elem<H>::up(PGT_LOAD(bb[(tile + k) * a.b.ld + n])) : 0.0f;
+            s_c[k][n] = there ? Elem<H>::up(PGT_LOAD(cc[(tile + k) * a.c.ld + n])) : 0.0f;
+        }
+        __syncthreads();
+        for (int k = 0; k < kScanTile && tile + k < stop; ++k) {
+            const int t = tile + k;
+            if (!is) break;
+            const float step = softplus(Elem<H>::up(PGT_LOAD(delta[t * a.delta.ld])) + bias), drive = step * Elem<H>::up(PGT_LOAD(u[t * a.u.ld]));
+            float dv = Elem<H>::up(PGT_LOAD(dy[t * a.dy.ld]));
+            if (z) {
+                const float v = Elem<H>::up(PGT_LOAD(z[t * a.z.ld]));
+                dv *= v * sigmoid(v);
+            }
+            sum += step;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float keep = ex2(step * rate[p]);
+                h[p] = fmaf(keep, h[p], drive * s_b[k][n0 + p]);
+                product[p] *= keep;
+                g[p] = fmaf(product[p] * dv, s_c[k][n0 + p], g[p]);
+            }
+        }
+    }
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * a.channels + d;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+        if (is && n0 + p < a.states) {
+            PGT_STORE(states[at * a.states + n0 + p], h[p]);
+            PGT_STORE(carries[at * a.states + n0 + p], g[p]);
+        }
+    if (is && n0 == 0) PGT_STORE(sums[at], sum);
+}
+
+// Sums v[0 .. 2P) over the warp's lanes with the same lane % LANES; a lane keeps 2P / (32 / LANES) of them, at least one: those from
+// the returned index on.
+template <int LANES, int V>
+__device__ __forceinline__ int scatter_sums(float (&v)[V]) {
+    const int lane = threadIdx.x & 31;
+    int at = 0, count = V;
+#pragma unroll
+    for (int o = 16; o >= LANES; o >>= 1) {
+        if (count > 1) {
+            count >>= 1;
+            const bool high = lane & o;
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                if (i >= count) break;
+                const float give = high ? v[i] : v[count + i], keep = high ? v[count + i] : v[i];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+            at += high ? count : 0;
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        }
+    }
+    return at;
+}
+
+// A block has one share of a worker's chunks and kScanThreads / LANES channels, whose dA, dskip and ddelta_bias stay in registers.
+// parts[block's channels][worker][token][2 N]: what these channels add to dB and dC.
+// partial[worker][share][channels][states + 2]: dA, then dskip and ddelta_bias.
+template <typename H, int LANES>
+__global__ void __launch_bounds__(kScanThreads)
+scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, const float* __restrict__ carries, float* __restrict__ parts,
+                 float* __restrict__ partial, int chunk, int chunks, int shares) {
+    constexpr int P = kGradStates, N = P * LANES, G = 32 / LANES, V = 2 * P, kKept = V / G > 1 ? V / G : 1;
+    extern __shared__ __align__(16) float s_all[];
+    const int groups = (chunk + kGroup - 1) / kGroup;
+    float* s_b = s_all;                                // [token][N]
+    float* s_c = s_b + groups * kGroup * N;
+    float* s_h = s_c + groups * kGroup * N;            // [group][P][thread]
+    float* s_red = s_h + groups * P * kScanThreads;    // [warp][token of the group][2 N]
+    const int64_t b = blockIdx.x / shares;
+    const int share = static_cast<int>(blockIdx.x % shares);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
+    const bool is = d < a.channels, writes = is && n0 == 0;
+    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
+    const float skip = is && a.skip ? PGT_LOAD(a.skip[b * a.skip_stride + d]) : 0.0f;
+    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
+    float rate[P], da[P], dskip = 0.0f, dbias = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        rate[p] = is && n0 + p < a.states ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
+        da[p] = 0.0f;
+    }
+    const int64_t tokens = static_cast<int64_t>(a.sequences) * a.length;
+    float* my_parts = parts + (static_cast<int64_t>(blockIdx.y) * a.batch + b) * tokens * 2 * N;
+    for (int64_t item = share; item < static_cast<int64_t>(a.sequences) * chunks; item += shares) {
+        const int s = static_cast<int>(item / chunks), at_chunk = static_cast<int>(item % chunks);
+        const int64_t sequence = b * a.sequences + s, first = static_cast<int64_t>(s) * a.length;
+        const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+        const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), stop = min(t1, have), count = max(0, stop - t0);
+        const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + (first + t0) * a.u.ld + d;
+        const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + (first + t0) * a.delta.ld + d;
+        const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + (first + t0) * a.z.ld + d : nullptr;
+        const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + (first + t0) * a.dy.ld + d;
+        const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + (first + t0) * a.b.ld;
+        const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + (first + t0) * a.c.ld;
+        uint16_t* du = static_cast<uint16_t*>(a.du.data) + b * a.du.stride + (first + t0) * a.du.ld + d;
+        uint16_t* ddelta = static_cast<uint16_t*>(a.ddelta.data) + b * a.ddelta.stride + (first + t0) * a.ddelta.ld + d;
+        uint16_t* dz = z ? static_cast<uint16_t*>(a.dz.data) + b * a.dz.stride + (first + t0) * a.dz.ld + d : nullptr;
+        __syncthreads();                               // (shared memory is free again)
+        for (int i = threadIdx.x; i < groups * kGroup * N; i += kScanThreads) {
+            const int k = i / N, n = i % N;
+            const bool there = k < count && n < a.states;
+            s_b[i] = there ? Elem<H>::up(PGT_LOAD(bb[k * a.b.ld + n])) : 0.0f;
+            s_c[i] = there ? Elem<H>::up(PGT_LOAD(cc[k * a.c.ld + n])) : 0.0f;
+        }
+        __syncthreads();
+        auto load = [&](const uint16_t* p, int64_t ld, int k) { return is && k < count ? Elem<H>::up(PGT_LOAD(p[k * ld])) : 0.0f; };
+        auto step_at = [&](int k) { return is && k < count ? softplus(load(delta, a.delta.ld, k) + bias) : 0.0f; };
+        float h[P], g[P];
+        const int64_t held = (sequence * a.channels + d) * a.states, chunk_at = ((sequence * chunks + at_chunk) * a.channels + d) * a.states;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool there = is && n0 + p < a.states;
+            h[p] = !there ? 0.0f : chunks > 1 ? PGT_LOAD(states[chunk_at + n0 + p]) : a.state ? PGT_LOAD(a.state[held + n0 + p]) : 0.0f;
+            g[p] = there && chunks > 1 ? PGT_LOAD(carries[chunk_at + n0 + p]) : 0.0f;
+        }
+        for (int k = 0; k < count; ++k) {              // forward
+            if (k % kGroup == 0)
+#pragma unroll
+                for (int p = 0; p < P; ++p) s_h[(k / kGroup * P + p) * kScanThreads + threadIdx.x] = h[p];
+            const float step = step_at(k), drive = step * load(u, a.u.ld, k);
+#pragma unroll
+            for (int p = 0; p < P; ++p) h[p] = fmaf(ex2(step * rate[p]), h[p], drive * s_b[k * N + n0 + p]);
+        }
+        for (int group = (count + kGroup - 1) / kGroup - 1; group >= 0; --group) {
+            float before[kGroup][P], keep[kGroup][P], step[kGroup], in[kGroup], dv[kGroup], inner[kGroup], slope_z[kGroup];
+#pragma unroll
+            for (int p = 0; p < P; ++p) h[p] = s_h[(group * P + p) * kScanThreads + threadIdx.x];
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) {
+                const int k = group * kGroup + i;      // tokens behind the last one change nothing: their step is zero
+                step[i] = step_at(k);
+                in[i] = load(u, a.u.ld, k);
+                const float drive = step[i] * in[i], gy = load(dy, a.dy.ld, k);
+                float out = 0.0f;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    before[i][p] = h[p];
+                    keep[i][p] = ex2(step[i] * rate[p]);
+                    h[p] = fmaf(keep[i][p], h[p], drive * s_b[k * N + n0 + p]);
+                    out = fmaf(h[p], s_c[k * N + n0 + p], out);
+                }
+                dv[i] = gy;
+                if (z) {
+#pragma unroll
+                    for (int o = 1; o < LANES; o <<= 1) out += __shfl_xor_sync(0xffffffffu, out, o);
+                    const float v = load(z, a.z.ld, k), sig = sigmoid(v);
+                    slope_z[i] = gy * fmaf(skip, in[i], out) * (sig * fmaf(v, 1.0f - sig, 1.0f));
+                    dv[i] = gy * v * sig;
+                }
+                inner[i] = out;
+            }
+#pragma unroll
+            for (int i = kGroup - 1; i >= 0; --i) {
+                const int k = group * kGroup + i;
+                float v[V], to_drive = 0.0f, to_step = 0.0f;
+                const float drive = step[i] * in[i];
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const float after = i + 1 < kGroup ? before[i + 1 < kGroup ? i + 1 : i][p] : h[p];
+                    g[p] = fmaf(dv[i], s_c[k * N + n0 + p], g[p]);
+                    v[p] = g[p] * drive;
+                    v[P + p] = dv[i] * after;
+                    to_drive = fmaf(g[p], s_b[k * N + n0 + p], to_drive);
+                    g[p] *= keep[i][p];
+                    const float e = g[p] * before[i][p];
+                    to_step = fmaf(e, rate[p], to_step);
+                    da[p] = fmaf(e, step[i], da[p]);
+                }
+#pragma unroll
+                for (int o = 1; o < LANES; o <<= 1) {
+                    to_drive += __shfl_xor_sync(0xffffffffu, to_drive, o);
+                    to_step += __shfl_xor_sync(0xffffffffu, to_step, o);
+                }
+                if (writes && k < count) {
+                    const float raw = load(delta, a.delta.ld, k) + bias;
+                    const float dd = fmaf(to_drive, in[i], to_step * kLn2) * sigmoid(raw);
+                    PGT_STORE(du[k * a.du.ld], Elem<H>::down(fmaf(to_drive, step[i], skip * dv[i])));
+                    PGT_STORE(ddelta[k * a.ddelta.ld], Elem<H>::down(dd));
+                    if (dz) PGT_STORE(dz[k * a.dz.ld], Elem<H>::down(slope_z[i]));
+                    dskip = fmaf(dv[i], in[i], dskip);
+                    dbias += dd;
+                }
+                const int at = scatter_sums<LANES>(v);
+#pragma unroll
+                for (int j = 0; j < kKept; ++j)
+                    if (V >= G || (lane & (G / V * LANES - 1)) < LANES)   // (of lanes that hold the same sum the first)
+                        s_red[(warp * kGroup + i) * 2 * N + (at + j < P ? n0 + at + j : N + n0 + at + j - P)] = v[j];
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < kGroup * 2 * N; i += kScanThreads) {
+                const int k = group * kGroup + i / (2 * N);
+                float v = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kScanThreads / 32; ++w) v += s_red[w * kGroup * 2 * N + i];
+                if (k < count) PGT_STORE(my_parts[(first + t0 + k) * 2 * N + i % (2 * N)], v);
+            }
+            __syncthreads();
+        }
+        for (int k = count; k < t1 - t0; ++k) {
+            if (writes) {
+                PGT_STORE(du[k * a.du.ld], static_cast<uint16_t>(0));
+                PGT_STORE(ddelta[k * a.ddelta.ld], static_cast<uint16_t>(0));
+                if (dz) PGT_STORE(dz[k * a.dz.ld], static_cast<uint16_t>(0));
+            }
+            for (int i = threadIdx.x; i < 2 * N; i += kScanThreads) PGT_STORE(my_parts[(first + t0 + k) * 2 * N + i], 0.0f);
+        }
+    }
+    float* mine = partial + (static_cast<int64_t>(blockIdx.x) * a.channels + d) * (a.states + 2);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+        if (is && n0 + p < a.states) PGT_STORE(mine[n0 + p], da[p]);
+    if (writes) {
+        PGT_STORE(mine[a.states], dskip);
+        PGT_STORE(mine[a.states + 1], dbias);
+    }
+}
+
+// dB and dC: the channel blocks' parts added up in order.
+template <typename H>
+__global__ void __launch_bounds__(256)
+sum_bc_kernel(const pg_scan_grad_args a, const float* __restrict__ parts, int blocks, int n_padded) {
+    const int64_t tokens = static_cast<int64_t>(a.sequences) * a.length, all = a.batch * tokens * 2 * n_padded;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= all) return;
+    const int n = static_cast<int>(i % (2 * n_padded));
+    const int64_t row = i / (2 * n_padded), b = row / tokens, t = row % tokens;
+    float v = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < blocks; ++k) v += PGT_LOAD(parts[k * all + i]);
+    const pg_matrix& m = n < n_padded ? a.db : a.dc;
+    const int to = n < n_padded ? n : n - n_padded;
+    if (to < a.states) PGT_STORE((static_cast<uint16_t*>(m.data) + b * m.stride + t * m.ld)[to], Elem<H>::down(v));
+}
+
+// ---------------------------------------------------------------- host
+int current_device() {
+    int d = 0;
+    return cudaGetDevice(&d) == cudaSuccess ? d : -1;
+}
+constexpr int64_t kMaxBlocks = (int64_t{1} << 31) - 1;
+constexpr int kMaxChannels = 1 << 19;
+constexpr int kMaxStates = 64;
+
+// Sizes of a batch of sequences; the product of sequences and length is the number of a worker's tokens.
+bool sequence_sizes_ok(int64_t dtype, int64_t batch, int64_t sequences, int64_t length, int64_t channels) {
+    return sizes_ok(dtype, batch, length, channels, 1) && sequences >= 0 && sequences <= kMaxDim && sequences * length <= kMaxDim;
+}
+bool array_ok(const void* p, uintptr_t align, int64_t count, int dev) { return count == 0 || device_pointer(p, align, dev); }
+Operands& span(Operands& o, const void* p, int64_t bytes, bool output) {
+    const pg_matrix m = {const_cast<void*>(p), bytes, 0};
+    return output ? o.output(m, 1, 1, bytes, 1) : o.input(m, 1, 1, bytes, 1);
+}
+
+template <typename F>
+void with_taps(int taps, F&& f) {
+    using std::integral_constant;
+    if (taps == 2) f(integral_constant<int, 2>{});
+    else if (taps == 3) f(integral_constant<int, 3>{});
+    else f(integral_constant<int, 4>{});
+}
+template <typename F>
+void with_widths(int in, int out, F&& f) {
+    using std::integral_constant;
+    if (out < 8) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    else if (in == 8) f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    else f(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+}
+template <typename F>
+void with_kind(int dtype, F&& f) {
+    if (dtype == PG_BF16) f(__nv_bfloat16{});
+    else f(__half{});
+}
+
+// Tokens of a thread's run: kRun, fewer where there would not be a block of four runs for each of an SM's eight places.
+int conv_run(int64_t sequences, int64_t length, int64_t strips) {
+    int run = static_cast<int>(std::min<int64_t>(kRun, std::max<int64_t>(length, 1)));
+    while (run > 8 && sequences * ((length + run - 1) / run) * strips < int64_t{kSMs} * 8 * 4) run = (run + 1) / 2;
+    return run;
+}
+// Blocks that share a worker's runs in the gradient.
+int conv_parts(const pg_conv_grad_args& a, int runs) {
+    const int64_t strips = (a.channels + 255) / 256, items = int64_t{a.sequences} * runs;
+    const int64_t most = std::max<int64_t>(1, int64_t{kSMs} * 6 / std::max<int64_t>(1, strips * a.batch));
+    return static_cast<int>(std::max<int64_t>(1, std::min(most, (items + 3) / 4)));
+}
+
+struct ScanPlan { int chunk, chunks; };
+// Chunks of a sequence for the forward scan: one unless there are too few threads for the GPU.
+ScanPlan scan_plan(const pg_scan_args& a, int lanes) {
+    const int64_t blocks = int64_t{a.batch} * a.sequences * ((int64_t{a.channels} * lanes + kScanThreads - 1) / kScanThreads);
+    int64_t chunks = std::max<int64_t>(1, int64_t{kSMs} * 4 / std::max<int64_t>(1, blocks));
+    int64_t chunk = std::max<int64_t>(64, (a.length + chunks - 1) / chunks);
+    if (blocks >= 2 * kSMs) chunk = std::max<int64_t>(a.length, 1);
+    chunks = std::max<int64_t>(1, (a.length + chunk - 1) / chunk);
+    return {static_cast<int>(chunk), static_cast<int>(chunks)};
+}
+int lanes_of(int states, int per_thread) {
+    int lanes = 1;
+    while (lanes * per_thread < states) lanes *= 2;
+    return lanes;
+}
+struct GradPlan { int chunk, chunks, lanes, shares; int64_t blocks; size_t states, sums, parts, partial; };
+GradPlan grad_plan(const pg_scan_grad_args& a) {
+    GradPlan p = {};
+    p.lanes = lanes_of(a.states, kGradStates);
+    const int64_t length = std::max(a.length, 1);
+    p.chunks = static_cast<int>((length + kGradChunk - 1) / kGradChunk);
+    p.chunk = static_cast<int>((length + p.chunks - 1) / p.chunks);
+    p.blocks = (int64_t{a.channels} * p.lanes + kScanThreads - 1) / kScanThreads;
+    const int64_t items = int64_t{a.sequences} * p.chunks;
+    p.shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(items, int64_t{kSMs} * 6 / std::max<int64_t>(1, p.blocks * a.batch))));
+    const size_t all = static_cast<size_t>(a.batch) * items;
+    auto round = [](size_t n) { return (n + 255) / 256 * 256; };
+    p.states = p.chunks > 1 ? round(sizeof(float) * all * a.channels * a.states) : 0;         // and as much for the carries
+    p.sums = p.chunks > 1 ? round(sizeof(float) * all * a.channels) : 0;
+    p.parts = round(sizeof(float) * p.blocks * a.batch * static_cast<size_t>(a.sequences) * a.length * 2 * kGradStates * p.lanes);
+    p.partial = round(sizeof(float) * static_cast<size_t>(a.batch) * p.shares * a.channels * (a.states + 2));
+    return p;
+}
+
+int conv_check(int dtype, int activation, int batch, int sequences, int length, int channels, int width) {
+    if (!sequence_sizes_ok(dtype, batch, sequences, length, channels) || width < 2 || width > 4) return PG_ERR_INVALID;
+    if (activation != PG_ACT_NONE && activation != PG_ACT_SILU) return PG_ERR_INVALID;
+    return channels > kMaxChannels ? PG_ERR_TOO_LARGE : PG_OK;
+}
+
+template <typename Args>
+int scan_check(const Args& a) {
+    if (!sequence_sizes_ok(a.dtype, a.batch, a.sequences, a.length, a.channels) || a.states < 1) return PG_ERR_INVALID;
+    return a.states > kMaxStates || a.channels > kMaxChannels ? PG_ERR_TOO_LARGE : PG_OK;
+}
+template <typename Args>
+bool scan_inputs_ok(const Args& a, int dev) {
+    const int64_t tokens = int64_t{a.sequences} * a.length, held = int64_t{a.batch} * a.sequences;
+    if (!matrix_ok(a.u, a.batch, tokens, a.channels, 2, false, dev) || !matrix_ok(a.delta, a.batch, tokens, a.channels, 2, false, dev)) return false;
+    if (!matrix_ok(a.b, a.batch, tokens, a.states, 2, false, dev) || !matrix_ok(a.c, a.batch, tokens, a.states, 2, false, dev)) return false;
+    if (!matrix_ok(a.a, a.batch, a.channels, a.states, 4, false, dev)) return false;
+    if (a.z.data && !matrix_ok(a.z, a.batch, tokens, a.channels, 2, false, dev)) return false;
+    if (a.delta_bias && !vector_ok(a.delta_bias, a.delta_bias_stride, a.batch, a.channels, false, dev)) return false;
+    if (a.skip && !vector_ok(a.skip, a.skip_stride, a.batch, a.channels, false, dev)) return false;
+    if (a.lengths && !array_ok(a.lengths, 4, held, dev)) return false;
+    return !a.state || array_ok(a.state, 4, held, dev);
+}
+template <typename Args>
+void scan_inputs(Operands& o, const Args& a) {
+    const int64_t tokens = int64_t{a.sequences} * a.length, held = int64_t{a.batch} * a.sequences;
+    o.input(a.u, a.batch, tokens, a.channels, 2).input(a.delta, a.batch, tokens, a.channels, 2).input(a.z, a.batch, tokens, a.channels, 2);
+    o.input(a.b, a.batch, tokens, a.states, 2).input(a.c, a.batch, tokens, a.states, 2).input(a.a, a.batch, a.channels, a.states, 4);
+    o.input(a.delta_bias, a.delta_bias_stride, a.batch, a.channels).input(a.skip, a.skip_stride, a.batch, a.channels);
+    span(o, a.lengths, held * 4, false);
+    span(o, a.state, held * a.channels * a.states * 4, false);
+}
+
+}  // namespace
+
+int take_sequence_errors(unsigned& value, cudaStream_t st) {
+    value = 0;
+#ifdef PG_BOUNDS_CHECK
+    void* word = nullptr;
+    if (cudaGetSymbolAddress(&word, g_outside) != cudaSuccess) return PG_ERR_CUDA;
+    return take_word(static_cast<unsigned*>(word), value, st);
+#else
+    static_cast<void>(st);
+    return PG_OK;
+#endif
+}
+
+}  // namespace pgt
+
+using namespace pgt;
+
+extern "C" {
+
+int pg_causal_conv(const pg_conv_args* args, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const pg_conv_args& a = *args;
+    const int dev = current_device(), rc = conv_check(a.dtype, a.activation, a.batch, a.sequences, a.length, a.channels, a.width);
+    if (rc == PG_ERR_INVALID) return rc;
+    const int64_t tokens = int64_t{a.sequences} * a.length, sequences = int64_t{a.batch} * a.sequences, held = sequences * (a.width - 1) * a.channels;
+    if (!matrix_ok(a.x, a.batch, tokens, a.channels, 2, false, dev) || !matrix_ok(a.y, a.batch, tokens, a.channels, 2, true, dev)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.weight, a.batch, a.channels, a.width, 4, false, dev)) return PG_ERR_INVALID;
+    if (a.bias && !vector_ok(a.bias, a.bias_stride, a.batch, a.channels, false, dev)) return PG_ERR_INVALID;
+    if ((a.lengths && !array_ok(a.lengths, 4, sequences, dev)) || (a.state && !array_ok(a.state, 2, held, dev)) ||
+        (a.state_out && !array_ok(a.state_out, 2, held, dev)))
+        return PG_ERR_INVALID;
+    const int strips = (a.channels + 255) / 256, run = conv_run(sequences, a.length, strips);
+    const int runs = std::max(1, (a.length + run - 1) / run);
+    const int64_t blocks = (sequences * runs + 3) / 4;
+    if (rc != PG_OK || blocks > kMaxBlocks) return PG_ERR_TOO_LARGE;
+    if (sequences == 0 || (a.length == 0 && !a.state_out)) return PG_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.y, a.batch, tokens, a.channels, 2);
+    span(operands, a.state_out, held * 2, true);
+    operands.input(a.x, a.batch, tokens, a.channels, 2).input(a.weight, a.batch, a.channels, a.width, 4).input(a.bias, a.bias_stride, a.batch, a.channels);
+    span(operands, a.lengths, sequences * 4, false);
+    span(operands, a.state, held * 2, false);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    with_kind(a.dtype, [&](auto h) {
+        with_widths(access_width({&a.x}, a.batch), access_width({&a.y}, a.batch), [&](auto in, auto out) {
+            with_taps(a.width, [&](auto taps) {
+                using H = decltype(h);
+                constexpr int W = decltype(in)::value, WO = decltype(out)::value, TAPS = decltype(taps)::value;
+                const dim3 grid(static_cast<unsigned>(blocks), strips);
+                if (a.activation == PG_ACT_SILU) conv_kernel<H, W, WO, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, run, runs);
+                else conv_kernel<H, W, WO, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, run, runs);
+            });
+        });
+    });
+    return launch_status();
+}
+
+int pg_causal_conv_grad_workspace_bytes(const pg_conv_grad_args* args, size_t* bytes_out) {
+    if (!args || !bytes_out) return PG_ERR_INVALID;
+    const pg_conv_grad_args& a = *args;
+    const int rc = conv_check(a.dtype, a.activation, a.batch, a.sequences, a.length, a.channels, a.width);
+    if (rc != PG_OK) return rc;
+    const int run = conv_run(int64_t{a.batch} * a.sequences, a.length, (a.channels + 255) / 256);
+    *bytes_out = sizeof(float) * static_cast<size_t>(a.batch) * conv_parts(a, std::max(1, (a.length + run - 1) / run)) * (a.width + 1) * a.channels;
+    return PG_OK;
+}
+
+int pg_causal_conv_grad(const pg_conv_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const pg_conv_grad_args& a = *args;
+    size_t need = 0;
+    const int dev = current_device(), rc = pg_causal_conv_grad_workspace_bytes(args, &need);
+    if (rc != PG_OK) return rc;
+    const int64_t tokens = int64_t{a.sequences} * a.length, sequences = int64_t{a.batch} * a.sequences, held = sequences * (a.width - 1) * a.channels;
+    for (const pg_matrix* m : {&a.x, &a.dy})
+        if (!matrix_ok(*m, a.batch, tokens, a.channels, 2, false, dev)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.dx, a.batch, tokens, a.channels, 2, true, dev)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.weight, a.batch, a.channels, a.width, 4, false, dev)) return PG_ERR_INVALID;
+    if (a.dweight.data && !matrix_ok(a.dweight, a.batch, a.channels, a.width, 4, true, dev)) return PG_ERR_INVALID;
+    if (a.bias && !vector_ok(a.bias, a.bias_stride, a.batch, a.channels, false, dev)) return PG_ERR_INVALID;
+    if (a.dbias && !vector_ok(a.dbias, a.dbias_stride, a.batch, a.channels, true, dev)) return PG_ERR_INVALID;
+    if ((a.lengths && !array_ok(a.lengths, 4, sequences, dev)) || (a.state && !array_ok(a.state, 2, held, dev))) return PG_ERR_INVALID;
+    if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
+    if (a.batch == 0) return PG_OK;
+    const int strips = (a.channels + 255) / 256, run = conv_run(sequences, a.length, strips);
+    const int runs = std::max(1, (a.length + run - 1) / run), parts = conv_parts(a, runs);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    float* partial = static_cast<float*>(workspace);
+    Operands operands;
+    operands.output(a.dx, a.batch, tokens, a.channels, 2).output(a.dweight, a.batch, a.channels, a.width, 4).output(a.dbias, a.dbias_stride, a.batch, a.channels);
+    span(operands, workspace, need, true);
+    operands.input(a.x, a.batch, tokens, a.channels, 2).input(a.dy, a.batch, tokens, a.channels, 2).input(a.weight, a.batch, a.channels, a.width, 4);
+    operands.input(a.bias, a.bias_stride, a.batch, a.channels);
+    span(operands, a.lengths, sequences * 4, false);
+    span(operands, a.state, held * 2, false);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    with_kind(a.dtype, [&](auto h) {
+        with_widths(access_width({&a.x, &a.dy}, a.batch), access_width({&a.dx}, a.batch), [&](auto in, auto out) {
+            with_taps(a.width, [&](auto taps) {
+                using H = decltype(h);
+                constexpr int W = decltype(in)::value, WO = decltype(out)::value, TAPS = decltype(taps)::value;
+                const dim3 grid(a.batch * parts, strips);
+                if (a.activation == PG_ACT_SILU) conv_grad_kernel<H, W, WO, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
+                else conv_grad_kernel<H, W, WO, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
+            });
+        });
+    });
+    const int64_t size = int64_t{a.width + 1} * a.channels;
+    if (a.dweight.data)
+        sum_parts_kernel<<<dim3(static_cast<unsigned>((int64_t{a.channels} * a.width + 31) / 32), a.batch), 256, 0, st>>>(
+            partial, parts, size, a.channels, a.width, 1, a.channels, true, static_cast<float*>(a.dweight.data), a.dweight.ld, a.dweight.stride, a.accumulate);
+    if (a.dbias)
+        sum_parts_kernel<<<dim3((a.channels + 31) / 32, a.batch), 256, 0, st>>>(partial + int64_t{a.width} * a.channels, parts, size, 1, a.channels, 0, 1, false,
+                                                                                a.dbias, a.channels, a.dbias_stride, a.accumulate);
+    return launch_status();
+}
+
+int pg_selective_scan_workspace_bytes(const pg_scan_args* args, size_t* bytes_out) {
+    if (!args || !bytes_out) return PG_ERR_INVALID;
+    const pg_scan_args& a = *args;
+    const int rc = scan_check(a);
+    if (rc != PG_OK) return rc;
+    const ScanPlan p = scan_plan(a, lanes_of(a.states, 16));
+    *bytes_out = p.chunks > 1 ? sizeof(float) * static_cast<size_t>(a.batch) * a.sequences * p.chunks * a.channels * (a.states + 1) : 0;
+    return PG_OK;
+}
+
+int pg_selective_scan(const pg_scan_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const pg_scan_args& a = *args;
+    size_t need = 0;
+    const int dev = current_device(), rc = pg_selective_scan_workspace_bytes(args, &need);
+    if (rc != PG_OK) return rc;
+    const int64_t tokens = int64_t{a.sequences} * a.length, sequences = int64_t{a.batch} * a.sequences, held = sequences * a.channels * a.states;
+    if (!scan_inputs_ok(a, dev) || !matrix_ok(a.y, a.batch, tokens, a.channels, 2, true, dev)) return PG_ERR_INVALID;
+    if (a.state_out && !array_ok(a.state_out, 4, held, dev)) return PG_ERR_INVALID;
+    if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
+    const int lanes = lanes_of(a.states, 16);
+    const ScanPlan p = scan_plan(a, lanes);
+    if (sequences * p.chunks > kMaxBlocks) return PG_ERR_TOO_LARGE;
+    if (sequences == 0 || (a.length == 0 && !a.state_out)) return PG_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.y, a.batch, tokens, a.channels, 2);
+    span(operands, a.state_out, held * 4, true);
+    span(operands, need > 0 ? workspace : nullptr, need, true);
+    scan_inputs(operands, a);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    float* states = static_cast<float*>(workspace);
+    float* sums = states + sequences * p.chunks * a.channels * a.states;
+    with_kind(a.dtype, [&](auto h) {
+        using H = decltype(h);
+        auto launch = [&](auto per, auto lane) {
+            constexpr int P = decltype(per)::value, LANES = decltype(lane)::value;
+            const dim3 grid(static_cast<unsigned>(sequences * p.chunks), (a.channels + kScanThreads / LANES - 1) / (kScanThreads / LANES));
+            if (p.chunks > 1) {
+                scan_kernel<H, P, LANES, true><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks);
+                join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
+                    a.a, a.state, states, nullptr, sums, a.sequences, a.channels, a.states, p.chunks);
+            }
+            scan_kernel<H, P, LANES, false><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks);
+        };
+        using std::integral_constant;
+        if (a.states <= 8) launch(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        else if (lanes == 1) launch(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+        else if (lanes == 2) launch(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+        else launch(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    });
+    return launch_status();
+}
+
+int pg_selective_scan_grad_workspace_bytes(const pg_scan_grad_args* args, size_t* bytes_out) {
+    if (!args || !bytes_out) return PG_ERR_INVALID;
+    const int rc = scan_check(*args);
+    if (rc != PG_OK) return rc;
+    const GradPlan p = grad_plan(*args);
+    *bytes_out = 2 * p.states + p.sums + p.parts + p.partial;
+    return PG_OK;
+}
+
+int pg_selective_scan_grad(const pg_scan_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!args) return PG_ERR_INVALID;
+    const pg_scan_grad_args& a = *args;
+    size_t need = 0;
+    const int dev = current_device(), rc = pg_selective_scan_grad_workspace_bytes(args, &need);
+    if (rc != PG_OK) return rc;
+    const int64_t tokens = int64_t{a.sequences} * a.length, sequences = int64_t{a.batch} * a.sequences;
+    if (!scan_inputs_ok(a, dev) || !matrix_ok(a.dy, a.batch, tokens, a.channels, 2, false, dev)) return PG_ERR_INVALID;
+    for (const pg_matrix* m : {&a.du, &a.ddelta})
+        if (!matrix_ok(*m, a.batch, tokens, a.channels, 2, true, dev)) return PG_ERR_INVALID;
+    if (a.z.data && !matrix_ok(a.dz, a.batch, tokens, a.channels, 2, true, dev)) return PG_ERR_INVALID;
+    for (const pg_matrix* m : {&a.db, &a.dc})
+        if (!matrix_ok(*m, a.batch, tokens, a.states, 2, true, dev)) return PG_ERR_INVALID;
+    if (!matrix_ok(a.da, a.batch, a.channels, a.states, 4, true, dev)) return PG_ERR_INVALID;
+    if (a.dskip && !vector_ok(a.dskip, a.dskip_stride, a.batch, a.channels, true, dev)) return PG_ERR_INVALID;
+    if (a.ddelta_bias && !vector_ok(a.ddelta_bias, a.ddelta_bias_stride, a.batch, a.channels, true, dev)) return PG_ERR_INVALID;
+    if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
+    const GradPlan p = grad_plan(a);
+    if (sequences * p.chunks > kMaxBlocks || int64_t{a.batch} * p.shares > kMaxBlocks || p.parts / 256 > static_cast<size_t>(kMaxBlocks)) return PG_ERR_TOO_LARGE;
+    if (a.batch == 0) return PG_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Operands operands;
+    operands.output(a.du, a.batch, tokens, a.channels, 2).output(a.ddelta, a.batch, tokens, a.channels, 2).output(a.db, a.batch, tokens, a.states, 2);
+    operands.output(a.dc, a.batch, tokens, a.states, 2).output(a.da, a.batch, a.channels, a.states, 4);
+    if (a.z.data) operands.output(a.dz, a.batch, tokens, a.channels, 2);
+    operands.output(a.dskip, a.dskip_stride, a.batch, a.channels).output(a.ddelta_bias, a.ddelta_bias_stride, a.batch, a.channels);
+    span(operands, workspace, need, true);
+    operands.input(a.dy, a.batch, tokens, a.channels, 2);
+    scan_inputs(operands, a);
+    if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
+    char* at = static_cast<char*>(workspace);
+    float* states = reinterpret_cast<float*>(at);
+    float* carries = reinterpret_cast<float*>(at + p.states);
+    float* sums = reinterpret_cast<float*>(at + 2 * p.states);
+    float* parts = reinterpret_cast<float*>(at + 2 * p.states + p.sums);
+    float* partial = reinterpret_cast<float*>(at + 2 * p.states + p.sums + p.parts);
+    int status = PG_OK;
+    with_kind(a.dtype, [&](auto h) {
+        using H = decltype(h);
+        auto launch = [&](auto lane) {
+            constexpr int LANES = decltype(lane)::value;
+            if (p.chunks > 1 && sequences > 0) {
+                scan_grad_local_kernel<H, LANES><<<dim3(static_cast<unsigned>(sequences * p.chunks), static_cast<unsigned>(p.blocks)), kScanThreads, 0, st>>>(
+                    a, states, carries, sums, p.chunk, p.chunks);
+                join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
+                    a.a, a.state, states, carries, sums, a.sequences, a.channels, a.states, p.chunks);
+            }
+            const int groups = (p.chunk + kGroup - 1) / kGroup, n = kGradStates * LANES;
+            const size_t smem = sizeof(float) * (2 * groups * kGroup * n + groups * kGradStates * kScanThreads + kScanThreads / 32 * kGroup * 2 * n);
+            const auto kernel = scan_grad_kernel<H, LANES>;
+            if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
+                cudaGetLastError();
+                status = PG_ERR_CUDA;
+                return;
+            }
+            kernel<<<dim3(static_cast<unsigned>(a.batch * p.shares), static_cast<unsigned>(p.blocks)), kScanThreads, smem, st>>>(a, states, carries, parts, partial,
+                                                                                                                               p.chunk, p.chunks, p.shares);
+        };
+        using std::integral_constant;
+        if (p.lanes == 1) launch(integral_constant<int, 1>{});
+        else if (p.lanes == 2) launch(integral_constant<int, 2>{});
+        else if (p.lanes == 4) launch(integral_constant<int, 4>{});
+        else launch(integral_constant<int, 8>{});
+        const int n = kGradStates * p.lanes;
+        const int64_t all = a.batch * tokens * 2 * n;
+        if (all > 0) sum_bc_kernel<H><<<static_cast<unsigned>((all + 255) / 256), 256, 0, st>>>(a, parts, static_cast<int>(p.blocks), n);
+    });
+    if (status != PG_OK) return status;
+    const int64_t row = a.states + 2, size = row * a.channels;
+    sum_parts_kernel<<<dim3(static_cast<unsigned>((int64_t{a.channels} * a.states + 31) / 32), a.batch), 256, 0, st>>>(
+        partial, p.shares, size, a.channels, a.states, row, 1, false, static_cast<float*>(a.da.data), a.da.ld, a.da.stride, a.accumulate);
+    for (int i = 0; i < 2; ++i) {
+        float* out = i ? a.ddelta_bias : a.dskip;
+        if (out)
+            sum_parts_kernel<<<dim3((a.channels + 31) / 32, a.batch), 256, 0, st>>>(partial + a.states + i, p.shares, size, 1, a.channels, 0, row, false, out, a.channels,
+                                                                                    i ? a.ddelta_bias_stride : a.dskip_stride, a.accumulate);
+    }
+    return launch_status();
+}
+
+}  // extern "C"
