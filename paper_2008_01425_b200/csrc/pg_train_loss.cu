@@ -1,9 +1,9 @@
 // The distillation loss (pg_distillation_loss): softmax statistics of every row of logits and what a teacher's top
 // logits and a label make of them, forward, backward, and both with one read of the logits.
 //
-// One block has one row.  With k = log2(e) / tau a logit x counts 2^(k x - r), r a whole number, the row's largest k x
-// rounded up: k x - r is then one fused multiply-add, and a thread whose r grows corrects its sums by an
-// exact power of two.  Where tau is 1, 2 or 4 the exponentials at temperature 1 are powers of these; elsewhere there
+// One block has one row.  With k = log2(e) / tau a logit x counts 2^(k x - r), r a whole number near the largest k x that a thread
+// has seen: k x - r is then one fused multiply-add, and sums of different r are joined by exact powers of two.  A thread's r is that of its
+// first logits, and grows when one is kSlack above it: fp32 has room for what is between.  Where tau is 1, 2 or 4 the exponentials at temperature 1 are powers of these; elsewhere there
 // are two per logit.  With the gradient the row stays in shared memory as it was read, so the logits are read once.
 // Memory bounds all of it: 2 bytes a logit for the loss, 4 with the gradient.
 #include <algorithm>
@@ -14,8 +14,10 @@
 namespace pgt {
 namespace {
 
+constexpr int kWide = 256;                              // threads of the widest rows
 constexpr int kMaxTop = 1024;                          // entries of a teacher's list
 constexpr float kNoLogit = -1e30f;                     // r before the first logit; 2^(kNoLogit - r) is 0
+constexpr float kSlack = 20.0f;                        // (of the fourth power, 2^80 and a sum of as many as there are)
 constexpr size_t kMaxRowBytes = 200 * 1024;            // of a block's shared memory
 
 __device__ __forceinline__ float ex2(float v) {
@@ -29,37 +31,48 @@ __device__ __forceinline__ F2 ex2(F2 v) {
     return pair(ex2(a), ex2(b));
 }
 
+// v rounded to a whole number, by adding and taking off 1.5 * 2^23 (a number too large for that is one).
+__device__ __forceinline__ float whole(float v) { return fabsf(v) < 4194304.0f ? (v + kRound) - kRound : v; }
+
 // What a block knows of its row.  Logits lie in 16-byte pieces of memory: piece j holds elements 8 j - off to 8 j - off + 7.
 struct Row {
     const uint16_t* x;
-    int off, classes, pieces;
+    int off, classes, pieces, first, last;             // first to last - 1: pieces that lie in the row whole
     __device__ Row(const pg_matrix& m, int64_t b, int64_t t, int n) {
         x = static_cast<const uint16_t*>(m.data) + b * m.stride + t * m.ld;
         off = static_cast<int>(reinterpret_cast<uintptr_t>(x) & 15) / 2;
         classes = n;
         pieces = (off + n + 7) / 8;
+        first = off > 0;
+        last = (off + n) / 8;
     }
+    __device__ const uint4* at(int j) const { return reinterpret_cast<const uint4*>(x - off) + j; }
     __device__ uint4 piece(int j) const {              // (every piece holds an element of the row)
-        const uint4* p = reinterpret_cast<const uint4*>(x - off) + j;
+        const uint4* p = at(j);
         return PGT_READ(p, 16) ? *p : make_uint4(0, 0, 0, 0);
     }
 };
 
-// fp32 values of an octet whose first element has index `at`; -inf where there is no element.
+// fp32 values of an octet; -inf in place of those that are not in the row, whose first has index `at` in it.
 template <typename H>
-__device__ __forceinline__ void logits_of(const uint4& p, int at, int classes, F2 (&v)[4]) {
+__device__ __forceinline__ void logits_of(const uint4& p, F2 (&v)[4]) {
     const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = Elem<H>::up2(w[i]);
-    if (at < 0 || at + 8 > classes) {
-        const float none = __int_as_float(0xff800000);
+}
+__device__ __forceinline__ void only_row(F2 (&v)[4], int at, int classes) {
+    const float none = __int_as_float(0xff800000);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float a, b;
-            split(v[i], a, b);
-            v[i] = pair(at + 2 * i >= 0 && at + 2 * i < classes ? a : none, at + 2 * i + 1 >= 0 && at + 2 * i + 1 < classes ? b : none);
-        }
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        split(v[i], a, b);
+        v[i] = pair(at + 2 * i >= 0 && at + 2 * i < classes ? a : none, at + 2 * i + 1 >= 0 && at + 2 * i + 1 < classes ? b : none);
     }
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 // POWER: exponentials at temperature 1 are those at tau to this power (1, 2, 4); 0: they are computed on their own.
@@ -74,71 +87,70 @@ __device__ __forceinline__ F2 power(F2 e) {
     else if constexpr (POWER == 2) return mul(e, e);
     else return mul(mul(e, e), mul(e, e));
 }
-template <int POWER>
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
-    Sums c;
-    c.r = fmaxf(a.r, b.r);
-    const float fa = ex2(a.r - c.r), fb = ex2(b.r - c.r);
-    c.s = a.s * fa + b.s * fb;
+// The sums of N neighbouring lanes (of all of them the same), brought to the largest r.
+template <int POWER, int N>
+__device__ __forceinline__ Sums join(Sums m) {
+    auto over = [](float v, auto f) {
+#pragma unroll
+        for (int o = N / 2; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
+    };
+    auto most = [](float a, float b) { return fmaxf(a, b); };
+    auto add = [](float a, float b) { return a + b; };
+    const float r = over(m.r, most), f = ex2(m.r - r);
+    m.s = over(m.s * f, add);
     if constexpr (POWER == 0) {
-        c.r1 = fmaxf(a.r1, b.r1);
-        c.s1 = a.s1 * ex2(a.r1 - c.r1) + b.s1 * ex2(b.r1 - c.r1);
+        const float r1 = over(m.r1, most);
+        m.s1 = over(m.s1 * ex2(m.r1 - r1), add);
+        m.r1 = r1;
     } else {
-        c.r1 = POWER * c.r;
-        c.s1 = POWER == 1 ? c.s : a.s1 * ex2(POWER * (a.r - c.r)) + b.s1 * ex2(POWER * (b.r - c.r));
+        float f1 = f;
+        if constexpr (POWER > 1) f1 *= f1;
+        if constexpr (POWER > 2) f1 *= f1;
+        m.s1 = POWER == 1 ? m.s : over(m.s1 * f1, add);
+        m.r1 = POWER * r;
     }
-    return c;
-}
-template <int POWER, int T>
-__device__ __forceinline__ Sums join_block(Sums m, Sums* shared) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Sums other;
-        other.r = __shfl_xor_sync(0xffffffffu, m.r, o);
-        other.s = __shfl_xor_sync(0xffffffffu, m.s, o);
-        other.r1 = POWER == 0 ? __shfl_xor_sync(0xffffffffu, m.r1, o) : 0.0f;
-        other.s1 = POWER == 1 ? 0.0f : __shfl_xor_sync(0xffffffffu, m.s1, o);
-        m = join<POWER>(m, other);
-    }
-    if constexpr (T > 32) {
-        if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
-        __syncthreads();
-        m = shared[0];
-#pragma unroll
-        for (int w = 1; w < T / 32; ++w) m = join<POWER>(m, shared[w]);
-    }
+    m.r = r;
     return m;
 }
-// An octet is counted in: its largest value first, then its exponentials.
+// A warp's sums go to shared memory; after the block's barrier every warp adds them up, in the same order.
+template <int POWER>
+__device__ __forceinline__ void join_warp(const Sums& m, Sums* shared) {
+    const Sums all = join<POWER, 32>(m);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = all;
+}
+template <int POWER, int WARPS>
+__device__ __forceinline__ Sums all_sums(const Sums* shared) {
+    return join<POWER, WARPS>(shared[threadIdx.x & (WARPS - 1)]);
+}
+
+// An octet is counted in.
 template <int POWER>
 __device__ __forceinline__ void count(Sums& m, F2& s, F2& s1, const F2 (&v)[4], float k) {
-    float top = __int_as_float(0xff800000);
+    float e[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a, b;
-        split(v[i], a, b);
-        top = fmaxf(top, fmaxf(a, b));
-    }
-    const float r = ceilf(top * k);
-    if (r > m.r) {
-        const float f = ex2(m.r - r);
+    for (int i = 0; i < 4; ++i) split(v[i], e[2 * i], e[2 * i + 1]);
+    const float top = max3(max3(max3(e[0], e[1], e[2]), e[3], e[4]), max3(e[5], e[6], e[7]), e[0]);
+    if (top * k > m.r + kSlack) {
+        const float r = whole(top * k), f = ex2(m.r - r);
         s = mul(s, both(f));
         if constexpr (POWER > 1) s1 = mul(s1, power<POWER>(both(f)));
         m.r = r;
     }
     if constexpr (POWER == 0) {
-        const float r1 = ceilf(top * kLog2e);
-        if (r1 > m.r1) {
+        if (top * kLog2e > m.r1 + kSlack) {
+            const float r1 = whole(top * kLog2e);
             s1 = mul(s1, both(ex2(m.r1 - r1)));
             m.r1 = r1;
         }
     }
+    const F2 minus = both(-m.r), minus1 = both(-m.r1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const F2 e = ex2(fma(v[i], both(k), both(-m.r)));
-        s = add(s, e);
-        if constexpr (POWER > 1) s1 = add(s1, power<POWER>(e));
-        if constexpr (POWER == 0) s1 = add(s1, ex2(fma(v[i], both(kLog2e), both(-m.r1))));
+        const F2 x = ex2(fma(v[i], both(k), minus));
+        s = add(s, x);
+        if constexpr (POWER > 1) s1 = add(s1, power<POWER>(x));
+        if constexpr (POWER == 0) s1 = add(s1, ex2(fma(v[i], both(kLog2e), minus1)));
     }
 }
 
@@ -147,7 +159,7 @@ struct List {
     int* id;
     float *p, *log_p, *x;
 };
-// By the first warp.  Returns whether the list has an entry that counts: its id is a class and its logit not -inf.
+// By one warp.  Returns whether the list has an entry that counts: its id is a class and its logit not -inf.
 template <typename H>
 __device__ __forceinline__ bool read_list(const pg_distillation_args& a, const Row& row, int64_t b, int64_t t, const List& list, float k) {
     const float none = __int_as_float(0xff800000);
@@ -166,7 +178,7 @@ __device__ __forceinline__ bool read_list(const pg_distillation_args& a, const R
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float r = fmaxf(ceilf(top * k), kNoLogit);
+    const float r = fmaxf(whole(top * k), kNoLogit);
     float sum = 0.0f;
     for (int i = lane; i < a.top; i += 32) {
         const float v = fmaf(list.log_p[i], k, -r), e = ex2(v);
@@ -185,31 +197,308 @@ __device__ __forceinline__ bool read_list(const pg_distillation_args& a, const R
     return any;
 }
 
-// FORWARD: loss and lse.  BOTH: the gradient too, from the row as it was kept in shared memory; AGAIN: the same for rows
-// that shared memory does not hold, which are read twice.  BACKWARD: the gradient from lse, a row by gridDim.z blocks.
+// A row's constants on the way back: the gradient of a logit x is
+//     by 2^(k x - r) + by1 2^(k1 x - r1),  less what list and label take off at their classes.
+template <int POWER>
+struct Slope {
+    float k, r, r1, by, by1;
+    __device__ F2 exponential(F2 x) const { return ex2(fma(x, both(k), both(-r))); }
+    __device__ F2 exponential1(F2 x, F2 e) const {
+        if constexpr (POWER == 0) return ex2(fma(x, both(kLog2e), both(-r1)));
+        else return power<POWER>(e);
+    }
+    template <typename H>
+    __device__ void apply(F2 (&v)[4], uint32_t (&w)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const F2 e = exponential(v[i]);
+            if constexpr (POWER == 1) v[i] = mul(e, both(by + by1));
+            else if constexpr (POWER == 2) v[i] = mul(e, fma(e, both(by1), both(by)));
+            else v[i] = fma(exponential1(v[i], e), both(by1), mul(e, both(by)));
+            w[i] = Elem<H>::down2(v[i]);
+        }
+    }
+};
+struct Out {                                           // a row of the gradient, in pieces as Row's
+    uint16_t* x;
+    int off, classes, pieces, first, last;
+    __device__ Out(const pg_matrix& m, int64_t b, int64_t t, int n) {
+        x = static_cast<uint16_t*>(m.data) + b * m.stride + t * m.ld;
+        off = static_cast<int>(reinterpret_cast<uintptr_t>(x) & 15) / 2;
+        classes = n;
+        pieces = (off + n + 7) / 8;
+        first = off > 0;
+        last = (off + n) / 8;
+    }
+    __device__ void store(int j, const uint32_t (&w)[4]) const { PGT_STORE(*reinterpret_cast<uint4*>(x + 8 * j - off), make_uint4(w[0], w[1], w[2], w[3])); }
+    __device__ void store_part(int j, const uint32_t (&w)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = 8 * j - off + i;
+            if (at >= 0 && at < classes) PGT_STORE(x[at], static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu));
+        }
+    }
+};
+// Piece j of the output, from the input's pieces (read(i): its i-th, zeros outside), whose rows start `shift` elements later in theirs.
+template <typename F>
+__device__ __forceinline__ uint4 moved(F&& read, int j, int shift) {
+    if (shift == 0) return read(j);
+    const int from = shift < 0 ? j - 1 : j;
+    const Oct o = cut(read(from), read(from + 1), shift & 7);
+    return make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
+}
+
+// The label and what it weighs.
+template <typename H>
+struct Label {
+    int at;
+    bool is;
+    float x;
+    __device__ Label(const pg_distillation_args& a, const Row& row, int64_t at_row, float hard) {
+        at = a.labels ? PGT_LOAD(a.labels[at_row]) : -1;
+        is = hard != 0.0f && at >= 0 && at < a.classes;
+        x = is ? Elem<H>::up(PGT_LOAD(row.x[at])) : 0.0f;
+    }
+};
+
+// The classes of the list and the label once more, with what the formula takes off there, by threads `at`, at + step, ..; classes from
+// `from` to `to` - 1 only.  A class that is listed twice is computed twice, from the same sum.
+template <typename H, int POWER>
+__device__ __forceinline__ void take_off(const Out& out, const List& list, int top, const Label<H>& label, const Slope<POWER>& slope, const Sums& m, bool soft,
+                                         float to_soft, float to_hard, int at, int step, int from, int to) {
+    const int entries = to_soft != 0.0f ? top : 0;
+    for (int i = at; i <= entries; i += step) {
+        if (i == entries && !label.is) break;
+        const int id = i < entries ? list.id[i] : label.at;
+        if (id < 0 || id < from || id >= to) continue;
+        float p = 0.0f;
+        for (int j = 0; j < entries; ++j) p += list.id[j] == id ? list.p[j] : 0.0f;
+        const F2 x = both(i < entries ? list.x[i] : label.x), e = slope.exponential(x), e1 = slope.exponential1(x, e);
+        float q, q1, same;
+        split(e, q, same);
+        split(e1, q1, same);
+        // (with the label's term only k belongs to that)
+        const float v = to_soft * (q / m.s - p) + to_hard * ((soft ? q1 : q) / m.s1 - (label.is && id == label.at ? 1.0f : 0.0f));
+        PGT_STORE(out.x[id], Elem<H>::down(v));
+    }
+}
+
+// Loss and log-sum-exps of a row, by one warp, from the row's sums.
+template <typename H, int POWER>
+__device__ __forceinline__ void store_loss(const pg_distillation_args& a, int64_t at_row, const List& list, const Label<H>& label, const Sums& m, float k, float soft,
+                                           float hard) {
+    const int lane = threadIdx.x & 31;
+    const float log_s = log2f(m.s), log_s1 = POWER == 1 ? log_s : log2f(m.s1), k1 = POWER == 0 ? kLog2e : POWER * k;
+    float loss = 0.0f;                                 // in bits
+    if (soft != 0.0f) {
+        for (int i = lane; i < a.top; i += 32) {
+            const float p = list.p[i];
+            if (p != 0.0f) loss += p * (list.log_p[i] - (fmaf(list.x[i], k, -m.r) - log_s));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+        loss *= soft * (kLog2e / k) * (kLog2e / k);
+    }
+    if (label.is) loss += hard * (log_s1 - fmaf(label.x, k1, -m.r1));
+    if (lane == 0) {
+        if (a.loss) PGT_STORE(a.loss[at_row], loss * kLn2);
+        if (a.lse) {
+            PGT_STORE(a.lse[2 * at_row], hard != 0.0f ? (m.r1 + log_s1) * kLn2 : 0.0f);
+            PGT_STORE(a.lse[2 * at_row + 1], soft != 0.0f ? (m.r + log_s) * kLn2 : 0.0f);
+        }
+    }
+}
+template <int ID>
+__device__ __forceinline__ void bar_sync(int threads) { asm volatile("bar.sync %0, %1;" ::"n"(ID), "r"(threads) : "memory"); }
+template <int ID>
+__device__ __forceinline__ void bar_arrive(int threads) { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "r"(threads) : "memory"); }
+__device__ __forceinline__ void copy16(void* shared, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Loss, and with GRAD the gradient too, of rows blockIdx.x, blockIdx.x + gridDim.x, ..  The row lies in shared memory, piece j the
+// business of thread j mod T alone: as soon as a thread has used a piece for the last time it asks for the same piece of the block's next row, so
+// that memory works while the exponentials do.  One more warp reads the teacher's list of the next row meanwhile (three dependent
+// trips to memory), computes the loss and corrects the gradient at the list's classes.
+// Per row: every thread's sums are there and the list is (barrier 1, all); the gradient is stored (barrier 2, which the list's warp waits at).
+// Sums and lists have two places each, the next row's being written while slower warps still read this one's.
+template <typename H, int POWER, int T, bool GRAD>
+__global__ void __launch_bounds__(T + 32, T == kWide ? 4 : T == 128 ? 7 : 14)
+distillation_kernel(const pg_distillation_args a, float k, float soft, float hard) {
+    extern __shared__ __align__(16) uint4 s_row[];     // the row's pieces, then two lists
+    __shared__ Sums s_sums[2][T / 32];
+    __shared__ bool s_any[2];
+    const int64_t rows = int64_t{a.batch} * a.tokens;
+    float* words = reinterpret_cast<float*>(s_row + (a.classes + 14) / 8);
+    auto list_of = [&](int which) {
+        float* w = words + 4 * a.top * which;
+        return List{reinterpret_cast<int*>(w), w + a.top, w + 2 * a.top, w + 3 * a.top};
+    };
+    auto row_of = [&](int64_t at) { return Row(a.logits, at / a.tokens, at % a.tokens, a.classes); };
+    int flip = 0;
+    if (threadIdx.x >= T) {                            // the list's warp
+        auto read = [&](int64_t at, int which) {
+            if (soft == 0.0f || at >= rows) return;
+            const bool any = read_list<H>(a, row_of(at), at / a.tokens, at % a.tokens, list_of(which), k);
+            if (threadIdx.x == T) s_any[which] = any;
+            __syncwarp();
+        };
+        read(blockIdx.x, 0);
+        for (int64_t at = blockIdx.x; at < rows; at += gridDim.x, flip ^= 1) {
+            const Label<H> label(a, row_of(at), at, hard);
+            const float g = GRAD && a.dloss ? PGT_LOAD(a.dloss[at]) : 1.0f;
+            bar_sync<1>(T + 32);
+            const Sums m = all_sums<POWER, T / 32>(s_sums[flip]);
+            const List list = list_of(flip);
+            store_loss<H, POWER>(a, at, list, label, m, k, soft, hard);
+            read(at + gridDim.x, flip ^ 1);
+            if constexpr (GRAD) {
+                const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
+                bar_sync<2>(T + 32);
+                const Slope<POWER> slope = {k, m.r, m.r1, 0.0f, 0.0f};
+                take_off<H, POWER>(Out(a.dlogits, at / a.tokens, at % a.tokens, a.classes), list, a.top, label, slope, m, soft != 0.0f, to_soft, to_hard,
+                                   threadIdx.x - T, 32, 0, a.classes);
+            }
+        }
+        return;
+    }
+    const uint4* from = nullptr;                       // piece threadIdx.x of the next row, which has `pieces`
+    int pieces = 0;
+    auto ask = [&](int j) {
+        if (j < pieces && PGT_READ(from + (j - static_cast<int>(threadIdx.x)), 16)) copy16(s_row + j, from + (j - static_cast<int>(threadIdx.x)));
+    };
+    // This thread's pieces of a row: f(j) for those that are the row's whole, part(j) for the first and the last if they are not.
+    auto walk = [&](const auto& row, auto&& f, auto&& part) {
+        int j = threadIdx.x;
+        if (j < row.first) {
+            part(j);
+            j += T;
+        }
+#pragma unroll 2
+        for (; j < row.last; j += T) f(j);
+        if (j < row.pieces) part(j);
+    };
+    {
+        const Row row = row_of(blockIdx.x);
+        from = row.at(threadIdx.x);
+        pieces = row.pieces;
+        for (int j = threadIdx.x; j < pieces; j += T) ask(j);
+    }
+    for (int64_t at = blockIdx.x; at < rows; at += gridDim.x, flip ^= 1) {
+        const Row row = row_of(at);
+        const bool more = at + gridDim.x < rows;
+        const Row next = row_of(more ? at + gridDim.x : at);
+        from = next.at(threadIdx.x);
+        pieces = more ? next.pieces : 0;
+        float g = 1.0f;
+        int label = -1;
+        if constexpr (GRAD) {
+            if (a.dloss) g = PGT_LOAD(a.dloss[at]);
+            if (a.labels && hard != 0.0f) label = PGT_LOAD(a.labels[at]);
+        }
+        Sums m = {kNoLogit, 0.0f, kNoLogit, 0.0f};
+        F2 s = both(0.0f), s1 = both(0.0f);
+        copies_wait();
+        walk(
+            row,
+            [&](int j) {
+                F2 v[4];
+                logits_of<H>(s_row[j], v);
+                count<POWER>(m, s, s1, v, k);
+                if constexpr (!GRAD) ask(j);
+            },
+            [&](int j) {
+                F2 v[4];
+                logits_of<H>(s_row[j], v);
+                only_row(v, 8 * j - row.off, a.classes);
+                count<POWER>(m, s, s1, v, k);
+                if constexpr (!GRAD) ask(j);
+            });
+        m.s = sum2(s);
+        m.s1 = POWER == 1 ? 0.0f : sum2(s1);
+        join_warp<POWER>(m, s_sums[flip]);
+        bar_sync<1>(T + 32);
+        const int rest = row.pieces + (static_cast<int>(threadIdx.x) - row.pieces % T + T) % T;      // this thread's first piece behind the row's
+        if constexpr (GRAD) {
+            m = all_sums<POWER, T / 32>(s_sums[flip]);
+            const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label >= 0 && label < a.classes ? g * hard : 0.0f;
+            const Slope<POWER> slope = {k, m.r, m.r1, to_soft / m.s, to_hard / m.s1};
+            const Out out(a.dlogits, at / a.tokens, at % a.tokens, a.classes);
+            const int shift = row.off - out.off;
+            if (shift == 0) {
+                walk(
+                    row,
+                    [&](int j) {
+                        F2 v[4];
+                        uint32_t w[4];
+                        logits_of<H>(s_row[j], v);
+                        slope.template apply<H>(v, w);
+                        out.store(j, w);
+                        ask(j);
+                    },
+                    [&](int j) {
+                        F2 v[4];
+                        uint32_t w[4];
+                        logits_of<H>(s_row[j], v);
+                        slope.template apply<H>(v, w);
+                        out.store_part(j, w);
+                        ask(j);
+                    });
+                for (int j = rest; j < pieces; j += T) ask(j);
+            } else {
+                auto read = [&](int j) { return j < 0 || j >= row.pieces ? make_uint4(0, 0, 0, 0) : s_row[j]; };
+                auto piece = [&](int j, uint32_t (&w)[4]) {
+                    F2 v[4];
+                    logits_of<H>(moved(read, j, shift), v);
+                    slope.template apply<H>(v, w);
+                };
+                walk(
+                    out,
+                    [&](int j) {
+                        uint32_t w[4];
+                        piece(j, w);
+                        out.store(j, w);
+                    },
+                    [&](int j) {
+                        uint32_t w[4];
+                        piece(j, w);
+                        out.store_part(j, w);
+                    });
+                bar_sync<3>(T);                        // others have read this thread's pieces, too
+                for (int j = threadIdx.x; j < pieces; j += T) ask(j);
+            }
+            __threadfence_block();
+            bar_arrive<2>(T + 32);
+        } else {
+            for (int j = rest; j < pieces; j += T) ask(j);
+        }
+    }
+}
+
+// Rows that shared memory does not hold: read twice (AGAIN), or with lse known once (BACKWARD), a row then by gridDim.z blocks.
 enum { FORWARD, BOTH, AGAIN, BACKWARD };
 template <typename H, int POWER, int T, int MODE>
-__global__ void __launch_bounds__(T, T == 512 ? 3 : 1)
-distillation_kernel(const pg_distillation_args a, float k, float soft, float hard) {
-    extern __shared__ __align__(16) uint4 s_row[];     // the row's pieces (BOTH), then the list
+__global__ void __launch_bounds__(T + 32, T == kWide ? 5 : 1)
+distillation_stream_kernel(const pg_distillation_args a, float k, float soft, float hard) {
+    extern __shared__ __align__(16) float s_list[];
     __shared__ Sums s_sums[T / 32];
     __shared__ bool s_any;
     const int64_t b = blockIdx.y, t = blockIdx.x, at_row = b * a.tokens + t;
     const Row row(a.logits, b, t, a.classes);
-    float* words = reinterpret_cast<float*>(s_row + (MODE == BOTH ? (a.classes + 14) / 8 : 0));
-    const List list = {reinterpret_cast<int*>(words), words + a.top, words + 2 * a.top, words + 3 * a.top};
-    const int label = a.labels ? PGT_LOAD(a.labels[at_row]) : -1;
-    const bool labelled = hard != 0.0f && label >= 0 && label < a.classes;
-    const float x_label = labelled ? Elem<H>::up(PGT_LOAD(row.x[label])) : 0.0f;
-    if (soft != 0.0f && threadIdx.x < 32) {
-        const bool any = read_list<H>(a, row, b, t, list, k);
-        if (threadIdx.x == 0) s_any = any;
-    }
+    const List list = {reinterpret_cast<int*>(s_list), s_list + a.top, s_list + 2 * a.top, s_list + 3 * a.top};
+    const Label<H> label(a, row, at_row, hard);
     const float g = a.dloss ? PGT_LOAD(a.dloss[at_row]) : 1.0f;
+    const bool lists = threadIdx.x >= T;
+    constexpr int U = 4;                               // pieces on their way at once
     Sums m = {kNoLogit, 0.0f, kNoLogit, 0.0f};
-    if constexpr (MODE != BACKWARD) {
+    if (lists) {
+        if (soft != 0.0f) {
+            const bool any = read_list<H>(a, row, b, t, list, k);
+            if (threadIdx.x == T) s_any = any;
+        }
+    } else if constexpr (MODE == AGAIN) {
         F2 s = both(0.0f), s1 = both(0.0f);
-        constexpr int U = 4;                           // pieces on their way at once
         for (int j0 = threadIdx.x; j0 < row.pieces; j0 += U * T) {
             uint4 p[U];
 #pragma unroll
@@ -217,123 +506,57 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * T;
-                if (j >= row.pieces) break;
-                if constexpr (MODE == BOTH) s_row[j] = p[u];
-                F2 v[4];
-                logits_of<H>(p[u], 8 * j - row.off, a.classes, v);
-                count<POWER>(m, s, s1, v, k);
+                if (j < row.pieces) {
+                    F2 v[4];
+                    logits_of<H>(p[u], v);
+                    if (j < row.first || j >= row.last) only_row(v, 8 * j - row.off, a.classes);
+                    count<POWER>(m, s, s1, v, k);
+                }
             }
         }
         m.s = sum2(s);
         m.s1 = POWER == 1 ? 0.0f : sum2(s1);
-        m = join_block<POWER, T>(m, s_sums);
-        if constexpr (POWER == 1) m.s1 = m.s;
-        if constexpr (POWER != 0) m.r1 = POWER * m.r;
-        if (threadIdx.x < 32) {
-            const float log_s = log2f(m.s), log_s1 = POWER == 1 ? log_s : log2f(m.s1), k1 = POWER == 0 ? kLog2e : POWER * k;
-            float loss = 0.0f;                         // in bits
-            if (soft != 0.0f) {
-                __syncwarp();
-                for (int i = threadIdx.x; i < a.top; i += 32) {
-                    const float p = list.p[i];
-                    if (p != 0.0f) loss += p * (list.log_p[i] - (fmaf(list.x[i], k, -m.r) - log_s));
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-                loss *= soft * (kLog2e / k) * (kLog2e / k);
-            }
-            if (labelled) loss += hard * (log_s1 - fmaf(x_label, k1, -m.r1));
-            if (threadIdx.x == 0) {
-                if (a.loss) PGT_STORE(a.loss[at_row], loss * kLn2);
-                if (a.lse) {
-                    PGT_STORE(a.lse[2 * at_row], hard != 0.0f ? (m.r1 + log_s1) * kLn2 : 0.0f);
-                    PGT_STORE(a.lse[2 * at_row + 1], soft != 0.0f ? (m.r + log_s) * kLn2 : 0.0f);
-                }
-            }
-        }
-        if constexpr (MODE == FORWARD) return;
+        join_warp<POWER>(m, s_sums);
+    }
+    __syncthreads();
+    if constexpr (MODE == AGAIN) {
+        m = all_sums<POWER, T / 32>(s_sums);
+        if (lists) store_loss<H, POWER>(a, at_row, list, label, m, k, soft, hard);
+        if (!a.dlogits.data) return;
     } else {
         // 2^(k x - r) is the softmax at k as it is; of its power at temperature 1, 1 / s1 is
-        const float lse1 = a.lse ? PGT_LOAD(a.lse[2 * at_row]) * kLog2e : 0.0f, lse = a.lse ? PGT_LOAD(a.lse[2 * at_row + 1]) * kLog2e : 0.0f;
+        const float lse1 = PGT_LOAD(a.lse[2 * at_row]) * kLog2e, lse = PGT_LOAD(a.lse[2 * at_row + 1]) * kLog2e;
         m.r = soft != 0.0f ? lse : lse1;
         m.r1 = POWER == 0 ? lse1 : POWER * m.r;
         m.s = 1.0f;
         m.s1 = POWER == 0 ? 1.0f : ex2(lse1 - m.r1);
     }
-    if constexpr (MODE == BACKWARD) __syncthreads();                   // the list
-    const float to_soft = soft != 0.0f && s_any ? g * soft * (kLog2e / k) : 0.0f, to_hard = labelled ? g * hard : 0.0f;
-    const float by = to_soft / m.s, by1 = to_hard / m.s1;
-    uint16_t* out = static_cast<uint16_t*>(a.dlogits.data) + b * a.dlogits.stride + t * a.dlogits.ld;
-    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(out) & 15) / 2, pieces = (off + a.classes + 7) / 8;
-    const int share = (pieces + gridDim.z - 1) / gridDim.z, first = blockIdx.z * share, last = min(pieces, first + share);
-    auto exponential = [&](F2 x) { return ex2(fma(x, both(k), both(-m.r))); };
-    auto exponential1 = [&](F2 x, F2 e) {
-        if constexpr (POWER == 0) return ex2(fma(x, both(kLog2e), both(-m.r1)));
-        else return power<POWER>(e);
-    };
-    auto read = [&](int j) {
-        if (j < 0 || j >= row.pieces) return make_uint4(0, 0, 0, 0);
-        if constexpr (MODE == BOTH) return s_row[j];
-        else return row.piece(j);
-    };
-    auto gradient = [&](uint4 p, int j) {
-        F2 v[4];
-        const int at = 8 * j - off;
-        logits_of<H>(p, at, a.classes, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const F2 e = exponential(v[i]);
-            if constexpr (POWER == 1) v[i] = mul(e, both(by + by1));
-            else if constexpr (POWER == 2) v[i] = mul(e, fma(e, both(by1), both(by)));
-            else v[i] = fma(exponential1(v[i], e), both(by1), mul(e, both(by)));
-        }
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = Elem<H>::down2(v[i]);
-        if (at >= 0 && at + 8 <= a.classes) {
-            PGT_STORE(*reinterpret_cast<uint4*>(out + at), make_uint4(w[0], w[1], w[2], w[3]));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (at + i >= 0 && at + i < a.classes) PGT_STORE(out[at + i], static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu));
-        }
-    };
-    const int shift = row.off - off;                   // elements from an input's piece to the output's
-    if (shift == 0) {
-        constexpr int U = 4;
+    const float to_soft = soft != 0.0f && s_any ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
+    const Slope<POWER> slope = {k, m.r, m.r1, to_soft / m.s, to_hard / m.s1};
+    const Out out(a.dlogits, b, t, a.classes);
+    const int share = (out.pieces + gridDim.z - 1) / gridDim.z, first = blockIdx.z * share, last = min(out.pieces, first + share);
+    const int shift = row.off - out.off;
+    auto read = [&](int j) { return j < 0 || j >= row.pieces ? make_uint4(0, 0, 0, 0) : row.piece(j); };
+    if (!lists)
         for (int j0 = first + threadIdx.x; j0 < last; j0 += U * T) {
             uint4 p[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) p[u] = read(j0 + u * T);
+            for (int u = 0; u < U; ++u) p[u] = j0 + u * T < last ? moved(read, j0 + u * T, shift) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (j0 + u * T < last) gradient(p[u], j0 + u * T);
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * T;
+                if (j < last) {
+                    F2 v[4];
+                    uint32_t w[4];
+                    logits_of<H>(p[u], v);
+                    slope.template apply<H>(v, w);
+                    if (j >= out.first && j < out.last) out.store(j, w);
+                    else out.store_part(j, w);
+                }
+            }
         }
-    } else {
-        for (int j = first + threadIdx.x; j < last; j += T) {
-            const int from = shift < 0 ? j - 1 : j;
-            const Oct o = cut(read(from), read(from + 1), shift & 7);
-            gradient(make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]), j);
-        }
-    }
-    // The classes of the list and the label once more, with what the formula takes off there.  A class that is listed twice is
-    // computed twice, from the same sum.
     __syncthreads();
-    const int entries = to_soft != 0.0f ? a.top : 0;
-    for (int i = threadIdx.x; i <= entries; i += T) {
-        if (i == entries && !labelled) break;
-        const int id = i < entries ? list.id[i] : label;
-        if (id < 0 || id < 8 * first - off || id >= 8 * last - off) continue;
-        float p = 0.0f;
-        for (int j = 0; j < entries; ++j) p += list.id[j] == id ? list.p[j] : 0.0f;
-        const F2 x = both(i < entries ? list.x[i] : x_label), e = exponential(x), e1 = exponential1(x, e);
-        float q, q1, same;
-        split(e, q, same);
-        split(e1, q1, same);
-        // (with the label's term only k belongs to that)
-        const float v = to_soft * (q / m.s - p) + to_hard * ((soft != 0.0f ? q1 : q) / m.s1 - (labelled && id == label ? 1.0f : 0.0f));
-        PGT_STORE(out[id], Elem<H>::down(v));
-    }
+    take_off<H, POWER>(out, list, a.top, label, slope, m, soft != 0.0f, to_soft, to_hard, threadIdx.x, T + 32, 8 * first - out.off, 8 * last - out.off);
 }
 
 int current_device() {
@@ -341,13 +564,13 @@ int current_device() {
     return cudaGetDevice(&d) == cudaSuccess ? d : -1;
 }
 
-// Threads of a row: a warp to 1024 classes, four to 8192, sixteen above.
+// Threads of a row: a warp to 1024 classes, four to 8192, eight above.
 template <typename F>
 void with_threads(int classes, F&& f) {
     using std::integral_constant;
     if (classes <= 1024) f(integral_constant<int, 32>{});
     else if (classes <= 8192) f(integral_constant<int, 128>{});
-    else f(integral_constant<int, 512>{});
+    else f(integral_constant<int, kWide>{});
 }
 
 int distillation(const pg_distillation_args* args, bool backward, void* stream) {
@@ -385,33 +608,41 @@ int distillation(const pg_distillation_args* args, bool backward, void* stream) 
     const bool two = soft != 0.0f && hard != 0.0f;
     const float k = static_cast<float>(1.4426950408889634 / (soft != 0.0f ? static_cast<double>(a.temperature) : 1.0));
     const size_t words = soft != 0.0f ? 16 * static_cast<size_t>(a.top) : 0, kept = (static_cast<size_t>(a.classes) + 14) / 8 * 16;
-    const int mode = backward ? BACKWARD : !a.dlogits.data ? FORWARD : kept + words <= kMaxRowBytes ? BOTH : AGAIN;
+    const int mode = backward ? BACKWARD : kept + 2 * words > kMaxRowBytes ? AGAIN : a.dlogits.data ? BOTH : FORWARD;
+    const int64_t rows_in_all = int64_t{a.batch} * a.tokens;
     int rc = PG_OK;
     auto launch = [&](auto h, auto power, auto threads, auto which) {
         using H = decltype(h);
         constexpr int POWER = decltype(power)::value, T = decltype(threads)::value, MODE = decltype(which)::value;
-        const auto kernel = distillation_kernel<H, POWER, T, MODE>;
-        const size_t smem = words + (MODE == BOTH ? kept : 0);
-        if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
-            cudaGetLastError();
-            rc = PG_ERR_CUDA;
-            return;
+        if constexpr (MODE == FORWARD || MODE == BOTH) {
+            const auto kernel = distillation_kernel<H, POWER, T, MODE == BOTH>;
+            const size_t smem = 2 * words + kept;
+            if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
+                cudaGetLastError();
+                rc = PG_ERR_CUDA;
+                return;
+            }
+            // as many blocks as are resident at once (a block takes 1 KB of shared memory and its sums besides)
+            const int64_t fit = std::min<int64_t>(T == kWide ? 4 : T == 128 ? 7 : 14, (228 * 1024) / (smem + 1024 + 2 * sizeof(Sums) * T / 32 + 16));
+            kernel<<<static_cast<unsigned>(std::min<int64_t>(rows_in_all, kSMs * std::max<int64_t>(fit, 1))), T + 32, smem, st>>>(a, k, soft, hard);
+        } else {
+            int splits = 1;
+            if (MODE == BACKWARD) {                    // few rows: as many blocks as there is room for, two steps of all threads each at least
+                const int64_t steps = (int64_t{a.classes} + 8 * T - 1) / (8 * T);
+                splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(steps / 2, 4 * kSMs / rows_in_all)));
+            }
+            distillation_stream_kernel<H, POWER, T, MODE><<<dim3(a.tokens, a.batch, splits), T + 32, words, st>>>(a, k, soft, hard);
         }
-        int splits = 1;
-        if (MODE == BACKWARD) {                        // few rows: as many blocks as there is room for, two steps of all threads each at least
-            const int64_t all = int64_t{a.batch} * a.tokens, steps = (int64_t{a.classes} + 8 * T - 1) / (8 * T);
-            splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(steps / 2, 4 * kSMs / all)));
-        }
-        kernel<<<dim3(a.tokens, a.batch, splits), T, smem, st>>>(a, k, soft, hard);
         rc = launch_status();
     };
     auto with_mode = [&](auto h, auto power) {
         with_threads(a.classes, [&](auto threads) {
             using std::integral_constant;
-            if (mode == FORWARD) launch(h, power, threads, integral_constant<int, FORWARD>{});
-            else if (mode == BOTH) launch(h, power, threads, integral_constant<int, BOTH>{});
-            else if (mode == BACKWARD) launch(h, power, threads, integral_constant<int, BACKWARD>{});
-            else launch(h, power, integral_constant<int, 512>{}, integral_constant<int, AGAIN>{});
+            constexpr int T = decltype(threads)::value;
+            if (mode == FORWARD) return launch(h, power, threads, integral_constant<int, FORWARD>{});
+            if (mode == BACKWARD) return launch(h, power, threads, integral_constant<int, BACKWARD>{});
+            if (mode == BOTH) return launch(h, power, threads, integral_constant<int, BOTH>{});
+            if constexpr (T == kWide) launch(h, power, threads, integral_constant<int, AGAIN>{});
         });
     };
     auto with_power = [&](auto h) {
