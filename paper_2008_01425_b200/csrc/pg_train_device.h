@@ -279,6 +279,17 @@ __device__ __forceinline__ F2 sigmoid_of(F2 v) {
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
     return pair(a, b);
 }
+// 2^x by the exponential unit, good to two units in the last place.
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ F2 ex2(F2 v) {
+    float a, b;
+    split(v, a, b);
+    return pair(ex2(a), ex2(b));
+}
 constexpr double kGelu0 = 1.5957691216057308;                  // 2 sqrt(2/pi)
 constexpr double kGelu1 = 0.044715 * kGelu0;
 __device__ __forceinline__ float relu(float z) { return z > 0.0f ? z : (z <= 0.0f ? 0.0f : z); }      // NaN stays NaN

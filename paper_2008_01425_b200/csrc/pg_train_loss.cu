@@ -20,16 +20,6 @@ constexpr float kNoLogit = -1e30f;                     // r before the first log
 constexpr float kSlack = 20.0f;                        // (of the fourth power, 2^80 and a sum of as many as there are)
 constexpr size_t kMaxRowBytes = 200 * 1024;            // of a block's shared memory
 
-__device__ __forceinline__ float ex2(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ F2 ex2(F2 v) {
-    float a, b;
-    split(v, a, b);
-    return pair(ex2(a), ex2(b));
-}
 
 // v rounded to a whole number, by adding and taking off 1.5 * 2^23 (a number too large for that is one).
 __device__ __forceinline__ float whole(float v) { return fabsf(v) < 4194304.0f ? (v + kRound) - kRound : v; }

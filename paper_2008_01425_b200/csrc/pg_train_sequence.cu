@@ -7,11 +7,6 @@
 namespace pgt {
 namespace {
 
-__device__ __forceinline__ float ex2(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ float rcp(float v) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -266,107 +261,274 @@ __device__ __forceinline__ float softplus(float v) {
     return fmaf(s, p, fmaxf(v, 0.0f));
 }
 __device__ __forceinline__ float sigmoid(float v) { return rcp(1.0f + ex2(-kLog2e * v)); }
+__device__ __forceinline__ F2 softplus(F2 v) {          // of two
+    float a, b;
+    split(v, a, b);
+    const F2 e = pair(ex2(-kLog2e * fabsf(a)), ex2(-kLog2e * fabsf(b)));
+    float c, d;
+    split(add(e, both(2.0f)), c, d);
+    const F2 s = mul(e, pair(rcp(c), rcp(d))), q = mul(s, s);
+    F2 p = both(2.0f / 13.0f);
+    p = fma(p, q, both(2.0f / 11.0f));
+    p = fma(p, q, both(2.0f / 9.0f));
+    p = fma(p, q, both(2.0f / 7.0f));
+    p = fma(p, q, both(2.0f / 5.0f));
+    p = fma(p, q, both(2.0f / 3.0f));
+    p = fma(p, q, both(2.0f));
+    return fma(s, p, pair(fmaxf(a, 0.0f), fmaxf(b, 0.0f)));
+}
 
-// A channel's states lie in LANES neighbouring threads, P each.  A block has CH channels of one sequence.
+__device__ __forceinline__ void copy16(void* shared, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Rows of CH neighbouring elements of a 16-bit matrix in shared memory, as the 16-byte pieces of memory that hold them: a row starts as far
+// into its first piece as it does in memory.
+template <int CH>
+struct Rows {
+    static constexpr int kPieces = CH / 8 + 1;
+    const uint16_t* x;                                 // first row's first element
+    int64_t ld;
+    __device__ Rows() : x(nullptr), ld(0) {}
+    __device__ Rows(const pg_matrix& m, int64_t b, int64_t row, int col) : ld(m.ld) {
+        x = static_cast<const uint16_t*>(m.data) + b * m.stride + row * m.ld + col;
+    }
+    __device__ int off(int t) const { return static_cast<int>((reinterpret_cast<uintptr_t>(x) / 2 + static_cast<uint32_t>(t) * static_cast<uint32_t>(ld)) & 7); }
+    // Asks for pieces at, at + 8, .. of row t, which has n elements.
+    __device__ void ask(uint4* to, int t, int at, int n) const {
+        const uint16_t* row = x + t * ld;
+        const int o = off(t);
+        const uint4* from = reinterpret_cast<const uint4*>(row - o);
+#pragma unroll
+        for (int i = 0; i < kPieces; i += 8)
+            if (i + at < kPieces && 8 * (i + at) < o + n && PGT_READ(from + i + at, 16)) copy16(to + i + at, from + i + at);
+    }
+    __device__ uint16_t get(const uint4* held, int t, int c) const { return reinterpret_cast<const uint16_t*>(held)[off(t) + c]; }
+};
+
+// A channel's states lie in LANES neighbouring threads, P each, in pairs.  A block takes CH channels of one sequence at a time, or of a
+// chunk of it (an item), in tiles of kScanTile tokens; the next tile is on its way while one is worked on.  Items are numbered by
+// worker, channels, sequence and chunk, and a block has neighbours of them, so that it keeps its channels' rates as long as possible.
+// The exponential unit bounds it: 16 states and the softplus and the gate take 20 exponentials or reciprocals per token and channel.
 constexpr int kScanThreads = 128;
-constexpr int kScanTile = 16;                          // tokens whose b and c are in shared memory
+constexpr int kScanTile = 16;                          // tokens; an eighth of the threads
+constexpr int kScanBlocks = 6;                       // resident per SM
+
+struct Item {
+    int64_t b, sequence;                               // sequence: of all workers
+    int s, d0, t0, t1, stop, chunk;                    // tokens t0 to t1, there to stop
+    __device__ Item(uint32_t at, uint32_t sequences, int length, int chunk_size, uint32_t chunks, uint32_t tiles, int ch, const int32_t* lengths) {
+        chunk = static_cast<int>(at % chunks);
+        at /= chunks;
+        s = static_cast<int>(at % sequences);
+        at /= sequences;
+        d0 = static_cast<int>(at % tiles) * ch;
+        b = at / tiles;
+        sequence = b * sequences + s;
+        t0 = chunk * chunk_size;
+        t1 = min(length, t0 + chunk_size);
+        stop = max(t0, min(t1, tokens_of(lengths, b, static_cast<int>(sequences), s, length)));
+    }
+};
+
+// P neighbouring fp32 numbers, `there` of them, in pairs.
+template <int P>
+__device__ __forceinline__ void load_states(const float* from, int there, bool wide, F2 (&v)[P / 2]) {
+#pragma unroll
+    for (int p = 0; p < P / 2; ++p) v[p] = both(0.0f);
+    if (wide && there >= P) {
+#pragma unroll
+        for (int p = 0; p < P / 4; ++p) {
+            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (PGT_READ(from + 4 * p, 16)) f = *reinterpret_cast<const float4*>(from + 4 * p);
+            v[2 * p] = pair(f.x, f.y);
+            v[2 * p + 1] = pair(f.z, f.w);
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < P / 2; ++p) v[p] = pair(2 * p < there ? PGT_LOAD(from[2 * p]) : 0.0f, 2 * p + 1 < there ? PGT_LOAD(from[2 * p + 1]) : 0.0f);
+    }
+}
+template <int P>
+__device__ __forceinline__ void store_states(float* to, int there, bool wide, const F2 (&v)[P / 2]) {
+    float e[P];
+#pragma unroll
+    for (int p = 0; p < P / 2; ++p) split(v[p], e[2 * p], e[2 * p + 1]);
+    if (wide && there >= P) {
+#pragma unroll
+        for (int p = 0; p < P / 4; ++p) PGT_STORE(*reinterpret_cast<float4*>(to + 4 * p), make_float4(e[4 * p], e[4 * p + 1], e[4 * p + 2], e[4 * p + 3]));
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (p < there) PGT_STORE(to[p], e[p]);
+    }
+}
 
 // LOCAL: a chunk's own part: its last state from a zero one, and the sum of its steps.  Otherwise the chunk's results, from the
 // state before it.
 template <typename H, int P, int LANES, bool LOCAL>
-__global__ void __launch_bounds__(kScanThreads)
-scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict__ sums, int chunk, int chunks) {
-    constexpr int N = P * LANES;
-    __shared__ __align__(16) float s_b[kScanTile][N], s_c[kScanTile][N];
-    const int64_t sequence = blockIdx.x / chunks;      // of all workers
-    const int at_chunk = static_cast<int>(blockIdx.x % chunks);
-    const int64_t b = sequence / a.sequences;
-    const int s = static_cast<int>(sequence % a.sequences);
-    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
-    const bool is = d < a.channels;
-    const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
-    const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), stop = min(t1, have);
-    const int64_t first = static_cast<int64_t>(s) * a.length;
-    const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + first * a.u.ld + d;
-    const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + first * a.delta.ld + d;
-    const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + first * a.z.ld + d : nullptr;
-    const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + first * a.b.ld;
-    const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + first * a.c.ld;
-    uint16_t* y = static_cast<uint16_t*>(a.y.data) + b * a.y.stride + first * a.y.ld + d;
-    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
-    const float skip = is && a.skip ? PGT_LOAD(a.skip[b * a.skip_stride + d]) : 0.0f;
-    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
-    const int64_t held = (sequence * a.channels + d) * a.states;
-    float rate[P], h[P], sum = 0.0f;
+__global__ void __launch_bounds__(kScanThreads, kScanBlocks)
+scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict__ sums, int chunk, int chunks, int tiles, uint32_t items) {
+    constexpr int N = P * LANES, CH = kScanThreads / LANES, A = LOCAL ? 2 : 3, kPieces = Rows<CH>::kPieces, kEach = kScanTile * N / kScanThreads;
+    __shared__ __align__(16) uint4 s_in[2][A][kScanTile][kPieces];
+    __shared__ __align__(16) float s_b[2][kScanTile][N], s_c[LOCAL ? 1 : 2][LOCAL ? 1 : kScanTile][LOCAL ? 1 : N];
+    const int c = threadIdx.x / LANES, n0 = threadIdx.x % LANES * P, there = min(max(a.states - n0, 0), P);
+    const uint32_t each = (items - 1) / gridDim.x + 1, begin = blockIdx.x * each, end = min(items, begin + each);      // (items + a block's are below 2^32)
+    if (begin >= end) return;
+    auto item_at = [&](uint32_t at) { return Item(at, a.sequences, a.length, chunk, chunks, tiles, CH, a.lengths); };
+    // What is on its way: the tile at `tile` of the item `next`.
+    uint32_t ahead = begin;
+    Item next = item_at(begin);
+    int tile = next.t0, buffer = 0;
+    uint16_t rb[kEach], rc[LOCAL ? 1 : kEach];
+    auto ask = [&](int to) {
+        const int64_t first = static_cast<int64_t>(next.s) * a.length;
+        const int count = min(kScanTile, next.stop - tile), n = min(CH, a.channels - next.d0);
+        const Rows<CH> in[3] = {Rows<CH>(a.u, next.b, first + tile, next.d0), Rows<CH>(a.delta, next.b, first + tile, next.d0),
+                                LOCAL || !a.z.data ? Rows<CH>() : Rows<CH>(a.z, next.b, first + tile, next.d0)};
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const bool there = is && n0 + p < a.states;
-        rate[p] = there ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
-        h[p] = 0.0f;
+        for (int k = 0; k < A; ++k) {
+            if (k == 2 && !a.z.data) break;
+            const int row = threadIdx.x / 8;           // eight threads a row
+            if (row < count) in[k].ask(&s_in[to][k][row][0], row, threadIdx.x % 8, n);
+        }
+        const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + next.b * a.b.stride + (first + tile) * a.b.ld;
+        const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + next.b * a.c.stride + (first + tile) * a.c.ld;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = i * kScanThreads + threadIdx.x, k = at / N, m = at % N;
+            const bool is = k < count && m < a.states;
+            rb[i] = is ? PGT_LOAD(bb[k * a.b.ld + m]) : 0;
+            if constexpr (!LOCAL) rc[i] = is ? PGT_LOAD(cc[k * a.c.ld + m]) : 0;
+        }
+    };
+    auto advance = [&] {                               // to the tile after the one on its way; false if that was the last
+        tile += kScanTile;
+        if (tile < next.stop) return true;
+        if (++ahead >= end) return false;
+        next = item_at(ahead);
+        tile = next.t0;
+        return true;
+    };
+    ask(0);
+    bool more = true;
+    int64_t of = -1;                                   // worker and channels whose rates are here
+    F2 rate[P / 2];
+    float bias = 0.0f, skip = 0.0f;
+    const bool wide = a.states % 4 == 0;
+    for (uint32_t at = begin; at < end; ++at) {
+        const Item item = next;                        // (its first tile is what is on its way)
+        const int d = item.d0 + c, mine = d < a.channels ? there : 0;
+        const bool is = d < a.channels, idle = item.d0 + threadIdx.x / 32 * (32 / LANES) >= a.channels;      // idle: the whole warp
+        if (of != item.b * tiles + item.d0 / CH) {
+            of = item.b * tiles + item.d0 / CH;
+            const float* rates = static_cast<const float*>(a.a.data) + item.b * a.a.stride + d * a.a.ld + n0;
+            load_states<P>(rates, mine, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
+#pragma unroll
+            for (int p = 0; p < P / 2; ++p) rate[p] = mul(rate[p], both(kLog2e));
+            bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[item.b * a.delta_bias_stride + d]) : 0.0f;
+            skip = is && a.skip ? PGT_LOAD(a.skip[item.b * a.skip_stride + d]) : 0.0f;
+        }
+        const int64_t held = (item.sequence * a.channels + d) * a.states + n0, chunk_at = (item.sequence * chunks + item.chunk) * a.channels + d;
+        F2 h[P / 2];
+#pragma unroll
+        for (int p = 0; p < P / 2; ++p) h[p] = both(0.0f);
         if constexpr (!LOCAL) {
-            if (there && chunks > 1) h[p] = PGT_LOAD(states[(static_cast<int64_t>(blockIdx.x) * a.channels + d) * a.states + n0 + p]);
-            else if (there && a.state) h[p] = PGT_LOAD(a.state[held + n0 + p]);
+            if (chunks > 1) load_states<P>(states + chunk_at * a.states + n0, mine, wide, h);
+            else if (a.state) load_states<P>(a.state + held, mine, wide && reinterpret_cast<uintptr_t>(a.state) % 16 == 0, h);
         }
-    }
-    for (int tile = t0; tile < stop; tile += kScanTile) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kScanTile * N; i += kScanThreads) {
-            const int k = i / N, n = i % N;
-            const bool there = tile + k < stop && n < a.states;
-            s_b[k][n] = there ? Elem<H>::up(PGT_LOAD(bb[(tile + k) * a.b.ld + n])) : 0.0f;
-            if constexpr (!LOCAL) s_c[k][n] = there ? Elem<H>::up(PGT_LOAD(cc[(tile + k) * a.c.ld + n])) : 0.0f;
-        }
-        __syncthreads();
-        constexpr int U = 8;
-        for (int k0 = 0; k0 < kScanTile && tile + k0 < stop; k0 += U) {
-            uint16_t ru[U], rd[U], rz[U];
+        float sum = 0.0f;
+        const int64_t first = static_cast<int64_t>(item.s) * a.length;
+        uint16_t* y = LOCAL ? nullptr : static_cast<uint16_t*>(a.y.data) + item.b * a.y.stride + first * a.y.ld + d;
+        int t = item.t0;
+        do {                                           // (an item without tokens has a tile all the same, an empty one)
+            copies_wait();
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int t = tile + k0 + k;
-                const bool there = is && t < stop;
-                ru[k] = there ? PGT_LOAD(u[t * a.u.ld]) : 0;
-                rd[k] = there ? PGT_LOAD(delta[t * a.delta.ld]) : 0;
-                if constexpr (!LOCAL) rz[k] = there && z ? PGT_LOAD(z[t * a.z.ld]) : 0;
+            for (int i = 0; i < kEach; ++i) {
+                const int k = i * kScanThreads + threadIdx.x;
+                (&s_b[buffer][0][0])[k] = Elem<H>::up(rb[i]);
+                if constexpr (!LOCAL) (&s_c[LOCAL ? 0 : buffer][0][0])[k] = Elem<H>::up(rc[i]);
             }
+            __syncthreads();                           // this tile is there, and nobody reads the one before it
+            more = more && advance();
+            if (more) ask(buffer ^ 1);
+            const Rows<CH> ru(a.u, item.b, first + t, item.d0), rd(a.delta, item.b, first + t, item.d0);
+            const Rows<CH> rz = LOCAL || !a.z.data ? Rows<CH>() : Rows<CH>(a.z, item.b, first + t, item.d0);
+            const int count = idle ? 0 : min(kScanTile, item.stop - t);
+            constexpr int U = 2;                       // tokens whose steps and gates are computed side by side; those behind the last change nothing
+            uint16_t* to = LOCAL ? nullptr : y + t * a.y.ld;
+            for (int k0 = 0; k0 < count; k0 += U) {
+                F2 in[U / 2], step[U / 2], v[U / 2];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int t = tile + k0 + k;
-                if (t >= stop) break;
-                const float step = softplus(Elem<H>::up(rd[k]) + bias), in = Elem<H>::up(ru[k]), drive = step * in;
-                float out = 0.0f;
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    h[p] = fmaf(ex2(step * rate[p]), h[p], drive * s_b[k0 + k][n0 + p]);
-                    if constexpr (!LOCAL) out = fmaf(h[p], s_c[k0 + k][n0 + p], out);
-                }
-                if constexpr (LOCAL) {
-                    sum += step;
-                } else {
-#pragma unroll
-                    for (int o = 1; o < LANES; o <<= 1) out += __shfl_xor_sync(0xffffffffu, out, o);
-                    out = fmaf(skip, in, out);
-                    if (z) {
-                        const float v = Elem<H>::up(rz[k]);
-                        out *= v * sigmoid(v);
+                for (int u = 0; u < U; u += 2) {
+                    auto two = [&](const Rows<CH>& r, int which) {
+                        return pair(Elem<H>::up(r.get(s_in[buffer][which][k0 + u], k0 + u, c)), Elem<H>::up(r.get(s_in[buffer][which][k0 + u + 1], k0 + u + 1, c)));
+                    };
+                    in[u / 2] = two(ru, 0);
+                    step[u / 2] = softplus(add(two(rd, 1), both(bias)));
+                    if constexpr (!LOCAL) v[u / 2] = a.z.data ? activate<PG_ACT_SILU>(two(rz, A - 1)) : both(1.0f);
+                    if (k0 + U > count) {
+                        float i0, i1, d0, d1;
+                        split(in[u / 2], i0, i1);
+                        split(step[u / 2], d0, d1);
+                        const bool first_is = k0 + u < count, second_is = k0 + u + 1 < count;
+                        in[u / 2] = pair(first_is ? i0 : 0.0f, second_is ? i1 : 0.0f);
+                        step[u / 2] = pair(first_is ? d0 : 0.0f, second_is ? d1 : 0.0f);
                     }
-                    if (is && n0 == 0) PGT_STORE(y[t * a.y.ld], Elem<H>::down(out));
+                }
+                float outs[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float lo, hi, lo2, hi2;
+                    split(step[u / 2], lo, hi);
+                    split(mul(step[u / 2], in[u / 2]), lo2, hi2);
+                    const F2 steps = both(u & 1 ? hi : lo), drive = both(u & 1 ? hi2 : lo2);
+                    F2 out[2] = {both(0.0f), both(0.0f)};
+                    const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(&s_b[buffer][k0 + u][n0]);
+                    const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(&s_c[LOCAL ? 0 : buffer][LOCAL ? 0 : k0 + u][LOCAL ? 0 : n0]);
+#pragma unroll
+                    for (int p = 0; p < P / 4; ++p) {
+                        const ulonglong2 bv = bk[p];
+                        h[2 * p] = fma(ex2(mul(steps, rate[2 * p])), h[2 * p], mul(drive, F2{bv.x}));
+                        h[2 * p + 1] = fma(ex2(mul(steps, rate[2 * p + 1])), h[2 * p + 1], mul(drive, F2{bv.y}));
+                        if constexpr (!LOCAL) {
+                            const ulonglong2 cv = ck[p];
+                            out[0] = fma(h[2 * p], F2{cv.x}, out[0]);
+                            out[1] = fma(h[2 * p + 1], F2{cv.y}, out[1]);
+                        }
+                    }
+                    if constexpr (LOCAL) sum += u & 1 ? hi : lo;
+                    else outs[u] = sum2(add(out[0], out[1]));
+                }
+                if constexpr (!LOCAL) {
+#pragma unroll
+                    for (int u = 0; u < U; u += 2) {
+#pragma unroll
+                        for (int o = 1; o < LANES; o <<= 1) {
+                            outs[u] += __shfl_xor_sync(0xffffffffu, outs[u], o);
+                            outs[u + 1] += __shfl_xor_sync(0xffffffffu, outs[u + 1], o);
+                        }
+                        const uint32_t w = Elem<H>::down2(mul(fma(both(skip), in[u / 2], pair(outs[u], outs[u + 1])), v[u / 2]));
+                        if (is && n0 == 0) {
+                            if (k0 + u < count) PGT_STORE(to[0], static_cast<uint16_t>(w & 0xffffu));
+                            if (k0 + u + 1 < count) PGT_STORE(to[a.y.ld], static_cast<uint16_t>(w >> 16));
+                        }
+                        to += 2 * a.y.ld;
+                    }
                 }
             }
+            t += kScanTile;
+            buffer ^= 1;
+        } while (t < item.stop);
+        if constexpr (LOCAL) {
+            store_states<P>(states + chunk_at * a.states + n0, mine, wide, h);
+            if (is && n0 == 0) PGT_STORE(sums[chunk_at], sum);
+        } else {
+            if (is && n0 == 0)
+                for (int k = item.stop; k < item.t1; ++k) PGT_STORE(y[k * a.y.ld], static_cast<uint16_t>(0));
+            if (a.state_out && item.chunk == chunks - 1) store_states<P>(a.state_out + held, mine, wide && reinterpret_cast<uintptr_t>(a.state_out) % 16 == 0, h);
         }
-    }
-    if constexpr (LOCAL) {
-        const int64_t at = static_cast<int64_t>(blockIdx.x) * a.channels + d;
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (is && n0 + p < a.states) PGT_STORE(states[at * a.states + n0 + p], h[p]);
-        if (is && n0 == 0) PGT_STORE(sums[at], sum);
-    } else {
-        if (is && n0 == 0)
-            for (int t = max(t0, stop); t < t1; ++t) PGT_STORE(y[t * a.y.ld], static_cast<uint16_t>(0));
-        if (a.state_out && at_chunk == chunks - 1)
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-                if (is && n0 + p < a.states) PGT_STORE(a.state_out[held + n0 + p], h[p]);
     }
 }
 
@@ -744,15 +906,17 @@ int conv_parts(const pg_conv_grad_args& a, int runs) {
     return static_cast<int>(std::max<int64_t>(1, std::min(most, (items + 3) / 4)));
 }
 
-struct ScanPlan { int chunk, chunks; };
-// Chunks of a sequence for the forward scan: one unless there are too few threads for the GPU.
+struct ScanPlan { int chunk, chunks, tiles; int64_t items; };
+// Chunks of a sequence for the forward scan.  With chunks every token is gone through twice, so there are some only where they make the
+// work of a block a third or less of a sequence.
 ScanPlan scan_plan(const pg_scan_args& a, int lanes) {
-    const int64_t blocks = int64_t{a.batch} * a.sequences * ((int64_t{a.channels} * lanes + kScanThreads - 1) / kScanThreads);
-    int64_t chunks = std::max<int64_t>(1, int64_t{kSMs} * 4 / std::max<int64_t>(1, blocks));
-    int64_t chunk = std::max<int64_t>(64, (a.length + chunks - 1) / chunks);
-    if (blocks >= 2 * kSMs) chunk = std::max<int64_t>(a.length, 1);
-    chunks = std::max<int64_t>(1, (a.length + chunk - 1) / chunk);
-    return {static_cast<int>(chunk), static_cast<int>(chunks)};
+    const int tiles = (a.channels + kScanThreads / lanes - 1) / (kScanThreads / lanes);
+    const int64_t whole = std::max<int64_t>(1, int64_t{a.batch} * a.sequences * tiles), length = std::max(a.length, 1);
+    int64_t chunks = std::min<int64_t>(int64_t{kSMs} * kScanBlocks / whole, length / 32);
+    if (chunks < 3) chunks = 1;
+    const int64_t chunk = (length + chunks - 1) / chunks;
+    chunks = (length + chunk - 1) / chunk;
+    return {static_cast<int>(chunk), static_cast<int>(chunks), tiles, int64_t{a.batch} * a.sequences * tiles * chunks};
 }
 int lanes_of(int states, int per_thread) {
     int lanes = 1;
@@ -952,7 +1116,7 @@ int pg_selective_scan(const pg_scan_args* args, void* workspace, size_t workspac
     if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
     const int lanes = lanes_of(a.states, 16);
     const ScanPlan p = scan_plan(a, lanes);
-    if (sequences * p.chunks > kMaxBlocks) return PG_ERR_TOO_LARGE;
+    if (p.items > kMaxBlocks) return PG_ERR_TOO_LARGE;
     if (sequences == 0 || (a.length == 0 && !a.state_out)) return PG_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Operands operands;
@@ -967,13 +1131,13 @@ int pg_selective_scan(const pg_scan_args* args, void* workspace, size_t workspac
         using H = decltype(h);
         auto launch = [&](auto per, auto lane) {
             constexpr int P = decltype(per)::value, LANES = decltype(lane)::value;
-            const dim3 grid(static_cast<unsigned>(sequences * p.chunks), (a.channels + kScanThreads / LANES - 1) / (kScanThreads / LANES));
+            const unsigned grid = static_cast<unsigned>(std::min<int64_t>(p.items, int64_t{kSMs} * kScanBlocks));
             if (p.chunks > 1) {
-                scan_kernel<H, P, LANES, true><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks);
+                scan_kernel<H, P, LANES, true><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks, p.tiles, static_cast<uint32_t>(p.items));
                 join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
                     a.a, a.state, states, nullptr, sums, a.sequences, a.channels, a.states, p.chunks);
             }
-            scan_kernel<H, P, LANES, false><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks);
+            scan_kernel<H, P, LANES, false><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks, p.tiles, static_cast<uint32_t>(p.items));
         };
         using std::integral_constant;
         if (a.states <= 8) launch(integral_constant<int, 8>{}, integral_constant<int, 1>{});
