@@ -571,14 +571,8 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
 // states of a group are computed once more.
 constexpr int kGradStates = 8;                         // states of a thread
 constexpr int kGroup = 4;
-constexpr int kGradChunk = 64;                         // tokens of a chunk at most
-
-template <typename H, int LANES>
-struct GradChannel {                                   // what a thread knows of its channel in one sequence
-    const uint16_t *u, *delta, *z, *dy;
-    float bias, skip;
-    bool is;
-};
+constexpr int kGradChunk = 40;                         // tokens of a chunk at most
+constexpr int kGradBlocks = 3;                         // resident per SM
 
 // Own parts of a chunk for the way in both directions: the last state from a zero one, and the gradient that reaches the state before it.
 template <typename H, int LANES>
@@ -673,165 +667,295 @@ __device__ __forceinline__ int scatter_sums(float (&v)[V]) {
     return at;
 }
 
-// A block has one share of a worker's chunks and kScanThreads / LANES channels, whose dA, dskip and ddelta_bias stay in registers.
+// Shared memory of a block for chunks of `rows` tokens, a multiple of kGroup; in bytes from the start.
+template <int LANES>
+struct GradLayout {
+    static constexpr int kN = kGradStates * LANES, kCh = kScanThreads / LANES;
+    static constexpr int kRed = kScanThreads / 32 * kGroup * 2 * kN * 4, kSlot = kGradStates * kScanThreads * 4;
+    static constexpr int kSlots = (kRed + kSlot - 1) / kSlot;          // groups whose states leave room for a group's sums
+    int u, dv, dz, b, c, h, red, all;                  // steps first; u in 16 bits; what dz is a multiple of; b and c; states before groups
+    __host__ __device__ explicit GradLayout(int rows) {
+        dv = rows * kCh * 4;
+        dz = dv + rows * kCh * 4;
+        u = dz + rows * kCh * 4;
+        b = (u + rows * kCh * 2 + 15) / 16 * 16;
+        c = b + rows * kN * 4;
+        h = c + rows * kN * 4;
+        red = h + rows / kGroup * kSlot;
+        all = red + kSlots * kRed;
+    }
+};
+
+// 1 - exp(-v), v >= 0: the softplus' slope where its value is v.  (Below 1/2 by its series, to v^8 / 8!; the difference would lose v's digits.)
+__device__ __forceinline__ float slope_of_step(float v) {
+    float p = -1.0f / 40320.0f;
+    p = fmaf(p, v, 1.0f / 5040.0f);
+    p = fmaf(p, v, -1.0f / 720.0f);
+    p = fmaf(p, v, 1.0f / 120.0f);
+    p = fmaf(p, v, -1.0f / 24.0f);
+    p = fmaf(p, v, 1.0f / 6.0f);
+    p = fmaf(p, v, -0.5f);
+    p = fmaf(p, v, 1.0f);
+    return v < 0.5f ? p * v : 1.0f - ex2(-kLog2e * v);
+}
+
+// A block has one share of a worker's chunks and CH channels, whose dA, dskip and ddelta_bias stay in registers.
 // parts[block's channels][worker][token][2 N]: what these channels add to dB and dC.
 // partial[worker][share][channels][states + 2]: dA, then dskip and ddelta_bias.
 template <typename H, int LANES>
-__global__ void __launch_bounds__(kScanThreads)
+__global__ void __launch_bounds__(kScanThreads, kGradBlocks)
 scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, const float* __restrict__ carries, float* __restrict__ parts,
                  float* __restrict__ partial, int chunk, int chunks, int shares) {
-    constexpr int P = kGradStates, N = P * LANES, G = 32 / LANES, V = 2 * P, kKept = V / G > 1 ? V / G : 1;
-    extern __shared__ __align__(16) float s_all[];
-    const int groups = (chunk + kGroup - 1) / kGroup;
-    float* s_b = s_all;                                // [token][N]
-    float* s_c = s_b + groups * kGroup * N;
-    float* s_h = s_c + groups * kGroup * N;            // [group][P][thread]
-    float* s_red = s_h + groups * P * kScanThreads;    // [warp][token of the group][2 N]
+    constexpr int P = kGradStates, N = P * LANES, G = 32 / LANES, V = 2 * P, kKept = V / G > 1 ? V / G : 1, CH = kScanThreads / LANES, kWarps = kScanThreads / 32;
+    extern __shared__ __align__(16) char s_all[];
+    const int rows = (chunk + kGroup - 1) / kGroup * kGroup;
+    const GradLayout<LANES> layout(rows);
+    float* s_step = reinterpret_cast<float*>(s_all);   // [token][channel], as are the next three
+    float* s_dv = reinterpret_cast<float*>(s_all + layout.dv);
+    float* s_dz = reinterpret_cast<float*>(s_all + layout.dz);
+    uint16_t* s_u = reinterpret_cast<uint16_t*>(s_all + layout.u);
+    float* s_b = reinterpret_cast<float*>(s_all + layout.b);
+    float* s_c = reinterpret_cast<float*>(s_all + layout.c);
+    float4* s_h = reinterpret_cast<float4*>(s_all + layout.h);
+    float* s_red = reinterpret_cast<float*>(s_all + layout.red);
     const int64_t b = blockIdx.x / shares;
     const int share = static_cast<int>(blockIdx.x % shares);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
-    const bool is = d < a.channels, writes = is && n0 == 0;
-    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
+    const int d0 = blockIdx.y * CH, d = d0 + c;
+    const bool is = d < a.channels;
+    const int there = is ? min(max(a.states - n0, 0), P) : 0, step_d = d0 + threadIdx.x % CH;
+    const float step_bias = step_d < a.channels && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + step_d]) : 0.0f;
     const float skip = is && a.skip ? PGT_LOAD(a.skip[b * a.skip_stride + d]) : 0.0f;
-    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
-    float rate[P], da[P], dskip = 0.0f, dbias = 0.0f;
+    const bool wide = a.states % 4 == 0;
+    F2 rate[P / 2], da[P / 2];
+    {
+        const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld + n0;
+        load_states<P>(rates, there, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        rate[p] = is && n0 + p < a.states ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
-        da[p] = 0.0f;
+        for (int p = 0; p < P / 2; ++p) {
+            rate[p] = mul(rate[p], both(kLog2e));
+            da[p] = both(0.0f);
+        }
     }
+    float dskip = 0.0f, dbias = 0.0f;
     const int64_t tokens = static_cast<int64_t>(a.sequences) * a.length;
     float* my_parts = parts + (static_cast<int64_t>(blockIdx.y) * a.batch + b) * tokens * 2 * N;
+    const bool gated = a.z.data != nullptr;
     for (int64_t item = share; item < static_cast<int64_t>(a.sequences) * chunks; item += shares) {
         const int s = static_cast<int>(item / chunks), at_chunk = static_cast<int>(item % chunks);
         const int64_t sequence = b * a.sequences + s, first = static_cast<int64_t>(s) * a.length;
         const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
-        const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), stop = min(t1, have), count = max(0, stop - t0);
-        const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + (first + t0) * a.u.ld + d;
-        const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + (first + t0) * a.delta.ld + d;
-        const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + (first + t0) * a.z.ld + d : nullptr;
-        const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + (first + t0) * a.dy.ld + d;
-        const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + (first + t0) * a.b.ld;
-        const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + (first + t0) * a.c.ld;
-        uint16_t* du = static_cast<uint16_t*>(a.du.data) + b * a.du.stride + (first + t0) * a.du.ld + d;
-        uint16_t* ddelta = static_cast<uint16_t*>(a.ddelta.data) + b * a.ddelta.stride + (first + t0) * a.ddelta.ld + d;
-        uint16_t* dz = z ? static_cast<uint16_t*>(a.dz.data) + b * a.dz.stride + (first + t0) * a.dz.ld + d : nullptr;
+        const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), count = max(0, min(t1, have) - t0);
+        const int groups = (count + kGroup - 1) / kGroup;
+        const int64_t at = first + t0;
         __syncthreads();                               // (shared memory is free again)
+        const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + at * a.b.ld;
+        const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + at * a.c.ld;
+#pragma unroll 4
         for (int i = threadIdx.x; i < groups * kGroup * N; i += kScanThreads) {
             const int k = i / N, n = i % N;
-            const bool there = k < count && n < a.states;
-            s_b[i] = there ? Elem<H>::up(PGT_LOAD(bb[k * a.b.ld + n])) : 0.0f;
-            s_c[i] = there ? Elem<H>::up(PGT_LOAD(cc[k * a.c.ld + n])) : 0.0f;
+            const bool is_there = k < count && n < a.states;
+            s_b[i] = is_there ? Elem<H>::up(PGT_LOAD(bb[k * a.b.ld + n])) : 0.0f;
+            s_c[i] = is_there ? Elem<H>::up(PGT_LOAD(cc[k * a.c.ld + n])) : 0.0f;
+        }
+        F2 h[P / 2], g[P / 2];
+        const int64_t state_at = (sequence * a.channels + d) * a.states + n0, chunk_at = ((sequence * chunks + at_chunk) * a.channels + d) * a.states + n0;
+#pragma unroll
+        for (int p = 0; p < P / 2; ++p) h[p] = g[p] = both(0.0f);
+        if (chunks > 1) {
+            load_states<P>(states + chunk_at, there, wide, h);
+            load_states<P>(carries + chunk_at, there, wide, g);
+        } else if (a.state) {
+            load_states<P>(a.state + state_at, there, wide && reinterpret_cast<uintptr_t>(a.state) % 16 == 0, h);
+        }
+        {                                              // every token and channel once: its step, and what reaches y before the gate
+            auto rows_of = [&](const pg_matrix& m) { return static_cast<const uint16_t*>(m.data) + b * m.stride + at * m.ld + step_d; };
+            const uint16_t *u = rows_of(a.u), *delta = rows_of(a.delta), *dy = rows_of(a.dy), *z = gated ? rows_of(a.z) : nullptr;
+            constexpr int U = 4;                       // tokens on their way at once
+            for (int k0 = threadIdx.x / CH; k0 < groups * kGroup; k0 += U * LANES) {
+                uint16_t ru[U], rd[U], rg[U], rz[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int k = k0 + i * LANES;
+                    const bool is_there = k < count && step_d < a.channels;
+                    ru[i] = is_there ? PGT_LOAD(u[k * a.u.ld]) : 0;
+                    rd[i] = is_there ? PGT_LOAD(delta[k * a.delta.ld]) : 0;
+                    rg[i] = is_there ? PGT_LOAD(dy[k * a.dy.ld]) : 0;
+                    rz[i] = is_there && gated ? PGT_LOAD(z[k * a.z.ld]) : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < U; i += 2) {
+                    const int k = k0 + i * LANES, k1 = k + LANES;
+                    float step[2], dv[2], dz[2] = {0.0f, 0.0f};
+                    split(softplus(pair(Elem<H>::up(rd[i]) + step_bias, Elem<H>::up(rd[i + 1]) + step_bias)), step[0], step[1]);
+                    const F2 gy = pair(Elem<H>::up(rg[i]), Elem<H>::up(rg[i + 1]));
+                    split(gy, dv[0], dv[1]);
+                    if (gated) {
+                        const F2 v = pair(Elem<H>::up(rz[i]), Elem<H>::up(rz[i + 1])), sig = sigmoid_of(mul(v, both(-kLog2e)));
+                        split(mul(gy, mul(v, sig)), dv[0], dv[1]);
+                        split(mul(gy, mul(sig, fma(v, fma(sig, both(-1.0f), both(1.0f)), both(1.0f)))), dz[0], dz[1]);
+                    }
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int to = w ? k1 : k, s_at = to * CH + threadIdx.x % CH;
+                        if (to < groups * kGroup) {
+                            s_step[s_at] = to < count && step_d < a.channels ? step[w] : 0.0f;
+                            s_dv[s_at] = dv[w];
+                            s_dz[s_at] = dz[w];
+                            s_u[s_at] = ru[i + w];
+                        }
+                    }
+                }
+            }
         }
         __syncthreads();
-        auto load = [&](const uint16_t* p, int64_t ld, int k) { return is && k < count ? Elem<H>::up(PGT_LOAD(p[k * ld])) : 0.0f; };
-        auto step_at = [&](int k) { return is && k < count ? softplus(load(delta, a.delta.ld, k) + bias) : 0.0f; };
-        float h[P], g[P];
-        const int64_t held = (sequence * a.channels + d) * a.states, chunk_at = ((sequence * chunks + at_chunk) * a.channels + d) * a.states;
+        for (int group = 0; group < groups; ++group) { // forward
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const bool there = is && n0 + p < a.states;
-            h[p] = !there ? 0.0f : chunks > 1 ? PGT_LOAD(states[chunk_at + n0 + p]) : a.state ? PGT_LOAD(a.state[held + n0 + p]) : 0.0f;
-            g[p] = there && chunks > 1 ? PGT_LOAD(carries[chunk_at + n0 + p]) : 0.0f;
+            for (int q = 0; q < P / 4; ++q) {
+                float4 f;
+                split(h[2 * q], f.x, f.y);
+                split(h[2 * q + 1], f.z, f.w);
+                s_h[(group * (P / 4) + q) * kScanThreads + threadIdx.x] = f;
+            }
+            if (group + 1 == groups) break;
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) {
+                const int k = group * kGroup + i;
+                const float step = s_step[k * CH + c], in = Elem<H>::up(s_u[k * CH + c]);
+                const F2 steps = both(step), drive = both(step * in);
+                const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
+#pragma unroll
+                for (int q = 0; q < P / 4; ++q) {
+                    const ulonglong2 bv = bk[q];
+                    h[2 * q] = fma(ex2(mul(steps, rate[2 * q])), h[2 * q], mul(drive, F2{bv.x}));
+                    h[2 * q + 1] = fma(ex2(mul(steps, rate[2 * q + 1])), h[2 * q + 1], mul(drive, F2{bv.y}));
+                }
+            }
         }
-        for (int k = 0; k < count; ++k) {              // forward
-            if (k % kGroup == 0)
+        for (int group = groups - 1; group >= 0; --group) {
+            F2 before[kGroup][P / 2], keep[kGroup][P / 2];
+            float step[kGroup], in[kGroup], dv[kGroup], to_z[kGroup];
 #pragma unroll
-                for (int p = 0; p < P; ++p) s_h[(k / kGroup * P + p) * kScanThreads + threadIdx.x] = h[p];
-            const float step = step_at(k), drive = step * load(u, a.u.ld, k);
-#pragma unroll
-            for (int p = 0; p < P; ++p) h[p] = fmaf(ex2(step * rate[p]), h[p], drive * s_b[k * N + n0 + p]);
-        }
-        for (int group = (count + kGroup - 1) / kGroup - 1; group >= 0; --group) {
-            float before[kGroup][P], keep[kGroup][P], step[kGroup], in[kGroup], dv[kGroup], inner[kGroup], slope_z[kGroup];
-#pragma unroll
-            for (int p = 0; p < P; ++p) h[p] = s_h[(group * P + p) * kScanThreads + threadIdx.x];
+            for (int q = 0; q < P / 4; ++q) {
+                const float4 f = s_h[(group * (P / 4) + q) * kScanThreads + threadIdx.x];
+                h[2 * q] = pair(f.x, f.y);
+                h[2 * q + 1] = pair(f.z, f.w);
+            }
 #pragma unroll
             for (int i = 0; i < kGroup; ++i) {
                 const int k = group * kGroup + i;      // tokens behind the last one change nothing: their step is zero
-                step[i] = step_at(k);
-                in[i] = load(u, a.u.ld, k);
-                const float drive = step[i] * in[i], gy = load(dy, a.dy.ld, k);
-                float out = 0.0f;
+                step[i] = s_step[k * CH + c];
+                in[i] = Elem<H>::up(s_u[k * CH + c]);
+                dv[i] = s_dv[k * CH + c];
+                const F2 steps = both(step[i]), drive = both(step[i] * in[i]);
+                const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
+                const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(s_c + k * N + n0);
+                F2 out = both(0.0f);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    before[i][p] = h[p];
-                    keep[i][p] = ex2(step[i] * rate[p]);
-                    h[p] = fmaf(keep[i][p], h[p], drive * s_b[k * N + n0 + p]);
-                    out = fmaf(h[p], s_c[k * N + n0 + p], out);
-                }
-                dv[i] = gy;
-                if (z) {
+                for (int q = 0; q < P / 4; ++q) {
+                    const ulonglong2 bv = bk[q], cv = ck[q];
 #pragma unroll
-                    for (int o = 1; o < LANES; o <<= 1) out += __shfl_xor_sync(0xffffffffu, out, o);
-                    const float v = load(z, a.z.ld, k), sig = sigmoid(v);
-                    slope_z[i] = gy * fmaf(skip, in[i], out) * (sig * fmaf(v, 1.0f - sig, 1.0f));
-                    dv[i] = gy * v * sig;
+                    for (int w = 0; w < 2; ++w) {
+                        const int p = 2 * q + w;
+                        before[i][p] = h[p];
+                        keep[i][p] = ex2(mul(steps, rate[p]));
+                        h[p] = fma(keep[i][p], h[p], mul(drive, F2{w ? bv.y : bv.x}));
+                        out = fma(h[p], F2{w ? cv.y : cv.x}, out);
+                    }
                 }
-                inner[i] = out;
+                if (gated) {
+                    float v = sum2(out);
+#pragma unroll
+                    for (int o = 1; o < LANES; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    to_z[i] = s_dz[k * CH + c] * fmaf(skip, in[i], v);
+                }
             }
+            // The sums go where the states of the groups behind this one were, or behind all states.
+            constexpr int kSlots = GradLayout<LANES>::kSlots;
+            float* reds = group + kSlots < groups ? reinterpret_cast<float*>(s_h + (group + 1) * (P / 4) * kScanThreads) : s_red + (groups - 1 - group) * (GradLayout<LANES>::kRed / 4);
+            float* red = reds + warp * kGroup * 2 * N;
 #pragma unroll
             for (int i = kGroup - 1; i >= 0; --i) {
                 const int k = group * kGroup + i;
-                float v[V], to_drive = 0.0f, to_step = 0.0f;
-                const float drive = step[i] * in[i];
+                const F2 steps = both(step[i]), drive = both(step[i] * in[i]), dvs = both(dv[i]);
+                const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
+                const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(s_c + k * N + n0);
+                F2 drives = both(0.0f), slopes = both(0.0f);
+                float v[V];
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const float after = i + 1 < kGroup ? before[i + 1 < kGroup ? i + 1 : i][p] : h[p];
-                    g[p] = fmaf(dv[i], s_c[k * N + n0 + p], g[p]);
-                    v[p] = g[p] * drive;
-                    v[P + p] = dv[i] * after;
-                    to_drive = fmaf(g[p], s_b[k * N + n0 + p], to_drive);
-                    g[p] *= keep[i][p];
-                    const float e = g[p] * before[i][p];
-                    to_step = fmaf(e, rate[p], to_step);
-                    da[p] = fmaf(e, step[i], da[p]);
+                for (int q = 0; q < P / 4; ++q) {
+                    const ulonglong2 bv = bk[q], cv = ck[q];
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int p = 2 * q + w;
+                        g[p] = fma(dvs, F2{w ? cv.y : cv.x}, g[p]);
+                        split(mul(g[p], drive), v[2 * p], v[2 * p + 1]);
+                        split(mul(dvs, i + 1 < kGroup ? before[i + 1 < kGroup ? i + 1 : i][p] : h[p]), v[P + 2 * p], v[P + 2 * p + 1]);
+                        drives = fma(g[p], F2{w ? bv.y : bv.x}, drives);
+                        g[p] = mul(g[p], keep[i][p]);
+                        const F2 e = mul(g[p], before[i][p]);
+                        slopes = fma(e, rate[p], slopes);
+                        da[p] = fma(e, steps, da[p]);
+                    }
                 }
+                float to_drive = sum2(drives), to_step = sum2(slopes);
 #pragma unroll
                 for (int o = 1; o < LANES; o <<= 1) {
                     to_drive += __shfl_xor_sync(0xffffffffu, to_drive, o);
                     to_step += __shfl_xor_sync(0xffffffffu, to_step, o);
                 }
-                if (writes && k < count) {
-                    const float raw = load(delta, a.delta.ld, k) + bias;
-                    const float dd = fmaf(to_drive, in[i], to_step * kLn2) * sigmoid(raw);
-                    PGT_STORE(du[k * a.du.ld], Elem<H>::down(fmaf(to_drive, step[i], skip * dv[i])));
-                    PGT_STORE(ddelta[k * a.ddelta.ld], Elem<H>::down(dd));
-                    if (dz) PGT_STORE(dz[k * a.dz.ld], Elem<H>::down(slope_z[i]));
+                if (n0 == 0) {                         // what the outputs are made of, in the places of what is used up
+                    s_dv[k * CH + c] = fmaf(to_drive, step[i], skip * dv[i]);
+                    s_step[k * CH + c] = fmaf(to_drive, in[i], to_step * kLn2) * slope_of_step(step[i]);
+                    if (gated) s_dz[k * CH + c] = to_z[i];
                     dskip = fmaf(dv[i], in[i], dskip);
-                    dbias += dd;
                 }
-                const int at = scatter_sums<LANES>(v);
+                const int from = scatter_sums<LANES>(v);
 #pragma unroll
-                for (int j = 0; j < kKept; ++j)
+                for (int w = 0; w < kKept; ++w)
                     if (V >= G || (lane & (G / V * LANES - 1)) < LANES)   // (of lanes that hold the same sum the first)
-                        s_red[(warp * kGroup + i) * 2 * N + (at + j < P ? n0 + at + j : N + n0 + at + j - P)] = v[j];
+                        red[i * 2 * N + (from + w < P ? n0 + from + w : N + n0 + from + w - P)] = v[w];
             }
-            __syncthreads();
+            __syncthreads();                           // (what the group before this one left is read by now)
             for (int i = threadIdx.x; i < kGroup * 2 * N; i += kScanThreads) {
                 const int k = group * kGroup + i / (2 * N);
+                const float* from = reds + i;
                 float v = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kScanThreads / 32; ++w) v += s_red[w * kGroup * 2 * N + i];
-                if (k < count) PGT_STORE(my_parts[(first + t0 + k) * 2 * N + i % (2 * N)], v);
+                for (int w = 0; w < kWarps; ++w) v += from[w * kGroup * 2 * N];
+                if (k < count) PGT_STORE(my_parts[(at + k) * 2 * N + i % (2 * N)], v);
             }
-            __syncthreads();
+            if constexpr (kSlots > 1) __syncthreads(); // (the next group's sums go over these)
         }
-        for (int k = count; k < t1 - t0; ++k) {
-            if (writes) {
-                PGT_STORE(du[k * a.du.ld], static_cast<uint16_t>(0));
-                PGT_STORE(ddelta[k * a.ddelta.ld], static_cast<uint16_t>(0));
-                if (dz) PGT_STORE(dz[k * a.dz.ld], static_cast<uint16_t>(0));
+        __syncthreads();
+        if (step_d < a.channels) {                     // outputs, rows behind the last token as zeros
+            auto rows_of = [&](const pg_matrix& m) { return static_cast<uint16_t*>(m.data) + b * m.stride + (at + threadIdx.x / CH) * m.ld + step_d; };
+            uint16_t *du = rows_of(a.du), *ddelta = rows_of(a.ddelta), *dz = gated ? rows_of(a.dz) : nullptr;
+#pragma unroll 2
+            for (int k = threadIdx.x / CH; k < t1 - t0; k += LANES) {
+                const int s_at = k * CH + threadIdx.x % CH;
+                const bool is_there = k < count;
+                const float dd = is_there ? s_step[s_at] : 0.0f;
+                dbias += dd;
+                PGT_STORE(du[0], Elem<H>::down(is_there ? s_dv[s_at] : 0.0f));
+                PGT_STORE(ddelta[0], Elem<H>::down(dd));
+                if (gated) PGT_STORE(dz[0], Elem<H>::down(is_there ? s_dz[s_at] : 0.0f));
+                du += LANES * a.du.ld;
+                ddelta += LANES * a.ddelta.ld;
+                if (gated) dz += LANES * a.dz.ld;
             }
-            for (int i = threadIdx.x; i < 2 * N; i += kScanThreads) PGT_STORE(my_parts[(first + t0 + k) * 2 * N + i], 0.0f);
         }
+        for (int i = count * 2 * N + threadIdx.x; i < (t1 - t0) * 2 * N; i += kScanThreads) PGT_STORE(my_parts[at * 2 * N + i], 0.0f);
     }
-    float* mine = partial + (static_cast<int64_t>(blockIdx.x) * a.channels + d) * (a.states + 2);
+    __syncthreads();
+    s_step[threadIdx.x] = dbias;                       // of channel threadIdx.x % CH
+    __syncthreads();
+    dbias = 0.0f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-        if (is && n0 + p < a.states) PGT_STORE(mine[n0 + p], da[p]);
-    if (writes) {
+    for (int i = 0; i < LANES; ++i) dbias += s_step[i * CH + c];
+    float* mine = partial + (static_cast<int64_t>(blockIdx.x) * a.channels + d) * (a.states + 2);
+    store_states<P>(mine + n0, there, false, da);
+    if (is && n0 == 0) {
         PGT_STORE(mine[a.states], dskip);
         PGT_STORE(mine[a.states + 1], dbias);
     }
@@ -932,7 +1056,17 @@ GradPlan grad_plan(const pg_scan_grad_args& a) {
     p.chunk = static_cast<int>((length + p.chunks - 1) / p.chunks);
     p.blocks = (int64_t{a.channels} * p.lanes + kScanThreads - 1) / kScanThreads;
     const int64_t items = int64_t{a.sequences} * p.chunks;
-    p.shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(items, int64_t{kSMs} * 6 / std::max<int64_t>(1, p.blocks * a.batch))));
+    // Shares of a worker's chunks: those whose waves of blocks take the fewest steps of a chunk, a block's start and end counted as a third of one.
+    double least = 0.0;
+    p.shares = 1;
+    for (int64_t s = 1; s <= std::min<int64_t>(items, 64); ++s) {
+        const double waves = static_cast<double>((p.blocks * a.batch * s + kSMs * kGradBlocks - 1) / (kSMs * kGradBlocks));
+        const double cost = waves * (static_cast<double>((items + s - 1) / s) + 0.33);
+        if (s == 1 || cost < least) {
+            least = cost;
+            p.shares = static_cast<int>(s);
+        }
+    }
     const size_t all = static_cast<size_t>(a.batch) * items;
     auto round = [](size_t n) { return (n + 255) / 256 * 256; };
     p.states = p.chunks > 1 ? round(sizeof(float) * all * a.channels * a.states) : 0;         // and as much for the carries
@@ -1204,8 +1338,7 @@ int pg_selective_scan_grad(const pg_scan_grad_args* args, void* workspace, size_
                 join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
                     a.a, a.state, states, carries, sums, a.sequences, a.channels, a.states, p.chunks);
             }
-            const int groups = (p.chunk + kGroup - 1) / kGroup, n = kGradStates * LANES;
-            const size_t smem = sizeof(float) * (2 * groups * kGroup * n + groups * kGradStates * kScanThreads + kScanThreads / 32 * kGroup * 2 * n);
+            const size_t smem = GradLayout<LANES>((p.chunk + kGroup - 1) / kGroup * kGroup).all;
             const auto kernel = scan_grad_kernel<H, LANES>;
             if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
                 cudaGetLastError();
