@@ -1,5 +1,6 @@
 // Operators along the tokens of a sequence: the short causal convolution of every channel, the selective scan, and their gradients.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "pg_train_device.h"
@@ -18,204 +19,252 @@ __device__ __forceinline__ int tokens_of(const int32_t* lengths, int64_t b, int 
     return lengths ? max(0, min(length, PGT_LOAD(lengths[b * sequences + s]))) : length;
 }
 
-// ---------------------------------------------------------------- convolution
-// A thread has eight neighbouring channels and runs along up to kRun tokens of one sequence, with the inputs of the last
-// width - 1 tokens in registers: every input is read once, but for the few before a run.  A block's four warps have runs of
-// their own.  Bound by memory, 4 bytes a value (6 in the gradient).
-constexpr int kRun = 64;
-constexpr int kConvThreads = 128;
+__device__ __forceinline__ void copy16(void* shared, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait_but_last() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Inputs at token t of the sequence that starts in row r0: of x, or for t < 0 of the state before it.
-template <typename H, int W>
-__device__ __forceinline__ void input_at(const uint16_t* x, int64_t ld, const uint16_t* state, int t, int taps, int col, int cols, F2 (&v)[4]) {
-    if (t >= 0) {
+// Rows of CH neighbouring elements of a 16-bit matrix in shared memory, as the 16-byte pieces of memory that hold them: a row starts as far
+// into its first piece as it does in memory.
+template <int CH>
+struct Rows {
+    static constexpr int kPieces = CH / 8 + 1;
+    const uint16_t* x;                                 // first row's first element
+    int64_t ld;
+    __device__ Rows() : x(nullptr), ld(0) {}
+    __device__ Rows(const pg_matrix& m, int64_t b, int64_t row, int col) : ld(m.ld) {
+        x = static_cast<const uint16_t*>(m.data) + b * m.stride + row * m.ld + col;
+    }
+    __device__ int off(int t) const { return static_cast<int>((reinterpret_cast<uintptr_t>(x) / 2 + static_cast<uint32_t>(t) * static_cast<uint32_t>(ld)) & 7); }
+    // Asks for pieces at, at + 8, .. of row t, which has n elements.
+    __device__ void ask(uint4* to, int t, int at, int n) const {
         const uint16_t* row = x + t * ld;
-        widen<H>(octet<W>(load_oct<W>(row, col, cols), row, col, cols), v);
-    } else {
-        const uint16_t* row = state + static_cast<int64_t>(taps - 1 + t) * cols;
+        const int o = off(t);
+        const uint4* from = reinterpret_cast<const uint4*>(row - o);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = col + 2 * i;
-            v[i] = pair(state && c < cols ? Elem<H>::up(PGT_LOAD(row[c])) : 0.0f, state && c + 1 < cols ? Elem<H>::up(PGT_LOAD(row[c + 1])) : 0.0f);
+        for (int i = 0; i < kPieces; i += 8)
+            if (i + at < kPieces && 8 * (i + at) < o + n && PGT_READ(from + i + at, 16)) copy16(to + i + at, from + i + at);
+    }
+    __device__ uint16_t get(const uint4* held, int t, int c) const { return reinterpret_cast<const uint16_t*>(held)[off(t) + c]; }
+};
+
+// ---------------------------------------------------------------- convolution
+// A warp has 64 neighbouring channels, a lane two of them, and runs along the tokens of (a part of) one sequence, with the inputs of
+// the last width - 1 tokens in registers: every input is read once, but for the few before a run.  Inputs come through shared memory in
+// 16-byte pieces, whatever the rows' alignment, a tile of tokens ahead.  Bound by memory, 4 bytes a value (6 in the gradient).
+constexpr int kRun = 64;                               // tokens of a run at most
+constexpr int kConvThreads = 128;
+constexpr int kStrip = 64;                             // channels
+constexpr int kConvTile = 8;                           // tokens
+
+// A lane's two channels.  W = 2: the output's rows start on 4-byte boundaries, and they are neighbours.  W = 1: 32 apart, so that
+// a warp's 2-byte accesses touch neighbouring elements.
+template <int W>
+struct Two {
+    static constexpr int kApart = W == 2 ? 1 : 32;
+    int c;
+    bool first, second;
+    __device__ explicit Two(int channels) : c((threadIdx.x & 31) * W) {
+        first = c < channels;
+        second = c + kApart < channels;
+    }
+    __device__ uint32_t load(const uint16_t* row) const {
+        const uint32_t lo = first ? PGT_LOAD(row[c]) : 0, hi = second ? PGT_LOAD(row[c + kApart]) : 0;
+        return lo | hi << 16;
+    }
+    template <int CH>
+    __device__ uint32_t get(const Rows<CH>& rows, const uint4* held, int t) const {
+        const uint32_t lo = rows.get(held, t, c), hi = rows.get(held, t, c + kApart);
+        return lo | hi << 16;
+    }
+    template <bool PAIRS = W == 2>
+    __device__ void store(uint16_t* row, uint32_t w) const {
+        if (PAIRS && second) {
+            PGT_STORE(*reinterpret_cast<uint32_t*>(row + c), w);
+        } else {
+            if (first) PGT_STORE(row[c], static_cast<uint16_t>(w & 0xffffu));
+            if (second) PGT_STORE(row[c + kApart], static_cast<uint16_t>(w >> 16));
         }
     }
-}
-// A thread's taps, [tap][pair of channels], and biases.
-template <int TAPS>
-__device__ __forceinline__ void load_taps(const pg_matrix& weight, const float* bias, int64_t bias_stride, int64_t b, int col, int cols, F2 (&w)[TAPS][4], F2 (&o)[4]) {
-    const float* base = static_cast<const float*>(weight.data) + b * weight.stride;
-    const float* add = bias ? bias + b * bias_stride : nullptr;
+    __device__ F2 numbers(const float* from, int64_t step) const { return pair(first ? PGT_LOAD(from[c * step]) : 0.0f, second ? PGT_LOAD(from[(c + kApart) * step]) : 0.0f); }
+};
+
+struct ConvPlace {
+    int64_t b, sequence;                               // sequence: of all workers
+    int have;                                          // tokens that are there
+    int64_t row;                                       // of the first token, in a worker's matrix
+    template <typename Args>
+    __device__ ConvPlace(const Args& a, int64_t of_all) : sequence(of_all) {
+        b = of_all / a.sequences;
+        const int s = static_cast<int>(of_all % a.sequences);
+        have = tokens_of(a.lengths, b, a.sequences, s, a.length);
+        row = static_cast<int64_t>(s) * a.length;
+    }
+    __device__ uint16_t* at(const pg_matrix& m, int col) const { return static_cast<uint16_t*>(m.data) + b * m.stride + row * m.ld + col; }
+};
+// Asks for the rows of a tile from token t on, of those before `stop`, eight lanes a row.
+__device__ __forceinline__ void ask_tile(const Rows<kStrip>& rows, uint4* to, int t, int stop, int n) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = col + 2 * i;
-#pragma unroll
-        for (int j = 0; j < TAPS; ++j)
-            w[j][i] = pair(c < cols ? PGT_LOAD(base[c * weight.ld + j]) : 0.0f, c + 1 < cols ? PGT_LOAD(base[(c + 1) * weight.ld + j]) : 0.0f);
-        o[i] = pair(add && c < cols ? PGT_LOAD(add[c]) : 0.0f, add && c + 1 < cols ? PGT_LOAD(add[c + 1]) : 0.0f);
+    for (int r = 0; r < kConvTile; r += 4) {
+        const int k = r + (threadIdx.x & 31) / 8;
+        if (t + k < stop) rows.ask(to + k * Rows<kStrip>::kPieces, t + k, threadIdx.x & 7, n);
     }
 }
 
-template <typename H, int W, int WO, int TAPS, int ACT>
+template <typename H, int W, int TAPS, int ACT>
 __global__ void __launch_bounds__(kConvThreads)
 conv_kernel(const pg_conv_args a, int run, int runs) {
-    const int col = (blockIdx.y * 32 + (threadIdx.x & 31)) * 8;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    const int64_t sequence = item / runs;              // of all workers
-    if (sequence >= static_cast<int64_t>(a.batch) * a.sequences || col >= a.channels) return;
-    const int64_t b = sequence / a.sequences;
-    const int s = static_cast<int>(sequence % a.sequences);
-    const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
-    const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run);
-    const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + static_cast<int64_t>(s) * a.length * a.x.ld;
-    uint16_t* y = static_cast<uint16_t*>(a.y.data) + b * a.y.stride + static_cast<int64_t>(s) * a.length * a.y.ld;
-    const int64_t held = sequence * (TAPS - 1) * a.channels;
+    __shared__ __align__(16) uint4 s_in[kConvThreads / 32][2][kConvTile * Rows<kStrip>::kPieces];
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), of_all = item / runs;
+    if (of_all >= static_cast<int64_t>(a.batch) * a.sequences) return;
+    const int col = blockIdx.y * kStrip, n = min(kStrip, a.channels - col);
+    const Two<W> two(n);
+    const ConvPlace at(a, of_all);
+    const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run), stop = min(t1, at.have);
+    uint4(&ring)[2][kConvTile * Rows<kStrip>::kPieces] = s_in[threadIdx.x >> 5];
+    const Rows<kStrip> rows(a.x, at.b, at.row, col);
+    ask_tile(rows, ring[0], t0, stop, n);
+    copies_end();
+    const uint16_t* x = at.at(a.x, col);
+    uint16_t* y = at.at(a.y, col) + t0 * a.y.ld;
+    const int64_t held = at.sequence * (TAPS - 1) * a.channels + col;
     const uint16_t* state = a.state ? static_cast<const uint16_t*>(a.state) + held : nullptr;
-    F2 w[TAPS][4], o[4], before[TAPS - 1][4];
-    load_taps<TAPS>(a.weight, a.bias, a.bias_stride, b, col, a.channels, w, o);
+    auto input = [&](int t) { return t >= 0 ? two.load(x + t * a.x.ld) : state ? two.load(state + static_cast<int64_t>(TAPS - 1 + t) * a.channels) : 0u; };
+    F2 w[TAPS], o = both(0.0f), before[TAPS - 1];
+    const float* weights = static_cast<const float*>(a.weight.data) + at.b * a.weight.stride + col * a.weight.ld;
 #pragma unroll
-    for (int j = 0; j < TAPS - 1; ++j)
-        if (t0 == 0 || t0 < have) input_at<H, W>(x, a.x.ld, state, t0 - (TAPS - 1) + j, TAPS, col, a.channels, before[j]);
-    if (t0 == 0 && a.state_out) {                      // the last inputs of the sequence; this thread has read the old ones
+    for (int j = 0; j < TAPS; ++j) w[j] = two.numbers(weights + j, a.weight.ld);
+    if (a.bias) o = two.numbers(a.bias + at.b * a.bias_stride + col, 1);
+#pragma unroll
+    for (int j = 0; j < TAPS - 1; ++j) before[j] = t0 == 0 || t0 < at.have ? Elem<H>::up2(input(t0 - (TAPS - 1) + j)) : both(0.0f);
+    if (t0 == 0 && a.state_out) {                      // the last inputs of the sequence; only this lane reads the old ones
         uint16_t* out = static_cast<uint16_t*>(a.state_out) + held;
-        F2 last[TAPS - 1][4];
+        uint32_t last[TAPS - 1];
 #pragma unroll
-        for (int j = 0; j < TAPS - 1; ++j) input_at<H, W>(x, a.x.ld, state, have - (TAPS - 1) + j, TAPS, col, a.channels, last[j]);
+        for (int j = 0; j < TAPS - 1; ++j) last[j] = input(at.have - (TAPS - 1) + j);
 #pragma unroll
-        for (int j = 0; j < TAPS - 1; ++j) store_oct<H, 1>(out + j * a.channels, col, a.channels, last[j]);
+        for (int j = 0; j < TAPS - 1; ++j) two.template store<false>(out + static_cast<int64_t>(j) * a.channels, last[j]);
     }
-    const int stop = min(t1, have);
-    constexpr int U = 4;                               // tokens on their way at once
-    int t = t0;
-    for (; t < stop; t += U) {
-        Piece<W> p[U];
+    for (int t = t0, stage = 0; t < stop; t += kConvTile, stage ^= 1) {
+        ask_tile(rows, ring[stage ^ 1], t + kConvTile, stop, n);
+        copies_end();
+        copies_wait_but_last();
+        __syncwarp();
 #pragma unroll
-        for (int u = 0; u < U; ++u) p[u] = load_oct<W>(x + (t + u) * a.x.ld, col, t + u < stop ? a.channels : 0);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < kConvTile; ++u) {
             if (t + u >= stop) break;
-            F2 v[4], z[4];
-            const uint16_t* row = x + (t + u) * a.x.ld;
-            widen<H>(octet<W>(p[u], row, col, a.channels), v);
+            const F2 v = Elem<H>::up2(two.get(rows, ring[stage] + u * Rows<kStrip>::kPieces, t + u));
+            F2 z = o;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                z[i] = o[i];
+            for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j], w[j], z);
+            z = activate<ACT>(fma(v, w[TAPS - 1], z));
 #pragma unroll
-                for (int j = 0; j < TAPS - 1; ++j) z[i] = fma(before[j][i], w[j][i], z[i]);
-                z[i] = activate<ACT>(fma(v[i], w[TAPS - 1][i], z[i]));
-#pragma unroll
-                for (int j = 0; j + 1 < TAPS - 1; ++j) before[j][i] = before[j + 1][i];
-                before[TAPS - 2][i] = v[i];
-            }
-            store_oct<H, WO>(y + (t + u) * a.y.ld, col, a.channels, z);
+            for (int j = 0; j + 1 < TAPS - 1; ++j) before[j] = before[j + 1];
+            before[TAPS - 2] = v;
+            two.store(y, Elem<H>::down2(z));
+            y += a.y.ld;
         }
+        __syncwarp();
     }
-    const F2 none[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
-    for (t = max(t0, stop); t < t1; ++t) store_oct<H, WO>(y + t * a.y.ld, col, a.channels, none);
+    for (int t = max(t0, stop); t < t1; ++t, y += a.y.ld) two.store(y, 0);
 }
 
 // The gradient.  dx of token t needs the pre-activations' gradients up to token t + TAPS - 1: a run recomputes those of the
-// tokens behind it.  Sums over tokens: a thread's run, the four warps of the block (shared memory), then the blocks, whose sums
+// tokens behind it.  Sums over tokens: a thread's runs, the four warps of the block (shared memory), then the blocks, whose sums
 // go to partial[worker][part][TAPS + 1][channels], the bias last.
-template <typename H, int W, int WO, int TAPS, int ACT>
+template <typename H, int W, int TAPS, int ACT>
 __global__ void __launch_bounds__(kConvThreads)
 conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run, int runs, int parts) {
-    __shared__ float s_sum[4][TAPS + 1][256];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int col = (blockIdx.y * 32 + lane) * 8;
+    __shared__ __align__(16) uint4 s_in[kConvThreads / 32][2][2][kConvTile * Rows<kStrip>::kPieces];
+    __shared__ float s_sum[4][TAPS + 1][kStrip];
+    const int warp = threadIdx.x >> 5, col = blockIdx.y * kStrip, n = min(kStrip, a.channels - col);
     const int64_t b = blockIdx.x / parts;
     const int part = static_cast<int>(blockIdx.x % parts);
     const int64_t items = static_cast<int64_t>(a.sequences) * runs;      // of a worker
-    F2 dw[TAPS][4], db[4];
+    const Two<W> two(n);
+    F2 w[TAPS], o = both(0.0f), dw[TAPS], db = both(0.0f);
+    const float* weights = static_cast<const float*>(a.weight.data) + b * a.weight.stride + col * a.weight.ld;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        db[i] = both(0.0f);
-#pragma unroll
-        for (int j = 0; j < TAPS; ++j) dw[j][i] = both(0.0f);
+    for (int j = 0; j < TAPS; ++j) {
+        w[j] = two.numbers(weights + j, a.weight.ld);
+        dw[j] = both(0.0f);
     }
-    if (col < a.channels) {
-        F2 w[TAPS][4], o[4];
-        load_taps<TAPS>(a.weight, a.bias, a.bias_stride, b, col, a.channels, w, o);
-        for (int64_t item = part * 4 + warp; item < items; item += 4 * parts) {
-            const int s = static_cast<int>(item / runs);
-            const int64_t sequence = b * a.sequences + s;
-            const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
-            const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run);
-            const int64_t first = static_cast<int64_t>(s) * a.length;
-            const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + b * a.x.stride + first * a.x.ld;
-            const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + first * a.dy.ld;
-            uint16_t* dx = static_cast<uint16_t*>(a.dx.data) + b * a.dx.stride + first * a.dx.ld;
-            const uint16_t* state = a.state ? static_cast<const uint16_t*>(a.state) + sequence * (TAPS - 1) * a.channels : nullptr;
-            const int own = min(t1, have);             // tokens to own have sums here
-            if (t0 < own) {
-                F2 before[TAPS - 1][4], dz[TAPS - 1][4];
+    if (a.bias) o = two.numbers(a.bias + b * a.bias_stride + col, 1);
+    for (int64_t item = part * 4 + warp; item < items; item += 4 * parts) {
+        const ConvPlace at(a, b * a.sequences + item / runs);
+        const int t0 = static_cast<int>(item % runs) * run, t1 = min(a.length, t0 + run);
+        const int own = min(t1, at.have), end = own + TAPS - 1, stop = min(at.have, end);        // tokens to own have sums here, those to stop count for dx
+        uint16_t* dx = at.at(a.dx, col) + t0 * a.dx.ld;
+        if (t0 < own) {
+            const Rows<kStrip> rx(a.x, at.b, at.row, col), rd(a.dy, at.b, at.row, col);
+            ask_tile(rx, s_in[warp][0][0], t0, stop, n);
+            ask_tile(rd, s_in[warp][0][1], t0, stop, n);
+            copies_end();
+            const uint16_t* x = at.at(a.x, col);
+            const uint16_t* state = a.state ? static_cast<const uint16_t*>(a.state) + at.sequence * (TAPS - 1) * a.channels + col : nullptr;
+            F2 before[TAPS - 1], dz[TAPS - 1];
 #pragma unroll
-                for (int j = 0; j < TAPS - 1; ++j) {
-                    input_at<H, W>(x, a.x.ld, state, t0 - (TAPS - 1) + j, TAPS, col, a.channels, before[j]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) dz[j][i] = both(0.0f);
-                }
-                const int stop = min(have, own + TAPS - 1);              // and those behind, for dx alone
-                constexpr int U = 2;
-                for (int t = t0; t < own + TAPS - 1; t += U) {
-                    Piece<W> px[U], pd[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        px[u] = load_oct<W>(x + (t + u) * a.x.ld, col, t + u < stop ? a.channels : 0);
-                        pd[u] = load_oct<W>(dy + (t + u) * a.dy.ld, col, t + u < stop ? a.channels : 0);
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int at = t + u, to = at - (TAPS - 1);
-                        if (at >= own + TAPS - 1) break;
-                        F2 v[4], g[4], out[4];
-                        widen<H>(octet<W>(px[u], x + at * a.x.ld, col, at < stop ? a.channels : 0), v);
-                        widen<H>(octet<W>(pd[u], dy + at * a.dy.ld, col, at < stop ? a.channels : 0), g);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if constexpr (ACT != PG_ACT_NONE) {
-                                F2 z = o[i];
-#pragma unroll
-                                for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j][i], w[j][i], z);
-                                z = fma(v[i], w[TAPS - 1][i], z);
-                                if (at < stop) g[i] = mul(g[i], slope<ACT>(z));
-                            }
-                            if (at < own) {
-                                db[i] = add(db[i], g[i]);
-#pragma unroll
-                                for (int j = 0; j < TAPS - 1; ++j) dw[j][i] = fma(g[i], before[j][i], dw[j][i]);
-                                dw[TAPS - 1][i] = fma(g[i], v[i], dw[TAPS - 1][i]);
-                            }
-                            // dz holds the gradients of tokens at - (TAPS - 1) to at - 1
-                            out[i] = mul(g[i], w[0][i]);
-#pragma unroll
-                            for (int j = 0; j < TAPS - 1; ++j) out[i] = fma(dz[j][i], w[TAPS - 1 - j][i], out[i]);
-#pragma unroll
-                            for (int j = 0; j + 1 < TAPS - 1; ++j) {
-                                before[j][i] = before[j + 1][i];
-                                dz[j][i] = dz[j + 1][i];
-                            }
-                            before[TAPS - 2][i] = v[i];
-                            dz[TAPS - 2][i] = g[i];
-                        }
-                        if (to >= t0) store_oct<H, WO>(dx + to * a.dx.ld, col, a.channels, out);
-                    }
-                }
+            for (int j = 0; j < TAPS - 1; ++j) {
+                const int t = t0 - (TAPS - 1) + j;
+                before[j] = Elem<H>::up2(t >= 0 ? two.load(x + t * a.x.ld) : state ? two.load(state + static_cast<int64_t>(TAPS - 1 + t) * a.channels) : 0u);
+                dz[j] = both(0.0f);
             }
-            const F2 none[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
-            for (int t = max(t0, own); t < t1; ++t) store_oct<H, WO>(dx + t * a.dx.ld, col, a.channels, none);
+            for (int t = t0, stage = 0; t < end; t += kConvTile, stage ^= 1) {
+                ask_tile(rx, s_in[warp][stage ^ 1][0], t + kConvTile, stop, n);
+                ask_tile(rd, s_in[warp][stage ^ 1][1], t + kConvTile, stop, n);
+                copies_end();
+                copies_wait_but_last();
+                __syncwarp();
+#pragma unroll
+                for (int u = 0; u < kConvTile; ++u) {
+                    if (t + u >= end) break;
+                    F2 v = both(0.0f), g = both(0.0f); // behind the last token: zeros
+                    if (t + u < stop) {
+                        v = Elem<H>::up2(two.get(rx, s_in[warp][stage][0] + u * Rows<kStrip>::kPieces, t + u));
+                        g = Elem<H>::up2(two.get(rd, s_in[warp][stage][1] + u * Rows<kStrip>::kPieces, t + u));
+                        if constexpr (ACT != PG_ACT_NONE) {
+                            F2 z = o;
+#pragma unroll
+                            for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j], w[j], z);
+                            g = mul(g, slope<ACT>(fma(v, w[TAPS - 1], z)));
+                        }
+                    }
+                    if (t + u < own) {
+                        db = add(db, g);
+#pragma unroll
+                        for (int j = 0; j < TAPS - 1; ++j) dw[j] = fma(g, before[j], dw[j]);
+                        dw[TAPS - 1] = fma(g, v, dw[TAPS - 1]);
+                    }
+                    F2 out = mul(g, w[0]);             // dz holds the gradients of the TAPS - 1 tokens before this one, the oldest first
+#pragma unroll
+                    for (int j = 0; j < TAPS - 1; ++j) out = fma(dz[j], w[TAPS - 1 - j], out);
+#pragma unroll
+                    for (int j = 0; j + 1 < TAPS - 1; ++j) {
+                        before[j] = before[j + 1];
+                        dz[j] = dz[j + 1];
+                    }
+                    before[TAPS - 2] = v;
+                    dz[TAPS - 2] = g;
+                    if (t + u - (TAPS - 1) >= t0) {
+                        two.store(dx, Elem<H>::down2(out));
+                        dx += a.dx.ld;
+                    }
+                }
+                __syncwarp();
+            }
         }
+        for (int t = max(t0, own); t < t1; ++t, dx += a.dx.ld) two.store(dx, 0);
     }
+    copies_wait();                                     // (the last, empty group)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int j = 0; j < TAPS; ++j) split(dw[j][i], s_sum[warp][j][lane * 8 + 2 * i], s_sum[warp][j][lane * 8 + 2 * i + 1]);
-        split(db[i], s_sum[warp][TAPS][lane * 8 + 2 * i], s_sum[warp][TAPS][lane * 8 + 2 * i + 1]);
-    }
+    for (int j = 0; j <= TAPS; ++j) split(j < TAPS ? dw[j < TAPS ? j : 0] : db, s_sum[warp][j][two.c], s_sum[warp][j][two.c + Two<W>::kApart]);
     __syncthreads();
-    float* out = partial + static_cast<int64_t>(blockIdx.x) * (TAPS + 1) * a.channels;
-    for (int i = threadIdx.x; i < (TAPS + 1) * 256; i += kConvThreads) {
-        const int j = i >> 8, c = i & 255, at = blockIdx.y * 256 + c;
-        if (at < a.channels) PGT_STORE(out[static_cast<int64_t>(j) * a.channels + at], s_sum[0][j][c] + s_sum[1][j][c] + s_sum[2][j][c] + s_sum[3][j][c]);
+    float* out = partial + static_cast<int64_t>(blockIdx.x) * (TAPS + 1) * a.channels + col;
+    for (int i = threadIdx.x; i < (TAPS + 1) * kStrip; i += kConvThreads) {
+        const int j = i / kStrip, c = i % kStrip;
+        if (c < n) PGT_STORE(out[static_cast<int64_t>(j) * a.channels + c], (s_sum[0][j][c] + s_sum[1][j][c]) + (s_sum[2][j][c] + s_sum[3][j][c]));
     }
 }
 
@@ -277,35 +326,6 @@ __device__ __forceinline__ F2 softplus(F2 v) {          // of two
     p = fma(p, q, both(2.0f));
     return fma(s, p, pair(fmaxf(a, 0.0f), fmaxf(b, 0.0f)));
 }
-
-__device__ __forceinline__ void copy16(void* shared, const void* global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
-}
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-// Rows of CH neighbouring elements of a 16-bit matrix in shared memory, as the 16-byte pieces of memory that hold them: a row starts as far
-// into its first piece as it does in memory.
-template <int CH>
-struct Rows {
-    static constexpr int kPieces = CH / 8 + 1;
-    const uint16_t* x;                                 // first row's first element
-    int64_t ld;
-    __device__ Rows() : x(nullptr), ld(0) {}
-    __device__ Rows(const pg_matrix& m, int64_t b, int64_t row, int col) : ld(m.ld) {
-        x = static_cast<const uint16_t*>(m.data) + b * m.stride + row * m.ld + col;
-    }
-    __device__ int off(int t) const { return static_cast<int>((reinterpret_cast<uintptr_t>(x) / 2 + static_cast<uint32_t>(t) * static_cast<uint32_t>(ld)) & 7); }
-    // Asks for pieces at, at + 8, .. of row t, which has n elements.
-    __device__ void ask(uint4* to, int t, int at, int n) const {
-        const uint16_t* row = x + t * ld;
-        const int o = off(t);
-        const uint4* from = reinterpret_cast<const uint4*>(row - o);
-#pragma unroll
-        for (int i = 0; i < kPieces; i += 8)
-            if (i + at < kPieces && 8 * (i + at) < o + n && PGT_READ(from + i + at, 16)) copy16(to + i + at, from + i + at);
-    }
-    __device__ uint16_t get(const uint4* held, int t, int c) const { return reinterpret_cast<const uint16_t*>(held)[off(t) + c]; }
-};
 
 // A channel's states lie in LANES neighbouring threads, P each, in pairs.  A block takes CH channels of one sequence at a time, or of a
 // chunk of it (an item), in tiles of kScanTile tokens; the next tile is on its way while one is worked on.  Items are numbered by
@@ -1004,12 +1024,13 @@ void with_taps(int taps, F&& f) {
     else if (taps == 3) f(integral_constant<int, 3>{});
     else f(integral_constant<int, 4>{});
 }
+// Calls f with 2 if all rows of the matrix start on 4-byte boundaries, else with 1.
 template <typename F>
-void with_widths(int in, int out, F&& f) {
+void with_two(const pg_matrix& m, int64_t batch, F&& f) {
     using std::integral_constant;
-    if (out < 8) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    else if (in == 8) f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
-    else f(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    const uint64_t bits = reinterpret_cast<uintptr_t>(m.data) | static_cast<uint64_t>(m.ld) * 2 | (batch > 1 ? static_cast<uint64_t>(m.stride) * 2 : 0);
+    if (bits % 4 == 0) f(integral_constant<int, 2>{});
+    else f(integral_constant<int, 1>{});
 }
 template <typename F>
 void with_kind(int dtype, F&& f) {
@@ -1017,17 +1038,16 @@ void with_kind(int dtype, F&& f) {
     else f(__half{});
 }
 
-// Tokens of a thread's run: kRun, fewer where there would not be a block of four runs for each of an SM's eight places.
+int conv_strips(int channels) { return (channels + kStrip - 1) / kStrip; }
+// Tokens of a run: kRun, fewer where there would not be 32 runs for every SM.  (Shorter runs read more of what is before and behind them.)
 int conv_run(int64_t sequences, int64_t length, int64_t strips) {
     int run = static_cast<int>(std::min<int64_t>(kRun, std::max<int64_t>(length, 1)));
-    while (run > 8 && sequences * ((length + run - 1) / run) * strips < int64_t{kSMs} * 8 * 4) run = (run + 1) / 2;
+    while (run > 8 && sequences * ((length + run - 1) / run) * strips < int64_t{kSMs} * 32) run = (run + 1) / 2;
     return run;
 }
-// Blocks that share a worker's runs in the gradient.
+// Blocks that share a worker's runs in the gradient: one for every four runs, to 1024 (a block's sums are small beside what its runs read).
 int conv_parts(const pg_conv_grad_args& a, int runs) {
-    const int64_t strips = (a.channels + 255) / 256, items = int64_t{a.sequences} * runs;
-    const int64_t most = std::max<int64_t>(1, int64_t{kSMs} * 6 / std::max<int64_t>(1, strips * a.batch));
-    return static_cast<int>(std::max<int64_t>(1, std::min(most, (items + 3) / 4)));
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024, (int64_t{a.sequences} * runs + 3) / 4)));
 }
 
 struct ScanPlan { int chunk, chunks, tiles; int64_t items; };
@@ -1141,7 +1161,7 @@ int pg_causal_conv(const pg_conv_args* args, void* stream) {
     if ((a.lengths && !array_ok(a.lengths, 4, sequences, dev)) || (a.state && !array_ok(a.state, 2, held, dev)) ||
         (a.state_out && !array_ok(a.state_out, 2, held, dev)))
         return PG_ERR_INVALID;
-    const int strips = (a.channels + 255) / 256, run = conv_run(sequences, a.length, strips);
+    const int strips = conv_strips(a.channels), run = conv_run(sequences, a.length, strips);
     const int runs = std::max(1, (a.length + run - 1) / run);
     const int64_t blocks = (sequences * runs + 3) / 4;
     if (rc != PG_OK || blocks > kMaxBlocks) return PG_ERR_TOO_LARGE;
@@ -1155,13 +1175,13 @@ int pg_causal_conv(const pg_conv_args* args, void* stream) {
     span(operands, a.state, held * 2, false);
     if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     with_kind(a.dtype, [&](auto h) {
-        with_widths(access_width({&a.x}, a.batch), access_width({&a.y}, a.batch), [&](auto in, auto out) {
+        with_two(a.y, a.batch, [&](auto two) {
             with_taps(a.width, [&](auto taps) {
                 using H = decltype(h);
-                constexpr int W = decltype(in)::value, WO = decltype(out)::value, TAPS = decltype(taps)::value;
+                constexpr int W = decltype(two)::value, TAPS = decltype(taps)::value;
                 const dim3 grid(static_cast<unsigned>(blocks), strips);
-                if (a.activation == PG_ACT_SILU) conv_kernel<H, W, WO, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, run, runs);
-                else conv_kernel<H, W, WO, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, run, runs);
+                if (a.activation == PG_ACT_SILU) conv_kernel<H, W, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, run, runs);
+                else conv_kernel<H, W, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, run, runs);
             });
         });
     });
@@ -1173,7 +1193,7 @@ int pg_causal_conv_grad_workspace_bytes(const pg_conv_grad_args* args, size_t* b
     const pg_conv_grad_args& a = *args;
     const int rc = conv_check(a.dtype, a.activation, a.batch, a.sequences, a.length, a.channels, a.width);
     if (rc != PG_OK) return rc;
-    const int run = conv_run(int64_t{a.batch} * a.sequences, a.length, (a.channels + 255) / 256);
+    const int run = conv_run(int64_t{a.batch} * a.sequences, a.length, conv_strips(a.channels));
     *bytes_out = sizeof(float) * static_cast<size_t>(a.batch) * conv_parts(a, std::max(1, (a.length + run - 1) / run)) * (a.width + 1) * a.channels;
     return PG_OK;
 }
@@ -1195,7 +1215,7 @@ int pg_causal_conv_grad(const pg_conv_grad_args* args, void* workspace, size_t w
     if ((a.lengths && !array_ok(a.lengths, 4, sequences, dev)) || (a.state && !array_ok(a.state, 2, held, dev))) return PG_ERR_INVALID;
     if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
     if (a.batch == 0) return PG_OK;
-    const int strips = (a.channels + 255) / 256, run = conv_run(sequences, a.length, strips);
+    const int strips = conv_strips(a.channels), run = conv_run(sequences, a.length, strips);
     const int runs = std::max(1, (a.length + run - 1) / run), parts = conv_parts(a, runs);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     float* partial = static_cast<float*>(workspace);
@@ -1208,13 +1228,13 @@ int pg_causal_conv_grad(const pg_conv_grad_args* args, void* workspace, size_t w
     span(operands, a.state, held * 2, false);
     if (operands.publish(st) != PG_OK) return PG_ERR_CUDA;
     with_kind(a.dtype, [&](auto h) {
-        with_widths(access_width({&a.x, &a.dy}, a.batch), access_width({&a.dx}, a.batch), [&](auto in, auto out) {
+        with_two(a.dx, a.batch, [&](auto two) {
             with_taps(a.width, [&](auto taps) {
                 using H = decltype(h);
-                constexpr int W = decltype(in)::value, WO = decltype(out)::value, TAPS = decltype(taps)::value;
+                constexpr int W = decltype(two)::value, TAPS = decltype(taps)::value;
                 const dim3 grid(a.batch * parts, strips);
-                if (a.activation == PG_ACT_SILU) conv_grad_kernel<H, W, WO, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
-                else conv_grad_kernel<H, W, WO, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
+                if (a.activation == PG_ACT_SILU) conv_grad_kernel<H, W, TAPS, PG_ACT_SILU><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
+                else conv_grad_kernel<H, W, TAPS, PG_ACT_NONE><<<grid, kConvThreads, 0, st>>>(a, partial, run, runs, parts);
             });
         });
     });
