@@ -114,7 +114,7 @@ __device__ __forceinline__ void ask_tile(const Rows<kStrip>& rows, uint4* to, in
 }
 
 template <typename H, int W, int TAPS, int ACT>
-__global__ void __launch_bounds__(kConvThreads)
+__global__ void __launch_bounds__(kConvThreads, 8)
 conv_kernel(const pg_conv_args a, int run, int runs) {
     __shared__ __align__(16) uint4 s_in[kConvThreads / 32][2][kConvTile * Rows<kStrip>::kPieces];
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), of_all = item / runs;
@@ -152,7 +152,7 @@ conv_kernel(const pg_conv_args a, int run, int runs) {
         copies_end();
         copies_wait_but_last();
         __syncwarp();
-#pragma unroll
+#pragma unroll 4
         for (int u = 0; u < kConvTile; ++u) {
             if (t + u >= stop) break;
             const F2 v = Elem<H>::up2(two.get(rows, ring[stage] + u * Rows<kStrip>::kPieces, t + u));
@@ -175,7 +175,7 @@ conv_kernel(const pg_conv_args a, int run, int runs) {
 // tokens behind it.  Sums over tokens: a thread's runs, the four warps of the block (shared memory), then the blocks, whose sums
 // go to partial[worker][part][TAPS + 1][channels], the bias last.
 template <typename H, int W, int TAPS, int ACT>
-__global__ void __launch_bounds__(kConvThreads)
+__global__ void __launch_bounds__(kConvThreads, 5)
 conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run, int runs, int parts) {
     __shared__ __align__(16) uint4 s_in[kConvThreads / 32][2][2][kConvTile * Rows<kStrip>::kPieces];
     __shared__ float s_sum[4][TAPS + 1][kStrip];
@@ -217,7 +217,7 @@ conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run
                 copies_end();
                 copies_wait_but_last();
                 __syncwarp();
-#pragma unroll
+#pragma unroll 4
                 for (int u = 0; u < kConvTile; ++u) {
                     if (t + u >= end) break;
                     F2 v = both(0.0f), g = both(0.0f); // behind the last token: zeros
