@@ -354,7 +354,7 @@ PG_API int pg_selective_scan_grad(const pg_scan_grad_args *args, void *workspace
  *
  * The gradient dloss (alpha tau (q - p) + (1 - alpha) (softmax(x) - [label])) goes to dlogits: by pg_distillation_loss
  * together with the loss, reading the logits once (to 100000 classes; twice above), or by pg_distillation_loss_grad from lse,
- * which it reads.  At most 1024 entries in a list (PG_ERR_TOO_LARGE).
+ * which it reads (and whose step, 2^-24 of its size, is the error of the probabilities' logarithms then).  At most 1024 entries in a list (PG_ERR_TOO_LARGE).
  */
 typedef struct pg_distillation_args {
     int32_t dtype, batch, tokens, classes, top;

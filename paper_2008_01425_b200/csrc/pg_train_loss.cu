@@ -1,11 +1,11 @@
 // The distillation loss (pg_distillation_loss): softmax statistics of every row of logits and what a teacher's top
 // logits and a label make of them, forward, backward, and both with one read of the logits.
 //
-// One block has one row.  With k = log2(e) / tau a logit x counts 2^(k x - r), r a whole number near the largest k x that a thread
-// has seen: k x - r is then one fused multiply-add, and sums of different r are joined by exact powers of two.  A thread's r is that of its
-// first logits, and grows when one is kSlack above it: fp32 has room for what is between.  Where tau is 1, 2 or 4 the exponentials at temperature 1 are powers of these; elsewhere there
-// are two per logit.  With the gradient the row stays in shared memory as it was read, so the logits are read once.
-// Memory bounds all of it: 2 bytes a logit for the loss, 4 with the gradient.
+// A logit x counts 2^(k (x - r)), k = log2(e) / tau and r a logit near the largest that a thread has seen: that of its first ones,
+// until one is kSlack bits above it (fp32 has room for what is between).  The difference comes first, so that logits of any
+// size, a type's lowest number among them, are told apart as well as the type does.  Where tau is 1, 2 or 4 the exponentials at temperature 1
+// are powers of these; elsewhere there are two per logit.  With the gradient the row stays in shared memory as it was read, so the
+// logits are read once.  Memory bounds it, 2 bytes a logit for the loss and 4 with the gradient, and nearly as much the exponential unit.
 #include <algorithm>
 #include <type_traits>
 
@@ -16,13 +16,10 @@ namespace {
 
 constexpr int kWide = 256;                              // threads of the widest rows
 constexpr int kMaxTop = 1024;                          // entries of a teacher's list
-constexpr float kNoLogit = -1e30f;                     // r before the first logit; 2^(kNoLogit - r) is 0
+constexpr float kNoLogit = -3.4028235e38f;             // r before the first logit, below all that are numbers
 constexpr float kSlack = 20.0f;                        // (of the fourth power, 2^80 and a sum of as many as there are)
 constexpr size_t kMaxRowBytes = 200 * 1024;            // of a block's shared memory
 
-
-// v rounded to a whole number, by adding and taking off 1.5 * 2^23 (a number too large for that is one).
-__device__ __forceinline__ float whole(float v) { return fabsf(v) < 4194304.0f ? (v + kRound) - kRound : v; }
 
 // What a block knows of its row.  Logits lie in 16-byte pieces of memory: piece j holds elements 8 j - off to 8 j - off + 7.
 struct Row {
@@ -69,7 +66,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // With one of the two terms only, POWER is 1 and k belongs to that term.
 struct Sums {
     float r, s;        // at k
-    float r1, s1;      // at temperature 1, where POWER != 1
+    float s1;          // at temperature 1, where POWER != 1
 };
 template <int POWER>
 __device__ __forceinline__ F2 power(F2 e) {
@@ -79,7 +76,7 @@ __device__ __forceinline__ F2 power(F2 e) {
 }
 // The sums of N neighbouring lanes (of all of them the same), brought to the largest r.
 template <int POWER, int N>
-__device__ __forceinline__ Sums join(Sums m) {
+__device__ __forceinline__ Sums join(Sums m, float k) {
     auto over = [](float v, auto f) {
 #pragma unroll
         for (int o = N / 2; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -87,31 +84,29 @@ __device__ __forceinline__ Sums join(Sums m) {
     };
     auto most = [](float a, float b) { return fmaxf(a, b); };
     auto add = [](float a, float b) { return a + b; };
-    const float r = over(m.r, most), f = ex2(m.r - r);
+    const float r = over(m.r, most), d = m.r - r, f = ex2(d * k);
     m.s = over(m.s * f, add);
-    if constexpr (POWER == 0) {
-        const float r1 = over(m.r1, most);
-        m.s1 = over(m.s1 * ex2(m.r1 - r1), add);
-        m.r1 = r1;
+    if constexpr (POWER == 1) {
+        m.s1 = m.s;
     } else {
         float f1 = f;
+        if constexpr (POWER == 0) f1 = ex2(d * kLog2e);
         if constexpr (POWER > 1) f1 *= f1;
         if constexpr (POWER > 2) f1 *= f1;
-        m.s1 = POWER == 1 ? m.s : over(m.s1 * f1, add);
-        m.r1 = POWER * r;
+        m.s1 = over(m.s1 * f1, add);
     }
     m.r = r;
     return m;
 }
 // A warp's sums go to shared memory; after the block's barrier every warp adds them up, in the same order.
 template <int POWER>
-__device__ __forceinline__ void join_warp(const Sums& m, Sums* shared) {
-    const Sums all = join<POWER, 32>(m);
+__device__ __forceinline__ void join_warp(const Sums& m, float k, Sums* shared) {
+    const Sums all = join<POWER, 32>(m, k);
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = all;
 }
 template <int POWER, int WARPS>
-__device__ __forceinline__ Sums all_sums(const Sums* shared) {
-    return join<POWER, WARPS>(shared[threadIdx.x & (WARPS - 1)]);
+__device__ __forceinline__ Sums all_sums(const Sums* shared, float k) {
+    return join<POWER, WARPS>(shared[threadIdx.x & (WARPS - 1)], k);
 }
 
 // An octet is counted in.
@@ -121,30 +116,32 @@ __device__ __forceinline__ void count(Sums& m, F2& s, F2& s1, const F2 (&v)[4], 
 #pragma unroll
     for (int i = 0; i < 4; ++i) split(v[i], e[2 * i], e[2 * i + 1]);
     const float top = max3(max3(max3(e[0], e[1], e[2]), e[3], e[4]), max3(e[5], e[6], e[7]), e[0]);
-    if (top * k > m.r + kSlack) {
-        const float r = whole(top * k), f = ex2(m.r - r);
+    if ((top - m.r) * k > kSlack) {
+        const float d = m.r - top, f = ex2(d * k);
         s = mul(s, both(f));
         if constexpr (POWER > 1) s1 = mul(s1, power<POWER>(both(f)));
-        m.r = r;
+        if constexpr (POWER == 0) s1 = mul(s1, both(ex2(d * kLog2e)));
+        m.r = top;
     }
-    if constexpr (POWER == 0) {
-        if (top * kLog2e > m.r1 + kSlack) {
-            const float r1 = whole(top * kLog2e);
-            s1 = mul(s1, both(ex2(m.r1 - r1)));
-            m.r1 = r1;
+    if constexpr (POWER == 0) {                        // (at tau > 1 the exponentials at temperature 1 grow faster)
+        if ((top - m.r) * kLog2e > kSlack) {
+            const float d = m.r - top;
+            s = mul(s, both(ex2(d * k)));
+            s1 = mul(s1, both(ex2(d * kLog2e)));
+            m.r = top;
         }
     }
-    const F2 minus = both(-m.r), minus1 = both(-m.r1);
+    const F2 minus = both(-m.r);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const F2 x = ex2(fma(v[i], both(k), minus));
+        const F2 d = add(v[i], minus), x = ex2(mul(d, both(k)));
         s = add(s, x);
         if constexpr (POWER > 1) s1 = add(s1, power<POWER>(x));
-        if constexpr (POWER == 0) s1 = add(s1, ex2(fma(v[i], both(kLog2e), minus1)));
+        if constexpr (POWER == 0) s1 = add(s1, ex2(mul(d, both(kLog2e))));
     }
 }
 
-// The teacher's list of a row in shared memory: class (-1: none), probability, its logarithm (base 2), the student's logit.
+// The teacher's list of a row in shared memory: class (-1: none), probability, its logarithm, the student's logit.
 struct List {
     int* id;
     float *p, *log_p, *x;
@@ -168,18 +165,18 @@ __device__ __forceinline__ bool read_list(const pg_distillation_args& a, const R
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float r = fmaxf(whole(top * k), kNoLogit);
+    const float r = fmaxf(top, kNoLogit);
     float sum = 0.0f;
     for (int i = lane; i < a.top; i += 32) {
-        const float v = fmaf(list.log_p[i], k, -r), e = ex2(v);
-        list.log_p[i] = v;
+        const float v = list.log_p[i] - r, e = ex2(v * k);
+        list.log_p[i] = v * (k * kLn2);
         list.p[i] = e;
         sum += e;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const bool any = sum != 0.0f;                      // (NaN is something, too)
-    const float inverse = any ? 1.0f / sum : 0.0f, log_sum = any ? log2f(sum) : 0.0f;
+    const float inverse = any ? 1.0f / sum : 0.0f, log_sum = any ? log2f(sum) * kLn2 : 0.0f;
     for (int i = lane; i < a.top; i += 32) {
         list.p[i] *= inverse;
         list.log_p[i] -= log_sum;
@@ -188,13 +185,13 @@ __device__ __forceinline__ bool read_list(const pg_distillation_args& a, const R
 }
 
 // A row's constants on the way back: the gradient of a logit x is
-//     by 2^(k x - r) + by1 2^(k1 x - r1),  less what list and label take off at their classes.
+//     by 2^(k (x - r)) + by1 2^(log2(e) (x - r1)),  less what list and label take off at their classes (r1 = r but for POWER = 0 from lse).
 template <int POWER>
 struct Slope {
     float k, r, r1, by, by1;
-    __device__ F2 exponential(F2 x) const { return ex2(fma(x, both(k), both(-r))); }
+    __device__ F2 exponential(F2 x) const { return ex2(mul(add(x, both(-r)), both(k))); }
     __device__ F2 exponential1(F2 x, F2 e) const {
-        if constexpr (POWER == 0) return ex2(fma(x, both(kLog2e), both(-r1)));
+        if constexpr (POWER == 0) return ex2(mul(add(x, both(-r1)), both(kLog2e)));
         else return power<POWER>(e);
     }
     template <typename H>
@@ -278,23 +275,31 @@ template <typename H, int POWER>
 __device__ __forceinline__ void store_loss(const pg_distillation_args& a, int64_t at_row, const List& list, const Label<H>& label, const Sums& m, float k, float soft,
                                            float hard) {
     const int lane = threadIdx.x & 31;
-    const float log_s = log2f(m.s), log_s1 = POWER == 1 ? log_s : log2f(m.s1), k1 = POWER == 0 ? kLog2e : POWER * k;
-    float loss = 0.0f;                                 // in bits
-    if (soft != 0.0f) {
+    const float log_s = log2f(m.s) * kLn2, log_s1 = POWER == 1 ? log_s : log2f(m.s1) * kLn2;
+    float loss = 0.0f;
+    if (soft != 0.0f) {                                // tau^2 sum p (log p + log s) - tau sum p (x - r): the logits' part in the logits' own range
+        float logs = 0.0f, logits = 0.0f;
         for (int i = lane; i < a.top; i += 32) {
             const float p = list.p[i];
-            if (p != 0.0f) loss += p * (list.log_p[i] - (fmaf(list.x[i], k, -m.r) - log_s));
+            if (p != 0.0f) {
+                logs += p * (list.log_p[i] + log_s);
+                logits += p * (list.x[i] - m.r);
+            }
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-        loss *= soft * (kLog2e / k) * (kLog2e / k);
+        for (int o = 16; o > 0; o >>= 1) {
+            logs += __shfl_xor_sync(0xffffffffu, logs, o);
+            logits += __shfl_xor_sync(0xffffffffu, logits, o);
+        }
+        const float tau = kLog2e / k;
+        loss = soft * tau * (tau * logs - logits);
     }
-    if (label.is) loss += hard * (log_s1 - fmaf(label.x, k1, -m.r1));
+    if (label.is) loss += hard * (log_s1 - (label.x - m.r));
     if (lane == 0) {
-        if (a.loss) PGT_STORE(a.loss[at_row], loss * kLn2);
+        if (a.loss) PGT_STORE(a.loss[at_row], loss);
         if (a.lse) {
-            PGT_STORE(a.lse[2 * at_row], hard != 0.0f ? (m.r1 + log_s1) * kLn2 : 0.0f);
-            PGT_STORE(a.lse[2 * at_row + 1], soft != 0.0f ? (m.r + log_s) * kLn2 : 0.0f);
+            PGT_STORE(a.lse[2 * at_row], hard != 0.0f ? m.r + log_s1 : 0.0f);
+            PGT_STORE(a.lse[2 * at_row + 1], soft != 0.0f ? fmaf(m.r, k * kLn2, log_s) : 0.0f);
         }
     }
 }
@@ -339,14 +344,14 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
             const Label<H> label(a, row_of(at), at, hard);
             const float g = GRAD && a.dloss ? PGT_LOAD(a.dloss[at]) : 1.0f;
             bar_sync<1>(T + 32);
-            const Sums m = all_sums<POWER, T / 32>(s_sums[flip]);
+            const Sums m = all_sums<POWER, T / 32>(s_sums[flip], k);
             const List list = list_of(flip);
             store_loss<H, POWER>(a, at, list, label, m, k, soft, hard);
             read(at + gridDim.x, flip ^ 1);
             if constexpr (GRAD) {
                 const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
                 bar_sync<2>(T + 32);
-                const Slope<POWER> slope = {k, m.r, m.r1, 0.0f, 0.0f};
+                const Slope<POWER> slope = {k, m.r, m.r, 0.0f, 0.0f};
                 take_off<H, POWER>(Out(a.dlogits, at / a.tokens, at % a.tokens, a.classes), list, a.top, label, slope, m, soft != 0.0f, to_soft, to_hard,
                                    threadIdx.x - T, 32, 0, a.classes);
             }
@@ -387,7 +392,7 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
             if (a.dloss) g = PGT_LOAD(a.dloss[at]);
             if (a.labels && hard != 0.0f) label = PGT_LOAD(a.labels[at]);
         }
-        Sums m = {kNoLogit, 0.0f, kNoLogit, 0.0f};
+        Sums m = {kNoLogit, 0.0f, 0.0f};
         F2 s = both(0.0f), s1 = both(0.0f);
         copies_wait();
         walk(
@@ -407,13 +412,13 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
             });
         m.s = sum2(s);
         m.s1 = POWER == 1 ? 0.0f : sum2(s1);
-        join_warp<POWER>(m, s_sums[flip]);
+        join_warp<POWER>(m, k, s_sums[flip]);
         bar_sync<1>(T + 32);
         const int rest = row.pieces + (static_cast<int>(threadIdx.x) - row.pieces % T + T) % T;      // this thread's first piece behind the row's
         if constexpr (GRAD) {
-            m = all_sums<POWER, T / 32>(s_sums[flip]);
+            m = all_sums<POWER, T / 32>(s_sums[flip], k);
             const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label >= 0 && label < a.classes ? g * hard : 0.0f;
-            const Slope<POWER> slope = {k, m.r, m.r1, to_soft / m.s, to_hard / m.s1};
+            const Slope<POWER> slope = {k, m.r, m.r, to_soft / m.s, to_hard / m.s1};
             const Out out(a.dlogits, at / a.tokens, at % a.tokens, a.classes);
             const int shift = row.off - out.off;
             if (shift == 0) {
@@ -481,7 +486,7 @@ distillation_stream_kernel(const pg_distillation_args a, float k, float soft, fl
     const float g = a.dloss ? PGT_LOAD(a.dloss[at_row]) : 1.0f;
     const bool lists = threadIdx.x >= T;
     constexpr int U = 4;                               // pieces on their way at once
-    Sums m = {kNoLogit, 0.0f, kNoLogit, 0.0f};
+    Sums m = {kNoLogit, 0.0f, 0.0f};
     if (lists) {
         if (soft != 0.0f) {
             const bool any = read_list<H>(a, row, b, t, list, k);
@@ -506,23 +511,25 @@ distillation_stream_kernel(const pg_distillation_args a, float k, float soft, fl
         }
         m.s = sum2(s);
         m.s1 = POWER == 1 ? 0.0f : sum2(s1);
-        join_warp<POWER>(m, s_sums);
+        join_warp<POWER>(m, k, s_sums);
     }
     __syncthreads();
+    float r1;
     if constexpr (MODE == AGAIN) {
-        m = all_sums<POWER, T / 32>(s_sums);
+        m = all_sums<POWER, T / 32>(s_sums, k);
         if (lists) store_loss<H, POWER>(a, at_row, list, label, m, k, soft, hard);
         if (!a.dlogits.data) return;
+        r1 = m.r;
     } else {
-        // 2^(k x - r) is the softmax at k as it is; of its power at temperature 1, 1 / s1 is
-        const float lse1 = PGT_LOAD(a.lse[2 * at_row]) * kLog2e, lse = PGT_LOAD(a.lse[2 * at_row + 1]) * kLog2e;
-        m.r = soft != 0.0f ? lse : lse1;
-        m.r1 = POWER == 0 ? lse1 : POWER * m.r;
+        // 2^(k (x - tau lse)) is the softmax at tau as it is; of its power at temperature 1, 1 / s1 is
+        const float lse1 = PGT_LOAD(a.lse[2 * at_row]), lse = PGT_LOAD(a.lse[2 * at_row + 1]);
+        m.r = soft != 0.0f ? lse * (kLog2e / k) : lse1;
         m.s = 1.0f;
-        m.s1 = POWER == 0 ? 1.0f : ex2(lse1 - m.r1);
+        m.s1 = POWER > 1 ? ex2((lse1 - m.r) * kLog2e) : 1.0f;
+        r1 = POWER == 0 ? lse1 : m.r;
     }
     const float to_soft = soft != 0.0f && s_any ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
-    const Slope<POWER> slope = {k, m.r, m.r1, to_soft / m.s, to_hard / m.s1};
+    const Slope<POWER> slope = {k, m.r, r1, to_soft / m.s, to_hard / m.s1};
     const Out out(a.dlogits, b, t, a.classes);
     const int share = (out.pieces + gridDim.z - 1) / gridDim.z, first = blockIdx.z * share, last = min(out.pieces, first + share);
     const int shift = row.off - out.off;
