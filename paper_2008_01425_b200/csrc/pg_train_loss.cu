@@ -312,6 +312,22 @@ __device__ __forceinline__ void copy16(void* shared, const void* global) {
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
+// Rows in steps of `step`, by worker and token, without a division for each.
+struct Walk {
+    int64_t at, b;
+    int t, tokens, step_b, step_t, step;
+    __device__ Walk(uint32_t first, uint32_t by, int n) : at(first), b(first / n), t(first % n), tokens(n), step_b(by / n), step_t(by % n), step(by) {}
+    __device__ void next() {
+        at += step;
+        b += step_b;
+        t += step_t;
+        if (t >= tokens) {
+            t -= tokens;
+            ++b;
+        }
+    }
+};
+
 // Loss, and with GRAD the gradient too, of rows blockIdx.x, blockIdx.x + gridDim.x, ..  The row lies in shared memory, piece j the
 // business of thread j mod T alone: as soon as a thread has used a piece for the last time it asks for the same piece of the block's next row, so
 // that memory works while the exponentials do.  One more warp reads the teacher's list of the next row meanwhile (three dependent
@@ -330,31 +346,35 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
         float* w = words + 4 * a.top * which;
         return List{reinterpret_cast<int*>(w), w + a.top, w + 2 * a.top, w + 3 * a.top};
     };
-    auto row_of = [&](int64_t at) { return Row(a.logits, at / a.tokens, at % a.tokens, a.classes); };
+    auto row_of = [&](const Walk& w) { return Row(a.logits, w.b, w.t, a.classes); };
     int flip = 0;
+    Walk next(blockIdx.x, gridDim.x, a.tokens);
     if (threadIdx.x >= T) {                            // the list's warp
-        auto read = [&](int64_t at, int which) {
-            if (soft == 0.0f || at >= rows) return;
-            const bool any = read_list<H>(a, row_of(at), at / a.tokens, at % a.tokens, list_of(which), k);
+        auto read = [&](const Walk& at, int which) {
+            if (soft == 0.0f || at.at >= rows) return;
+            const bool any = read_list<H>(a, row_of(at), at.b, at.t, list_of(which), k);
             if (threadIdx.x == T) s_any[which] = any;
             __syncwarp();
         };
-        read(blockIdx.x, 0);
-        for (int64_t at = blockIdx.x; at < rows; at += gridDim.x, flip ^= 1) {
-            const Label<H> label(a, row_of(at), at, hard);
-            const float g = GRAD && a.dloss ? PGT_LOAD(a.dloss[at]) : 1.0f;
+        read(next, 0);
+        while (next.at < rows) {
+            const Walk at = next;
+            next.next();
+            const Label<H> label(a, row_of(at), at.at, hard);
+            const float g = GRAD && a.dloss ? PGT_LOAD(a.dloss[at.at]) : 1.0f;
             bar_sync<1>(T + 32);
             const Sums m = all_sums<POWER, T / 32>(s_sums[flip], k);
             const List list = list_of(flip);
-            store_loss<H, POWER>(a, at, list, label, m, k, soft, hard);
-            read(at + gridDim.x, flip ^ 1);
+            store_loss<H, POWER>(a, at.at, list, label, m, k, soft, hard);
+            read(next, flip ^ 1);
             if constexpr (GRAD) {
                 const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
                 bar_sync<2>(T + 32);
                 const Slope<POWER> slope = {k, m.r, m.r, 0.0f, 0.0f};
-                take_off<H, POWER>(Out(a.dlogits, at / a.tokens, at % a.tokens, a.classes), list, a.top, label, slope, m, soft != 0.0f, to_soft, to_hard,
-                                   threadIdx.x - T, 32, 0, a.classes);
+                take_off<H, POWER>(Out(a.dlogits, at.b, at.t, a.classes), list, a.top, label, slope, m, soft != 0.0f, to_soft, to_hard, threadIdx.x - T, 32, 0,
+                                   a.classes);
             }
+            flip ^= 1;
         }
         return;
     }
@@ -374,23 +394,25 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
         for (; j < row.last; j += T) f(j);
         if (j < row.pieces) part(j);
     };
-    {
-        const Row row = row_of(blockIdx.x);
-        from = row.at(threadIdx.x);
-        pieces = row.pieces;
-        for (int j = threadIdx.x; j < pieces; j += T) ask(j);
-    }
-    for (int64_t at = blockIdx.x; at < rows; at += gridDim.x, flip ^= 1) {
-        const Row row = row_of(at);
-        const bool more = at + gridDim.x < rows;
-        const Row next = row_of(more ? at + gridDim.x : at);
-        from = next.at(threadIdx.x);
-        pieces = more ? next.pieces : 0;
+    Row coming = row_of(next);
+    from = coming.at(threadIdx.x);
+    pieces = coming.pieces;
+    for (int j = threadIdx.x; j < pieces; j += T) ask(j);
+    for (; next.at < rows; flip ^= 1) {
+        const Walk at = next;
+        const Row row = coming;
+        next.next();
+        pieces = 0;
+        if (next.at < rows) {
+            coming = row_of(next);
+            from = coming.at(threadIdx.x);
+            pieces = coming.pieces;
+        }
         float g = 1.0f;
         int label = -1;
         if constexpr (GRAD) {
-            if (a.dloss) g = PGT_LOAD(a.dloss[at]);
-            if (a.labels && hard != 0.0f) label = PGT_LOAD(a.labels[at]);
+            if (a.dloss) g = PGT_LOAD(a.dloss[at.at]);
+            if (a.labels && hard != 0.0f) label = PGT_LOAD(a.labels[at.at]);
         }
         Sums m = {kNoLogit, 0.0f, 0.0f};
         F2 s = both(0.0f), s1 = both(0.0f);
@@ -419,7 +441,7 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
             m = all_sums<POWER, T / 32>(s_sums[flip], k);
             const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label >= 0 && label < a.classes ? g * hard : 0.0f;
             const Slope<POWER> slope = {k, m.r, m.r, to_soft / m.s, to_hard / m.s1};
-            const Out out(a.dlogits, at / a.tokens, at % a.tokens, a.classes);
+            const Out out(a.dlogits, at.b, at.t, a.classes);
             const int shift = row.off - out.off;
             if (shift == 0) {
                 walk(
