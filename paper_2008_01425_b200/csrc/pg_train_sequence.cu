@@ -557,8 +557,9 @@ scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict_
 __global__ void __launch_bounds__(128)
 join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float* __restrict__ states, float* __restrict__ carries, const float* __restrict__ sums,
                    int sequences, int channels, int n_states, int chunks) {
-    const int64_t sequence = blockIdx.x, b = sequence / sequences;
-    const int64_t width = static_cast<int64_t>(channels) * n_states, at = static_cast<int64_t>(blockIdx.y) * 128 + threadIdx.x;
+    const int64_t width = static_cast<int64_t>(channels) * n_states;
+    const uint32_t blocks = static_cast<uint32_t>((width + 127) / 128);                  // of a sequence
+    const int64_t sequence = blockIdx.x / blocks, b = sequence / sequences, at = static_cast<int64_t>(blockIdx.x % blocks) * 128 + threadIdx.x;
     if (at >= width) return;
     const int64_t d = at / n_states, n = at % n_states;
     const float rate = PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]) * kLog2e;
@@ -1062,6 +1063,8 @@ ScanPlan scan_plan(const pg_scan_args& a, int lanes) {
     chunks = (length + chunk - 1) / chunk;
     return {static_cast<int>(chunk), static_cast<int>(chunks), tiles, int64_t{a.batch} * a.sequences * tiles * chunks};
 }
+template <typename Args>
+int64_t join_blocks(const Args& a) { return int64_t{a.batch} * a.sequences * ((int64_t{a.channels} * a.states + 127) / 128); }
 int lanes_of(int states, int per_thread) {
     int lanes = 1;
     while (lanes * per_thread < states) lanes *= 2;
@@ -1270,7 +1273,7 @@ int pg_selective_scan(const pg_scan_args* args, void* workspace, size_t workspac
     if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
     const int lanes = lanes_of(a.states, 16);
     const ScanPlan p = scan_plan(a, lanes);
-    if (p.items > kMaxBlocks) return PG_ERR_TOO_LARGE;
+    if (p.items > kMaxBlocks || (p.chunks > 1 && join_blocks(a) > kMaxBlocks)) return PG_ERR_TOO_LARGE;
     if (sequences == 0 || (a.length == 0 && !a.state_out)) return PG_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Operands operands;
@@ -1288,7 +1291,7 @@ int pg_selective_scan(const pg_scan_args* args, void* workspace, size_t workspac
             const unsigned grid = static_cast<unsigned>(std::min<int64_t>(p.items, int64_t{kSMs} * kScanBlocks));
             if (p.chunks > 1) {
                 scan_kernel<H, P, LANES, true><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks, p.tiles, static_cast<uint32_t>(p.items));
-                join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
+                join_chunks_kernel<<<static_cast<unsigned>(join_blocks(a)), 128, 0, st>>>(
                     a.a, a.state, states, nullptr, sums, a.sequences, a.channels, a.states, p.chunks);
             }
             scan_kernel<H, P, LANES, false><<<grid, kScanThreads, 0, st>>>(a, states, sums, p.chunk, p.chunks, p.tiles, static_cast<uint32_t>(p.items));
@@ -1329,7 +1332,9 @@ int pg_selective_scan_grad(const pg_scan_grad_args* args, void* workspace, size_
     if (a.ddelta_bias && !vector_ok(a.ddelta_bias, a.ddelta_bias_stride, a.batch, a.channels, true, dev)) return PG_ERR_INVALID;
     if (need > 0 && (workspace_bytes < need || !device_pointer(workspace, 16, dev))) return PG_ERR_WORKSPACE;
     const GradPlan p = grad_plan(a);
-    if (sequences * p.chunks > kMaxBlocks || int64_t{a.batch} * p.shares > kMaxBlocks || p.parts / 256 > static_cast<size_t>(kMaxBlocks)) return PG_ERR_TOO_LARGE;
+    if (sequences * p.chunks > kMaxBlocks || int64_t{a.batch} * p.shares > kMaxBlocks || p.parts / 256 > static_cast<size_t>(kMaxBlocks) ||
+        (p.chunks > 1 && join_blocks(a) > kMaxBlocks))
+        return PG_ERR_TOO_LARGE;
     if (a.batch == 0) return PG_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Operands operands;
@@ -1355,7 +1360,7 @@ int pg_selective_scan_grad(const pg_scan_grad_args* args, void* workspace, size_
             if (p.chunks > 1 && sequences > 0) {
                 scan_grad_local_kernel<H, LANES><<<dim3(static_cast<unsigned>(sequences * p.chunks), static_cast<unsigned>(p.blocks)), kScanThreads, 0, st>>>(
                     a, states, carries, sums, p.chunk, p.chunks);
-                join_chunks_kernel<<<dim3(static_cast<unsigned>(sequences), static_cast<unsigned>((int64_t{a.channels} * a.states + 127) / 128)), 128, 0, st>>>(
+                join_chunks_kernel<<<static_cast<unsigned>(join_blocks(a)), 128, 0, st>>>(
                     a.a, a.state, states, carries, sums, a.sequences, a.channels, a.states, p.chunks);
             }
             const size_t smem = GradLayout<LANES>((p.chunk + kGroup - 1) / kGroup * kGroup).all;

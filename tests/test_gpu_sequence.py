@@ -856,3 +856,15 @@ def test_refusals_of_the_sequence_binding(tr):
     with pytest.raises(pg.PowerGossipError) as e:
         tr.pg_distillation_loss(wide, torch.zeros(1, 2, 1025, dtype=torch.int32, device="cuda"), torch.zeros(1, 2, 1025, dtype=BF, device="cuda"))
     assert e.value.status == pg.PG_ERR_TOO_LARGE
+
+
+def test_more_states_than_a_grid_has_rows(tr):
+    """A chunked gradient of 8.96 million states per sequence: a channel's gradients are those it has on its own."""
+    n, m, t = 140000, 64, 41
+    c, more = scan_inputs(gen(11), 1, 1, t, n, m, BF, False, False, False, 0)
+    dy = rand(gen(12), 1, t, n).to(BF)
+    got = tr.pg_selective_scan_grad(dy, **c, **more)
+    last = slice(n - 16, n)
+    part = {k: v[..., last].contiguous() if k in ("u", "delta", "skip", "delta_bias") else v[:, last].contiguous() if k == "a" else v for k, v in c.items()}
+    want = tr.pg_selective_scan_grad(dy[..., last].contiguous(), **part, **more)
+    assert torch.equal(got.du[..., last], want.du) and torch.equal(got.ddelta[..., last], want.ddelta)
