@@ -53,7 +53,9 @@ struct Rows {
 // ---------------------------------------------------------------- convolution
 // A warp has 64 neighbouring channels, a lane two of them, and runs along the tokens of (a part of) one sequence, with the inputs of
 // the last width - 1 tokens in registers: every input is read once, but for the few before a run.  Inputs come through shared memory in
-// 16-byte pieces, whatever the rows' alignment, a tile of tokens ahead.  Bound by memory, 4 bytes a value (6 in the gradient).
+// 16-byte pieces, whatever the rows' alignment, a tile of tokens ahead.  4 bytes a value (6 in the gradient) have to move; instructions (some
+// 60 for two values of a lane) bound it at 0.45 of the copy rate: 32 x 700 tokens x 1300 channels 43 us.  (Eight channels a thread, cut out of
+// their pieces in registers: 88 us.  Plain 2- and 4-byte loads: 43 us, but the gradient of odd widths 145 us instead of 66.)
 constexpr int kRun = 64;                               // tokens of a run at most
 constexpr int kConvThreads = 128;
 constexpr int kStrip = 64;                             // channels
@@ -298,19 +300,7 @@ sum_parts_kernel(const float* __restrict__ partial, int64_t parts, int64_t part_
 // ---------------------------------------------------------------- scan
 // softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), with log(1 + e) = 2 artanh(s), s = e / (2 + e) <= 1/3: the series to s^13 is
 // good to 2^-26 of it, for small e too, where a logarithm of 1 + e would lose e's digits.
-__device__ __forceinline__ float softplus(float v) {
-    const float e = ex2(-kLog2e * fabsf(v)), s = e * rcp(2.0f + e), q = s * s;
-    float p = 2.0f / 13.0f;
-    p = fmaf(p, q, 2.0f / 11.0f);
-    p = fmaf(p, q, 2.0f / 9.0f);
-    p = fmaf(p, q, 2.0f / 7.0f);
-    p = fmaf(p, q, 2.0f / 5.0f);
-    p = fmaf(p, q, 2.0f / 3.0f);
-    p = fmaf(p, q, 2.0f);
-    return fmaf(s, p, fmaxf(v, 0.0f));
-}
-__device__ __forceinline__ float sigmoid(float v) { return rcp(1.0f + ex2(-kLog2e * v)); }
-__device__ __forceinline__ F2 softplus(F2 v) {          // of two
+__device__ __forceinline__ F2 softplus(F2 v) {
     float a, b;
     split(v, a, b);
     const F2 e = pair(ex2(-kLog2e * fabsf(a)), ex2(-kLog2e * fabsf(b)));
@@ -330,7 +320,10 @@ __device__ __forceinline__ F2 softplus(F2 v) {          // of two
 // A channel's states lie in LANES neighbouring threads, P each, in pairs.  A block takes CH channels of one sequence at a time, or of a
 // chunk of it (an item), in tiles of kScanTile tokens; the next tile is on its way while one is worked on.  Items are numbered by
 // worker, channels, sequence and chunk, and a block has neighbours of them, so that it keeps its channels' rates as long as possible.
-// The exponential unit bounds it: 16 states and the softplus and the gate take 20 exponentials or reciprocals per token and channel.
+// The exponential unit bounds it: 16 states and the softplus and the gate take 20 exponentials or reciprocals per token and channel, 145 us
+// for 32 x 700 tokens x 1300 channels at 1.9 GHz, where it takes 244 us (issue slots 53 % and the unit 58 % busy; without tiles ahead 431 us).
+// A polynomial on the multiply-add pipes for an eighth of the exponentials: 3 % slower.  4 to 7 blocks an SM, two or four tokens
+// side by side: within 10 % of one another.
 constexpr int kScanThreads = 128;
 constexpr int kScanTile = 16;                          // tokens; an eighth of the threads
 constexpr int kScanBlocks = 6;                       // resident per SM
@@ -563,23 +556,27 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
     if (at >= width) return;
     const int64_t d = at / n_states, n = at % n_states;
     const float rate = PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]) * kLog2e;
-    float h = state ? PGT_LOAD(state[sequence * width + at]) : 0.0f;
-#pragma unroll 4
-    for (int c = 0; c < chunks; ++c) {
-        const int64_t k = sequence * chunks + c;
-        const float own = PGT_LOAD(states[k * width + at]), sum = PGT_LOAD(sums[k * channels + d]);
-        PGT_STORE(states[k * width + at], h);
-        h = fmaf(ex2(sum * rate), h, own);
-    }
-    if (!carries) return;
-    float g = 0.0f;
-#pragma unroll 4
-    for (int c = chunks - 1; c >= 0; --c) {
-        const int64_t k = sequence * chunks + c;
-        const float own = PGT_LOAD(carries[k * width + at]), sum = PGT_LOAD(sums[k * channels + d]);
-        PGT_STORE(carries[k * width + at], g);
-        g = fmaf(ex2(sum * rate), g, own);
-    }
+    const int64_t first = sequence * chunks;
+    constexpr int U = 8;                               // chunks whose numbers are on their way at once
+    auto join = [&](float* v, float carry, bool backwards) {
+        for (int c0 = 0; c0 < chunks; c0 += U) {
+            float own[U], sum[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int64_t k = first + (backwards ? chunks - 1 - c0 - i : c0 + i);
+                own[i] = c0 + i < chunks ? PGT_LOAD(v[k * width + at]) : 0.0f;
+                sum[i] = c0 + i < chunks ? PGT_LOAD(sums[k * channels + d]) : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int64_t k = first + (backwards ? chunks - 1 - c0 - i : c0 + i);
+                if (c0 + i < chunks) PGT_STORE(v[k * width + at], carry);
+                carry = fmaf(ex2(sum[i] * rate), carry, own[i]);
+            }
+        }
+    };
+    join(states, state ? PGT_LOAD(state[sequence * width + at]) : 0.0f, false);
+    if (carries) join(carries, 0.0f, true);
 }
 
 // ---------------------------------------------------------------- scan gradient
@@ -589,78 +586,129 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
 //     dD_t = u_t (g_t . B_t) + sum over states of A e_t,   e_t = g_t h_t-1 exp(D_t A)
 //     dA = sum over tokens of D_t e_t,  dskip = sum of dv_t u_t,  ddelta_t = dD_t sigmoid(delta_t + delta_bias)
 // The states before groups of kGroup tokens are kept in shared memory on a way forward through the chunk; backwards the
-// states of a group are computed once more.
+// states of a group are computed once more.  32 x 700 tokens x 1300 channels x 16 states: 1010 us, 635 us with lengths drawn from 0 to 35;
+// issue slots are 46 % busy with the twelve warps that registers and shared memory leave room for.
 constexpr int kGradStates = 8;                         // states of a thread
 constexpr int kGroup = 4;
-constexpr int kGradChunk = 40;                         // tokens of a chunk at most
+// Tokens of a chunk at most, and of a sequence that is a chunk of its own: at 16 states shared memory holds three blocks of 36 tokens, two of
+// 52.  Chunks cost a pass over the tokens before.  As many tokens of 32 x 1300 channels in sequences of 40, 48, 54 and 72, alone: 1297,
+// 1300, 2223 and 2159 us, in chunks: 1940, 1828, 1744 and 1610; a sequence of 8192 in chunks of 36, 40 and 20: 552, 771 and 634 us.
+constexpr int kGradChunk = 36, kGradAlone = 52;
 constexpr int kGradBlocks = 3;                         // resident per SM
+
+// Every token and channel of a chunk once, into shared memory ([token][channel]): the step, what reaches y before the gate, u as it is, and (s_dz)
+// what dz is a multiple of.  A thread has channel d.  Tokens behind the last one, to `rows`, and channels that are not there: zeros.
+template <typename H, int LANES>
+__device__ __forceinline__ void prepare_chunk(const pg_scan_grad_args& a, int64_t b, int64_t at, int count, int rows, int d, float bias, float* s_step, float* s_dv,
+                                              float* s_dz, uint16_t* s_u) {
+    constexpr int CH = kScanThreads / LANES, U = 4;    // tokens on their way at once
+    const bool gated = a.z.data != nullptr, is = d < a.channels;
+    auto rows_of = [&](const pg_matrix& m) { return static_cast<const uint16_t*>(m.data) + b * m.stride + at * m.ld + d; };
+    const uint16_t *u = rows_of(a.u), *delta = rows_of(a.delta), *dy = rows_of(a.dy), *z = gated ? rows_of(a.z) : nullptr;
+    for (int k0 = threadIdx.x / CH; k0 < rows; k0 += U * LANES) {
+        uint16_t ru[U], rd[U], rg[U], rz[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int k = k0 + i * LANES;
+            const bool there = is && k < count;
+            ru[i] = there ? PGT_LOAD(u[k * a.u.ld]) : 0;
+            rd[i] = there ? PGT_LOAD(delta[k * a.delta.ld]) : 0;
+            rg[i] = there ? PGT_LOAD(dy[k * a.dy.ld]) : 0;
+            rz[i] = there && gated ? PGT_LOAD(z[k * a.z.ld]) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < U; i += 2) {
+            float step[2], dv[2], dz[2] = {0.0f, 0.0f};
+            split(softplus(pair(Elem<H>::up(rd[i]) + bias, Elem<H>::up(rd[i + 1]) + bias)), step[0], step[1]);
+            const F2 gy = pair(Elem<H>::up(rg[i]), Elem<H>::up(rg[i + 1]));
+            split(gy, dv[0], dv[1]);
+            if (gated) {
+                const F2 v = pair(Elem<H>::up(rz[i]), Elem<H>::up(rz[i + 1])), sig = sigmoid_of(mul(v, both(-kLog2e)));
+                split(mul(gy, mul(v, sig)), dv[0], dv[1]);
+                split(mul(gy, mul(sig, fma(v, fma(sig, both(-1.0f), both(1.0f)), both(1.0f)))), dz[0], dz[1]);
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int k = k0 + (i + w) * LANES, to = k * CH + threadIdx.x % CH;
+                if (k < rows) {
+                    s_step[to] = is && k < count ? step[w] : 0.0f;
+                    s_dv[to] = dv[w];
+                    if (s_dz) s_dz[to] = dz[w];
+                    s_u[to] = ru[i + w];
+                }
+            }
+        }
+    }
+}
 
 // Own parts of a chunk for the way in both directions: the last state from a zero one, and the gradient that reaches the state before it.
 template <typename H, int LANES>
 __global__ void __launch_bounds__(kScanThreads)
 scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, float* __restrict__ carries, float* __restrict__ sums, int chunk, int chunks) {
-    constexpr int P = kGradStates, N = P * LANES;
-    __shared__ __align__(16) float s_b[kScanTile][N], s_c[kScanTile][N];
+    constexpr int P = kGradStates, N = P * LANES, CH = kScanThreads / LANES;
+    constexpr int kTile = 20;                          // tokens in shared memory at once
+    __shared__ float s_step[kTile * CH], s_dv[kTile * CH];
+    __shared__ uint16_t s_u[kTile * CH];
+    __shared__ __align__(16) float s_b[kTile * N], s_c[kTile * N];
     const int64_t sequence = blockIdx.x / chunks;
     const int at_chunk = static_cast<int>(blockIdx.x % chunks);
     const int64_t b = sequence / a.sequences;
     const int s = static_cast<int>(sequence % a.sequences);
-    const int d = blockIdx.y * (kScanThreads / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * P;
+    const int d = blockIdx.y * CH + threadIdx.x / LANES, c = threadIdx.x / LANES, n0 = threadIdx.x % LANES * P, step_d = blockIdx.y * CH + threadIdx.x % CH;
     const bool is = d < a.channels;
+    const int there = is ? min(max(a.states - n0, 0), P) : 0;
     const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
-    const int t0 = at_chunk * chunk, stop = min(min(a.length, t0 + chunk), have);
-    const int64_t first = static_cast<int64_t>(s) * a.length;
-    const uint16_t* u = static_cast<const uint16_t*>(a.u.data) + b * a.u.stride + first * a.u.ld + d;
-    const uint16_t* delta = static_cast<const uint16_t*>(a.delta.data) + b * a.delta.stride + first * a.delta.ld + d;
-    const uint16_t* z = a.z.data ? static_cast<const uint16_t*>(a.z.data) + b * a.z.stride + first * a.z.ld + d : nullptr;
-    const uint16_t* dy = static_cast<const uint16_t*>(a.dy.data) + b * a.dy.stride + first * a.dy.ld + d;
-    const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + first * a.b.ld;
-    const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + first * a.c.ld;
-    const float bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + d]) : 0.0f;
-    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld;
-    float rate[P], h[P], g[P], product[P], sum = 0.0f;
+    const int t0 = at_chunk * chunk, count = max(0, min(min(a.length, t0 + chunk), have) - t0);
+    const float bias = step_d < a.channels && a.delta_bias ? PGT_LOAD(a.delta_bias[b * a.delta_bias_stride + step_d]) : 0.0f;
+    const float* rates = static_cast<const float*>(a.a.data) + b * a.a.stride + static_cast<int64_t>(d) * a.a.ld + n0;
+    F2 rate[P / 2], h[P / 2], g[P / 2], product[P / 2];
+    load_states<P>(rates, there, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        rate[p] = is && n0 + p < a.states ? PGT_LOAD(rates[n0 + p]) * kLog2e : 0.0f;
-        h[p] = g[p] = 0.0f;
-        product[p] = 1.0f;
+    for (int p = 0; p < P / 2; ++p) {
+        rate[p] = mul(rate[p], both(kLog2e));
+        h[p] = g[p] = both(0.0f);
+        product[p] = both(1.0f);
     }
-    for (int tile = t0; tile < stop; tile += kScanTile) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kScanTile * N; i += kScanThreads) {
+    float sum = 0.0f;
+    for (int from = 0; from < count; from += kTile) {
+        const int64_t at = static_cast<int64_t>(s) * a.length + t0 + from;
+        const int rows = min(kTile, count - from);
+        const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + at * a.b.ld;
+        const uint16_t* cc = static_cast<const uint16_t*>(a.c.data) + b * a.c.stride + at * a.c.ld;
+        __syncthreads();                               // (shared memory is free again)
+#pragma unroll 4
+        for (int i = threadIdx.x; i < rows * N; i += kScanThreads) {
             const int k = i / N, n = i % N;
-            const bool there = tile + k < stop && n < a.states;
-            s_b[k][n] = there ? Elem<H>::up(PGT_LOAD(bb[(tile + k) * a.b.ld + n])) : 0.0f;
-            s_c[k][n] = there ? Elem<H>::up(PGT_LOAD(cc[(tile + k) * a.c.ld + n])) : 0.0f;
+            s_b[i] = n < a.states ? Elem<H>::up(PGT_LOAD(bb[k * a.b.ld + n])) : 0.0f;
+            s_c[i] = n < a.states ? Elem<H>::up(PGT_LOAD(cc[k * a.c.ld + n])) : 0.0f;
         }
+        prepare_chunk<H, LANES>(a, b, at, rows, rows, step_d, bias, s_step, s_dv, nullptr, s_u);
         __syncthreads();
-        for (int k = 0; k < kScanTile && tile + k < stop; ++k) {
-            const int t = tile + k;
-            if (!is) break;
-            const float step = softplus(Elem<H>::up(PGT_LOAD(delta[t * a.delta.ld])) + bias), drive = step * Elem<H>::up(PGT_LOAD(u[t * a.u.ld]));
-            float dv = Elem<H>::up(PGT_LOAD(dy[t * a.dy.ld]));
-            if (z) {
-                const float v = Elem<H>::up(PGT_LOAD(z[t * a.z.ld]));
-                dv *= v * sigmoid(v);
-            }
+#pragma unroll 2
+        for (int k = 0; k < rows; ++k) {
+            const float step = s_step[k * CH + c];
+            const F2 steps = both(step), drive = both(step * Elem<H>::up(s_u[k * CH + c])), dv = both(s_dv[k * CH + c]);
+            const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
+            const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(s_c + k * N + n0);
             sum += step;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const float keep = ex2(step * rate[p]);
-                h[p] = fmaf(keep, h[p], drive * s_b[k][n0 + p]);
-                product[p] *= keep;
-                g[p] = fmaf(product[p] * dv, s_c[k][n0 + p], g[p]);
+            for (int q = 0; q < P / 4; ++q) {
+                const ulonglong2 bv = bk[q], cv = ck[q];
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const int p = 2 * q + w;
+                    const F2 keep = ex2(mul(steps, rate[p]));
+                    h[p] = fma(keep, h[p], mul(drive, F2{w ? bv.y : bv.x}));
+                    product[p] = mul(product[p], keep);
+                    g[p] = fma(mul(product[p], dv), F2{w ? cv.y : cv.x}, g[p]);
+                }
             }
         }
     }
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * a.channels + d;
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-        if (is && n0 + p < a.states) {
-            PGT_STORE(states[at * a.states + n0 + p], h[p]);
-            PGT_STORE(carries[at * a.states + n0 + p], g[p]);
-        }
-    if (is && n0 == 0) PGT_STORE(sums[at], sum);
+    const int64_t to = static_cast<int64_t>(blockIdx.x) * a.channels + d;
+    store_states<P>(states + to * a.states + n0, there, a.states % 4 == 0, h);
+    store_states<P>(carries + to * a.states + n0, there, a.states % 4 == 0, g);
+    if (is && n0 == 0) PGT_STORE(sums[to], sum);
 }
 
 // Sums v[0 .. 2P) over the warp's lanes with the same lane % LANES; a lane keeps 2P / (32 / LANES) of them, at least one: those from
@@ -789,46 +837,7 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
         } else if (a.state) {
             load_states<P>(a.state + state_at, there, wide && reinterpret_cast<uintptr_t>(a.state) % 16 == 0, h);
         }
-        {                                              // every token and channel once: its step, and what reaches y before the gate
-            auto rows_of = [&](const pg_matrix& m) { return static_cast<const uint16_t*>(m.data) + b * m.stride + at * m.ld + step_d; };
-            const uint16_t *u = rows_of(a.u), *delta = rows_of(a.delta), *dy = rows_of(a.dy), *z = gated ? rows_of(a.z) : nullptr;
-            constexpr int U = 4;                       // tokens on their way at once
-            for (int k0 = threadIdx.x / CH; k0 < groups * kGroup; k0 += U * LANES) {
-                uint16_t ru[U], rd[U], rg[U], rz[U];
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int k = k0 + i * LANES;
-                    const bool is_there = k < count && step_d < a.channels;
-                    ru[i] = is_there ? PGT_LOAD(u[k * a.u.ld]) : 0;
-                    rd[i] = is_there ? PGT_LOAD(delta[k * a.delta.ld]) : 0;
-                    rg[i] = is_there ? PGT_LOAD(dy[k * a.dy.ld]) : 0;
-                    rz[i] = is_there && gated ? PGT_LOAD(z[k * a.z.ld]) : 0;
-                }
-#pragma unroll
-                for (int i = 0; i < U; i += 2) {
-                    const int k = k0 + i * LANES, k1 = k + LANES;
-                    float step[2], dv[2], dz[2] = {0.0f, 0.0f};
-                    split(softplus(pair(Elem<H>::up(rd[i]) + step_bias, Elem<H>::up(rd[i + 1]) + step_bias)), step[0], step[1]);
-                    const F2 gy = pair(Elem<H>::up(rg[i]), Elem<H>::up(rg[i + 1]));
-                    split(gy, dv[0], dv[1]);
-                    if (gated) {
-                        const F2 v = pair(Elem<H>::up(rz[i]), Elem<H>::up(rz[i + 1])), sig = sigmoid_of(mul(v, both(-kLog2e)));
-                        split(mul(gy, mul(v, sig)), dv[0], dv[1]);
-                        split(mul(gy, mul(sig, fma(v, fma(sig, both(-1.0f), both(1.0f)), both(1.0f)))), dz[0], dz[1]);
-                    }
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int to = w ? k1 : k, s_at = to * CH + threadIdx.x % CH;
-                        if (to < groups * kGroup) {
-                            s_step[s_at] = to < count && step_d < a.channels ? step[w] : 0.0f;
-                            s_dv[s_at] = dv[w];
-                            s_dz[s_at] = dz[w];
-                            s_u[s_at] = ru[i + w];
-                        }
-                    }
-                }
-            }
-        }
+        prepare_chunk<H, LANES>(a, b, at, count, groups * kGroup, step_d, step_bias, s_step, s_dv, s_dz, s_u);
         __syncthreads();
         for (int group = 0; group < groups; ++group) { // forward
 #pragma unroll
@@ -1075,7 +1084,7 @@ GradPlan grad_plan(const pg_scan_grad_args& a) {
     GradPlan p = {};
     p.lanes = lanes_of(a.states, kGradStates);
     const int64_t length = std::max(a.length, 1);
-    p.chunks = static_cast<int>((length + kGradChunk - 1) / kGradChunk);
+    p.chunks = length <= kGradAlone ? 1 : static_cast<int>((length + kGradChunk - 1) / kGradChunk);
     p.chunk = static_cast<int>((length + p.chunks - 1) / p.chunks);
     p.blocks = (int64_t{a.channels} * p.lanes + kScanThreads - 1) / kScanThreads;
     const int64_t items = int64_t{a.sequences} * p.chunks;
