@@ -493,6 +493,18 @@ def test_distillation_loss(tr, shape, k, pad, dtype, tau, alpha):
     check_loss(tr, x, ids if alpha else None, teacher if alpha else None, labels, tau, alpha, dloss, dtype)
 
 
+@pytest.mark.parametrize("n,k,pad", [(60, 3, 0), (1029, 5, 1), (4099, 0, 8)])
+@pytest.mark.parametrize("dtype,tau", [(BF, 2.0), (HF, 1.7), (BF, 1.0)])
+def test_distillation_loss_of_many_rows(tr, n, k, pad, dtype, tau):
+    """Rows enough for every warp of the GPU."""
+    g = gen(n)
+    x = strided(rand(g, 2, 2300, n, scale=3.0).to(dtype), pad)
+    ids = torch.randint(-1, n + 1, (2, 2300, k), device="cuda", generator=g).to(torch.int32) if k else None
+    teacher = rand(g, 2, 2300, k).to(dtype) if k else None
+    labels = torch.randint(-1, n, (2, 2300), device="cuda", generator=g).to(torch.int32)
+    check_loss(tr, x, ids, teacher, labels, tau, 0.4 if k else 0.0, rand(g, 2, 2300), dtype)
+
+
 @pytest.mark.parametrize("n", [50, 3000, 30001, 110000])
 @pytest.mark.parametrize("tau", [1.0, 2.0, 0.7])
 def test_lists_labels_and_masks_at_their_ends(tr, n, tau):
