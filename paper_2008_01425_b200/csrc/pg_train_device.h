@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "pg_training.h"
@@ -419,6 +420,19 @@ inline int take_word(unsigned* word, unsigned& value, cudaStream_t st) {
 int take_row_errors(unsigned& value, cudaStream_t st);     // of the row kernels (pg_train_rows.cu)
 int take_loss_errors(unsigned& value, cudaStream_t st);    // of the loss (pg_train_loss.cu)
 int take_sequence_errors(unsigned& value, cudaStream_t st);    // of convolution and scan (pg_train_sequence.cu)
+// Lets launches of a kernel ask for up to `most` bytes of dynamic shared memory.  The limit belongs to the kernel on a device, and setting it can lower
+// it, too: it is the same for all calls, since what a call set for itself another host thread could change before the launch.
+inline bool allow_shared_memory(const void* kernel, size_t most, std::atomic<bool> (&done)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return false;
+    if (done[dev].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    done[dev].store(true, std::memory_order_release);
+    return true;
+}
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PG_OK : PG_ERR_CUDA; }
 
 }  // namespace pgt

@@ -719,8 +719,8 @@ int distillation(const pg_distillation_args* args, bool backward, void* stream) 
         if constexpr (MODE == FORWARD || MODE == BOTH) {
             const auto kernel = distillation_kernel<H, POWER, T, MODE == BOTH>;
             const size_t smem = 2 * words + kept;
-            if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
-                cudaGetLastError();
+            static std::atomic<bool> allowed[64];
+            if (smem > 48 * 1024 && !allow_shared_memory(reinterpret_cast<const void*>(kernel), kMaxRowBytes, allowed)) {
                 rc = PG_ERR_CUDA;
                 return;
             }

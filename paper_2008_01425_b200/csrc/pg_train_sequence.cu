@@ -1374,8 +1374,9 @@ int pg_selective_scan_grad(const pg_scan_grad_args* args, void* workspace, size_
             }
             const size_t smem = GradLayout<LANES>((p.chunk + kGroup - 1) / kGroup * kGroup).all;
             const auto kernel = scan_grad_kernel<H, LANES>;
-            if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) {
-                cudaGetLastError();
+            static_assert(kGradAlone % kGroup == 0 && kGradChunk <= kGradAlone, "the most tokens of a chunk");
+            static std::atomic<bool> allowed[64];
+            if (smem > 48 * 1024 && !allow_shared_memory(reinterpret_cast<const void*>(kernel), GradLayout<LANES>(kGradAlone).all, allowed)) {
                 status = PG_ERR_CUDA;
                 return;
             }

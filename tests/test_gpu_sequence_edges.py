@@ -1,0 +1,89 @@
+"""The sequence operators where calls, tokens, rows and chunks end: against their formulas in 64 bits, by the tolerances of test_gpu_sequence.py, and
+against calls that must give the same bits."""
+import ctypes
+import math
+import threading
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests.test_gpu_sequence import (loss_inputs, norm_grad_reference, scan_forward, scan_grad_reference, scan_inputs,  # noqa: E402
+                                     scan_output)
+from tests.test_gpu_sequence import test_selective_scan as scan_case, test_selective_scan_gradient as scan_gradient_case  # noqa: E402
+from tests.test_gpu_training import BF, HF, U, check, eight, gen, make8, rand, strided  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2008_01425_b200 import build as pg_build
+
+    pg_build.build()
+
+
+@pytest.fixture(scope="module")
+def tr():
+    from paper_2008_01425_b200 import training
+
+    yield training
+    assert training.pg_training_status() == 0
+
+
+# ---------------------------------------------------------------- calls from several host threads
+def loss_of(tr, classes):
+    x, ids, teacher, labels = loss_inputs(gen(classes), 1, 3, classes, 4, BF, True, 0)
+    dloss = torch.ones(1, 3, device="cuda")
+    return lambda: list(tr.pg_distillation_loss(x, ids, teacher, labels, 2.0, 0.5, dloss=dloss))
+
+
+def scan_gradient_of(tr, length):
+    g = gen(length)
+    c, more = scan_inputs(g, 1, 2, length, 20, 16, BF, False, False, False, 0)
+    dy = rand(g, 1, 2 * length, 20).to(BF)
+    return lambda: list(tr.pg_selective_scan_grad(dy, **c, **more))[:-1]
+
+
+def again(tr, monkeypatch, call):
+    """The outputs of a call, and the C call by itself, on any stream, with the same outputs."""
+    held = []
+
+    def run(self, fn, args, size_fn=None):
+        need = ctypes.c_size_t(0)
+        if size_fn is not None:
+            assert size_fn(ctypes.byref(args), ctypes.byref(need)) == 0
+        scratch = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        rest = () if size_fn is None else (scratch.data_ptr(), need.value)
+        held.append((lambda stream: fn(ctypes.byref(args), *rest, stream), scratch, call))   # (and what it works on)
+        assert held[-1][0](self.handle) == 0
+
+    with monkeypatch.context() as m:
+        m.setattr(tr._Call, "run", run)
+        outputs = call()
+    return outputs, held[0]
+
+
+@pytest.mark.parametrize("make,sizes", [(loss_of, (28000, 50000)), (scan_gradient_of, (36, 50))])
+def test_calls_of_two_sizes_from_several_host_threads(tr, monkeypatch, make, sizes):
+    """The shared memory that a kernel may ask for belongs to the kernel and not to the call: a small call must not take it from a large one."""
+    jobs = [again(tr, monkeypatch, make(tr, sizes[k % 2])) for k in range(4)]
+    torch.cuda.synchronize()
+    want = [[v.clone() for v in outputs] for outputs, _ in jobs]
+    wrong, start = [], threading.Barrier(len(jobs))
+
+    def run(k):
+        stream = torch.cuda.Stream()
+        call, handle = jobs[k][1][0], stream.cuda_stream
+        start.wait()
+        wrong.extend(status for status in [call(handle) for _ in range(2000)] if status)
+        stream.synchronize()
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, "%d calls failed, the first with %d" % (len(wrong), wrong[0])
+    for (outputs, _), w in zip(jobs, want):
+        assert all(torch.equal(p, q) for p, q in zip(outputs, w))
