@@ -348,9 +348,10 @@ PG_API int pg_selective_scan_grad(const pg_scan_grad_args *args, void *workspace
  *     loss = alpha tau^2 sum p (log p - log q)  +  (1 - alpha) (log sum exp(x) - x[label])
  * The first term is there with top > 0, the second with labels; a weight of 0 leaves a term out.  Rows whose label is no class
  * (negative, or too large) have no second term.  Entries whose id is no class do not count, nor do those whose logit is -inf;
- * a row without any other has no first term.  An id may occur more than once: each entry counts.  A logit x of -inf has probability 0
- * (and an infinite loss, where p is not 0); a row of nothing else, or with a NaN or +inf, gives NaN.
- * lse gets log sum exp(x) and log sum exp(x / tau) of every row, 0 where the loss does not need it.
+ * a row without any other has no first term.  A row of no terms has a loss and a gradient of 0, whatever its logits are.  An id
+ * may occur more than once: each entry counts.  A logit x of -inf has probability 0 (and an infinite loss, where p is not 0); a row
+ * of nothing else, or with a NaN or +inf, gives NaN.
+ * lse gets log sum exp(x) and log sum exp(x / tau) of every row; the first is 0 where the call has no second term, the second where it has no first.
  *
  * The gradient dloss (alpha tau (q - p) + (1 - alpha) (softmax(x) - [label])) goes to dlogits: by pg_distillation_loss
  * together with the loss, reading the logits once (to 100000 classes; twice above), or by pg_distillation_loss_grad from lse,

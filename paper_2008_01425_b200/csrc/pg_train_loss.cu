@@ -442,11 +442,16 @@ distillation_kernel(const pg_distillation_args a, float k, float soft, float har
         const int rest = row.pieces + (static_cast<int>(threadIdx.x) - row.pieces % T + T) % T;      // this thread's first piece behind the row's
         if constexpr (GRAD) {
             m = all_sums<POWER, T / 32>(s_sums[flip], k);
-            const float to_soft = soft != 0.0f && s_any[flip] ? g * soft * (kLog2e / k) : 0.0f, to_hard = label >= 0 && label < a.classes ? g * hard : 0.0f;
+            const bool listed = soft != 0.0f && s_any[flip], labelled = label >= 0 && label < a.classes;
+            const float to_soft = listed ? g * soft * (kLog2e / k) : 0.0f, to_hard = labelled ? g * hard : 0.0f;
             const Slope<POWER> slope = {k, m.r, m.r, to_soft / m.s, to_hard / m.s1};
             const Out out(a.dlogits, at.b, at.t, a.classes);
             const int shift = row.off - out.off;
-            if (shift == 0) {
+            if (!listed && !labelled) {                // no term depends on the row: zeros, whatever its logits are
+                const uint32_t zeros[4] = {};
+                walk(out, [&](int j) { out.store(j, zeros); }, [&](int j) { out.store_part(j, zeros); });
+                for (int j = threadIdx.x; j < pieces; j += T) ask(j);
+            } else if (shift == 0) {
                 walk(
                     row,
                     [&](int j) {
@@ -623,7 +628,8 @@ distillation_stream_kernel(const pg_distillation_args a, float k, float soft, fl
         m.s1 = POWER > 1 ? ex2((lse1 - m.r) * kLog2e) : 1.0f;
         r1 = POWER == 0 ? lse1 : m.r;
     }
-    const float to_soft = soft != 0.0f && s_any ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
+    const bool listed = soft != 0.0f && s_any, none = !listed && !label.is;               // none: zeros, whatever logits and lse are
+    const float to_soft = listed ? g * soft * (kLog2e / k) : 0.0f, to_hard = label.is ? g * hard : 0.0f;
     const Slope<POWER> slope = {k, m.r, r1, to_soft / m.s, to_hard / m.s1};
     const Out out(a.dlogits, b, t, a.classes);
     const int share = (out.pieces + gridDim.z - 1) / gridDim.z, first = blockIdx.z * share, last = min(out.pieces, first + share);
@@ -639,9 +645,9 @@ distillation_stream_kernel(const pg_distillation_args a, float k, float soft, fl
                 const int j = j0 + u * T;
                 if (j < last) {
                     F2 v[4];
-                    uint32_t w[4];
+                    uint32_t w[4] = {};
                     logits_of<H>(p[u], v);
-                    slope.template apply<H>(v, w);
+                    if (!none) slope.template apply<H>(v, w);
                     if (j >= out.first && j < out.last) out.store(j, w);
                     else out.store_part(j, w);
                 }

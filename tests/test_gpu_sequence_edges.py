@@ -87,3 +87,43 @@ def test_calls_of_two_sizes_from_several_host_threads(tr, monkeypatch, make, siz
     assert not wrong, "%d calls failed, the first with %d" % (len(wrong), wrong[0])
     for (outputs, _), w in zip(jobs, want):
         assert all(torch.equal(p, q) for p, q in zip(outputs, w))
+
+
+# ---------------------------------------------------------------- loss
+@pytest.mark.parametrize("n", [70, 3000, 30001, 110000])
+@pytest.mark.parametrize("which", ["neither", "list at weight 0", "labels at weight 0"])
+def test_the_gradient_of_a_loss_without_terms(tr, n, which):
+    x, ids, teacher, labels = loss_inputs(gen(n), 1, 3, n, 4, HF, True, 0)
+    x[0, 0, 5], x[0, 1, 7], x[0, 2] = 1000.0, math.nan, -math.inf
+    kw = {"neither": {}, "list at weight 0": dict(ids=ids, teacher=teacher, alpha=0.0), "labels at weight 0": dict(labels=labels, alpha=1.0)}[which]
+    ones = torch.ones(1, 3, device="cuda")
+    r = tr.pg_distillation_loss(x, dloss=ones, **kw)
+    assert not r.loss.any() and not r.lse.any() and not r.dlogits.any()
+    assert not tr.pg_distillation_loss_grad(ones, x, r.lse, **kw).any()
+
+
+@pytest.mark.parametrize("n", [50, 3000, 30001, 110000])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 1.7])
+def test_rows_without_a_term_have_no_gradient(tr, n, tau):
+    """Rows of padding: no label, an empty list or one of logits -inf, and any numbers as logits.  The rows around them stay as they are."""
+    g = gen(n)
+    x, ids, teacher, labels = loss_inputs(g, 2, 6, n, 8, BF, True, 0)
+    ids[0, 1], ids[0, 4], teacher[1, 2], ids[1, 5] = -1, n, -math.inf, -7
+    none = torch.zeros(2, 6, dtype=torch.bool, device="cuda")
+    for row in ((0, 1), (0, 4), (1, 2), (1, 5)):
+        labels[row], none[row] = -100, True
+    dloss = rand(g, 2, 6)
+    kw = dict(ids=ids, teacher=teacher, labels=labels, temperature=tau, alpha=0.4)
+    clean = tr.pg_distillation_loss(x, dloss=dloss, **kw)
+    assert not clean.loss[none].any() and not clean.dlogits[none].any()
+    x[0, 1], x[0, 4, n // 2], x[1, 2], x[1, 5, 0] = math.nan, math.inf, -math.inf, 3e38
+    for pad in (0, 1):
+        out = strided(torch.ones_like(x), pad)
+        r = tr.pg_distillation_loss(x, dloss=dloss, out=out, **kw)
+        back = strided(torch.ones_like(x), pad)
+        tr.pg_distillation_loss_grad(dloss, x, r.lse, out=back, **kw)
+        assert not r.loss[none].any() and not out[none].any() and not back[none].any()
+        assert torch.equal(r.loss[~none], clean.loss[~none]) and torch.equal(out[~none], clean.dlogits[~none])
+    here = x.clone()
+    tr.pg_distillation_loss(here, dloss=dloss, out=here, **kw)
+    assert torch.equal(here, clean.dlogits)
