@@ -558,25 +558,35 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
     const float rate = PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]) * kLog2e;
     const int64_t first = sequence * chunks;
     constexpr int U = 8;                               // chunks whose numbers are on their way at once
-    auto join = [&](float* v, float carry, bool backwards) {
-        for (int c0 = 0; c0 < chunks; c0 += U) {
-            float own[U], sum[U];
+    auto join = [&](float* v, float carry, int64_t from, int64_t step) {       // from chunk `from` on, forwards or backwards
+        float* mine = v + (first + from) * width + at;
+        const float* steps = sums + (first + from) * channels + d;
+        const int64_t by = step * width, steps_by = step * channels;
+        for (int left = chunks; left > 0; left -= U, mine += U * by, steps += U * steps_by) {
+            float own[U], keep[U];
+            auto load = [&](auto place) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    own[i] = PGT_LOAD(mine[place(i) * by]);
+                    keep[i] = PGT_LOAD(steps[place(i) * steps_by]);
+                }
+            };
+            if (left >= U) load([](int i) { return i; });
+            else load([&](int i) { return min(i, left - 1); });
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int64_t k = first + (backwards ? chunks - 1 - c0 - i : c0 + i);
-                own[i] = c0 + i < chunks ? PGT_LOAD(v[k * width + at]) : 0.0f;
-                sum[i] = c0 + i < chunks ? PGT_LOAD(sums[k * channels + d]) : 0.0f;
+                const float sum = keep[i];             // (0: no tokens, which keep everything whatever the rate is)
+                keep[i] = ex2(sum == 0.0f ? 0.0f : sum * rate);
             }
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int64_t k = first + (backwards ? chunks - 1 - c0 - i : c0 + i);
-                if (c0 + i < chunks) PGT_STORE(v[k * width + at], carry);
-                carry = fmaf(ex2(sum[i] * rate), carry, own[i]);
+                if (i < left) PGT_STORE(mine[i * by], carry);
+                carry = fmaf(keep[i], carry, own[i]);
             }
         }
     };
-    join(states, state ? PGT_LOAD(state[sequence * width + at]) : 0.0f, false);
-    if (carries) join(carries, 0.0f, true);
+    join(states, state ? PGT_LOAD(state[sequence * width + at]) : 0.0f, 0, 1);
+    if (carries) join(carries, 0.0f, chunks - 1, -1);
 }
 
 // ---------------------------------------------------------------- scan gradient
@@ -597,20 +607,22 @@ constexpr int kGradChunk = 36, kGradAlone = 52;
 constexpr int kGradBlocks = 3;                         // resident per SM
 
 // Every token and channel of a chunk once, into shared memory ([token][channel]): the step, what reaches y before the gate, u as it is, and (s_dz)
-// what dz is a multiple of.  A thread has channel d.  Tokens behind the last one, to `rows`, and channels that are not there: zeros.
+// what dz is a multiple of.  A thread has channel d.  The chunk's tokens are the last `count` of `rows`; in place of those before them, and of channels
+// that are not there: zeros.
 template <typename H, int LANES>
 __device__ __forceinline__ void prepare_chunk(const pg_scan_grad_args& a, int64_t b, int64_t at, int count, int rows, int d, float bias, float* s_step, float* s_dv,
                                               float* s_dz, uint16_t* s_u) {
     constexpr int CH = kScanThreads / LANES, U = 4;    // tokens on their way at once
     const bool gated = a.z.data != nullptr, is = d < a.channels;
-    auto rows_of = [&](const pg_matrix& m) { return static_cast<const uint16_t*>(m.data) + b * m.stride + at * m.ld + d; };
+    const int pad = rows - count;
+    auto rows_of = [&](const pg_matrix& m) { return static_cast<const uint16_t*>(m.data) + b * m.stride + (at - pad) * m.ld + d; };
     const uint16_t *u = rows_of(a.u), *delta = rows_of(a.delta), *dy = rows_of(a.dy), *z = gated ? rows_of(a.z) : nullptr;
     for (int k0 = threadIdx.x / CH; k0 < rows; k0 += U * LANES) {
         uint16_t ru[U], rd[U], rg[U], rz[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int k = k0 + i * LANES;
-            const bool there = is && k < count;
+            const bool there = is && k >= pad && k < rows;
             ru[i] = there ? PGT_LOAD(u[k * a.u.ld]) : 0;
             rd[i] = there ? PGT_LOAD(delta[k * a.delta.ld]) : 0;
             rg[i] = there ? PGT_LOAD(dy[k * a.dy.ld]) : 0;
@@ -631,7 +643,7 @@ __device__ __forceinline__ void prepare_chunk(const pg_scan_grad_args& a, int64_
             for (int w = 0; w < 2; ++w) {
                 const int k = k0 + (i + w) * LANES, to = k * CH + threadIdx.x % CH;
                 if (k < rows) {
-                    s_step[to] = is && k < count ? step[w] : 0.0f;
+                    s_step[to] = is && k >= pad ? step[w] : 0.0f;
                     s_dv[to] = dv[w];
                     if (s_dz) s_dz[to] = dz[w];
                     s_u[to] = ru[i + w];
@@ -815,7 +827,10 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
         const int64_t sequence = b * a.sequences + s, first = static_cast<int64_t>(s) * a.length;
         const int have = tokens_of(a.lengths, b, a.sequences, s, a.length);
         const int t0 = at_chunk * chunk, t1 = min(a.length, t0 + chunk), count = max(0, min(t1, have) - t0);
-        const int groups = (count + kGroup - 1) / kGroup;
+        // Token k is at place k + pad, so that the last group is full.  The places before the first token change nothing: their step is zero, their
+        // decay 1, and what they would add to dA is 0 times what the first token adds; behind the last one it would be 0 times a
+        // state that dA does not depend on, and that may not be finite.
+        const int groups = (count + kGroup - 1) / kGroup, pad = groups * kGroup - count;
         const int64_t at = first + t0;
         __syncthreads();                               // (shared memory is free again)
         const uint16_t* bb = static_cast<const uint16_t*>(a.b.data) + b * a.b.stride + at * a.b.ld;
@@ -823,9 +838,9 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
 #pragma unroll 4
         for (int i = threadIdx.x; i < groups * kGroup * N; i += kScanThreads) {
             const int k = i / N, n = i % N;
-            const bool is_there = k < count && n < a.states;
-            s_b[i] = is_there ? Elem<H>::up(PGT_LOAD(bb[k * a.b.ld + n])) : 0.0f;
-            s_c[i] = is_there ? Elem<H>::up(PGT_LOAD(cc[k * a.c.ld + n])) : 0.0f;
+            const bool is_there = k >= pad && n < a.states;
+            s_b[i] = is_there ? Elem<H>::up(PGT_LOAD(bb[(k - pad) * a.b.ld + n])) : 0.0f;
+            s_c[i] = is_there ? Elem<H>::up(PGT_LOAD(cc[(k - pad) * a.c.ld + n])) : 0.0f;
         }
         F2 h[P / 2], g[P / 2];
         const int64_t state_at = (sequence * a.channels + d) * a.states + n0, chunk_at = ((sequence * chunks + at_chunk) * a.channels + d) * a.states + n0;
@@ -873,7 +888,7 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
             }
 #pragma unroll
             for (int i = 0; i < kGroup; ++i) {
-                const int k = group * kGroup + i;      // tokens behind the last one change nothing: their step is zero
+                const int k = group * kGroup + i;
                 step[i] = s_step[k * CH + c];
                 in[i] = Elem<H>::up(s_u[k * CH + c]);
                 dv[i] = s_dv[k * CH + c];
@@ -948,12 +963,12 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
             }
             __syncthreads();                           // (what the group before this one left is read by now)
             for (int i = threadIdx.x; i < kGroup * 2 * N; i += kScanThreads) {
-                const int k = group * kGroup + i / (2 * N);
+                const int k = group * kGroup + i / (2 * N) - pad;
                 const float* from = reds + i;
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) v += from[w * kGroup * 2 * N];
-                if (k < count) PGT_STORE(my_parts[(at + k) * 2 * N + i % (2 * N)], v);
+                if (k >= 0) PGT_STORE(my_parts[(at + k) * 2 * N + i % (2 * N)], v);
             }
             if constexpr (kSlots > 1) __syncthreads(); // (the next group's sums go over these)
         }
@@ -963,7 +978,7 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
             uint16_t *du = rows_of(a.du), *ddelta = rows_of(a.ddelta), *dz = gated ? rows_of(a.dz) : nullptr;
 #pragma unroll 2
             for (int k = threadIdx.x / CH; k < t1 - t0; k += LANES) {
-                const int s_at = k * CH + threadIdx.x % CH;
+                const int s_at = (k + pad) * CH + threadIdx.x % CH;
                 const bool is_there = k < count;
                 const float dd = is_there ? s_step[s_at] : 0.0f;
                 dbias += dd;

@@ -127,3 +127,33 @@ def test_rows_without_a_term_have_no_gradient(tr, n, tau):
     here = x.clone()
     tr.pg_distillation_loss(here, dloss=dloss, out=here, **kw)
     assert torch.equal(here, clean.dlogits)
+
+
+# ---------------------------------------------------------------- scan
+# (length of the sequence, tokens that are there)
+@pytest.mark.parametrize("length,have", [(4, 4), (5, 5), (5, 4), (7, 6), (52, 51), (90, 90), (90, 31), (90, 61)])
+@pytest.mark.parametrize("gate", [False, True])
+def test_what_the_last_token_does_not_reach(tr, length, have, gate):
+    """dA depends on neither the last token's u nor its b, and what the last token gives dB, du and ddelta does not depend on a, or only through
+    the state before it: a NaN there leaves those as they are, bit for bit, wherever the last token lies in its group of tokens and chunk."""
+    g = gen(length + have)
+    n, m = 40, 16
+    c, more = scan_inputs(g, 1, 1, length, n, m, BF, gate, True, False, 0)
+    more["lengths"] = torch.tensor([[have]], dtype=torch.int32, device="cuda")
+    dy = rand(g, 1, length, n).to(BF)
+    want = tr.pg_selective_scan_grad(dy, **c, **more)
+    assert all(torch.isfinite(v).all() for v in want if v is not None)
+    other = [d for d in range(n) if d != 3]
+    u = c["u"].clone()
+    u[0, have - 1, 3] = math.nan
+    got = tr.pg_selective_scan_grad(dy, **{**c, "u": u}, **more)
+    assert torch.equal(got.da, want.da) and torch.equal(got.ddelta_bias[0, other], want.ddelta_bias[0, other])
+    b = c["b"].clone()
+    b[0, have - 1, 5] = math.inf
+    got = tr.pg_selective_scan_grad(dy, **{**c, "b": b}, **more)
+    assert torch.equal(got.da, want.da) and torch.equal(got.dskip, want.dskip)
+    a = c["a"].clone()
+    a[0, 3, 5] = math.nan
+    got = tr.pg_selective_scan_grad(dy, **{**c, "a": a}, **more)
+    assert torch.equal(got.du[0, have - 1], want.du[0, have - 1]) and torch.equal(got.db[0, have - 1], want.db[0, have - 1])
+    assert torch.equal(got.da[0, other], want.da[0, other]) and torch.isnan(got.da[0, 3, 5])
