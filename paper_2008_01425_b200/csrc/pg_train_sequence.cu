@@ -345,6 +345,18 @@ struct Item {
     }
 };
 
+// A rate a as a power of two's exponent for a step of 1.  The least finite number stands for -inf, whose product with the step 0 (of tokens that only
+// fill a tile) would be NaN.
+__device__ __forceinline__ float exponent_of(float rate) {
+    const float e = rate * kLog2e;
+    return e == __int_as_float(0xff800000) ? -3.4028235e38f : e;
+}
+__device__ __forceinline__ F2 exponent_of(F2 rate) {
+    float a, b;
+    split(rate, a, b);
+    return pair(exponent_of(a), exponent_of(b));
+}
+
 // P neighbouring fp32 numbers, `there` of them, in pairs.
 template <int P>
 __device__ __forceinline__ void load_states(const float* from, int there, bool wide, F2 (&v)[P / 2]) {
@@ -439,7 +451,7 @@ scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict_
             const float* rates = static_cast<const float*>(a.a.data) + item.b * a.a.stride + d * a.a.ld + n0;
             load_states<P>(rates, mine, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
 #pragma unroll
-            for (int p = 0; p < P / 2; ++p) rate[p] = mul(rate[p], both(kLog2e));
+            for (int p = 0; p < P / 2; ++p) rate[p] = exponent_of(rate[p]);
             bias = is && a.delta_bias ? PGT_LOAD(a.delta_bias[item.b * a.delta_bias_stride + d]) : 0.0f;
             skip = is && a.skip ? PGT_LOAD(a.skip[item.b * a.skip_stride + d]) : 0.0f;
         }
@@ -555,7 +567,7 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
     const int64_t sequence = blockIdx.x / blocks, b = sequence / sequences, at = static_cast<int64_t>(blockIdx.x % blocks) * 128 + threadIdx.x;
     if (at >= width) return;
     const int64_t d = at / n_states, n = at % n_states;
-    const float rate = PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]) * kLog2e;
+    const float rate = exponent_of(PGT_LOAD(static_cast<const float*>(rates.data)[b * rates.stride + d * rates.ld + n]));
     const int64_t first = sequence * chunks;
     constexpr int U = 8;                               // chunks whose numbers are on their way at once
     auto join = [&](float* v, float carry, int64_t from, int64_t step) {       // from chunk `from` on, forwards or backwards
@@ -677,7 +689,7 @@ scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, fl
     load_states<P>(rates, there, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
 #pragma unroll
     for (int p = 0; p < P / 2; ++p) {
-        rate[p] = mul(rate[p], both(kLog2e));
+        rate[p] = exponent_of(rate[p]);
         h[p] = g[p] = both(0.0f);
         product[p] = both(1.0f);
     }
@@ -814,7 +826,7 @@ scan_grad_kernel(const pg_scan_grad_args a, const float* __restrict__ states, co
         load_states<P>(rates, there, reinterpret_cast<uintptr_t>(rates) % 16 == 0, rate);
 #pragma unroll
         for (int p = 0; p < P / 2; ++p) {
-            rate[p] = mul(rate[p], both(kLog2e));
+            rate[p] = exponent_of(rate[p]);
             da[p] = both(0.0f);
         }
     }

@@ -157,3 +157,28 @@ def test_what_the_last_token_does_not_reach(tr, length, have, gate):
     got = tr.pg_selective_scan_grad(dy, **{**c, "a": a}, **more)
     assert torch.equal(got.du[0, have - 1], want.du[0, have - 1]) and torch.equal(got.db[0, have - 1], want.db[0, have - 1])
     assert torch.equal(got.da[0, other], want.da[0, other]) and torch.isnan(got.da[0, 3, 5])
+
+
+@pytest.mark.parametrize("length,n,states", [(1, 20, 16), (2, 20, 3), (5, 20, 16), (53, 20, 17), (700, 33, 16)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_states_that_are_forgotten_at_once(tr, length, n, states, ragged):
+    """a = -inf, or so large that a log2(e) is: exp(D a) = 0 for every token, and a sequence without tokens keeps its state."""
+    g = gen(length)
+    c, more = scan_inputs(g, 1, 3, length, n, states, BF, True, True, ragged, 0)
+    if ragged:
+        more["lengths"][0, 0] = 0
+    dy = rand(g, 1, 3 * length, n).to(BF)
+    some = torch.rand(c["a"].shape, device="cuda", generator=g) < 0.5
+    c["a"] = torch.where(some, torch.full_like(c["a"], -1e30), c["a"])
+    f = scan_forward(c, more, length)
+    _, y, slack = scan_output(c, more, f)
+    want, last = tr.pg_selective_scan(**c, **more, state_out=True)
+    check(want, y, slack, BF)
+    check(last, f["h"][-1], f["e"][-1] + 2 * U * f["h"][-1].abs())
+    grads = tr.pg_selective_scan_grad(dy, **c, **more)
+    for rate in (-math.inf, -3.4e38):
+        c["a"] = torch.where(some, torch.full_like(c["a"], rate), c["a"])
+        got, state = tr.pg_selective_scan(**c, **more, state_out=True)
+        assert torch.equal(got, want) and torch.equal(state, last)
+        for p, q in zip(tr.pg_selective_scan_grad(dy, **c, **more), grads):
+            assert torch.equal(p, q)
