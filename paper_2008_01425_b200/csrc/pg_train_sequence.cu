@@ -558,7 +558,8 @@ scan_kernel(const pg_scan_args a, float* __restrict__ states, float* __restrict_
 }
 
 // From the chunks' own parts to the states before them, in place; carries: backwards, from the adjoints' own parts to what reaches
-// a chunk from those behind it.
+// a chunk from those behind it.  A chunk's decay is the square of 2 to half its exponent, at most 2^254: where a state grows beyond fp32's range over a
+// chunk, what is zero before it stays zero.
 __global__ void __launch_bounds__(128)
 join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float* __restrict__ states, float* __restrict__ carries, const float* __restrict__ sums,
                    int sequences, int channels, int n_states, int chunks) {
@@ -587,13 +588,13 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
             else load([&](int i) { return min(i, left - 1); });
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const float sum = keep[i];             // (0: no tokens, which keep everything whatever the rate is)
-                keep[i] = ex2(sum == 0.0f ? 0.0f : sum * rate);
+                const float sum = keep[i], half = 0.5f * (sum * rate);         // (0: no tokens, which keep everything whatever the rate is)
+                keep[i] = ex2(sum == 0.0f ? 0.0f : half > 127.0f ? 127.0f : half);
             }
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 if (i < left) PGT_STORE(mine[i * by], carry);
-                carry = fmaf(keep[i], carry, own[i]);
+                carry = fmaf(keep[i] * carry, keep[i], own[i]);
             }
         }
     };
@@ -665,9 +666,16 @@ __device__ __forceinline__ void prepare_chunk(const pg_scan_grad_args& a, int64_
     }
 }
 
+// fp32's largest number in place of +inf.
+__device__ __forceinline__ F2 finite(F2 v) {
+    float a, b;
+    split(v, a, b);
+    return pair(a > 3.4028235e38f ? 3.4028235e38f : a, b > 3.4028235e38f ? 3.4028235e38f : b);
+}
+
 // Own parts of a chunk for the way in both directions: the last state from a zero one, and the gradient that reaches the state before it.
 template <typename H, int LANES>
-__global__ void __launch_bounds__(kScanThreads)
+__global__ void __launch_bounds__(kScanThreads, 4)
 scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, float* __restrict__ carries, float* __restrict__ sums, int chunk, int chunks) {
     constexpr int P = kGradStates, N = P * LANES, CH = kScanThreads / LANES;
     constexpr int kTile = 20;                          // tokens in shared memory at once
@@ -693,6 +701,14 @@ scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, fl
         h[p] = g[p] = both(0.0f);
         product[p] = both(1.0f);
     }
+    bool growing = false;                              // a rate of the warp's is positive: the product may leave fp32's range
+#pragma unroll
+    for (int p = 0; p < P / 2; ++p) {
+        float lo, hi;
+        split(rate[p], lo, hi);
+        growing = growing || lo > 0.0f || hi > 0.0f;
+    }
+    growing = __any_sync(0xffffffffu, growing);
     float sum = 0.0f;
     for (int from = 0; from < count; from += kTile) {
         const int64_t at = static_cast<int64_t>(s) * a.length + t0 + from;
@@ -708,26 +724,31 @@ scan_grad_local_kernel(const pg_scan_grad_args a, float* __restrict__ states, fl
         }
         prepare_chunk<H, LANES>(a, b, at, rows, rows, step_d, bias, s_step, s_dv, nullptr, s_u);
         __syncthreads();
+        auto walk = [&](auto grows) {
 #pragma unroll 2
-        for (int k = 0; k < rows; ++k) {
-            const float step = s_step[k * CH + c];
-            const F2 steps = both(step), drive = both(step * Elem<H>::up(s_u[k * CH + c])), dv = both(s_dv[k * CH + c]);
-            const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
-            const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(s_c + k * N + n0);
-            sum += step;
+            for (int k = 0; k < rows; ++k) {
+                const float step = s_step[k * CH + c];
+                const F2 steps = both(step), drive = both(step * Elem<H>::up(s_u[k * CH + c])), dv = both(s_dv[k * CH + c]);
+                const ulonglong2* bk = reinterpret_cast<const ulonglong2*>(s_b + k * N + n0);
+                const ulonglong2* ck = reinterpret_cast<const ulonglong2*>(s_c + k * N + n0);
+                sum += step;
 #pragma unroll
-            for (int q = 0; q < P / 4; ++q) {
-                const ulonglong2 bv = bk[q], cv = ck[q];
+                for (int q = 0; q < P / 4; ++q) {
+                    const ulonglong2 bv = bk[q], cv = ck[q];
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int p = 2 * q + w;
-                    const F2 keep = ex2(mul(steps, rate[p]));
-                    h[p] = fma(keep, h[p], mul(drive, F2{w ? bv.y : bv.x}));
-                    product[p] = mul(product[p], keep);
-                    g[p] = fma(mul(product[p], dv), F2{w ? cv.y : cv.x}, g[p]);
+                    for (int w = 0; w < 2; ++w) {
+                        const int p = 2 * q + w;
+                        const F2 keep = ex2(mul(steps, rate[p]));
+                        h[p] = fma(keep, h[p], mul(drive, F2{w ? bv.y : bv.x}));
+                        product[p] = mul(product[p], keep);
+                        if constexpr (decltype(grows)::value) product[p] = finite(product[p]);          // (0 times it is 0)
+                        g[p] = fma(product[p], mul(dv, F2{w ? cv.y : cv.x}), g[p]);
+                    }
                 }
             }
-        }
+        };
+        if (growing) walk(std::true_type{});
+        else walk(std::false_type{});
     }
     const int64_t to = static_cast<int64_t>(blockIdx.x) * a.channels + d;
     store_states<P>(states + to * a.states + n0, there, a.states % 4 == 0, h);

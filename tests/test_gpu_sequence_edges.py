@@ -182,3 +182,43 @@ def test_states_that_are_forgotten_at_once(tr, length, n, states, ragged):
         assert torch.equal(got, want) and torch.equal(state, last)
         for p, q in zip(tr.pg_selective_scan_grad(dy, **c, **more), grads):
             assert torch.equal(p, q)
+
+
+def scan_gradient_needs(tr, b, length, n, m):
+    """Bytes of workspace of the scan's gradient of one sequence a worker."""
+    from paper_2008_01425_b200.binding import load_library
+
+    args, size = tr.pg_scan_grad_args(0, b, 1, length, n, m), ctypes.c_size_t()
+    assert load_library().pg_selective_scan_grad_workspace_bytes(ctypes.byref(args), ctypes.byref(size)) == 0
+    return size.value
+
+
+def gradient_is_chunked(tr, b, length, n, m):
+    """Whether there is room for the states and carries of two chunks besides what grows with the tokens."""
+    per_token = (scan_gradient_needs(tr, b, 33, n, m) - scan_gradient_needs(tr, b, 1, n, m)) / 32
+    return scan_gradient_needs(tr, b, length, n, m) - scan_gradient_needs(tr, b, 1, n, m) - per_token * (length - 1) >= 16 * b * n * m
+
+
+@pytest.mark.parametrize("n,states", [(5, 16), (33, 3), (20, 40)])
+def test_growing_states_that_nothing_has_reached(tr, n, states):
+    """a > 0: over a chunk exp of the sum of steps leaves fp32's range, but what is zero stays zero.  Inputs come with the last tokens, gradients
+    with the first."""
+    g = gen(n)
+    length = 700
+    c, more = scan_inputs(g, 1, 1, length, n, states, BF, False, False, False, 0)
+    c["a"] = torch.rand(1, n, states, device="cuda", generator=g) + 0.5
+    c["delta"] = torch.full_like(c["delta"], 5.0)
+    c["delta_bias"] = torch.zeros_like(c["delta_bias"])
+    c["u"][:, :-8] = 0
+    dy = rand(g, 1, length, n).to(BF)
+    dy[:, 8:] = 0
+    f = scan_forward(c, more, length)
+    _, y, slack = scan_output(c, more, f)
+    got, last = tr.pg_selective_scan(**c, **more, state_out=True)
+    check(got, y, slack, BF)
+    check(last, f["h"][-1], f["e"][-1] + 2 * U * f["h"][-1].abs())
+    assert gradient_is_chunked(tr, 1, length, n, states)
+    want, off = scan_grad_reference(c, more, dy, 64)
+    r = tr.pg_selective_scan_grad(dy, **c, **more)
+    for name in want:
+        check(getattr(r, name), want[name], off[name] + 2 * U * want[name].abs(), None if name in ("da", "dskip", "ddelta_bias") else BF)
