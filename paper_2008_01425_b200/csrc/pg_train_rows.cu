@@ -291,6 +291,24 @@ norm_grad_kernel(const Args a, float* __restrict__ partial, int rows_per_group) 
                 if constexpr (!EIGHT) h_raw[k][c] = octet<W>(h_piece[k][c], row_of(a.h, k), col, a.cols);
                 if (a.dh.data) dh_raw[k][c] = octet<W>(dh_piece[k][c], row_of(a.dh, k), col, a.cols);
             }
+        // Two numbers near bf16's ends are up to twice fp32's range apart.  There, and no other rows have so small an rstd, h and the mean are taken by a quarter.
+        constexpr bool kFar = kMean && std::is_same_v<H, __nv_bfloat16>;
+        constexpr float kFarRstd = 7.8886091e-31f;     // 2^-100
+        if constexpr (kFar) {
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (rstd[k] < kFarRstd) {
+                    mean[k] *= 0.25f;
+                    rstd[k] *= 4.0f;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        if constexpr (EIGHT) q_scale[k][c] = q_scale[k][c] == 255u ? 255u : q_scale[k][c] > 2u ? q_scale[k][c] - 2u : 0u;
+                        else
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h_raw[k][c].w[i] = Elem<H>::down2(mul(Elem<H>::up2(h_raw[k][c].w[i]), both(0.25f)));
+                    }
+                }
+        }
         auto unit = [&](int k, int c, F2 (&u)[4]) {
             if constexpr (EIGHT) widen8(q_raw[k][c], scale_value(q_scale[k][c]), u);
             else widen<H>(h_raw[k][c], u);
@@ -343,7 +361,7 @@ norm_grad_kernel(const Args a, float* __restrict__ partial, int rows_per_group) 
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const F2 minus = both(-dot[k * D] / a.cols), by = both(rstd[k]), less = both(kMean ? -dot[k * D + D - 1] / a.cols : 0.0f);
+            const F2 minus = both(-dot[k * D] / a.cols), by = both(kFar && rstd[k] < 4.0f * kFarRstd ? 0.25f * rstd[k] : rstd[k]), less = both(kMean ? -dot[k * D + D - 1] / a.cols : 0.0f);
             uint16_t* out = static_cast<uint16_t*>(a.dx.data) + b * a.dx.stride + (r + k) * a.dx.ld;
 #pragma unroll
             for (int c = 0; c < C; ++c) {

@@ -222,3 +222,26 @@ def test_growing_states_that_nothing_has_reached(tr, n, states):
     r = tr.pg_selective_scan_grad(dy, **c, **more)
     for name in want:
         check(getattr(r, name), want[name], off[name] + 2 * U * want[name].abs(), None if name in ("da", "dskip", "ddelta_bias") else BF)
+
+
+# ---------------------------------------------------------------- layer norm
+@pytest.mark.parametrize("n", [64, 650, 1029, 5000])
+@pytest.mark.parametrize("from8", [False, True])
+def test_layer_norm_gradient_where_differences_leave_fp32(tr, n, from8):
+    """Rows near bf16's ends: an element may be further from the mean than fp32's largest number."""
+    g = gen(n)
+    b, t = 2, 9
+    h = torch.full((b, t, n), -1.2e38, device="cuda")
+    h[..., 1::7] = 3.2e38
+    h[0, 0], h[0, 1] = -h[0, 0], rand(g, n)           # the other way round, and a row like others
+    h = h.to(BF)
+    held = make8(tr, h, BF) if from8 else h
+    if from8:
+        h = eight(h, BF)[2].to(BF)
+    out = tr.pg_add_layer_norm(h, eps=0.0)
+    dy, gain = rand(g, b, t, n).to(BF), rand(g, b, n)
+    dx, dgain, dbias = tr.pg_add_layer_norm_grad(dy, held, out.mean, out.rstd, gain)
+    want, slack, wg, sg, wb, sb = norm_grad_reference(dy, h, out.mean, out.rstd, gain, None)
+    check(dx, want, slack + 2.0 ** -149, BF)
+    check(dgain, wg, sg)
+    check(dbias, wb, sb)
