@@ -1,13 +1,18 @@
 """The sequence operators where calls, tokens, rows and chunks end: against their formulas in 64 bits, by the tolerances of test_gpu_sequence.py, and
 against calls that must give the same bits."""
 import ctypes
+import json
 import math
+import os
+import subprocess
+import sys
 import threading
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
+from tests import test_gpu_sequence_bounds_checked as bounds  # noqa: E402
 from tests.test_gpu_sequence import (loss_inputs, norm_grad_reference, scan_forward, scan_grad_reference, scan_inputs,  # noqa: E402
                                      scan_output)
 from tests.test_gpu_sequence import test_selective_scan as scan_case, test_selective_scan_gradient as scan_gradient_case  # noqa: E402
@@ -245,3 +250,85 @@ def test_layer_norm_gradient_where_differences_leave_fp32(tr, n, from8):
     check(dx, want, slack + 2.0 ** -149, BF)
     check(dgain, wg, sg)
     check(dbias, wb, sb)
+
+
+# ---------------------------------------------------------------- chunks, and 17 to 32 states
+CHUNKS = [((1, 2, 52, 50), 16, 1), ((1, 2, 53, 50), 16, 0), ((2, 1, 73, 130), 8, 1), ((1, 2, 45, 40), 32, 0), ((1, 1, 300, 20), 24, 1), ((2, 1, 300, 33), 32, 0), ((1, 1, 1100, 9), 20, 0)]
+KINDS = [(BF, True, True, True), (HF, False, False, False)]
+
+
+@pytest.mark.parametrize("shape,states,pad", CHUNKS)
+@pytest.mark.parametrize("dtype,gate,carried,ragged", KINDS)
+def test_scan_at_the_ends_of_chunks(tr, shape, states, pad, dtype, gate, carried, ragged):
+    scan_case(tr, shape, states, pad, dtype, gate, carried, ragged)
+
+
+@pytest.mark.parametrize("shape,states,pad", CHUNKS)
+@pytest.mark.parametrize("dtype,gate,carried,ragged", KINDS)
+def test_scan_gradient_at_the_ends_of_chunks(tr, shape, states, pad, dtype, gate, carried, ragged):
+    assert gradient_is_chunked(tr, 1, shape[2], shape[3], states) == (shape[2] > 52)
+    scan_gradient_case(tr, shape, states, pad, dtype, gate, carried, ragged)
+
+
+def test_chunks_of_more_states_than_a_grid_has_rows(tr):
+    """8.96 million states per sequence, in chunks: a channel's gradients are those it has on its own."""
+    n, m, t = 140000, 64, 73
+    assert gradient_is_chunked(tr, 1, t, n, m) and gradient_is_chunked(tr, 1, t, 16, m)
+    c, more = scan_inputs(gen(11), 1, 1, t, n, m, BF, False, False, False, 0)
+    dy = rand(gen(12), 1, t, n).to(BF)
+    got = tr.pg_selective_scan_grad(dy, **c, **more)
+    for last in (slice(n - 16, n), slice(70000, 70016)):
+        part = {k: v[..., last].contiguous() if k in ("u", "delta", "skip", "delta_bias") else v[:, last].contiguous() if k == "a" else v for k, v in c.items()}
+        want = tr.pg_selective_scan_grad(dy[..., last].contiguous(), **part, **more)
+        assert torch.equal(got.du[..., last], want.du) and torch.equal(got.ddelta[..., last], want.ddelta)
+
+
+def test_what_is_behind_a_sequence_is_not_used_in_chunks(tr):
+    g = gen(9)
+    b, s, length, n, m = 2, 4, 90, 50, 24
+    assert gradient_is_chunked(tr, 1, length, n, m)
+    c, more = scan_inputs(g, b, s, length, n, m, BF, True, True, False, 0)
+    dy = rand(g, b, s * length, n).to(BF)
+    lengths = torch.tensor([[0, 1, 40, 90], [90, 89, 30, 61]], dtype=torch.int32, device="cuda")
+    beyond = (torch.arange(length, device="cuda") >= lengths[..., None]).reshape(b, s * length, 1)
+    dirty = lambda v: torch.where(beyond, torch.full_like(v, math.nan), v)
+    bad = {**c, **{k: dirty(c[k]) for k in ("u", "delta", "b", "c", "z")}}
+    kw = {**more, "lengths": lengths}
+    for f in (lambda q, d: list(tr.pg_selective_scan(**q, **kw, state_out=True)), lambda q, d: list(tr.pg_selective_scan_grad(d, **q, **kw))):
+        for p, q in zip(f(c, dy), f(bad, dirty(dy))):
+            assert torch.isfinite(p).all() and torch.equal(p, q)
+            if p.shape[:2] == (b, s * length):
+                assert not p[beyond.expand_as(p)].any()
+
+
+# ---------------------------------------------------------------- the bounds-checked build
+# workers, sequences, length, channels, states, classes
+MORE_SHAPES = [(1, 2, 52, 50, 16, 33), (1, 2, 53, 50, 16, 700), (2, 1, 73, 65, 8, 64), (1, 2, 45, 40, 24, 70), (2, 1, 300, 33, 32, 500), (1, 1, 130, 9, 20, 9001)]
+
+
+def more_cases():
+    for i, shape in enumerate(MORE_SHAPES):
+        for pad in (0, 1):
+            yield shape + (pad, "float16" if (i + pad) % 2 else "bfloat16")
+
+
+def test_chunks_in_the_bounds_checked_build():
+    """Chunked gradients and 17 to 32 states, as test_gpu_sequence_bounds_checked.py does with its shapes."""
+    from paper_2008_01425_b200 import build as pg_build
+
+    child = bounds.CHILD.replace("test_gpu_sequence_bounds_checked import cases", "test_gpu_sequence_edges import more_cases as cases").replace(
+        "cases, outputs", "cases\nfrom tests.test_gpu_sequence_bounds_checked import outputs")
+    results = []
+    for library in (pg_build.build(checked=True), None):
+        env = {k: v for k, v in os.environ.items() if k != "PG_LIBRARY"}
+        if library:
+            env["PG_LIBRARY"] = library
+        r = subprocess.run([sys.executable, "-c", child % {"root": bounds.ROOT}], cwd=bounds.ROOT, env=env, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, timeout=600)
+        text = r.stdout.decode()
+        assert r.returncode == 0, text[-3000:]
+        results.append(json.loads([l for l in text.splitlines() if l.startswith("RESULT ")][-1][len("RESULT "):]))
+    got, want = results
+    assert sorted(got) == sorted(want) and len(got) == 2 * len(MORE_SHAPES)
+    for name in got:
+        assert got[name][0] == want[name][0] == 0, "%s: status %d in the checked build" % (name, got[name][0])
+        assert got[name][1] == want[name][1], "%s: the checked build gives other bits" % name
