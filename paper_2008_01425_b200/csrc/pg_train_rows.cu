@@ -152,8 +152,8 @@ norm_kernel(const Args a) {
     float sum = sum_of_squares(std::false_type{}), eps = a.eps;
     // bf16 reaches to 2^128 and fp32 squares do not: where the sum leaves fp32's range, at the upper end or (with an eps too small
     // to matter there) at the lower one, it is taken once more of the row times a power of two.  The same for the whole row.
-    if (!(sum <= 3.4028235e38f) || (sum < 8.2718061e-25f && eps < 7.8886091e-31f)) {       // 2^-80, 2^-100
-        scale = sum < 1.0f ? 7.9228163e28f : 1.2621774e-29f;                               // 2^96, 2^-96
+    if (!(sum <= 3.4028235e38f) || (sum < 0x1p-80f && eps < 0x1p-100f)) {
+        scale = sum < 1.0f ? 0x1p96f : 0x1p-96f;
         eps = eps * scale * scale;
         if constexpr (T > 32) __syncthreads();         // (the shares of the first sum have been read)
         sum = sum_of_squares(std::true_type{});
@@ -293,7 +293,7 @@ norm_grad_kernel(const Args a, float* __restrict__ partial, int rows_per_group) 
             }
         // Two numbers near bf16's ends are up to twice fp32's range apart.  There, and no other rows have so small an rstd, h and the mean are taken by a quarter.
         constexpr bool kFar = kMean && std::is_same_v<H, __nv_bfloat16>;
-        constexpr float kFarRstd = 7.8886091e-31f;     // 2^-100
+        constexpr float kFarRstd = 0x1p-100f;
         if constexpr (kFar) {
 #pragma unroll
             for (int k = 0; k < R; ++k)

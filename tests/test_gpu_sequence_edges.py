@@ -252,6 +252,20 @@ def test_layer_norm_gradient_where_differences_leave_fp32(tr, n, from8):
     check(dbias, wb, sb)
 
 
+@pytest.mark.parametrize("n", [70, 650, 1029, 5000])
+@pytest.mark.parametrize("power", [100, -100])
+def test_norms_of_far_rows_are_those_of_near_ones(tr, n, power):
+    """Rows whose squares leave fp32's range are scaled by a power of two, which rounds nothing: the same bits as of the rows at home."""
+    x = rand(gen(n), 2, 6, n).to(BF)
+    far = (x.double() * 2.0 ** power).to(BF)
+    assert torch.equal(far.double(), x.double() * 2.0 ** power)
+    for norm in (tr.pg_add_rms_norm, tr.pg_add_layer_norm):
+        near, out = norm(x, eps=0.0), norm(far, eps=0.0)
+        assert torch.equal(out.y, near.y) and torch.equal(out.rstd.double() * 2.0 ** power, near.rstd.double())
+        if norm is tr.pg_add_layer_norm:
+            assert torch.equal(out.mean.double(), near.mean.double() * 2.0 ** power)
+
+
 # ---------------------------------------------------------------- chunks, and 17 to 32 states
 CHUNKS = [((1, 2, 52, 50), 16, 1), ((1, 2, 53, 50), 16, 0), ((2, 1, 73, 130), 8, 1), ((1, 2, 45, 40), 32, 0), ((1, 1, 300, 20), 24, 1), ((2, 1, 300, 33), 32, 0), ((1, 1, 1100, 9), 20, 0)]
 KINDS = [(BF, True, True, True), (HF, False, False, False)]
