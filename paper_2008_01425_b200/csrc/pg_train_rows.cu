@@ -152,11 +152,17 @@ norm_kernel(const Args a) {
     float sum = sum_of_squares(std::false_type{}), eps = a.eps;
     // bf16 reaches to 2^128 and fp32 squares do not: where the sum leaves fp32's range, at the upper end or (with an eps too small
     // to matter there) at the lower one, it is taken once more of the row times a power of two.  The same for the whole row.
-    if (!(sum <= 3.4028235e38f) || (sum < 0x1p-80f && eps < 0x1p-100f)) {
+    // (Differences that small, from a mean of 1 or more, are zeros.)
+    if (!(sum <= 3.4028235e38f) || (sum < 0x1p-80f && eps < 0x1p-100f && fabsf(mean) < 1.0f)) {
         scale = sum < 1.0f ? 0x1p96f : 0x1p-96f;
         eps = eps * scale * scale;
         if constexpr (T > 32) __syncthreads();         // (the shares of the first sum have been read)
         sum = sum_of_squares(std::true_type{});
+        if (kMean && sum == 0.0f) {                    // equal values: eps as it is decides
+            mean *= 1.0f / scale;
+            scale = 1.0f;
+            eps = a.eps;
+        }
     }
     const float rstd = rsqrtf(sum / a.cols + eps);     // of the scaled row
     if (a.rstd && t == 0) PGT_STORE(a.rstd[b * a.tokens + tok], rstd * scale);
@@ -306,6 +312,16 @@ norm_grad_kernel(const Args a, float* __restrict__ partial, int rows_per_group) 
                         else
 #pragma unroll
                             for (int i = 0; i < 4; ++i) h_raw[k][c].w[i] = Elem<H>::down2(mul(Elem<H>::up2(h_raw[k][c].w[i]), both(0.25f)));
+                    }
+                } else if (!EIGHT && !(fabsf(mean[k] * rstd[k]) <= 3.4028235e38f)) {
+                    // A row of equal values far from zero, the mean.  What is past the row's end is that, too: from zero it would be infinitely far.
+                    const uint32_t same = Elem<H>::down2(both(mean[k]));
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        const int left = a.cols - (c * T + t) * 8;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            h_raw[k][c].w[i] = 2 * i + 1 < left ? h_raw[k][c].w[i] : 2 * i < left ? (h_raw[k][c].w[i] & 0xffffu) | (same & 0xffff0000u) : same;
                     }
                 }
         }

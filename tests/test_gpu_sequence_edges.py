@@ -266,6 +266,26 @@ def test_norms_of_far_rows_are_those_of_near_ones(tr, n, power):
             assert torch.equal(out.mean.double(), near.mean.double() * 2.0 ** power)
 
 
+@pytest.mark.parametrize("n", [2, 64, 650, 1029, 5000, 16384])
+@pytest.mark.parametrize("eps", [1e-5, 1e-35])
+def test_layer_norm_of_rows_of_equal_values(tr, n, eps):
+    """Rows that a mask filled with bf16's lowest number, and others: y is the bias and rstd is eps ^ -1/2 (sums of equal 16-bit values are exact)."""
+    g = gen(n)
+    values = [torch.finfo(BF).min, torch.finfo(BF).max, 3e36, 1e10, 1.0, 1e-20, 0.0]
+    x = torch.tensor(values, device="cuda").to(BF)[:, None].expand(-1, n).contiguous()
+    gain, bias = rand(g, n), rand(g, n)
+    out = tr.pg_add_layer_norm(x, gain, bias, eps=eps)
+    root = torch.full((len(values),), float(torch.tensor(eps, dtype=torch.float32)), dtype=torch.float64, device="cuda") ** -0.5
+    check(out.y, bias.double().expand_as(x), torch.zeros_like(x, dtype=torch.float64), BF)
+    check(out.mean, x[:, 0].double(), 0 * root)
+    check(out.rstd, root, 32 * U * root)
+    dy = rand(g, len(values), n).to(BF)
+    dx, dgain, dbias = tr.pg_add_layer_norm_grad(dy, x, out.mean, out.rstd, gain)
+    want, slack = norm_grad_reference(dy[None], x[None], out.mean[None], out.rstd[None], gain[None], None)[:2]
+    check(dx, want[0], slack[0], BF)
+    assert not dgain.any()
+
+
 # ---------------------------------------------------------------- chunks, and 17 to 32 states
 CHUNKS = [((1, 2, 52, 50), 16, 1), ((1, 2, 53, 50), 16, 0), ((2, 1, 73, 130), 8, 1), ((1, 2, 45, 40), 32, 0), ((1, 1, 300, 20), 24, 1), ((2, 1, 300, 33), 32, 0), ((1, 1, 1100, 9), 20, 0)]
 KINDS = [(BF, True, True, True), (HF, False, False, False)]
