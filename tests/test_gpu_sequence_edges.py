@@ -13,7 +13,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import test_gpu_sequence_bounds_checked as bounds  # noqa: E402
-from tests.test_gpu_sequence import (loss_inputs, norm_grad_reference, scan_forward, scan_grad_reference, scan_inputs,  # noqa: E402
+from tests.test_gpu_sequence import (check_loss, loss_inputs, norm_grad_reference, scan_forward, scan_grad_reference, scan_inputs,  # noqa: E402
                                      scan_output)
 from tests.test_gpu_sequence import test_selective_scan as scan_case, test_selective_scan_gradient as scan_gradient_case  # noqa: E402
 from tests.test_gpu_training import BF, HF, U, check, eight, gen, make8, rand, strided  # noqa: E402
@@ -132,6 +132,13 @@ def test_rows_without_a_term_have_no_gradient(tr, n, tau):
     here = x.clone()
     tr.pg_distillation_loss(here, dloss=dloss, out=here, **kw)
     assert torch.equal(here, clean.dlogits)
+
+
+@pytest.mark.parametrize("top", [127, 128, 129, 1024])
+def test_lists_as_long_as_a_row_a_warp_has_room_for(tr, top):
+    """Up to 128 entries the loss alone of many rows is computed by a warp each, whose lists fill a block's shared memory then."""
+    x, ids, teacher, labels = loss_inputs(gen(top), 1, 4736, 1500, top, BF, True, 1)
+    check_loss(tr, x, ids, teacher, labels, 2.0, 0.5, torch.ones(1, 4736, device="cuda"), BF)
 
 
 # ---------------------------------------------------------------- scan
