@@ -286,7 +286,8 @@ PG_API int pg_causal_conv_grad(const pg_conv_grad_args *args, void *workspace, s
  *     D_t = log(1 + exp(delta_t + delta_bias))
  *     h_t = exp(D_t a) h_{t-1} + D_t u_t b_t,   y_t = (sum over states of c_t h_t + skip u_t) s(z_t) z_t
  * with s as above; without z the last factors are left out.  u, delta, z and y have a column per channel, b and c one per state, a
- * is fp32, channels x states (a layer of the stack), and not positive where states are to decay.  States are fp32.
+ * is fp32, channels x states (a layer of the stack), and not positive where states are to decay; -inf forgets a state at every token.
+ * States are fp32.
  * Where there are few sequences they are cut into chunks that run side by side, whose states the workspace joins.
  */
 typedef struct pg_scan_args {
@@ -355,7 +356,8 @@ PG_API int pg_selective_scan_grad(const pg_scan_grad_args *args, void *workspace
  *
  * The gradient dloss (alpha tau (q - p) + (1 - alpha) (softmax(x) - [label])) goes to dlogits: by pg_distillation_loss
  * together with the loss, reading the logits once (to 100000 classes; twice above), or by pg_distillation_loss_grad from lse,
- * which it reads (and whose step, 2^-24 of its size, is the error of the probabilities' logarithms then).  At most 1024 entries in a list (PG_ERR_TOO_LARGE).
+ * which it reads (and whose step, 2^-24 of its size, is the error of the probabilities' logarithms then).  At most 1024 entries in a
+ * list (PG_ERR_TOO_LARGE); the gradient's time goes with the square of their number from some 100 on.
  */
 typedef struct pg_distillation_args {
     int32_t dtype, batch, tokens, classes, top;

@@ -6,9 +6,11 @@
 // size, a type's lowest number among them, are told apart as well as the type does.  Where tau is 1, 2 or 4 the exponentials at temperature 1
 // are powers of these; elsewhere there are two per logit.  With the gradient the row stays in shared memory as it was read, so the
 // logits are read once.  Memory bounds it, 2 bytes a logit for the loss and 4 with the gradient, and nearly as much the exponential unit:
-// 22400 rows of 28000 classes at tau = 2 take 245 us (0.78 of the copy rate), with the gradient 489 us (0.78), in a steady run under the power cap
-// 276 and 560; with two exponentials a logit (tau = 1.7) 365 and 720 us.  Exponentials of the first pass kept in registers for the second
+// 22400 rows of 28000 classes at tau = 2 take 245 us (0.78 of the copy rate), with the gradient 493 us (0.78), in a steady run under the power cap
+// 270 and 558; with two exponentials a logit (tau = 1.7) 365 and 720 us.  Exponentials of the first pass kept in registers for the second
 // (512 threads, one block an SM): 1.3 times as long, since a block's phases then wait for one another.
+// Fewer blocks are resident where rows are longer, one above 57000 classes: 5600 rows of 50000, 64000, 98000 and 128000 classes take 119, 168, 231
+// and 244 us (bytes: 85, 109, 167, 218), with the gradient 262, 410, 558 and, the logits read twice, 679 us; 128000 from lse 469 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -252,7 +254,9 @@ struct Label {
 };
 
 // The classes of the list and the label once more, with what the formula takes off there, by threads `at`, at + step, ..; classes from
-// `from` to `to` - 1 only.  A class that is listed twice is computed twice, from the same sum.
+// `from` to `to` - 1 only.  A class that is listed twice is computed twice, from the same sum.  The work goes with the square of the list's length; a
+// warp beside the row's hides it to some 32 entries: 22400 rows of 28000 classes with gradient take 493 us with 32 entries, 559 with 64, 710
+// with 128, 1840 with 300 and 20900 with 1024.
 template <typename H, int POWER>
 __device__ __forceinline__ void take_off(const Out& out, const List& list, int top, const Label<H>& label, const Slope<POWER>& slope, const Sums& m, bool soft,
                                          float to_soft, float to_hard, int at, int step, int from, int to) {

@@ -56,7 +56,8 @@ __device__ __forceinline__ void octet_to_8(F2 (&v)[4], int8_t* row, uint8_t* sca
 // T threads hold one row, C octets each; a block has 256 / T rows of one worker, at least one.  The row is read
 // once; the sum of squares comes from the registers, and so does the mean before it in the layer norm (Args =
 // pg_layer_norm_args), whose squares are those of the differences from the mean: no digits cancel, at the price of a second sum.
-// (Its two sums keep a row waiting longer: four blocks an SM to 768 columns, 64 registers, instead of three: 32 x 700 x 650 39.6 -> 35.8 us.)
+// (Its two sums keep a row waiting longer: to 768 columns four blocks an SM, 64 registers, instead of what the compiler takes: 32 x 700 x 650 in 34 instead
+// of 37 us with 16-bit output, 40 instead of 43 with 8 bits beside it, all with host and allocation in a steady run.)
 template <typename Args> constexpr bool kCentred = std::is_same_v<Args, pg_layer_norm_args> || std::is_same_v<Args, pg_layer_norm_grad_args>;
 template <typename H, int W, int WO, int C, int T, typename Args>
 __global__ void __launch_bounds__(T > 32 ? T : 256, kCentred<Args> && T == 32 && C <= 3 ? 4 : 0)
@@ -617,6 +618,10 @@ constexpr int kMaxNormCols = 16384;
 // the exchange between warps or there is no room for more threads.  `blocks`: resident per SM.  The last one holds kMaxNormCols.
 // 134 MB matrices of 64 workers, 1024 to 16384 columns by powers of two: 94, 114, 128, 109 and 174 us (4.3, 3.5, 3.1, 3.7 and 2.3
 // TB/s).  Above 4096 columns the registers of 512 and 1024 threads do not hold it all and 112 to 560 bytes a thread are spilled.
+// Those are the root-mean-square norm's.  The layer norm's second sum per column takes as many registers again as its first: 0 to 40 bytes a thread are
+// spilled at 257 to 512 columns (120 to 210 where rows start anywhere), 24 to 44 at 513 to 1024 columns where rows start anywhere, 316 to
+// 672 from 4097 and 660 to 792 from 8193 columns on.  32 workers' 29 MB matrices of 512, 650, 1024, 2048 and 4608 columns: 36, 67, 40, 46 and 81 us;
+// from the 8-bit form 36, 63, 41, 51 and 90 us.
 struct GradRow { int octets, threads, rows, blocks; };
 constexpr int kGradShapes = 7;
 constexpr GradRow kGradRows[kGradShapes] = {{1, 32, 2, 4}, {2, 32, 2, 3}, {1, 128, 2, 5}, {1, 256, 2, 2}, {1, 512, 2, 1}, {2, 512, 2, 1}, {2, 1024, 1, 1}};

@@ -55,7 +55,7 @@ struct Rows {
 // the last width - 1 tokens in registers: every input is read once, but for the few before a run.  Inputs come through shared memory in
 // 16-byte pieces, whatever the rows' alignment, a tile of tokens ahead.  4 bytes a value (6 in the gradient) have to move; instructions (some
 // 60 for two values of a lane) bound it at 0.45 of the copy rate: 32 x 700 tokens x 1300 channels 43 us.  (Eight channels a thread, cut out of
-// their pieces in registers: 88 us.  Plain 2- and 4-byte loads: 43 us, but the gradient of odd widths 145 us instead of 66.)
+// their pieces in registers: 88 us.  Plain 2- and 4-byte loads: 43 us, but the gradient of odd widths 145 us instead of 63.)
 constexpr int kRun = 64;                               // tokens of a run at most
 constexpr int kConvThreads = 128;
 constexpr int kStrip = 64;                             // channels
@@ -320,8 +320,11 @@ __device__ __forceinline__ F2 softplus(F2 v) {
 // A channel's states lie in LANES neighbouring threads, P each, in pairs.  A block takes CH channels of one sequence at a time, or of a
 // chunk of it (an item), in tiles of kScanTile tokens; the next tile is on its way while one is worked on.  Items are numbered by
 // worker, channels, sequence and chunk, and a block has neighbours of them, so that it keeps its channels' rates as long as possible.
-// The exponential unit bounds it: 16 states and the softplus and the gate take 20 exponentials or reciprocals per token and channel, 145 us
-// for 32 x 700 tokens x 1300 channels at 1.9 GHz, where it takes 244 us (issue slots 53 % and the unit 58 % busy; without tiles ahead 431 us).
+// The exponential unit is its floor: 16 states and the softplus and the gate take 20 exponentials or reciprocals per token and channel, 145 us
+// for 32 x 700 tokens x 1300 channels at 1.9 GHz, where it takes 244 us (issue slots 55 % and the unit 58 % busy, the rest is waiting with 24 warps an SM;
+// without tiles ahead 431 us).  Without states carried: 170 us with 4 and 8 states, 236 with 16, 526 with 32, 1197 with 64.  B and C of the tile
+// on its way take 4 registers a thread at 16 states and 16 at 64; of the 80 that six blocks leave, 16 to 26 bytes are spilled to 16 states, 198
+// to 32 and 280 to 64.
 // A polynomial on the multiply-add pipes for an eighth of the exponentials: 3 % slower.  4 to 7 blocks an SM, two or four tokens
 // side by side: within 10 % of one another.
 constexpr int kScanThreads = 128;
@@ -609,13 +612,16 @@ join_chunks_kernel(const pg_matrix rates, const float* __restrict__ state, float
 //     dD_t = u_t (g_t . B_t) + sum over states of A e_t,   e_t = g_t h_t-1 exp(D_t A)
 //     dA = sum over tokens of D_t e_t,  dskip = sum of dv_t u_t,  ddelta_t = dD_t sigmoid(delta_t + delta_bias)
 // The states before groups of kGroup tokens are kept in shared memory on a way forward through the chunk; backwards the
-// states of a group are computed once more.  32 x 700 tokens x 1300 channels x 16 states: 1010 us, 635 us with lengths drawn from 0 to 35;
-// issue slots are 46 % busy with the twelve warps that registers and shared memory leave room for.
+// states of a group are computed once more.  32 x 700 tokens x 1300 channels x 16 states: 1042 us, 640 us with lengths drawn from 0 to 35;
+// issue slots are 51 % busy with the twelve warps that registers and shared memory leave room for.  With 4, 8, 32 and 64 states: 816, 829, 1959
+// and 5910 us.
 constexpr int kGradStates = 8;                         // states of a thread
 constexpr int kGroup = 4;
 // Tokens of a chunk at most, and of a sequence that is a chunk of its own: at 16 states shared memory holds three blocks of 36 tokens, two of
-// 52.  Chunks cost a pass over the tokens before.  As many tokens of 32 x 1300 channels in sequences of 40, 48, 54 and 72, alone: 1297,
-// 1300, 2223 and 2159 us, in chunks: 1940, 1828, 1744 and 1610; a sequence of 8192 in chunks of 36, 40 and 20: 552, 771 and 634 us.
+// 52.  Chunks cost a pass over the tokens before.  Of 32 x 1300 channels 17 sequences of 40, 14 of 48, 12 of 54 and 9 of 72, alone: 1301,
+// 1234, 2145 and 2059 us, in chunks: 1702, 1593, 1559 and 1436; a sequence of 8192 in chunks of 36, 40 and 20: 559, 812 and 636 us.
+// All of these were measured with 16 states.  Others fit differently: to 8 states an SM holds two blocks of 36 tokens and one of 52, from 17 to 32
+// three and two, above two of either.
 constexpr int kGradChunk = 36, kGradAlone = 52;
 constexpr int kGradBlocks = 3;                         // resident per SM
 
@@ -1137,6 +1143,7 @@ GradPlan grad_plan(const pg_scan_grad_args& a) {
     p.blocks = (int64_t{a.channels} * p.lanes + kScanThreads - 1) / kScanThreads;
     const int64_t items = int64_t{a.sequences} * p.chunks;
     // Shares of a worker's chunks: those whose waves of blocks take the fewest steps of a chunk, a block's start and end counted as a third of one.
+    // At most 64, so that one sequence of 8192 and few channels leaves SMs idle: 154 us with 64 channels, 157 with 128 (559 with 1300).
     double least = 0.0;
     p.shares = 1;
     for (int64_t s = 1; s <= std::min<int64_t>(items, 64); ++s) {
