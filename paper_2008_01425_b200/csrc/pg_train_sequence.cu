@@ -55,7 +55,7 @@ struct Rows {
 // the last width - 1 tokens in registers: every input is read once, but for the few before a run.  Inputs come through shared memory in
 // 16-byte pieces, whatever the rows' alignment, a tile of tokens ahead.  4 bytes a value (6 in the gradient) have to move; instructions (some
 // 60 for two values of a lane) bound it at 0.45 of the copy rate: 32 x 700 tokens x 1300 channels 43 us.  (Eight channels a thread, cut out of
-// their pieces in registers: 88 us.  Plain 2- and 4-byte loads: 43 us, but the gradient of odd widths 145 us instead of 63.)
+// their pieces in registers: 88 us.  Plain 2- and 4-byte loads: 43 us, but the gradient of odd widths 145 us instead of 60.)
 constexpr int kRun = 64;                               // tokens of a run at most
 constexpr int kConvThreads = 128;
 constexpr int kStrip = 64;                             // channels
@@ -174,7 +174,8 @@ conv_kernel(const pg_conv_args a, int run, int runs) {
 }
 
 // The gradient.  dx of token t needs the pre-activations' gradients up to token t + TAPS - 1: a run recomputes those of the
-// tokens behind it.  Sums over tokens: a thread's runs, the four warps of the block (shared memory), then the blocks, whose sums
+// tokens behind it, as far as they are there; what a sequence's last tokens get comes after its loop (with zeros for tokens that are not there, in
+// the loop, 32 x 700 x 1300 took 90 us instead of 86).  Sums over tokens: a thread's runs, the four warps of the block (shared memory), then the blocks, whose sums
 // go to partial[worker][part][TAPS + 1][channels], the bias last.
 template <typename H, int W, int TAPS, int ACT>
 __global__ void __launch_bounds__(kConvThreads, 5)
@@ -213,7 +214,7 @@ conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run
                 before[j] = Elem<H>::up2(t >= 0 ? two.load(x + t * a.x.ld) : state ? two.load(state + static_cast<int64_t>(TAPS - 1 + t) * a.channels) : 0u);
                 dz[j] = both(0.0f);
             }
-            for (int t = t0, stage = 0; t < end; t += kConvTile, stage ^= 1) {
+            for (int t = t0, stage = 0; t < stop; t += kConvTile, stage ^= 1) {
                 ask_tile(rx, s_in[warp][stage ^ 1][0], t + kConvTile, stop, n);
                 ask_tile(rd, s_in[warp][stage ^ 1][1], t + kConvTile, stop, n);
                 copies_end();
@@ -221,17 +222,14 @@ conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run
                 __syncwarp();
 #pragma unroll 4
                 for (int u = 0; u < kConvTile; ++u) {
-                    if (t + u >= end) break;
-                    F2 v = both(0.0f), g = both(0.0f); // behind the last token: zeros
-                    if (t + u < stop) {
-                        v = Elem<H>::up2(two.get(rx, s_in[warp][stage][0] + u * Rows<kStrip>::kPieces, t + u));
-                        g = Elem<H>::up2(two.get(rd, s_in[warp][stage][1] + u * Rows<kStrip>::kPieces, t + u));
-                        if constexpr (ACT != PG_ACT_NONE) {
-                            F2 z = o;
+                    if (t + u >= stop) break;
+                    const F2 v = Elem<H>::up2(two.get(rx, s_in[warp][stage][0] + u * Rows<kStrip>::kPieces, t + u));
+                    F2 g = Elem<H>::up2(two.get(rd, s_in[warp][stage][1] + u * Rows<kStrip>::kPieces, t + u));
+                    if constexpr (ACT != PG_ACT_NONE) {
+                        F2 z = o;
 #pragma unroll
-                            for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j], w[j], z);
-                            g = mul(g, slope<ACT>(fma(v, w[TAPS - 1], z)));
-                        }
+                        for (int j = 0; j < TAPS - 1; ++j) z = fma(before[j], w[j], z);
+                        g = mul(g, slope<ACT>(fma(v, w[TAPS - 1], z)));
                     }
                     if (t + u < own) {
                         db = add(db, g);
@@ -255,6 +253,15 @@ conv_grad_kernel(const pg_conv_grad_args a, float* __restrict__ partial, int run
                     }
                 }
                 __syncwarp();
+            }
+#pragma unroll
+            for (int i = 0; i < TAPS - 1; ++i) {       // the sequence's last tokens, from what is there behind them
+                if (stop + i >= end || stop + i - (TAPS - 1) < t0) continue;
+                F2 out = both(0.0f);
+#pragma unroll
+                for (int j = i; j < TAPS - 1; ++j) out = fma(dz[j], w[TAPS - 1 - j + i], out);
+                two.store(dx, Elem<H>::down2(out));
+                dx += a.dx.ld;
             }
         }
         for (int t = max(t0, own); t < t1; ++t, dx += a.dx.ld) two.store(dx, 0);

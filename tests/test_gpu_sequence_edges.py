@@ -293,6 +293,24 @@ def test_layer_norm_of_rows_of_equal_values(tr, n, eps):
     assert not dgain.any()
 
 
+# ---------------------------------------------------------------- convolution
+@pytest.mark.parametrize("length,have", [(1, 1), (2, 2), (9, 9), (9, 5), (70, 64), (70, 65), (130, 130)])
+@pytest.mark.parametrize("taps", [2, 3, 4])
+def test_weights_of_tokens_behind_the_last_do_not_count(tr, length, have, taps):
+    """dx of a token takes a weight for every token up to taps - 1 behind it that is there: an infinite one of another changes nothing."""
+    g = gen(length + taps)
+    n = 70
+    x, dy, weight = rand(g, 1, length, n).to(BF), rand(g, 1, length, n).to(BF), rand(g, 1, n, taps)
+    kw = dict(activation="none", lengths=torch.tensor([[have]], dtype=torch.int32, device="cuda"))
+    want = tr.pg_causal_conv_grad(dy, x, weight, **kw)
+    weight[0, ::2, 0] = math.inf                       # the oldest input's: of dx of tokens that have taps - 1 behind them
+    got = tr.pg_causal_conv_grad(dy, x, weight, **kw)
+    last = slice(max(0, have - taps + 1), length)
+    assert torch.equal(got[0][:, last], want[0][:, last]) and torch.equal(got[0][..., 1::2], want[0][..., 1::2])
+    assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    assert not torch.isfinite(got[0][0, :max(0, have - taps + 1), ::2]).any()
+
+
 # ---------------------------------------------------------------- chunks, and 17 to 32 states
 CHUNKS = [((1, 2, 52, 50), 16, 1), ((1, 2, 53, 50), 16, 0), ((2, 1, 73, 130), 8, 1), ((1, 2, 45, 40), 32, 0), ((1, 1, 300, 20), 24, 1), ((2, 1, 300, 33), 32, 0), ((1, 1, 1100, 9), 20, 0)]
 KINDS = [(BF, True, True, True), (HF, False, False, False)]
