@@ -355,7 +355,7 @@ PG_API int pg_selective_scan_grad(const pg_scan_grad_args *args, void *workspace
  * lse gets log sum exp(x) and log sum exp(x / tau) of every row; the first is 0 where the call has no second term, the second where it has no first.
  *
  * The gradient dloss (alpha tau (q - p) + (1 - alpha) (softmax(x) - [label])) goes to dlogits: by pg_distillation_loss
- * together with the loss, reading the logits once (to 100000 classes; twice above), or by pg_distillation_loss_grad from lse,
+ * together with the loss, reading the logits once (to 100000 classes with lists to 100 entries; twice above), or by pg_distillation_loss_grad from lse,
  * which it reads (and whose step, 2^-24 of its size, is the error of the probabilities' logarithms then).  At most 1024 entries in a
  * list (PG_ERR_TOO_LARGE); the gradient's time goes with the square of their number from some 100 on.
  */
